@@ -66,13 +66,59 @@ typedef enum {
   LT_OP_LAYER_NORM_GRAD,   /* (dy, x, gamma, mean, rstd) -> dx                               */
   LT_OP_XENT,              /* (logits[B,C], labels i32[B]) -> f32[B]: logsumexp - picked     */
   LT_OP_XENT_GRAD,         /* (logits, labels, scale rank 0) -> (softmax - onehot) * scale   */
-  LT_OP_MATMUL = 96        /* (a, b), attrs LT_ATTR_TRANS_A/B, optional LT_ATTR_DTYPE;        */
+  LT_OP_MATMUL = 96,       /* (a, b), attrs LT_ATTR_TRANS_A/B, optional LT_ATTR_DTYPE;        */
                            /* leading axes of a and b equal, or b a plain matrix             */
+  LT_OP_ROPE = 112,        /* (x, positions), attrs LT_ATTR_ROPE_*: rotary positions, below    */
+  LT_OP_ROPE_GRAD,         /* (dy, positions), the same attrs -> dx                          */
+  LT_OP_CACHE_APPEND,      /* (cache, k, v, lengths, table[, offsets]) -> the cache with the   */
+                           /* new rows written; attrs LT_ATTR_ROPE_*: k is rotated on the way  */
+  LT_OP_PAGED_ATTENTION    /* (q, cache, lengths, table), attr LT_ATTR_SCALE                  */
 } lt_opcode;
+
+/*
+ * Rotary positions (LT_OP_ROPE, LT_OP_ROPE_GRAD, and the keys of LT_OP_CACHE_APPEND).  x is
+ * [..., heads, dim], fp32 or bf16; positions is int32 and has the axes before `heads`, or the last of
+ * them (then it is shared along the others).  The first n = LT_ATTR_ROPE_DIMS elements of a head (even,
+ * at most 256; default: all of it) are n / 2 pairs: (i, i + n / 2), or (2 i, 2 i + 1) with
+ * LT_ATTR_ROPE_INTERLEAVED.  Pair i turns by a = position * f_i,
+ *     f_i = base^(-2 i / n) * (g_i + (1 - g_i) / factor),
+ *     g_i = clamp((original * base^(-2 i / n) / 2 pi - low) / (high - low), 0, 1), or 0 if original is 0:
+ * with a factor over 1 (long contexts) every pair is slowed down, or, where the length that the model
+ * was trained on is given (original), only those that turn fewer than `high` times over it, and
+ * those that turn fewer than `low` times in full.  (x, y) -> amplitude * (x cos a - y sin a, y cos a + x sin a); what
+ * is behind n stays as it is.  Defaults: base 10000, factor 1, original 0, low 1, high 32, amplitude 1.
+ * base >= 1, factor >= 1, original >= 0, 0 <= low < high, all finite.  Angles are formed in 64 bits; any int32 is
+ * a position.  The gradient turns the other way (and takes the amplitude as it is).
+ *
+ * A paged cache of keys and values is one tensor [pages, 2, key heads, rows, dim], fp32 or bf16: keys at 0,
+ * values at 1.  Sequence s holds its position p in row p % rows of page table[s][p / rows]; table
+ * is int32 [sequences, slots], lengths int32 [sequences].
+ *
+ * LT_OP_CACHE_APPEND: k and v are [tokens, key heads, dim], fp32 or bf16, both alike, rounded to the
+ * cache's type.  offsets (int32 [sequences + 1], not decreasing) says whose they are: tokens offsets[s] ..
+ * offsets[s + 1] - 1 are the last ones of sequence s, the last one at position lengths[s] - 1: lengths count
+ * the new tokens in.  Tokens before offsets[0] and from offsets[sequences] on are not used.  Without offsets
+ * token s is sequence s's (tokens = sequences).  A token whose position is negative or behind
+ * the table's slots, or whose page is not one of the cache's, is not written.  Two tokens of a call have to
+ * have different rows of the cache: where they have not, what the row holds is one's or the other's, or
+ * pieces of both.  No attrs: k is not rotated.  With lt_assign to a donatable cache the rows are written in place; otherwise
+ * the cache is copied first.
+ *
+ * LT_OP_PAGED_ATTENTION: q is [sequences, heads, dim] of the cache's type, one new token each; heads is a
+ * multiple of the key heads, and query head h reads key head h / (heads / key heads); dim is at most
+ * 256.  The result, of q's type and shape, is softmax(scale * q K^T) V over the first lengths[s] positions
+ * of the sequence.  Positions behind the table's slots and those in pages that are not the cache's do not count;
+ * a sequence with nothing that counts (length 0 or negative) gets zeros.  Default scale: 1 / sqrt(dim).
+ *
+ * LT_ERR_SHAPE where pages * rows, slots * rows or tokens is 2^31 or more.
+ */
 
 typedef enum {
   LT_ATTR_VALUE = 1, LT_ATTR_DTYPE = 2, LT_ATTR_AXIS = 3, LT_ATTR_EPS = 4,
-  LT_ATTR_TRANS_A = 5, LT_ATTR_TRANS_B = 6, LT_ATTR_START = 7, LT_ATTR_LENGTH = 8, LT_ATTR_DIM0 = 16
+  LT_ATTR_TRANS_A = 5, LT_ATTR_TRANS_B = 6, LT_ATTR_START = 7, LT_ATTR_LENGTH = 8, LT_ATTR_DIM0 = 16,
+  LT_ATTR_ROPE_DIMS = 32, LT_ATTR_ROPE_INTERLEAVED = 33,   /* integers */
+  LT_ATTR_ROPE_BASE = 34, LT_ATTR_ROPE_FACTOR = 35, LT_ATTR_ROPE_ORIGINAL = 36, LT_ATTR_ROPE_LOW = 37,
+  LT_ATTR_ROPE_HIGH = 38, LT_ATTR_ROPE_AMPLITUDE = 39, LT_ATTR_SCALE = 40
 } lt_attr_key;
 
 typedef struct {

@@ -371,6 +371,74 @@ class Eager:
         out_dt = dtype if dtype is not None else (a.dtype if a.dtype == b.dtype else F32)
         return self._store(np.matmul(A, B), out_dt)
 
+    # ---- rotary positions, a paged cache of keys and values --------------------
+    @staticmethod
+    def _angles(positions, rotary, dim):
+        """a = position * f_i of the pairs, and the indices of their two elements."""
+        n = dim if rotary.dims is None else rotary.dims
+        f = np.array([float(rotary.base) ** (-2.0 * i / n) for i in range(n // 2)])
+        keep = np.zeros_like(f)
+        if rotary.original:
+            keep = np.clip((rotary.original * f / (2.0 * math.pi) - rotary.low) / (rotary.high - rotary.low), 0.0, 1.0)
+        first = np.arange(0, n, 2) if rotary.interleaved else np.arange(n // 2)
+        second = first + (1 if rotary.interleaved else n // 2)
+        return np.asarray(positions, dtype=np.float64)[..., None] * (f * (keep + (1.0 - keep) / rotary.factor)), first, second
+
+    def _rotated(self, x, positions, rotary, sign):
+        """x [..., heads, dim] in float64, positions [...] or the last of these axes."""
+        a, first, second = self._angles(positions, rotary, x.shape[-1])
+        cos, sin = np.cos(a)[..., None, :] * rotary.amplitude, np.sin(sign * a)[..., None, :] * rotary.amplitude
+        out = x.copy()
+        out[..., first] = x[..., first] * cos - x[..., second] * sin
+        out[..., second] = x[..., second] * cos + x[..., first] * sin
+        return out
+
+    def rope(self, x, positions, rotary):
+        x = self._t(x)
+        return self._store(self._rotated(self._wide(x), positions.data, rotary, 1.0), x.dtype)
+
+    def rope_grad(self, dy, positions, rotary):
+        dy = self._t(dy)
+        return self._store(self._rotated(self._wide(dy), positions.data, rotary, -1.0), dy.dtype)
+
+    def cache_append(self, cache, k, v, lengths, table, offsets=None, rotary=None):
+        """Token by token: the tokens of sequence s are its last positions; one whose position, slot or page does not exist is dropped."""
+        out = self._wide(cache).copy()
+        kk, vv, lens, tab = self._wide(k), self._wide(v), lengths.data, table.data
+        pages, rows = out.shape[0], out.shape[3]
+        off = offsets.data if offsets is not None else np.arange(len(lens) + 1)
+        for s in range(len(lens)):
+            for t in range(max(0, int(off[s])), min(kk.shape[0], int(off[s + 1]))):
+                pos = int(lens[s]) - int(off[s + 1]) + t
+                if not 0 <= pos < tab.shape[1] * rows or not 0 <= tab[s, pos // rows] < pages:
+                    continue
+                key = kk[t] if rotary is None else self._rotated(kk[t], np.array(pos), rotary, 1.0)
+                out[tab[s, pos // rows], 0, :, pos % rows] = key
+                out[tab[s, pos // rows], 1, :, pos % rows] = vv[t]
+        return self._store(out, cache.dtype)
+
+    def paged_attention(self, q, cache, lengths, table, scale=None):
+        """Sequence by sequence, head by head, over the positions that are in a page of the cache; nothing there: zeros."""
+        qq, held, tab = self._wide(q), self._wide(cache), table.data
+        seqs, heads, dim = qq.shape
+        pages, _, kv_heads, rows, _ = held.shape
+        scale = 1.0 / math.sqrt(dim) if scale is None else scale
+        out = np.zeros_like(qq)
+        for s in range(seqs):
+            pos = np.arange(max(0, min(int(lengths.data[s]), tab.shape[1] * rows)))
+            pos = pos[(tab[s, pos // rows] >= 0) & (tab[s, pos // rows] < pages)] if len(pos) else pos
+            if not len(pos):
+                continue
+            for h in range(heads):
+                kh = h // (heads // kv_heads)
+                score = held[tab[s, pos // rows], 0, kh, pos % rows] @ qq[s, h] * scale
+                top = score.max()
+                if top == -np.inf:
+                    continue
+                p = np.exp(score - top)
+                out[s, h] = p @ held[tab[s, pos // rows], 1, kh, pos % rows] / p.sum()
+        return self._store(out, q.dtype)
+
     # ---- mutation, barrier, fetch -------------------------------------------
     def assign(self, dst: ETensor, src: ETensor) -> None:
         """In-place update = rebind the destination to the new value; a tensor whose memory is

@@ -46,6 +46,7 @@ EXPAND, RESHAPE, PERMUTE, NARROW, SLICE_UPDATE = 48, 49, 50, 51, 52
 SUM, AMAX, MEAN = 64, 65, 66
 SOFTMAX, SOFTMAX_GRAD, LAYER_NORM, LAYER_NORM_GRAD, XENT, XENT_GRAD = range(80, 86)
 MATMUL = 96
+ROPE, ROPE_GRAD, CACHE_APPEND, PAGED_ATTENTION = range(112, 116)
 
 OP_NAME = {
     DEVICE_DATA: "xla::device_data", SCALAR_PARAM: "xla::device_data", CONSTANT: "prim::Constant",
@@ -60,10 +61,13 @@ OP_NAME = {
     LAYER_NORM: "aten::native_layer_norm", LAYER_NORM_GRAD: "aten::native_layer_norm_backward",
     XENT: "aten::nll_loss_of_log_softmax", XENT_GRAD: "aten::nll_loss_of_log_softmax_backward",
     MATMUL: "aten::matmul",
+    ROPE: "lt::rope", ROPE_GRAD: "lt::rope_backward", CACHE_APPEND: "lt::cache_append", PAGED_ATTENTION: "lt::paged_attention",
 }
 
 # ---- attribute keys -----------------------------------------------------------
 A_VALUE, A_DTYPE, A_AXIS, A_EPS, A_TRANS_A, A_TRANS_B, A_START, A_LENGTH, A_DIM0 = 1, 2, 3, 4, 5, 6, 7, 8, 16
+
+A_ROPE_DIMS, A_ROPE_INTERLEAVED, A_ROPE_BASE, A_ROPE_FACTOR, A_ROPE_ORIGINAL, A_ROPE_LOW, A_ROPE_HIGH, A_ROPE_AMPLITUDE, A_SCALE = range(32, 41)
 
 UNARY = {NEG, ABS, EXP, LOG, TANH, SQRT, RSQRT, RECIP, RELU, GELU, SQUARE, CAST, SIGMOID}
 BINARY = {ADD, SUB, MUL, DIV, MAXIMUM, MINIMUM, RELU_GRAD, GELU_GRAD}
@@ -431,6 +435,32 @@ class Tracer:
                  (A_TRANS_B, False, int(bool(trans_b)))]
         return self._emit(MATMUL, out_dt, lead + (m, n), attrs, [a, b])
 
+    @staticmethod
+    def _rotary(rotary, dim):
+        """The canonical attributes: all eight, defaults filled in."""
+        r = rotary
+        reals = [(A_ROPE_BASE, r.base), (A_ROPE_FACTOR, r.factor), (A_ROPE_ORIGINAL, r.original), (A_ROPE_LOW, r.low), (A_ROPE_HIGH, r.high), (A_ROPE_AMPLITUDE, r.amplitude)]
+        return ([(A_ROPE_DIMS, False, dim if r.dims is None else int(r.dims)), (A_ROPE_INTERLEAVED, False, int(r.interleaved))] +
+                [(k, True, float(v)) for k, v in reals])
+
+    def rope(self, x, positions, rotary):
+        x = self._t(x)
+        assert positions.shape == x.shape[len(x.shape) - 2 - len(positions.shape):-2]
+        return self._emit(ROPE, x.dtype, x.shape, self._rotary(rotary, x.shape[-1]), [x, positions])
+
+    def rope_grad(self, dy, positions, rotary):
+        dy = self._t(dy)
+        return self._emit(ROPE_GRAD, dy.dtype, dy.shape, self._rotary(rotary, dy.shape[-1]), [dy, positions])
+
+    def cache_append(self, cache, k, v, lengths, table, offsets=None, rotary=None):
+        cache = self._t(cache)
+        attrs = () if rotary is None else self._rotary(rotary, cache.shape[-1])
+        return self._emit(CACHE_APPEND, cache.dtype, cache.shape, attrs, [cache, k, v, lengths, table] + ([] if offsets is None else [offsets]))
+
+    def paged_attention(self, q, cache, lengths, table, scale=None):
+        q = self._t(q)
+        return self._emit(PAGED_ATTENTION, q.dtype, q.shape, [(A_SCALE, True, 1.0 / math.sqrt(q.shape[-1]) if scale is None else float(scale))], [q, cache, lengths, table])
+
     def assign(self, dst: STensor, src: STensor):
         """In-place update as substitution of the destination's computation."""
         assert dst.alive and src.alive
@@ -697,7 +727,13 @@ class Tracer:
             live[i] = True
             stack.extend(v[0] for v in rins[i])
 
-        LEAF, VIEW, EW, ROW, COL, ALL, MM, SLICE = "LEAF", "VIEW", "EW", "ROW", "COL", "ALL", "MM", "SLICE"
+        LEAF, VIEW, EW, ROW, COL, ALL, MM, SLICE, OP = "LEAF", "VIEW", "EW", "ROW", "COL", "ALL", "MM", "SLICE", "OP"
+
+        def reads_heads(i, u):
+            # a window of heads, or of the first axis, that operator u reads as [..., heads, dim] where it lies
+            rank, axis = len(nd[i].shape), [a for a in nd[i].attrs if a[0] == A_AXIS][0][2]
+            heads = {ROPE: (0,), ROPE_GRAD: (0,), CACHE_APPEND: (1, 2), PAGED_ATTENTION: (0,)}.get(nd[u].op, ())
+            return bool(heads) and rank >= 3 and axis in (0, rank - 2) and all(k in heads for k, v in enumerate(rins[u]) if v[0] == i)
 
         def klass(i):
             n = nd[i]
@@ -712,7 +748,7 @@ class Tracer:
             if n.op == NARROW:
                 # a window is addressing for elementwise ops, contractions and permutations; otherwise a copy
                 ok = not is_root[i] and pre_users[i] and all(
-                    nd[u].op in UNARY or nd[u].op in BINARY or nd[u].op in (MATMUL, PERMUTE) for u in pre_users[i])
+                    nd[u].op in UNARY or nd[u].op in BINARY or nd[u].op in (MATMUL, PERMUTE) or reads_heads(i, u) for u in pre_users[i])
                 return VIEW if ok else EW
             if n.op == SLICE_UPDATE:
                 return SLICE
@@ -733,6 +769,8 @@ class Tracer:
                 return ROW
             if n.op == MATMUL:
                 return MM
+            if n.op in (ROPE, ROPE_GRAD, CACHE_APPEND, PAGED_ATTENTION):
+                return OP
             raise NotImplementedError(n.op)
 
         is_root = [False] * N
@@ -784,7 +822,7 @@ class Tracer:
             return r["anchor"] if r["anchor"] is not None else min(r["members"])
 
         for i in range(N):
-            if cls[i] in (EW, ROW, COL, ALL, MM, SLICE):
+            if cls[i] in (EW, ROW, COL, ALL, MM, SLICE, OP):
                 r = {"kind": cls[i], "anchor": None if cls[i] == EW else i, "members": {i}, "fin_shape": None}
                 regions[id(r)] = r
                 region_of[i] = r
@@ -992,6 +1030,10 @@ class Tracer:
                             # a window update may overwrite its own base (operand 0) in place
                             if (m == rw["anchor"] and nd[m].op == SLICE_UPDATE and x in pn and x == rins[m][0]
                                     and base(rins[m][1]) not in pn):
+                                continue
+                            # new rows may go into their own cache
+                            if (m == rw["anchor"] and nd[m].op == CACHE_APPEND and x in pn and x == rins[m][0]
+                                    and base(rins[m][1]) not in pn and base(rins[m][2]) not in pn):
                                 continue
                             if m == rw["anchor"] or x not in pn or nd[m].shape != nd[x[0]].shape or nd[m].op in (PERMUTE, EXPAND, RESHAPE, NARROW):
                                 ok = False

@@ -51,6 +51,8 @@ const char* op_name(uint16_t op) {
     case LT_OP_XENT: return "aten::nll_loss_of_log_softmax";
     case LT_OP_XENT_GRAD: return "aten::nll_loss_of_log_softmax_backward";
     case LT_OP_MATMUL: return "aten::matmul";
+    case LT_OP_ROPE: return "lt::rope"; case LT_OP_ROPE_GRAD: return "lt::rope_backward";
+    case LT_OP_CACHE_APPEND: return "lt::cache_append"; case LT_OP_PAGED_ATTENTION: return "lt::paged_attention";
     default: return "?";
   }
 }
@@ -294,6 +296,51 @@ static void push_attr(Node* n, uint16_t key, bool isf, int64_t i, double f) {
   a.is_float = isf ? 1 : 0;
   if (isf) a.v.f = f;
   else a.v.i = i;
+}
+
+// The rotation's attributes, checked, with their defaults filled in.
+static lt_status rotary_attrs(lt_ctx* ctx, const std::string& op, const lt_attr* attrs, int n_attr, int64_t dim, Node* n) {
+  auto integer = [&](uint16_t key, int64_t other) {
+    const lt_attr* a = find_attr(attrs, n_attr, key);
+    return a ? (a->is_float ? (int64_t)-1 : a->v.i) : other;
+  };
+  auto real = [&](uint16_t key, double other) {
+    const lt_attr* a = find_attr(attrs, n_attr, key);
+    return a ? (a->is_float ? a->v.f : (double)a->v.i) : other;
+  };
+  const int64_t dims = integer(LT_ATTR_ROPE_DIMS, dim), interleaved = integer(LT_ATTR_ROPE_INTERLEAVED, 0);
+  const double base = real(LT_ATTR_ROPE_BASE, 10000.0), factor = real(LT_ATTR_ROPE_FACTOR, 1.0), original = real(LT_ATTR_ROPE_ORIGINAL, 0.0),
+               low = real(LT_ATTR_ROPE_LOW, 1.0), high = real(LT_ATTR_ROPE_HIGH, 32.0), amplitude = real(LT_ATTR_ROPE_AMPLITUDE, 1.0);
+  if (dims < 2 || dims > 2 * (int64_t)ltk::kMaxPairs || dims % 2 != 0 || dims > dim)
+    return fail(ctx, LT_ERR_ARG, op + ": the rotated part of a head must be an even number of elements, from 2 to 256 and to the head's size");
+  if (interleaved != 0 && interleaved != 1) return fail(ctx, LT_ERR_ARG, op + ": LT_ATTR_ROPE_INTERLEAVED must be 0 or 1");
+  if (!(std::isfinite(base) && base >= 1.0) || !(std::isfinite(factor) && factor >= 1.0) || !(std::isfinite(original) && original >= 0.0) ||
+      !(std::isfinite(low) && std::isfinite(high) && low >= 0.0 && high > low) || !std::isfinite(amplitude) || !std::isfinite((float)amplitude))
+    return fail(ctx, LT_ERR_ARG, op + ": base and factor must be at least 1, original at least 0, 0 <= low < high, and all finite");
+  push_attr(n, LT_ATTR_ROPE_DIMS, false, dims, 0);
+  push_attr(n, LT_ATTR_ROPE_INTERLEAVED, false, interleaved, 0);
+  push_attr(n, LT_ATTR_ROPE_BASE, true, 0, base);
+  push_attr(n, LT_ATTR_ROPE_FACTOR, true, 0, factor);
+  push_attr(n, LT_ATTR_ROPE_ORIGINAL, true, 0, original);
+  push_attr(n, LT_ATTR_ROPE_LOW, true, 0, low);
+  push_attr(n, LT_ATTR_ROPE_HIGH, true, 0, high);
+  push_attr(n, LT_ATTR_ROPE_AMPLITUDE, true, 0, amplitude);
+  return LT_OK;
+}
+
+// What every reader and writer of a paged cache asks of it, its lengths and its table.
+static lt_status check_paged(lt_ctx* ctx, const std::string& op, const Handle* cache, const Handle* lengths, const Handle* table) {
+  if (!is_float(cache->dtype)) return fail(ctx, LT_ERR_DTYPE, op + ": the cache must be f32 or bf16");
+  if (lengths->dtype != LT_I32 || table->dtype != LT_I32) return fail(ctx, LT_ERR_DTYPE, op + ": lengths and table must be int32");
+  if (cache->rank != 5 || cache->dims[1] != 2 || cache->dims[2] < 1 || cache->dims[3] < 1 || cache->dims[4] < 1)
+    return fail(ctx, LT_ERR_SHAPE, op + ": the cache must be [pages, 2, key heads, rows, dim]");
+  if (lengths->rank != 1 || table->rank != 2 || table->dims[0] != lengths->dims[0])
+    return fail(ctx, LT_ERR_SHAPE, op + ": lengths must be [sequences] and table [sequences, slots]");
+  const int64_t most = ((int64_t)1 << 31) - 1;
+  auto over = [&](int64_t a, int64_t b) { return a > most || b > most || a * b > most; };
+  if (over(cache->dims[0], cache->dims[3]) || over(table->dims[1], cache->dims[3]) || over(cache->dims[2], cache->dims[4]) || lengths->dims[0] > most)
+    return fail(ctx, LT_ERR_SHAPE, op + ": pages * rows, slots * rows, key heads * dim and sequences must be below 2^31");
+  return LT_OK;
 }
 
 }  // namespace lt
@@ -649,6 +696,55 @@ static lt_status record_op(lt_ctx* ctx, uint16_t opcode, const lt_tensor* inputs
       push_attr(&n, LT_ATTR_AXIS, false, axis, 0);
       push_attr(&n, LT_ATTR_START, false, st->v.i, 0);
     } break;
+    case LT_OP_ROPE: case LT_OP_ROPE_GRAD: {
+      const std::string op = opcode == LT_OP_ROPE ? "rope" : "rope_grad";
+      if (!need(2)) return fail(ctx, LT_ERR_ARG, op + " takes (x, positions)");
+      const Handle* p = in[1];
+      if (!is_float(a->dtype) || p->dtype != LT_I32) return fail(ctx, LT_ERR_DTYPE, op + ": x must be f32 or bf16, positions int32");
+      bool fits = a->rank >= 3 && p->rank >= 1 && p->rank <= a->rank - 2;
+      for (int i = 0; fits && i < p->rank; ++i) fits = p->dims[i] == a->dims[a->rank - 2 - p->rank + i];
+      if (!fits) return fail(ctx, LT_ERR_SHAPE, op + ": x must be [..., heads, dim], positions its leading axes or the last of them");
+      if (numel(a->dims, a->rank - 2) >= ((int64_t)1 << 31) || a->dims[a->rank - 2] >= ((int64_t)1 << 31) || a->dims[a->rank - 1] >= ((int64_t)1 << 31))
+        return fail(ctx, LT_ERR_SHAPE, op + ": tokens, heads and dim must be below 2^31");
+      const lt_status st = rotary_attrs(ctx, op, attrs, n_attr, a->dims[a->rank - 1], &n);
+      if (st != LT_OK) return st;
+      n.dtype = a->dtype;
+      set_shape(a->dims, a->rank);
+    } break;
+    case LT_OP_CACHE_APPEND: {
+      if (!need(5) && !need(6)) return fail(ctx, LT_ERR_ARG, "cache_append takes (cache, k, v, lengths, table[, offsets])");
+      const Handle *k = in[1], *v = in[2];
+      lt_status st = check_paged(ctx, "cache_append", a, in[3], in[4]);
+      if (st != LT_OK) return st;
+      if (!is_float(k->dtype) || v->dtype != k->dtype) return fail(ctx, LT_ERR_DTYPE, "cache_append: k and v must both be f32 or both bf16");
+      if (k->rank != 3 || v->rank != 3 || std::memcmp(k->dims, v->dims, 3 * sizeof(int64_t)) || k->dims[1] != a->dims[2] || k->dims[2] != a->dims[4])
+        return fail(ctx, LT_ERR_SHAPE, "cache_append: k and v must be [tokens, key heads, dim] of the cache's key heads and dim");
+      if (k->dims[0] >= ((int64_t)1 << 31)) return fail(ctx, LT_ERR_SHAPE, "cache_append: tokens must be below 2^31");
+      if (n_in == 6 && in[5]->dtype != LT_I32) return fail(ctx, LT_ERR_DTYPE, "cache_append: offsets must be int32");
+      if (n_in == 6 ? in[5]->rank != 1 || in[5]->dims[0] != in[3]->dims[0] + 1 : k->dims[0] != in[3]->dims[0])
+        return fail(ctx, LT_ERR_SHAPE, n_in == 6 ? "cache_append: offsets must be [sequences + 1]" : "cache_append: without offsets there is one token a sequence");
+      if (n_attr > 0) st = rotary_attrs(ctx, "cache_append", attrs, n_attr, a->dims[4], &n);
+      if (st != LT_OK) return st;
+      n.dtype = a->dtype;
+      set_shape(a->dims, a->rank);
+    } break;
+    case LT_OP_PAGED_ATTENTION: {
+      if (!need(4)) return fail(ctx, LT_ERR_ARG, "paged_attention takes (q, cache, lengths, table)");
+      const Handle* c = in[1];
+      const lt_status st = check_paged(ctx, "paged_attention", c, in[2], in[3]);
+      if (st != LT_OK) return st;
+      if (a->dtype != c->dtype) return fail(ctx, LT_ERR_DTYPE, "paged_attention: q must have the cache's type");
+      if (a->rank != 3 || a->dims[0] != in[2]->dims[0] || a->dims[2] != c->dims[4] || a->dims[1] < 1 || a->dims[1] % c->dims[2] != 0)
+        return fail(ctx, LT_ERR_SHAPE, "paged_attention: q must be [sequences, heads, dim], heads a multiple of the key heads");
+      if (a->dims[2] > 256) return fail(ctx, LT_ERR_SHAPE, "paged_attention: heads of at most 256 elements");
+      if (a->dims[0] * a->dims[1] >= ((int64_t)1 << 31) || a->dims[1] >= ((int64_t)1 << 31)) return fail(ctx, LT_ERR_SHAPE, "paged_attention: sequences * heads must be below 2^31");
+      const lt_attr* sc = find_attr(attrs, n_attr, LT_ATTR_SCALE);
+      const double scale = sc ? (sc->is_float ? sc->v.f : (double)sc->v.i) : 1.0 / std::sqrt((double)a->dims[2]);
+      if (!std::isfinite(scale) || !std::isfinite((float)scale)) return fail(ctx, LT_ERR_ARG, "paged_attention: LT_ATTR_SCALE must be finite");
+      push_attr(&n, LT_ATTR_SCALE, true, 0, scale);
+      n.dtype = a->dtype;
+      set_shape(a->dims, a->rank);
+    } break;
     default:
       if (ctx->fallback && opcode >= LT_OP_CUSTOM) return run_fallback(ctx, opcode, inputs, n_in, attrs, n_attr, outputs, n_out, nullptr);
       return fail(ctx, LT_ERR_UNSUPPORTED, "lt_op: opcode " + std::to_string(opcode) + " has no lowering");
@@ -966,7 +1062,7 @@ lt_status lt_dump_schedule(lt_ctx* ctx, char* buf, size_t cap, size_t* len) {
   if (!ctx) return LT_ERR_ARG;
   std::string s;
   if (ctx->last_plan) {
-    static const char* const kinds[] = {"EW", "ROW", "ALL", "COL", "ROWOP", "MM", "SPLITPOST", "SLICE", "ATTN"};
+    static const char* const kinds[] = {"EW", "ROW", "ALL", "COL", "ROWOP", "MM", "SPLITPOST", "SLICE", "ATTN", "ROPE", "APPEND", "PAGED"};
     static_assert(sizeof(kinds) / sizeof(kinds[0]) == kLaunchKinds, "a name per kind of launch");
     const Plan& p = *ctx->last_plan;
     for (size_t i = 0; i < p.launches.size(); ++i) {

@@ -148,6 +148,25 @@ static lt_status hip_fail(lt_ctx* ctx, const char* what, hipError_t e) {
   return fail(ctx, LT_ERR_DEVICE, std::string(what) + ": " + hipGetErrorString(e));
 }
 
+}  // namespace lt
+
+namespace ltk {
+static OperatorLauncher* operators() {   // (filled while the library's other files are initialised, in any order)
+  static OperatorLauncher table[kOperatorKernels] = {};
+  return table;
+}
+bool set_operator(OperatorKernel which, OperatorLauncher launch) {
+  operators()[which] = launch;
+  return true;
+}
+static hipError_t launch_operator(OperatorKernel which, const void* args, hipStream_t s) {
+  const OperatorLauncher f = operators()[which];
+  return f ? f(args, s) : hipErrorInvalidValue;
+}
+}  // namespace ltk
+
+namespace lt {
+
 static hipError_t launch_one(const Launch& l, const uint8_t* args, hipStream_t s) {
   switch (l.kind) {
     case L_EW: return ltk::launch_ew(*(const ltk::EwArgs*)args, l.grid_x, s);
@@ -159,6 +178,9 @@ static hipError_t launch_one(const Launch& l, const uint8_t* args, hipStream_t s
     case L_SPLITPOST: return ltk::launch_split_post(*(const ltk::SplitPostArgs*)args, l.grid_x, s);
     case L_ATTN: return ltk::launch_attention(*(const ltk::AttnArgs*)args, s);
     case L_SLICE: return ltk::launch_slice_update(*(const ltk::SliceArgs*)args, l.grid_x, s);
+    case L_ROPE: return ltk::launch_operator(ltk::kOpRope, args, s);
+    case L_APPEND: return ltk::launch_operator(ltk::kOpCacheAppend, args, s);
+    case L_PAGED: return ltk::launch_operator(ltk::kOpPagedAttention, args, s);
   }
   return hipErrorInvalidValue;
 }
@@ -174,6 +196,9 @@ static const char* kind_name(LaunchKind k) {
     case L_SPLITPOST: return "lt_split_post_kernel";
     case L_ATTN: return "lt_attention_kernel";
     case L_SLICE: return "lt_slice_update_kernel";
+    case L_ROPE: return "lt_rope_kernel";
+    case L_APPEND: return "lt_cache_append_kernel";
+    case L_PAGED: return "lt_paged_attention_kernel";
   }
   return "?";
 }

@@ -23,7 +23,7 @@ namespace lt {
 enum : uint16_t { OP_DEVICE_DATA = 1, OP_SCALAR_PARAM = 2, OP_CONSTANT = 3 };
 
 constexpr int kMaxAttrs = 8;
-constexpr int kMaxIns = 5;
+constexpr int kMaxIns = 6;
 
 // caps on one fused region (part of the partition rules)
 constexpr int kMaxRegionInputs = 8;
@@ -112,8 +112,8 @@ struct Handle {
 
 // ---- a lowered, cached program ------------------------------------------------------------
 
-enum LaunchKind : uint8_t { L_EW, L_ROW, L_ALL, L_COL, L_ROWOP, L_GEMM, L_SPLITPOST, L_SLICE, L_ATTN };
-constexpr size_t kLaunchKinds = L_ATTN + 1;
+enum LaunchKind : uint8_t { L_EW, L_ROW, L_ALL, L_COL, L_ROWOP, L_GEMM, L_SPLITPOST, L_SLICE, L_ATTN, L_ROPE, L_APPEND, L_PAGED };
+constexpr size_t kLaunchKinds = L_PAGED + 1;
 
 struct Storage {
   int param = -1;        // >= 0: the buffer of device parameter `param` (input, or donated output)

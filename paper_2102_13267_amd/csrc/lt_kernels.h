@@ -283,10 +283,77 @@ struct SliceArgs {
   uint32_t window_only;
 };
 
+// ---- rotary positions, and a paged cache of keys and values ------------------------------------
+// Quarter turns per position of every rotated pair (frequency * 2 / pi), in 64 bits: position * turns
+// is then exact to 2^-22 of a turn at the largest position, and its fraction is what is left to
+// compute a sine of.
+constexpr uint32_t kMaxPairs = 128;
+struct Rotary {
+  double turns[kMaxPairs];
+  uint32_t dims, interleaved;   // dims 0: nothing is rotated
+  float amplitude;
+  uint32_t back;                // turn the other way
+};
+
+// n / d for n < 2^31, 1 <= d < 2^31: the product with ceil(2^(31 + shift) / d), shift = ceil(log2 d)
+struct Divider {
+  uint32_t d = 1, magic = 1u << 31, shift = 0;
+  void set(uint32_t div) {
+    d = div;
+    shift = 0;
+    while (shift < 31u && (1u << shift) < div) ++shift;
+    magic = (uint32_t)((((uint64_t)1 << (31u + shift)) + div - 1u) / div);
+  }
+};
+
+// out[t][h] = x[t][h] rotated by positions[t % n_pos].  Token t of x is at (t / inner) * s_outer + (t % inner) * s_inner,
+// its head h s_head further, elements contiguous; out is dense.
+struct RopeArgs {
+  const void* x;
+  const int32_t* positions;
+  void* out;
+  uint64_t tokens;
+  uint32_t dtype, heads, dim, inner, n_pos, pad;
+  int64_t s_outer, s_inner, s_head;
+  Rotary rotary;
+};
+
+// New rows of a paged cache [pages][2][heads][rows][dim].  copy_from: the cache to copy to `cache` first
+// (null: `cache` holds it already).  offsets null: token t is sequence t's.
+struct AppendArgs {
+  void* cache;
+  const void* copy_from;
+  const void* k;
+  const void* v;
+  const int32_t* lengths;
+  const int32_t* table;
+  const int32_t* offsets;
+  uint64_t cache_elems;
+  uint32_t cache_dtype, dtype, tokens, seqs, slots, pages, heads, dim;
+  Divider rows;                 // of a page
+  uint32_t pad;
+  int64_t k_token, k_head, v_token, v_head;   // element strides
+  Rotary rotary;
+};
+
+// out[s][h] = softmax(scale q K^T) V over sequence s's keys in the paged cache.
+struct PagedArgs {
+  const void* q;
+  const void* cache;
+  const int32_t* lengths;
+  const int32_t* table;
+  void* out;
+  uint32_t dtype, seqs, heads, kv_heads, dim, slots, pages;
+  uint32_t capacity;            // most keys of a sequence: slots * rows of a page (0 without pages)
+  Divider rows;                 // of a page
+  float scale;
+  int64_t q_seq, q_head;        // element strides
+};
+
 // Argument blocks travel by value in the kernel argument segment, which holds 4 KiB.
 static_assert(sizeof(EwArgs) <= 4096 && sizeof(RowArgs) <= 4096 && sizeof(AllArgs) <= 4096 && sizeof(ColArgs) <= 4096 &&
                   sizeof(GemmArgs) <= 4096 && sizeof(SplitPostArgs) <= 4096 && sizeof(SliceArgs) <= 4096 &&
-                  sizeof(AttnArgs) <= 4096,
+                  sizeof(AttnArgs) <= 4096 && sizeof(RopeArgs) <= 4096 && sizeof(AppendArgs) <= 4096 && sizeof(PagedArgs) <= 4096,
               "a kernel's argument block must fit the kernel argument segment");
 
 }  // namespace ltk

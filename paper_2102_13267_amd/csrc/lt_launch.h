@@ -18,6 +18,12 @@ hipError_t launch_gemm(const GemmArgs& a, hipStream_t s);
 hipError_t launch_attention(const AttnArgs& a, hipStream_t s);
 hipError_t launch_gemm_bf16(const GemmArgs& a, hipStream_t s);   // 128 x 128 tiles, split-K (called by launch_gemm)
 
+// Operators that nothing fuses with.  Their kernel files hand their launchers over when the library is
+// loaded, so that the host files link into a program without any of them.
+enum OperatorKernel : uint32_t { kOpRope = 0, kOpCacheAppend, kOpPagedAttention, kOperatorKernels };
+typedef hipError_t (*OperatorLauncher)(const void* args, hipStream_t s);
+bool set_operator(OperatorKernel which, OperatorLauncher launch);   // true
+
 // The library's static device scratch (lt_static_scratch.hip): its size, its address on `device`
 // (looked up once per device; `device` must be current), and a fill kernel.
 constexpr size_t kStaticScratchBytes = (size_t)16 << 20;

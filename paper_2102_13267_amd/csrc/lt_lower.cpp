@@ -9,8 +9,8 @@
 // Partition rules (deterministic; an independent implementation must produce the same list):
 //   classes   LEAF (device_data, scalar, constant), VIEW (expand / reshape that is not a root),
 //             EW (elementwise, permute, root views), ROW / COL / ALL (reductions by axis; the
-//             fixed row operators are ROW), MM (matmul).
-//   pass 0    every live EW / ROW / COL / ALL / MM node is a region of its own.
+//             fixed row operators are ROW), MM (matmul), OP (rotary positions and the paged cache: nothing joins them).
+//   pass 0    every live EW / ROW / COL / ALL / MM / OP node is a region of its own.
 //   pass 1    plain reductions absorb, walking down from the anchor, every elementwise node of the
 //             reduced tensor's shape whose users all lie inside the region (prologue).
 //   pass 2    in canonical order each still-single elementwise node joins the region of one of
@@ -36,7 +36,7 @@
 namespace lt {
 namespace {
 
-enum Class : uint8_t { C_DEAD, C_LEAF, C_VIEW, C_EW, C_ROW, C_COL, C_ALL, C_MM, C_SLICE };
+enum Class : uint8_t { C_DEAD, C_LEAF, C_VIEW, C_EW, C_ROW, C_COL, C_ALL, C_MM, C_SLICE, C_OP };
 
 struct Region {
   Class kind;
@@ -106,6 +106,19 @@ struct Lowering {
   static bool is_unary(uint16_t op) { return op >= LT_OP_NEG && op <= LT_OP_SIGMOID; }
   static bool is_binary(uint16_t op) { return op >= LT_OP_ADD && op <= LT_OP_GELU_GRAD; }
   static bool is_row_op(uint16_t op) { return op >= LT_OP_SOFTMAX && op <= LT_OP_XENT_GRAD; }
+  static bool is_operator(uint16_t op) { return op >= LT_OP_ROPE && op <= LT_OP_PAGED_ATTENTION; }
+  // operand k of an operator is [..., heads, dim], read where it lies: any strides before the last axis
+  static bool heads_operand(uint16_t op, size_t k) { return op == LT_OP_CACHE_APPEND ? k == 1 || k == 2 : k == 0; }
+  // a window of heads or of the first axis (the queries, keys and values of one projection) that such an operand can be
+  bool heads_window(int32_t i, int32_t u) const {
+    const Node* n = nd[i];
+    if (!is_operator(nd[u]->op) || n->rank < 3) return false;
+    for (int k = 0; k < n->n_attr; ++k)
+      if (n->attrs[k].key == LT_ATTR_AXIS && n->attrs[k].v.i != 0 && n->attrs[k].v.i != n->rank - 2) return false;
+    for (size_t k = 0; k < rins[u].size(); ++k)
+      if (rins[u][k].node == i && !heads_operand(nd[u]->op, k)) return false;
+    return true;
+  }
 
   // value of a node known at lowering time (constants 0 / 1, seen through views)
   bool const_of(Val v, double* out, const std::vector<std::vector<Val>>& ins) const {
@@ -200,10 +213,10 @@ struct Lowering {
         cls[i] = only_mm ? C_VIEW : C_EW;
       } else if (op == LT_OP_NARROW) {
         // a window is addressing (an offset and the base's strides) for the consumers that can
-        // address it: elementwise ops, contractions, permutations; otherwise a copy
+        // address it: elementwise ops, contractions, permutations, operators that read heads; otherwise a copy
         bool addr = !is_root[i] && !users[i].empty();
         for (int32_t u : users[i])
-          addr = addr && (is_unary(nd[u]->op) || is_binary(nd[u]->op) || nd[u]->op == LT_OP_MATMUL || nd[u]->op == LT_OP_PERMUTE);
+          addr = addr && (is_unary(nd[u]->op) || is_binary(nd[u]->op) || nd[u]->op == LT_OP_MATMUL || nd[u]->op == LT_OP_PERMUTE || heads_window(i, u));
         cls[i] = addr ? C_VIEW : C_EW;
       } else if (op == LT_OP_SLICE_UPDATE) cls[i] = C_SLICE;
       else if (is_unary(op) || is_binary(op)) cls[i] = C_EW;
@@ -215,6 +228,7 @@ struct Lowering {
         else return bad(LT_ERR_UNSUPPORTED, "reduction over a middle axis has no lowering");
       } else if (is_row_op(op)) cls[i] = C_ROW;
       else if (op == LT_OP_MATMUL) cls[i] = C_MM;
+      else if (is_operator(op)) cls[i] = C_OP;
       else return bad(LT_ERR_UNSUPPORTED, "opcode has no lowering");
     }
     return true;
@@ -472,6 +486,10 @@ struct Lowering {
               if (names_donor(base(x))) {
                 // a window update may overwrite its own base (operand 0, read in place) ...
                 if (m == rw->anchor && nd[m]->op == LT_OP_SLICE_UPDATE && names_donor(x) && x == rins[m][0] && !names_donor(base(rins[m][1]))) continue;
+                // ... and new rows may go into their own cache ...
+                if (m == rw->anchor && nd[m]->op == LT_OP_CACHE_APPEND && names_donor(x) && x == rins[m][0] && !names_donor(base(rins[m][1])) &&
+                    !names_donor(base(rins[m][2])))
+                  continue;
                 // ... everything else must read the donor position by position (an operand of another
                 // shape is broadcast: x[64, 64] * b[64] summed over rows into b)
                 if (m == rw->anchor || !names_donor(x) || shape_of(m) != out_shape(x) || nd[m]->op == LT_OP_PERMUTE || nd[m]->op == LT_OP_EXPAND ||
@@ -524,7 +542,7 @@ struct Lowering {
     char tmp[64];
     for (size_t k = 0; k < ordered.size(); ++k) {
       const Region* r = ordered[k];
-      static const char* names[] = {"DEAD", "LEAF", "VIEW", "EW", "ROW", "COL", "ALL", "MM", "SLICE"};
+      static const char* names[] = {"DEAD", "LEAF", "VIEW", "EW", "ROW", "COL", "ALL", "MM", "SLICE", "OP"};
       std::vector<Val> in, o;
       region_io(r->members, &in, &o);
       if (k) out += "\n";
@@ -1195,6 +1213,7 @@ struct Lowering {
     }
     if (r->kind == C_MM) return emit_gemm(k, r, post_m, out);
     if (r->kind == C_SLICE) return emit_slice(k, r);
+    if (r->kind == C_OP) return an->op == LT_OP_CACHE_APPEND ? emit_append(k, a) : an->op == LT_OP_PAGED_ATTENTION ? emit_paged(k, a) : emit_rope(k, a);
     if (!plain_reduce(an->op)) return emit_row_op(k, r, out);
     // ---- plain reduction
     const Val src = rins[a][0];
@@ -1712,6 +1731,186 @@ struct Lowering {
     plan->ptr_patches.push_back(PtrPatch{(uint32_t)launch, (uint32_t)offsetof(ltk::SliceArgs, out), so, 0, 1});
     touch(au.storage, launch);
     touch(so, launch);
+    return true;
+  }
+
+  // ---- rotary positions and the paged cache --------------------------------------------------------
+  // An operand [..., heads, dim] as it lies: the axes before `heads` are tokens, which one or two strides have to
+  // reach.
+  struct Heads {
+    int32_t storage;
+    uint8_t dtype;
+    int64_t byte_offset, inner, s_outer, s_inner, s_head;
+  };
+  bool operand_heads(Val v, Heads* h) {
+    if (is_imm(v)) return bad(LT_ERR_UNSUPPORTED, "heads that are a scalar's broadcast have no lowering");
+    Pattern pat;
+    if (!pattern_of(v, &pat)) return false;
+    const size_t r = pat.shape.size();
+    h->storage = pat.storage;
+    h->dtype = out_dtype(base(v));
+    h->byte_offset = pat.offset * (int64_t)dtype_size(h->dtype);
+    h->s_head = pat.stride[r - 2];
+    if (pat.shape[r - 1] > 1 && pat.stride[r - 1] != 1) return bad(LT_ERR_UNSUPPORTED, "heads whose elements are not next to each other have no lowering");
+    std::vector<int64_t> len, step;   // innermost first, neighbours that one stride reaches as one
+    for (size_t d = r - 2; d-- > 0;) {
+      if (pat.shape[d] == 1) continue;
+      if (!len.empty() && pat.stride[d] == step.back() * len.back()) len.back() *= pat.shape[d];
+      else {
+        len.push_back(pat.shape[d]);
+        step.push_back(pat.stride[d]);
+      }
+    }
+    if (len.size() > 2) return bad(LT_ERR_UNSUPPORTED, "tokens that two strides do not reach have no lowering");
+    h->inner = len.empty() ? 1 : std::max<int64_t>(1, len[0]);
+    h->s_inner = len.empty() ? 0 : step[0];
+    h->s_outer = len.size() < 2 ? 0 : step[1];
+    return true;
+  }
+
+  // A whole tensor in memory (lengths, tables, positions, a cache).
+  bool operand_dense(Val v, int32_t* storage, int64_t* byte_offset) {
+    if (is_imm(v)) return bad(LT_ERR_UNSUPPORTED, "lengths, tables, positions and caches must be tensors in memory");
+    Pattern pat;
+    if (!pattern_of(v, &pat)) return false;
+    const std::vector<int64_t> cs = contiguous(pat.shape);
+    for (size_t d = 0; d < pat.shape.size(); ++d)
+      if (pat.shape[d] > 1 && pat.stride[d] != cs[d]) return bad(LT_ERR_UNSUPPORTED, "lengths, tables, positions and caches that are broadcast have no lowering");
+    *storage = pat.storage;
+    *byte_offset = pat.offset * (int64_t)dtype_size(out_dtype(base(v)));
+    return true;
+  }
+
+  void patch(int launch, size_t at, int32_t storage, int64_t byte_offset, bool write = false) {
+    plan->ptr_patches.push_back(PtrPatch{(uint32_t)launch, (uint32_t)at, storage, byte_offset, (uint8_t)(write ? 1 : 0)});
+    touch(storage, launch);
+  }
+
+  void rotary_of(const Node* n, bool back, ltk::Rotary* r) const {
+    auto get = [&](uint16_t key) -> const Attr& {
+      int k = 0;
+      while (n->attrs[k].key != key) ++k;
+      return n->attrs[k];
+    };
+    const double pi = 3.14159265358979323846;
+    r->dims = (uint32_t)get(LT_ATTR_ROPE_DIMS).v.i;
+    r->interleaved = (uint32_t)get(LT_ATTR_ROPE_INTERLEAVED).v.i;
+    r->amplitude = (float)get(LT_ATTR_ROPE_AMPLITUDE).v.f;
+    r->back = back ? 1u : 0u;
+    const double theta = get(LT_ATTR_ROPE_BASE).v.f, factor = get(LT_ATTR_ROPE_FACTOR).v.f, original = get(LT_ATTR_ROPE_ORIGINAL).v.f;
+    const double low = get(LT_ATTR_ROPE_LOW).v.f, high = get(LT_ATTR_ROPE_HIGH).v.f;
+    for (uint32_t i = 0; i < r->dims / 2; ++i) {
+      const double f = std::pow(theta, -2.0 * i / r->dims);
+      const double keep = original == 0.0 ? 0.0 : std::min(1.0, std::max(0.0, (original * f / (2.0 * pi) - low) / (high - low)));
+      r->turns[i] = f * (keep + (1.0 - keep) / factor) * 2.0 / pi;
+    }
+  }
+
+  bool emit_rope(int k, int32_t a) {
+    const Node* an = nd[a];
+    const int launch = (int)plan->launches.size();
+    Heads x;
+    int32_t ps = -1;
+    int64_t po = 0;
+    if (!operand_heads(rins[a][0], &x) || !operand_dense(rins[a][1], &ps, &po)) return false;
+    ltk::RopeArgs args{};
+    args.dtype = an->dtype;
+    args.dim = (uint32_t)an->dims[an->rank - 1];
+    args.heads = (uint32_t)an->dims[an->rank - 2];
+    args.tokens = (uint64_t)numel(an->dims, an->rank - 2);
+    args.n_pos = (uint32_t)std::max<int64_t>(1, count(out_shape(rins[a][1])));
+    args.inner = (uint32_t)x.inner;
+    args.s_outer = x.s_outer;
+    args.s_inner = x.s_inner;
+    args.s_head = x.s_head;
+    rotary_of(an, an->op == LT_OP_ROPE_GRAD, &args.rotary);
+    Launch l = make_launch(L_ROPE, k, args);
+    l.bytes = 2 * (uint64_t)count(shape_of(a)) * dtype_size(an->dtype) + 4 * (uint64_t)count(out_shape(rins[a][1]));
+    plan->launches.push_back(std::move(l));
+    patch(launch, offsetof(ltk::RopeArgs, x), x.storage, x.byte_offset);
+    patch(launch, offsetof(ltk::RopeArgs, positions), ps, po);
+    patch(launch, offsetof(ltk::RopeArgs, out), storage_of[a][0], 0, true);
+    return true;
+  }
+
+  // New rows of a cache: written into its own (donated) buffer, or into a copy.
+  bool emit_append(int k, int32_t a) {
+    const Node* an = nd[a];
+    const int launch = (int)plan->launches.size();
+    Heads kv[2];
+    int32_t s[4] = {-1, -1, -1, -1};   // cache, lengths, table, offsets
+    int64_t o[4] = {0, 0, 0, 0};
+    const bool ragged = rins[a].size() == 6;
+    if (!operand_heads(rins[a][1], &kv[0]) || !operand_heads(rins[a][2], &kv[1]) || !operand_dense(rins[a][0], &s[0], &o[0]) ||
+        !operand_dense(rins[a][3], &s[1], &o[1]) || !operand_dense(rins[a][4], &s[2], &o[2]) || (ragged && !operand_dense(rins[a][5], &s[3], &o[3])))
+      return false;
+    const int32_t out = storage_of[a][0];
+    const bool in_place = plan->storages[out].param >= 0 && plan->storages[out].param == plan->storages[s[0]].param && o[0] == 0;
+    const std::vector<int64_t> ks = out_shape(rins[a][1]), ts = out_shape(rins[a][4]);
+    ltk::AppendArgs args{};
+    args.cache_dtype = an->dtype;
+    args.dtype = kv[0].dtype;
+    args.cache_elems = (uint64_t)count(shape_of(a));
+    args.tokens = (uint32_t)ks[0];
+    args.seqs = (uint32_t)ts[0];
+    args.slots = (uint32_t)ts[1];
+    args.pages = (uint32_t)an->dims[0];
+    args.heads = (uint32_t)an->dims[2];
+    args.dim = (uint32_t)an->dims[4];
+    args.rows.set((uint32_t)an->dims[3]);
+    args.k_token = kv[0].s_inner;
+    args.k_head = kv[0].s_head;
+    args.v_token = kv[1].s_inner;
+    args.v_head = kv[1].s_head;
+    if (an->n_attr > 0) rotary_of(an, false, &args.rotary);
+    Launch l = make_launch(L_APPEND, k, args);
+    const uint64_t n = (uint64_t)count(ks);
+    l.bytes = 2 * n * (dtype_size(args.dtype) + dtype_size(an->dtype)) + (in_place ? 0 : 2 * args.cache_elems * dtype_size(an->dtype));
+    plan->launches.push_back(std::move(l));
+    patch(launch, offsetof(ltk::AppendArgs, cache), out, 0, true);
+    if (!in_place) patch(launch, offsetof(ltk::AppendArgs, copy_from), s[0], o[0]);
+    patch(launch, offsetof(ltk::AppendArgs, k), kv[0].storage, kv[0].byte_offset);
+    patch(launch, offsetof(ltk::AppendArgs, v), kv[1].storage, kv[1].byte_offset);
+    patch(launch, offsetof(ltk::AppendArgs, lengths), s[1], o[1]);
+    patch(launch, offsetof(ltk::AppendArgs, table), s[2], o[2]);
+    if (ragged) patch(launch, offsetof(ltk::AppendArgs, offsets), s[3], o[3]);
+    return true;
+  }
+
+  bool emit_paged(int k, int32_t a) {
+    const Node* an = nd[a];
+    const int launch = (int)plan->launches.size();
+    Heads q;
+    int32_t s[3] = {-1, -1, -1};   // cache, lengths, table
+    int64_t o[3] = {0, 0, 0};
+    if (!operand_heads(rins[a][0], &q)) return false;
+    for (int i = 0; i < 3; ++i)
+      if (!operand_dense(rins[a][1 + i], &s[i], &o[i])) return false;
+    const std::vector<int64_t> cs = out_shape(rins[a][1]), ts = out_shape(rins[a][3]);
+    ltk::PagedArgs args{};
+    args.dtype = an->dtype;
+    args.seqs = (uint32_t)an->dims[0];
+    args.heads = (uint32_t)an->dims[1];
+    args.dim = (uint32_t)an->dims[2];
+    args.kv_heads = (uint32_t)cs[2];
+    args.slots = (uint32_t)ts[1];
+    args.pages = (uint32_t)cs[0];
+    args.rows.set((uint32_t)cs[3]);
+    args.capacity = args.pages == 0 ? 0u : args.slots * args.rows.d;
+    args.scale = (float)an->attrs[0].v.f;
+    args.q_seq = q.s_inner;
+    args.q_head = q.s_head;
+    Launch l = make_launch(L_PAGED, k, args);
+    // (how long the sequences are is known on the device alone: as if every page were read once)
+    const uint64_t held = (uint64_t)count(cs), w = dtype_size(an->dtype);
+    l.bytes = held * w + 2 * (uint64_t)count(shape_of(a)) * w;
+    l.flops = 2 * held * (args.heads / args.kv_heads);
+    plan->launches.push_back(std::move(l));
+    patch(launch, offsetof(ltk::PagedArgs, q), q.storage, q.byte_offset);
+    patch(launch, offsetof(ltk::PagedArgs, cache), s[0], o[0]);
+    patch(launch, offsetof(ltk::PagedArgs, lengths), s[1], o[1]);
+    patch(launch, offsetof(ltk::PagedArgs, table), s[2], o[2]);
+    patch(launch, offsetof(ltk::PagedArgs, out), storage_of[a][0], 0, true);
     return true;
   }
 

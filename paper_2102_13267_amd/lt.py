@@ -3,6 +3,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from typing import NamedTuple
 
 import numpy as np
 
@@ -21,10 +22,32 @@ OPCODES = {
     "sum": 64, "amax": 65, "mean": 66,
     "softmax": 80, "softmax_grad": 81, "layer_norm": 82, "layer_norm_grad": 83, "xent": 84, "xent_grad": 85,
     "matmul": 96,
+    "rope": 112, "rope_grad": 113, "cache_append": 114, "paged_attention": 115,
 }
 ATTR_VALUE, ATTR_DTYPE, ATTR_AXIS, ATTR_EPS, ATTR_TRANS_A, ATTR_TRANS_B, ATTR_START, ATTR_LENGTH, ATTR_DIM0 = 1, 2, 3, 4, 5, 6, 7, 8, 16
+ATTR_ROPE_DIMS, ATTR_ROPE_INTERLEAVED, ATTR_ROPE_BASE, ATTR_ROPE_FACTOR, ATTR_ROPE_ORIGINAL, ATTR_ROPE_LOW, ATTR_ROPE_HIGH, ATTR_ROPE_AMPLITUDE = range(32, 40)
+ATTR_SCALE = 40
 LT_DONATABLE = 1
 MAX_RANK = 6
+
+
+class Rotary(NamedTuple):
+    """How rotary positions turn a head (include/lt.h has the formulas): the first `dims` elements of it (None: all),
+    in pairs (i, i + dims / 2) or, interleaved, (2 i, 2 i + 1).  For contexts longer than a model was trained on: `factor`
+    slows the pairs down, all of them, or, with the length it was trained on as `original`, those of low frequency."""
+    dims: int | None = None
+    base: float = 10000.0
+    interleaved: bool = False
+    factor: float = 1.0
+    original: float = 0.0
+    low: float = 1.0
+    high: float = 32.0
+    amplitude: float = 1.0
+
+    def attrs(self):
+        real = [(ATTR_ROPE_BASE, float(self.base)), (ATTR_ROPE_FACTOR, float(self.factor)), (ATTR_ROPE_ORIGINAL, float(self.original)), (ATTR_ROPE_LOW, float(self.low)),
+                (ATTR_ROPE_HIGH, float(self.high)), (ATTR_ROPE_AMPLITUDE, float(self.amplitude))]
+        return ([] if self.dims is None else [(ATTR_ROPE_DIMS, int(self.dims))]) + [(ATTR_ROPE_INTERLEAVED, int(bool(self.interleaved)))] + real
 
 
 class _AttrV(C.Union):
@@ -220,6 +243,7 @@ _CAST, _EXPAND, _RESHAPE, _PERMUTE = OPCODES["cast"], OPCODES["expand"], OPCODES
 _NARROW, _SLICE_UPDATE = OPCODES["narrow"], OPCODES["slice_update"]
 _SUM, _AMAX, _MEAN = OPCODES["sum"], OPCODES["amax"], OPCODES["mean"]
 _LAYER_NORM, _MATMUL = OPCODES["layer_norm"], OPCODES["matmul"]
+_ROPE, _ROPE_GRAD, _CACHE_APPEND, _PAGED_ATTENTION = OPCODES["rope"], OPCODES["rope_grad"], OPCODES["cache_append"], OPCODES["paged_attention"]
 
 
 class Context:
@@ -399,6 +423,38 @@ class Context:
                 attrs.append((ATTR_DTYPE, DTYPES[dtype]))
             at = self._encode(key, attrs)
         return _rec_op(self, self._hv, _MATMUL, (a, b), at[0], at[1], 1)
+
+    # rotary positions, and a paged cache of keys and values [pages, 2, key heads, rows, dim]
+    def _rotary(self, code, inputs, rotary):
+        key = (code, rotary)
+        at = self._attrs.get(key) or self._encode(key, rotary.attrs())
+        return _rec_op(self, self._hv, code, inputs, at[0], at[1], 1)
+
+    def rope(self, x, positions, rotary=Rotary()):
+        """x [..., heads, dim] with each head rotated by its token's position (int32 [...], or the last of these axes)."""
+        return self._rotary(_ROPE, (x, positions), rotary)
+
+    def rope_grad(self, dy, positions, rotary=Rotary()):
+        """The gradient of rope's x: dy turned back."""
+        return self._rotary(_ROPE_GRAD, (dy, positions), rotary)
+
+    def cache_append(self, cache, k, v, lengths, table, offsets=None, rotary=None):
+        """The cache with the new rows of k and v [tokens, key heads, dim] in it, k rotated if `rotary` is given.  Assigned to a donatable
+        cache, it is written in place: ctx.assign(cache, ctx.cache_append(cache, ...)).  Tokens offsets[s] to offsets[s + 1] - 1 are sequence
+        s's last ones, lengths (int32) counting them; without offsets token s is sequence s's."""
+        inputs = (cache, k, v, lengths, table) if offsets is None else (cache, k, v, lengths, table, offsets)
+        if rotary is None:
+            return _rec_op(self, self._hv, _CACHE_APPEND, inputs, _NO_ATTRS_ADDR, 0, 1)
+        return self._rotary(_CACHE_APPEND, inputs, rotary)
+
+    def paged_attention(self, q, cache, lengths, table, scale=None):
+        """softmax(scale q K^T) V of one token a sequence, q [sequences, heads, dim], over the first lengths[s] positions that
+        table [sequences, slots] places in the cache.  scale: 1 / sqrt(dim)."""
+        if scale is None:
+            return _rec_op(self, self._hv, _PAGED_ATTENTION, (q, cache, lengths, table), _NO_ATTRS_ADDR, 0, 1)
+        key = (_PAGED_ATTENTION, float(scale))
+        at = self._attrs.get(key) or self._encode(key, [(ATTR_SCALE, key[1])])
+        return _rec_op(self, self._hv, _PAGED_ATTENTION, (q, cache, lengths, table), at[0], at[1], 1)
 
     def narrow(self, x, axis, start, length):
         key = (_NARROW, int(axis), int(start), int(length))

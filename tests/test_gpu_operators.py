@@ -1,0 +1,564 @@
+"""Rotary positions, appending to a paged cache, and attention that reads it, against the oracle in 64 bits.
+
+Tolerances, from the arithmetic.  E = 2^-24 is half a step of fp32, R half a step of the result's type (2^-24, bf16 2^-8).
+Rotation: cosine and sine err by at most 3 E (their argument's rounding, polynomials, the amplitude), and two products and a sum
+round three times: |got - ref| <= 6 E amplitude (|x| + |y|) + R |ref|.
+Attention: a score is a sum of dim products and some factors, ds = (dim + 8) E scale max_k sum_d |q_d k_d| off at most, which
+puts exp(score) 2 ds + 4 E off; a weight may be rounded to the cache's type before its product (R), sums of n terms
+err by n E of their magnitudes: |got - ref| <= (2 (2 ds + 4 E + n E) + R) sum_k p |v| + R |ref|.
+Values and rows that are only moved are exact."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle.numeric import Eager, round_to_bf16
+from paper_2102_13267_amd import Context, Rotary
+
+pytestmark = pytest.mark.gpu
+E24 = 2.0 ** -24
+HALF = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8}
+
+
+def context(**kw):
+    return Context(device=0, workspace_bytes=kw.pop("workspace_bytes", 256 << 20), **kw)
+
+
+def data(rg, shape, dtype, scale=1.0):
+    x = (rg.standard_normal(shape) * scale).astype(np.float32)
+    return round_to_bf16(x) if dtype == "bf16" else x
+
+
+def ints(a):
+    return np.asarray(a, np.int32)
+
+
+# ---- rotary positions ---------------------------------------------------------------------------
+def rope_bound(x, ref, r, dtype):
+    """elementwise, from the pairs' magnitudes"""
+    n = x.shape[-1] if r.dims is None else r.dims
+    _, first, second = Eager._angles(np.zeros(1), r, x.shape[-1])
+    pair = np.zeros(x.shape)
+    pair[..., first] = pair[..., second] = np.abs(x[..., first]).astype(np.float64) + np.abs(x[..., second])
+    assert n == 2 * len(first)
+    return 6 * E24 * abs(r.amplitude) * pair + HALF[dtype] * np.abs(ref) + 1e-37
+
+
+def check_rope(shape, positions, r, dtype, seed=0):
+    rg = np.random.default_rng(seed)
+    ctx, E = context(), Eager("f64")
+    x, dy, p = data(rg, shape, dtype), data(rg, shape, dtype), ints(positions)
+    X, DY, P = ctx.tensor(x, dtype), ctx.tensor(dy, dtype), ctx.tensor(p)
+    y, dx = ctx.rope(X, P, r), ctx.rope_grad(DY, P, r)
+    for got, src, op in ((y, x, E.rope), (dx, dy, E.rope_grad)):
+        ref = E.fetch(op(E.tensor(src, dtype), E.tensor(p), r))
+        g = ctx.fetch(got)
+        assert g.shape == ref.shape
+        assert (np.abs(g - ref) <= rope_bound(src, ref, r, dtype)).all(), np.max(np.abs(g - ref) - rope_bound(src, ref, r, dtype))
+        n = shape[-1] if r.dims is None else r.dims
+        assert np.array_equal(g[..., n:], src[..., n:])
+    ctx.close()
+
+
+SHAPES = [((1, 1, 2), None), ((5, 3, 64), None), ((33, 2, 80), 40), ((7, 32, 128), None), ((3, 1, 7), 4), ((2, 9, 50), 50), ((4, 5, 72), 36), ((3, 2, 256), 256), ((2, 3, 300), 256),
+          ((129, 7, 20), 12), ((2, 1, 257), 2), ((6, 4, 24), 24), ((1, 70, 96), 64), ((9, 2, 112), 96)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("shape,dims", SHAPES)
+def test_rope(shape, dims, interleaved, dtype):
+    r = Rotary(dims=dims if dims is not None or shape[-1] % 2 == 0 else shape[-1] - 1, interleaved=interleaved)
+    check_rope(shape, np.random.default_rng(9).integers(0, 5000, shape[0]), r, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rope_positions_of_any_size_and_sign(dtype):
+    p = [0, 1, -1, 2 ** 31 - 1, -2 ** 31, 1 << 20, 123456789, -7]
+    for r in (Rotary(), Rotary(interleaved=True, base=1.0, amplitude=-0.5), Rotary(dims=16, factor=8.0, original=8192.0, base=500000.0, amplitude=1.3), Rotary(factor=3.5)):
+        check_rope((len(p), 3, 32), p, r, dtype, 1)
+
+
+@pytest.mark.parametrize("lead,pos", [((2, 5), (2, 5)), ((2, 5), (5,)), ((3, 2, 5), (2, 5)), ((2, 3, 2, 3), (3,)), ((1, 6), (6,)), ((6, 1), (1,))])
+def test_rope_positions_shared_by_leading_axes(lead, pos):
+    for dtype, dim in (("bf16", 64), ("f32", 36)):
+        check_rope(lead + (3, dim), np.random.default_rng(2).integers(0, 1000, pos), Rotary(dims=32), dtype, 2)
+
+
+def test_rope_of_many_tokens_and_of_few_long_ones():
+    check_rope((70001, 2, 32), np.arange(70001), Rotary(), "bf16", 3)
+    check_rope((1, 3000, 64), [77], Rotary(interleaved=True), "f32", 4)
+    check_rope((2, 3, 5000), [5, 6], Rotary(dims=200), "bf16", 5)
+
+
+def test_rope_of_views():
+    """windows of heads of one projection (also off 16 bytes), windows of rows, permuted and broadcast operands"""
+    rg = np.random.default_rng(6)
+    for dtype, dim in (("bf16", 64), ("bf16", 20), ("f32", 16), ("f32", 7)):
+        r = Rotary(dims=6, interleaved=True) if dim == 7 else Rotary()
+        ctx, E = context(), Eager("f64")
+        x, p = data(rg, (4, 6, 5, dim), dtype), ints(rg.integers(0, 99, (4, 6)))
+
+        def run(B, fx):
+            X, P = B.tensor(x, dtype), B.tensor(p)
+            P6 = B.tensor(p[0])
+            return [B.rope(B.narrow(X, 2, 1, 3), P, r), B.rope_grad(B.narrow(X, 0, 1, 2), P6, r), B.rope(B.narrow(X, 1, 1, 3), B.tensor(p[1, :3]), r),
+                    B.rope(B.permute(X, (0, 2, 1, 3)), B.tensor(p[2, :5]), r), B.rope(B.expand(B.narrow(X, 0, 2, 1), (4, 6, 5, dim)), P, r),
+                    B.rope(B.expand(B.reshape(B.narrow(X, 1, 0, 1), (4, 1, 5, dim)), (4, 6, 5, dim)), P, r), B.rope(B.reshape(X, (24, 5, dim)), B.reshape(P, (24,)), r)]
+        outs, refs = run(ctx, x), run(E, x)
+        for o, ref in zip(outs, refs):
+            g, w = ctx.fetch(o), E.fetch(ref)
+            # (|x| + |y| of a pair is at most sqrt 2 of its rotated length, itself at most sqrt 2 of the larger result)
+            assert (np.abs(g - w) <= 6 * E24 * 2 * np.abs(x).max() + HALF[dtype] * np.abs(w)).all()
+        ctx.close()
+
+
+def test_rope_gradient_is_the_difference_quotient_and_the_adjoint():
+    rg = np.random.default_rng(7)
+    ctx, r = context(), Rotary(dims=48, factor=2.0, amplitude=1.2)
+    x, d, dy = (rg.standard_normal((40, 3, 64)).astype(np.float32) for _ in range(3))
+    P = ctx.tensor(ints(rg.integers(0, 9999, 40)))
+    h = 0.5                                             # rope is linear: any step serves
+    up, down, dx = (ctx.fetch(t) for t in (ctx.rope(ctx.tensor(x + h * d), P, r), ctx.rope(ctx.tensor(x - h * d), P, r), ctx.rope_grad(ctx.tensor(dy), P, r)))
+    lhs, rhs = ((up.astype(np.float64) - down) / (2 * h) * dy).sum(), (dx.astype(np.float64) * d).sum()
+    # every element of both sides errs by at most 7 E of magnitudes below 8, independently enough to add up as they are: 7680 terms of up to 8 * 8
+    assert abs(lhs - rhs) <= 7 * E24 * 1.2 * 2 * sum((np.abs(a).sum() * 8) for a in (dy, d)), (lhs, rhs)
+    ctx.close()
+
+
+# ---- the paged cache ------------------------------------------------------------------------------
+def paged_case(rg, lens, kv, rows, dim, dtype, spare=2, fill=None, slots=None):
+    """A cache whose pages are handed out in random order; entries behind a sequence's pages name no page."""
+    need = [-(-max(n, 0) // rows) for n in lens]
+    slots = max(max(need, default=0), 1) + 1 if slots is None else slots
+    need = [min(n, slots) for n in need]
+    pages = sum(need) + spare
+    order = rg.permutation(pages)
+    table = np.full((len(lens), slots), -1, np.int32)
+    at = 0
+    for s, n in enumerate(need):
+        table[s, :n] = order[at:at + n]
+        at += n
+        table[s, n:] = rg.choice([-1, pages, 2 ** 31 - 1, -2 ** 31], slots - n)
+    cache = data(rg, (pages, 2, kv, rows, dim), dtype)
+    if fill is not None:     # what no sequence holds
+        held = np.zeros((pages, rows), bool)
+        for s, n in enumerate(lens):
+            for p in range(max(0, min(n, slots * rows))):
+                held[table[s, p // rows], p % rows] = True
+        cache[np.broadcast_to(~held[:, None, None, :, None], cache.shape)] = fill
+    return cache, table
+
+
+def check_append(lens, news, kv, rows, dim, cache_dtype, dtype, rotary, pad=0, donate=True, seed=0, offsets=True):
+    rg = np.random.default_rng(seed)
+    ctx, E = context(), Eager("f64")
+    cache, table = paged_case(rg, lens, kv, rows, dim, cache_dtype)
+    tokens = sum(news) + pad
+    k, v = data(rg, (tokens, kv, dim), dtype), data(rg, (tokens, kv, dim), dtype)
+    off = ints(np.concatenate([[0], np.cumsum(news)])) if offsets else None
+    args = lambda B: [B.tensor(cache, cache_dtype, donatable=donate), B.tensor(k, dtype), B.tensor(v, dtype), B.tensor(ints(lens)), B.tensor(table)]     # noqa: E731
+    T, R = args(ctx), args(E)
+    new = ctx.cache_append(*T, offsets=None if off is None else ctx.tensor(off), rotary=rotary)
+    if donate:
+        ctx.assign(T[0], new)
+        new = T[0]
+    got = ctx.fetch(new)
+    if donate:
+        assert "->p" in ctx.dump_plan()
+    else:
+        assert np.array_equal(ctx.fetch(T[0]), cache)
+    ref = E.fetch(E.cache_append(*R, offsets=None if off is None else E.tensor(off), rotary=rotary))
+    wrote = ref != cache
+    assert np.array_equal(got[:, 1], round_to_bf16(ref[:, 1]) if cache_dtype == "bf16" else ref[:, 1].astype(np.float32))
+    n = 0 if rotary is None else dim if rotary.dims is None else rotary.dims
+    rest = ref[:, 0, ..., n:]
+    assert np.array_equal(got[:, 0, ..., n:], round_to_bf16(rest) if cache_dtype == "bf16" else rest.astype(np.float32))
+    # a rotated key: its pair is no longer than sqrt 2 times the pair it came from, which is as long
+    big = np.abs(k).max(initial=0.0) * 2 * (abs(rotary.amplitude) if rotary else 1.0)
+    tol = np.where(wrote[:, 0], 6 * E24 * big + HALF[cache_dtype] * np.abs(ref[:, 0]), 0.0)
+    assert (np.abs(got[:, 0] - ref[:, 0]) <= tol).all()
+    ctx.close()
+
+
+@pytest.mark.parametrize("cache_dtype,dtype", [("f32", "f32"), ("bf16", "bf16"), ("bf16", "f32"), ("f32", "bf16")])
+@pytest.mark.parametrize("kv,rows,dim,rotary", [(1, 1, 2, Rotary()), (3, 16, 64, Rotary()), (2, 24, 72, Rotary(dims=36, interleaved=True)), (8, 16, 128, Rotary(factor=8.0, original=512.0)),
+                                                (2, 7, 20, None), (1, 64, 7, Rotary(dims=2)), (5, 8, 50, Rotary(interleaved=True)), (2, 5, 300, Rotary(dims=256))])
+def test_append(kv, rows, dim, rotary, cache_dtype, dtype):
+    check_append([5, 1, 40, 0, 17, 33], [2, 1, 40, 0, 0, 16], kv, rows, dim, cache_dtype, dtype, rotary, pad=3)
+    check_append([5, 1, 40, 0, 17, 33], [1] * 6, kv, rows, dim, cache_dtype, dtype, rotary, offsets=False)
+
+
+def test_append_leaves_a_cache_that_somebody_else_reads():
+    check_append([5, 1, 40], [2, 1, 40], 2, 16, 64, "bf16", "bf16", Rotary(), donate=False)
+    check_append([3], [1], 1, 3, 5, "bf16", "f32", None, donate=False)       # (an odd number of two-byte elements)
+
+
+def test_append_of_many_sequences_and_of_long_prompts():
+    rg = np.random.default_rng(8)
+    lens = rg.integers(0, 60, 700)
+    check_append([int(n) for n in lens], [int(rg.integers(0, n + 1)) for n in lens], 2, 16, 32, "bf16", "bf16", Rotary(), pad=70, seed=1)
+    check_append([int(n) for n in lens], [1] * 700, 2, 16, 32, "bf16", "bf16", Rotary(interleaved=True), offsets=False, seed=2)
+    check_append([4000, 2], [4000, 1], 4, 64, 64, "bf16", "bf16", Rotary(), seed=3)
+
+
+def test_append_drops_tokens_without_a_place():
+    """positions before 0 or behind the table, pages that the cache has not, tokens before the first and behind the last sequence"""
+    rg = np.random.default_rng(9)
+    E = Eager("f64")
+    for dtype, dim in (("bf16", 32), ("f32", 6)):
+        ctx = context()
+        cache, k, v = data(rg, (6, 2, 2, 4, dim), dtype), data(rg, (30, 2, dim), dtype), data(rg, (30, 2, dim), dtype)
+        table = ints([[0, 1, -1], [2, 6, 3], [2 ** 31 - 1, -2 ** 31, 4], [5, 5, 5]])
+        lens, off = ints([9, 12, 30, -5]), ints([2, 9, 15, 27, 28])
+        args = lambda B: [B.tensor(cache, dtype, donatable=True), B.tensor(k, dtype), B.tensor(v, dtype), B.tensor(lens), B.tensor(table)]     # noqa: E731
+        got = ctx.fetch(ctx.cache_append(*args(ctx), offsets=ctx.tensor(off)))
+        ref = E.fetch(E.cache_append(*args(E), offsets=E.tensor(off)))
+        assert np.array_equal(got, ref.astype(np.float32)) and (ref != cache).any()
+        # offsets that decrease, or lie outside: which tokens are written is open, nothing else is touched
+        for bad in ([0, 20, 10, 5, 30], [-5, -5, -5, -5, -5], [100, 0, 100, 0, 100], [0, 2 ** 31 - 1, -2 ** 31, 7, 30]):
+            C = ctx.tensor(cache, dtype, donatable=True)
+            got = ctx.fetch(ctx.cache_append(C, *args(ctx)[1:], offsets=ctx.tensor(ints(bad))))
+            assert np.isin(got[got != cache], np.concatenate([k.ravel(), v.ravel()])).all()
+        ctx.close()
+
+
+def check_attention(lens, heads, kv, rows, dim, dtype, scale=None, seed=0, fill=np.nan, spread=1.0, table_edit=None, slots=None):
+    rg = np.random.default_rng(seed)
+    ctx, E = context(), Eager("f64")
+    cache, table = paged_case(rg, lens, kv, rows, dim, dtype, fill=fill, slots=slots)
+    if table_edit:
+        table_edit(table)
+    q = data(rg, (len(lens), heads, dim), dtype, spread)
+    args = lambda B: [B.tensor(q, dtype), B.tensor(cache, dtype), B.tensor(ints(lens)), B.tensor(table)]     # noqa: E731
+    got = ctx.fetch(ctx.paged_attention(*args(ctx), scale=scale))
+    with np.errstate(invalid="ignore"):
+        ref = E.fetch(E.paged_attention(*args(E), scale=scale))
+    compare_attention(got, ref, q, cache, lens, table, dtype, scale)
+    ctx.close()
+    return got
+
+
+def compare_attention(got, ref, q, cache, lens, table, dtype, scale=None):
+    seqs, heads, dim = q.shape
+    pages, _, kv, rows, _ = cache.shape
+    scale = 1 / math.sqrt(dim) if scale is None else scale
+    for s in range(seqs):
+        pos = np.arange(max(0, min(lens[s], table.shape[1] * rows)))
+        ids = table[s, pos // rows]
+        pos, ids = pos[(ids >= 0) & (ids < pages)], ids[(ids >= 0) & (ids < pages)]
+        if not len(pos):
+            assert not got[s].any()
+            continue
+        for h in range(heads):
+            k, v = (cache[ids, i, h // (heads // kv), pos % rows].astype(np.float64) for i in (0, 1))
+            qq = q[s, h].astype(np.float64)
+            ds = (dim + 8) * E24 * abs(scale) * (np.abs(k) @ np.abs(qq)).max()
+            e = np.exp(k @ qq * scale - (k @ qq * scale).max())
+            mass = (e / e.sum()) @ np.abs(v)
+            tol = (2 * (2 * ds + 4 * E24 + len(pos) * E24) + HALF[dtype]) * mass + HALF[dtype] * np.abs(ref[s, h]) + 1e-37
+            assert (np.abs(got[s, h] - ref[s, h]) <= tol).all(), (s, h, np.max(np.abs(got[s, h] - ref[s, h]) / tol))
+
+
+LENS = [0, 1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 100, 127, 128, 129, 257, -3]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("heads,kv,rows,dim", [(1, 1, 16, 64), (4, 4, 16, 128), (8, 2, 32, 128), (7, 1, 16, 80), (12, 3, 24, 72), (16, 1, 64, 128), (17, 1, 16, 64), (40, 2, 8, 96),
+                                               (70, 1, 16, 32), (4, 2, 1, 20), (6, 2, 5, 50), (3, 3, 7, 7), (2, 1, 16, 256), (33, 1, 16, 256), (4, 2, 48, 160), (2, 2, 100, 1), (6, 1, 128, 33)])
+def test_attention(heads, kv, rows, dim, dtype):
+    """every length around a tile's ends, none and negative ones among them; what no sequence holds is NaN"""
+    check_attention(LENS, heads, kv, rows, dim, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_attention_of_one_long_sequence(dtype):
+    for n, heads, kv, rows, dim in ((20000, 8, 1, 64, 128), (9001, 4, 4, 16, 64), (5003, 12, 2, 24, 80), (3333, 2, 1, 7, 256), (6007, 40, 1, 16, 128)):
+        check_attention([n], heads, kv, rows, dim, dtype, seed=n)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_attention_of_lengths_far_apart(dtype):
+    rg = np.random.default_rng(10)
+    check_attention([8000, 1, 0, 300, 5000, 2, 0, 0, 129, 64] + [int(n) for n in rg.integers(0, 40, 60)], 8, 2, 16, 64, dtype)
+    check_attention([int(n) for n in rg.integers(0, 700, 300)], 4, 2, 16, 32, dtype)
+    check_attention([int(n) for n in rg.integers(0, 9, 1100)], 2, 1, 8, 32, dtype)
+    check_attention([40] * 5, 4, 2, 16, 64, dtype, slots=2000)                    # a table far wider than anybody needs
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_attention_with_missing_pages(dtype):
+    def edit(table):
+        table[0, 1], table[1, 0], table[2, :] = -1, 2 ** 31 - 1, -7
+        table[3, 2:5] = -2 ** 31
+    for rows in (16, 10):
+        check_attention([100, 40, 70, 300, 90], 4, 2, rows, 64, dtype, table_edit=edit, fill=None)
+    check_attention([1000, 40], 4, 2, 16, 64, dtype, slots=3)                     # longer than the table: its slots are all there is
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_attention_next_to_values_that_do_not_count(dtype):
+    """infinities and the type's lowest value in rows behind the end, within the last page"""
+    for fill in (np.inf, -np.inf, float(round_to_bf16(np.float32(-3.3e38)))):
+        check_attention([1, 5, 20, 45, 0], 4, 2, 16, 64, dtype, fill=fill)
+        check_attention([1, 5, 20, 45, 0], 4, 2, 24, 40, dtype, fill=fill)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_attention_of_peaked_and_flat_scores(dtype):
+    check_attention([700, 33], 4, 2, 16, 64, dtype, spread=30.0)                  # one key takes it all
+    check_attention([700, 33], 4, 2, 16, 64, dtype, scale=0.0)
+    check_attention([700, 33], 4, 2, 16, 64, dtype, scale=-0.7)
+    got = check_attention([1, 1], 2, 2, 16, 64, dtype)
+    assert np.isfinite(got).all()
+
+
+def test_attention_passes_nan_and_infinite_scores_on():
+    rg = np.random.default_rng(11)
+    for dtype in ("f32", "bf16"):
+        ctx = context()
+        cache, table = paged_case(rg, [40, 40, 200], 1, 16, 64, dtype)
+        cache[table[0, 1], 0, 0, 3, 5] = np.nan
+        cache[table[2, 0], 1, 0, 2, 7] = np.inf
+        got = ctx.fetch(ctx.paged_attention(ctx.tensor(data(rg, (3, 2, 64), dtype), dtype), ctx.tensor(cache, dtype), ctx.tensor(ints([40, 40, 200])), ctx.tensor(table)))
+        assert np.isnan(got[0]).all() and np.isfinite(got[1]).all()
+        assert (got[2, :, 7] == np.inf).all() and np.isfinite(np.delete(got[2], 7, axis=-1)).all()
+        ctx.close()
+
+
+def test_attention_sequences_share_pages():
+    """the same pages in several sequences, and twice in one"""
+    rg = np.random.default_rng(12)
+    for dtype in ("f32", "bf16"):
+        ctx, E = context(), Eager("f64")
+        cache, table = data(rg, (5, 2, 2, 16, 64), dtype), ints([[3, 1, 4], [3, 1, 0], [3, 3, 3]])
+        q, lens = data(rg, (3, 4, 64), dtype), [47, 33, 40]
+        args = lambda B: [B.tensor(q, dtype), B.tensor(cache, dtype), B.tensor(ints(lens)), B.tensor(table)]     # noqa: E731
+        compare_attention(ctx.fetch(ctx.paged_attention(*args(ctx))), E.fetch(E.paged_attention(*args(E))), q, cache, lens, table, dtype)
+        ctx.close()
+
+
+def test_queries_keys_and_values_of_one_projection():
+    """windows of heads, read where they lie, also off 16 bytes"""
+    rg = np.random.default_rng(13)
+    for dtype, dim in (("bf16", 64), ("bf16", 20), ("f32", 10), ("bf16", 9)):
+        r = Rotary(dims=8)
+        ctx, E = context(), Eager("f64")
+        lens = [9, 1, 40]
+        cache, table = paged_case(rg, lens, 2, 16, dim, dtype)
+        x = data(rg, (3, 7, dim), dtype)
+
+        def run(B):
+            X = B.tensor(x, dtype)
+            q, k, v = B.narrow(X, 1, 1, 2), B.narrow(X, 1, 3, 2), B.narrow(X, 1, 5, 2)
+            L, T, C = B.tensor(ints(lens)), B.tensor(table), B.tensor(cache, dtype, donatable=True)
+            B.assign(C, B.cache_append(C, k, v, L, T, rotary=r))
+            return C, B.paged_attention(q, C, L, T)
+        (C, o), (Cr, orf) = run(ctx), run(E)
+        got, held = ctx.fetch(o), ctx.fetch(C)
+        assert " EW " not in ctx.dump_plan()
+        # (over the keys as the cache holds them)
+        ref = E.fetch(E.paged_attention(E.narrow(E.tensor(x, dtype), 1, 1, 2), E.tensor(held, dtype), E.tensor(ints(lens)), E.tensor(table)))
+        assert np.abs(held - E.fetch(Cr)).max() <= 6 * E24 * 2 * np.abs(x).max() + HALF[dtype] * np.abs(x).max() * 2
+        compare_attention(got, ref, x[:, 1:3], held, lens, table, dtype)
+        ctx.close()
+
+
+# ---- as they are used -------------------------------------------------------------------------------
+def test_operands_of_no_size():
+    ctx = context()
+    z = lambda shape, dtype="f32": ctx.from_device(ctx._workspace.data_ptr() + (200 << 20), dtype, shape)     # noqa: E731
+    assert ctx.fetch(ctx.rope(z((0, 3, 8)), z((0,), "s32"))).shape == (0, 3, 8)
+    assert ctx.fetch(ctx.rope(z((5, 0, 8)), ctx.tensor(ints(range(5))))).shape == (5, 0, 8)
+    rg = np.random.default_rng(14)
+    for seqs, slots, pages in ((0, 3, 4), (2, 0, 4), (2, 3, 0)):
+        q, k = (ctx.tensor(data(rg, (seqs, 2, 8), "f32")) if seqs else z((seqs, 2, 8)) for _ in range(2))
+        c = data(rg, (pages, 2, 2, 4, 8), "f32")
+        cache = ctx.tensor(c, donatable=True) if pages else z(c.shape)
+        lens, table = ctx.tensor(ints([3] * seqs)) if seqs else z((0,), "s32"), ctx.tensor(np.zeros((seqs, slots), np.int32)) if seqs * slots else z((seqs, slots), "s32")
+        new = ctx.cache_append(cache, k, k, lens, table)
+        o = ctx.paged_attention(q, cache, lens, table)
+        assert np.array_equal(ctx.fetch(new), c) and not ctx.fetch(o).any()
+    ctx.close()
+
+
+class Decoder:
+    """A layer's cache in use: prompts in, then token by token, against attention over the whole sequence in 64 bits."""
+
+    def __init__(self, ctx, dtype, rg, seqs=5, heads=6, kv=2, dim=32, rows=16, longest=90):
+        self.ctx, self.dtype, self.rg, self.r = ctx, dtype, rg, Rotary(dims=24, factor=2.0)
+        self.shape = seqs, heads, kv, dim
+        self.q, self.k, self.v = (data(rg, (seqs, longest, h, dim), dtype) for h in (heads, kv, kv))
+        cache, table = paged_case(rg, [longest] * seqs, kv, rows, dim, dtype, fill=np.nan)
+        dev = lambda a: torch.from_numpy(np.ascontiguousarray(a)).to("cuda:0")     # noqa: E731
+        self.tcache, self.tlens = dev(cache).to(torch.bfloat16 if dtype == "bf16" else torch.float32), dev(np.zeros(seqs, np.int32))
+        cache[:] = np.nan
+        self.tcache.fill_(float("nan"))
+        self.C, self.L, self.T, self.table = ctx.tensor(self.tcache, donatable=True), ctx.tensor(self.tlens), ctx.tensor(table), table
+        self.at = np.zeros(seqs, np.int32)
+
+    def prompt(self, news):
+        ctx = self.ctx
+        rows = [np.concatenate([z[s, :n] for s, n in enumerate(news)] + [z[0, :3]]) for z in (self.k, self.v)]
+        self.at += ints(news)
+        self.tlens.copy_(torch.from_numpy(self.at))
+        ctx.assign(self.C, ctx.cache_append(self.C, ctx.tensor(rows[0], self.dtype), ctx.tensor(rows[1], self.dtype), self.L, self.T,
+                                            offsets=ctx.tensor(ints(np.concatenate([[0], np.cumsum(news)]))), rotary=self.r))
+        ctx.barrier()
+
+    def next(self):
+        """the next token's q, k, v of every sequence, on the device; lengths move on"""
+        self.at += 1
+        pick = lambda z: torch.from_numpy(np.stack([z[s, n - 1] for s, n in enumerate(self.at)])).to("cuda:0").to(self.tcache.dtype)     # noqa: E731
+        self.tlens.copy_(torch.from_numpy(self.at))
+        return pick(self.q), pick(self.k), pick(self.v), torch.from_numpy(self.at - 1).to("cuda:0")
+
+    def record(self, q, k, v, p):
+        ctx = self.ctx
+        ctx.assign(self.C, ctx.cache_append(self.C, k, v, self.L, self.T, rotary=self.r))
+        return ctx.paged_attention(ctx.rope(q, p, self.r), self.C, self.L, self.T)
+
+    def expected(self):
+        E = Eager("f64")
+        out = []
+        for s, n in enumerate(self.at):
+            pos = E.tensor(np.arange(n, dtype=np.int32))
+            rot = lambda z: E.fetch(E.rope(E.tensor(z[s, :n], self.dtype), pos, self.r))     # noqa: E731,B023
+            q, k = rot(self.q)[-1], rot(self.k)
+            if self.dtype == "bf16":     # the query and the cache hold rounded values
+                q, k = round_to_bf16(q.astype(np.float32)).astype(np.float64), round_to_bf16(k.astype(np.float32)).astype(np.float64)
+            g = self.shape[1] // self.shape[2]
+            sc = np.einsum("hd,nhd->hn", q, np.repeat(k, g, 1)) / math.sqrt(self.shape[3])
+            e = np.exp(sc - sc.max(-1, keepdims=True))
+            out.append(np.einsum("hn,nhd->hd", e / e.sum(-1, keepdims=True), np.repeat(self.v[s, :n].astype(np.float64), g, 1)))
+        return np.stack(out)
+
+    def check(self, got):
+        ref = self.expected()
+        # beyond attention's own bound (2^-8 twice in bf16, scores below 16): a rotated value near a tie may round the other way,
+        # one step (2 R) of a product in a sum of 32, which moves a score of magnitude 16 by 2 R * 16 / 32 * 4 at most
+        tol = {"bf16": 2 * HALF["bf16"] + 4 * HALF["bf16"], "f32": 2 ** 11 * E24}[self.dtype]
+        assert np.abs(got - ref).max() <= tol * np.abs(self.v).max(), np.abs(got - ref).max() / np.abs(self.v).max()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("graphs", [False, True])
+def test_decoding_step_by_step(dtype, graphs):
+    ctx = context()
+    ctx.set_graphs(graphs)
+    d = Decoder(ctx, dtype, np.random.default_rng(15))
+    d.prompt([17, 1, 0, 60, 33])
+    for _ in range(12):
+        o = d.record(*(ctx.tensor(t) for t in d.next()))
+        d.check(ctx.fetch(o))
+        assert "->p" in ctx.dump_plan()
+        del o
+    ctx.close()
+
+
+@pytest.mark.parametrize("graphs", [False, True])
+def test_decoding_replays_a_captured_step(graphs):
+    ctx = context()
+    ctx.set_graphs(graphs)
+    d = Decoder(ctx, "bf16", np.random.default_rng(16))
+    d.prompt([17, 1, 2, 60, 33])
+    fixed = [t.clone() for t in d.next()]
+    held = [ctx.tensor(t) for t in fixed]
+    o = d.record(*held)
+    ctx.barrier()
+    d.check(ctx.fetch(o))
+    step = ctx.capture_step()
+    for i in range(14):
+        for dst, src in zip(fixed, d.next()):
+            dst.copy_(src)
+        if i % 5 == 3:                       # the program's own work between the replays
+            torch.randn(1 << 20, device="cuda:0").sum()
+            torch.cuda.synchronize()
+        step.replay()
+        d.check(ctx.fetch(o))
+    assert not graphs or ctx.stats().graph_launches > 3
+    ctx.close()
+
+
+def test_decoding_through_the_static_barrier():
+    ctx = context()
+    d = Decoder(ctx, "bf16", np.random.default_rng(17))
+    d.prompt([17, 1, 2, 60, 33])
+    for _ in range(3):
+        o = d.record(*(ctx.tensor(t) for t in d.next()))
+        ctx.barrier_static()
+        d.check(ctx.fetch(o))
+    ctx.close()
+
+
+def test_two_contexts_on_streams_of_their_own():
+    rg = np.random.default_rng(18)
+    streams = [torch.cuda.Stream(device=0) for _ in range(2)]
+    ctxs = [context(stream=s) for s in streams]
+    ds = [Decoder(c, "bf16", rg, longest=400 + 100 * i) for i, c in enumerate(ctxs)]
+    for d in ds:
+        d.prompt([300, 1, 2, 350, 33])
+    torch.cuda.synchronize()
+    for _ in range(4):
+        outs, ins = [], []
+        for d in ds:
+            ins.append(d.next())
+        torch.cuda.synchronize()
+        for c, d, t in zip(ctxs, ds, ins):
+            outs.append(d.record(*(c.tensor(x) for x in t)))
+            c.barrier(False)
+        for c, d, o in zip(ctxs, ds, outs):
+            d.check(c.fetch(o))
+    for c in ctxs:
+        c.close()
+
+
+def test_runs_of_the_same_step_are_the_same_bits():
+    rg = np.random.default_rng(19)
+    ctx = context()
+    lens = [5000, 1, 300, 0, 2200]
+    for dtype, rows in (("bf16", 16), ("f32", 10)):
+        cache, table = paged_case(rg, lens, 2, rows, 64, dtype)
+        args = [ctx.tensor(data(rg, (5, 8, 64), dtype), dtype), ctx.tensor(cache, dtype), ctx.tensor(ints(lens)), ctx.tensor(table)]
+        first = ctx.fetch(ctx.paged_attention(*args))
+        for _ in range(5):
+            assert np.array_equal(ctx.fetch(ctx.paged_attention(*args)), first)
+    ctx.close()
+
+
+def test_a_cache_longer_than_32_bits_reach():
+    """pages at the far end of a cache of 2^32 elements and more, next to the same rows in a small one"""
+    rg = np.random.default_rng(20)
+    kv, rows, dim, lens = 4, 16, 128, [70, 33]
+    small, table = paged_case(rg, lens, kv, rows, dim, "bf16", spare=0)
+    pages = (2 ** 32 // (2 * kv * rows * dim)) + 300
+    far = torch.empty((pages, 2, kv, rows, dim), dtype=torch.bfloat16, device="cuda:0")
+    shift = pages - small.shape[0]
+    far[shift:] = torch.from_numpy(small).to("cuda:0")
+    moved = np.where((table >= 0) & (table < small.shape[0]), table + shift, -1).astype(np.int32)
+    q, k, v = (data(rg, (2, h, dim), "bf16") for h in (8, kv, kv))
+    outs = []
+    for cache, tab in ((torch.from_numpy(small).to("cuda:0").to(torch.bfloat16), np.where(moved < 0, -1, table)), (far, moved)):
+        ctx = context()
+        C, L, T = ctx.tensor(cache, donatable=True), ctx.tensor(ints(lens)), ctx.tensor(ints(tab))
+        ctx.assign(C, ctx.cache_append(C, ctx.tensor(k, "bf16"), ctx.tensor(v, "bf16"), L, T, rotary=Rotary()))
+        o = ctx.fetch(ctx.paged_attention(ctx.tensor(q, "bf16"), C, L, T))
+        outs.append((o, cache[-small.shape[0]:].float().cpu().numpy()))
+        ctx.close()
+    assert np.array_equal(outs[0][0], outs[1][0]) and np.array_equal(outs[0][1], outs[1][1]) and (outs[0][1] != small).any()
+    del far
+
+
+def test_rope_of_more_than_32_bits_of_elements():
+    tokens, heads, dim = 2 ** 32 // (64 * 128) + 3, 64, 128
+    x = torch.empty((tokens, heads, dim), dtype=torch.bfloat16, device="cuda:0")
+    x[-3:] = torch.randn((3, heads, dim), device="cuda:0")
+    ctx = context(workspace_bytes=(9 << 30) + (64 << 20))
+    y = ctx.rope(ctx.tensor(x), ctx.tensor(torch.arange(tokens, dtype=torch.int32, device="cuda:0")), Rotary())
+    tail = ctx.narrow(y, 0, tokens - 3, 3)
+    small = ctx.rope(ctx.tensor(x[-3:].clone()), ctx.tensor(torch.arange(tokens - 3, tokens, dtype=torch.int32, device="cuda:0")), Rotary())
+    ctx.barrier()
+    assert np.array_equal(ctx.fetch(tail), ctx.fetch(small))
+    ctx.close()
+    del x

@@ -1,0 +1,283 @@
+"""Rotary positions and the paged cache without a GPU: what is recorded and refused, what a plan does with it (against the structural
+oracle), and the definitions in the numeric oracle against hand-typed values, differences and a plain attention."""
+import math
+
+import numpy as np
+import pytest
+
+from oracle.numeric import Eager
+from oracle.structural import Tracer
+from paper_2102_13267_amd import Context, LtError, Rotary
+from paper_2102_13267_amd.lt import ATTR_ROPE_BASE, ATTR_ROPE_DIMS, ATTR_ROPE_FACTOR, ATTR_ROPE_HIGH, ATTR_ROPE_INTERLEAVED, ATTR_ROPE_LOW, ATTR_ROPE_ORIGINAL, ATTR_SCALE
+
+ARG, SHAPE, DTYPE, UNSUPPORTED = 1, 3, 4, 5
+
+
+def zeros(B, shape, dtype="f32", donatable=False):
+    return B.tensor(np.zeros(shape, np.int32 if dtype == "s32" else np.float32), dtype=dtype, donatable=donatable)
+
+
+def paged(B, seqs=3, heads=4, kv=2, dim=8, rows=4, slots=5, pages=7, dtype="f32"):
+    return {"cache": zeros(B, (pages, 2, kv, rows, dim), dtype, True), "k": zeros(B, (seqs, kv, dim), dtype), "v": zeros(B, (seqs, kv, dim), dtype),
+            "q": zeros(B, (seqs, heads, dim), dtype), "lengths": zeros(B, (seqs,), "s32"), "table": zeros(B, (seqs, slots), "s32"), "offsets": zeros(B, (seqs + 1,), "s32")}
+
+
+def refused(status, call, *args, **kwargs):
+    with pytest.raises(LtError) as e:
+        call(*args, **kwargs)
+    assert e.value.status == status, e.value
+
+
+# ---- refusals -----------------------------------------------------------------------------------
+def test_rope_refuses_what_it_does_not_take():
+    c = Context()
+    x, p = zeros(c, (5, 3, 8)), zeros(c, (5,), "s32")
+    for call in (c.rope, c.rope_grad):
+        refused(DTYPE, call, zeros(c, (5, 3, 8), "s32"), p)
+        refused(DTYPE, call, x, zeros(c, (5,)))
+        refused(DTYPE, call, x, c.tensor(np.zeros(5, np.int64)))
+        refused(SHAPE, call, zeros(c, (5, 8)), p)
+        refused(SHAPE, call, x, zeros(c, (4,), "s32"))
+        refused(SHAPE, call, x, zeros(c, (5, 3), "s32"))
+        refused(SHAPE, call, x, c.scalar(1, "s32"))
+        refused(SHAPE, call, zeros(c, (2, 5, 3, 8)), zeros(c, (2,), "s32"))      # (the first axis alone is no suffix)
+        for bad in (Rotary(dims=3), Rotary(dims=0), Rotary(dims=-2), Rotary(dims=10), Rotary(base=0.5), Rotary(base=math.nan), Rotary(base=math.inf), Rotary(factor=0.9),
+                    Rotary(factor=math.inf), Rotary(original=-1.0), Rotary(low=2.0, high=2.0), Rotary(low=-1.0), Rotary(amplitude=math.inf), Rotary(amplitude=1e39)):
+            refused(ARG, call, x, p, bad)
+        refused(ARG, call, zeros(c, (5, 3, 7)), p)                               # an odd head has to say which part of it turns
+        call(zeros(c, (5, 3, 7)), p, Rotary(dims=6))
+        refused(ARG, call, zeros(c, (5, 3, 258)), p)
+        call(zeros(c, (5, 3, 258)), p, Rotary(dims=256))
+    refused(ARG, c.op, "rope", (x, p), [(ATTR_ROPE_INTERLEAVED, 2)])
+    refused(ARG, c.op, "rope", (x, p), [(ATTR_ROPE_DIMS, 4.0)])
+    refused(ARG, c.op, "rope", (x,))
+    refused(ARG, c.op, "rope", (x, p, p))
+    assert c.rope(x, p).shape == (5, 3, 8) and c.rope(zeros(c, (2, 5, 3, 8), "bf16"), p).dtype == "bf16"
+
+
+def test_cache_append_refuses_what_it_does_not_take():
+    c = Context()
+    t = paged(c)
+    ok = lambda **o: c.cache_append(*({**t, **o}[k] for k in ("cache", "k", "v", "lengths", "table")), offsets=o.get("offsets"), rotary=o.get("rotary"))     # noqa: E731
+    ok()
+    ok(offsets=t["offsets"], k=zeros(c, (9, 2, 8)), v=zeros(c, (9, 2, 8)), rotary=Rotary())
+    ok(k=zeros(c, (3, 2, 8), "bf16"), v=zeros(c, (3, 2, 8), "bf16"))
+    refused(DTYPE, ok, cache=zeros(c, (7, 2, 2, 4, 8), "s32"))
+    refused(DTYPE, ok, k=zeros(c, (3, 2, 8), "bf16"))
+    refused(DTYPE, ok, k=zeros(c, (3, 2, 8), "s32"), v=zeros(c, (3, 2, 8), "s32"))
+    refused(DTYPE, ok, lengths=zeros(c, (3,)))
+    refused(DTYPE, ok, table=zeros(c, (3, 5)))
+    refused(DTYPE, ok, offsets=zeros(c, (4,)))
+    for shape in ((7, 2, 2, 4), (7, 1, 2, 4, 8), (7, 2, 0, 4, 8), (7, 2, 2, 0, 8), (7, 2, 2, 4, 0)):
+        refused(SHAPE, ok, cache=zeros(c, shape))
+    refused(SHAPE, ok, k=zeros(c, (3, 3, 8)), v=zeros(c, (3, 3, 8)))
+    refused(SHAPE, ok, k=zeros(c, (3, 2, 9)), v=zeros(c, (3, 2, 9)))
+    refused(SHAPE, ok, v=zeros(c, (4, 2, 8)))
+    refused(SHAPE, ok, k=zeros(c, (4, 2, 8)), v=zeros(c, (4, 2, 8)))             # without offsets: a token a sequence
+    refused(SHAPE, ok, offsets=zeros(c, (3,), "s32"))
+    refused(SHAPE, ok, lengths=zeros(c, (2,), "s32"))
+    refused(SHAPE, ok, table=zeros(c, (15,), "s32"))
+    refused(ARG, ok, rotary=Rotary(dims=16))
+    refused(ARG, c.op, "cache_append", (t["cache"], t["k"], t["v"], t["lengths"]))
+    many = 1 << 30                                                                # (nothing is allocated on the null device)
+    refused(SHAPE, ok, table=c.from_device(0, "s32", (3, many)))
+    refused(SHAPE, ok, cache=c.from_device(0, "f32", (many, 2, 2, 4, 8)))
+
+
+def test_paged_attention_refuses_what_it_does_not_take():
+    c = Context()
+    t = paged(c)
+    ok = lambda **o: c.paged_attention(*({**t, **o}[k] for k in ("q", "cache", "lengths", "table")), scale=o.get("scale"))     # noqa: E731
+    assert ok().shape == (3, 4, 8) and ok(scale=0.0).dtype == "f32"
+    refused(DTYPE, ok, q=zeros(c, (3, 4, 8), "bf16"))
+    refused(DTYPE, ok, lengths=zeros(c, (3,)))
+    refused(SHAPE, ok, q=zeros(c, (3, 3, 8)))
+    refused(SHAPE, ok, q=zeros(c, (3, 0, 8)))
+    refused(SHAPE, ok, q=zeros(c, (2, 4, 8)))
+    refused(SHAPE, ok, q=zeros(c, (3, 4, 9)))
+    refused(SHAPE, ok, q=zeros(c, (3, 4, 257)), cache=zeros(c, (7, 2, 2, 4, 257)))
+    refused(ARG, ok, scale=math.inf)
+    refused(ARG, ok, scale=1e39)
+    refused(ARG, c.op, "paged_attention", (t["q"], t["cache"], t["lengths"]))
+
+
+def test_operands_that_have_no_memory_or_no_strides_are_refused_at_the_barrier():
+    for build in (lambda c, t: c.rope(c.expand(c.scalar(2.0), (3, 2, 8)), t["lengths"]), lambda c, t: c.rope(t["k"], c.expand(c.scalar(2, "s32"), (3,))),
+                  lambda c, t: c.rope(c.expand(zeros(c, (3, 2, 1)), (3, 2, 8)), t["lengths"]),
+                  lambda c, t: c.paged_attention(t["q"], t["cache"], t["lengths"], c.expand(zeros(c, (3, 1), "s32"), (3, 5)))):
+        c = Context()
+        t = paged(c)
+        out = build(c, t)      # noqa: F841
+        refused(UNSUPPORTED, c.barrier)
+
+
+# ---- recording and plans, against the structural oracle ---------------------------------------------
+ROT = Rotary(dims=6, interleaved=True, factor=4.0, original=100.0)
+
+
+def decode(B):
+    t = paged(B)
+    B.assign(t["cache"], B.cache_append(t["cache"], t["k"], t["v"], t["lengths"], t["table"], rotary=ROT))
+    return t, B.paged_attention(B.rope(t["q"], t["lengths"], ROT), t["cache"], t["lengths"], t["table"])
+
+
+def windows(B):
+    """queries, keys and values of one projection, as windows of heads"""
+    t = paged(B)
+    qkv = B.reshape(B.matmul(zeros(B, (3, 16)), zeros(B, (16, 64))), (3, 8, 8))
+    q, k, v = B.narrow(qkv, 1, 0, 4), B.narrow(qkv, 1, 4, 2), B.narrow(qkv, 1, 6, 2)
+    cache = B.cache_append(t["cache"], k, v, t["lengths"], t["table"], offsets=t["offsets"], rotary=ROT)
+    B.assign(t["cache"], cache)
+    return t, B.paged_attention(B.rope(q, t["lengths"]) if isinstance(B, Context) else B.rope(q, t["lengths"], Rotary()), t["cache"], t["lengths"], t["table"], scale=0.5)
+
+
+def copies(B):
+    """windows that an operator cannot read where they lie, and a cache that somebody still reads"""
+    x = zeros(B, (6, 5, 4, 8))
+    a = B.rope(B.narrow(x, 1, 1, 3), zeros(B, (3,), "s32"), ROT)
+    b = B.rope_grad(B.narrow(x, 0, 1, 3), zeros(B, (3, 5), "s32"), ROT)
+    t = paged(B)
+    new = B.cache_append(t["cache"], t["k"], t["v"], t["lengths"], t["table"])
+    return t, a, b, new, B.add(new, t["cache"]), B.permute(B.rope(B.permute(x, (0, 2, 1, 3)), zeros(B, (6, 4), "s32"), ROT), (0, 2, 1, 3))
+
+
+def own_rows(B):
+    """keys that are the cache's own memory are never written in place"""
+    t = paged(B, seqs=7)
+    k = B.narrow(B.reshape(t["cache"], (56, 2, 8)), 0, 3, 7)
+    B.assign(t["cache"], B.cache_append(t["cache"], k, t["v"], t["lengths"], t["table"]))
+    return t
+
+
+@pytest.mark.parametrize("program", [decode, windows, copies, own_rows])
+def test_plans_equal_the_structural_oracles(program):
+    ctx, ref = Context(), Tracer()
+    keep = program(ctx), program(ref)
+    for _ in range(2):
+        info, want = ctx.barrier(), ref.barrier()
+        assert info.hash == want["hash"] and ctx.dump_plan() == want["plan"]
+        keep = (program(ctx), program(ref), keep)
+
+
+def test_new_rows_are_written_in_place_and_read_behind_that():
+    c = Context()
+    t, o = decode(c)      # noqa: F841
+    c.barrier()
+    plan, sched = c.dump_plan(), c.dump_schedule()
+    assert "->p" in plan and plan.count(" OP ") == 3 and sorted(line.split()[1] for line in sched.splitlines()) == ["APPEND", "PAGED", "ROPE"]
+    append = next(line for line in sched.splitlines() if " APPEND " in line)
+    wrote = append.split("writes=[")[1].split("]")[0]
+    assert wrote.startswith("p") and wrote in next(line for line in sched.splitlines() if " PAGED " in line).split("reads=[")[1].split("]")[0].split(",")
+
+
+def test_a_cache_whose_own_rows_are_appended_is_copied():
+    c = Context()
+    t = own_rows(c)      # noqa: F841
+    c.barrier()
+    assert "->p" not in c.dump_plan()
+
+
+def test_windows_of_heads_are_read_where_they_lie():
+    c = Context()
+    keep = windows(c)     # noqa: F841
+    c.barrier()
+    assert " EW " not in c.dump_plan()
+
+
+def test_a_rotation_is_part_of_the_key_and_its_defaults_are_filled_in():
+    c = Context()
+    x, p = zeros(c, (5, 3, 8)), zeros(c, (5,), "s32")
+    hashes = []
+    for r in (Rotary(), Rotary(dims=8), Rotary(dims=6), Rotary(interleaved=True), Rotary(factor=2.0), Rotary(amplitude=0.5), Rotary(base=5000.0)):
+        y = c.rope(x, p, r)
+        hashes.append(c.barrier().hash)
+        del y
+    assert hashes[0] == hashes[1] and len(set(hashes)) == len(hashes) - 1
+    y = c.op("rope", (x, p))
+    assert c.barrier().hash == hashes[0]
+    y = c.op("rope", (x, p), [(ATTR_ROPE_BASE, 10000), (ATTR_ROPE_FACTOR, 1), (ATTR_ROPE_ORIGINAL, 0), (ATTR_ROPE_LOW, 1), (ATTR_ROPE_HIGH, 32)])   # integers where reals are meant
+    assert c.barrier().hash == hashes[0]
+    t = paged(c)
+    y = c.paged_attention(t["q"], t["cache"], t["lengths"], t["table"])      # noqa: F841
+    h = c.barrier().hash
+    y = c.op("paged_attention", (t["q"], t["cache"], t["lengths"], t["table"]), [(ATTR_SCALE, 1.0 / math.sqrt(8))])      # noqa: F841
+    assert c.barrier().hash == h
+
+
+def test_sizes_of_nothing_are_planned():
+    c = Context()
+    keep = [c.rope(zeros(c, (0, 3, 8)), zeros(c, (0,), "s32")), c.rope(zeros(c, (5, 0, 8)), zeros(c, (5,), "s32"))]
+    for kw in ({"seqs": 0}, {"slots": 0}, {"pages": 0}):
+        t = paged(c, **kw)
+        c.assign(t["cache"], c.cache_append(t["cache"], t["k"], t["v"], t["lengths"], t["table"]))
+        keep += [t, c.paged_attention(t["q"], t["cache"], t["lengths"], t["table"])]
+    c.barrier()
+
+
+# ---- the definitions ------------------------------------------------------------------------------
+def test_rotations_by_hand():
+    E = Eager("f64")
+    x = E.tensor(np.array([[[1.0, 0.0, 2.0, 0.0, 5.0]], [[0.0, 1.0, 0.0, 2.0, 5.0]]]))
+    p = E.tensor(np.array([1, 2], np.int32))
+    f = [1.0, 10000.0 ** -0.5]
+    half = E.fetch(E.rope(x, p, Rotary(dims=4, amplitude=3.0)))
+    c, s = np.cos, np.sin
+    a, b = f[0], 2 * f[1]
+    assert np.allclose(half[0, 0], [3 * (c(a) - 2 * s(a)), 0, 3 * (2 * c(a) + s(a)), 0, 5])
+    assert np.allclose(half[1, 0], [0, 3 * (c(b) - 2 * s(b)), 0, 3 * (2 * c(b) + s(b)), 5])
+    il = E.fetch(E.rope(x, p, Rotary(dims=4, interleaved=True)))
+    assert np.allclose(il[0, 0], [c(f[0]), s(f[0]), 2 * c(f[1]), 2 * s(f[1]), 5])
+    assert np.allclose(il[1, 0], [-s(2 * f[0]), c(2 * f[0]), -2 * s(2 * f[1]), 2 * c(2 * f[1]), 5])
+
+
+def test_frequencies_for_long_contexts():
+    ang = lambda r: Eager._angles(np.array([1.0]), r, 8)[0][0]      # noqa: E731
+    plain = ang(Rotary())
+    assert np.allclose(ang(Rotary(factor=4.0)), plain / 4)
+    turns = 1000.0 * plain / (2 * math.pi)                       # 159, 15.9, 1.59, 0.159
+    keep = np.clip((turns - 1) / 31, 0, 1)
+    assert keep[0] == 1 and 0 < keep[1] < 1 and 0 < keep[2] < 1 and keep[3] == 0
+    assert np.allclose(ang(Rotary(factor=4.0, original=1000.0)), plain * (keep + (1 - keep) / 4))
+
+
+def test_the_gradient_against_differences():
+    rg = np.random.default_rng(3)
+    E, h = Eager("f64"), 1e-6
+    for r in (Rotary(dims=6, amplitude=1.3), Rotary(interleaved=True, factor=2.0)):
+        x, dy, p = rg.standard_normal((2, 3, 2, 8)), rg.standard_normal((2, 3, 2, 8)), E.tensor(np.array([7, -4, 100000], np.int32))
+        run = lambda v: E.fetch(E.rope(E.tensor(v), p, r))       # noqa: E731,B023
+        dx = E.fetch(E.rope_grad(E.tensor(dy), p, r))
+        for _ in range(20):
+            d = rg.standard_normal(x.shape)
+            assert abs(((run(x + h * d) - run(x - h * d)) / (2 * h) * dy).sum() - (dx * d).sum()) < 1e-6
+
+
+def test_decoding_is_causal_attention():
+    """Prompts, then token by token, against attention over the whole sequence at once."""
+    rg = np.random.default_rng(5)
+    E, S, H, KV, D, rows = Eager("f64"), 3, 4, 2, 6, 4
+    r, news = Rotary(dims=4), [[5, 1, 1], [1, 1, 1], [0, 9, 1]]
+    total = [sum(n) for n in news]
+    q, k, v = (rg.standard_normal((S, max(total), h, D)) for h in (H, KV, KV))
+    table = E.tensor(np.array([[2, 5, 0], [7, -1, -1], [1, 4, 9]], np.int32))
+    cache = E.tensor(np.full((10, 2, KV, rows, D), np.nan))
+    at = np.zeros(S, int)
+    for step in range(3):
+        n = np.array([news[s][step] for s in range(S)])
+        off = np.concatenate([[0], np.cumsum(n)])
+        kk, vv = (np.concatenate([z[s, at[s]:at[s] + n[s]] for s in range(S)] + [np.ones((2, KV, D))]) for z in (k, v))    # (two rows behind the last sequence)
+        at += n
+        lengths = E.tensor(at.astype(np.int32))
+        cache = E.cache_append(cache, E.tensor(kk), E.tensor(vv), lengths, table, offsets=E.tensor(off.astype(np.int32)), rotary=r)
+        last = E.tensor(np.stack([q[s, max(at[s] - 1, 0)] for s in range(S)]))
+        got = E.fetch(E.paged_attention(E.rope(last, E.tensor((at - 1).astype(np.int32)), r), cache, lengths, table))
+        for s in range(S):
+            if at[s] == 0:
+                assert not got[s].any()
+                continue
+            pos = E.tensor(np.arange(at[s], dtype=np.int32))
+            kr = E.fetch(E.rope(E.tensor(k[s, :at[s]]), pos, r))
+            qr = E.fetch(E.rope(E.tensor(q[s, :at[s]]), pos, r))[-1]
+            for h in range(H):
+                e = np.exp(kr[:, h // 2] @ qr[h] / math.sqrt(D))
+                assert np.allclose(got[s, h], e @ v[s, :at[s], h // 2] / e.sum())
