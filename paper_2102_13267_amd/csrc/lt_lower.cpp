@@ -1900,6 +1900,8 @@ struct Lowering {
     args.scale = (float)an->attrs[0].v.f;
     args.q_seq = q.s_inner;
     args.q_head = q.s_head;
+    args.share_out();
+    if ((uint64_t)args.seqs * args.pairs >= ((uint64_t)1 << 31)) return bad(LT_ERR_UNSUPPORTED, "paged_attention: 2^31 or more blocks of query heads");
     Launch l = make_launch(L_PAGED, k, args);
     // (how long the sequences are is known on the device alone: as if every page were read once)
     const uint64_t held = (uint64_t)count(cs), w = dtype_size(an->dtype);
@@ -1911,6 +1913,13 @@ struct Lowering {
     patch(launch, offsetof(ltk::PagedArgs, lengths), s[1], o[1]);
     patch(launch, offsetof(ltk::PagedArgs, table), s[2], o[2]);
     patch(launch, offsetof(ltk::PagedArgs, out), storage_of[a][0], 0, true);
+    if (args.split) {   // two parts a workgroup: of the sequence it begins in, and of the one it ends in
+      Storage parts;
+      parts.first_launch = -1;
+      parts.bytes = 2 * (size_t)args.workgroups * args.part_floats() * sizeof(float);
+      plan->storages.push_back(parts);
+      patch(launch, offsetof(ltk::PagedArgs, parts), (int32_t)plan->storages.size() - 1, 0, true);
+    }
     return true;
   }
 

@@ -98,63 +98,510 @@ hipError_t launch_append(const void* args, hipStream_t s) {
 }
 
 // ---- attention of one new token -------------------------------------------------------------------
-// One workgroup per sequence and query head; its four waves take every fourth key each, a lane four elements of the
-// head, with a running maximum and sum; the waves' parts meet in LDS.
-template <typename T>
-__global__ __launch_bounds__(kBlock) void lt_paged_attention_kernel(const PagedArgs a) {
-  const uint32_t s = blockIdx.x / a.heads, h = blockIdx.x % a.heads, kh = h / (a.heads / a.kv_heads);
-  const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
-  int64_t len = a.lengths[s];
-  len = len < 0 ? 0 : len > (int64_t)a.capacity ? (int64_t)a.capacity : len;
-  const T* q = (const T*)a.q + (int64_t)s * a.q_seq + (int64_t)h * a.q_head;
-  const float scale = a.scale * kLog2e;
-  float qv[4], acc[4] = {0, 0, 0, 0}, top = -INFINITY, sum = 0.0f;
-  for (uint32_t i = 0; i < 4u; ++i) qv[i] = lane + 64u * i < a.dim ? to_float(q[lane + 64u * i]) : 0.0f;
-  for (uint32_t p = wave; p < (uint32_t)len; p += 4u) {
-    const uint32_t slot = divide(a.rows, p);
-    const int32_t page = a.table[(uint64_t)s * a.slots + slot];
-    if (page < 0 || (uint32_t)page >= a.pages) continue;
-    const T* k = (const T*)a.cache + (((uint64_t)page * 2u * a.kv_heads + kh) * a.rows.d + (p - slot * a.rows.d)) * a.dim;
-    const T* v = k + (uint64_t)a.kv_heads * a.rows.d * a.dim;
-    float dot = 0.0f;
-    for (uint32_t i = 0; i < 4u; ++i)
-      if (lane + 64u * i < a.dim) dot = fmaf(qv[i], to_float(k[lane + 64u * i]), dot);
-    for (int m = 32; m >= 1; m >>= 1) dot += __shfl_xor(dot, m, 64);
-    dot *= scale;
-    const float t = fmaxf(top, dot), safe = t == -INFINITY ? 0.0f : t;
-    const float keep = exp2f(top - safe), w = exp2f(dot - safe);
-    top = t;
-    sum = fmaf(sum, keep, w);
-    for (uint32_t i = 0; i < 4u; ++i)
-      if (lane + 64u * i < a.dim) acc[i] = fmaf(acc[i], keep, w * to_float(v[lane + 64u * i]));
+// Every key and value is read once, for all query heads of its key head together: what bounds it is memory, so that the arithmetic is
+// given to the matrix cores, where sixteen heads cost what one does, and nothing goes through LDS on its way there.
+//
+// A wave takes steps of WK keys (bf16 32, fp32 16).  Scores transposed, s = K q^T (MFMA 16x16: A 16 keys, B 16 query heads, which stay in
+// registers): lane (n, g), n = lane & 15, g = lane / 16, reads 16-byte pieces of key n's row, and of the result holds keys
+// 4 g .. 4 g + 3 of a tile for head n.  So a head's maximum is a maximum over registers and two exchanges between lanes, and o = V^T p takes
+// the weights as they lie: which key an MFMA's k stands for is free as long as both operands agree, so lane (n, g) holds in B what it
+// computed and reads for A the rows of the same keys, 1 / 16 of a row of dim elements each (bf16: two rows' halves are put together by
+// v_perm_b32).  The accumulator has head n in lane n, so that rescaling by a new maximum is a product in place.  K of the
+// next step is on its way while this one's weights are computed, V of this one too.
+//
+// Four waves share a tile of 4 WK keys; their maxima, sums and products meet in LDS at a segment's end.
+template <typename T, int DP, int NH> struct Geo {
+  static constexpr bool BF = sizeof(T) == 2;
+  static constexpr int KT = BF ? 2 : 1;              // tiles of 16 keys in a wave's step
+  static constexpr int WK = 16 * KT, TILE = 4 * WK;
+  static constexpr int CE = 16 / (int)sizeof(T);     // elements of 16 bytes
+  static constexpr int NC = DP / (4 * CE);           // 16-byte pieces of a key's row per lane
+  static constexpr int NV = DP / 16;                 // elements of a value's row per lane
+  static constexpr int VB = NV * (int)sizeof(T) < 16 ? NV * (int)sizeof(T) : 16;   // bytes of a piece of it,
+  static constexpr int NP = NV * (int)sizeof(T) / VB;                               // and their number
+  static constexpr int PITCH = DP + 4;
+};
+
+typedef uint32_t U4 __attribute__((ext_vector_type(4)));
+typedef float F4 __attribute__((ext_vector_type(4)));
+typedef __bf16 B8 __attribute__((ext_vector_type(8)));
+
+constexpr int kSlots = 1024;   // page numbers of a stretch of a sequence that a workgroup holds
+
+// BYTES of a row from element d on, in pieces of AL bytes; pieces behind the row's end are read from `other`.
+template <typename T, int BYTES, int AL>
+__device__ __forceinline__ U4 load_piece(const T* row, uint32_t d, uint32_t dim, const T* other) {
+  U4 r = {0u, 0u, 0u, 0u};
+  if constexpr (AL >= BYTES) {
+    const T* p = d < dim ? row + d : other;
+    if constexpr (BYTES == 16) r = *(const U4*)p;
+    else if constexpr (BYTES == 8) {
+      const uint2 t = *(const uint2*)p;
+      r.x = t.x;
+      r.y = t.y;
+    } else r.x = *(const uint32_t*)p;
+  } else {
+#pragma unroll
+    for (int i = 0; i < BYTES / AL; ++i) {
+      const uint32_t e = d + (uint32_t)(i * AL / (int)sizeof(T));
+      const T* p = e < dim ? row + e : other;
+      if constexpr (AL == 4) r[i] = *(const uint32_t*)p;
+      else r[i / 2] |= (uint32_t)*(const uint16_t*)p << (16 * (i & 1));
+    }
   }
-  __shared__ float tops[4], sums[4], parts[4][256];
-  for (uint32_t i = 0; i < 4u; ++i) parts[wave][lane + 64u * i] = acc[i];
-  if (lane == 0u) {
-    tops[wave] = top;
-    sums[wave] = sum;
+  return r;
+}
+
+// What is read in place of the elements behind a head's last one: they count nothing, next to infinities too.
+__device__ __attribute__((aligned(16))) const uint32_t zeros[4] = {0u, 0u, 0u, 0u};
+
+__device__ __forceinline__ float max_over_groups(float v) {
+  v = fmaxf(v, __shfl_xor(v, 16, 64));
+  return fmaxf(v, __shfl_xor(v, 32, 64));
+}
+__device__ __forceinline__ float sum_over_groups(float v) {
+  v += __shfl_xor(v, 16, 64);
+  return v + __shfl_xor(v, 32, 64);
+}
+__device__ __forceinline__ float power2(float v) { return __builtin_amdgcn_exp2f(v); }
+
+__device__ __forceinline__ uint32_t length_of(const PagedArgs& a, uint32_t s) {
+  const int32_t n = a.lengths[s];
+  return n < 0 ? 0u : (uint32_t)n > a.capacity ? a.capacity : (uint32_t)n;
+}
+
+// Tiles of a sequence, one at least: an empty one has zeros to write.
+__device__ __forceinline__ uint32_t tiles_of(const PagedArgs& a, uint32_t len) { return len == 0u ? 1u : (len - 1u) / a.tile + 1u; }
+
+// The tiles of all sequences in a row (sequence by sequence, and in each key head by key head, blocks of 16 NH query heads apart)
+// are dealt out evenly: workgroup w has `per` of them from w * per on.  Found by the block together: the sequence
+// that `at` falls into, how many tiles come before it, and `per`.
+struct Deal {
+  uint64_t per, before;
+  uint32_t seq;
+};
+__device__ __forceinline__ Deal deal(const PagedArgs& a, uint64_t (*shared)[8], uint64_t at_workgroup, uint32_t of_sequence) {
+  const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, each = (a.seqs + kBlock - 1u) / kBlock, from = threadIdx.x * each;
+  uint64_t mine = 0;
+  for (uint32_t i = 0; i < each; ++i)
+    if (from + i < a.seqs) mine += tiles_of(a, length_of(a, from + i));
+  uint64_t up = mine;   // inclusive sums over the wave, then over the waves
+  for (int m = 1; m < 64; m <<= 1) {
+    const uint64_t t = __shfl_up(up, m, 64);
+    if ((int)lane >= m) up += t;
+  }
+  if (lane == 63u) shared[0][wave] = up;
+  __syncthreads();
+  uint64_t total = 0, below = up - mine;
+  for (uint32_t w = 0; w < kBlock / 64u; ++w) {
+    if (w < wave) below += shared[0][w];
+    total += shared[0][w];
+  }
+  Deal d;
+  total *= a.pairs;
+  d.per = (total + a.workgroups - 1u) / a.workgroups;
+  if (d.per < a.least) d.per = a.least;
+  const uint64_t at = at_workgroup * d.per;
+  const bool here = of_sequence != 0xFFFFFFFFu ? from <= of_sequence && of_sequence < from + each : at < total && below * a.pairs <= at && at < (below + mine) * a.pairs;
+  if (threadIdx.x == 0u) shared[1][0] = a.seqs;
+  __syncthreads();
+  if (here) {
+    uint32_t s = from;
+    for (;; ++s) {
+      const uint64_t n = tiles_of(a, length_of(a, s));
+      if (of_sequence != 0xFFFFFFFFu ? s == of_sequence : at < (below + n) * a.pairs) break;
+      below += n;
+    }
+    shared[1][0] = s;
+    shared[1][1] = below * a.pairs;
   }
   __syncthreads();
-  float all = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-  if (all == -INFINITY) all = 0.0f;
-  float total = 0.0f, o = 0.0f;
-  for (int w = 0; w < 4; ++w) {
-    const float f = exp2f(tops[w] - all);
-    total = fmaf(sums[w], f, total);
-    o = fmaf(parts[w][threadIdx.x], f, o);
+  d.seq = (uint32_t)shared[1][0];
+  d.before = shared[1][1];
+  return d;
+}
+
+// Parts of a segment that is not a sequence's whole: [16 NH heads][DP] sums, [16 NH] maxima, [16 NH] sums of weights.
+template <int DP, int NH> constexpr uint32_t kPartFloats = 16 * NH * DP + 32 * NH;
+
+template <typename T, int DP, int NH, bool PG, int AL>
+__global__ __launch_bounds__(kBlock, DP <= 128 && NH == 1 ? 2 : 1) void lt_paged_attention_kernel(const PagedArgs a) {
+  using G = Geo<T, DP, NH>;
+  constexpr int KT = G::KT, NC = G::NC, NV = G::NV, NP = G::NP;
+  __shared__ int32_t pages[kSlots];
+  __shared__ uint64_t found[2][8];
+  __shared__ float tops[4][16 * NH], sums[4][16 * NH];
+  __shared__ __attribute__((aligned(16))) float meet[4][16 * G::PITCH];
+  const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15u, g = lane >> 4;
+  const uint32_t group = a.heads / a.kv_heads, blocks = a.pairs / a.kv_heads;
+  const float scale = a.scale * kLog2e;
+  const int64_t value = (int64_t)a.kv_heads * a.rows.d * a.dim;   // from a key to its value
+
+  uint64_t at, end, before;
+  uint32_t seq;
+  if (a.split) {
+    const Deal d = deal(a, found, blockIdx.x, 0xFFFFFFFFu);
+    if (d.seq >= a.seqs) return;
+    at = blockIdx.x * d.per;
+    end = at + d.per;
+    before = d.before;
+    seq = d.seq;
+  } else {
+    seq = blockIdx.x / a.pairs;
+    before = 0;
+    at = 0;
+    end = 1;
   }
-  if (threadIdx.x < a.dim) ((T*)a.out)[((uint64_t)s * a.heads + h) * a.dim + threadIdx.x] = (T)(total > 0.0f || total != total ? o / total : 0.0f);
+
+  while (at < end && seq < a.seqs) {
+    const uint32_t len = length_of(a, seq), tiles = tiles_of(a, len);
+    uint32_t pair, t0, t1;
+    if (a.split) {
+      const uint64_t rel = at - before;
+      pair = rel >> 32 ? (uint32_t)(rel / tiles) : (uint32_t)rel / tiles;
+      t0 = (uint32_t)(rel - (uint64_t)pair * tiles);
+      t1 = (uint32_t)(end - at < tiles - t0 ? t0 + (end - at) : tiles);
+    } else {
+      pair = blockIdx.x % a.pairs;
+      t0 = 0;
+      t1 = tiles;
+    }
+    const uint32_t kh = pair / blocks, h0 = kh * group + (pair - kh * blocks) * 16u * NH, heads = min(16u * NH, (kh + 1u) * group - h0);
+
+    // B of the scores: lane (n, g) has head n's elements (4 c + g) CE .. + CE - 1; zeros behind the last head and the last element
+    U4 q[NH][NC];
+    uint32_t dim = a.dim;
+    asm volatile("" : "+s"(dim));   // (what follows is done anew for every segment: kept over them, its conditions fill the scalar registers)
+#pragma unroll
+    for (int b = 0; b < NH; ++b) {
+      const uint32_t h = 16u * b + n, to = h < heads ? dim : 0u;
+      const T* row = (const T*)a.q + (int64_t)seq * a.q_seq + (int64_t)(h0 + (h < heads ? h : 0u)) * a.q_head;
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        if (a.q_whole) q[b][c] = load_piece<T, 16, 16>(row, (4u * c + g) * G::CE, to, (const T*)zeros);
+        else q[b][c] = load_piece<T, 16, (int)sizeof(T)>(row, (4u * c + g) * G::CE, to, (const T*)zeros);
+      }
+    }
+
+    F4 acc[NH][NV];
+    float top[NH], sum[NH];
+#pragma unroll
+    for (int b = 0; b < NH; ++b) {
+      top[b] = -INFINITY;
+      sum[b] = 0.0f;
+#pragma unroll
+      for (int j = 0; j < NV; ++j) acc[b][j] = F4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+
+    const uint32_t stretch = max(1u, (uint32_t)min((uint64_t)(kSlots - 2) * a.rows.d / G::TILE, (uint64_t)0x7fffffffu / G::TILE));   // tiles whose pages fit
+    for (uint32_t first = t0; first < t1; first += stretch) {
+      const uint32_t last = min(t1, first + stretch);
+      const uint32_t k0 = first * G::TILE, k1 = (uint32_t)min((uint64_t)last * G::TILE, (uint64_t)len);
+      if (k0 >= k1) break;   // (an empty sequence)
+      const uint32_t slot0 = divide(a.rows, k0), n_slots = divide(a.rows, k1 - 1u) - slot0 + 1u;
+      __syncthreads();       // (the stretch before has been read)
+      for (uint32_t i = threadIdx.x; i < n_slots; i += kBlock) {
+        const int32_t p = a.table[(uint64_t)seq * a.slots + slot0 + i];
+        pages[i] = p >= 0 && (uint32_t)p < a.pages ? p : -1;
+      }
+      __syncthreads();
+
+      // Where a step's keys lie.  PG: a page holds whole tiles of 16, so a tile has one page: its first row, and how many
+      // of its keys there are.  Otherwise every lane finds its own keys.
+      struct Where {
+        int64_t tile[KT];
+        uint32_t there[KT];
+      };
+      auto find_tiles = [&](uint32_t key0) {
+        Where w;
+#pragma unroll
+        for (int t = 0; t < KT; ++t) {
+          const uint32_t k = key0 + 16u * t;
+          uint32_t there = k < k1 ? min(16u, k1 - k) : 0u;
+          const uint32_t slot = divide(a.rows, k);
+          int32_t p = there ? pages[slot - slot0] : -1;
+          p = __builtin_amdgcn_readfirstlane(p);
+          if (p < 0) there = 0u;
+          w.there[t] = there;
+          w.tile[t] = there ? (((int64_t)p * 2 * a.kv_heads + kh) * a.rows.d + (k - slot * a.rows.d)) * a.dim : (int64_t)0;
+        }
+        return w;
+      };
+      auto find_row = [&](uint32_t key, bool* ok) {
+        const uint32_t slot = divide(a.rows, key);
+        const int32_t p = key < k1 ? pages[slot - slot0] : -1;
+        *ok = p >= 0;
+        return p >= 0 ? (((int64_t)p * 2 * a.kv_heads + kh) * a.rows.d + (key - slot * a.rows.d)) * a.dim : (int64_t)0;
+      };
+      auto load_keys = [&](const Where& w, uint32_t key0, U4 (&k)[KT][NC]) {
+#pragma unroll
+        for (int t = 0; t < KT; ++t) {
+          const T* row;
+          if constexpr (PG) row = (const T*)a.cache + w.tile[t] + (uint64_t)(min(n, max(w.there[t], 1u) - 1u) * a.dim);
+          else {
+            bool ok;
+            row = (const T*)a.cache + find_row(key0 + 16u * t + n, &ok);
+          }
+#pragma unroll
+          for (int c = 0; c < NC; ++c) k[t][c] = load_piece<T, 16, AL>(row, (4u * c + g) * G::CE, a.dim, (const T*)zeros);
+        }
+      };
+      auto load_values = [&](const Where& w, uint32_t key0, U4 (&v)[4 * KT][NP], uint32_t* there) {
+        *there = 0u;
+#pragma unroll
+        for (int i = 0; i < 4 * KT; ++i) {
+          const uint32_t t = i >> 2, r = 4u * g + (i & 3u);
+          const T* row;
+          bool ok;
+          if constexpr (PG) {
+            ok = r < w.there[t];
+            row = (const T*)a.cache + value + w.tile[t] + (uint64_t)(min(r, max(w.there[t], 1u) - 1u) * a.dim);
+          } else row = (const T*)a.cache + value + find_row(key0 + 16u * t + r, &ok);
+          *there |= ok ? 1u << i : 0u;
+#pragma unroll
+          for (int p = 0; p < NP; ++p) v[i][p] = load_piece<T, G::VB, AL>(row, n * NV + p * (G::VB / sizeof(T)), a.dim, row);   // (never stored)
+        }
+      };
+
+      uint32_t key0 = k0 + wave * G::WK;
+      Where w = {};
+      U4 k[KT][NC];
+      if (key0 < k1) {
+        if constexpr (PG) w = find_tiles(key0);
+        load_keys(w, key0, k);
+      }
+      for (; key0 < k1; key0 += G::TILE) {
+        U4 v[4 * KT][NP];
+        uint32_t there;
+        load_values(w, key0, v, &there);
+        // ---- scores
+        F4 s[NH][KT];
+#pragma unroll
+        for (int b = 0; b < NH; ++b)
+#pragma unroll
+          for (int t = 0; t < KT; ++t) {
+            s[b][t] = F4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+              if constexpr (G::BF) {
+                s[b][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(B8, k[t][c]), __builtin_bit_cast(B8, q[b][c]), s[b][t], 0, 0, 0);
+              } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                  s[b][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[t][c][e]), __uint_as_float(q[b][c][e]), s[b][t], 0, 0, 0);
+              }
+            }
+          }
+        const uint32_t next = key0 + G::TILE;
+        if (next < k1) {
+          if constexpr (PG) w = find_tiles(next);
+          load_keys(w, next, k);
+        }
+        // ---- weights
+        const bool all = __all(there == (1u << (4 * KT)) - 1u);
+#pragma unroll
+        for (int b = 0; b < NH; ++b) {
+          float mx = -INFINITY;
+#pragma unroll
+          for (int t = 0; t < KT; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              s[b][t][r] *= scale;
+              mx = fmaxf(mx, s[b][t][r]);
+            }
+          if (!all) {
+            mx = -INFINITY;
+#pragma unroll
+            for (int t = 0; t < KT; ++t)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) {
+                s[b][t][r] = there >> (4 * t + r) & 1u ? s[b][t][r] : -INFINITY;
+                mx = fmaxf(mx, s[b][t][r]);
+              }
+          }
+          const float fresh = fmaxf(top[b], max_over_groups(mx)), safe = fresh == -INFINITY ? 0.0f : fresh, keep = power2(top[b] - safe);
+          top[b] = fresh;
+          float part = 0.0f;
+#pragma unroll
+          for (int t = 0; t < KT; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              s[b][t][r] = power2(s[b][t][r] - safe);
+              part += s[b][t][r];
+            }
+          sum[b] = fmaf(sum[b], keep, part);
+#pragma unroll
+          for (int j = 0; j < NV; ++j) acc[b][j] *= keep;
+        }
+        // ---- products
+        if (!all) {
+#pragma unroll
+          for (int i = 0; i < 4 * KT; ++i)
+#pragma unroll
+            for (int p = 0; p < NP; ++p)
+              if (!(there >> i & 1u)) v[i][p] = U4{0u, 0u, 0u, 0u};
+        }
+        if constexpr (G::BF) {
+          B8 weight[NH];
+#pragma unroll
+          for (int b = 0; b < NH; ++b)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) weight[b][i] = (__bf16)s[b][i >> 2][i & 3];
+#pragma unroll
+          for (int j = 0; j < NV; ++j) {
+            constexpr uint32_t kLow = 0x05040100u, kHigh = 0x07060302u;
+            U4 f;
+#pragma unroll
+            for (int p = 0; p < 4; ++p)
+              f[p] = __builtin_amdgcn_perm(v[2 * p + 1][j / 8][j / 2 % 4], v[2 * p][j / 8][j / 2 % 4], (j & 1) ? kHigh : kLow);
+#pragma unroll
+            for (int b = 0; b < NH; ++b) acc[b][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(B8, f), weight[b], acc[b][j], 0, 0, 0);
+          }
+        } else {
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+#pragma unroll
+              for (int b = 0; b < NH; ++b) acc[b][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[r][j / 4][j % 4]), s[b][0][r], acc[b][j], 0, 0, 0);
+        }
+      }
+    }
+
+    // ---- the four waves' parts
+    __syncthreads();
+#pragma unroll
+    for (int b = 0; b < NH; ++b) {
+      const float all = sum_over_groups(sum[b]);
+      if (g == 0u) {
+        tops[wave][16 * b + n] = top[b];
+        sums[wave][16 * b + n] = all;
+      }
+    }
+    __syncthreads();
+    const bool whole = t0 == 0u && t1 == tiles;
+    float* part = whole ? nullptr : a.parts + (uint64_t)(2u * blockIdx.x + (t0 == 0u ? 1u : 0u)) * kPartFloats<DP, NH>;
+#pragma unroll
+    for (int b = 0; b < NH; ++b) {
+      auto common = [&](uint32_t h) {
+        const float t = fmaxf(fmaxf(tops[0][h], tops[1][h]), fmaxf(tops[2][h], tops[3][h]));
+        return t == -INFINITY ? 0.0f : t;
+      };
+      const float f = power2(top[b] - common(16u * b + n));
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int j = 0; j < NV; j += 4)
+          *(F4*)&meet[wave][n * G::PITCH + (4u * g + r) * NV + j] = F4{acc[b][j][r] * f, acc[b][j + 1][r] * f, acc[b][j + 2][r] * f, acc[b][j + 3][r] * f};
+      __syncthreads();
+      for (uint32_t i = threadIdx.x; i < 16u * DP / 4u; i += kBlock) {
+        const uint32_t h = i / (DP / 4u), d = i % (DP / 4u) * 4u, hh = 16u * b + h;
+        if (hh >= heads || d >= a.dim) continue;
+        F4 o = *(const F4*)&meet[0][h * G::PITCH + d];
+#pragma unroll
+        for (int x = 1; x < 4; ++x) o += *(const F4*)&meet[x][h * G::PITCH + d];
+        if (whole) {
+          const float t = common(hh);
+          float total = 0.0f;
+#pragma unroll
+          for (int x = 0; x < 4; ++x) total = fmaf(sums[x][hh], power2(tops[x][hh] - t), total);
+          const float inv = total > 0.0f || total != total ? 1.0f / total : 0.0f;
+          T* y = (T*)a.out + ((uint64_t)seq * a.heads + h0 + hh) * a.dim + d;
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (d + e < a.dim) y[e] = (T)(o[e] * inv);
+        } else {
+          *(F4*)&part[hh * DP + d] = o;
+        }
+      }
+      __syncthreads();
+    }
+    if (!whole && threadIdx.x < 16u * NH) {
+      const uint32_t h = threadIdx.x;
+      const float t = fmaxf(fmaxf(tops[0][h], tops[1][h]), fmaxf(tops[2][h], tops[3][h])), safe = t == -INFINITY ? 0.0f : t;
+      float total = 0.0f;
+      for (int x = 0; x < 4; ++x) total = fmaf(sums[x][h], power2(tops[x][h] - safe), total);
+      part[16 * NH * DP + h] = t;
+      part[16 * NH * DP + 16 * NH + h] = total;
+    }
+
+    if (!a.split) break;
+    at += t1 - t0;
+    if (at == before + (uint64_t)tiles * a.pairs) {
+      before = at;
+      ++seq;
+    }
+  }
+}
+
+// Sequences whose tiles went to several workgroups: their parts, joined in order.  One workgroup per sequence and query head.
+template <typename T, int DP, int NH>
+__global__ __launch_bounds__(kBlock) void lt_paged_join_kernel(const PagedArgs a) {
+  __shared__ uint64_t found[2][8];
+  __shared__ float meet[kBlock], weight[kBlock / DP];
+  const uint32_t seq = blockIdx.x / a.heads, head = blockIdx.x % a.heads, group = a.heads / a.kv_heads, blocks = a.pairs / a.kv_heads;
+  const Deal deal_ = deal(a, found, 0, seq);
+  const uint32_t tiles = tiles_of(a, length_of(a, seq)), kh = head / group, block = (head - kh * group) / (16u * NH), h = (head - kh * group) % (16u * NH);
+  const uint64_t from = deal_.before + (uint64_t)(kh * blocks + block) * tiles, w0 = from / deal_.per, w1 = (from + tiles - 1u) / deal_.per;
+  if (w0 == w1) return;
+  const uint32_t d = threadIdx.x % DP, lane = threadIdx.x / DP, lanes = kBlock / DP;
+  float top = -INFINITY, sum = 0.0f, o = 0.0f;
+  for (uint64_t w = w0 + lane; w <= w1; w += lanes) {
+    const float* part = a.parts + (2u * w + (w == w0 ? 1u : 0u)) * kPartFloats<DP, NH>;
+    const float t = part[16 * NH * DP + h], fresh = fmaxf(top, t), safe = fresh == -INFINITY ? 0.0f : fresh, keep = power2(top - safe), f = power2(t - safe);
+    top = fresh;
+    sum = fmaf(sum, keep, f * part[16 * NH * DP + 16 * NH + h]);
+    o = fmaf(o, keep, f * part[h * DP + d]);
+  }
+  __shared__ float tops[kBlock];
+  tops[threadIdx.x] = top;
+  __syncthreads();
+  float all = top;
+  for (uint32_t l = 0; l < lanes; ++l) all = fmaxf(all, tops[l * DP + d]);
+  const float f = power2(top - (all == -INFINITY ? 0.0f : all));
+  meet[threadIdx.x] = o * f;
+  if (d == 0u) weight[lane] = sum * f;
+  __syncthreads();
+  if (lane != 0u || d >= a.dim) return;
+  float total = 0.0f;
+  o = 0.0f;
+  for (uint32_t l = 0; l < lanes; ++l) {
+    total += weight[l];
+    o += meet[l * DP + d];
+  }
+  ((T*)a.out)[((uint64_t)seq * a.heads + head) * a.dim + d] = (T)(total > 0.0f || total != total ? o / total : 0.0f);
+}
+
+template <typename T, int DP, int NH>
+hipError_t launch_paged_as(const PagedArgs& a, hipStream_t s) {
+  // rows of whole 16 bytes are read in such pieces, others in the largest that they are made of
+  const uint32_t row = a.dim * (uint32_t)sizeof(T);
+  const bool whole = row % 16u == 0u && (uintptr_t)a.cache % 16u == 0u;
+  if (whole && a.rows.d % 16u == 0u) LT_LAUNCH((lt_paged_attention_kernel<T, DP, NH, true, 16>), dim3(a.workgroups), dim3(kBlock), s, a);
+  else if (whole) LT_LAUNCH((lt_paged_attention_kernel<T, DP, NH, false, 16>), dim3(a.workgroups), dim3(kBlock), s, a);
+  else if (row % 4u == 0u) LT_LAUNCH((lt_paged_attention_kernel<T, DP, NH, false, 4>), dim3(a.workgroups), dim3(kBlock), s, a);
+  else if constexpr (sizeof(T) == 2) LT_LAUNCH((lt_paged_attention_kernel<T, DP, NH, false, 2>), dim3(a.workgroups), dim3(kBlock), s, a);
+  if (a.split) LT_LAUNCH((lt_paged_join_kernel<T, DP, NH>), dim3(a.seqs * a.heads), dim3(kBlock), s, a);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_paged_of(const PagedArgs& a, hipStream_t s) {
+  if (a.padded == 64u) return a.blocks_of == 16u ? launch_paged_as<T, 64, 1>(a, s) : launch_paged_as<T, 64, 2>(a, s);
+  if (a.padded == 128u) return a.blocks_of == 16u ? launch_paged_as<T, 128, 1>(a, s) : launch_paged_as<T, 128, 2>(a, s);
+  return launch_paged_as<T, 256, 1>(a, s);
 }
 
 hipError_t launch_paged(const void* args, hipStream_t s) {
-  const PagedArgs& a = *(const PagedArgs*)args;
+  PagedArgs a = *(const PagedArgs*)args;
   if (a.seqs == 0) return hipSuccess;
-  if (!a.q || !a.lengths || !a.out || (a.capacity > 0 && (!a.cache || !a.table)) || a.dim == 0 || a.dim > 256u || a.kv_heads == 0 || a.heads % a.kv_heads != 0 || a.rows.d == 0)
+  if (!a.q || !a.lengths || !a.out || (a.capacity > 0 && (!a.cache || !a.table)) || a.dim == 0 || a.dim > a.padded || a.kv_heads == 0 || a.heads % a.kv_heads != 0 ||
+      a.rows.d == 0 || a.workgroups == 0 || (a.split && !a.parts) || a.tile != (a.dtype == kF32 ? 64u : 128u) ||
+      a.blocks_of > (a.padded == 256u ? 16u : 32u))
     return hipErrorInvalidValue;
-  if (a.dtype == kF32) LT_LAUNCH(lt_paged_attention_kernel<float>, dim3(a.seqs * a.heads), dim3(kBlock), s, a);
-  else if (a.dtype == kBF16) LT_LAUNCH(lt_paged_attention_kernel<__bf16>, dim3(a.seqs * a.heads), dim3(kBlock), s, a);
-  else return hipErrorInvalidValue;
-  return hipGetLastError();
+  const int64_t size = a.dtype == kF32 ? 4 : 2;
+  a.q_whole = (uintptr_t)a.q % 16u == 0u && a.q_seq * size % 16 == 0 && a.q_head * size % 16 == 0 && a.dim * size % 16 == 0;
+  return a.dtype == kF32 ? launch_paged_of<float>(a, s) : a.dtype == kBF16 ? launch_paged_of<__bf16>(a, s) : hipErrorInvalidValue;
 }
 
 const bool registered = set_operator(kOpCacheAppend, launch_append) && set_operator(kOpPagedAttention, launch_paged);
