@@ -485,6 +485,8 @@ static lt_status execute(lt_ctx* ctx, Plan* plan, const std::vector<BufRef>& par
         ltk::GemmArgs* a = (ltk::GemmArgs*)args.data();
         a->split_ws = red_partials + l.scratch_slot * (kPartialFloats / kScratchSlots);
         a->tickets = red_tickets + l.scratch_slot * (kTickets / kScratchSlots);
+      } else if (paged_tickets(l) != 0) {
+        ((ltk::PagedArgs*)args.data())->tickets = red_tickets + l.scratch_slot * (kTickets / kScratchSlots);
       }
       hipStream_t stream = ctx->stream;
       if (multi) {

@@ -299,6 +299,7 @@ namespace lt {
 
 constexpr size_t kPartialFloats = 1 << 20;   // reduction partials (4 MiB of the workspace)
 constexpr size_t kTickets = 1024;
+static_assert(2 * ltk::kMaxPagedWorkgroups <= kTickets, "two tickets for every workgroup of an attention over a paged cache");
 
 
 lt_status fail(lt_ctx* ctx, lt_status code, const std::string& msg);
@@ -334,6 +335,7 @@ bool spreads(const lt_ctx* ctx, const Plan* plan);
 // tiles through the reduction scratch and take tickets); 0 for every other launch
 uint64_t gemm_shared_tiles(const Launch& l);
 bool row_op_total(const Launch& l);   // a row operator whose workgroups exchange a sum
+uint64_t paged_tickets(const Launch& l);   // of an attention over a paged cache whose workgroups share sequences; 0 for every other launch
 
 }  // namespace lt
 #endif  // LT_CORE_H_

@@ -338,7 +338,9 @@ struct AppendArgs {
 
 // out[s][h] = softmax(scale q K^T) V over sequence s's keys in the paged cache.  Work is counted in tiles of `tile` keys for
 // blocks of `blocks_of` query heads of one key head; `pairs` such blocks a sequence.  split: tiles are dealt out evenly to
-// `workgroups`, `least` or more to each, and what several of them have of a sequence meets in `parts`; otherwise a workgroup has a block of a sequence.
+// `workgroups`, and what several of them have of a block meets in `parts`, two pieces a workgroup, with a ticket each (zero before and after a
+// launch); otherwise a workgroup has a block of a sequence.
+constexpr uint32_t kMaxPagedWorkgroups = 512;
 struct PagedArgs {
   const void* q;
   const void* cache;
@@ -351,9 +353,10 @@ struct PagedArgs {
   float scale;
   int64_t q_seq, q_head;        // element strides
   float* parts;
+  uint32_t* tickets;
   uint32_t padded, blocks_of, pairs, tile;   // padded: the kernel instance's head size
-  uint32_t workgroups, split, least;
-  uint32_t q_whole;             // rows of q are whole 16-byte pieces (the launcher sets it)
+  uint32_t workgroups, split;
+  uint32_t pad, q_whole;        // q_whole: rows of q are whole 16-byte pieces (the launcher sets it)
 
   uint64_t part_floats() const { return (uint64_t)blocks_of * padded + 2u * blocks_of; }
   // The instance, and how the work is shared out; `capacity` and what comes before it are set.
@@ -364,9 +367,8 @@ struct PagedArgs {
     pairs = kv_heads * ((group + blocks_of - 1u) / blocks_of);
     tile = dtype == kF32 ? 64u : 128u;
     const uint64_t most = capacity == 0 ? 1 : (capacity - 1u) / tile + 1u, all = (uint64_t)seqs * pairs;
-    const uint64_t resident = padded <= 128u && blocks_of == 16u ? 512u : 256u;
-    least = 2;
-    split = most > 2u ? 1u : 0u;
+    const uint64_t resident = padded <= 128u && blocks_of == 16u ? kMaxPagedWorkgroups : kMaxPagedWorkgroups / 2u;
+    split = most > 1u ? 1u : 0u;
     workgroups = (uint32_t)(split ? (resident < all * most ? resident : all * most) : all);
   }
 };

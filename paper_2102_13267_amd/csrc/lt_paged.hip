@@ -6,6 +6,8 @@
 #include <hip/hip_runtime.h>
 
 #include "lt_launch.h"
+#include "lt_interp.h"
+#include "lt_reduce.h"
 #include "lt_rotary.h"
 
 namespace ltk {
@@ -110,6 +112,12 @@ hipError_t launch_append(const void* args, hipStream_t s) {
 // next step is on its way while this one's weights are computed, V of this one too.
 //
 // Four waves share a tile of 4 WK keys; their maxima, sums and products meet in LDS at a segment's end.
+//
+// The tiles of all sequences in a row (sequence by sequence, and in each block of query heads by block) are dealt out evenly, `per` to a workgroup,
+// so that a long sequence among short ones holds nobody up.  What a workgroup has of a block that others have a share of goes to memory
+// (relaxed accesses of device scope, as the reductions exchange theirs), and whoever comes last joins the pieces in their order: up
+// to eight of them at once, more in groups of about their root, whose last ones then join the groups.  So results do not depend on
+// who comes when.
 template <typename T, int DP, int NH> struct Geo {
   static constexpr bool BF = sizeof(T) == 2;
   static constexpr int KT = BF ? 2 : 1;              // tiles of 16 keys in a wave's step
@@ -173,14 +181,13 @@ __device__ __forceinline__ uint32_t length_of(const PagedArgs& a, uint32_t s) {
 // Tiles of a sequence, one at least: an empty one has zeros to write.
 __device__ __forceinline__ uint32_t tiles_of(const PagedArgs& a, uint32_t len) { return len == 0u ? 1u : (len - 1u) / a.tile + 1u; }
 
-// The tiles of all sequences in a row (sequence by sequence, and in each key head by key head, blocks of 16 NH query heads apart)
-// are dealt out evenly: workgroup w has `per` of them from w * per on.  Found by the block together: the sequence
-// that `at` falls into, how many tiles come before it, and `per`.
+// Workgroup w has the tiles from w * per on.  Found by the block together: the sequence that its first one falls into, and
+// how many tiles come before that sequence.
 struct Deal {
   uint64_t per, before;
   uint32_t seq;
 };
-__device__ __forceinline__ Deal deal(const PagedArgs& a, uint64_t (*shared)[8], uint64_t at_workgroup, uint32_t of_sequence) {
+__device__ __forceinline__ Deal deal(const PagedArgs& a, uint64_t (*shared)[8]) {
   const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, each = (a.seqs + kBlock - 1u) / kBlock, from = threadIdx.x * each;
   uint64_t mine = 0;
   for (uint32_t i = 0; i < each; ++i)
@@ -191,6 +198,7 @@ __device__ __forceinline__ Deal deal(const PagedArgs& a, uint64_t (*shared)[8], 
     if ((int)lane >= m) up += t;
   }
   if (lane == 63u) shared[0][wave] = up;
+  if (threadIdx.x == 0u) shared[1][0] = a.seqs;
   __syncthreads();
   uint64_t total = 0, below = up - mine;
   for (uint32_t w = 0; w < kBlock / 64u; ++w) {
@@ -198,18 +206,13 @@ __device__ __forceinline__ Deal deal(const PagedArgs& a, uint64_t (*shared)[8], 
     total += shared[0][w];
   }
   Deal d;
-  total *= a.pairs;
-  d.per = (total + a.workgroups - 1u) / a.workgroups;
-  if (d.per < a.least) d.per = a.least;
-  const uint64_t at = at_workgroup * d.per;
-  const bool here = of_sequence != 0xFFFFFFFFu ? from <= of_sequence && of_sequence < from + each : at < total && below * a.pairs <= at && at < (below + mine) * a.pairs;
-  if (threadIdx.x == 0u) shared[1][0] = a.seqs;
-  __syncthreads();
-  if (here) {
+  d.per = (total * a.pairs + a.workgroups - 1u) / a.workgroups;
+  const uint64_t at = blockIdx.x * d.per;
+  if (below * a.pairs <= at && at < (below + mine) * a.pairs) {
     uint32_t s = from;
     for (;; ++s) {
       const uint64_t n = tiles_of(a, length_of(a, s));
-      if (of_sequence != 0xFFFFFFFFu ? s == of_sequence : at < (below + n) * a.pairs) break;
+      if (at < (below + n) * a.pairs) break;
       below += n;
     }
     shared[1][0] = s;
@@ -221,8 +224,22 @@ __device__ __forceinline__ Deal deal(const PagedArgs& a, uint64_t (*shared)[8], 
   return d;
 }
 
-// Parts of a segment that is not a sequence's whole: [16 NH heads][DP] sums, [16 NH] maxima, [16 NH] sums of weights.
-template <int DP, int NH> constexpr uint32_t kPartFloats = 16 * NH * DP + 32 * NH;
+// A piece: [16 NH heads][DP] sums of weights times values, [16 NH] maxima, [16 NH] sums of weights.
+template <int DP, int NH> constexpr uint32_t kPieceFloats = 16 * NH * DP + 32 * NH;
+constexpr uint32_t kMostPieces = 32;   // at once: the root of the largest grid is 23
+
+// Whether the calling workgroup is the last of `count` to come here.
+__device__ __forceinline__ bool last_of(uint32_t* ticket, uint32_t count, uint32_t* flag) {
+  all_published();
+  __syncthreads();
+  if (threadIdx.x == 0u) {
+    const bool last = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == count - 1u;
+    if (last) __hip_atomic_store(ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    *flag = last ? 1u : 0u;
+  }
+  __syncthreads();
+  return *flag != 0u;
+}
 
 template <typename T, int DP, int NH, bool PG, int AL>
 __global__ __launch_bounds__(kBlock, DP <= 128 && NH == 1 ? 2 : 1) void lt_paged_attention_kernel(const PagedArgs a) {
@@ -230,17 +247,19 @@ __global__ __launch_bounds__(kBlock, DP <= 128 && NH == 1 ? 2 : 1) void lt_paged
   constexpr int KT = G::KT, NC = G::NC, NV = G::NV, NP = G::NP;
   __shared__ int32_t pages[kSlots];
   __shared__ uint64_t found[2][8];
-  __shared__ float tops[4][16 * NH], sums[4][16 * NH];
+  __shared__ float tops[4][16 * NH], sums[4][16 * NH], factor[kMostPieces][16 * NH], total_of[16 * NH];
+  __shared__ uint32_t last_flag;
   __shared__ __attribute__((aligned(16))) float meet[4][16 * G::PITCH];
   const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15u, g = lane >> 4;
   const uint32_t group = a.heads / a.kv_heads, blocks = a.pairs / a.kv_heads;
   const float scale = a.scale * kLog2e;
   const int64_t value = (int64_t)a.kv_heads * a.rows.d * a.dim;   // from a key to its value
 
-  uint64_t at, end, before;
+  uint64_t at, end, before, per = 1;
   uint32_t seq;
   if (a.split) {
-    const Deal d = deal(a, found, blockIdx.x, 0xFFFFFFFFu);
+    const Deal d = deal(a, found);
+    per = d.per;
     if (d.seq >= a.seqs) return;
     at = blockIdx.x * d.per;
     end = at + d.per;
@@ -480,7 +499,18 @@ __global__ __launch_bounds__(kBlock, DP <= 128 && NH == 1 ? 2 : 1) void lt_paged
     }
     __syncthreads();
     const bool whole = t0 == 0u && t1 == tiles;
-    float* part = whole ? nullptr : a.parts + (uint64_t)(2u * blockIdx.x + (t0 == 0u ? 1u : 0u)) * kPartFloats<DP, NH>;
+    // the pieces of this block of heads: piece i is workgroup w0 + i's, in the place of those that begin a block (the first) or of the others
+    const uint64_t tile0 = before + (uint64_t)pair * tiles;
+    const uint32_t w0 = whole ? 0u : (uint32_t)(tile0 / per), pieces = whole ? 1u : (uint32_t)((tile0 + tiles - 1u) / per) - w0 + 1u, mine = blockIdx.x - w0;
+    auto place_of = [&](uint32_t i) { return i == 0u ? 2u * w0 + 1u : 2u * (w0 + i); };
+    auto piece = [&](uint32_t i) { return a.parts + (uint64_t)place_of(i) * kPieceFloats<DP, NH>; };
+    auto put = [&](uint32_t hh, uint32_t d, const F4& o, float inv) {
+      T* y = (T*)a.out + ((uint64_t)seq * a.heads + h0 + hh) * a.dim + d;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (d + e < a.dim) y[e] = (T)(o[e] * inv);
+    };
+    auto inverse = [](float total) { return total > 0.0f || total != total ? 1.0f / total : 0.0f; };
 #pragma unroll
     for (int b = 0; b < NH; ++b) {
       auto common = [&](uint32_t h) {
@@ -505,24 +535,70 @@ __global__ __launch_bounds__(kBlock, DP <= 128 && NH == 1 ? 2 : 1) void lt_paged
           float total = 0.0f;
 #pragma unroll
           for (int x = 0; x < 4; ++x) total = fmaf(sums[x][hh], power2(tops[x][hh] - t), total);
-          const float inv = total > 0.0f || total != total ? 1.0f / total : 0.0f;
-          T* y = (T*)a.out + ((uint64_t)seq * a.heads + h0 + hh) * a.dim + d;
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (d + e < a.dim) y[e] = (T)(o[e] * inv);
+          put(hh, d, o, inverse(total));
         } else {
-          *(F4*)&part[hh * DP + d] = o;
+          publish4(piece(mine) + hh * DP + d, make_float4(o[0], o[1], o[2], o[3]));
         }
       }
       __syncthreads();
     }
-    if (!whole && threadIdx.x < 16u * NH) {
-      const uint32_t h = threadIdx.x;
-      const float t = fmaxf(fmaxf(tops[0][h], tops[1][h]), fmaxf(tops[2][h], tops[3][h])), safe = t == -INFINITY ? 0.0f : t;
-      float total = 0.0f;
-      for (int x = 0; x < 4; ++x) total = fmaf(sums[x][h], power2(tops[x][h] - safe), total);
-      part[16 * NH * DP + h] = t;
-      part[16 * NH * DP + 16 * NH + h] = total;
+    if (!whole) {
+      if (threadIdx.x < heads) {
+        const uint32_t h = threadIdx.x;
+        const float t = fmaxf(fmaxf(tops[0][h], tops[1][h]), fmaxf(tops[2][h], tops[3][h])), safe = t == -INFINITY ? 0.0f : t;
+        float total = 0.0f;
+        for (int x = 0; x < 4; ++x) total = fmaf(sums[x][h], power2(tops[x][h] - safe), total);
+        publish(piece(mine) + 16 * NH * DP + h, t);
+        publish(piece(mine) + 16 * NH * DP + 16 * NH + h, total);
+      }
+      // pieces first, first + step, ... : joined, into the output or into the first one's place
+      auto join = [&](uint32_t first, uint32_t step, uint32_t count, bool out) {
+        for (uint32_t i = threadIdx.x; i < count * 16u * NH; i += kBlock) {
+          const uint32_t p = i / (16u * NH), h = i % (16u * NH);
+          if (h < heads) factor[p][h] = published(piece(first + p * step) + 16 * NH * DP + h);
+        }
+        __syncthreads();
+        if (threadIdx.x < heads) {
+          const uint32_t h = threadIdx.x;
+          float t = -INFINITY, total = 0.0f;
+          for (uint32_t p = 0; p < count; ++p) t = fmaxf(t, factor[p][h]);
+          const float safe = t == -INFINITY ? 0.0f : t;
+          for (uint32_t p = 0; p < count; ++p) {
+            const float f = power2(factor[p][h] - safe);
+            factor[p][h] = f;
+            total = fmaf(published(piece(first + p * step) + 16 * NH * DP + 16 * NH + h), f, total);
+          }
+          total_of[h] = total;
+          if (!out) {
+            publish(piece(first) + 16 * NH * DP + h, t);
+            publish(piece(first) + 16 * NH * DP + 16 * NH + h, total);
+          }
+        }
+        __syncthreads();
+        for (uint32_t i = threadIdx.x; i < heads * DP / 4u; i += kBlock) {
+          const uint32_t hh = i / (DP / 4u), d = i % (DP / 4u) * 4u;
+          if (d >= a.dim) continue;
+          F4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+          for (uint32_t p = 0; p < count; ++p) {
+            const float4 t = published4(piece(first + p * step) + hh * DP + d);
+            const float f = factor[p][hh];
+            o = F4{fmaf(t.x, f, o[0]), fmaf(t.y, f, o[1]), fmaf(t.z, f, o[2]), fmaf(t.w, f, o[3])};
+          }
+          if (out) put(hh, d, o, inverse(total_of[hh]));
+          else publish4(piece(first) + hh * DP + d, make_float4(o[0], o[1], o[2], o[3]));
+        }
+      };
+      uint32_t each = pieces;
+      if (pieces > 8u)
+        for (each = 3u; each * each < pieces;) ++each;
+      const uint32_t first = mine / each * each, groups = (pieces + each - 1u) / each;
+      if (last_of(a.tickets + place_of(first), min(each, pieces - first), &last_flag)) {
+        join(first, 1u, min(each, pieces - first), groups == 1u);
+        // (the second piece begins no group: its ticket is that of the groups)
+        if (groups > 1u && last_of(a.tickets + place_of(1u), groups, &last_flag)) join(0u, each, groups, true);
+      }
+      __syncthreads();   // (factor and the flag are free)
     }
 
     if (!a.split) break;
@@ -534,44 +610,6 @@ __global__ __launch_bounds__(kBlock, DP <= 128 && NH == 1 ? 2 : 1) void lt_paged
   }
 }
 
-// Sequences whose tiles went to several workgroups: their parts, joined in order.  One workgroup per sequence and query head.
-template <typename T, int DP, int NH>
-__global__ __launch_bounds__(kBlock) void lt_paged_join_kernel(const PagedArgs a) {
-  __shared__ uint64_t found[2][8];
-  __shared__ float meet[kBlock], weight[kBlock / DP];
-  const uint32_t seq = blockIdx.x / a.heads, head = blockIdx.x % a.heads, group = a.heads / a.kv_heads, blocks = a.pairs / a.kv_heads;
-  const Deal deal_ = deal(a, found, 0, seq);
-  const uint32_t tiles = tiles_of(a, length_of(a, seq)), kh = head / group, block = (head - kh * group) / (16u * NH), h = (head - kh * group) % (16u * NH);
-  const uint64_t from = deal_.before + (uint64_t)(kh * blocks + block) * tiles, w0 = from / deal_.per, w1 = (from + tiles - 1u) / deal_.per;
-  if (w0 == w1) return;
-  const uint32_t d = threadIdx.x % DP, lane = threadIdx.x / DP, lanes = kBlock / DP;
-  float top = -INFINITY, sum = 0.0f, o = 0.0f;
-  for (uint64_t w = w0 + lane; w <= w1; w += lanes) {
-    const float* part = a.parts + (2u * w + (w == w0 ? 1u : 0u)) * kPartFloats<DP, NH>;
-    const float t = part[16 * NH * DP + h], fresh = fmaxf(top, t), safe = fresh == -INFINITY ? 0.0f : fresh, keep = power2(top - safe), f = power2(t - safe);
-    top = fresh;
-    sum = fmaf(sum, keep, f * part[16 * NH * DP + 16 * NH + h]);
-    o = fmaf(o, keep, f * part[h * DP + d]);
-  }
-  __shared__ float tops[kBlock];
-  tops[threadIdx.x] = top;
-  __syncthreads();
-  float all = top;
-  for (uint32_t l = 0; l < lanes; ++l) all = fmaxf(all, tops[l * DP + d]);
-  const float f = power2(top - (all == -INFINITY ? 0.0f : all));
-  meet[threadIdx.x] = o * f;
-  if (d == 0u) weight[lane] = sum * f;
-  __syncthreads();
-  if (lane != 0u || d >= a.dim) return;
-  float total = 0.0f;
-  o = 0.0f;
-  for (uint32_t l = 0; l < lanes; ++l) {
-    total += weight[l];
-    o += meet[l * DP + d];
-  }
-  ((T*)a.out)[((uint64_t)seq * a.heads + head) * a.dim + d] = (T)(total > 0.0f || total != total ? o / total : 0.0f);
-}
-
 template <typename T, int DP, int NH>
 hipError_t launch_paged_as(const PagedArgs& a, hipStream_t s) {
   // rows of whole 16 bytes are read in such pieces, others in the largest that they are made of
@@ -581,7 +619,6 @@ hipError_t launch_paged_as(const PagedArgs& a, hipStream_t s) {
   else if (whole) LT_LAUNCH((lt_paged_attention_kernel<T, DP, NH, false, 16>), dim3(a.workgroups), dim3(kBlock), s, a);
   else if (row % 4u == 0u) LT_LAUNCH((lt_paged_attention_kernel<T, DP, NH, false, 4>), dim3(a.workgroups), dim3(kBlock), s, a);
   else if constexpr (sizeof(T) == 2) LT_LAUNCH((lt_paged_attention_kernel<T, DP, NH, false, 2>), dim3(a.workgroups), dim3(kBlock), s, a);
-  if (a.split) LT_LAUNCH((lt_paged_join_kernel<T, DP, NH>), dim3(a.seqs * a.heads), dim3(kBlock), s, a);
   return hipGetLastError();
 }
 
@@ -596,7 +633,7 @@ hipError_t launch_paged(const void* args, hipStream_t s) {
   PagedArgs a = *(const PagedArgs*)args;
   if (a.seqs == 0) return hipSuccess;
   if (!a.q || !a.lengths || !a.out || (a.capacity > 0 && (!a.cache || !a.table)) || a.dim == 0 || a.dim > a.padded || a.kv_heads == 0 || a.heads % a.kv_heads != 0 ||
-      a.rows.d == 0 || a.workgroups == 0 || (a.split && !a.parts) || a.tile != (a.dtype == kF32 ? 64u : 128u) ||
+      a.rows.d == 0 || a.workgroups == 0 || (a.split && (!a.parts || !a.tickets || a.workgroups > kMaxPagedWorkgroups)) || a.tile != (a.dtype == kF32 ? 64u : 128u) ||
       a.blocks_of > (a.padded == 256u ? 16u : 32u))
     return hipErrorInvalidValue;
   const int64_t size = a.dtype == kF32 ? 4 : 2;

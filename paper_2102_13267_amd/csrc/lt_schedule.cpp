@@ -55,6 +55,12 @@ uint64_t gemm_shared_tiles(const Launch& l) {
 
 bool row_op_total(const Launch& l) { return l.kind == L_ROWOP && ((const ltk::RowOpArgs*)l.args.data())->has_total != 0u; }
 
+uint64_t paged_tickets(const Launch& l) {
+  if (l.kind != L_PAGED) return 0;
+  const ltk::PagedArgs* a = (const ltk::PagedArgs*)l.args.data();
+  return a->split ? 2ull * a->workgroups : 0;
+}
+
 void schedule_streams(Plan* plan) {
   const size_t n = plan->launches.size();
   plan->n_streams = 1;
@@ -83,12 +89,15 @@ void schedule_streams(Plan* plan) {
     l.scratch_slot = 0;
     l.waits.clear();
     const uint64_t shared_tiles = gemm_shared_tiles(l);   // (a small contraction whose workgroups share tiles)
-    if (l.kind != L_ALL && l.kind != L_COL && shared_tiles == 0 && !row_op_total(l)) continue;
+    if (l.kind != L_ALL && l.kind != L_COL && shared_tiles == 0 && !row_op_total(l) && paged_tickets(l) == 0) continue;
     uint64_t floats = l.grid_x, tickets = 1;
     if (l.kind == L_COL) {
       const ltk::ColArgs* a = (const ltk::ColArgs*)l.args.data();
       floats = (uint64_t)l.grid_y * ((a->cols + 3u) & ~3u) * (a->sum2 ? 2u : 1u);
       tickets = l.grid_x;
+    } else if (l.kind == L_PAGED) {
+      floats = 0;   // (its pieces have a storage of their own)
+      tickets = paged_tickets(l);
     } else if (l.kind == L_GEMM) {
       {
         const ltk::GemmArgs* a = (const ltk::GemmArgs*)l.args.data();
