@@ -299,7 +299,7 @@ namespace lt {
 
 constexpr size_t kPartialFloats = 1 << 20;   // reduction partials (4 MiB of the workspace)
 constexpr size_t kTickets = 1024;
-static_assert(2 * ltk::kMaxPagedWorkgroups <= kTickets, "two tickets for every workgroup of an attention over a paged cache");
+static_assert(2 * ltk::kPagedChunks <= kTickets, "a ticket for every piece of an attention over a paged cache");
 
 
 lt_status fail(lt_ctx* ctx, lt_status code, const std::string& msg);

@@ -337,10 +337,11 @@ struct AppendArgs {
 };
 
 // out[s][h] = softmax(scale q K^T) V over sequence s's keys in the paged cache.  Work is counted in tiles of `tile` keys for
-// blocks of `blocks_of` query heads of one key head; `pairs` such blocks a sequence.  split: tiles are dealt out evenly to
-// `workgroups`, and what several of them have of a block meets in `parts`, two pieces a workgroup, with a ticket each (zero before and after a
-// launch); otherwise a workgroup has a block of a sequence.
-constexpr uint32_t kMaxPagedWorkgroups = 512;
+// blocks of `blocks_of` query heads of one key head; `pairs` such blocks a sequence.  split: sequences are cut into chunks of c
+// tiles, c = max(least, all sequences' tiles / kPagedChunks), a workgroup each, and what several of them have of a block meets in `parts`, with a ticket a
+// piece (zero before and after a launch).  A sequence of t > c tiles has ceil(t / c) < 2 t / c chunks, so there are fewer than 2 kPagedChunks pieces.
+// Otherwise a workgroup has a block of a sequence.
+constexpr uint32_t kPagedChunks = 512;
 struct PagedArgs {
   const void* q;
   const void* cache;
@@ -355,11 +356,11 @@ struct PagedArgs {
   float* parts;
   uint32_t* tickets;
   uint32_t padded, blocks_of, pairs, tile;   // padded: the kernel instance's head size
-  uint32_t workgroups, split;
-  uint32_t pad, q_whole;        // q_whole: rows of q are whole 16-byte pieces (the launcher sets it)
+  uint32_t workgroups, split, least;
+  uint32_t pieces, q_whole;     // pieces: that parts and tickets are for.  q_whole: rows of q are whole 16-byte pieces (the launcher sets it)
 
   uint64_t part_floats() const { return (uint64_t)blocks_of * padded + 2u * blocks_of; }
-  // The instance, and how the work is shared out; `capacity` and what comes before it are set.
+  // The instance, and how the work is shared out; `capacity` and what comes before it are set.  Tiles of all sequences must be below 2^32.
   void share_out() {
     const uint32_t group = heads / kv_heads;
     padded = dim <= 64u ? 64u : dim <= 128u ? 128u : 256u;
@@ -367,9 +368,11 @@ struct PagedArgs {
     pairs = kv_heads * ((group + blocks_of - 1u) / blocks_of);
     tile = dtype == kF32 ? 64u : 128u;
     const uint64_t most = capacity == 0 ? 1 : (capacity - 1u) / tile + 1u, all = (uint64_t)seqs * pairs;
-    const uint64_t resident = padded <= 128u && blocks_of == 16u ? kMaxPagedWorkgroups : kMaxPagedWorkgroups / 2u;
-    split = most > 1u ? 1u : 0u;
-    workgroups = (uint32_t)(split ? (resident < all * most ? resident : all * most) : all);
+    least = 4;
+    split = most > least ? 1u : 0u;
+    const uint64_t each = (most + least - 1u) / least;   // chunks of a sequence at most
+    workgroups = (uint32_t)(split && each > 1u ? (all + kPagedChunks < all * each ? all + kPagedChunks : all * each) : all);
+    pieces = (uint32_t)(split ? (2u * kPagedChunks < all * each ? 2u * kPagedChunks : all * each) : 0u);
   }
 };
 

@@ -1901,7 +1901,7 @@ struct Lowering {
     args.q_seq = q.s_inner;
     args.q_head = q.s_head;
     args.share_out();
-    if ((uint64_t)args.seqs * args.pairs >= ((uint64_t)1 << 31)) return bad(LT_ERR_UNSUPPORTED, "paged_attention: 2^31 or more blocks of query heads");
+    if ((double)args.seqs * args.pairs * (args.capacity / args.tile + 1u) >= 2147483648.0) return bad(LT_ERR_UNSUPPORTED, "paged_attention: sequences * slots * key heads too large");
     Launch l = make_launch(L_PAGED, k, args);
     // (how long the sequences are is known on the device alone: as if every page were read once)
     const uint64_t held = (uint64_t)count(cs), w = dtype_size(an->dtype);
@@ -1913,10 +1913,10 @@ struct Lowering {
     patch(launch, offsetof(ltk::PagedArgs, lengths), s[1], o[1]);
     patch(launch, offsetof(ltk::PagedArgs, table), s[2], o[2]);
     patch(launch, offsetof(ltk::PagedArgs, out), storage_of[a][0], 0, true);
-    if (args.split) {   // two parts a workgroup: of the sequence it begins in, and of the one it ends in
+    if (args.pieces > 0) {
       Storage parts;
       parts.first_launch = -1;
-      parts.bytes = 2 * (size_t)args.workgroups * args.part_floats() * sizeof(float);
+      parts.bytes = (size_t)args.pieces * args.part_floats() * sizeof(float);
       plan->storages.push_back(parts);
       patch(launch, offsetof(ltk::PagedArgs, parts), (int32_t)plan->storages.size() - 1, 0, true);
     }

@@ -109,14 +109,16 @@ hipError_t launch_append(const void* args, hipStream_t s) {
 // the weights as they lie: which key an MFMA's k stands for is free as long as both operands agree, so lane (n, g) holds in B what it
 // computed and reads for A the rows of the same keys, 1 / 16 of a row of dim elements each (bf16: two rows' halves are put together by
 // v_perm_b32).  The accumulator has head n in lane n, so that rescaling by a new maximum is a product in place.  K of the
-// next step is on its way while this one's weights are computed, V of this one too.
+// next step is on its way while this one's weights are computed, V of this one too.  Weights are rounded to bf16 for their product with
+// bf16 values, as an operand of the matrix cores has to be; their sum is that of the unrounded ones.
 //
-// Four waves share a tile of 4 WK keys; their maxima, sums and products meet in LDS at a segment's end.
+// Four waves share a tile of 4 WK keys; their maxima, sums and products meet in LDS at the end.
 //
-// The tiles of all sequences in a row (sequence by sequence, and in each block of query heads by block) are dealt out evenly, `per` to a workgroup,
-// so that a long sequence among short ones holds nobody up.  What a workgroup has of a block that others have a share of goes to memory
-// (relaxed accesses of device scope, as the reductions exchange theirs), and whoever comes last joins the pieces in their order: up
-// to eight of them at once, more in groups of about their root, whose last ones then join the groups.  So results do not depend on
+// A workgroup has one chunk of a sequence, for one block of up to 16 NH query heads of a key head.  Chunks are of at most c tiles, c the
+// smallest that gives all sequences together about kPagedChunks of them, but at least a.least: a join costs what a few tiles do.
+// A sequence's chunks are of equal length, so that a long one among short ones holds nobody up.  Pieces of a block meet in memory
+// (relaxed accesses of device scope, as the reductions exchange theirs), and whoever comes last joins them in their order: up
+// to eight at once, more in groups of about their root, whose last ones then join the groups.  So results do not depend on
 // who comes when.
 template <typename T, int DP, int NH> struct Geo {
   static constexpr bool BF = sizeof(T) == 2;
@@ -131,37 +133,50 @@ template <typename T, int DP, int NH> struct Geo {
 };
 
 typedef uint32_t U4 __attribute__((ext_vector_type(4)));
+typedef uint32_t U2 __attribute__((ext_vector_type(2)));
 typedef float F4 __attribute__((ext_vector_type(4)));
 typedef __bf16 B8 __attribute__((ext_vector_type(8)));
 
 constexpr int kSlots = 1024;   // page numbers of a stretch of a sequence that a workgroup holds
 
-// BYTES of a row from element d on, in pieces of AL bytes; pieces behind the row's end are read from `other`.
-template <typename T, int BYTES, int AL>
-__device__ __forceinline__ U4 load_piece(const T* row, uint32_t d, uint32_t dim, const T* other) {
+template <int BYTES> __device__ __forceinline__ U4 load_bytes(const void* p) {
   U4 r = {0u, 0u, 0u, 0u};
-  if constexpr (AL >= BYTES) {
-    const T* p = d < dim ? row + d : other;
-    if constexpr (BYTES == 16) r = *(const U4*)p;
-    else if constexpr (BYTES == 8) {
-      const uint2 t = *(const uint2*)p;
-      r.x = t.x;
-      r.y = t.y;
-    } else r.x = *(const uint32_t*)p;
-  } else {
+  if constexpr (BYTES == 16) r = *(const U4*)p;
+  else if constexpr (BYTES == 8) {
+    const U2 t = *(const U2*)p;
+    r.x = t.x;
+    r.y = t.y;
+  } else r.x = *(const uint32_t*)p;
+  return r;
+}
+
+// BYTES of a row from element d on, in pieces of AL bytes; what is behind the row's end is read from its beginning.
+template <typename T, int BYTES, int AL>
+__device__ __forceinline__ U4 load_piece(const T* row, uint32_t d, uint32_t dim) {
+  if constexpr (AL >= BYTES) return load_bytes<BYTES>(row + (d < dim ? d : 0u));
+  U4 r = {0u, 0u, 0u, 0u};
 #pragma unroll
-    for (int i = 0; i < BYTES / AL; ++i) {
-      const uint32_t e = d + (uint32_t)(i * AL / (int)sizeof(T));
-      const T* p = e < dim ? row + e : other;
-      if constexpr (AL == 4) r[i] = *(const uint32_t*)p;
-      else r[i / 2] |= (uint32_t)*(const uint16_t*)p << (16 * (i & 1));
-    }
+  for (int i = 0; i < BYTES / AL; ++i) {
+    const uint32_t e = d + (uint32_t)(i * AL / (int)sizeof(T));
+    const T* p = row + (e < dim ? e : 0u);
+    if constexpr (AL == 4) r[i] = *(const uint32_t*)p;
+    else r[i / 2] |= (uint32_t)*(const uint16_t*)p << (16 * (i & 1));
   }
   return r;
 }
 
-// What is read in place of the elements behind a head's last one: they count nothing, next to infinities too.
-__device__ __attribute__((aligned(16))) const uint32_t zeros[4] = {0u, 0u, 0u, 0u};
+// Zeros in place of the elements from dim on: they count nothing, next to infinities too.
+template <typename T, int AL>
+__device__ __forceinline__ U4 cut(U4 v, uint32_t d, uint32_t dim) {
+  constexpr uint32_t kEach = 4 / sizeof(T);
+  if constexpr (AL == 16) return d < dim ? v : U4{0u, 0u, 0u, 0u};
+#pragma unroll
+  for (uint32_t e = 0; e < 4u; ++e) {
+    if (d + e * kEach >= dim) v[e] = 0u;
+    else if (kEach == 2u && d + e * kEach + 1u >= dim) v[e] &= 0xFFFFu;
+  }
+  return v;
+}
 
 __device__ __forceinline__ float max_over_groups(float v) {
   v = fmaxf(v, __shfl_xor(v, 16, 64));
@@ -179,54 +194,89 @@ __device__ __forceinline__ uint32_t length_of(const PagedArgs& a, uint32_t s) {
 }
 
 // Tiles of a sequence, one at least: an empty one has zeros to write.
-__device__ __forceinline__ uint32_t tiles_of(const PagedArgs& a, uint32_t len) { return len == 0u ? 1u : (len - 1u) / a.tile + 1u; }
+template <uint32_t TILE> __device__ __forceinline__ uint32_t tiles_of(uint32_t len) { return len == 0u ? 1u : (len - 1u) / TILE + 1u; }
 
-// Workgroup w has the tiles from w * per on.  Found by the block together: the sequence that its first one falls into, and
-// how many tiles come before that sequence.
-struct Deal {
-  uint64_t per, before;
-  uint32_t seq;
+// Inclusive sums over the wave, every lane active: shifts inside rows of 16 lanes, then the rows' last lanes.
+__device__ __forceinline__ uint32_t sums_over_wave(uint32_t v) {
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xf, 0xf, false);
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xf, 0xf, false);
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xf, 0xf, false);
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xf, 0xf, false);
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xa, 0xf, false);
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, false);
+  return v;
+}
+
+// A workgroup's share.
+struct Chunk {
+  uint32_t seq, len, tiles;      // tiles: of the whole sequence
+  uint32_t pair;                 // its block of query heads
+  uint32_t part, parts, piece0;  // part of `parts`, whose pieces lie from piece0 on
 };
-__device__ __forceinline__ Deal deal(const PagedArgs& a, uint64_t (*shared)[8]) {
+
+// Found by the block together, as a sum over the sequences; false: there is none for this workgroup.
+template <uint32_t TILE>
+__device__ __forceinline__ bool find_chunk(const PagedArgs& a, uint32_t (*shared)[8], Chunk* w) {
   const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, each = (a.seqs + kBlock - 1u) / kBlock, from = threadIdx.x * each;
-  uint64_t mine = 0;
+  uint32_t tiles = 0;
   for (uint32_t i = 0; i < each; ++i)
-    if (from + i < a.seqs) mine += tiles_of(a, length_of(a, from + i));
-  uint64_t up = mine;   // inclusive sums over the wave, then over the waves
-  for (int m = 1; m < 64; m <<= 1) {
-    const uint64_t t = __shfl_up(up, m, 64);
-    if ((int)lane >= m) up += t;
-  }
-  if (lane == 63u) shared[0][wave] = up;
-  if (threadIdx.x == 0u) shared[1][0] = a.seqs;
+    if (from + i < a.seqs) tiles += tiles_of<TILE>(length_of(a, from + i));
+  tiles = sums_over_wave(tiles);
+  if (lane == 63u) shared[0][wave] = tiles;
   __syncthreads();
-  uint64_t total = 0, below = up - mine;
-  for (uint32_t w = 0; w < kBlock / 64u; ++w) {
-    if (w < wave) below += shared[0][w];
-    total += shared[0][w];
-  }
-  Deal d;
-  d.per = (total * a.pairs + a.workgroups - 1u) / a.workgroups;
-  const uint64_t at = blockIdx.x * d.per;
-  if (below * a.pairs <= at && at < (below + mine) * a.pairs) {
-    uint32_t s = from;
-    for (;; ++s) {
-      const uint64_t n = tiles_of(a, length_of(a, s));
-      if (at < (below + n) * a.pairs) break;
-      below += n;
+  const uint32_t all = (shared[0][0] + shared[0][1] + shared[0][2] + shared[0][3]) * a.pairs;
+  const uint32_t c = max(a.least, (all + kPagedChunks - 1u) / kPagedChunks);
+  uint32_t chunks = 0, split = 0;
+  for (uint32_t i = 0; i < each; ++i)
+    if (from + i < a.seqs) {
+      const uint32_t k = (tiles_of<TILE>(length_of(a, from + i)) + c - 1u) / c;
+      chunks += k;
+      split += k > 1u ? k : 0u;
     }
-    shared[1][0] = s;
-    shared[1][1] = below * a.pairs;
+  const uint32_t chunks_to = sums_over_wave(chunks), split_to = sums_over_wave(split);
+  if (lane == 63u) {
+    shared[1][wave] = chunks_to;
+    shared[1][4 + wave] = split_to;
+  }
+  if (threadIdx.x == 0u) shared[2][0] = a.seqs;
+  __syncthreads();
+  uint32_t before = chunks_to - chunks, split_before = split_to - split;
+  for (uint32_t i = 0; i < wave; ++i) {
+    before += shared[1][i];
+    split_before += shared[1][4 + i];
+  }
+  const uint32_t at = blockIdx.x;
+  if (before * a.pairs <= at && at < (before + chunks) * a.pairs) {
+    uint32_t s = from, len, t, k;
+    for (;; ++s) {
+      len = length_of(a, s);
+      t = tiles_of<TILE>(len);
+      k = (t + c - 1u) / c;
+      if (at < (before + k) * a.pairs) break;
+      before += k;
+      split_before += k > 1u ? k : 0u;
+    }
+    const uint32_t rel = at - before * a.pairs, pair = rel / k;
+    shared[2][0] = s;
+    shared[2][1] = len;
+    shared[2][2] = t;
+    shared[2][3] = pair;
+    shared[2][4] = rel - pair * k;
+    shared[2][5] = k;
+    shared[2][6] = split_before * a.pairs + pair * k;
   }
   __syncthreads();
-  d.seq = (uint32_t)shared[1][0];
-  d.before = shared[1][1];
-  return d;
+  if (shared[2][0] >= a.seqs) return false;
+  uint32_t r[7];
+#pragma unroll
+  for (int i = 0; i < 7; ++i) r[i] = (uint32_t)__builtin_amdgcn_readfirstlane((int)shared[2][i]);
+  *w = Chunk{r[0], r[1], r[2], r[3], r[4], r[5], r[6]};
+  return true;
 }
 
 // A piece: [16 NH heads][DP] sums of weights times values, [16 NH] maxima, [16 NH] sums of weights.
 template <int DP, int NH> constexpr uint32_t kPieceFloats = 16 * NH * DP + 32 * NH;
-constexpr uint32_t kMostPieces = 32;   // at once: the root of the largest grid is 23
+constexpr uint32_t kMostPieces = 32;   // at once: the root of the largest number of them is 23
 
 // Whether the calling workgroup is the last of `count` to come here.
 __device__ __forceinline__ bool last_of(uint32_t* ticket, uint32_t count, uint32_t* flag) {
@@ -242,372 +292,333 @@ __device__ __forceinline__ bool last_of(uint32_t* ticket, uint32_t count, uint32
 }
 
 template <typename T, int DP, int NH, bool PG, int AL>
-__global__ __launch_bounds__(kBlock, DP <= 128 && NH == 1 ? 2 : 1) void lt_paged_attention_kernel(const PagedArgs a) {
+__global__ __launch_bounds__(kBlock, DP <= 128 && NH == 1 && AL == 16 ? (DP == 64 ? 4 : 3) : 1) void lt_paged_attention_kernel(const PagedArgs a) {
   using G = Geo<T, DP, NH>;
   constexpr int KT = G::KT, NC = G::NC, NV = G::NV, NP = G::NP;
+  constexpr uint32_t kSize = sizeof(T);
   __shared__ int32_t pages[kSlots];
-  __shared__ uint64_t found[2][8];
-  __shared__ float tops[4][16 * NH], sums[4][16 * NH], factor[kMostPieces][16 * NH], total_of[16 * NH];
-  __shared__ uint32_t last_flag;
+  __shared__ uint32_t found[3][8], last_flag;
+  __shared__ float tops[4][16 * NH], sums[4][16 * NH], factor[kMostPieces][16 * NH], weight_of[kMostPieces][16 * NH], total_of[16 * NH];
   __shared__ __attribute__((aligned(16))) float meet[4][16 * G::PITCH];
   const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15u, g = lane >> 4;
-  const uint32_t group = a.heads / a.kv_heads, blocks = a.pairs / a.kv_heads;
-  const float scale = a.scale * kLog2e;
+
+  Chunk w;
+  if (a.split) {
+    if (!find_chunk<G::TILE>(a, found, &w)) return;
+  } else {
+    w.seq = blockIdx.x / a.pairs;
+    w.pair = blockIdx.x - w.seq * a.pairs;
+    w.len = length_of(a, w.seq);
+    w.tiles = tiles_of<G::TILE>(w.len);
+    w.part = w.piece0 = 0u;
+    w.parts = 1u;
+  }
+  const uint32_t group = a.heads / a.kv_heads, blocks = a.pairs / a.kv_heads, kh = w.pair / blocks, h0 = kh * group + (w.pair - kh * blocks) * 16u * NH,
+                 heads = min(16u * NH, (kh + 1u) * group - h0);
+  const uint32_t even = w.tiles / w.parts, odd = w.tiles - even * w.parts, t0 = w.part * even + min(w.part, odd), t1 = t0 + even + (w.part < odd ? 1u : 0u);
+  const uint32_t key_end = (uint32_t)min((uint64_t)t1 * G::TILE, (uint64_t)w.len);
   const int64_t value = (int64_t)a.kv_heads * a.rows.d * a.dim;   // from a key to its value
 
-  uint64_t at, end, before, per = 1;
-  uint32_t seq;
-  if (a.split) {
-    const Deal d = deal(a, found);
-    per = d.per;
-    if (d.seq >= a.seqs) return;
-    at = blockIdx.x * d.per;
-    end = at + d.per;
-    before = d.before;
-    seq = d.seq;
-  } else {
-    seq = blockIdx.x / a.pairs;
-    before = 0;
-    at = 0;
-    end = 1;
+  // B of the scores: lane (n, g) has head n's elements (4 c + g) CE .. + CE - 1; zeros behind the last head and the last element
+  U4 q[NH][NC];
+#pragma unroll
+  for (int b = 0; b < NH; ++b) {
+    const uint32_t h = 16u * b + n, to = h < heads ? a.dim : 0u;
+    const T* row = (const T*)a.q + (int64_t)w.seq * a.q_seq + (int64_t)(h0 + (h < heads ? h : 0u)) * a.q_head;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      const uint32_t d = (4u * c + g) * G::CE;
+      if (a.q_whole) q[b][c] = cut<T, 16>(load_piece<T, 16, 16>(row, d, to), d, to);
+      else q[b][c] = cut<T, (int)sizeof(T)>(load_piece<T, 16, (int)sizeof(T)>(row, d, to), d, to);
+    }
   }
 
-  while (at < end && seq < a.seqs) {
-    const uint32_t len = length_of(a, seq), tiles = tiles_of(a, len);
-    uint32_t pair, t0, t1;
-    if (a.split) {
-      const uint64_t rel = at - before;
-      pair = rel >> 32 ? (uint32_t)(rel / tiles) : (uint32_t)rel / tiles;
-      t0 = (uint32_t)(rel - (uint64_t)pair * tiles);
-      t1 = (uint32_t)(end - at < tiles - t0 ? t0 + (end - at) : tiles);
-    } else {
-      pair = blockIdx.x % a.pairs;
-      t0 = 0;
-      t1 = tiles;
-    }
-    const uint32_t kh = pair / blocks, h0 = kh * group + (pair - kh * blocks) * 16u * NH, heads = min(16u * NH, (kh + 1u) * group - h0);
+  F4 acc[NH][NV];
+  float top[NH], sum[NH];
+#pragma unroll
+  for (int b = 0; b < NH; ++b) {
+    top[b] = -INFINITY;
+    sum[b] = 0.0f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) acc[b][j] = F4{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+  const float scale = a.scale * kLog2e;
+  // (PG) bytes from a tile's first row to what this lane reads of its own
+  const uint32_t key_at = (n * a.dim + g * G::CE) * kSize, key_at0 = g * 16u, value_at0 = (n * NV < a.dim ? n * NV : 0u) * kSize;
 
-    // B of the scores: lane (n, g) has head n's elements (4 c + g) CE .. + CE - 1; zeros behind the last head and the last element
-    U4 q[NH][NC];
-    uint32_t dim = a.dim;
-    asm volatile("" : "+s"(dim));   // (what follows is done anew for every segment: kept over them, its conditions fill the scalar registers)
+  const uint32_t stretch = (uint32_t)min((uint64_t)(kSlots - 2) * a.rows.d / G::TILE, (uint64_t)0x7fffffffu / G::TILE);   // tiles whose pages fit
+  for (uint32_t first = t0; first < t1; first += stretch) {
+    const uint32_t k0 = first * G::TILE, k1 = (uint32_t)min((uint64_t)first * G::TILE + (uint64_t)stretch * G::TILE, (uint64_t)key_end);
+    if (k0 >= k1) break;   // (an empty sequence)
+    const uint32_t slot0 = divide(a.rows, k0), n_slots = divide(a.rows, k1 - 1u) - slot0 + 1u;
+    if (first != t0) __syncthreads();       // (the stretch before has been read)
+    for (uint32_t i = threadIdx.x; i < n_slots; i += kBlock) {
+      const int32_t p = a.table[(uint64_t)w.seq * a.slots + slot0 + i];
+      pages[i] = p >= 0 && (uint32_t)p < a.pages ? p : -1;
+    }
+    __syncthreads();
+
+    // Where a step's keys lie.  PG: a page holds whole tiles of 16, so a tile has one page: its first row, and how many
+    // of its keys there are.  Otherwise every lane finds its own keys.
+    const char* tile[KT];
+    uint32_t there[KT];
+    auto find_tiles = [&](uint32_t key0) {
 #pragma unroll
-    for (int b = 0; b < NH; ++b) {
-      const uint32_t h = 16u * b + n, to = h < heads ? dim : 0u;
-      const T* row = (const T*)a.q + (int64_t)seq * a.q_seq + (int64_t)(h0 + (h < heads ? h : 0u)) * a.q_head;
-#pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        if (a.q_whole) q[b][c] = load_piece<T, 16, 16>(row, (4u * c + g) * G::CE, to, (const T*)zeros);
-        else q[b][c] = load_piece<T, 16, (int)sizeof(T)>(row, (4u * c + g) * G::CE, to, (const T*)zeros);
+      for (int t = 0; t < KT; ++t) {
+        const uint32_t k = key0 + 16u * t, slot = divide(a.rows, k);
+        const int32_t p = __builtin_amdgcn_readfirstlane(k < k1 ? pages[slot - slot0] : -1);
+        there[t] = p >= 0 ? min(16u, k1 - k) : 0u;
+        tile[t] = (const char*)a.cache + (p >= 0 ? (((int64_t)p * 2 * a.kv_heads + kh) * a.rows.d + (k - slot * a.rows.d)) * a.dim * kSize : (int64_t)0);
       }
-    }
-
-    F4 acc[NH][NV];
-    float top[NH], sum[NH];
+    };
+    auto find_row = [&](uint32_t key, bool* ok) {
+      const uint32_t slot = divide(a.rows, key);
+      const int32_t p = key < k1 ? pages[slot - slot0] : -1;
+      *ok = p >= 0;
+      return p >= 0 ? (((int64_t)p * 2 * a.kv_heads + kh) * a.rows.d + (key - slot * a.rows.d)) * a.dim : (int64_t)0;
+    };
+    U4 k[KT][NC];
+    // (PG: a piece behind the row's end is the next row's, or the values' behind the last one)
+    auto load_keys = [&](uint32_t key0) {
 #pragma unroll
-    for (int b = 0; b < NH; ++b) {
-      top[b] = -INFINITY;
-      sum[b] = 0.0f;
+      for (int t = 0; t < KT; ++t) {
+        if constexpr (PG) {
+          const uint32_t at = n < there[t] ? key_at : key_at0;
 #pragma unroll
-      for (int j = 0; j < NV; ++j) acc[b][j] = F4{0.0f, 0.0f, 0.0f, 0.0f};
-    }
-
-    const uint32_t stretch = max(1u, (uint32_t)min((uint64_t)(kSlots - 2) * a.rows.d / G::TILE, (uint64_t)0x7fffffffu / G::TILE));   // tiles whose pages fit
-    for (uint32_t first = t0; first < t1; first += stretch) {
-      const uint32_t last = min(t1, first + stretch);
-      const uint32_t k0 = first * G::TILE, k1 = (uint32_t)min((uint64_t)last * G::TILE, (uint64_t)len);
-      if (k0 >= k1) break;   // (an empty sequence)
-      const uint32_t slot0 = divide(a.rows, k0), n_slots = divide(a.rows, k1 - 1u) - slot0 + 1u;
-      __syncthreads();       // (the stretch before has been read)
-      for (uint32_t i = threadIdx.x; i < n_slots; i += kBlock) {
-        const int32_t p = a.table[(uint64_t)seq * a.slots + slot0 + i];
-        pages[i] = p >= 0 && (uint32_t)p < a.pages ? p : -1;
-      }
-      __syncthreads();
-
-      // Where a step's keys lie.  PG: a page holds whole tiles of 16, so a tile has one page: its first row, and how many
-      // of its keys there are.  Otherwise every lane finds its own keys.
-      struct Where {
-        int64_t tile[KT];
-        uint32_t there[KT];
-      };
-      auto find_tiles = [&](uint32_t key0) {
-        Where w;
-#pragma unroll
-        for (int t = 0; t < KT; ++t) {
-          const uint32_t k = key0 + 16u * t;
-          uint32_t there = k < k1 ? min(16u, k1 - k) : 0u;
-          const uint32_t slot = divide(a.rows, k);
-          int32_t p = there ? pages[slot - slot0] : -1;
-          p = __builtin_amdgcn_readfirstlane(p);
-          if (p < 0) there = 0u;
-          w.there[t] = there;
-          w.tile[t] = there ? (((int64_t)p * 2 * a.kv_heads + kh) * a.rows.d + (k - slot * a.rows.d)) * a.dim : (int64_t)0;
-        }
-        return w;
-      };
-      auto find_row = [&](uint32_t key, bool* ok) {
-        const uint32_t slot = divide(a.rows, key);
-        const int32_t p = key < k1 ? pages[slot - slot0] : -1;
-        *ok = p >= 0;
-        return p >= 0 ? (((int64_t)p * 2 * a.kv_heads + kh) * a.rows.d + (key - slot * a.rows.d)) * a.dim : (int64_t)0;
-      };
-      auto load_keys = [&](const Where& w, uint32_t key0, U4 (&k)[KT][NC]) {
-#pragma unroll
-        for (int t = 0; t < KT; ++t) {
-          const T* row;
-          if constexpr (PG) row = (const T*)a.cache + w.tile[t] + (uint64_t)(min(n, max(w.there[t], 1u) - 1u) * a.dim);
-          else {
-            bool ok;
-            row = (const T*)a.cache + find_row(key0 + 16u * t + n, &ok);
-          }
-#pragma unroll
-          for (int c = 0; c < NC; ++c) k[t][c] = load_piece<T, 16, AL>(row, (4u * c + g) * G::CE, a.dim, (const T*)zeros);
-        }
-      };
-      auto load_values = [&](const Where& w, uint32_t key0, U4 (&v)[4 * KT][NP], uint32_t* there) {
-        *there = 0u;
-#pragma unroll
-        for (int i = 0; i < 4 * KT; ++i) {
-          const uint32_t t = i >> 2, r = 4u * g + (i & 3u);
-          const T* row;
+          for (int c = 0; c < NC; ++c) k[t][c] = load_bytes<16>(tile[t] + at + c * 64);
+        } else {
           bool ok;
-          if constexpr (PG) {
-            ok = r < w.there[t];
-            row = (const T*)a.cache + value + w.tile[t] + (uint64_t)(min(r, max(w.there[t], 1u) - 1u) * a.dim);
-          } else row = (const T*)a.cache + value + find_row(key0 + 16u * t + r, &ok);
-          *there |= ok ? 1u << i : 0u;
+          const T* row = (const T*)a.cache + find_row(key0 + 16u * t + n, &ok);
 #pragma unroll
-          for (int p = 0; p < NP; ++p) v[i][p] = load_piece<T, G::VB, AL>(row, n * NV + p * (G::VB / sizeof(T)), a.dim, row);   // (never stored)
+          for (int c = 0; c < NC; ++c) k[t][c] = load_piece<T, 16, AL>(row, (4u * c + g) * G::CE, a.dim);
         }
-      };
-
-      uint32_t key0 = k0 + wave * G::WK;
-      Where w = {};
-      U4 k[KT][NC];
-      if (key0 < k1) {
-        if constexpr (PG) w = find_tiles(key0);
-        load_keys(w, key0, k);
       }
-      for (; key0 < k1; key0 += G::TILE) {
-        U4 v[4 * KT][NP];
-        uint32_t there;
-        load_values(w, key0, v, &there);
-        // ---- scores
-        F4 s[NH][KT];
+    };
+
+    uint32_t key0 = k0 + wave * G::WK;
+    if (key0 < k1) {
+      if constexpr (PG) find_tiles(key0);
+      load_keys(key0);
+    }
+    for (; key0 < k1; key0 += G::TILE) {
+      U4 v[4 * KT][NP];
+      uint32_t mine = 0u;   // which of this lane's keys there are
+#pragma unroll
+      for (int i = 0; i < 4 * KT; ++i) {
+        const uint32_t t = i >> 2, r = 4u * g + (i & 3u);
+        bool ok;
+        if constexpr (PG) {
+          ok = r < there[t];
+          const uint32_t at = (ok ? r * a.dim * kSize : 0u) + value_at0;
+          const char* row = tile[t] + value * kSize;
+#pragma unroll
+          for (int p = 0; p < NP; ++p) v[i][p] = load_bytes<G::VB>(row + at + (NP == 1 || n * NV + p * (G::VB / kSize) < a.dim ? p * G::VB : 0));
+        } else {
+          const T* row = (const T*)a.cache + value + find_row(key0 + 16u * t + r, &ok);
+#pragma unroll
+          for (int p = 0; p < NP; ++p) v[i][p] = load_piece<T, G::VB, AL>(row, n * NV + p * (G::VB / kSize), a.dim);   // (what is behind the end is not stored)
+        }
+        mine |= ok ? 1u << i : 0u;
+      }
+      // ---- scores
+      if (a.dim != DP) {
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+          for (int c = 0; c < NC; ++c) k[t][c] = cut<T, AL>(k[t][c], (4u * c + g) * G::CE, a.dim);
+      }
+      F4 s[NH][KT];
+#pragma unroll
+      for (int b = 0; b < NH; ++b)
+#pragma unroll
+        for (int t = 0; t < KT; ++t) {
+          s[b][t] = F4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+          for (int c = 0; c < NC; ++c) {
+            if constexpr (G::BF) {
+              s[b][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(B8, k[t][c]), __builtin_bit_cast(B8, q[b][c]), s[b][t], 0, 0, 0);
+            } else {
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                s[b][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[t][c][e]), __uint_as_float(q[b][c][e]), s[b][t], 0, 0, 0);
+            }
+          }
+        }
+      if (key0 + G::TILE < k1) {
+        if constexpr (PG) find_tiles(key0 + G::TILE);
+        load_keys(key0 + G::TILE);
+      }
+      // ---- weights
+      const bool all = __all(mine == (1u << (4 * KT)) - 1u);
+#pragma unroll
+      for (int b = 0; b < NH; ++b) {
+        float mx = -INFINITY;
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            s[b][t][r] *= scale;
+            mx = fmaxf(mx, s[b][t][r]);
+          }
+        if (!all) {
+          mx = -INFINITY;
+#pragma unroll
+          for (int t = 0; t < KT; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              s[b][t][r] = mine >> (4 * t + r) & 1u ? s[b][t][r] : -INFINITY;
+              mx = fmaxf(mx, s[b][t][r]);
+            }
+        }
+        const float fresh = fmaxf(top[b], max_over_groups(mx)), safe = fresh == -INFINITY ? 0.0f : fresh, keep = power2(top[b] - safe);
+        top[b] = fresh;
+        float part = 0.0f;
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            s[b][t][r] = power2(s[b][t][r] - safe);
+            part += s[b][t][r];
+          }
+        sum[b] = fmaf(sum[b], keep, part);
+#pragma unroll
+        for (int j = 0; j < NV; ++j) acc[b][j] *= keep;
+      }
+      // ---- products
+      if (!all) {
+#pragma unroll
+        for (int i = 0; i < 4 * KT; ++i)
+#pragma unroll
+          for (int p = 0; p < NP; ++p)
+            if (!(mine >> i & 1u)) v[i][p] = U4{0u, 0u, 0u, 0u};
+      }
+      if constexpr (G::BF) {
+        B8 weight[NH];
 #pragma unroll
         for (int b = 0; b < NH; ++b)
 #pragma unroll
-          for (int t = 0; t < KT; ++t) {
-            s[b][t] = F4{0.0f, 0.0f, 0.0f, 0.0f};
+          for (int i = 0; i < 8; ++i) weight[b][i] = (__bf16)s[b][i >> 2][i & 3];
 #pragma unroll
-            for (int c = 0; c < NC; ++c) {
-              if constexpr (G::BF) {
-                s[b][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(B8, k[t][c]), __builtin_bit_cast(B8, q[b][c]), s[b][t], 0, 0, 0);
-              } else {
+        for (int j = 0; j < NV; ++j) {
+          constexpr uint32_t kLow = 0x05040100u, kHigh = 0x07060302u;
+          U4 f;
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                  s[b][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[t][c][e]), __uint_as_float(q[b][c][e]), s[b][t], 0, 0, 0);
-              }
-            }
-          }
-        const uint32_t next = key0 + G::TILE;
-        if (next < k1) {
-          if constexpr (PG) w = find_tiles(next);
-          load_keys(w, next, k);
+          for (int p = 0; p < 4; ++p)
+            f[p] = __builtin_amdgcn_perm(v[2 * p + 1][j / 8][j / 2 % 4], v[2 * p][j / 8][j / 2 % 4], (j & 1) ? kHigh : kLow);
+#pragma unroll
+          for (int b = 0; b < NH; ++b) acc[b][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(B8, f), weight[b], acc[b][j], 0, 0, 0);
         }
-        // ---- weights
-        const bool all = __all(there == (1u << (4 * KT)) - 1u);
+      } else {
 #pragma unroll
-        for (int b = 0; b < NH; ++b) {
-          float mx = -INFINITY;
+        for (int r = 0; r < 4; ++r)
 #pragma unroll
-          for (int t = 0; t < KT; ++t)
+          for (int j = 0; j < NV; ++j)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              s[b][t][r] *= scale;
-              mx = fmaxf(mx, s[b][t][r]);
-            }
-          if (!all) {
-            mx = -INFINITY;
-#pragma unroll
-            for (int t = 0; t < KT; ++t)
-#pragma unroll
-              for (int r = 0; r < 4; ++r) {
-                s[b][t][r] = there >> (4 * t + r) & 1u ? s[b][t][r] : -INFINITY;
-                mx = fmaxf(mx, s[b][t][r]);
-              }
-          }
-          const float fresh = fmaxf(top[b], max_over_groups(mx)), safe = fresh == -INFINITY ? 0.0f : fresh, keep = power2(top[b] - safe);
-          top[b] = fresh;
-          float part = 0.0f;
-#pragma unroll
-          for (int t = 0; t < KT; ++t)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              s[b][t][r] = power2(s[b][t][r] - safe);
-              part += s[b][t][r];
-            }
-          sum[b] = fmaf(sum[b], keep, part);
-#pragma unroll
-          for (int j = 0; j < NV; ++j) acc[b][j] *= keep;
-        }
-        // ---- products
-        if (!all) {
-#pragma unroll
-          for (int i = 0; i < 4 * KT; ++i)
-#pragma unroll
-            for (int p = 0; p < NP; ++p)
-              if (!(there >> i & 1u)) v[i][p] = U4{0u, 0u, 0u, 0u};
-        }
-        if constexpr (G::BF) {
-          B8 weight[NH];
-#pragma unroll
-          for (int b = 0; b < NH; ++b)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) weight[b][i] = (__bf16)s[b][i >> 2][i & 3];
-#pragma unroll
-          for (int j = 0; j < NV; ++j) {
-            constexpr uint32_t kLow = 0x05040100u, kHigh = 0x07060302u;
-            U4 f;
-#pragma unroll
-            for (int p = 0; p < 4; ++p)
-              f[p] = __builtin_amdgcn_perm(v[2 * p + 1][j / 8][j / 2 % 4], v[2 * p][j / 8][j / 2 % 4], (j & 1) ? kHigh : kLow);
-#pragma unroll
-            for (int b = 0; b < NH; ++b) acc[b][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(B8, f), weight[b], acc[b][j], 0, 0, 0);
-          }
-        } else {
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-#pragma unroll
-            for (int j = 0; j < NV; ++j)
-#pragma unroll
-              for (int b = 0; b < NH; ++b) acc[b][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[r][j / 4][j % 4]), s[b][0][r], acc[b][j], 0, 0, 0);
-        }
+            for (int b = 0; b < NH; ++b) acc[b][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[r][j / 4][j % 4]), s[b][0][r], acc[b][j], 0, 0, 0);
       }
-    }
-
-    // ---- the four waves' parts
-    __syncthreads();
-#pragma unroll
-    for (int b = 0; b < NH; ++b) {
-      const float all = sum_over_groups(sum[b]);
-      if (g == 0u) {
-        tops[wave][16 * b + n] = top[b];
-        sums[wave][16 * b + n] = all;
-      }
-    }
-    __syncthreads();
-    const bool whole = t0 == 0u && t1 == tiles;
-    // the pieces of this block of heads: piece i is workgroup w0 + i's, in the place of those that begin a block (the first) or of the others
-    const uint64_t tile0 = before + (uint64_t)pair * tiles;
-    const uint32_t w0 = whole ? 0u : (uint32_t)(tile0 / per), pieces = whole ? 1u : (uint32_t)((tile0 + tiles - 1u) / per) - w0 + 1u, mine = blockIdx.x - w0;
-    auto place_of = [&](uint32_t i) { return i == 0u ? 2u * w0 + 1u : 2u * (w0 + i); };
-    auto piece = [&](uint32_t i) { return a.parts + (uint64_t)place_of(i) * kPieceFloats<DP, NH>; };
-    auto put = [&](uint32_t hh, uint32_t d, const F4& o, float inv) {
-      T* y = (T*)a.out + ((uint64_t)seq * a.heads + h0 + hh) * a.dim + d;
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (d + e < a.dim) y[e] = (T)(o[e] * inv);
-    };
-    auto inverse = [](float total) { return total > 0.0f || total != total ? 1.0f / total : 0.0f; };
-#pragma unroll
-    for (int b = 0; b < NH; ++b) {
-      auto common = [&](uint32_t h) {
-        const float t = fmaxf(fmaxf(tops[0][h], tops[1][h]), fmaxf(tops[2][h], tops[3][h]));
-        return t == -INFINITY ? 0.0f : t;
-      };
-      const float f = power2(top[b] - common(16u * b + n));
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-#pragma unroll
-        for (int j = 0; j < NV; j += 4)
-          *(F4*)&meet[wave][n * G::PITCH + (4u * g + r) * NV + j] = F4{acc[b][j][r] * f, acc[b][j + 1][r] * f, acc[b][j + 2][r] * f, acc[b][j + 3][r] * f};
-      __syncthreads();
-      for (uint32_t i = threadIdx.x; i < 16u * DP / 4u; i += kBlock) {
-        const uint32_t h = i / (DP / 4u), d = i % (DP / 4u) * 4u, hh = 16u * b + h;
-        if (hh >= heads || d >= a.dim) continue;
-        F4 o = *(const F4*)&meet[0][h * G::PITCH + d];
-#pragma unroll
-        for (int x = 1; x < 4; ++x) o += *(const F4*)&meet[x][h * G::PITCH + d];
-        if (whole) {
-          const float t = common(hh);
-          float total = 0.0f;
-#pragma unroll
-          for (int x = 0; x < 4; ++x) total = fmaf(sums[x][hh], power2(tops[x][hh] - t), total);
-          put(hh, d, o, inverse(total));
-        } else {
-          publish4(piece(mine) + hh * DP + d, make_float4(o[0], o[1], o[2], o[3]));
-        }
-      }
-      __syncthreads();
-    }
-    if (!whole) {
-      if (threadIdx.x < heads) {
-        const uint32_t h = threadIdx.x;
-        const float t = fmaxf(fmaxf(tops[0][h], tops[1][h]), fmaxf(tops[2][h], tops[3][h])), safe = t == -INFINITY ? 0.0f : t;
-        float total = 0.0f;
-        for (int x = 0; x < 4; ++x) total = fmaf(sums[x][h], power2(tops[x][h] - safe), total);
-        publish(piece(mine) + 16 * NH * DP + h, t);
-        publish(piece(mine) + 16 * NH * DP + 16 * NH + h, total);
-      }
-      // pieces first, first + step, ... : joined, into the output or into the first one's place
-      auto join = [&](uint32_t first, uint32_t step, uint32_t count, bool out) {
-        for (uint32_t i = threadIdx.x; i < count * 16u * NH; i += kBlock) {
-          const uint32_t p = i / (16u * NH), h = i % (16u * NH);
-          if (h < heads) factor[p][h] = published(piece(first + p * step) + 16 * NH * DP + h);
-        }
-        __syncthreads();
-        if (threadIdx.x < heads) {
-          const uint32_t h = threadIdx.x;
-          float t = -INFINITY, total = 0.0f;
-          for (uint32_t p = 0; p < count; ++p) t = fmaxf(t, factor[p][h]);
-          const float safe = t == -INFINITY ? 0.0f : t;
-          for (uint32_t p = 0; p < count; ++p) {
-            const float f = power2(factor[p][h] - safe);
-            factor[p][h] = f;
-            total = fmaf(published(piece(first + p * step) + 16 * NH * DP + 16 * NH + h), f, total);
-          }
-          total_of[h] = total;
-          if (!out) {
-            publish(piece(first) + 16 * NH * DP + h, t);
-            publish(piece(first) + 16 * NH * DP + 16 * NH + h, total);
-          }
-        }
-        __syncthreads();
-        for (uint32_t i = threadIdx.x; i < heads * DP / 4u; i += kBlock) {
-          const uint32_t hh = i / (DP / 4u), d = i % (DP / 4u) * 4u;
-          if (d >= a.dim) continue;
-          F4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 4
-          for (uint32_t p = 0; p < count; ++p) {
-            const float4 t = published4(piece(first + p * step) + hh * DP + d);
-            const float f = factor[p][hh];
-            o = F4{fmaf(t.x, f, o[0]), fmaf(t.y, f, o[1]), fmaf(t.z, f, o[2]), fmaf(t.w, f, o[3])};
-          }
-          if (out) put(hh, d, o, inverse(total_of[hh]));
-          else publish4(piece(first) + hh * DP + d, make_float4(o[0], o[1], o[2], o[3]));
-        }
-      };
-      uint32_t each = pieces;
-      if (pieces > 8u)
-        for (each = 3u; each * each < pieces;) ++each;
-      const uint32_t first = mine / each * each, groups = (pieces + each - 1u) / each;
-      if (last_of(a.tickets + place_of(first), min(each, pieces - first), &last_flag)) {
-        join(first, 1u, min(each, pieces - first), groups == 1u);
-        // (the second piece begins no group: its ticket is that of the groups)
-        if (groups > 1u && last_of(a.tickets + place_of(1u), groups, &last_flag)) join(0u, each, groups, true);
-      }
-      __syncthreads();   // (factor and the flag are free)
-    }
-
-    if (!a.split) break;
-    at += t1 - t0;
-    if (at == before + (uint64_t)tiles * a.pairs) {
-      before = at;
-      ++seq;
     }
   }
+
+  // ---- the four waves' parts
+#pragma unroll
+  for (int b = 0; b < NH; ++b) {
+    const float all = sum_over_groups(sum[b]);
+    if (g == 0u) {
+      tops[wave][16 * b + n] = top[b];
+      sums[wave][16 * b + n] = all;
+    }
+  }
+  __syncthreads();
+  const bool whole = w.parts == 1u;
+  auto piece = [&](uint32_t i) { return a.parts + (uint64_t)(w.piece0 + i) * kPieceFloats<DP, NH>; };
+  auto put = [&](uint32_t hh, uint32_t d, const F4& o, float total) {
+    const float inv = total > 0.0f || total != total ? 1.0f / total : 0.0f;
+    T* y = (T*)a.out + ((uint64_t)w.seq * a.heads + h0 + hh) * a.dim + d;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (d + e < a.dim) y[e] = (T)(o[e] * inv);
+  };
+  auto common = [&](uint32_t h) { return fmaxf(fmaxf(tops[0][h], tops[1][h]), fmaxf(tops[2][h], tops[3][h])); };
+  auto safe_of = [](float t) { return t == -INFINITY ? 0.0f : t; };
+  auto total_at = [&](uint32_t h) {
+    const float t = safe_of(common(h));
+    float total = 0.0f;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) total = fmaf(sums[x][h], power2(tops[x][h] - t), total);
+    return total;
+  };
+#pragma unroll
+  for (int b = 0; b < NH; ++b) {
+    const float f = power2(top[b] - safe_of(common(16u * b + n)));
+    if (b > 0) __syncthreads();
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int j = 0; j < NV; j += 4)
+        *(F4*)&meet[wave][n * G::PITCH + (4u * g + r) * NV + j] = F4{acc[b][j][r] * f, acc[b][j + 1][r] * f, acc[b][j + 2][r] * f, acc[b][j + 3][r] * f};
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < 16u * DP / 4u; i += kBlock) {
+      const uint32_t h = i / (DP / 4u), d = i % (DP / 4u) * 4u, hh = 16u * b + h;
+      if (hh >= heads || d >= a.dim) continue;
+      F4 o = *(const F4*)&meet[0][h * G::PITCH + d];
+#pragma unroll
+      for (int x = 1; x < 4; ++x) o += *(const F4*)&meet[x][h * G::PITCH + d];
+      if (whole) put(hh, d, o, total_at(hh));
+      else publish4(piece(w.part) + hh * DP + d, make_float4(o[0], o[1], o[2], o[3]));
+    }
+  }
+  if (whole) return;
+  if (threadIdx.x < heads) {
+    publish(piece(w.part) + 16 * NH * DP + threadIdx.x, common(threadIdx.x));
+    publish(piece(w.part) + 16 * NH * DP + 16 * NH + threadIdx.x, total_at(threadIdx.x));
+  }
+  // pieces first, first + step, ... : joined, into the output or into the first one's place
+  auto join = [&](uint32_t first, uint32_t step, uint32_t count, bool out) {
+    for (uint32_t i = threadIdx.x; i < count * 16u * NH; i += kBlock) {
+      const uint32_t p = i / (16u * NH), h = i % (16u * NH);
+      if (h >= heads) continue;
+      factor[p][h] = published(piece(first + p * step) + 16 * NH * DP + h);
+      weight_of[p][h] = published(piece(first + p * step) + 16 * NH * DP + 16 * NH + h);
+    }
+    __syncthreads();
+    if (threadIdx.x < heads) {
+      const uint32_t h = threadIdx.x;
+      float t = -INFINITY, total = 0.0f;
+      for (uint32_t p = 0; p < count; ++p) t = fmaxf(t, factor[p][h]);
+      for (uint32_t p = 0; p < count; ++p) {
+        const float f = power2(factor[p][h] - safe_of(t));
+        factor[p][h] = f;
+        total = fmaf(weight_of[p][h], f, total);
+      }
+      total_of[h] = total;
+      if (!out) {
+        publish(piece(first) + 16 * NH * DP + h, t);
+        publish(piece(first) + 16 * NH * DP + 16 * NH + h, total);
+      }
+    }
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < heads * DP / 4u; i += kBlock) {
+      const uint32_t hh = i / (DP / 4u), d = i % (DP / 4u) * 4u;
+      if (d >= a.dim) continue;
+      F4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 8
+      for (uint32_t p = 0; p < count; ++p) {
+        const float4 t = published4(piece(first + p * step) + hh * DP + d);
+        const float f = factor[p][hh];
+        o = F4{fmaf(t.x, f, o[0]), fmaf(t.y, f, o[1]), fmaf(t.z, f, o[2]), fmaf(t.w, f, o[3])};
+      }
+      if (out) put(hh, d, o, total_of[hh]);
+      else publish4(piece(first) + hh * DP + d, make_float4(o[0], o[1], o[2], o[3]));
+    }
+  };
+  uint32_t each = w.parts;
+  if (w.parts > 8u)
+    for (each = 3u; each * each < w.parts;) ++each;
+  const uint32_t first = w.part / each * each, groups = (w.parts + each - 1u) / each;
+  if (!last_of(a.tickets + w.piece0 + first, min(each, w.parts - first), &last_flag)) return;
+  join(first, 1u, min(each, w.parts - first), groups == 1u);
+  // (the second piece begins no group: its ticket is that of the groups)
+  if (groups > 1u && last_of(a.tickets + w.piece0 + 1u, groups, &last_flag)) join(0u, each, groups, true);
 }
 
 template <typename T, int DP, int NH>
@@ -633,7 +644,7 @@ hipError_t launch_paged(const void* args, hipStream_t s) {
   PagedArgs a = *(const PagedArgs*)args;
   if (a.seqs == 0) return hipSuccess;
   if (!a.q || !a.lengths || !a.out || (a.capacity > 0 && (!a.cache || !a.table)) || a.dim == 0 || a.dim > a.padded || a.kv_heads == 0 || a.heads % a.kv_heads != 0 ||
-      a.rows.d == 0 || a.workgroups == 0 || (a.split && (!a.parts || !a.tickets || a.workgroups > kMaxPagedWorkgroups)) || a.tile != (a.dtype == kF32 ? 64u : 128u) ||
+      a.rows.d == 0 || a.workgroups == 0 || (a.split && (!a.parts || !a.tickets || a.least == 0)) || a.tile != (a.dtype == kF32 ? 64u : 128u) ||
       a.blocks_of > (a.padded == 256u ? 16u : 32u))
     return hipErrorInvalidValue;
   const int64_t size = a.dtype == kF32 ? 4 : 2;

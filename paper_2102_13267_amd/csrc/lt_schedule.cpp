@@ -57,8 +57,7 @@ bool row_op_total(const Launch& l) { return l.kind == L_ROWOP && ((const ltk::Ro
 
 uint64_t paged_tickets(const Launch& l) {
   if (l.kind != L_PAGED) return 0;
-  const ltk::PagedArgs* a = (const ltk::PagedArgs*)l.args.data();
-  return a->split ? 2ull * a->workgroups : 0;
+  return ((const ltk::PagedArgs*)l.args.data())->pieces;
 }
 
 void schedule_streams(Plan* plan) {
