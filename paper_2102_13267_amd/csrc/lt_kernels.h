@@ -295,9 +295,9 @@ struct Rotary {
   uint32_t back;                // turn the other way
 };
 
-// n / d for n < 2^31, 1 <= d < 2^31: the product with ceil(2^(31 + shift) / d), shift = ceil(log2 d)
+// n / d for n < 2^31, 1 <= d <= 2^31: the product with ceil(2^(31 + shift) / d), shift = ceil(log2 d)
 struct Divider {
-  uint32_t d = 1, magic = 1u << 31, shift = 0;
+  uint32_t d, magic, shift;
   void set(uint32_t div) {
     d = div;
     shift = 0;
@@ -312,9 +312,13 @@ struct RopeArgs {
   const void* x;
   const int32_t* positions;
   void* out;
-  uint64_t tokens;
-  uint32_t dtype, heads, dim, inner, n_pos, pad;
+  uint64_t tokens;              // below 2^31
+  uint32_t dtype, dim;
+  Divider heads, inner, n_pos;
+  uint32_t whole;               // inner is all of the tokens
   int64_t s_outer, s_inner, s_head;
+  Divider slots, pairs;         // of a row: these three are the launcher's
+  uint32_t rows_each, pad;
   Rotary rotary;
 };
 

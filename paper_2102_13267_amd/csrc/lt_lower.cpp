@@ -1816,10 +1816,11 @@ struct Lowering {
     ltk::RopeArgs args{};
     args.dtype = an->dtype;
     args.dim = (uint32_t)an->dims[an->rank - 1];
-    args.heads = (uint32_t)an->dims[an->rank - 2];
-    args.tokens = (uint64_t)numel(an->dims, an->rank - 2);
-    args.n_pos = (uint32_t)std::max<int64_t>(1, count(out_shape(rins[a][1])));
-    args.inner = (uint32_t)x.inner;
+    args.heads.set((uint32_t)std::max<int64_t>(1, an->dims[an->rank - 2]));
+    args.tokens = an->dims[an->rank - 2] == 0 ? 0 : (uint64_t)numel(an->dims, an->rank - 2);
+    args.n_pos.set((uint32_t)std::max<int64_t>(1, count(out_shape(rins[a][1]))));
+    args.inner.set((uint32_t)x.inner);
+    args.whole = (uint64_t)x.inner >= args.tokens;
     args.s_outer = x.s_outer;
     args.s_inner = x.s_inner;
     args.s_head = x.s_head;

@@ -16,8 +16,6 @@ namespace {
 constexpr uint32_t kBlock = 256;
 constexpr float kLog2e = 1.44269504088896340736f;
 
-__device__ __forceinline__ uint32_t divide(const Divider& d, uint32_t n) { return (uint32_t)(((uint64_t)n * d.magic) >> (31u + d.shift)); }
-
 // ---- new rows ------------------------------------------------------------------------------------
 __global__ __launch_bounds__(kBlock) void lt_cache_copy_kernel(const AppendArgs a) {
   const uint64_t n = a.cache_elems * (a.cache_dtype == kF32 ? 4u : 2u), stride = (uint64_t)gridDim.x * kBlock * 16u;

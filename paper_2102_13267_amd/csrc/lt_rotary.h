@@ -1,4 +1,9 @@
-// What the kernels of rotary positions share: a pair's turn, and rotating with it.
+// What the kernels of rotary positions share: a pair's turn, and rows of heads that are read, rotated and written in
+// pieces.
+//
+// A row (a token's head) is made of slots, a thread each: rotated ones first, then the rest.  Half layout: a slot has V elements at
+// V i and their partners at n / 2 + V i; interleaved: V / 2 pairs at V i.  A workgroup takes rows in a row, so that all heads of a token
+// share its turns: they are computed once a workgroup, into LDS, while the rows are on their way.
 #ifndef LT_ROTARY_H_
 #define LT_ROTARY_H_
 
@@ -8,15 +13,19 @@
 
 namespace ltk {
 
-struct Turn {
+constexpr uint32_t kRowBlock = 256;       // threads of a workgroup
+constexpr uint32_t kMaxTurns = 4096;      // of its tokens' pairs: 32 KB of LDS
+constexpr int kMaxRows = 4;               // of a thread, all of them on their way at once
+
+struct __attribute__((aligned(8))) Turn {
   float c, s;   // amplitude * cos, amplitude * sin
 };
 
-// The turn of pair i at a position.  Quarter turns in 64 bits: the whole ones go, their last two bits are the quadrant,
+// The turn of a pair at a position.  Quarter turns in 64 bits: the whole ones go, their last two bits are the quadrant,
 // and the rest, half a quarter at most, is exact in 32 bits to 2^-25 of itself.  On |x| <= pi / 4 the
 // Taylor polynomials to x^9 and x^10 err by 2e-9 and 1e-10, below half a unit of the last place.
-__device__ __forceinline__ Turn turn_of(const Rotary& r, int32_t position, uint32_t i) {
-  const double q = (double)position * r.turns[i];
+__device__ __forceinline__ Turn turn_of(const Rotary& r, int32_t position, uint32_t pair) {
+  const double q = (double)position * r.turns[pair];
   const double whole = rint(q);
   const int quadrant = (int)whole;
   const float x = (float)(q - whole) * 1.57079632679489662f, xx = x * x;
@@ -37,6 +46,91 @@ __device__ __forceinline__ void rotate(const Turn& t, float x, float y, float* a
 
 __device__ __forceinline__ float to_float(float v) { return v; }
 __device__ __forceinline__ float to_float(__bf16 v) { return (float)v; }
+
+__host__ __device__ inline uint32_t divide(const Divider& d, uint32_t n) { return (uint32_t)(((uint64_t)n * d.magic) >> (31u + d.shift)); }
+
+// V elements that lie next to each other, as they are in memory.
+template <typename T, int V> struct Piece { typedef T type __attribute__((ext_vector_type(V))); };
+template <typename T> struct Piece<T, 1> { typedef T type; };
+
+template <typename T, int V> __device__ __forceinline__ float element(const typename Piece<T, V>::type& p, int i) {
+  if constexpr (V == 1) return to_float(p);
+  else return to_float(p[i]);
+}
+template <typename T, int V> __device__ __forceinline__ typename Piece<T, V>::type rounded(const float (&v)[V]) {
+  typename Piece<T, V>::type p;
+  if constexpr (V == 1) p = (T)v[0];
+  else
+#pragma unroll
+    for (int i = 0; i < V; ++i) p[i] = (T)v[i];
+  return p;
+}
+
+// A slot of a row on its way: its elements and, in the half layout, their partners.
+template <typename T, int V, bool IL> struct Slot {
+  typename Piece<T, V>::type a, b;
+};
+
+// Where slot u of a row is: its first element, and (half layout) its partners' first.
+template <int V, bool IL> __device__ __forceinline__ uint32_t slot_at(const Rotary& r, uint32_t u, bool* turned) {
+  const uint32_t rotated = IL ? r.dims / V : r.dims / 2u / V;
+  *turned = u < rotated;
+  return *turned ? u * V : r.dims + (u - rotated) * V;
+}
+
+template <typename T, int V, bool IL> __device__ __forceinline__ void load_slot(const T* row, const Rotary& r, uint32_t at, bool turned, Slot<T, V, IL>* s) {
+  typedef typename Piece<T, V>::type P;
+  s->a = *(const P*)(row + at);
+  if (!IL && turned) s->b = *(const P*)(row + at + r.dims / 2u);
+}
+
+// turns: those of the row's token, one for each pair; null: nothing is rotated.  PAST: results larger than the last-level cache
+// are stored past it.
+template <typename C, typename T, int V, bool IL, bool PAST>
+__device__ __forceinline__ void store_slot(C* row, const Rotary& r, uint32_t at, bool turned, const Slot<T, V, IL>& s, const Turn* turns) {
+  typedef typename Piece<C, V>::type P;
+  float a[V], b[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) a[i] = element<T, V>(s.a, i);
+  if (!IL && turned) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) b[i] = element<T, V>(s.b, i);
+  }
+  if (turned && turns) {
+    if constexpr (IL) {
+#pragma unroll
+      for (int i = 0; i < V / 2; ++i) rotate(turns[at / 2u + i], a[2 * i], a[2 * i + 1], &a[2 * i], &a[2 * i + 1]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i) rotate(turns[at + i], a[i], b[i], &a[i], &b[i]);
+    }
+  }
+  const P p = rounded<C, V>(a);
+  if constexpr (PAST) __builtin_nontemporal_store(p, (P*)(row + at));
+  else *(P*)(row + at) = p;
+  if (!IL && turned) {
+    const P q = rounded<C, V>(b);
+    if constexpr (PAST) __builtin_nontemporal_store(q, (P*)(row + at + r.dims / 2u));
+    else *(P*)(row + at + r.dims / 2u) = q;
+  }
+}
+
+// Elements of a piece: the most, up to `most`, that row starts (all multiples of `aligned` elements apart and from 16 bytes),
+// the rotated part and the rest are made of; 0: not even one piece fits the layout (interleaved pairs at odd places).
+inline uint32_t piece_of(const Rotary& r, uint32_t dim, uint64_t aligned, uint32_t most) {
+  uint32_t v = most;
+  const uint32_t part = r.interleaved ? r.dims : r.dims / 2u;
+  while (v > 1u && (part % v != 0u || (dim - r.dims) % v != 0u || aligned % v != 0u)) v /= 2u;
+  return r.interleaved && v < 2u ? 0u : v;
+}
+inline uint32_t slots_of(const Rotary& r, uint32_t dim, uint32_t v) { return (r.interleaved ? r.dims / v : r.dims / 2u / v) + (dim - r.dims) / v; }
+
+// The largest power of two, up to 16, that divides all of a row's strides (in elements) and, in bytes, its address.
+inline uint64_t row_alignment(const void* p, uint64_t size, int64_t s0, int64_t s1, int64_t s2) {
+  uint64_t bits = (uint64_t)s0 | (uint64_t)s1 | (uint64_t)s2 | 16u | ((uint64_t)(uintptr_t)p / size);
+  if ((uintptr_t)p % size != 0u) return 1;
+  return bits & (~bits + 1u);
+}
 
 }  // namespace ltk
 #endif
