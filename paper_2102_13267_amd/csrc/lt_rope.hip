@@ -2,7 +2,13 @@
 // position and the pair's frequency give, and the rest as it is; the gradient turns back.
 //
 // Bound by memory: every element is read and written once.  16 bytes a lane where rows allow, up to four rows of a thread on
-// their way while the workgroup computes its tokens' turns (lt_rotary.h); computed per thread and pair they took half of the time.
+// their way while the workgroup computes its tokens' turns (lt_rotary.h).  65536 tokens of 32 x 128 bf16: 172 us, 6.2 TB/s (one thread
+// a pair, each with a turn of its own, 550).
+//
+// Past the last-level cache (256 MB) goes what does not fit it: reads where operand and result together are larger, two rows a
+// thread (134 MB + 134 MB alone 51.0 -> 46.0 us, with scores behind it 1414 -> 1405), results where they alone are.  Smaller ones are plain: 33 MB + 33 MB
+// among other data that fills the cache take 16.8 us a launch, 12.1 with results stored past it, but whoever reads the result next loses more
+// (an elementwise pass behind it 26.6 / 29.1, scores, softmax and product 308 / 320).
 #include <hip/hip_runtime.h>
 
 #include "lt_launch.h"
@@ -11,7 +17,9 @@
 namespace ltk {
 namespace {
 
-template <typename T, int V, bool IL, bool PAST>
+enum Past { kNothingPast, kReadsPast, kAllPast };
+
+template <typename T, int V, bool IL, Past PAST>
 __global__ __launch_bounds__(kRowBlock) void lt_rope_kernel(const RopeArgs a) {
   __shared__ Turn turns[kMaxTurns];
   const uint32_t pairs = a.rotary.dims / 2u, lane = divide(a.slots, threadIdx.x), u = threadIdx.x - lane * a.slots.d, lanes = kRowBlock / a.slots.d;
@@ -29,7 +37,7 @@ __global__ __launch_bounds__(kRowBlock) void lt_rope_kernel(const RopeArgs a) {
     if (r >= n || lane >= lanes) continue;
     const uint32_t h = head0 + r - token[i] * a.heads.d, t = token0 + token[i], o = a.s_outer == 0 ? 0u : divide(a.inner, t);
     const T* row = (const T*)a.x + (int64_t)o * a.s_outer + (int64_t)(a.whole ? t : t - divide(a.inner, t) * a.inner.d) * a.s_inner + (int64_t)h * a.s_head;
-    load_slot<T, V, IL>(row, a.rotary, at, turned, &s[i]);
+    load_slot<T, V, IL, PAST != kNothingPast>(row, a.rotary, at, turned, &s[i]);
   }
   const uint32_t tokens = divide(a.heads, head0 + n - 1u) + 1u;
   for (uint32_t i = threadIdx.x; i < tokens * pairs; i += kRowBlock) {
@@ -41,7 +49,7 @@ __global__ __launch_bounds__(kRowBlock) void lt_rope_kernel(const RopeArgs a) {
   for (int i = 0; i < kMaxRows; ++i) {
     const uint32_t r = lane + i * lanes;
     if (r >= n || lane >= lanes) continue;
-    store_slot<T, T, V, IL, PAST>((T*)a.out + (row0 + r) * a.dim, a.rotary, at, turned, s[i], turns + token[i] * pairs);
+    store_slot<T, T, V, IL, PAST == kAllPast>((T*)a.out + (row0 + r) * a.dim, a.rotary, at, turned, s[i], turns + token[i] * pairs);
   }
 }
 
@@ -69,17 +77,20 @@ __global__ __launch_bounds__(kRowBlock) void lt_rope_any_kernel(const RopeArgs a
 }
 
 template <typename T, int V, bool IL>
-void launch_rows(const RopeArgs& a, uint32_t grid, bool past, hipStream_t s) {
-  if (past) LT_LAUNCH((lt_rope_kernel<T, V, IL, true>), dim3(grid), dim3(kRowBlock), s, a);
-  else LT_LAUNCH((lt_rope_kernel<T, V, IL, false>), dim3(grid), dim3(kRowBlock), s, a);
+void launch_rows(const RopeArgs& a, uint32_t grid, Past past, hipStream_t s) {
+  if (past == kAllPast) LT_LAUNCH((lt_rope_kernel<T, V, IL, kAllPast>), dim3(grid), dim3(kRowBlock), s, a);
+  else if (past == kReadsPast) LT_LAUNCH((lt_rope_kernel<T, V, IL, kReadsPast>), dim3(grid), dim3(kRowBlock), s, a);
+  else LT_LAUNCH((lt_rope_kernel<T, V, IL, kNothingPast>), dim3(grid), dim3(kRowBlock), s, a);
 }
 
 template <typename T>
 hipError_t launch_rope_of(RopeArgs a, hipStream_t s) {
   const uint64_t rows = a.tokens * a.heads.d, aligned = row_alignment(a.x, sizeof(T), a.s_outer, a.s_inner, a.s_head);
   const uint32_t v = piece_of(a.rotary, a.dim, aligned, 16u / sizeof(T)), slots = v ? slots_of(a.rotary, a.dim, v) : 0u, pairs = a.rotary.dims / 2u;
+  const uint64_t bytes = rows * a.dim * sizeof(T), cache = (uint64_t)256 << 20;
+  const Past past = bytes >= cache ? kAllPast : 2 * bytes >= cache ? kReadsPast : kNothingPast;
   // rows a thread: four where that leaves four workgroups a compute unit, and the tokens' turns fit
-  a.rows_each = kMaxRows;
+  a.rows_each = past == kNothingPast ? kMaxRows : 2u;
   if (v && slots <= kRowBlock) {
     const uint32_t lanes = kRowBlock / slots;
     auto tokens = [&](uint32_t each) { return (lanes * each + a.heads.d - 2u) / a.heads.d + 1u; };
@@ -88,7 +99,6 @@ hipError_t launch_rope_of(RopeArgs a, hipStream_t s) {
       a.slots.set(slots);
       a.pairs.set(pairs);
       const uint64_t grid = (rows + lanes * a.rows_each - 1) / (lanes * a.rows_each);
-      const bool past = rows * a.dim * sizeof(T) >= ((uint64_t)256 << 20);
       if (grid < ((uint64_t)1 << 31)) {
         if (a.rotary.interleaved) {
           if (v * sizeof(T) == 16u) launch_rows<T, 16 / sizeof(T), true>(a, (uint32_t)grid, past, s);

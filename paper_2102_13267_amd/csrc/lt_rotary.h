@@ -78,10 +78,16 @@ template <int V, bool IL> __device__ __forceinline__ uint32_t slot_at(const Rota
   return *turned ? u * V : r.dims + (u - rotated) * V;
 }
 
-template <typename T, int V, bool IL> __device__ __forceinline__ void load_slot(const T* row, const Rotary& r, uint32_t at, bool turned, Slot<T, V, IL>* s) {
+// PAST: what does not fit the last-level cache together with its result is read past it
+template <typename T, int V, bool IL, bool PAST> __device__ __forceinline__ void load_slot(const T* row, const Rotary& r, uint32_t at, bool turned, Slot<T, V, IL>* s) {
   typedef typename Piece<T, V>::type P;
-  s->a = *(const P*)(row + at);
-  if (!IL && turned) s->b = *(const P*)(row + at + r.dims / 2u);
+  if constexpr (PAST) {
+    s->a = __builtin_nontemporal_load((const P*)(row + at));
+    if (!IL && turned) s->b = __builtin_nontemporal_load((const P*)(row + at + r.dims / 2u));
+  } else {
+    s->a = *(const P*)(row + at);
+    if (!IL && turned) s->b = *(const P*)(row + at + r.dims / 2u);
+  }
 }
 
 // turns: those of the row's token, one for each pair; null: nothing is rotated.  PAST: results larger than the last-level cache
