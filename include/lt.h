@@ -110,7 +110,7 @@ typedef enum {
  * of the sequence.  Positions behind the table's slots and those in pages that are not the cache's do not count;
  * a sequence with nothing that counts (length 0 or negative) gets zeros.  Default scale: 1 / sqrt(dim).
  *
- * LT_ERR_SHAPE where pages * rows, slots * rows or tokens is 2^31 or more.
+ * LT_ERR_SHAPE where pages * rows, slots * rows, 2 * key heads * dim, sequences or tokens is 2^31 or more.
  */
 
 typedef enum {

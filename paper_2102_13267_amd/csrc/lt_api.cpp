@@ -338,8 +338,8 @@ static lt_status check_paged(lt_ctx* ctx, const std::string& op, const Handle* c
     return fail(ctx, LT_ERR_SHAPE, op + ": lengths must be [sequences] and table [sequences, slots]");
   const int64_t most = ((int64_t)1 << 31) - 1;
   auto over = [&](int64_t a, int64_t b) { return a > most || b > most || a * b > most; };
-  if (over(cache->dims[0], cache->dims[3]) || over(table->dims[1], cache->dims[3]) || over(cache->dims[2], cache->dims[4]) || lengths->dims[0] > most)
-    return fail(ctx, LT_ERR_SHAPE, op + ": pages * rows, slots * rows, key heads * dim and sequences must be below 2^31");
+  if (over(cache->dims[0], cache->dims[3]) || over(table->dims[1], cache->dims[3]) || over(2 * cache->dims[2], cache->dims[4]) || lengths->dims[0] > most)
+    return fail(ctx, LT_ERR_SHAPE, op + ": pages * rows, slots * rows, 2 * key heads * dim and sequences must be below 2^31");
   return LT_OK;
 }
 

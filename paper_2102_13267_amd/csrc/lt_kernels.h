@@ -334,8 +334,9 @@ struct AppendArgs {
   const int32_t* offsets;
   uint64_t cache_elems;
   uint32_t cache_dtype, dtype, tokens, seqs, slots, pages, heads, dim;
-  Divider rows;                 // of a page
-  uint32_t pad;
+  Divider rows, token_rows;     // of a page; of a token: 2 heads
+  uint32_t rows_each, pad;      // (this, and the next two, are the launcher's)
+  Divider slots_each, pairs;
   int64_t k_token, k_head, v_token, v_head;   // element strides
   Rotary rotary;
 };

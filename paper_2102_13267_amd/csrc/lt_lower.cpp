@@ -1859,6 +1859,7 @@ struct Lowering {
     args.heads = (uint32_t)an->dims[2];
     args.dim = (uint32_t)an->dims[4];
     args.rows.set((uint32_t)an->dims[3]);
+    args.token_rows.set(2u * args.heads);
     args.k_token = kv[0].s_inner;
     args.k_head = kv[0].s_head;
     args.v_token = kv[1].s_inner;

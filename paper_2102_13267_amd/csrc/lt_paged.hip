@@ -5,6 +5,8 @@
 // What lengths and tables say is checked here, key by key: nothing outside the cache is read or written.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "lt_launch.h"
 #include "lt_interp.h"
 #include "lt_reduce.h"
@@ -17,6 +19,8 @@ constexpr uint32_t kBlock = 256;
 constexpr float kLog2e = 1.44269504088896340736f;
 
 // ---- new rows ------------------------------------------------------------------------------------
+// Bound by memory for prompts, by latency for single tokens: a workgroup has all rows (keys and values, head by head) of a few tokens
+// on their way while it finds out where these go and computes their turns.
 __global__ __launch_bounds__(kBlock) void lt_cache_copy_kernel(const AppendArgs a) {
   const uint64_t n = a.cache_elems * (a.cache_dtype == kF32 ? 4u : 2u), stride = (uint64_t)gridDim.x * kBlock * 16u;
   for (uint64_t i = ((uint64_t)blockIdx.x * kBlock + threadIdx.x) * 16u; i < n; i += stride) {
@@ -26,75 +30,181 @@ __global__ __launch_bounds__(kBlock) void lt_cache_copy_kernel(const AppendArgs 
   }
 }
 
-// Where token t goes: its position, and its row of the cache as page * rows + row; false: nowhere.
-__device__ __forceinline__ bool place(const AppendArgs& a, uint32_t t, int32_t* position, uint32_t* page, uint32_t* row) {
-  uint32_t s = t;
-  int64_t pos;
+// The sequence that token t belongs to, found by a wave together: the last one whose offset is not behind t.  Offsets that decrease lead
+// to some sequence, never out of the table.
+__device__ __forceinline__ uint32_t sequence_of(const AppendArgs& a, uint32_t t) {
+  const uint32_t lane = threadIdx.x & 63u;
+  uint32_t lo = 0, n = a.seqs + 1u;
+  while (n > 1u) {
+    const uint32_t step = (n + 63u) / 64u, j = lo + lane * step;
+    const uint32_t before = (uint32_t)__popcll(__ballot(lane * step < n && (int64_t)a.offsets[lane * step < n ? j : lo] <= (int64_t)t));
+    if (before == 0u) break;
+    const uint32_t skip = (before - 1u) * step;
+    lo += skip;
+    n = min(step, n - skip);
+  }
+  return lo;
+}
+
+// Where token t of sequence s goes: its position, and the place of its first key in the cache (elements); false: nowhere.
+__device__ __forceinline__ bool place(const AppendArgs& a, uint32_t t, uint32_t s, int32_t* position, int64_t* at) {
+  if (s >= a.seqs) return false;
+  int64_t pos = (int64_t)a.lengths[s] - 1;
   if (a.offsets) {
-    // the last sequence that starts at or before t; between its neighbours' offsets, whatever they hold
-    uint32_t lo = 0, hi = a.seqs;   // offsets[lo] <= t (or lo = 0), offsets[hi] > t (or hi = seqs)
-    while (hi - lo > 1u) {
-      const uint32_t mid = (lo + hi) / 2u;
-      if (a.offsets[mid] <= (int64_t)t) lo = mid;
-      else hi = mid;
-    }
-    s = lo;
-    if (s >= a.seqs || (int64_t)a.offsets[s] > (int64_t)t || (int64_t)a.offsets[s + 1] <= (int64_t)t) return false;
-    pos = (int64_t)a.lengths[s] - a.offsets[s + 1] + t;
-  } else {
-    pos = (int64_t)a.lengths[s] - 1;
+    const int64_t from = a.offsets[s], to = a.offsets[s + 1u];
+    if ((int64_t)t < from || (int64_t)t >= to) return false;
+    pos += 1 - to + t;
   }
   if (pos < 0 || pos >= (int64_t)a.slots * a.rows.d) return false;
   const uint32_t slot = divide(a.rows, (uint32_t)pos);
   const int32_t p = a.table[(uint64_t)s * a.slots + slot];
   if (p < 0 || (uint32_t)p >= a.pages) return false;
   *position = (int32_t)pos;
-  *page = (uint32_t)p;
-  *row = (uint32_t)pos - slot * a.rows.d;
+  *at = ((int64_t)p * 2 * a.heads * a.rows.d + ((uint32_t)pos - slot * a.rows.d)) * a.dim;
   return true;
 }
 
-template <typename C, typename T>
+constexpr uint32_t kMaxTokens = 256;   // of a workgroup
+
+template <typename C, typename T, int V, bool IL>
 __global__ __launch_bounds__(kBlock) void lt_cache_append_kernel(const AppendArgs a) {
+  __shared__ Turn turns[kMaxTurns];
+  __shared__ int64_t to[kMaxTokens];
+  __shared__ int32_t position[kMaxTokens];
+  __shared__ uint32_t sequence[kMaxTokens];
+  const uint32_t pairs = a.rotary.dims / 2u, lane = divide(a.slots_each, threadIdx.x), u = threadIdx.x - lane * a.slots_each.d, lanes = kBlock / a.slots_each.d;
+  // rows: token by token its keys' heads, then its values'
+  const uint64_t row0 = (uint64_t)blockIdx.x * (lanes * a.rows_each), rows = (uint64_t)a.tokens * a.token_rows.d;
+  const uint32_t n = (uint32_t)(rows - row0 < (uint64_t)lanes * a.rows_each ? rows - row0 : (uint64_t)lanes * a.rows_each);
+  const uint32_t token0 = rows < 0x7fffffffu ? divide(a.token_rows, (uint32_t)row0) : (uint32_t)(row0 / a.token_rows.d), first = (uint32_t)(row0 - (uint64_t)token0 * a.token_rows.d);
+  const uint32_t tokens = divide(a.token_rows, first + n - 1u) + 1u;
+  bool turned;
+  const uint32_t at = slot_at<V, IL>(a.rotary, u, &turned);
+  Slot<T, V, IL> s[kMaxRows];
+  uint32_t token[kMaxRows], head[kMaxRows];
+#pragma unroll
+  for (int i = 0; i < kMaxRows; ++i) {
+    const uint32_t r = first + lane + i * lanes;
+    token[i] = divide(a.token_rows, r);   // (after the first)
+    head[i] = r - token[i] * a.token_rows.d;
+    if (lane + i * lanes >= n || lane >= lanes) continue;
+    const int64_t t = token0 + token[i];
+    const T* row = head[i] < a.heads ? (const T*)a.k + t * a.k_token + (int64_t)head[i] * a.k_head : (const T*)a.v + t * a.v_token + (int64_t)(head[i] - a.heads) * a.v_head;
+    load_slot<T, V, IL, false>(row, a.rotary, at, turned, &s[i]);
+  }
+  if (a.offsets) {
+    for (uint32_t i = threadIdx.x >> 6; i < tokens; i += kBlock / 64u) {
+      const uint32_t q = sequence_of(a, token0 + i);
+      if ((threadIdx.x & 63u) == 0u) sequence[i] = q;
+    }
+    __syncthreads();
+  }
+  for (uint32_t i = threadIdx.x; i < tokens; i += kBlock) {
+    int32_t p = 0;
+    int64_t where = -1;
+    if (!place(a, token0 + i, a.offsets ? sequence[i] : token0 + i, &p, &where)) where = -1;
+    position[i] = p;
+    to[i] = where;
+  }
+  __syncthreads();
+  if (pairs > 0u) {
+    for (uint32_t i = threadIdx.x; i < tokens * pairs; i += kBlock) {
+      const uint32_t k = divide(a.pairs, i);
+      turns[i] = turn_of(a.rotary, position[k], i - k * pairs);
+    }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int i = 0; i < kMaxRows; ++i) {
+    if (lane + i * lanes >= n || lane >= lanes) continue;
+    const int64_t where = to[token[i]];
+    if (where < 0) continue;
+    // (a page's keys, head by head, are followed by its values)
+    C* row = (C*)a.cache + where + (int64_t)head[i] * a.rows.d * a.dim;
+    store_slot<C, T, V, IL, false>(row, a.rotary, at, turned, s[i], pairs > 0u && head[i] < a.heads ? turns + token[i] * pairs : nullptr);
+  }
+}
+
+// Rows that the above does not take: interleaved pairs at odd places, rows of very many slots.  One thread per pair (or element of the rest).
+template <typename C, typename T>
+__global__ __launch_bounds__(kBlock) void lt_cache_append_any_kernel(const AppendArgs a) {
   const uint32_t half = a.rotary.dims / 2u, unit = a.dim - half;
-  const uint64_t n = (uint64_t)a.tokens * 2u * a.heads * unit, stride = (uint64_t)gridDim.x * kBlock;
+  const uint64_t n = (uint64_t)a.tokens * a.token_rows.d * unit, stride = (uint64_t)gridDim.x * kBlock;
   for (uint64_t i = (uint64_t)blockIdx.x * kBlock + threadIdx.x; i < n; i += stride) {
-    const uint32_t u = (uint32_t)(i % unit), h = (uint32_t)(i / unit % a.heads), kind = (uint32_t)(i / unit / a.heads % 2u), t = (uint32_t)(i / unit / a.heads / 2u);
+    const uint32_t u = (uint32_t)(i % unit), h = (uint32_t)(i / unit % a.token_rows.d), t = (uint32_t)(i / unit / a.token_rows.d);
+    uint32_t lo = 0, hi = a.seqs;   // offsets[lo] <= t (or lo = 0), offsets[hi] > t (or hi = seqs)
+    while (a.offsets && hi - lo > 1u) {
+      const uint32_t mid = (lo + hi) / 2u;
+      if ((int64_t)a.offsets[mid] <= (int64_t)t) lo = mid;
+      else hi = mid;
+    }
     int32_t position;
-    uint32_t page, row;
-    if (!place(a, t, &position, &page, &row)) continue;
-    const T* x = kind == 0u ? (const T*)a.k + (int64_t)t * a.k_token + (int64_t)h * a.k_head : (const T*)a.v + (int64_t)t * a.v_token + (int64_t)h * a.v_head;
-    C* y = (C*)a.cache + ((((uint64_t)page * 2u + kind) * a.heads + h) * a.rows.d + row) * a.dim;
+    int64_t where;
+    if (!place(a, t, a.offsets ? lo : t, &position, &where)) continue;
+    const T* x = h < a.heads ? (const T*)a.k + (int64_t)t * a.k_token + (int64_t)h * a.k_head : (const T*)a.v + (int64_t)t * a.v_token + (int64_t)(h - a.heads) * a.v_head;
+    C* y = (C*)a.cache + where + (int64_t)h * a.rows.d * a.dim;
     if (u >= half) {
       y[half + u] = (C)to_float(x[half + u]);
       continue;
     }
     const uint32_t p = a.rotary.interleaved ? 2u * u : u, q = a.rotary.interleaved ? 2u * u + 1u : u + half;
     float v = to_float(x[p]), w = to_float(x[q]);
-    if (kind == 0u) rotate(turn_of(a.rotary, position, u), v, w, &v, &w);
+    if (h < a.heads) rotate(turn_of(a.rotary, position, u), v, w, &v, &w);
     y[p] = (C)v;
     y[q] = (C)w;
   }
 }
 
+template <typename C, typename T>
+hipError_t launch_append_of(AppendArgs a, hipStream_t s) {
+  constexpr uint32_t kMost = 16u / (sizeof(C) > sizeof(T) ? sizeof(C) : sizeof(T));
+  const uint64_t rows = (uint64_t)a.tokens * a.token_rows.d;
+  const uint64_t aligned = std::min(row_alignment(a.k, sizeof(T), a.k_token, a.k_head, 0), row_alignment(a.v, sizeof(T), a.v_token, a.v_head, 0));
+  const uint32_t v = piece_of(a.rotary, a.dim, aligned, kMost), slots = v ? slots_of(a.rotary, a.dim, v) : 0u, pairs = a.rotary.dims / 2u;
+  a.rows_each = kMaxRows;
+  if (v && slots <= kBlock) {
+    const uint32_t lanes = kBlock / slots;
+    auto tokens = [&](uint32_t each) { return (lanes * each + a.token_rows.d - 2u) / a.token_rows.d + 1u; };
+    auto fits = [&](uint32_t each) { return tokens(each) * pairs <= kMaxTurns && tokens(each) <= kMaxTokens; };
+    while (a.rows_each > 1u && (rows / (lanes * a.rows_each) < 1024u || !fits(a.rows_each))) a.rows_each /= 2u;
+    const uint64_t grid = (rows + lanes * a.rows_each - 1) / (lanes * a.rows_each);
+    if (fits(a.rows_each) && grid < ((uint64_t)1 << 31)) {
+      a.slots_each.set(slots);
+      a.pairs.set(pairs ? pairs : 1u);
+      const dim3 g((uint32_t)grid), b(kBlock);
+      if (a.rotary.interleaved) {
+        if (v == kMost) LT_LAUNCH((lt_cache_append_kernel<C, T, kMost, true>), g, b, s, a);
+        else if (v == 4u) LT_LAUNCH((lt_cache_append_kernel<C, T, 4, true>), g, b, s, a);
+        else LT_LAUNCH((lt_cache_append_kernel<C, T, 2, true>), g, b, s, a);
+      } else {
+        if (v == kMost) LT_LAUNCH((lt_cache_append_kernel<C, T, kMost, false>), g, b, s, a);
+        else if (v == 4u) LT_LAUNCH((lt_cache_append_kernel<C, T, 4, false>), g, b, s, a);
+        else if (v == 2u) LT_LAUNCH((lt_cache_append_kernel<C, T, 2, false>), g, b, s, a);
+        else LT_LAUNCH((lt_cache_append_kernel<C, T, 1, false>), g, b, s, a);
+      }
+      return hipGetLastError();
+    }
+  }
+  const uint64_t n = (rows * (a.dim - pairs) + kBlock - 1) / kBlock;
+  LT_LAUNCH((lt_cache_append_any_kernel<C, T>), dim3((uint32_t)(n < 65536u ? n : 65536u)), dim3(kBlock), s, a);
+  return hipGetLastError();
+}
+
 hipError_t launch_append(const void* args, hipStream_t s) {
   const AppendArgs& a = *(const AppendArgs*)args;
   if (a.cache_elems == 0) return hipSuccess;
-  if (!a.cache || a.rows.d == 0 || a.rotary.dims > a.dim || a.rotary.dims > 2u * kMaxPairs) return hipErrorInvalidValue;
+  if (!a.cache || a.rows.d == 0 || a.token_rows.d != 2u * a.heads || a.rotary.dims > a.dim || a.rotary.dims > 2u * kMaxPairs) return hipErrorInvalidValue;
   if (a.copy_from) {
     const uint64_t pieces = (a.cache_elems + 2047u) / 2048u;
     LT_LAUNCH(lt_cache_copy_kernel, dim3((uint32_t)(pieces < 16384u ? pieces : 16384u)), dim3(kBlock), s, a);
   }
-  const uint64_t n = (uint64_t)a.tokens * 2u * a.heads * (a.dim - a.rotary.dims / 2u);
-  if (n == 0 || a.seqs == 0 || a.slots == 0) return hipGetLastError();
+  if (a.tokens == 0 || a.seqs == 0 || a.slots == 0) return hipGetLastError();
   if (!a.k || !a.v || !a.lengths || !a.table) return hipErrorInvalidValue;
-  const uint32_t grid = (uint32_t)((n + kBlock - 1) / kBlock < 65536u ? (n + kBlock - 1) / kBlock : 65536u);
-  if (a.cache_dtype == kF32 && a.dtype == kF32) LT_LAUNCH((lt_cache_append_kernel<float, float>), dim3(grid), dim3(kBlock), s, a);
-  else if (a.cache_dtype == kF32 && a.dtype == kBF16) LT_LAUNCH((lt_cache_append_kernel<float, __bf16>), dim3(grid), dim3(kBlock), s, a);
-  else if (a.cache_dtype == kBF16 && a.dtype == kF32) LT_LAUNCH((lt_cache_append_kernel<__bf16, float>), dim3(grid), dim3(kBlock), s, a);
-  else if (a.cache_dtype == kBF16 && a.dtype == kBF16) LT_LAUNCH((lt_cache_append_kernel<__bf16, __bf16>), dim3(grid), dim3(kBlock), s, a);
-  else return hipErrorInvalidValue;
-  return hipGetLastError();
+  if (a.cache_dtype == kF32 && a.dtype == kF32) return launch_append_of<float, float>(a, s);
+  if (a.cache_dtype == kF32 && a.dtype == kBF16) return launch_append_of<float, __bf16>(a, s);
+  if (a.cache_dtype == kBF16 && a.dtype == kF32) return launch_append_of<__bf16, float>(a, s);
+  if (a.cache_dtype == kBF16 && a.dtype == kBF16) return launch_append_of<__bf16, __bf16>(a, s);
+  return hipErrorInvalidValue;
 }
 
 // ---- attention of one new token -------------------------------------------------------------------
