@@ -368,12 +368,12 @@ struct PagedArgs {
   // The instance, and how the work is shared out; `capacity` and what comes before it are set.  Tiles of all sequences must be below 2^32.
   void share_out() {
     const uint32_t group = heads / kv_heads;
-    padded = dim <= 64u ? 64u : dim <= 128u ? 128u : 256u;
+    padded = dim <= 64u ? 64u : dim <= 96u ? 96u : dim <= 128u ? 128u : 256u;
     blocks_of = group <= 16u || padded == 256u ? 16u : 32u;
     pairs = kv_heads * ((group + blocks_of - 1u) / blocks_of);
     tile = dtype == kF32 ? 64u : 128u;
     const uint64_t most = capacity == 0 ? 1 : (capacity - 1u) / tile + 1u, all = (uint64_t)seqs * pairs;
-    least = 4;
+    least = dtype == kF32 ? 2u : 4u;
     split = most > least ? 1u : 0u;
     const uint64_t each = (most + least - 1u) / least;   // chunks of a sequence at most
     workgroups = (uint32_t)(split && each > 1u ? (all + kPagedChunks < all * each ? all + kPagedChunks : all * each) : all);

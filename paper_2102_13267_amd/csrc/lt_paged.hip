@@ -235,26 +235,29 @@ template <typename T, int DP, int NH> struct Geo {
   static constexpr int CE = 16 / (int)sizeof(T);     // elements of 16 bytes
   static constexpr int NC = DP / (4 * CE);           // 16-byte pieces of a key's row per lane
   static constexpr int NV = DP / 16;                 // elements of a value's row per lane
-  static constexpr int VB = NV * (int)sizeof(T) < 16 ? NV * (int)sizeof(T) : 16;   // bytes of a piece of it,
-  static constexpr int NP = NV * (int)sizeof(T) / VB;                               // and their number
+  // bytes of a piece of it (96: of two elements, so that none ends behind a head of an even number of them), their number, and dwords of one
+  static constexpr int VB = NV * (int)sizeof(T) % 16 == 0 ? 16 : DP == 96 ? 2 * (int)sizeof(T) : 8;
+  static constexpr int NP = NV * (int)sizeof(T) / VB, DW = VB / 4;
   static constexpr int PITCH = DP + 4;
 };
 
 typedef uint32_t U4 __attribute__((ext_vector_type(4)));
 typedef uint32_t U2 __attribute__((ext_vector_type(2)));
 typedef float F4 __attribute__((ext_vector_type(4)));
+typedef float F2 __attribute__((ext_vector_type(2)));
 typedef __bf16 B8 __attribute__((ext_vector_type(8)));
 
 constexpr int kSlots = 1024;   // page numbers of a stretch of a sequence that a workgroup holds
 
-template <int BYTES> __device__ __forceinline__ U4 load_bytes(const void* p) {
+// PAST: read past the last-level cache, for what will not be found there the next time either
+template <int BYTES, bool PAST = false> __device__ __forceinline__ U4 load_bytes(const void* p) {
   U4 r = {0u, 0u, 0u, 0u};
-  if constexpr (BYTES == 16) r = *(const U4*)p;
+  if constexpr (BYTES == 16) r = PAST ? __builtin_nontemporal_load((const U4*)p) : *(const U4*)p;
   else if constexpr (BYTES == 8) {
-    const U2 t = *(const U2*)p;
+    const U2 t = PAST ? __builtin_nontemporal_load((const U2*)p) : *(const U2*)p;
     r.x = t.x;
     r.y = t.y;
-  } else r.x = *(const uint32_t*)p;
+  } else r.x = PAST ? __builtin_nontemporal_load((const uint32_t*)p) : *(const uint32_t*)p;
   return r;
 }
 
@@ -399,7 +402,7 @@ __device__ __forceinline__ bool last_of(uint32_t* ticket, uint32_t count, uint32
   return *flag != 0u;
 }
 
-template <typename T, int DP, int NH, bool PG, int AL>
+template <typename T, int DP, int NH, bool PG, int AL, bool PAST>
 __global__ __launch_bounds__(kBlock, DP <= 128 && NH == 1 && AL == 16 ? (DP == 64 ? 4 : 3) : 1) void lt_paged_attention_kernel(const PagedArgs a) {
   using G = Geo<T, DP, NH>;
   constexpr int KT = G::KT, NC = G::NC, NV = G::NV, NP = G::NP;
@@ -493,7 +496,7 @@ __global__ __launch_bounds__(kBlock, DP <= 128 && NH == 1 && AL == 16 ? (DP == 6
         if constexpr (PG) {
           const uint32_t at = n < there[t] ? key_at : key_at0;
 #pragma unroll
-          for (int c = 0; c < NC; ++c) k[t][c] = load_bytes<16>(tile[t] + at + c * 64);
+          for (int c = 0; c < NC; ++c) k[t][c] = load_bytes<16, PAST>(tile[t] + at + c * 64);
         } else {
           bool ok;
           const T* row = (const T*)a.cache + find_row(key0 + 16u * t + n, &ok);
@@ -520,7 +523,7 @@ __global__ __launch_bounds__(kBlock, DP <= 128 && NH == 1 && AL == 16 ? (DP == 6
           const uint32_t at = (ok ? r * a.dim * kSize : 0u) + value_at0;
           const char* row = tile[t] + value * kSize;
 #pragma unroll
-          for (int p = 0; p < NP; ++p) v[i][p] = load_bytes<G::VB>(row + at + (NP == 1 || n * NV + p * (G::VB / kSize) < a.dim ? p * G::VB : 0));
+          for (int p = 0; p < NP; ++p) v[i][p] = load_bytes<G::VB, PAST>(row + at + (NP == 1 || n * NV + p * (G::VB / kSize) < a.dim ? p * G::VB : 0));
         } else {
           const T* row = (const T*)a.cache + value + find_row(key0 + 16u * t + r, &ok);
 #pragma unroll
@@ -545,7 +548,7 @@ __global__ __launch_bounds__(kBlock, DP <= 128 && NH == 1 && AL == 16 ? (DP == 6
           for (int c = 0; c < NC; ++c) {
             if constexpr (G::BF) {
               s[b][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(B8, k[t][c]), __builtin_bit_cast(B8, q[b][c]), s[b][t], 0, 0, 0);
-            } else {
+            } else if (c * 4 * G::CE < (int)a.dim) {   // (pieces wholly behind the head are not multiplied)
 #pragma unroll
               for (int e = 0; e < 4; ++e)
                 s[b][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[t][c][e]), __uint_as_float(q[b][c][e]), s[b][t], 0, 0, 0);
@@ -612,7 +615,7 @@ __global__ __launch_bounds__(kBlock, DP <= 128 && NH == 1 && AL == 16 ? (DP == 6
           U4 f;
 #pragma unroll
           for (int p = 0; p < 4; ++p)
-            f[p] = __builtin_amdgcn_perm(v[2 * p + 1][j / 8][j / 2 % 4], v[2 * p][j / 8][j / 2 % 4], (j & 1) ? kHigh : kLow);
+            f[p] = __builtin_amdgcn_perm(v[2 * p + 1][j / 2 / G::DW][j / 2 % G::DW], v[2 * p][j / 2 / G::DW][j / 2 % G::DW], (j & 1) ? kHigh : kLow);
 #pragma unroll
           for (int b = 0; b < NH; ++b) acc[b][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(B8, f), weight[b], acc[b][j], 0, 0, 0);
         }
@@ -622,7 +625,7 @@ __global__ __launch_bounds__(kBlock, DP <= 128 && NH == 1 && AL == 16 ? (DP == 6
 #pragma unroll
           for (int j = 0; j < NV; ++j)
 #pragma unroll
-            for (int b = 0; b < NH; ++b) acc[b][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[r][j / 4][j % 4]), s[b][0][r], acc[b][j], 0, 0, 0);
+            for (int b = 0; b < NH; ++b) acc[b][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[r][j / G::DW][j % G::DW]), s[b][0][r], acc[b][j], 0, 0, 0);
       }
     }
   }
@@ -662,8 +665,7 @@ __global__ __launch_bounds__(kBlock, DP <= 128 && NH == 1 && AL == 16 ? (DP == 6
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
-      for (int j = 0; j < NV; j += 4)
-        *(F4*)&meet[wave][n * G::PITCH + (4u * g + r) * NV + j] = F4{acc[b][j][r] * f, acc[b][j + 1][r] * f, acc[b][j + 2][r] * f, acc[b][j + 3][r] * f};
+      for (int j = 0; j < NV; j += 2) *(F2*)&meet[wave][n * G::PITCH + (4u * g + r) * NV + j] = F2{acc[b][j][r] * f, acc[b][j + 1][r] * f};
     __syncthreads();
     for (uint32_t i = threadIdx.x; i < 16u * DP / 4u; i += kBlock) {
       const uint32_t h = i / (DP / 4u), d = i % (DP / 4u) * 4u, hh = 16u * b + h;
@@ -734,16 +736,20 @@ hipError_t launch_paged_as(const PagedArgs& a, hipStream_t s) {
   // rows of whole 16 bytes are read in such pieces, others in the largest that they are made of
   const uint32_t row = a.dim * (uint32_t)sizeof(T);
   const bool whole = row % 16u == 0u && (uintptr_t)a.cache % 16u == 0u;
-  if (whole && a.rows.d % 16u == 0u) LT_LAUNCH((lt_paged_attention_kernel<T, DP, NH, true, 16>), dim3(a.workgroups), dim3(kBlock), s, a);
-  else if (whole) LT_LAUNCH((lt_paged_attention_kernel<T, DP, NH, false, 16>), dim3(a.workgroups), dim3(kBlock), s, a);
-  else if (row % 4u == 0u) LT_LAUNCH((lt_paged_attention_kernel<T, DP, NH, false, 4>), dim3(a.workgroups), dim3(kBlock), s, a);
-  else if constexpr (sizeof(T) == 2) LT_LAUNCH((lt_paged_attention_kernel<T, DP, NH, false, 2>), dim3(a.workgroups), dim3(kBlock), s, a);
+  // caches larger than the last-level cache are read past it (one block of query heads a key head: others read the same keys)
+  const bool past = (uint64_t)a.pages * 2u * a.kv_heads * a.rows.d * row >= ((uint64_t)256 << 20) && a.pairs == a.kv_heads;
+  if (whole && a.rows.d % 16u == 0u && past) LT_LAUNCH((lt_paged_attention_kernel<T, DP, NH, true, 16, true>), dim3(a.workgroups), dim3(kBlock), s, a);
+  else if (whole && a.rows.d % 16u == 0u) LT_LAUNCH((lt_paged_attention_kernel<T, DP, NH, true, 16, false>), dim3(a.workgroups), dim3(kBlock), s, a);
+  else if (whole) LT_LAUNCH((lt_paged_attention_kernel<T, DP, NH, false, 16, false>), dim3(a.workgroups), dim3(kBlock), s, a);
+  else if (row % 4u == 0u) LT_LAUNCH((lt_paged_attention_kernel<T, DP, NH, false, 4, false>), dim3(a.workgroups), dim3(kBlock), s, a);
+  else if constexpr (sizeof(T) == 2) LT_LAUNCH((lt_paged_attention_kernel<T, DP, NH, false, 2, false>), dim3(a.workgroups), dim3(kBlock), s, a);
   return hipGetLastError();
 }
 
 template <typename T>
 hipError_t launch_paged_of(const PagedArgs& a, hipStream_t s) {
   if (a.padded == 64u) return a.blocks_of == 16u ? launch_paged_as<T, 64, 1>(a, s) : launch_paged_as<T, 64, 2>(a, s);
+  if (a.padded == 96u) return a.blocks_of == 16u ? launch_paged_as<T, 96, 1>(a, s) : launch_paged_as<T, 96, 2>(a, s);
   if (a.padded == 128u) return a.blocks_of == 16u ? launch_paged_as<T, 128, 1>(a, s) : launch_paged_as<T, 128, 2>(a, s);
   return launch_paged_as<T, 256, 1>(a, s);
 }
