@@ -289,13 +289,18 @@ __device__ __forceinline__ U4 cut(U4 v, uint32_t d, uint32_t dim) {
   return v;
 }
 
+// Over the four rows of 16 lanes: neighbouring rows trade places, then halves of the wave.
 __device__ __forceinline__ float max_over_groups(float v) {
-  v = fmaxf(v, __shfl_xor(v, 16, 64));
-  return fmaxf(v, __shfl_xor(v, 32, 64));
+  auto t = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(t[0]), __uint_as_float(t[1]));
+  t = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(t[0]), __uint_as_float(t[1]));
 }
 __device__ __forceinline__ float sum_over_groups(float v) {
-  v += __shfl_xor(v, 16, 64);
-  return v + __shfl_xor(v, 32, 64);
+  auto t = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(t[0]) + __uint_as_float(t[1]);
+  t = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(t[0]) + __uint_as_float(t[1]);
 }
 __device__ __forceinline__ float power2(float v) { return __builtin_amdgcn_exp2f(v); }
 
@@ -325,63 +330,49 @@ struct Chunk {
   uint32_t part, parts, piece0;  // part of `parts`, whose pieces lie from piece0 on
 };
 
-// Found by the block together, as a sum over the sequences; false: there is none for this workgroup.
+// Found by every wave for itself (four waves that meet at barriers took longer), as sums over the sequences, `each` of them a lane;
+// false: there is none for this workgroup.
 template <uint32_t TILE>
-__device__ __forceinline__ bool find_chunk(const PagedArgs& a, uint32_t (*shared)[8], Chunk* w) {
-  const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, each = (a.seqs + kBlock - 1u) / kBlock, from = threadIdx.x * each;
-  uint32_t tiles = 0;
-  for (uint32_t i = 0; i < each; ++i)
-    if (from + i < a.seqs) tiles += tiles_of<TILE>(length_of(a, from + i));
-  tiles = sums_over_wave(tiles);
-  if (lane == 63u) shared[0][wave] = tiles;
-  __syncthreads();
-  const uint32_t all = (shared[0][0] + shared[0][1] + shared[0][2] + shared[0][3]) * a.pairs;
+__device__ __forceinline__ bool find_chunk(const PagedArgs& a, Chunk* w) {
+  const uint32_t lane = threadIdx.x & 63u, each = (a.seqs + 63u) / 64u, from = lane * each;
+  // (the first four stay in registers)
+  uint32_t len[4], tiles = 0;
+#pragma unroll
+  for (uint32_t i = 0; i < 4u; ++i) len[i] = i < each && from + i < a.seqs ? length_of(a, from + i) : 0xFFFFFFFFu;
+  auto length = [&](uint32_t i) { return i == 0u ? len[0] : i == 1u ? len[1] : i == 2u ? len[2] : i == 3u ? len[3] : length_of(a, from + i); };
+  const uint32_t mine = from < a.seqs ? min(each, a.seqs - from) : 0u;
+  for (uint32_t i = 0; i < mine; ++i) tiles += tiles_of<TILE>(length(i));
+  const uint32_t all = (uint32_t)__builtin_amdgcn_readlane((int)sums_over_wave(tiles), 63) * a.pairs;
   const uint32_t c = max(a.least, (all + kPagedChunks - 1u) / kPagedChunks);
   uint32_t chunks = 0, split = 0;
-  for (uint32_t i = 0; i < each; ++i)
-    if (from + i < a.seqs) {
-      const uint32_t k = (tiles_of<TILE>(length_of(a, from + i)) + c - 1u) / c;
-      chunks += k;
-      split += k > 1u ? k : 0u;
-    }
-  const uint32_t chunks_to = sums_over_wave(chunks), split_to = sums_over_wave(split);
-  if (lane == 63u) {
-    shared[1][wave] = chunks_to;
-    shared[1][4 + wave] = split_to;
+  for (uint32_t i = 0; i < mine; ++i) {
+    const uint32_t k = (tiles_of<TILE>(length(i)) + c - 1u) / c;
+    chunks += k;
+    split += k > 1u ? k : 0u;
   }
-  if (threadIdx.x == 0u) shared[2][0] = a.seqs;
-  __syncthreads();
-  uint32_t before = chunks_to - chunks, split_before = split_to - split;
-  for (uint32_t i = 0; i < wave; ++i) {
-    before += shared[1][i];
-    split_before += shared[1][4 + i];
-  }
+  uint32_t before = sums_over_wave(chunks) - chunks, split_before = sums_over_wave(split) - split;
   const uint32_t at = blockIdx.x;
-  if (before * a.pairs <= at && at < (before + chunks) * a.pairs) {
-    uint32_t s = from, len, t, k;
-    for (;; ++s) {
-      len = length_of(a, s);
-      t = tiles_of<TILE>(len);
-      k = (t + c - 1u) / c;
-      if (at < (before + k) * a.pairs) break;
-      before += k;
-      split_before += k > 1u ? k : 0u;
-    }
-    const uint32_t rel = at - before * a.pairs, pair = rel / k;
-    shared[2][0] = s;
-    shared[2][1] = len;
-    shared[2][2] = t;
-    shared[2][3] = pair;
-    shared[2][4] = rel - pair * k;
-    shared[2][5] = k;
-    shared[2][6] = split_before * a.pairs + pair * k;
+  const uint64_t here = __ballot(before * a.pairs <= at && at < (before + chunks) * a.pairs);
+  if (here == 0u) return false;
+  uint32_t i = 0, n, t, k;
+  for (;; ++i) {
+    n = i < mine ? length(i) : 0u;
+    t = tiles_of<TILE>(n);
+    k = (t + c - 1u) / c;
+    if (i + 1u >= mine || at < (before + k) * a.pairs) break;
+    before += k;
+    split_before += k > 1u ? k : 0u;
   }
-  __syncthreads();
-  if (shared[2][0] >= a.seqs) return false;
-  uint32_t r[7];
-#pragma unroll
-  for (int i = 0; i < 7; ++i) r[i] = (uint32_t)__builtin_amdgcn_readfirstlane((int)shared[2][i]);
-  *w = Chunk{r[0], r[1], r[2], r[3], r[4], r[5], r[6]};
+  const int owner = __ffsll((unsigned long long)here) - 1;
+  auto of_owner = [&](uint32_t v) { return (uint32_t)__builtin_amdgcn_readlane((int)v, owner); };
+  w->seq = of_owner(from + i);
+  w->len = of_owner(n);
+  w->tiles = of_owner(t);
+  w->parts = of_owner(k);
+  const uint32_t rel = at - of_owner(before) * a.pairs;
+  w->pair = rel / w->parts;
+  w->part = rel - w->pair * w->parts;
+  w->piece0 = of_owner(split_before) * a.pairs + w->pair * w->parts;
   return true;
 }
 
@@ -407,15 +398,15 @@ __global__ __launch_bounds__(kBlock, DP <= 128 && NH == 1 && AL == 16 ? (DP == 6
   using G = Geo<T, DP, NH>;
   constexpr int KT = G::KT, NC = G::NC, NV = G::NV, NP = G::NP;
   constexpr uint32_t kSize = sizeof(T);
-  __shared__ int32_t pages[kSlots];
-  __shared__ uint32_t found[3][8], last_flag;
+  __shared__ int32_t pages[PG ? 1 : kSlots];
+  __shared__ uint32_t last_flag;
   __shared__ float tops[4][16 * NH], sums[4][16 * NH], factor[kMostPieces][16 * NH], weight_of[kMostPieces][16 * NH], total_of[16 * NH];
   __shared__ __attribute__((aligned(16))) float meet[4][16 * G::PITCH];
   const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15u, g = lane >> 4;
 
   Chunk w;
   if (a.split) {
-    if (!find_chunk<G::TILE>(a, found, &w)) return;
+    if (!find_chunk<G::TILE>(a, &w)) return;
   } else {
     w.seq = blockIdx.x / a.pairs;
     w.pair = blockIdx.x - w.seq * a.pairs;
@@ -457,30 +448,45 @@ __global__ __launch_bounds__(kBlock, DP <= 128 && NH == 1 && AL == 16 ? (DP == 6
   // (PG) bytes from a tile's first row to what this lane reads of its own
   const uint32_t key_at = (n * a.dim + g * G::CE) * kSize, key_at0 = g * 16u, value_at0 = (n * NV < a.dim ? n * NV : 0u) * kSize;
 
-  const uint32_t stretch = (uint32_t)min((uint64_t)(kSlots - 2) * a.rows.d / G::TILE, (uint64_t)0x7fffffffu / G::TILE);   // tiles whose pages fit
+  // Where a step's keys lie.  PG: a page holds whole tiles of 16, so a tile has one page: its first row, and how many of its keys there are.
+  // The page numbers of a wave's next 64 tiles lie in its lanes, and those of the 64 after that are on their way.  Otherwise every lane finds
+  // its own keys, and a stretch's page numbers lie in LDS.
+  const uint32_t stretch = PG ? 0x7fffffffu / G::TILE : (uint32_t)min((uint64_t)(kSlots - 2) * a.rows.d / G::TILE, (uint64_t)0x7fffffffu / G::TILE);
   for (uint32_t first = t0; first < t1; first += stretch) {
     const uint32_t k0 = first * G::TILE, k1 = (uint32_t)min((uint64_t)first * G::TILE + (uint64_t)stretch * G::TILE, (uint64_t)key_end);
     if (k0 >= k1) break;   // (an empty sequence)
-    const uint32_t slot0 = divide(a.rows, k0), n_slots = divide(a.rows, k1 - 1u) - slot0 + 1u;
-    if (first != t0) __syncthreads();       // (the stretch before has been read)
-    for (uint32_t i = threadIdx.x; i < n_slots; i += kBlock) {
-      const int32_t p = a.table[(uint64_t)w.seq * a.slots + slot0 + i];
-      pages[i] = p >= 0 && (uint32_t)p < a.pages ? p : -1;
+    const uint32_t slot0 = divide(a.rows, k0);
+    if constexpr (!PG) {
+      const uint32_t n_slots = divide(a.rows, k1 - 1u) - slot0 + 1u;
+      if (first != t0) __syncthreads();       // (the stretch before has been read)
+      for (uint32_t i = threadIdx.x; i < n_slots; i += kBlock) {
+        const int32_t p = a.table[(uint64_t)w.seq * a.slots + slot0 + i];
+        pages[i] = p >= 0 && (uint32_t)p < a.pages ? p : -1;
+      }
+      __syncthreads();
     }
-    __syncthreads();
-
-    // Where a step's keys lie.  PG: a page holds whole tiles of 16, so a tile has one page: its first row, and how many
-    // of its keys there are.  Otherwise every lane finds its own keys.
+    const uint32_t wave0 = k0 + wave * G::WK;
+    auto pages_from = [&](uint32_t step) {   // lane KT s + t: of tile t of the wave's step number step + s
+      const uint32_t k = wave0 + (step + lane / KT) * G::TILE + lane % KT * 16u;
+      const int32_t p = k < k1 ? a.table[(uint64_t)w.seq * a.slots + divide(a.rows, k)] : -1;
+      return p >= 0 && (uint32_t)p < a.pages ? p : -1;
+    };
+    int32_t pages_now = -1, pages_next = -1;
     const char* tile[KT];
-    uint32_t there[KT];
+    uint32_t there[KT], step = 0;
     auto find_tiles = [&](uint32_t key0) {
+      if (step % (64 / KT) == 0u) {
+        pages_now = step == 0u ? pages_from(0u) : pages_next;
+        pages_next = pages_from(step + 64 / KT);
+      }
 #pragma unroll
       for (int t = 0; t < KT; ++t) {
-        const uint32_t k = key0 + 16u * t, slot = divide(a.rows, k);
-        const int32_t p = __builtin_amdgcn_readfirstlane(k < k1 ? pages[slot - slot0] : -1);
+        const uint32_t k = key0 + 16u * t;
+        const int32_t p = __builtin_amdgcn_readlane(pages_now, (int)(step % (64 / KT) * KT + t));
         there[t] = p >= 0 ? min(16u, k1 - k) : 0u;
-        tile[t] = (const char*)a.cache + (p >= 0 ? (((int64_t)p * 2 * a.kv_heads + kh) * a.rows.d + (k - slot * a.rows.d)) * a.dim * kSize : (int64_t)0);
+        tile[t] = (const char*)a.cache + (p >= 0 ? (((int64_t)p * 2 * a.kv_heads + kh) * a.rows.d + (k - divide(a.rows, k) * a.rows.d)) * a.dim * kSize : (int64_t)0);
       }
+      ++step;
     };
     auto find_row = [&](uint32_t key, bool* ok) {
       const uint32_t slot = divide(a.rows, key);
@@ -506,7 +512,7 @@ __global__ __launch_bounds__(kBlock, DP <= 128 && NH == 1 && AL == 16 ? (DP == 6
       }
     };
 
-    uint32_t key0 = k0 + wave * G::WK;
+    uint32_t key0 = wave0;
     if (key0 < k1) {
       if constexpr (PG) find_tiles(key0);
       load_keys(key0);
@@ -662,6 +668,7 @@ __global__ __launch_bounds__(kBlock, DP <= 128 && NH == 1 && AL == 16 ? (DP == 6
   for (int b = 0; b < NH; ++b) {
     const float f = power2(top[b] - safe_of(common(16u * b + n)));
     if (b > 0) __syncthreads();
+    if (16u * b + n < heads)
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
