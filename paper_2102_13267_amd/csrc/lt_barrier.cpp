@@ -159,7 +159,7 @@ bool set_operator(OperatorKernel which, OperatorLauncher launch) {
   operators()[which] = launch;
   return true;
 }
-static hipError_t launch_operator(OperatorKernel which, const void* args, hipStream_t s) {
+hipError_t launch_operator(OperatorKernel which, const void* args, hipStream_t s) {
   const OperatorLauncher f = operators()[which];
   return f ? f(args, s) : hipErrorInvalidValue;
 }

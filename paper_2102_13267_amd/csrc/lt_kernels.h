@@ -335,10 +335,12 @@ struct AppendArgs {
   uint64_t cache_elems;
   uint32_t cache_dtype, dtype, tokens, seqs, slots, pages, heads, dim;
   Divider rows, token_rows;     // of a page; of a token: 2 heads
-  uint32_t rows_each, pad;      // (this, and the next two, are the launcher's)
+  uint32_t rows_each, append_grid;   // (these two, and the next two, are the launcher's)
   Divider slots_each, pairs;
   int64_t k_token, k_head, v_token, v_head;   // element strides
   Rotary rotary;
+  // a rotation that shares the launch (the queries of the tokens whose keys are appended); rope.out null: none
+  RopeArgs rope;
 };
 
 // out[s][h] = softmax(scale q K^T) V over sequence s's keys in the paged cache.  Work is counted in tiles of `tile` keys for

@@ -23,6 +23,7 @@ hipError_t launch_gemm_bf16(const GemmArgs& a, hipStream_t s);   // 128 x 128 ti
 enum OperatorKernel : uint32_t { kOpRope = 0, kOpCacheAppend, kOpPagedAttention, kOperatorKernels };
 typedef hipError_t (*OperatorLauncher)(const void* args, hipStream_t s);
 bool set_operator(OperatorKernel which, OperatorLauncher launch);   // true
+hipError_t launch_operator(OperatorKernel which, const void* args, hipStream_t s);
 
 // The library's static device scratch (lt_static_scratch.hip): its size, its address on `device`
 // (looked up once per device; `device` must be current), and a fill kernel.

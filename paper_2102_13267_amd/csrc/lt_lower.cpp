@@ -1825,19 +1825,48 @@ struct Lowering {
     args.s_inner = x.s_inner;
     args.s_head = x.s_head;
     rotary_of(an, an->op == LT_OP_ROPE_GRAD, &args.rotary);
-    Launch l = make_launch(L_ROPE, k, args);
-    l.bytes = 2 * (uint64_t)count(shape_of(a)) * dtype_size(an->dtype) + 4 * (uint64_t)count(out_shape(rins[a][1]));
-    plan->launches.push_back(std::move(l));
-    patch(launch, offsetof(ltk::RopeArgs, x), x.storage, x.byte_offset);
-    patch(launch, offsetof(ltk::RopeArgs, positions), ps, po);
-    patch(launch, offsetof(ltk::RopeArgs, out), storage_of[a][0], 0, true);
+    const uint64_t bytes = 2 * (uint64_t)count(shape_of(a)) * dtype_size(an->dtype) + 4 * (uint64_t)count(out_shape(rins[a][1]));
+    const int32_t out = storage_of[a][0];
+    // behind an append that it has nothing to do with, it shares that one's launch
+    const int before = launch - 1;
+    const bool rides = merge && launch > 0 && plan->launches[before].kind == L_APPEND && !((const ltk::AppendArgs*)plan->launches[before].args.data())->rope.dim &&
+                       apart(before, {x.storage, ps}, out);
+    const int at = rides ? before : launch;
+    const size_t base = rides ? offsetof(ltk::AppendArgs, rope) : 0;
+    if (rides) {
+      ((ltk::AppendArgs*)plan->launches[before].args.data())->rope = args;
+      plan->launches[before].bytes += bytes;
+      plan->merged = true;
+    } else {
+      Launch l = make_launch(L_ROPE, k, args);
+      l.bytes = bytes;
+      plan->launches.push_back(std::move(l));
+    }
+    patch(at, base + offsetof(ltk::RopeArgs, x), x.storage, x.byte_offset);
+    patch(at, base + offsetof(ltk::RopeArgs, positions), ps, po);
+    patch(at, base + offsetof(ltk::RopeArgs, out), out, 0, true);
+    return true;
+  }
+
+  // Whether a launch that reads `in` and writes `out` may run next to launch `l`: neither touches what the other writes.
+  bool apart(int l, const std::vector<int32_t>& in, int32_t out) const {
+    auto same = [&](int32_t s, int32_t t) {
+      const Storage &x = plan->storages[s], &y = plan->storages[t];
+      return s == t || (x.param >= 0 && x.param == y.param);
+    };
+    for (const PtrPatch& p : plan->ptr_patches) {
+      if ((int)p.launch != l) continue;
+      if (same(p.storage, out)) return false;
+      for (int32_t s : in)
+        if (p.write && same(p.storage, s)) return false;
+    }
     return true;
   }
 
   // New rows of a cache: written into its own (donated) buffer, or into a copy.
   bool emit_append(int k, int32_t a) {
     const Node* an = nd[a];
-    const int launch = (int)plan->launches.size();
+    int launch = (int)plan->launches.size();
     Heads kv[2];
     int32_t s[4] = {-1, -1, -1, -1};   // cache, lengths, table, offsets
     int64_t o[4] = {0, 0, 0, 0};
@@ -1865,10 +1894,24 @@ struct Lowering {
     args.v_token = kv[1].s_inner;
     args.v_head = kv[1].s_head;
     if (an->n_attr > 0) rotary_of(an, false, &args.rotary);
+    // a rotation just before it that it has nothing to do with shares its launch
+    const bool takes = merge && launch > 0 && plan->launches[launch - 1].kind == L_ROPE &&
+                       apart(launch - 1, ragged ? std::vector<int32_t>{s[0], kv[0].storage, kv[1].storage, s[1], s[2], s[3]} : std::vector<int32_t>{s[0], kv[0].storage, kv[1].storage, s[1], s[2]}, out);
     Launch l = make_launch(L_APPEND, k, args);
     const uint64_t n = (uint64_t)count(ks);
     l.bytes = 2 * n * (dtype_size(args.dtype) + dtype_size(an->dtype)) + (in_place ? 0 : 2 * args.cache_elems * dtype_size(an->dtype));
-    plan->launches.push_back(std::move(l));
+    if (takes) {
+      launch -= 1;
+      Launch& r = plan->launches[launch];
+      ((ltk::AppendArgs*)l.args.data())->rope = *(const ltk::RopeArgs*)r.args.data();
+      l.bytes += r.bytes;
+      for (PtrPatch& p : plan->ptr_patches)
+        if ((int)p.launch == launch) p.offset += (uint32_t)offsetof(ltk::AppendArgs, rope);
+      r = std::move(l);
+      plan->merged = true;
+    } else {
+      plan->launches.push_back(std::move(l));
+    }
     patch(launch, offsetof(ltk::AppendArgs, cache), out, 0, true);
     if (!in_place) patch(launch, offsetof(ltk::AppendArgs, copy_from), s[0], o[0]);
     patch(launch, offsetof(ltk::AppendArgs, k), kv[0].storage, kv[0].byte_offset);

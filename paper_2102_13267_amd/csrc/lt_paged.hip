@@ -67,8 +67,7 @@ __device__ __forceinline__ bool place(const AppendArgs& a, uint32_t t, uint32_t 
 constexpr uint32_t kMaxTokens = 256;   // of a workgroup
 
 template <typename C, typename T, int V, bool IL>
-__global__ __launch_bounds__(kBlock) void lt_cache_append_kernel(const AppendArgs a) {
-  __shared__ Turn turns[kMaxTurns];
+__device__ __forceinline__ void append_rows(const AppendArgs& a, Turn* turns) {
   __shared__ int64_t to[kMaxTokens];
   __shared__ int32_t position[kMaxTokens];
   __shared__ uint32_t sequence[kMaxTokens];
@@ -125,6 +124,14 @@ __global__ __launch_bounds__(kBlock) void lt_cache_append_kernel(const AppendArg
   }
 }
 
+// RIDE: the workgroups behind the first `append_grid` rotate (AppendArgs::rope).
+template <typename C, typename T, int V, bool IL, bool RIDE>
+__global__ __launch_bounds__(kBlock) void lt_cache_append_kernel(const AppendArgs a) {
+  __shared__ Turn turns[kMaxTurns];
+  if (!RIDE || blockIdx.x < a.append_grid) append_rows<C, T, V, IL>(a, turns);
+  else if constexpr (RIDE) rope_rows<T, V, IL, kNothingPast>(a.rope, blockIdx.x - a.append_grid, turns);
+}
+
 // Rows that the above does not take: interleaved pairs at odd places, rows of very many slots.  One thread per pair (or element of the rest).
 template <typename C, typename T>
 __global__ __launch_bounds__(kBlock) void lt_cache_append_any_kernel(const AppendArgs a) {
@@ -156,7 +163,7 @@ __global__ __launch_bounds__(kBlock) void lt_cache_append_any_kernel(const Appen
 }
 
 template <typename C, typename T>
-hipError_t launch_append_of(AppendArgs a, hipStream_t s) {
+hipError_t launch_append_of(AppendArgs a, bool* rode, hipStream_t s) {
   constexpr uint32_t kMost = 16u / (sizeof(C) > sizeof(T) ? sizeof(C) : sizeof(T));
   const uint64_t rows = (uint64_t)a.tokens * a.token_rows.d;
   const uint64_t aligned = std::min(row_alignment(a.k, sizeof(T), a.k_token, a.k_head, 0), row_alignment(a.v, sizeof(T), a.v_token, a.v_head, 0));
@@ -168,19 +175,31 @@ hipError_t launch_append_of(AppendArgs a, hipStream_t s) {
     auto fits = [&](uint32_t each) { return tokens(each) * pairs <= kMaxTurns && tokens(each) <= kMaxTokens; };
     while (a.rows_each > 1u && (rows / (lanes * a.rows_each) < 1024u || !fits(a.rows_each))) a.rows_each /= 2u;
     const uint64_t grid = (rows + lanes * a.rows_each - 1) / (lanes * a.rows_each);
-    if (fits(a.rows_each) && grid < ((uint64_t)1 << 31)) {
+    if (fits(a.rows_each) && grid < ((uint64_t)1 << 30)) {
       a.slots_each.set(slots);
       a.pairs.set(pairs ? pairs : 1u);
+      a.append_grid = (uint32_t)grid;
       const dim3 g((uint32_t)grid), b(kBlock);
+      if constexpr (sizeof(C) == sizeof(T)) {
+        // a rotation of the same type and layout, in pieces of 16 bytes too, takes the launch's other workgroups
+        RopeLayout l;
+        if (a.rope.out && v == kMost && a.rope.dtype == a.dtype && a.rope.rotary.interleaved == a.rotary.interleaved && fit_to_run(a.rope) &&
+            lay_out(&a.rope, sizeof(T), &l) && l.v == kMost && l.past == kNothingPast && l.grid < (1u << 30)) {
+          *rode = true;
+          if (a.rotary.interleaved) LT_LAUNCH((lt_cache_append_kernel<C, T, kMost, true, true>), dim3(a.append_grid + l.grid), b, s, a);
+          else LT_LAUNCH((lt_cache_append_kernel<C, T, kMost, false, true>), dim3(a.append_grid + l.grid), b, s, a);
+          return hipGetLastError();
+        }
+      }
       if (a.rotary.interleaved) {
-        if (v == kMost) LT_LAUNCH((lt_cache_append_kernel<C, T, kMost, true>), g, b, s, a);
-        else if (v == 4u) LT_LAUNCH((lt_cache_append_kernel<C, T, 4, true>), g, b, s, a);
-        else LT_LAUNCH((lt_cache_append_kernel<C, T, 2, true>), g, b, s, a);
+        if (v == kMost) LT_LAUNCH((lt_cache_append_kernel<C, T, kMost, true, false>), g, b, s, a);
+        else if (v == 4u) LT_LAUNCH((lt_cache_append_kernel<C, T, 4, true, false>), g, b, s, a);
+        else LT_LAUNCH((lt_cache_append_kernel<C, T, 2, true, false>), g, b, s, a);
       } else {
-        if (v == kMost) LT_LAUNCH((lt_cache_append_kernel<C, T, kMost, false>), g, b, s, a);
-        else if (v == 4u) LT_LAUNCH((lt_cache_append_kernel<C, T, 4, false>), g, b, s, a);
-        else if (v == 2u) LT_LAUNCH((lt_cache_append_kernel<C, T, 2, false>), g, b, s, a);
-        else LT_LAUNCH((lt_cache_append_kernel<C, T, 1, false>), g, b, s, a);
+        if (v == kMost) LT_LAUNCH((lt_cache_append_kernel<C, T, kMost, false, false>), g, b, s, a);
+        else if (v == 4u) LT_LAUNCH((lt_cache_append_kernel<C, T, 4, false, false>), g, b, s, a);
+        else if (v == 2u) LT_LAUNCH((lt_cache_append_kernel<C, T, 2, false, false>), g, b, s, a);
+        else LT_LAUNCH((lt_cache_append_kernel<C, T, 1, false, false>), g, b, s, a);
       }
       return hipGetLastError();
     }
@@ -190,8 +209,7 @@ hipError_t launch_append_of(AppendArgs a, hipStream_t s) {
   return hipGetLastError();
 }
 
-hipError_t launch_append(const void* args, hipStream_t s) {
-  const AppendArgs& a = *(const AppendArgs*)args;
+hipError_t launch_new_rows(const AppendArgs& a, bool* rode, hipStream_t s) {
   if (a.cache_elems == 0) return hipSuccess;
   if (!a.cache || a.rows.d == 0 || a.token_rows.d != 2u * a.heads || a.rotary.dims > a.dim || a.rotary.dims > 2u * kMaxPairs) return hipErrorInvalidValue;
   if (a.copy_from) {
@@ -200,11 +218,20 @@ hipError_t launch_append(const void* args, hipStream_t s) {
   }
   if (a.tokens == 0 || a.seqs == 0 || a.slots == 0) return hipGetLastError();
   if (!a.k || !a.v || !a.lengths || !a.table) return hipErrorInvalidValue;
-  if (a.cache_dtype == kF32 && a.dtype == kF32) return launch_append_of<float, float>(a, s);
-  if (a.cache_dtype == kF32 && a.dtype == kBF16) return launch_append_of<float, __bf16>(a, s);
-  if (a.cache_dtype == kBF16 && a.dtype == kF32) return launch_append_of<__bf16, float>(a, s);
-  if (a.cache_dtype == kBF16 && a.dtype == kBF16) return launch_append_of<__bf16, __bf16>(a, s);
+  if (a.cache_dtype == kF32 && a.dtype == kF32) return launch_append_of<float, float>(a, rode, s);
+  if (a.cache_dtype == kF32 && a.dtype == kBF16) return launch_append_of<float, __bf16>(a, rode, s);
+  if (a.cache_dtype == kBF16 && a.dtype == kF32) return launch_append_of<__bf16, float>(a, rode, s);
+  if (a.cache_dtype == kBF16 && a.dtype == kBF16) return launch_append_of<__bf16, __bf16>(a, rode, s);
   return hipErrorInvalidValue;
+}
+
+// (a rotation that cannot share the launch gets its own)
+hipError_t launch_append(const void* args, hipStream_t s) {
+  const AppendArgs& a = *(const AppendArgs*)args;
+  bool rode = false;
+  const hipError_t e = launch_new_rows(a, &rode, s);
+  if (e != hipSuccess || rode || !a.rope.out) return e;
+  return launch_operator(kOpRope, &a.rope, s);
 }
 
 // ---- attention of one new token -------------------------------------------------------------------
@@ -405,8 +432,12 @@ __global__ __launch_bounds__(kBlock, DP <= 128 && NH == 1 && AL == 16 ? (DP == 6
   const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15u, g = lane >> 4;
 
   Chunk w;
+  uint32_t t0, t1;
   if (a.split) {
     if (!find_chunk<G::TILE>(a, &w)) return;
+    const uint32_t even = w.tiles / w.parts, odd = w.tiles - even * w.parts;
+    t0 = w.part * even + min(w.part, odd);
+    t1 = t0 + even + (w.part < odd ? 1u : 0u);
   } else {
     w.seq = blockIdx.x / a.pairs;
     w.pair = blockIdx.x - w.seq * a.pairs;
@@ -414,10 +445,18 @@ __global__ __launch_bounds__(kBlock, DP <= 128 && NH == 1 && AL == 16 ? (DP == 6
     w.tiles = tiles_of<G::TILE>(w.len);
     w.part = w.piece0 = 0u;
     w.parts = 1u;
+    t0 = 0u;
+    t1 = w.tiles;
   }
+  // PG: the page numbers of a wave's next 64 tiles of 16 keys lie in its lanes, lane KT s + t those of tile t of its step s; the first are
+  // asked for before the sequence's length has to be known
+  auto pages_from = [&](uint32_t key0) {
+    const uint32_t k = key0 + lane / KT * G::TILE + lane % KT * 16u;
+    return k < a.capacity ? a.table[(uint64_t)w.seq * a.slots + divide(a.rows, k)] : -1;
+  };
+  int32_t pages_next = PG ? pages_from(t0 * G::TILE + wave * G::WK) : -1;
   const uint32_t group = a.heads / a.kv_heads, blocks = a.pairs / a.kv_heads, kh = w.pair / blocks, h0 = kh * group + (w.pair - kh * blocks) * 16u * NH,
                  heads = min(16u * NH, (kh + 1u) * group - h0);
-  const uint32_t even = w.tiles / w.parts, odd = w.tiles - even * w.parts, t0 = w.part * even + min(w.part, odd), t1 = t0 + even + (w.part < odd ? 1u : 0u);
   const uint32_t key_end = (uint32_t)min((uint64_t)t1 * G::TILE, (uint64_t)w.len);
   const int64_t value = (int64_t)a.kv_heads * a.rows.d * a.dim;   // from a key to its value
 
@@ -449,8 +488,7 @@ __global__ __launch_bounds__(kBlock, DP <= 128 && NH == 1 && AL == 16 ? (DP == 6
   const uint32_t key_at = (n * a.dim + g * G::CE) * kSize, key_at0 = g * 16u, value_at0 = (n * NV < a.dim ? n * NV : 0u) * kSize;
 
   // Where a step's keys lie.  PG: a page holds whole tiles of 16, so a tile has one page: its first row, and how many of its keys there are.
-  // The page numbers of a wave's next 64 tiles lie in its lanes, and those of the 64 after that are on their way.  Otherwise every lane finds
-  // its own keys, and a stretch's page numbers lie in LDS.
+  // Otherwise every lane finds its own keys, and a stretch's page numbers lie in LDS.
   const uint32_t stretch = PG ? 0x7fffffffu / G::TILE : (uint32_t)min((uint64_t)(kSlots - 2) * a.rows.d / G::TILE, (uint64_t)0x7fffffffu / G::TILE);
   for (uint32_t first = t0; first < t1; first += stretch) {
     const uint32_t k0 = first * G::TILE, k1 = (uint32_t)min((uint64_t)first * G::TILE + (uint64_t)stretch * G::TILE, (uint64_t)key_end);
@@ -466,25 +504,20 @@ __global__ __launch_bounds__(kBlock, DP <= 128 && NH == 1 && AL == 16 ? (DP == 6
       __syncthreads();
     }
     const uint32_t wave0 = k0 + wave * G::WK;
-    auto pages_from = [&](uint32_t step) {   // lane KT s + t: of tile t of the wave's step number step + s
-      const uint32_t k = wave0 + (step + lane / KT) * G::TILE + lane % KT * 16u;
-      const int32_t p = k < k1 ? a.table[(uint64_t)w.seq * a.slots + divide(a.rows, k)] : -1;
-      return p >= 0 && (uint32_t)p < a.pages ? p : -1;
-    };
-    int32_t pages_now = -1, pages_next = -1;
+    int32_t pages_now = -1;
     const char* tile[KT];
     uint32_t there[KT], step = 0;
     auto find_tiles = [&](uint32_t key0) {
       if (step % (64 / KT) == 0u) {
-        pages_now = step == 0u ? pages_from(0u) : pages_next;
-        pages_next = pages_from(step + 64 / KT);
+        pages_now = pages_next >= 0 && (uint32_t)pages_next < a.pages ? pages_next : -1;
+        pages_next = pages_from(key0 + 64 / KT * G::TILE);
       }
 #pragma unroll
       for (int t = 0; t < KT; ++t) {
         const uint32_t k = key0 + 16u * t;
         const int32_t p = __builtin_amdgcn_readlane(pages_now, (int)(step % (64 / KT) * KT + t));
-        there[t] = p >= 0 ? min(16u, k1 - k) : 0u;
-        tile[t] = (const char*)a.cache + (p >= 0 ? (((int64_t)p * 2 * a.kv_heads + kh) * a.rows.d + (k - divide(a.rows, k) * a.rows.d)) * a.dim * kSize : (int64_t)0);
+        there[t] = p >= 0 && k < k1 ? min(16u, k1 - k) : 0u;
+        tile[t] = (const char*)a.cache + (there[t] > 0u ? (((int64_t)p * 2 * a.kv_heads + kh) * a.rows.d + (k - divide(a.rows, k) * a.rows.d)) * a.dim * kSize : (int64_t)0);
       }
       ++step;
     };

@@ -17,40 +17,10 @@
 namespace ltk {
 namespace {
 
-enum Past { kNothingPast, kReadsPast, kAllPast };
-
 template <typename T, int V, bool IL, Past PAST>
 __global__ __launch_bounds__(kRowBlock) void lt_rope_kernel(const RopeArgs a) {
   __shared__ Turn turns[kMaxTurns];
-  const uint32_t pairs = a.rotary.dims / 2u, lane = divide(a.slots, threadIdx.x), u = threadIdx.x - lane * a.slots.d, lanes = kRowBlock / a.slots.d;
-  const uint64_t row0 = (uint64_t)blockIdx.x * (lanes * a.rows_each), rows = a.tokens * a.heads.d;
-  const uint32_t n = (uint32_t)(rows - row0 < (uint64_t)lanes * a.rows_each ? rows - row0 : (uint64_t)lanes * a.rows_each);
-  const uint32_t token0 = rows < 0x7fffffffu ? divide(a.heads, (uint32_t)row0) : (uint32_t)(row0 / a.heads.d), head0 = (uint32_t)(row0 - (uint64_t)token0 * a.heads.d);
-  bool turned;
-  const uint32_t at = slot_at<V, IL>(a.rotary, u, &turned);
-  Slot<T, V, IL> s[kMaxRows];
-  uint32_t token[kMaxRows];
-#pragma unroll
-  for (int i = 0; i < kMaxRows; ++i) {
-    const uint32_t r = lane + i * lanes;
-    token[i] = divide(a.heads, head0 + r);   // (after the first)
-    if (r >= n || lane >= lanes) continue;
-    const uint32_t h = head0 + r - token[i] * a.heads.d, t = token0 + token[i], o = a.s_outer == 0 ? 0u : divide(a.inner, t);
-    const T* row = (const T*)a.x + (int64_t)o * a.s_outer + (int64_t)(a.whole ? t : t - divide(a.inner, t) * a.inner.d) * a.s_inner + (int64_t)h * a.s_head;
-    load_slot<T, V, IL, PAST != kNothingPast>(row, a.rotary, at, turned, &s[i]);
-  }
-  const uint32_t tokens = divide(a.heads, head0 + n - 1u) + 1u;
-  for (uint32_t i = threadIdx.x; i < tokens * pairs; i += kRowBlock) {
-    const uint32_t k = divide(a.pairs, i), t = token0 + k;
-    turns[i] = turn_of(a.rotary, a.positions[t - divide(a.n_pos, t) * a.n_pos.d], i - k * pairs);
-  }
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < kMaxRows; ++i) {
-    const uint32_t r = lane + i * lanes;
-    if (r >= n || lane >= lanes) continue;
-    store_slot<T, T, V, IL, PAST == kAllPast>((T*)a.out + (row0 + r) * a.dim, a.rotary, at, turned, s[i], turns + token[i] * pairs);
-  }
+  rope_rows<T, V, IL, PAST>(a, blockIdx.x, turns);
 }
 
 // Rows that the above does not take: interleaved pairs at odd places, rows of very many slots.  One thread per pair (or element of the rest).
@@ -77,44 +47,30 @@ __global__ __launch_bounds__(kRowBlock) void lt_rope_any_kernel(const RopeArgs a
 }
 
 template <typename T, int V, bool IL>
-void launch_rows(const RopeArgs& a, uint32_t grid, Past past, hipStream_t s) {
-  if (past == kAllPast) LT_LAUNCH((lt_rope_kernel<T, V, IL, kAllPast>), dim3(grid), dim3(kRowBlock), s, a);
-  else if (past == kReadsPast) LT_LAUNCH((lt_rope_kernel<T, V, IL, kReadsPast>), dim3(grid), dim3(kRowBlock), s, a);
-  else LT_LAUNCH((lt_rope_kernel<T, V, IL, kNothingPast>), dim3(grid), dim3(kRowBlock), s, a);
+void launch_rows(const RopeArgs& a, const RopeLayout& l, hipStream_t s) {
+  if (l.past == kAllPast) LT_LAUNCH((lt_rope_kernel<T, V, IL, kAllPast>), dim3(l.grid), dim3(kRowBlock), s, a);
+  else if (l.past == kReadsPast) LT_LAUNCH((lt_rope_kernel<T, V, IL, kReadsPast>), dim3(l.grid), dim3(kRowBlock), s, a);
+  else LT_LAUNCH((lt_rope_kernel<T, V, IL, kNothingPast>), dim3(l.grid), dim3(kRowBlock), s, a);
 }
 
 template <typename T>
 hipError_t launch_rope_of(RopeArgs a, hipStream_t s) {
-  const uint64_t rows = a.tokens * a.heads.d, aligned = row_alignment(a.x, sizeof(T), a.s_outer, a.s_inner, a.s_head);
-  const uint32_t v = piece_of(a.rotary, a.dim, aligned, 16u / sizeof(T)), slots = v ? slots_of(a.rotary, a.dim, v) : 0u, pairs = a.rotary.dims / 2u;
-  const uint64_t bytes = rows * a.dim * sizeof(T), cache = (uint64_t)256 << 20;
-  const Past past = bytes >= cache ? kAllPast : 2 * bytes >= cache ? kReadsPast : kNothingPast;
-  // rows a thread: four where that leaves four workgroups a compute unit, and the tokens' turns fit
-  a.rows_each = past == kNothingPast ? kMaxRows : 2u;
-  if (v && slots <= kRowBlock) {
-    const uint32_t lanes = kRowBlock / slots;
-    auto tokens = [&](uint32_t each) { return (lanes * each + a.heads.d - 2u) / a.heads.d + 1u; };
-    while (a.rows_each > 1u && (rows / (lanes * a.rows_each) < 1024u || tokens(a.rows_each) * pairs > kMaxTurns)) a.rows_each /= 2u;
-    if (tokens(a.rows_each) * pairs <= kMaxTurns) {
-      a.slots.set(slots);
-      a.pairs.set(pairs);
-      const uint64_t grid = (rows + lanes * a.rows_each - 1) / (lanes * a.rows_each);
-      if (grid < ((uint64_t)1 << 31)) {
-        if (a.rotary.interleaved) {
-          if (v * sizeof(T) == 16u) launch_rows<T, 16 / sizeof(T), true>(a, (uint32_t)grid, past, s);
-          else if (v == 4u) launch_rows<T, 4, true>(a, (uint32_t)grid, past, s);
-          else launch_rows<T, 2, true>(a, (uint32_t)grid, past, s);
-        } else {
-          if (v * sizeof(T) == 16u) launch_rows<T, 16 / sizeof(T), false>(a, (uint32_t)grid, past, s);
-          else if (v == 4u) launch_rows<T, 4, false>(a, (uint32_t)grid, past, s);
-          else if (v == 2u) launch_rows<T, 2, false>(a, (uint32_t)grid, past, s);
-          else launch_rows<T, 1, false>(a, (uint32_t)grid, past, s);
-        }
-        return hipGetLastError();
-      }
+  constexpr int kMost = 16 / sizeof(T);
+  RopeLayout l;
+  if (lay_out(&a, sizeof(T), &l)) {
+    if (a.rotary.interleaved) {
+      if (l.v == kMost) launch_rows<T, kMost, true>(a, l, s);
+      else if (l.v == 4u) launch_rows<T, 4, true>(a, l, s);
+      else launch_rows<T, 2, true>(a, l, s);
+    } else {
+      if (l.v == kMost) launch_rows<T, kMost, false>(a, l, s);
+      else if (l.v == 4u) launch_rows<T, 4, false>(a, l, s);
+      else if (l.v == 2u) launch_rows<T, 2, false>(a, l, s);
+      else launch_rows<T, 1, false>(a, l, s);
     }
+    return hipGetLastError();
   }
-  const uint64_t n = (rows * (a.dim - pairs) + kRowBlock - 1) / kRowBlock;
+  const uint64_t n = (a.tokens * a.heads.d * (a.dim - a.rotary.dims / 2u) + kRowBlock - 1) / kRowBlock;
   LT_LAUNCH(lt_rope_any_kernel<T>, dim3((uint32_t)(n < 65536u ? n : 65536u)), dim3(kRowBlock), s, a);
   return hipGetLastError();
 }
@@ -122,7 +78,7 @@ hipError_t launch_rope_of(RopeArgs a, hipStream_t s) {
 hipError_t launch_rope(const void* args, hipStream_t s) {
   const RopeArgs& a = *(const RopeArgs*)args;
   if (a.tokens * a.heads.d * a.dim == 0) return hipSuccess;
-  if (!a.x || !a.positions || !a.out || a.inner.d == 0 || a.n_pos.d == 0 || a.rotary.dims > a.dim || a.rotary.dims > 2u * kMaxPairs) return hipErrorInvalidValue;
+  if (!fit_to_run(a)) return hipErrorInvalidValue;
   return a.dtype == kF32 ? launch_rope_of<float>(a, s) : a.dtype == kBF16 ? launch_rope_of<__bf16>(a, s) : hipErrorInvalidValue;
 }
 

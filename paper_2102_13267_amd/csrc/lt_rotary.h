@@ -138,5 +138,71 @@ inline uint64_t row_alignment(const void* p, uint64_t size, int64_t s0, int64_t 
   return bits & (~bits + 1u);
 }
 
+enum Past { kNothingPast, kReadsPast, kAllPast };
+
+// Workgroup `block` of a rotation: its rows (see above).
+template <typename T, int V, bool IL, Past PAST>
+__device__ __forceinline__ void rope_rows(const RopeArgs& a, uint32_t block, Turn* turns) {
+  const uint32_t pairs = a.rotary.dims / 2u, lane = divide(a.slots, threadIdx.x), u = threadIdx.x - lane * a.slots.d, lanes = kRowBlock / a.slots.d;
+  const uint64_t row0 = (uint64_t)block * (lanes * a.rows_each), rows = a.tokens * a.heads.d;
+  const uint32_t n = (uint32_t)(rows - row0 < (uint64_t)lanes * a.rows_each ? rows - row0 : (uint64_t)lanes * a.rows_each);
+  const uint32_t token0 = rows < 0x7fffffffu ? divide(a.heads, (uint32_t)row0) : (uint32_t)(row0 / a.heads.d), head0 = (uint32_t)(row0 - (uint64_t)token0 * a.heads.d);
+  bool turned;
+  const uint32_t at = slot_at<V, IL>(a.rotary, u, &turned);
+  Slot<T, V, IL> s[kMaxRows];
+  uint32_t token[kMaxRows];
+#pragma unroll
+  for (int i = 0; i < kMaxRows; ++i) {
+    const uint32_t r = lane + i * lanes;
+    token[i] = divide(a.heads, head0 + r);   // (after the first)
+    if (r >= n || lane >= lanes) continue;
+    const uint32_t h = head0 + r - token[i] * a.heads.d, t = token0 + token[i], o = a.s_outer == 0 ? 0u : divide(a.inner, t);
+    const T* row = (const T*)a.x + (int64_t)o * a.s_outer + (int64_t)(a.whole ? t : t - divide(a.inner, t) * a.inner.d) * a.s_inner + (int64_t)h * a.s_head;
+    load_slot<T, V, IL, PAST != kNothingPast>(row, a.rotary, at, turned, &s[i]);
+  }
+  const uint32_t tokens = divide(a.heads, head0 + n - 1u) + 1u;
+  for (uint32_t i = threadIdx.x; i < tokens * pairs; i += kRowBlock) {
+    const uint32_t k = divide(a.pairs, i), t = token0 + k;
+    turns[i] = turn_of(a.rotary, a.positions[t - divide(a.n_pos, t) * a.n_pos.d], i - k * pairs);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kMaxRows; ++i) {
+    const uint32_t r = lane + i * lanes;
+    if (r >= n || lane >= lanes) continue;
+    store_slot<T, T, V, IL, PAST == kAllPast>((T*)a.out + (row0 + r) * a.dim, a.rotary, at, turned, s[i], turns + token[i] * pairs);
+  }
+}
+
+// How a rotation's rows are laid out over workgroups: the launcher's part of its arguments, the elements of a piece, and the grid.
+// false: rows that the above does not take (interleaved pairs at odd places, rows of very many slots).
+struct RopeLayout {
+  uint32_t v, grid;
+  Past past;
+};
+inline bool lay_out(RopeArgs* a, uint32_t size, RopeLayout* l) {
+  const uint64_t rows = a->tokens * a->heads.d, aligned = row_alignment(a->x, size, a->s_outer, a->s_inner, a->s_head);
+  const uint32_t v = piece_of(a->rotary, a->dim, aligned, 16u / size), slots = v ? slots_of(a->rotary, a->dim, v) : 0u, pairs = a->rotary.dims / 2u;
+  if (v == 0 || slots > kRowBlock) return false;
+  const uint64_t bytes = rows * a->dim * size, cache = (uint64_t)256 << 20;
+  l->past = bytes >= cache ? kAllPast : 2 * bytes >= cache ? kReadsPast : kNothingPast;
+  // rows a thread: four where that leaves four workgroups a compute unit, and the tokens' turns fit
+  a->rows_each = l->past == kNothingPast ? kMaxRows : 2u;
+  const uint32_t lanes = kRowBlock / slots;
+  auto tokens = [&](uint32_t each) { return (lanes * each + a->heads.d - 2u) / a->heads.d + 1u; };
+  while (a->rows_each > 1u && (rows / (lanes * a->rows_each) < 1024u || tokens(a->rows_each) * pairs > kMaxTurns)) a->rows_each /= 2u;
+  const uint64_t grid = (rows + lanes * a->rows_each - 1) / (lanes * a->rows_each);
+  if (tokens(a->rows_each) * pairs > kMaxTurns || grid >= ((uint64_t)1 << 31)) return false;
+  a->slots.set(slots);
+  a->pairs.set(pairs);
+  l->v = v;
+  l->grid = (uint32_t)grid;
+  return true;
+}
+
+inline bool fit_to_run(const RopeArgs& a) {
+  return a.x && a.positions && a.out && a.inner.d > 0 && a.n_pos.d > 0 && a.rotary.dims <= a.dim && a.rotary.dims <= 2u * kMaxPairs;
+}
+
 }  // namespace ltk
 #endif

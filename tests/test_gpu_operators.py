@@ -481,6 +481,32 @@ def test_decoding_replays_a_captured_step(graphs):
     ctx.close()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dim,rq,rk", [(64, Rotary(), Rotary()), (64, Rotary(interleaved=True), Rotary(interleaved=True, factor=2.0)), (64, Rotary(), Rotary(interleaved=True)), (64, Rotary(), None),
+                                       (20, Rotary(), Rotary()), (64, Rotary(dims=20), Rotary()), (7, Rotary(dims=6, interleaved=True), Rotary(dims=2))])
+def test_a_rotation_in_the_launch_of_an_append(dim, rq, rk, dtype):
+    """of the same layout and of others, which get a launch of their own: the bits of the two by themselves"""
+    rg = np.random.default_rng(21)
+    lens = [5, 1, 40, 0, 17]
+    cache, table = paged_case(rg, lens, 2, 16, dim, dtype)
+    q, k, v = (data(rg, (n, h, dim), dtype) for n, h in ((9, 6), (5, 2), (5, 2)))
+    outs = []
+    for fusion in (True, False):
+        ctx = context()
+        ctx.set_fusion(fusion)
+        C, L, T, P = ctx.tensor(cache, dtype, donatable=True), ctx.tensor(ints(lens)), ctx.tensor(table), ctx.tensor(ints(rg.integers(0, 1, 9) + np.arange(9)))
+        ctx.assign(C, ctx.cache_append(C, ctx.tensor(k, dtype), ctx.tensor(v, dtype), L, T, rotary=rk))
+        y = ctx.rope(ctx.tensor(q, dtype), P, rq)
+        ctx.barrier()
+        assert len(ctx.dump_schedule().splitlines()) == (1 if fusion else 2)
+        outs.append((ctx.fetch(C), ctx.fetch(y)))
+        ctx.close()
+    assert np.array_equal(outs[0][0], outs[1][0]) and np.array_equal(outs[0][1], outs[1][1])
+    E = Eager("f64")
+    ref = E.fetch(E.rope(E.tensor(q, dtype), E.tensor(ints(np.arange(9))), rq))
+    assert (np.abs(outs[0][1] - ref) <= rope_bound(q, ref, rq, dtype)).all()
+
+
 def test_decoding_through_the_static_barrier():
     ctx = context()
     d = Decoder(ctx, "bf16", np.random.default_rng(17))

@@ -164,10 +164,61 @@ def test_new_rows_are_written_in_place_and_read_behind_that():
     t, o = decode(c)      # noqa: F841
     c.barrier()
     plan, sched = c.dump_plan(), c.dump_schedule()
-    assert "->p" in plan and plan.count(" OP ") == 3 and sorted(line.split()[1] for line in sched.splitlines()) == ["APPEND", "PAGED", "ROPE"]
+    assert "->p" in plan and plan.count(" OP ") == 3 and kinds(c) == ["APPEND", "PAGED"]
     append = next(line for line in sched.splitlines() if " APPEND " in line)
     wrote = append.split("writes=[")[1].split("]")[0]
-    assert wrote.startswith("p") and wrote in next(line for line in sched.splitlines() if " PAGED " in line).split("reads=[")[1].split("]")[0].split(",")
+    assert wrote.startswith("p") and set(wrote.split(",")) <= set(next(line for line in sched.splitlines() if " PAGED " in line).split("reads=[")[1].split("]")[0].split(","))
+
+
+def kinds(c):
+    return [line.split()[1] for line in c.dump_schedule().splitlines()]
+
+
+def test_a_rotation_shares_the_launch_of_an_append_that_it_has_nothing_to_do_with():
+    for first in (False, True):                 # whichever of the two comes first
+        c = Context()
+        t = paged(c)
+        q = c.rope(t["q"], t["lengths"]) if first else None
+        new = c.cache_append(t["cache"], t["k"], t["v"], t["lengths"], t["table"], rotary=Rotary())
+        q = q or c.rope(t["q"], t["lengths"])
+        c.barrier()
+        assert kinds(c) == ["APPEND"] and len(c.dump_plan().splitlines()) == 2
+        line = c.dump_schedule()
+        assert len(line.split("writes=[")[1].split("]")[0].split(",")) == 2
+        del new, q
+    c = Context()                               # one region per op: a launch each
+    c.set_fusion(False)
+    t, o = decode(c)      # noqa: F841
+    c.barrier()
+    assert sorted(kinds(c)) == ["APPEND", "PAGED", "ROPE"]
+
+
+def test_a_rotation_keeps_its_launch_next_to_an_append_that_reads_or_writes_what_it_does():
+    c = Context()
+    t = paged(c)
+    v = zeros(c, (3, 2, 8), donatable=True)
+    new = c.cache_append(t["cache"], t["k"], v, t["lengths"], t["table"])      # noqa: F841
+    c.assign(v, c.rope(t["k"], t["lengths"]))   # overwrites what the append reads
+    c.barrier()
+    assert kinds(c) == ["APPEND", "ROPE"] and "->p" in c.dump_plan()
+    c = Context()
+    t = paged(c)
+    k = c.rope(t["k"], t["lengths"])            # what the append reads
+    new = c.cache_append(t["cache"], k, t["v"], t["lengths"], t["table"])      # noqa: F841
+    c.barrier()
+    assert kinds(c) == ["ROPE", "APPEND"]
+    c = Context()
+    t = paged(c, seqs=7)
+    new = c.cache_append(t["cache"], t["k"], t["v"], t["lengths"], t["table"])
+    out = c.rope(c.narrow(c.reshape(new, (56, 2, 8)), 0, 3, 7), t["lengths"])      # noqa: F841  what the append writes
+    c.barrier()
+    assert kinds(c) == ["APPEND", "ROPE"]
+    c = Context()                               # a second one finds the place taken
+    t = paged(c)
+    new = c.cache_append(t["cache"], t["k"], t["v"], t["lengths"], t["table"])
+    out = [c.rope(t["q"], t["lengths"]), c.rope(t["k"], t["lengths"])]      # noqa: F841
+    c.barrier()
+    assert sorted(kinds(c)) == ["APPEND", "ROPE"]
 
 
 def test_a_cache_whose_own_rows_are_appended_is_copied():
