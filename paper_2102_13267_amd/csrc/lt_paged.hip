@@ -253,7 +253,7 @@ hipError_t launch_append(const void* args, hipStream_t s) {
 // smallest that gives all sequences together about kPagedChunks of them, but at least a.least: a join costs what a few tiles do.
 // A sequence's chunks are of equal length, so that a long one among short ones holds nobody up.  Pieces of a block meet in memory
 // (relaxed accesses of device scope, as the reductions exchange theirs), and whoever comes last joins them in their order: up
-// to eight at once, more in groups of about their root, whose last ones then join the groups.  So results do not depend on
+// to 32 at once, more in groups of about their root, whose last ones then join the groups.  So results do not depend on
 // who comes when.
 template <typename T, int DP, int NH> struct Geo {
   static constexpr bool BF = sizeof(T) == 2;
@@ -405,7 +405,7 @@ __device__ __forceinline__ bool find_chunk(const PagedArgs& a, Chunk* w) {
 
 // A piece: [16 NH heads][DP] sums of weights times values, [16 NH] maxima, [16 NH] sums of weights.
 template <int DP, int NH> constexpr uint32_t kPieceFloats = 16 * NH * DP + 32 * NH;
-constexpr uint32_t kMostPieces = 32;   // at once: the root of the largest number of them is 23
+constexpr uint32_t kMostPieces = 32;   // at once; in two steps at most 23 (the root of 512)
 
 // Whether the calling workgroup is the last of `count` to come here.
 __device__ __forceinline__ bool last_of(uint32_t* ticket, uint32_t count, uint32_t* flag) {
@@ -722,7 +722,10 @@ __global__ __launch_bounds__(kBlock, DP <= 128 && NH == 1 && AL == 16 ? (DP == 6
     publish(piece(w.part) + 16 * NH * DP + threadIdx.x, common(threadIdx.x));
     publish(piece(w.part) + 16 * NH * DP + 16 * NH + threadIdx.x, total_at(threadIdx.x));
   }
-  // pieces first, first + step, ... : joined, into the output or into the first one's place
+  // pieces first, first + step, ... : joined, into the output or into the first one's place.  A lane has four elements of a head; where the heads
+  // leave lanes over, several share an element's pieces.  Eight of a lane's pieces are on their way at once, the first of them
+  // together with the maxima.
+  const uint32_t units = heads * (DP / 4u), ways = units <= kBlock ? kBlock / units : 1u;
   auto join = [&](uint32_t first, uint32_t step, uint32_t count, bool out) {
     for (uint32_t i = threadIdx.x; i < count * 16u * NH; i += kBlock) {
       const uint32_t p = i / (16u * NH), h = i % (16u * NH);
@@ -730,39 +733,60 @@ __global__ __launch_bounds__(kBlock, DP <= 128 && NH == 1 && AL == 16 ? (DP == 6
       factor[p][h] = published(piece(first + p * step) + 16 * NH * DP + h);
       weight_of[p][h] = published(piece(first + p * step) + 16 * NH * DP + 16 * NH + h);
     }
-    __syncthreads();
-    if (threadIdx.x < heads) {
-      const uint32_t h = threadIdx.x;
-      float t = -INFINITY, total = 0.0f;
-      for (uint32_t p = 0; p < count; ++p) t = fmaxf(t, factor[p][h]);
-      for (uint32_t p = 0; p < count; ++p) {
-        const float f = power2(factor[p][h] - safe_of(t));
-        factor[p][h] = f;
-        total = fmaf(weight_of[p][h], f, total);
+    const uint32_t way = ways == 1u ? 0u : threadIdx.x / units;
+    for (uint32_t u = threadIdx.x - way * units; u < units || u < kBlock; u += kBlock) {
+      const uint32_t hh = u / (DP / 4u), d = u % (DP / 4u) * 4u;
+      const bool mine = u < units && way < ways && d < a.dim;
+      float4 t[8];
+      auto load = [&](uint32_t p0) {
+#pragma unroll
+        for (uint32_t i = 0; i < 8u; ++i)
+          if (mine && p0 + i * ways < count) t[i] = published4(piece(first + (p0 + i * ways) * step) + hh * DP + d);
+      };
+      load(way);
+      if (u < kBlock) {   // (the first time round)
+        __syncthreads();
+        if (threadIdx.x < heads) {
+          const uint32_t h = threadIdx.x;
+          float most = -INFINITY, total = 0.0f;
+          for (uint32_t p = 0; p < count; ++p) most = fmaxf(most, factor[p][h]);
+          for (uint32_t p = 0; p < count; ++p) {
+            const float f = power2(factor[p][h] - safe_of(most));
+            factor[p][h] = f;
+            total = fmaf(weight_of[p][h], f, total);
+          }
+          total_of[h] = total;
+          if (!out) {
+            publish(piece(first) + 16 * NH * DP + h, most);
+            publish(piece(first) + 16 * NH * DP + 16 * NH + h, total);
+          }
+        }
+        __syncthreads();
       }
-      total_of[h] = total;
-      if (!out) {
-        publish(piece(first) + 16 * NH * DP + h, t);
-        publish(piece(first) + 16 * NH * DP + 16 * NH + h, total);
-      }
-    }
-    __syncthreads();
-    for (uint32_t i = threadIdx.x; i < heads * DP / 4u; i += kBlock) {
-      const uint32_t hh = i / (DP / 4u), d = i % (DP / 4u) * 4u;
-      if (d >= a.dim) continue;
       F4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 8
-      for (uint32_t p = 0; p < count; ++p) {
-        const float4 t = published4(piece(first + p * step) + hh * DP + d);
-        const float f = factor[p][hh];
-        o = F4{fmaf(t.x, f, o[0]), fmaf(t.y, f, o[1]), fmaf(t.z, f, o[2]), fmaf(t.w, f, o[3])};
+      for (uint32_t p0 = way; mine && p0 < count; p0 += 8u * ways) {
+        if (p0 != way) load(p0);
+#pragma unroll
+        for (uint32_t i = 0; i < 8u; ++i)
+          if (p0 + i * ways < count) {
+            const float f = factor[p0 + i * ways][hh];
+            o = F4{fmaf(t[i].x, f, o[0]), fmaf(t[i].y, f, o[1]), fmaf(t[i].z, f, o[2]), fmaf(t[i].w, f, o[3])};
+          }
       }
+      if (ways > 1u) {   // (once round: units <= kBlock)
+        *(F4*)&meet[0][threadIdx.x * 4u] = o;
+        __syncthreads();
+        if (way != 0u) continue;
+        for (uint32_t x = 1; mine && x < ways; ++x) o += *(const F4*)&meet[0][(x * units + u) * 4u];
+      }
+      if (!mine) continue;
       if (out) put(hh, d, o, total_of[hh]);
       else publish4(piece(first) + hh * DP + d, make_float4(o[0], o[1], o[2], o[3]));
     }
   };
+  // (24 pieces at once and in two steps: 7 sequences of up to 3001 keys 12.9 / 15.1 us; 64: one of 131072 95.4 / 91.4)
   uint32_t each = w.parts;
-  if (w.parts > 8u)
+  if (w.parts > kMostPieces)
     for (each = 3u; each * each < w.parts;) ++each;
   const uint32_t first = w.part / each * each, groups = (w.parts + each - 1u) / each;
   if (!last_of(a.tickets + w.piece0 + first, min(each, w.parts - first), &last_flag)) return;
