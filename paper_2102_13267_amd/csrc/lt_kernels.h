@@ -349,6 +349,9 @@ struct AppendArgs {
 // piece (zero before and after a launch).  A sequence of t > c tiles has ceil(t / c) < 2 t / c chunks, so there are fewer than 2 kPagedChunks pieces.
 // Otherwise a workgroup has a block of a sequence.
 constexpr uint32_t kPagedChunks = 512;
+// Up to so many sequences a workgroup finds its chunk by itself; of more a list of them is written first (lengths of 100 to 1000, 2 key heads of
+// 128 bf16, by themselves / from a list, us: 128 sequences 22.7 / 25.2, 256 31.0 / 33.3, 1024 143 / 111, 16384 10870 / 1492).
+constexpr uint32_t kPagedFind = 256;
 struct PagedArgs {
   const void* q;
   const void* cache;
@@ -364,6 +367,8 @@ struct PagedArgs {
   uint32_t* tickets;
   uint32_t padded, blocks_of, pairs, tile;   // padded: the kernel instance's head size
   uint32_t workgroups, split, least;
+  uint32_t listed;              // entries of the list, one for each chunk there can be (0: none is written)
+  void* list;                   // behind the pieces (the launcher sets it)
   uint32_t pieces, q_whole;     // pieces: that parts and tickets are for.  q_whole: rows of q are whole 16-byte pieces (the launcher sets it)
 
   uint64_t part_floats() const { return (uint64_t)blocks_of * padded + 2u * blocks_of; }
@@ -380,7 +385,9 @@ struct PagedArgs {
     const uint64_t each = (most + least - 1u) / least;   // chunks of a sequence at most
     workgroups = (uint32_t)(split && each > 1u ? (all + kPagedChunks < all * each ? all + kPagedChunks : all * each) : all);
     pieces = (uint32_t)(split ? (2u * kPagedChunks < all * each ? 2u * kPagedChunks : all * each) : 0u);
+    listed = split && seqs > kPagedFind ? (workgroups + pairs - 1u) / pairs : 0u;
   }
+  uint64_t parts_bytes() const { return (uint64_t)pieces * part_floats() * sizeof(float) + 16u * (uint64_t)listed; }
 };
 
 // Argument blocks travel by value in the kernel argument segment, which holds 4 KiB.

@@ -1961,7 +1961,7 @@ struct Lowering {
     if (args.pieces > 0) {
       Storage parts;
       parts.first_launch = -1;
-      parts.bytes = (size_t)args.pieces * args.part_floats() * sizeof(float);
+      parts.bytes = (size_t)args.parts_bytes();
       plan->storages.push_back(parts);
       patch(launch, offsetof(ltk::PagedArgs, parts), (int32_t)plan->storages.size() - 1, 0, true);
     }

@@ -357,49 +357,116 @@ struct Chunk {
   uint32_t part, parts, piece0;  // part of `parts`, whose pieces lie from piece0 on
 };
 
-// Found by every wave for itself (four waves that meet at barriers took longer), as sums over the sequences, `each` of them a lane;
+// Found by every wave for itself (four waves that meet at barriers took longer), as sums over the sequences, up to four of them a lane;
 // false: there is none for this workgroup.
 template <uint32_t TILE>
 __device__ __forceinline__ bool find_chunk(const PagedArgs& a, Chunk* w) {
+  static_assert(kPagedFind <= 4 * 64, "lengths stay in registers");
   const uint32_t lane = threadIdx.x & 63u, each = (a.seqs + 63u) / 64u, from = lane * each;
-  // (the first four stay in registers)
   uint32_t len[4], tiles = 0;
 #pragma unroll
-  for (uint32_t i = 0; i < 4u; ++i) len[i] = i < each && from + i < a.seqs ? length_of(a, from + i) : 0xFFFFFFFFu;
-  auto length = [&](uint32_t i) { return i == 0u ? len[0] : i == 1u ? len[1] : i == 2u ? len[2] : i == 3u ? len[3] : length_of(a, from + i); };
+  for (uint32_t i = 0; i < 4u; ++i) len[i] = i < each && from + i < a.seqs ? length_of(a, from + i) : 0u;
   const uint32_t mine = from < a.seqs ? min(each, a.seqs - from) : 0u;
-  for (uint32_t i = 0; i < mine; ++i) tiles += tiles_of<TILE>(length(i));
+#pragma unroll
+  for (uint32_t i = 0; i < 4u; ++i) tiles += i < mine ? tiles_of<TILE>(len[i]) : 0u;
   const uint32_t all = (uint32_t)__builtin_amdgcn_readlane((int)sums_over_wave(tiles), 63) * a.pairs;
   const uint32_t c = max(a.least, (all + kPagedChunks - 1u) / kPagedChunks);
-  uint32_t chunks = 0, split = 0;
-  for (uint32_t i = 0; i < mine; ++i) {
-    const uint32_t k = (tiles_of<TILE>(length(i)) + c - 1u) / c;
-    chunks += k;
-    split += k > 1u ? k : 0u;
+  uint32_t k[4], chunks = 0, split = 0;
+#pragma unroll
+  for (uint32_t i = 0; i < 4u; ++i) {
+    k[i] = i < mine ? (tiles_of<TILE>(len[i]) + c - 1u) / c : 0u;
+    chunks += k[i];
+    split += k[i] > 1u ? k[i] : 0u;
   }
   uint32_t before = sums_over_wave(chunks) - chunks, split_before = sums_over_wave(split) - split;
   const uint32_t at = blockIdx.x;
   const uint64_t here = __ballot(before * a.pairs <= at && at < (before + chunks) * a.pairs);
   if (here == 0u) return false;
-  uint32_t i = 0, n, t, k;
-  for (;; ++i) {
-    n = i < mine ? length(i) : 0u;
-    t = tiles_of<TILE>(n);
-    k = (t + c - 1u) / c;
-    if (i + 1u >= mine || at < (before + k) * a.pairs) break;
-    before += k;
-    split_before += k > 1u ? k : 0u;
+  uint32_t i = 0, n = len[0], parts = k[0];
+#pragma unroll
+  for (uint32_t j = 1; j < 4u; ++j) {
+    const bool behind = j < mine && at >= (before + parts) * a.pairs;   // (stays false once it is)
+    before += behind ? parts : 0u;
+    split_before += behind && parts > 1u ? parts : 0u;
+    i = behind ? j : i;
+    n = behind ? len[j] : n;
+    parts = behind ? k[j] : parts;
   }
   const int owner = __ffsll((unsigned long long)here) - 1;
   auto of_owner = [&](uint32_t v) { return (uint32_t)__builtin_amdgcn_readlane((int)v, owner); };
   w->seq = of_owner(from + i);
   w->len = of_owner(n);
-  w->tiles = of_owner(t);
-  w->parts = of_owner(k);
+  w->tiles = tiles_of<TILE>(w->len);
+  w->parts = of_owner(parts);
   const uint32_t rel = at - of_owner(before) * a.pairs;
   w->pair = rel / w->parts;
   w->part = rel - w->pair * w->parts;
   w->piece0 = of_owner(split_before) * a.pairs + w->pair * w->parts;
+  return true;
+}
+
+// Of more than kPagedFind sequences one workgroup writes down the chunks, for every chunk (of all blocks of heads) what the above finds: sequence, length, its
+// first chunk's number, and its parts together with the pieces before them in 16 bits each (at most 2 kPagedChunks).  No parts:
+// behind the last chunk.
+constexpr uint32_t kListBlock = 1024;
+__global__ __launch_bounds__(kListBlock) void lt_paged_list_kernel(const PagedArgs a) {
+  __shared__ uint32_t sums[3][kListBlock / 64];
+  const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, each = (a.seqs + kListBlock - 1u) / kListBlock;
+  const uint32_t from = (uint32_t)min((uint64_t)threadIdx.x * each, (uint64_t)a.seqs), to = min(a.seqs, from + each), most = a.listed;
+  uint4* list = (uint4*)a.list;
+  auto tiles_at = [&](uint32_t s, uint32_t* len) {
+    *len = length_of(a, s);
+    return *len == 0u ? 1u : (*len - 1u) / a.tile + 1u;
+  };
+  // what the threads before this one have, and all of them together
+  auto before = [&](uint32_t v, uint32_t which, uint32_t* all) {
+    const uint32_t sum = sums_over_wave(v);
+    if (lane == 63u) sums[which][wave] = sum;
+    __syncthreads();
+    uint32_t b = 0;
+    *all = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < kListBlock / 64u; ++i) {
+      if (i < wave) b += sums[which][i];
+      *all += sums[which][i];
+    }
+    return b + sum - v;
+  };
+  uint32_t len, tiles = 0, all, chunks = 0, split = 0, total, ignored;
+#pragma unroll 4
+  for (uint32_t s = from; s < to; ++s) tiles += tiles_at(s, &len);
+  before(tiles, 0, &all);
+  const uint32_t c = max(a.least, (all * a.pairs + kPagedChunks - 1u) / kPagedChunks);
+#pragma unroll 4
+  for (uint32_t s = from; s < to; ++s) {
+    const uint32_t k = (tiles_at(s, &len) + c - 1u) / c;
+    chunks += k;
+    split += k > 1u ? k : 0u;
+  }
+  uint32_t at = before(chunks, 1, &total), pieces = before(split, 2, &ignored);
+#pragma unroll 4
+  for (uint32_t s = from; s < to; ++s) {
+    const uint32_t k = (tiles_at(s, &len) + c - 1u) / c;
+    for (uint32_t i = 0; i < k; ++i)
+      if (at + i < most) list[at + i] = make_uint4(s, len, at, k | pieces << 16);
+    at += k;
+    pieces += k > 1u ? k : 0u;
+  }
+  for (uint32_t i = total + threadIdx.x; i < most; i += kListBlock) list[i] = make_uint4(0u, 0u, 0u, 0u);
+}
+
+template <uint32_t TILE>
+__device__ __forceinline__ bool read_chunk(const PagedArgs& a, Chunk* w) {
+  const uint4 e = ((const uint4*)a.list)[blockIdx.x / a.pairs];
+  w->parts = e.w & 0xFFFFu;
+  if (w->parts == 0u) return false;
+  w->seq = e.x;
+  w->len = e.y;
+  w->tiles = tiles_of<TILE>(w->len);
+  const uint32_t rel = blockIdx.x - e.z * a.pairs;
+  w->pair = rel / w->parts;
+  w->part = rel - w->pair * w->parts;
+  w->piece0 = (e.w >> 16) * a.pairs + w->pair * w->parts;
   return true;
 }
 
@@ -434,7 +501,7 @@ __global__ __launch_bounds__(kBlock, DP <= 128 && NH == 1 && AL == 16 ? (DP == 6
   Chunk w;
   uint32_t t0, t1;
   if (a.split) {
-    if (!find_chunk<G::TILE>(a, &w)) return;
+    if (!(a.listed > 0u ? read_chunk<G::TILE>(a, &w) : find_chunk<G::TILE>(a, &w))) return;
     const uint32_t even = w.tiles / w.parts, odd = w.tiles - even * w.parts;
     t0 = w.part * even + min(w.part, odd);
     t1 = t0 + even + (w.part < odd ? 1u : 0u);
@@ -823,9 +890,14 @@ hipError_t launch_paged(const void* args, hipStream_t s) {
   if (a.seqs == 0) return hipSuccess;
   if (!a.q || !a.lengths || !a.out || (a.capacity > 0 && (!a.cache || !a.table)) || a.dim == 0 || a.dim > a.padded || a.kv_heads == 0 || a.heads % a.kv_heads != 0 ||
       a.rows.d == 0 || a.workgroups == 0 || (a.split && (!a.parts || !a.tickets || a.least == 0)) || a.tile != (a.dtype == kF32 ? 64u : 128u) ||
-      a.blocks_of > (a.padded == 256u ? 16u : 32u))
+      a.blocks_of > (a.padded == 256u ? 16u : 32u) ||
+      (a.split && a.seqs > kPagedFind && a.listed != (a.workgroups + a.pairs - 1u) / a.pairs))
     return hipErrorInvalidValue;
   const int64_t size = a.dtype == kF32 ? 4 : 2;
+  if (a.listed > 0u) {
+    a.list = a.parts + (uint64_t)a.pieces * a.part_floats();
+    LT_LAUNCH(lt_paged_list_kernel, dim3(1), dim3(kListBlock), s, a);
+  }
   a.q_whole = (uintptr_t)a.q % 16u == 0u && a.q_seq * size % 16 == 0 && a.q_head * size % 16 == 0 && a.dim * size % 16 == 0;
   return a.dtype == kF32 ? launch_paged_of<float>(a, s) : a.dtype == kBF16 ? launch_paged_of<__bf16>(a, s) : hipErrorInvalidValue;
 }

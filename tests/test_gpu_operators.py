@@ -288,6 +288,42 @@ def test_attention_of_lengths_far_apart(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_attention_of_very_many_sequences(dtype):
+    """the chunks of so many are written down first: short ones, long ones among them, and whole ones"""
+    rg = np.random.default_rng(22)
+    check_attention([9000] + [int(n) for n in rg.integers(-2, 40, 255)], 4, 2, 16, 32, dtype)             # the most that find them by themselves
+    check_attention([int(n) for n in rg.integers(-2, 40, 256)] + [9000], 4, 2, 16, 32, dtype)
+    check_attention([int(n) for n in rg.integers(0, 30, 1023)] + [3000, 700], 2, 1, 16, 20, dtype)
+    check_attention([3000] + [int(n) for n in rg.integers(0, 8, 2600)] + [0, 2900], 3, 3, 5, 8, dtype)
+    check_attention([600] * 700, 2, 2, 16, 16, dtype)
+
+
+@pytest.mark.parametrize("graphs", [False, True])
+def test_attention_of_very_many_sequences_replayed(graphs):
+    """lengths that change between the replays of a step"""
+    rg = np.random.default_rng(23)
+    ctx, E = context(), Eager("f64")
+    ctx.set_graphs(graphs)
+    most = [int(n) for n in rg.integers(1, 30, 400)] + [2500, 1300]
+    cache, table = paged_case(rg, most, 2, 16, 32, "bf16")
+    q = data(rg, (len(most), 4, 32), "bf16")
+    held = torch.from_numpy(ints(most)).to("cuda:0")
+    Q, C, L, T = ctx.tensor(q, "bf16"), ctx.tensor(cache, "bf16"), ctx.tensor(held), ctx.tensor(table)
+    o = ctx.paged_attention(Q, C, L, T)
+    ctx.barrier()
+    step = ctx.capture_step()
+    for i in range(6):
+        lens = ints(most) if i % 3 == 2 else ints([int(n) for n in rg.integers(0, np.array(most) + 1)])
+        held.copy_(torch.from_numpy(lens))
+        torch.cuda.synchronize()
+        step.replay()
+        with np.errstate(invalid="ignore"):
+            ref = E.fetch(E.paged_attention(E.tensor(q, "bf16"), E.tensor(cache, "bf16"), E.tensor(lens), E.tensor(table)))
+        compare_attention(ctx.fetch(o), ref, q, cache, lens, table, "bf16")
+    ctx.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_attention_with_missing_pages(dtype):
     def edit(table):
         table[0, 1], table[1, 0], table[2, :] = -1, 2 ** 31 - 1, -7
