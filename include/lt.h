@@ -108,7 +108,8 @@ typedef enum {
  * multiple of the key heads, and query head h reads key head h / (heads / key heads); dim is at most
  * 256.  The result, of q's type and shape, is softmax(scale * q K^T) V over the first lengths[s] positions
  * of the sequence.  Positions behind the table's slots and those in pages that are not the cache's do not count;
- * a sequence with nothing that counts (length 0 or negative) gets zeros.  Default scale: 1 / sqrt(dim).
+ * a sequence with nothing that counts (length 0 or negative) gets zeros.  Default scale: 1 / sqrt(dim); its magnitude is
+ * at most 1e38.
  *
  * LT_ERR_SHAPE where pages * rows, slots * rows, 2 * key heads * dim, sequences or tokens is 2^31 or more.
  */

@@ -740,7 +740,8 @@ static lt_status record_op(lt_ctx* ctx, uint16_t opcode, const lt_tensor* inputs
       if (a->dims[0] * a->dims[1] >= ((int64_t)1 << 31) || a->dims[1] >= ((int64_t)1 << 31)) return fail(ctx, LT_ERR_SHAPE, "paged_attention: sequences * heads must be below 2^31");
       const lt_attr* sc = find_attr(attrs, n_attr, LT_ATTR_SCALE);
       const double scale = sc ? (sc->is_float ? sc->v.f : (double)sc->v.i) : 1.0 / std::sqrt((double)a->dims[2]);
-      if (!std::isfinite(scale) || !std::isfinite((float)scale)) return fail(ctx, LT_ERR_ARG, "paged_attention: LT_ATTR_SCALE must be finite");
+      // (scores are formed for powers of two: scale * log2(e) has to be finite too)
+      if (!(std::fabs(scale) <= 1e38)) return fail(ctx, LT_ERR_ARG, "paged_attention: LT_ATTR_SCALE must be finite, and at most 1e38");
       push_attr(&n, LT_ATTR_SCALE, true, 0, scale);
       n.dtype = a->dtype;
       set_shape(a->dims, a->rank);
