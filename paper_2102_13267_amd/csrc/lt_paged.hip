@@ -20,7 +20,9 @@ constexpr float kLog2e = 1.44269504088896340736f;
 
 // ---- new rows ------------------------------------------------------------------------------------
 // Bound by memory for prompts, by latency for single tokens: a workgroup has all rows (keys and values, head by head) of a few tokens
-// on their way while it finds out where these go and computes their turns.
+// on their way while it finds out where these go and computes their turns.  8 prompts of up to 2048 tokens, 8 key heads of 128 bf16,
+// 49 MB: 11.6 us, 4.2 TB/s (one thread a pair, each with a search and a turn of its own, 42); 64 single tokens 4.3 us on the device, less
+// than a call costs the host.
 __global__ __launch_bounds__(kBlock) void lt_cache_copy_kernel(const AppendArgs a) {
   const uint64_t n = a.cache_elems * (a.cache_dtype == kF32 ? 4u : 2u), stride = (uint64_t)gridDim.x * kBlock * 16u;
   for (uint64_t i = ((uint64_t)blockIdx.x * kBlock + threadIdx.x) * 16u; i < n; i += stride) {
@@ -124,7 +126,7 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, Turn* turns) {
   }
 }
 
-// RIDE: the workgroups behind the first `append_grid` rotate (AppendArgs::rope).
+// RIDE: the workgroups behind the first `append_grid` rotate (AppendArgs::rope): a step for 32 sequences 27.6 us, in two launches 30.6.
 template <typename C, typename T, int V, bool IL, bool RIDE>
 __global__ __launch_bounds__(kBlock) void lt_cache_append_kernel(const AppendArgs a) {
   __shared__ Turn turns[kMaxTurns];
@@ -173,7 +175,7 @@ hipError_t launch_append_of(AppendArgs a, bool* rode, hipStream_t s) {
     const uint32_t lanes = kBlock / slots;
     auto tokens = [&](uint32_t each) { return (lanes * each + a.token_rows.d - 2u) / a.token_rows.d + 1u; };
     auto fits = [&](uint32_t each) { return tokens(each) * pairs <= kMaxTurns && tokens(each) <= kMaxTokens; };
-    while (a.rows_each > 1u && (rows / (lanes * a.rows_each) < 1024u || !fits(a.rows_each))) a.rows_each /= 2u;
+    while (a.rows_each > 1u && (rows / (lanes * a.rows_each) < kRowGrid || !fits(a.rows_each))) a.rows_each /= 2u;
     const uint64_t grid = (rows + lanes * a.rows_each - 1) / (lanes * a.rows_each);
     if (fits(a.rows_each) && grid < ((uint64_t)1 << 30)) {
       a.slots_each.set(slots);
@@ -250,11 +252,16 @@ hipError_t launch_append(const void* args, hipStream_t s) {
 // Four waves share a tile of 4 WK keys; their maxima, sums and products meet in LDS at the end.
 //
 // A workgroup has one chunk of a sequence, for one block of up to 16 NH query heads of a key head.  Chunks are of at most c tiles, c the
-// smallest that gives all sequences together about kPagedChunks of them, but at least a.least: a join costs what a few tiles do.
+// smallest that gives all sequences together about kPagedChunks of them, but at least a.least: a join costs what a few tiles do (bf16 at
+// least 2 / 4 / 8 tiles of 128, us: 300 keys 9.8 / 7.3 / 7.3, 32 sequences of up to 2048 28.8 / 27.5 / 32.0; fp32 2 / 4 tiles of 64, 7 sequences of up to 3001 12.9 / 15.1).
 // A sequence's chunks are of equal length, so that a long one among short ones holds nobody up.  Pieces of a block meet in memory
 // (relaxed accesses of device scope, as the reductions exchange theirs), and whoever comes last joins them in their order: up
 // to 32 at once, more in groups of about their root, whose last ones then join the groups.  So results do not depend on
 // who comes when.
+//
+// 32 query heads, 8 key heads of 128 bf16: one sequence of 131072 keys, 537 MB, 91 us, 5.9 TB/s; 60 sequences of 256 to 4096 74 us, 4.7 TB/s
+// (workgroups whose waves happen to run late hold up the end, 15 to 20 us of it); one of 300 7.3 us, of which the chain length, page, keys,
+// softmax, join takes most.  fp32, 7 sequences of up to 3001, 4 key heads of 80: 12.9 us.  One workgroup per sequence and query head: 63749, 2070, 70 and 805.
 template <typename T, int DP, int NH> struct Geo {
   static constexpr bool BF = sizeof(T) == 2;
   static constexpr int KT = BF ? 2 : 1;              // tiles of 16 keys in a wave's step
@@ -867,7 +874,8 @@ hipError_t launch_paged_as(const PagedArgs& a, hipStream_t s) {
   // rows of whole 16 bytes are read in such pieces, others in the largest that they are made of
   const uint32_t row = a.dim * (uint32_t)sizeof(T);
   const bool whole = row % 16u == 0u && (uintptr_t)a.cache % 16u == 0u;
-  // caches larger than the last-level cache are read past it (one block of query heads a key head: others read the same keys)
+  // caches larger than the last-level cache are read past it (one block of query heads a key head: others read the same keys): 537 MB 100.6 -> 91.1 us,
+  // 345 MB 75.2 -> 74.1; of 93 MB, which stay in it, the next read would take 27.5 -> 29.7
   const bool past = (uint64_t)a.pages * 2u * a.kv_heads * a.rows.d * row >= ((uint64_t)256 << 20) && a.pairs == a.kv_heads;
   if (whole && a.rows.d % 16u == 0u && past) LT_LAUNCH((lt_paged_attention_kernel<T, DP, NH, true, 16, true>), dim3(a.workgroups), dim3(kBlock), s, a);
   else if (whole && a.rows.d % 16u == 0u) LT_LAUNCH((lt_paged_attention_kernel<T, DP, NH, true, 16, false>), dim3(a.workgroups), dim3(kBlock), s, a);

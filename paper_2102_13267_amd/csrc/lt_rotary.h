@@ -16,6 +16,9 @@ namespace ltk {
 constexpr uint32_t kRowBlock = 256;       // threads of a workgroup
 constexpr uint32_t kMaxTurns = 4096;      // of its tokens' pairs: 32 KB of LDS
 constexpr int kMaxRows = 4;               // of a thread, all of them on their way at once
+// Workgroups that are worth more than further rows a thread: two a compute unit (at least 256 / 512 / 1024, us: 8 prompts of up to 2048 tokens appended
+// 11.6 / 11.6 / 12.8, of 512 each 10.3 / 10.2 / 9.8; fp32 rotation of 5331 x 12 x 80 18.6 / 18.6 / 19.4; of one row a thread always 14.0 and 20.0).
+constexpr uint32_t kRowGrid = 512;
 
 struct __attribute__((aligned(8))) Turn {
   float c, s;   // amplitude * cos, amplitude * sin
@@ -186,11 +189,11 @@ inline bool lay_out(RopeArgs* a, uint32_t size, RopeLayout* l) {
   if (v == 0 || slots > kRowBlock) return false;
   const uint64_t bytes = rows * a->dim * size, cache = (uint64_t)256 << 20;
   l->past = bytes >= cache ? kAllPast : 2 * bytes >= cache ? kReadsPast : kNothingPast;
-  // rows a thread: four where that leaves four workgroups a compute unit, and the tokens' turns fit
+  // rows a thread: four where that leaves kRowGrid workgroups, and the tokens' turns fit
   a->rows_each = l->past == kNothingPast ? kMaxRows : 2u;
   const uint32_t lanes = kRowBlock / slots;
   auto tokens = [&](uint32_t each) { return (lanes * each + a->heads.d - 2u) / a->heads.d + 1u; };
-  while (a->rows_each > 1u && (rows / (lanes * a->rows_each) < 1024u || tokens(a->rows_each) * pairs > kMaxTurns)) a->rows_each /= 2u;
+  while (a->rows_each > 1u && (rows / (lanes * a->rows_each) < kRowGrid || tokens(a->rows_each) * pairs > kMaxTurns)) a->rows_each /= 2u;
   const uint64_t grid = (rows + lanes * a->rows_each - 1) / (lanes * a->rows_each);
   if (tokens(a->rows_each) * pairs > kMaxTurns || grid >= ((uint64_t)1 << 31)) return false;
   a->slots.set(slots);
