@@ -576,6 +576,36 @@ def test_two_contexts_on_streams_of_their_own():
         c.close()
 
 
+@pytest.mark.parametrize("graphs", [False, True])
+def test_operators_spread_over_streams(graphs):
+    """several attentions and appends that do not depend on each other, whose pieces and tickets must not meet"""
+    rg = np.random.default_rng(24)
+    cases = []
+    for lens, rows, kv, heads in (([9000, 300, 0, 5000], 16, 2, 8), ([700] * 40, 16, 2, 8), ([3000, 2], 8, 1, 4), ([20] * 300 + [4000], 16, 1, 2)):
+        cache, table = paged_case(rg, lens, kv, rows, 64, "bf16", fill=0.0, spare=(1 << 23) // (kv * rows * 64))   # (as large as makes a launch worth a stream)
+        cases.append((cache, table, ints(lens), data(rg, (len(lens), heads, 64), "bf16"), data(rg, (len(lens), kv, 64), "bf16")))
+    runs = []
+    for streams in (1, 4):
+        ctx = context(workspace_bytes=512 << 20)
+        ctx.set_graphs(graphs)
+        ctx.set_streams(streams)
+        held = [[ctx.tensor(c, "bf16", donatable=True), ctx.tensor(t), ctx.tensor(n), ctx.tensor(q, "bf16"), ctx.tensor(k, "bf16")] for c, t, n, q, k in cases]
+        for _ in range(3):     # (a plan of 24 launches and more is spread)
+            outs = []
+            for C, T, N, Q, K in held:
+                ctx.assign(C, ctx.cache_append(C, K, K, N, T, rotary=Rotary()))
+                outs.append(ctx.paged_attention(Q, C, N, T))
+                outs += [ctx.paged_attention(ctx.rope(Q, N, Rotary(base=b)), C, N, T) for b in (10000.0, 100.0, 7.0)]
+            ctx.barrier()
+            assert (ctx.plan_streams() > 1) == (streams > 1)
+            runs.append([ctx.fetch(o) for o in outs])
+            del outs
+        ctx.close()
+    for r in runs[1:]:
+        for a, b in zip(r, runs[0]):
+            assert np.array_equal(a, b)
+
+
 def test_runs_of_the_same_step_are_the_same_bits():
     rg = np.random.default_rng(19)
     ctx = context()
