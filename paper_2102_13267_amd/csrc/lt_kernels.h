@@ -344,11 +344,17 @@ struct AppendArgs {
 };
 
 // out[s][h] = softmax(scale q K^T) V over sequence s's keys in the paged cache.  Work is counted in tiles of `tile` keys for
-// blocks of `blocks_of` query heads of one key head; `pairs` such blocks a sequence.  split: sequences are cut into chunks of c
-// tiles, c = max(least, all sequences' tiles / kPagedChunks), a workgroup each, and what several of them have of a block meets in `parts`, with a ticket a
-// piece (zero before and after a launch).  A sequence of t > c tiles has ceil(t / c) < 2 t / c chunks, so there are fewer than 2 kPagedChunks pieces.
+// blocks of `blocks_of` query heads of one key head; `pairs` such blocks a sequence.  split: sequences of more than `whole` tiles are cut into chunks of c
+// tiles, c = max(least, all sequences' tiles / chunks), a workgroup each, and what several of them have of a block meets in `parts`, with a ticket a
+// piece (zero before and after a launch).  A sequence of t > c tiles has ceil(t / c) < 2 t / c chunks, so there are fewer than 2 `chunks` pieces.
 // Otherwise a workgroup has a block of a sequence.
-// (512 / 768 / 1024: one sequence of 131072 keys 91 / 96 / 107 us)
+//
+// Fewer blocks than compute units: one chunk a compute unit, of two tiles at least, but up to five tiles of bf16 stay whole, which a join would take as long as
+// (chunks 256 / 512, us, 8 key heads of 128 bf16: one sequence of 131072 keys 86.2 / 91.1, of 20000 24.4 / 28.8, 4 of 5000 21.9 / 25.5; least two / four tiles:
+// one of 3000 11.3 / 13.4, of 1500 11.1 / 12.9; of 600, five tiles, 10.4 in three parts, 9.8 whole; fp32 7 of up to 3001 13.5 so, 12.9 cut).  Otherwise two chunks a compute unit, of four
+// tiles (fp32, tiles of 64 keys: two) at least, so that short ones fill up beside long ones (256 / 512: 60 sequences of 256 to 4096 84 / 74, 32 of up to 2048
+// with their append 29.6 / 27.6; least two / four: 28.9 / 27.6).  More chunks gain nothing (768: one of 131072 96, 60 of up to 4096 76.5).
+constexpr uint32_t kPagedFull = 256;            // blocks, a workgroup each, that leave no compute unit without one
 constexpr uint32_t kPagedChunks = 512;
 // Up to so many sequences a workgroup finds its chunk by itself; of more a list of them is written first (lengths of 100 to 1000, 2 key heads of
 // 128 bf16, by themselves / from a list, us: 128 sequences 22.7 / 25.2, 256 31.0 / 33.3, 1024 143 / 111, 16384 10870 / 1492).
@@ -367,7 +373,7 @@ struct PagedArgs {
   float* parts;
   uint32_t* tickets;
   uint32_t padded, blocks_of, pairs, tile;   // padded: the kernel instance's head size
-  uint32_t workgroups, split, least;
+  uint32_t workgroups, split, least, whole, chunks;
   uint32_t listed;              // entries of the list, one for each chunk there can be (0: none is written)
   void* list;                   // behind the pieces (the launcher sets it)
   uint32_t pieces, q_whole;     // pieces: that parts and tickets are for.  q_whole: rows of q are whole 16-byte pieces (the launcher sets it)
@@ -382,11 +388,14 @@ struct PagedArgs {
     pairs = kv_heads * ((group + blocks_of - 1u) / blocks_of);
     tile = dtype == kF32 ? 64u : 128u;
     const uint64_t most = capacity == 0 ? 1 : (capacity - 1u) / tile + 1u, all = (uint64_t)seqs * pairs;
-    least = dtype == kF32 ? 2u : 4u;
-    split = most > least ? 1u : 0u;
+    const bool few = all < kPagedFull;
+    chunks = few ? kPagedFull : kPagedChunks;
+    least = few || dtype == kF32 ? 2u : 4u;
+    whole = few && dtype != kF32 ? 5u : least;
+    split = most > whole ? 1u : 0u;
     const uint64_t each = (most + least - 1u) / least;   // chunks of a sequence at most
-    workgroups = (uint32_t)(split && each > 1u ? (all + kPagedChunks < all * each ? all + kPagedChunks : all * each) : all);
-    pieces = (uint32_t)(split ? (2u * kPagedChunks < all * each ? 2u * kPagedChunks : all * each) : 0u);
+    workgroups = (uint32_t)(split ? (all + chunks < all * each ? all + chunks : all * each) : all);
+    pieces = (uint32_t)(split ? (2u * chunks < all * each ? 2u * chunks : all * each) : 0u);
     listed = split && seqs > kPagedFind ? (workgroups + pairs - 1u) / pairs : 0u;
   }
   uint64_t parts_bytes() const { return (uint64_t)pieces * part_floats() * sizeof(float) + 16u * (uint64_t)listed; }

@@ -251,15 +251,13 @@ hipError_t launch_append(const void* args, hipStream_t s) {
 //
 // Four waves share a tile of 4 WK keys; their maxima, sums and products meet in LDS at the end.
 //
-// A workgroup has one chunk of a sequence, for one block of up to 16 NH query heads of a key head.  Chunks are of at most c tiles, c the
-// smallest that gives all sequences together about kPagedChunks of them, but at least a.least: a join costs what a few tiles do (bf16 at
-// least 2 / 4 / 8 tiles of 128, us: 300 keys 9.8 / 7.3 / 7.3, 32 sequences of up to 2048 28.8 / 27.5 / 32.0; fp32 2 / 4 tiles of 64, 7 sequences of up to 3001 12.9 / 15.1).
+// A workgroup has one chunk of a sequence, for one block of up to 16 NH query heads of a key head (PagedArgs has how long chunks are).
 // A sequence's chunks are of equal length, so that a long one among short ones holds nobody up.  Pieces of a block meet in memory
 // (relaxed accesses of device scope, as the reductions exchange theirs), and whoever comes last joins them in their order: up
 // to 32 at once, more in groups of about their root, whose last ones then join the groups.  So results do not depend on
 // who comes when.
 //
-// 32 query heads, 8 key heads of 128 bf16: one sequence of 131072 keys, 537 MB, 91 us, 5.9 TB/s; 60 sequences of 256 to 4096 74 us, 4.7 TB/s
+// 32 query heads, 8 key heads of 128 bf16: one sequence of 131072 keys, 537 MB, 86 us, 6.2 TB/s; 60 sequences of 256 to 4096 74 us, 4.7 TB/s
 // (workgroups whose waves happen to run late hold up the end, 15 to 20 us of it); one of 300 7.3 us, of which the chain length, page, keys,
 // softmax, join takes most.  fp32, 7 sequences of up to 3001, 4 key heads of 80: 12.9 us.  One workgroup per sequence and query head: 63749, 2070, 70 and 805.
 template <typename T, int DP, int NH> struct Geo {
@@ -357,6 +355,9 @@ __device__ __forceinline__ uint32_t sums_over_wave(uint32_t v) {
   return v;
 }
 
+__device__ __forceinline__ uint32_t chunk_of(const PagedArgs& a, uint32_t all) { return max(a.least, (all * a.pairs + a.chunks - 1u) / a.chunks); }
+__device__ __forceinline__ uint32_t chunks_of(const PagedArgs& a, uint32_t tiles, uint32_t c) { return tiles <= a.whole ? 1u : (tiles + c - 1u) / c; }
+
 // A workgroup's share.
 struct Chunk {
   uint32_t seq, len, tiles;      // tiles: of the whole sequence
@@ -376,12 +377,11 @@ __device__ __forceinline__ bool find_chunk(const PagedArgs& a, Chunk* w) {
   const uint32_t mine = from < a.seqs ? min(each, a.seqs - from) : 0u;
 #pragma unroll
   for (uint32_t i = 0; i < 4u; ++i) tiles += i < mine ? tiles_of<TILE>(len[i]) : 0u;
-  const uint32_t all = (uint32_t)__builtin_amdgcn_readlane((int)sums_over_wave(tiles), 63) * a.pairs;
-  const uint32_t c = max(a.least, (all + kPagedChunks - 1u) / kPagedChunks);
+  const uint32_t c = chunk_of(a, (uint32_t)__builtin_amdgcn_readlane((int)sums_over_wave(tiles), 63));
   uint32_t k[4], chunks = 0, split = 0;
 #pragma unroll
   for (uint32_t i = 0; i < 4u; ++i) {
-    k[i] = i < mine ? (tiles_of<TILE>(len[i]) + c - 1u) / c : 0u;
+    k[i] = i < mine ? chunks_of(a, tiles_of<TILE>(len[i]), c) : 0u;
     chunks += k[i];
     split += k[i] > 1u ? k[i] : 0u;
   }
@@ -443,17 +443,17 @@ __global__ __launch_bounds__(kListBlock) void lt_paged_list_kernel(const PagedAr
 #pragma unroll 4
   for (uint32_t s = from; s < to; ++s) tiles += tiles_at(s, &len);
   before(tiles, 0, &all);
-  const uint32_t c = max(a.least, (all * a.pairs + kPagedChunks - 1u) / kPagedChunks);
+  const uint32_t c = chunk_of(a, all);
 #pragma unroll 4
   for (uint32_t s = from; s < to; ++s) {
-    const uint32_t k = (tiles_at(s, &len) + c - 1u) / c;
+    const uint32_t k = chunks_of(a, tiles_at(s, &len), c);
     chunks += k;
     split += k > 1u ? k : 0u;
   }
   uint32_t at = before(chunks, 1, &total), pieces = before(split, 2, &ignored);
 #pragma unroll 4
   for (uint32_t s = from; s < to; ++s) {
-    const uint32_t k = (tiles_at(s, &len) + c - 1u) / c;
+    const uint32_t k = chunks_of(a, tiles_at(s, &len), c);
     for (uint32_t i = 0; i < k; ++i)
       if (at + i < most) list[at + i] = make_uint4(s, len, at, k | pieces << 16);
     at += k;
@@ -858,7 +858,8 @@ __global__ __launch_bounds__(kBlock, DP <= 128 && NH == 1 && AL == 16 ? (DP == 6
       else publish4(piece(first) + hh * DP + d, make_float4(o[0], o[1], o[2], o[3]));
     }
   };
-  // (24 pieces at once and in two steps: 7 sequences of up to 3001 keys 12.9 / 15.1 us; 64: one of 131072 95.4 / 91.4)
+  // (24 pieces at once and in two steps: 7 sequences of up to 3001 keys 12.9 / 15.1 us; 64, where one of 131072 has 64 chunks a
+  // key head: 95.4 / 91.4)
   uint32_t each = w.parts;
   if (w.parts > kMostPieces)
     for (each = 3u; each * each < w.parts;) ++each;
@@ -897,7 +898,7 @@ hipError_t launch_paged(const void* args, hipStream_t s) {
   PagedArgs a = *(const PagedArgs*)args;
   if (a.seqs == 0) return hipSuccess;
   if (!a.q || !a.lengths || !a.out || (a.capacity > 0 && (!a.cache || !a.table)) || a.dim == 0 || a.dim > a.padded || a.kv_heads == 0 || a.heads % a.kv_heads != 0 ||
-      a.rows.d == 0 || a.workgroups == 0 || (a.split && (!a.parts || !a.tickets || a.least == 0)) || a.tile != (a.dtype == kF32 ? 64u : 128u) ||
+      a.rows.d == 0 || a.workgroups == 0 || (a.split && (!a.parts || !a.tickets || a.least == 0 || a.chunks == 0 || a.chunks > kPagedChunks)) || a.tile != (a.dtype == kF32 ? 64u : 128u) ||
       a.blocks_of > (a.padded == 256u ? 16u : 32u) ||
       (a.split && a.seqs > kPagedFind && a.listed != (a.workgroups + a.pairs - 1u) / a.pairs))
     return hipErrorInvalidValue;

@@ -115,15 +115,15 @@ static void shares(std::mt19937& rng) {
     t = n == 0 ? 1 : (n - 1) / a.tile + 1;
     all += t;
   }
-  const uint64_t c = std::max<uint64_t>(a.least, (all * a.pairs + ltk::kPagedChunks - 1) / ltk::kPagedChunks);
+  const uint64_t c = std::max<uint64_t>(a.least, (all * a.pairs + a.chunks - 1) / a.chunks);
   uint64_t chunks = 0, pieces = 0;
   for (uint64_t t : tiles) {
-    const uint64_t k = (t + c - 1) / c;
+    const uint64_t k = t <= a.whole ? 1 : (t + c - 1) / c;
     chunks += k;
     if (k > 1) pieces += k;
     CHECK(k < 65536);
   }
-  CHECK(chunks * a.pairs <= a.workgroups && pieces * a.pairs <= a.pieces && a.pieces <= 2 * ltk::kPagedChunks);
+  CHECK(chunks * a.pairs <= a.workgroups && pieces * a.pairs <= a.pieces && a.pieces <= 2 * a.chunks && a.chunks <= ltk::kPagedChunks);
   CHECK((a.listed != 0) == (a.seqs > ltk::kPagedFind) && (a.listed == 0 || ((uint64_t)a.listed * a.pairs >= a.workgroups && chunks <= a.listed)));
   CHECK(a.parts_bytes() % 16 == 0 && a.parts_bytes() >= 4 * a.pieces * a.part_floats());
 }
