@@ -382,9 +382,10 @@ struct PagedArgs {
   // The instance, and how the work is shared out; `capacity` and what comes before it are set.  Tiles of all sequences must be below 2^32.
   void share_out() {
     const uint32_t group = heads / kv_heads;
-    // (heads of 80 in the instance of 96 12.9 us, of 128 14.6)
-    padded = dim <= 64u ? 64u : dim <= 96u ? 96u : dim <= 128u ? 128u : 256u;
-    blocks_of = group <= 16u || padded == 256u ? 16u : 32u;
+    // (heads of 80 in the instance of 96 12.9 us, of 128 14.6; 148 short sequences with 8 key heads of 160 in that of 160 14.9, of 256 29.2; 75 with 4 of 20
+    // and their append in that of 32 16.4, of 64 18.3)
+    padded = dim <= 32u ? 32u : dim <= 64u ? 64u : dim <= 96u ? 96u : dim <= 128u ? 128u : dim <= 160u ? 160u : 256u;
+    blocks_of = group <= 16u || padded > 128u ? 16u : 32u;
     pairs = kv_heads * ((group + blocks_of - 1u) / blocks_of);
     tile = dtype == kF32 ? 64u : 128u;
     const uint64_t most = capacity == 0 ? 1 : (capacity - 1u) / tile + 1u, all = (uint64_t)seqs * pairs;

@@ -164,6 +164,17 @@ __global__ __launch_bounds__(kBlock) void lt_cache_append_any_kernel(const Appen
   }
 }
 
+template <typename C, typename T, int V, bool IL>
+void launch_append_rows(const AppendArgs& a, bool ride, uint32_t workgroups, hipStream_t s) {
+  if constexpr (sizeof(C) == sizeof(T)) {
+    if (ride) {
+      LT_LAUNCH((lt_cache_append_kernel<C, T, V, IL, true>), dim3(workgroups), dim3(kBlock), s, a);
+      return;
+    }
+  }
+  LT_LAUNCH((lt_cache_append_kernel<C, T, V, IL, false>), dim3(workgroups), dim3(kBlock), s, a);
+}
+
 template <typename C, typename T>
 hipError_t launch_append_of(AppendArgs a, bool* rode, hipStream_t s) {
   constexpr uint32_t kMost = 16u / (sizeof(C) > sizeof(T) ? sizeof(C) : sizeof(T));
@@ -181,27 +192,21 @@ hipError_t launch_append_of(AppendArgs a, bool* rode, hipStream_t s) {
       a.slots_each.set(slots);
       a.pairs.set(pairs ? pairs : 1u);
       a.append_grid = (uint32_t)grid;
-      const dim3 g((uint32_t)grid), b(kBlock);
-      if constexpr (sizeof(C) == sizeof(T)) {
-        // a rotation of the same type and layout, in pieces of 16 bytes too, takes the launch's other workgroups
-        RopeLayout l;
-        if (a.rope.out && v == kMost && a.rope.dtype == a.dtype && a.rope.rotary.interleaved == a.rotary.interleaved && fit_to_run(a.rope) &&
-            lay_out(&a.rope, sizeof(T), &l) && l.v == kMost && l.past == kNothingPast && l.grid < (1u << 30)) {
-          *rode = true;
-          if (a.rotary.interleaved) LT_LAUNCH((lt_cache_append_kernel<C, T, kMost, true, true>), dim3(a.append_grid + l.grid), b, s, a);
-          else LT_LAUNCH((lt_cache_append_kernel<C, T, kMost, false, true>), dim3(a.append_grid + l.grid), b, s, a);
-          return hipGetLastError();
-        }
-      }
+      // a rotation of the same type and layout, in pieces of the same size, takes the launch's other workgroups
+      RopeLayout l{};
+      if constexpr (sizeof(C) == sizeof(T))
+        *rode = a.rope.out && a.rope.dtype == a.dtype && a.rope.rotary.interleaved == a.rotary.interleaved && fit_to_run(a.rope) &&
+                lay_out(&a.rope, sizeof(T), &l) && l.v == v && l.past == kNothingPast && l.grid < (1u << 30);
+      const uint32_t workgroups = a.append_grid + (*rode ? l.grid : 0u);
       if (a.rotary.interleaved) {
-        if (v == kMost) LT_LAUNCH((lt_cache_append_kernel<C, T, kMost, true, false>), g, b, s, a);
-        else if (v == 4u) LT_LAUNCH((lt_cache_append_kernel<C, T, 4, true, false>), g, b, s, a);
-        else LT_LAUNCH((lt_cache_append_kernel<C, T, 2, true, false>), g, b, s, a);
+        if (v == kMost) launch_append_rows<C, T, kMost, true>(a, *rode, workgroups, s);
+        else if (v == 4u) launch_append_rows<C, T, 4, true>(a, *rode, workgroups, s);
+        else launch_append_rows<C, T, 2, true>(a, *rode, workgroups, s);
       } else {
-        if (v == kMost) LT_LAUNCH((lt_cache_append_kernel<C, T, kMost, false, false>), g, b, s, a);
-        else if (v == 4u) LT_LAUNCH((lt_cache_append_kernel<C, T, 4, false, false>), g, b, s, a);
-        else if (v == 2u) LT_LAUNCH((lt_cache_append_kernel<C, T, 2, false, false>), g, b, s, a);
-        else LT_LAUNCH((lt_cache_append_kernel<C, T, 1, false, false>), g, b, s, a);
+        if (v == kMost) launch_append_rows<C, T, kMost, false>(a, *rode, workgroups, s);
+        else if (v == 4u) launch_append_rows<C, T, 4, false>(a, *rode, workgroups, s);
+        else if (v == 2u) launch_append_rows<C, T, 2, false>(a, *rode, workgroups, s);
+        else launch_append_rows<C, T, 1, false>(a, *rode, workgroups, s);
       }
       return hipGetLastError();
     }
@@ -267,8 +272,8 @@ template <typename T, int DP, int NH> struct Geo {
   static constexpr int CE = 16 / (int)sizeof(T);     // elements of 16 bytes
   static constexpr int NC = DP / (4 * CE);           // 16-byte pieces of a key's row per lane
   static constexpr int NV = DP / 16;                 // elements of a value's row per lane
-  // bytes of a piece of it (96: of two elements, so that none ends behind a head of an even number of them), their number, and dwords of one
-  static constexpr int VB = NV * (int)sizeof(T) % 16 == 0 ? 16 : DP == 96 ? 2 * (int)sizeof(T) : 8;
+  // bytes of a piece of it (96 and 160: of two elements, so that none ends behind a head of an even number of them), their number, and dwords of one
+  static constexpr int VB = DP == 32 || DP == 96 || DP == 160 ? 2 * (int)sizeof(T) : NV * (int)sizeof(T) % 16 == 0 ? 16 : 8;
   static constexpr int NP = NV * (int)sizeof(T) / VB, DW = VB / 4;
   static constexpr int PITCH = DP + 4;
 };
@@ -293,17 +298,41 @@ template <int BYTES, bool PAST = false> __device__ __forceinline__ U4 load_bytes
   return r;
 }
 
-// BYTES of a row from element d on, in pieces of AL bytes; what is behind the row's end is read from its beginning.
-template <typename T, int BYTES, int AL>
+typedef U4 U4Any __attribute__((aligned(2)));   // wherever elements are
+typedef U2 U2Any __attribute__((aligned(2)));
+typedef uint32_t U1Any __attribute__((aligned(2)));
+
+// BYTES of a row from element d on.  AL 16: a row is made of such pieces; what is behind its end is read from its beginning.  kWide: a row of 16 bytes and
+// more that starts anywhere and ends inside a piece; KEY: read across the row's end, as values lie behind every key (otherwise from further
+// back, so that the last row's end is the last that is read, and moved down).  Elements behind dim are anything.  2 or 4: row by element.
+constexpr int kWide = 0;
+template <typename T, int BYTES, int AL, bool KEY>
 __device__ __forceinline__ U4 load_piece(const T* row, uint32_t d, uint32_t dim) {
   if constexpr (AL >= BYTES) return load_bytes<BYTES>(row + (d < dim ? d : 0u));
   U4 r = {0u, 0u, 0u, 0u};
+  if constexpr (AL == kWide && KEY) r = *(const U4Any*)(row + (d < dim ? d : 0u));
+  else if constexpr (AL == kWide && BYTES == 4) {
+    constexpr uint32_t kEach = 4 / sizeof(T);
+    const uint32_t at = min(d, dim - kEach), back = (d - at) * 8u * (uint32_t)sizeof(T);
+    r.x = *(const U1Any*)(row + at) >> (back & 31u);
+  } else if constexpr (AL == kWide) {
+    constexpr uint32_t kEach = 8 / sizeof(T);
 #pragma unroll
-  for (int i = 0; i < BYTES / AL; ++i) {
-    const uint32_t e = d + (uint32_t)(i * AL / (int)sizeof(T));
-    const T* p = row + (e < dim ? e : 0u);
-    if constexpr (AL == 4) r[i] = *(const uint32_t*)p;
-    else r[i / 2] |= (uint32_t)*(const uint16_t*)p << (16 * (i & 1));
+    for (uint32_t i = 0; i < BYTES / 8u; ++i) {
+      const uint32_t e = d + i * kEach, at = min(e, dim - kEach), back = (e - at) * 8u * (uint32_t)sizeof(T);
+      const U2 t = *(const U2Any*)(row + at);
+      const uint64_t v = ((uint64_t)t.y << 32 | t.x) >> (back & 63u);
+      r[2 * i] = (uint32_t)v;
+      r[2 * i + 1] = (uint32_t)(v >> 32);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < BYTES / AL; ++i) {
+      const uint32_t e = d + (uint32_t)(i * AL / (int)sizeof(T));
+      const T* p = row + (e < dim ? e : 0u);
+      if constexpr (AL == 4) r[i] = *(const uint32_t*)p;
+      else r[i / 2] |= (uint32_t)*(const uint16_t*)p << (16 * (i & 1));
+    }
   }
   return r;
 }
@@ -495,7 +524,7 @@ __device__ __forceinline__ bool last_of(uint32_t* ticket, uint32_t count, uint32
 }
 
 template <typename T, int DP, int NH, bool PG, int AL, bool PAST>
-__global__ __launch_bounds__(kBlock, DP <= 128 && NH == 1 && AL == 16 ? (DP == 64 ? 4 : 3) : 1) void lt_paged_attention_kernel(const PagedArgs a) {
+__global__ __launch_bounds__(kBlock, NH == 1 && (AL == 16 || AL == kWide) ? (DP <= 64 ? 4 : DP <= 128 ? 3 : DP == 160 ? 2 : 1) : 1) void lt_paged_attention_kernel(const PagedArgs a) {
   using G = Geo<T, DP, NH>;
   constexpr int KT = G::KT, NC = G::NC, NV = G::NV, NP = G::NP;
   constexpr uint32_t kSize = sizeof(T);
@@ -543,8 +572,8 @@ __global__ __launch_bounds__(kBlock, DP <= 128 && NH == 1 && AL == 16 ? (DP == 6
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
       const uint32_t d = (4u * c + g) * G::CE;
-      if (a.q_whole) q[b][c] = cut<T, 16>(load_piece<T, 16, 16>(row, d, to), d, to);
-      else q[b][c] = cut<T, (int)sizeof(T)>(load_piece<T, 16, (int)sizeof(T)>(row, d, to), d, to);
+      if (a.q_whole) q[b][c] = cut<T, 16>(load_piece<T, 16, 16, true>(row, d, to), d, to);
+      else q[b][c] = cut<T, (int)sizeof(T)>(load_piece<T, 16, (int)sizeof(T), true>(row, d, to), d, to);
     }
   }
 
@@ -614,7 +643,7 @@ __global__ __launch_bounds__(kBlock, DP <= 128 && NH == 1 && AL == 16 ? (DP == 6
           bool ok;
           const T* row = (const T*)a.cache + find_row(key0 + 16u * t + n, &ok);
 #pragma unroll
-          for (int c = 0; c < NC; ++c) k[t][c] = load_piece<T, 16, AL>(row, (4u * c + g) * G::CE, a.dim);
+          for (int c = 0; c < NC; ++c) k[t][c] = load_piece<T, 16, AL, true>(row, (4u * c + g) * G::CE, a.dim);
         }
       }
     };
@@ -640,7 +669,7 @@ __global__ __launch_bounds__(kBlock, DP <= 128 && NH == 1 && AL == 16 ? (DP == 6
         } else {
           const T* row = (const T*)a.cache + value + find_row(key0 + 16u * t + r, &ok);
 #pragma unroll
-          for (int p = 0; p < NP; ++p) v[i][p] = load_piece<T, G::VB, AL>(row, n * NV + p * (G::VB / kSize), a.dim);   // (what is behind the end is not stored)
+          for (int p = 0; p < NP; ++p) v[i][p] = load_piece<T, G::VB, AL, false>(row, n * NV + p * (G::VB / kSize), a.dim);   // (what is behind the end is not stored)
         }
         mine |= ok ? 1u << i : 0u;
       }
@@ -848,10 +877,11 @@ __global__ __launch_bounds__(kBlock, DP <= 128 && NH == 1 && AL == 16 ? (DP == 6
           }
       }
       if (ways > 1u) {   // (once round: units <= kBlock)
-        *(F4*)&meet[0][threadIdx.x * 4u] = o;
+        float* shared = &meet[0][0];   // (all four waves' of it)
+        *(F4*)(shared + threadIdx.x * 4u) = o;
         __syncthreads();
         if (way != 0u) continue;
-        for (uint32_t x = 1; mine && x < ways; ++x) o += *(const F4*)&meet[0][(x * units + u) * 4u];
+        for (uint32_t x = 1; mine && x < ways; ++x) o += *(const F4*)(shared + (x * units + u) * 4u);
       }
       if (!mine) continue;
       if (out) put(hh, d, o, total_of[hh]);
@@ -872,7 +902,6 @@ __global__ __launch_bounds__(kBlock, DP <= 128 && NH == 1 && AL == 16 ? (DP == 6
 
 template <typename T, int DP, int NH>
 hipError_t launch_paged_as(const PagedArgs& a, hipStream_t s) {
-  // rows of whole 16 bytes are read in such pieces, others in the largest that they are made of
   const uint32_t row = a.dim * (uint32_t)sizeof(T);
   const bool whole = row % 16u == 0u && (uintptr_t)a.cache % 16u == 0u;
   // caches larger than the last-level cache are read past it (one block of query heads a key head: others read the same keys): 537 MB 100.6 -> 91.1 us,
@@ -881,16 +910,18 @@ hipError_t launch_paged_as(const PagedArgs& a, hipStream_t s) {
   if (whole && a.rows.d % 16u == 0u && past) LT_LAUNCH((lt_paged_attention_kernel<T, DP, NH, true, 16, true>), dim3(a.workgroups), dim3(kBlock), s, a);
   else if (whole && a.rows.d % 16u == 0u) LT_LAUNCH((lt_paged_attention_kernel<T, DP, NH, true, 16, false>), dim3(a.workgroups), dim3(kBlock), s, a);
   else if (whole) LT_LAUNCH((lt_paged_attention_kernel<T, DP, NH, false, 16, false>), dim3(a.workgroups), dim3(kBlock), s, a);
-  else if (row % 4u == 0u) LT_LAUNCH((lt_paged_attention_kernel<T, DP, NH, false, 4, false>), dim3(a.workgroups), dim3(kBlock), s, a);
-  else if constexpr (sizeof(T) == 2) LT_LAUNCH((lt_paged_attention_kernel<T, DP, NH, false, 2, false>), dim3(a.workgroups), dim3(kBlock), s, a);
+  else if (row >= 16u) LT_LAUNCH((lt_paged_attention_kernel<T, DP, NH, false, kWide, false>), dim3(a.workgroups), dim3(kBlock), s, a);
+  else if constexpr (DP == 32) LT_LAUNCH((lt_paged_attention_kernel<T, DP, NH, false, (int)sizeof(T), false>), dim3(a.workgroups), dim3(kBlock), s, a);
   return hipGetLastError();
 }
 
 template <typename T>
 hipError_t launch_paged_of(const PagedArgs& a, hipStream_t s) {
+  if (a.padded == 32u) return a.blocks_of == 16u ? launch_paged_as<T, 32, 1>(a, s) : launch_paged_as<T, 32, 2>(a, s);
   if (a.padded == 64u) return a.blocks_of == 16u ? launch_paged_as<T, 64, 1>(a, s) : launch_paged_as<T, 64, 2>(a, s);
   if (a.padded == 96u) return a.blocks_of == 16u ? launch_paged_as<T, 96, 1>(a, s) : launch_paged_as<T, 96, 2>(a, s);
   if (a.padded == 128u) return a.blocks_of == 16u ? launch_paged_as<T, 128, 1>(a, s) : launch_paged_as<T, 128, 2>(a, s);
+  if (a.padded == 160u) return launch_paged_as<T, 160, 1>(a, s);
   return launch_paged_as<T, 256, 1>(a, s);
 }
 
@@ -899,7 +930,7 @@ hipError_t launch_paged(const void* args, hipStream_t s) {
   if (a.seqs == 0) return hipSuccess;
   if (!a.q || !a.lengths || !a.out || (a.capacity > 0 && (!a.cache || !a.table)) || a.dim == 0 || a.dim > a.padded || a.kv_heads == 0 || a.heads % a.kv_heads != 0 ||
       a.rows.d == 0 || a.workgroups == 0 || (a.split && (!a.parts || !a.tickets || a.least == 0 || a.chunks == 0 || a.chunks > kPagedChunks)) || a.tile != (a.dtype == kF32 ? 64u : 128u) ||
-      a.blocks_of > (a.padded == 256u ? 16u : 32u) ||
+      a.blocks_of > (a.padded > 128u ? 16u : 32u) ||
       (a.split && a.seqs > kPagedFind && a.listed != (a.workgroups + a.pairs - 1u) / a.pairs))
     return hipErrorInvalidValue;
   const int64_t size = a.dtype == kF32 ? 4 : 2;

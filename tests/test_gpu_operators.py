@@ -273,6 +273,21 @@ def test_attention(heads, kv, rows, dim, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", [16, 3])
+@pytest.mark.parametrize("dim", [2, 3, 4, 5, 8, 9, 17, 32, 34, 35, 63, 65, 96, 97, 101, 128, 130, 131, 152, 160, 161, 200, 251, 255])
+def test_attention_of_any_head(dim, rows, dtype):
+    """heads that end anywhere inside the pieces they are read in, the cache's last row among them"""
+    check_attention([40, 1, 0, 130, 33], 4, 2, rows, dim, dtype)
+    rg = np.random.default_rng(25)
+    ctx, E = context(), Eager("f64")
+    cache, q = data(rg, (2, 2, 1, rows, dim), dtype), data(rg, (1, 20, dim), dtype)
+    lens, table = ints([2 * rows]), ints([[0, 1]])                          # (every row of the cache is one of the sequence's)
+    args = lambda B: [B.tensor(q, dtype), B.tensor(cache, dtype), B.tensor(lens), B.tensor(table)]     # noqa: E731
+    compare_attention(ctx.fetch(ctx.paged_attention(*args(ctx))), E.fetch(E.paged_attention(*args(E))), q, cache, lens, table, dtype)
+    ctx.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_attention_of_one_long_sequence(dtype):
     for n, heads, kv, rows, dim in ((20000, 8, 1, 64, 128), (9001, 4, 4, 16, 64), (5003, 12, 2, 24, 80), (3333, 2, 1, 7, 256), (6007, 40, 1, 16, 128)):
         check_attention([n], heads, kv, rows, dim, dtype, seed=n)
