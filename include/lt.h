@@ -111,7 +111,8 @@ typedef enum {
  * a sequence with nothing that counts (length 0 or negative) gets zeros.  Default scale: 1 / sqrt(dim); its magnitude is
  * at most 1e38.
  *
- * LT_ERR_SHAPE where pages * rows, slots * rows, 2 * key heads * dim, sequences or tokens is 2^31 or more.
+ * LT_ERR_SHAPE where pages * rows, slots * rows, 2 * key heads * dim, sequences or tokens is 2^31 or more.  An attention of 2^24 sequences times
+ * key heads or more (less 512), or of 2^31 tiles of 64 keys (bf16: 128) that these could hold, has no lowering (LT_ERR_UNSUPPORTED at the barrier).
  */
 
 typedef enum {

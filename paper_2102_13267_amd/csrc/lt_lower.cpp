@@ -1946,7 +1946,8 @@ struct Lowering {
     args.q_seq = q.s_inner;
     args.q_head = q.s_head;
     args.share_out();
-    if ((double)args.seqs * args.pairs * (args.capacity / args.tile + 1u) >= 2147483648.0) return bad(LT_ERR_UNSUPPORTED, "paged_attention: sequences * slots * key heads too large");
+    // (a launch holds less than 2^32 threads)
+    if ((double)args.seqs * args.pairs * (args.capacity / args.tile + 1u) >= 2147483648.0 || args.workgroups >= 1u << 24) return bad(LT_ERR_UNSUPPORTED, "paged_attention: sequences * slots * key heads too large");
     Launch l = make_launch(L_PAGED, k, args);
     // (how long the sequences are is known on the device alone: as if every page were read once)
     const uint64_t held = (uint64_t)count(cs), w = dtype_size(an->dtype);

@@ -188,7 +188,7 @@ hipError_t launch_append_of(AppendArgs a, bool* rode, hipStream_t s) {
     auto fits = [&](uint32_t each) { return tokens(each) * pairs <= kMaxTurns && tokens(each) <= kMaxTokens; };
     while (a.rows_each > 1u && (rows / (lanes * a.rows_each) < kRowGrid || !fits(a.rows_each))) a.rows_each /= 2u;
     const uint64_t grid = (rows + lanes * a.rows_each - 1) / (lanes * a.rows_each);
-    if (fits(a.rows_each) && grid < ((uint64_t)1 << 30)) {
+    if (fits(a.rows_each) && grid < kMostGrid) {
       a.slots_each.set(slots);
       a.pairs.set(pairs ? pairs : 1u);
       a.append_grid = (uint32_t)grid;
@@ -196,7 +196,7 @@ hipError_t launch_append_of(AppendArgs a, bool* rode, hipStream_t s) {
       RopeLayout l{};
       if constexpr (sizeof(C) == sizeof(T))
         *rode = a.rope.out && a.rope.dtype == a.dtype && a.rope.rotary.interleaved == a.rotary.interleaved && fit_to_run(a.rope) &&
-                lay_out(&a.rope, sizeof(T), &l) && l.v == v && l.past == kNothingPast && l.grid < (1u << 30);
+                lay_out(&a.rope, sizeof(T), &l) && l.v == v && l.past == kNothingPast && grid + l.grid < kMostGrid;
       const uint32_t workgroups = a.append_grid + (*rode ? l.grid : 0u);
       if (a.rotary.interleaved) {
         if (v == kMost) launch_append_rows<C, T, kMost, true>(a, *rode, workgroups, s);

@@ -19,6 +19,7 @@ constexpr int kMaxRows = 4;               // of a thread, all of them on their w
 // Workgroups that are worth more than further rows a thread: two a compute unit (at least 256 / 512 / 1024, us: 8 prompts of up to 2048 tokens appended
 // 11.6 / 11.6 / 12.8, of 512 each 10.3 / 10.2 / 9.8; fp32 rotation of 5331 x 12 x 80 18.6 / 18.6 / 19.4; of one row a thread always 14.0 and 20.0).
 constexpr uint32_t kRowGrid = 512;
+constexpr uint64_t kMostGrid = (uint64_t)1 << 24;   // workgroups are below that: a launch holds less than 2^32 threads
 
 struct __attribute__((aligned(8))) Turn {
   float c, s;   // amplitude * cos, amplitude * sin
@@ -195,7 +196,7 @@ inline bool lay_out(RopeArgs* a, uint32_t size, RopeLayout* l) {
   auto tokens = [&](uint32_t each) { return (lanes * each + a->heads.d - 2u) / a->heads.d + 1u; };
   while (a->rows_each > 1u && (rows / (lanes * a->rows_each) < kRowGrid || tokens(a->rows_each) * pairs > kMaxTurns)) a->rows_each /= 2u;
   const uint64_t grid = (rows + lanes * a->rows_each - 1) / (lanes * a->rows_each);
-  if (tokens(a->rows_each) * pairs > kMaxTurns || grid >= ((uint64_t)1 << 31)) return false;
+  if (tokens(a->rows_each) * pairs > kMaxTurns || grid >= kMostGrid) return false;
   a->slots.set(slots);
   a->pairs.set(pairs);
   l->v = v;

@@ -89,6 +89,15 @@ static void refusals() {
   for (lt_tensor h : {x, p, cache, l, t, huge, wide, one}) CHECK(lt_release(ctx, h) == LT_OK);
 }
 
+// More blocks than a launch has threads for, and more tiles than 31 bits count.
+static void too_large(int64_t seqs, int64_t kv, int64_t slots, int64_t rows, lt_status expected) {
+  const lt_tensor q = dev({seqs, kv, 4}, LT_F32), cache = dev({9, 2, kv, rows, 4}, LT_F32), l = dev({seqs}, LT_I32), t = dev({seqs, slots}, LT_I32);
+  lt_tensor out = 0;
+  CHECK(op(LT_OP_PAGED_ATTENTION, {q, cache, l, t}, {}, &out) == LT_OK);
+  CHECK(lt_barrier(ctx, 1, nullptr) == expected);
+  for (lt_tensor h : {q, cache, l, t, out}) CHECK(lt_release(ctx, h) == LT_OK);
+}
+
 // What workgroups of an attention take: every tile of every block once, and never more pieces, workgroups or entries than there is room for.
 static void shares(std::mt19937& rng) {
   auto pick = [&](int64_t lo, int64_t hi) { return std::uniform_int_distribution<int64_t>(lo, hi)(rng); };
@@ -143,6 +152,12 @@ int main() {
     steps(0, 0, 6, 3, 20, 5, 2, 4, dt);    // no sequences
     steps(0, 5, 6, 3, 20, 5, 2, 4, dt);
   }
+  too_large((int64_t)1 << 24, 1, 1, 1, LT_ERR_UNSUPPORTED);
+  too_large(((int64_t)1 << 24) - 1, 1, 1, 1, LT_OK);
+  too_large(((int64_t)1 << 24) - 1, 1, 1000, 1, LT_ERR_UNSUPPORTED);
+  too_large((int64_t)1 << 20, 8, 2, 1, LT_OK);
+  too_large((int64_t)1 << 20, 16, 2, 1, LT_ERR_UNSUPPORTED);
+  too_large(64, 1, ((int64_t)1 << 31) - 1, 1, LT_ERR_UNSUPPORTED);
   std::mt19937 rng(1);
   for (int i = 0; i < 4000; ++i) shares(rng);
   CHECK(lt_shutdown(ctx) == LT_OK);
