@@ -904,8 +904,8 @@ template <typename T, int DP, int NH>
 hipError_t launch_paged_as(const PagedArgs& a, hipStream_t s) {
   const uint32_t row = a.dim * (uint32_t)sizeof(T);
   const bool whole = row % 16u == 0u && (uintptr_t)a.cache % 16u == 0u;
-  // caches larger than the last-level cache are read past it (one block of query heads a key head: others read the same keys): 537 MB 100.6 -> 91.1 us,
-  // 345 MB 75.2 -> 74.1; of 93 MB, which stay in it, the next read would take 27.5 -> 29.7
+  // caches larger than the last-level cache are read past it (one block of query heads a key head: others read the same keys): 537 MB 99.0 -> 86.4 us,
+  // 345 MB 75.3 -> 74.1; of 93 MB, which stay in it, the next read would take 27.5 -> 29.7
   const bool past = (uint64_t)a.pages * 2u * a.kv_heads * a.rows.d * row >= ((uint64_t)256 << 20) && a.pairs == a.kv_heads;
   if (whole && a.rows.d % 16u == 0u && past) LT_LAUNCH((lt_paged_attention_kernel<T, DP, NH, true, 16, true>), dim3(a.workgroups), dim3(kBlock), s, a);
   else if (whole && a.rows.d % 16u == 0u) LT_LAUNCH((lt_paged_attention_kernel<T, DP, NH, true, 16, false>), dim3(a.workgroups), dim3(kBlock), s, a);
