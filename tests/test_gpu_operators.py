@@ -569,6 +569,35 @@ def test_decoding_through_the_static_barrier():
     ctx.close()
 
 
+def test_decoding_in_a_captured_graph():
+    """a step recorded into the caller's own graph, replayed for token after token with other work between the replays"""
+    stream = torch.cuda.Stream(device=0)
+    ctx = context(stream=stream)
+    d = Decoder(ctx, "bf16", np.random.default_rng(26), longest=900)
+    d.prompt([700, 1, 2, 610, 33])
+    fixed = [t.clone() for t in d.next()]
+    torch.cuda.synchronize()
+    held = [ctx.tensor(t) for t in fixed]
+    o = d.record(*held)
+    ctx.barrier_static()
+    d.check(ctx.fetch(o))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        o = d.record(*held)
+        ctx.barrier_static(False)
+    for i in range(8):
+        for dst, src in zip(fixed, d.next()):
+            dst.copy_(src)
+        if i % 3 == 1:
+            torch.randn(1 << 20, device="cuda:0").sum()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        d.check(ctx.fetch(o))
+    del graph
+    ctx.close()
+
+
 def test_two_contexts_on_streams_of_their_own():
     rg = np.random.default_rng(18)
     streams = [torch.cuda.Stream(device=0) for _ in range(2)]
