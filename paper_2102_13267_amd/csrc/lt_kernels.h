@@ -385,7 +385,10 @@ struct PagedArgs {
     // (heads of 80 in the instance of 96 12.9 us, of 128 14.6; 148 short sequences with 8 key heads of 160 in that of 160 14.9, of 256 29.2; 75 with 4 of 20
     // and their append in that of 32 16.4, of 64 18.3)
     padded = dim <= 32u ? 32u : dim <= 64u ? 64u : dim <= 96u ? 96u : dim <= 128u ? 128u : dim <= 160u ? 160u : 256u;
-    blocks_of = group <= 16u || padded > 128u ? 16u : 32u;
+    // Two blocks of 16 in one read keys once for more heads, but a workgroup takes longer: only where there are many anyway (in 16s / 32s, us: one sequence of
+    // 20000 keys, 32 query heads on a key head of 128 bf16 19.6 / 30.0; 60 of 256 to 4096 26.0 / 25.8, with twice 32 on 64 23.6 / 20.7).  Their
+    // sums do not fit the registers for heads over 128.
+    blocks_of = group <= 16u || padded > 128u || (uint64_t)seqs * kv_heads < 64u ? 16u : 32u;
     pairs = kv_heads * ((group + blocks_of - 1u) / blocks_of);
     tile = dtype == kF32 ? 64u : 128u;
     const uint64_t most = capacity == 0 ? 1 : (capacity - 1u) / tile + 1u, all = (uint64_t)seqs * pairs;

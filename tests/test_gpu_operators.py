@@ -288,6 +288,14 @@ def test_attention_of_any_head(dim, rows, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("heads,kv,rows,dim", [(40, 2, 16, 64), (17, 1, 16, 128), (35, 1, 5, 96), (70, 2, 16, 20), (33, 1, 16, 5), (64, 2, 24, 80), (24, 1, 7, 33), (20, 1, 16, 160)])
+def test_attention_of_many_heads_a_key_head(heads, kv, rows, dim, dtype):
+    """of many sequences 32 at once, the last block short, a long sequence in pieces"""
+    rg = np.random.default_rng(27)
+    check_attention([2500, 700] + [int(n) for n in rg.integers(-1, 50, 66)], heads, kv, rows, dim, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_attention_of_one_long_sequence(dtype):
     for n, heads, kv, rows, dim in ((20000, 8, 1, 64, 128), (9001, 4, 4, 16, 64), (5003, 12, 2, 24, 80), (3333, 2, 1, 7, 256), (6007, 40, 1, 16, 128)):
         check_attention([n], heads, kv, rows, dim, dtype, seed=n)
