@@ -1,0 +1,80 @@
+"""How exact the operators are where the type of their data does not limit them, against 64 bits.
+
+Tolerances, from the arithmetic.  E = 2^-24 is half a step of fp32, R half a step of the result's type (2^-24, bf16 2^-8).
+Attention: ds = (dim + 8) E scale max_k sum_d |q_d k_d| bounds a score's error, which puts exp(score) 2 ds + 4 E off; sums of n terms
+err by n E of their magnitudes, numerator and denominator each.  A weight meets bf16 values as two bf16 numbers: what the first one
+leaves is below 2^-7 of it and is rounded by 2^-8 of itself (2^-15), the second one is made 2^-20 of the weight larger, and the exponent is
+rounded where it is below 64 (2^-19, times ln 2): below W = 2^-14 together.  |got - ref| <= (2 (2 ds + 4 E + n E) + W) sum_k p |v| + R |ref|."""
+import math
+
+import numpy as np
+import pytest
+
+from paper_2102_13267_amd import Context
+from test_gpu_operators import data, ints, paged_case
+
+pytestmark = pytest.mark.gpu
+E24 = 2.0 ** -24
+HALF = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8}
+WEIGHT = {"f32": 0.0, "bf16": 2.0 ** -14}
+
+
+def attend(cache, table, lens, q, dtype, scale=None):
+    ctx = Context(device=0, workspace_bytes=256 << 20)
+    got = ctx.fetch(ctx.paged_attention(ctx.tensor(q, dtype), ctx.tensor(cache, dtype), ctx.tensor(ints(lens)), ctx.tensor(table), scale=scale))
+    ctx.close()
+    return got
+
+
+def check(got, cache, table, lens, q, dtype):
+    seqs, heads, dim = q.shape
+    rows, group = cache.shape[3], heads // cache.shape[2]
+    scale = 1 / math.sqrt(dim)
+    for s, n in enumerate(lens):
+        if n == 0:
+            assert not got[s].any()
+            continue
+        pos = np.arange(n)
+        for h in range(heads):
+            k, v = (cache[table[s, pos // rows], i, h // group, pos % rows].astype(np.float64) for i in (0, 1))
+            qq = q[s, h].astype(np.float64)
+            ds = (dim + 8) * E24 * scale * (np.abs(k) @ np.abs(qq)).max()
+            e = np.exp(k @ qq * scale - (k @ qq * scale).max())
+            p = e / e.sum()
+            ref = p @ v
+            tol = (2 * (2 * ds + 4 * E24 + n * E24) + WEIGHT[dtype]) * (p @ np.abs(v)) + HALF[dtype] * np.abs(ref) + 1e-37
+            assert (np.abs(got[s, h] - ref) <= tol).all(), (s, h, np.max(np.abs(got[s, h] - ref) / tol))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("heads,kv,rows,dim", [(8, 2, 16, 128), (4, 4, 16, 64), (6, 2, 5, 96), (5, 1, 16, 32), (3, 3, 8, 20), (2, 1, 16, 256), (4, 2, 24, 160)])
+def test_weights_are_not_rounded_to_the_cache_s_type(heads, kv, rows, dim, dtype):
+    rg = np.random.default_rng(dim)
+    lens = [2, 3, 17, 40, 100, 200, 0, 77]
+    cache, table = paged_case(rg, lens, kv, rows, dim, dtype)
+    q = data(rg, (len(lens), heads, dim), dtype)
+    check(attend(cache, table, lens, q, dtype), cache, table, lens, q, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_weights_of_many_heads_a_key_head_are_not_rounded(dtype):
+    rg = np.random.default_rng(1)
+    lens = [int(n) for n in rg.integers(1, 90, 70)]
+    cache, table = paged_case(rg, lens, 1, 16, 64, dtype)
+    q = data(rg, (len(lens), 24, 64), dtype)
+    check(attend(cache, table, lens, q, dtype), cache, table, lens, q, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", [16, 5])
+def test_an_infinite_value_that_counts_is_the_result(rows, dtype):
+    """also where its weight is a number of few bits, whose rest is nothing"""
+    rg = np.random.default_rng(2)
+    lens = [1, 2, 8, 40]
+    cache, table = paged_case(rg, lens, 1, rows, 64, dtype)
+    for s in range(len(lens)):
+        cache[table[s, 0], 1, 0, 0, 3], cache[table[s, 0], 1, 0, 0, 60] = np.inf, -np.inf
+    q = data(rg, (len(lens), 4, 64), dtype)
+    for scale in (0.0, None):
+        got = attend(cache, table, lens, q, dtype, scale)
+        assert (got[..., 3] == np.inf).all() and (got[..., 60] == -np.inf).all() and np.isfinite(np.delete(got, (3, 60), axis=-1)).all()
