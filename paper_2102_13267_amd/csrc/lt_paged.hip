@@ -592,6 +592,10 @@ __global__ __launch_bounds__(kBlock, NH == 1 && (AL == 16 || AL == kWide) ? (DP 
     for (int j = 0; j < NV; ++j) acc[b][j] = F4{0.0f, 0.0f, 0.0f, 0.0f};
   }
   const float scale = a.scale * kLog2e;
+  // Weights are 2^-spread at most, so that those of all `len` keys add up to less than one, and no sum of theirs with values passes the largest of these.  bf16: the
+  // exponents are that much smaller (rounded, 2^-20 of a weight); fp32: the powers are.
+  const uint32_t spread = 32u - (uint32_t)__builtin_clz(w.len | 1u);
+  const float shift = G::BF ? (float)spread : 0.0f, share = __uint_as_float((127u - spread) << 23);
   // (PG) bytes from a tile's first row to what this lane reads of its own
   const uint32_t key_at = (n * a.dim + g * G::CE) * kSize, key_at0 = g * 16u, value_at0 = (n * NV < a.dim ? n * NV : 0u) * kSize;
 
@@ -728,7 +732,7 @@ __global__ __launch_bounds__(kBlock, NH == 1 && (AL == 16 || AL == kWide) ? (DP 
               mx = fmaxf(mx, s[b][t][r]);
             }
         }
-        const float fresh = fmaxf(top[b], max_over_groups(mx)), safe = fresh == -INFINITY ? 0.0f : fresh, keep = power2(top[b] - safe);
+        const float fresh = fmaxf(top[b], max_over_groups(mx) + shift), safe = fresh == -INFINITY ? 0.0f : fresh, keep = power2(top[b] - safe);
         top[b] = fresh;
         float part = 0.0f;
 #pragma unroll
@@ -736,6 +740,7 @@ __global__ __launch_bounds__(kBlock, NH == 1 && (AL == 16 || AL == kWide) ? (DP 
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             s[b][t][r] = power2(s[b][t][r] - safe);
+            if constexpr (!G::BF) s[b][t][r] *= share;
             part += s[b][t][r];
           }
         sum[b] = fmaf(sum[b], keep, part);

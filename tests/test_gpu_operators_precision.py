@@ -10,6 +10,7 @@ import math
 import numpy as np
 import pytest
 
+from oracle.numeric import round_to_bf16
 from paper_2102_13267_amd import Context
 from test_gpu_operators import data, ints, paged_case
 
@@ -78,3 +79,21 @@ def test_an_infinite_value_that_counts_is_the_result(rows, dtype):
     for scale in (0.0, None):
         got = attend(cache, table, lens, q, dtype, scale)
         assert (got[..., 3] == np.inf).all() and (got[..., 60] == -np.inf).all() and np.isfinite(np.delete(got, (3, 60), axis=-1)).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,dim", [(16, 64), (24, 80)])
+def test_an_average_of_values_near_the_largest_is_finite(rows, dim, dtype):
+    """of one chunk and of several, of all signs"""
+    rg = np.random.default_rng(3)
+    lens = [1, 2, 3, 64, 200, 300, 0]
+    for more in ([], [5000]):
+        at = lens + more
+        cache, table = paged_case(rg, at, 2, rows, dim, dtype)
+        v = np.float32(2.0 ** 127) * rg.uniform(1.0, 1.984375, cache[:, 1].shape).astype(np.float32)
+        v[..., ::2] *= rg.choice([-1.0, 1.0], v[..., ::2].shape).astype(np.float32)
+        cache[:, 1] = round_to_bf16(v) if dtype == "bf16" else v
+        q = data(rg, (len(at), 4, dim), dtype)
+        got = attend(cache, table, at, q, dtype)
+        assert np.isfinite(got).all()
+        check(got, cache, table, at, q, dtype)
