@@ -284,15 +284,14 @@ struct SliceArgs {
 };
 
 // ---- rotary positions, and a paged cache of keys and values ------------------------------------
-// Quarter turns per position of every rotated pair (frequency * 2 / pi), in 64 bits: position * turns
-// is then exact to 2^-22 of a turn at the largest position, and its fraction is what is left to
-// compute a sine of.
+// Quarter turns per position of every rotated pair (frequency * 2 / pi), in 64 bits: it and position * turns are rounded six times, 2^-50 of
+// the quarter turns together, which is 2^-20 of one at the largest position; their fraction is what is left to compute a sine of.
 constexpr uint32_t kMaxPairs = 128;
 struct Rotary {
   double turns[kMaxPairs];
+  double amplitude;
   uint32_t dims, interleaved;   // dims 0: nothing is rotated
-  float amplitude;
-  uint32_t back;                // turn the other way
+  uint32_t back, pad;           // back: turn the other way
 };
 
 // n / d for n < 2^31, 1 <= d <= 2^31: the product with ceil(2^(31 + shift) / d), shift = ceil(log2 d)

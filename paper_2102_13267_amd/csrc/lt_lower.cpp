@@ -1795,7 +1795,7 @@ struct Lowering {
     const double pi = 3.14159265358979323846;
     r->dims = (uint32_t)get(LT_ATTR_ROPE_DIMS).v.i;
     r->interleaved = (uint32_t)get(LT_ATTR_ROPE_INTERLEAVED).v.i;
-    r->amplitude = (float)get(LT_ATTR_ROPE_AMPLITUDE).v.f;
+    r->amplitude = get(LT_ATTR_ROPE_AMPLITUDE).v.f;
     r->back = back ? 1u : 0u;
     const double theta = get(LT_ATTR_ROPE_BASE).v.f, factor = get(LT_ATTR_ROPE_FACTOR).v.f, original = get(LT_ATTR_ROPE_ORIGINAL).v.f;
     const double low = get(LT_ATTR_ROPE_LOW).v.f, high = get(LT_ATTR_ROPE_HIGH).v.f;

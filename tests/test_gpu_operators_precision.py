@@ -4,14 +4,17 @@ Tolerances, from the arithmetic.  E = 2^-24 is half a step of fp32, R half a ste
 Attention: ds = (dim + 8) E scale max_k sum_d |q_d k_d| bounds a score's error, which puts exp(score) 2 ds + 4 E off; sums of n terms
 err by n E of their magnitudes, numerator and denominator each.  A weight meets bf16 values as two bf16 numbers: what the first one
 leaves is below 2^-7 of it and is rounded by 2^-8 of itself (2^-15), the second one is made 2^-20 of the weight larger, and the exponent is
-rounded where it is below 64 (2^-19, times ln 2): below W = 2^-14 together.  |got - ref| <= (2 (2 ds + 4 E + n E) + W) sum_k p |v| + R |ref|."""
+rounded where it is below 64 (2^-19, times ln 2): below W = 2^-14 together.  |got - ref| <= (2 (2 ds + 4 E + n E) + W) sum_k p |v| + R |ref|.
+Rotation: a turn is the product of amplitude and a sine of 64 bits, rounded once (E of each product); y s and the sum are rounded once
+each: |got - ref| <= E (|x c| + 2 |y s| + |ref|) + A (|x| + |y|), where A is what 64 bits lose of an angle: position 2^-50 (its product and the
+frequency's roundings) + 2^-40 (what the polynomials leave out, the terms of E^2)."""
 import math
 
 import numpy as np
 import pytest
 
-from oracle.numeric import round_to_bf16
-from paper_2102_13267_amd import Context
+from oracle.numeric import Eager, round_to_bf16
+from paper_2102_13267_amd import Context, Rotary
 from test_gpu_operators import data, ints, paged_case
 
 pytestmark = pytest.mark.gpu
@@ -97,3 +100,27 @@ def test_an_average_of_values_near_the_largest_is_finite(rows, dim, dtype):
         got = attend(cache, table, at, q, dtype)
         assert np.isfinite(got).all()
         check(got, cache, table, at, q, dtype)
+
+
+@pytest.mark.parametrize("r", [Rotary(), Rotary(interleaved=True), Rotary(factor=8.0, original=8192.0, amplitude=1.3), Rotary(dims=32, base=500000.0, amplitude=-0.7)])
+def test_sines_are_rounded_once(r):
+    rg = np.random.default_rng(4)
+    tokens, heads, dim = 700, 3, 64
+    p = ints(np.concatenate([np.arange(300), rg.integers(-(1 << 17), 1 << 17, tokens - 300)]))
+    a, first, second = Eager._angles(p, r, dim)
+    ctx = Context(device=0, workspace_bytes=64 << 20)
+    one, other, some = np.zeros((tokens, heads, dim), np.float32), np.zeros((tokens, heads, dim), np.float32), rg.standard_normal((tokens, heads, dim)).astype(np.float32)
+    one[..., first] = 1.0
+    other[..., second] = 1.0
+    for sign, op in ((1.0, ctx.rope), (-1.0, ctx.rope_grad)):
+        c, s = (r.amplitude * f(a)[:, None] for f in (np.cos, lambda z: np.sin(sign * z)))      # noqa: B023
+        for x in (one, other, some):
+            got = ctx.fetch(op(ctx.tensor(x), ctx.tensor(p), r)).astype(np.float64)
+            u, w = x[..., first].astype(np.float64), x[..., second].astype(np.float64)
+            lost = (np.abs(p)[:, None, None] * 2.0 ** -50 + 2.0 ** -40) * abs(r.amplitude) * (np.abs(u) + np.abs(w))
+            for at, y, z in ((first, u * c, -w * s), (second, w * c, u * s)):
+                tol = E24 * (np.abs(y) + 2 * np.abs(z) + np.abs(y + z)) + lost
+                if x is not some:      # a product with one and a sum with nothing are exact
+                    tol = E24 * np.abs(y + z) + lost
+                assert (np.abs(got[..., at] - (y + z)) <= tol).all(), np.max(np.abs(got[..., at] - (y + z)) / tol)
+    ctx.close()
