@@ -111,6 +111,15 @@ typedef enum {
  * a sequence with nothing that counts (length 0 or negative) gets zeros.  Default scale: 1 / sqrt(dim); its magnitude is
  * at most 1e38.
  *
+ * Operands that are not tensors of their own.  x, q, k and v are read where they lie if they are windows of heads or of the first axis, or broadcast along any
+ * axis but the last; caches, lengths, tables, positions and offsets if they are windows along the first axis (also reshaped, as one layer of [layers, pages, 2,
+ * ...]).  Other windows and permutations are copied first (heads are best told apart by a reshape before the windows), and so are broadcast lengths,
+ * tables, positions and offsets.  LT_ERR_UNSUPPORTED at the barrier: a host scalar's broadcast, a broadcast along the last of several axes or of a
+ * cache, and a broadcast x whose axes before `heads` take more than two strides.
+ * Rows are written in place where an assigned cache is a tensor of its own (one layer of a larger tensor, which the trace does not read otherwise:
+ * lt_tensor_from_device at its address; a window of it would be copied), and by the last append to it in a trace (those before it copy the cache: a barrier
+ * between them does not).
+ *
  * LT_ERR_SHAPE where pages * rows, slots * rows, 2 * key heads * dim, sequences or tokens is 2^31 or more.  An attention of 2^24 sequences times
  * key heads or more (less 512), or of 2^31 tiles of 64 keys (bf16: 128) that these could hold, has no lowering (LT_ERR_UNSUPPORTED at the barrier).
  */

@@ -735,20 +735,47 @@ class Tracer:
             heads = {ROPE: (0,), ROPE_GRAD: (0,), CACHE_APPEND: (1, 2), PAGED_ATTENTION: (0,)}.get(nd[u].op, ())
             return bool(heads) and rank >= 3 and axis in (0, rank - 2) and all(k in heads for k, v in enumerate(rins[u]) if v[0] == i)
 
+        OPERATORS = (ROPE, ROPE_GRAD, CACHE_APPEND, PAGED_ATTENTION)
+
+        def reads_dense(i, u):
+            # operator u reads node i as one tensor in memory: lengths, tables, positions, a cache
+            heads = {CACHE_APPEND: (1, 2)}.get(nd[u].op, (0,))
+            return nd[u].op in OPERATORS and not any(v[0] == i and k in heads for k, v in enumerate(rins[u]))
+
+        def first_axis(i):
+            return next((a[2] for a in nd[i].attrs if a[0] == A_AXIS), 0) == 0
+
+        def reads_window(i, u):
+            # a window along the first axis of elements that lie one behind the other, read where it lies (also through a reshape for operators alone)
+            j = rins[i][0][0]
+            while cls[j] == VIEW and (nd[j].op == RESHAPE or (nd[j].op == NARROW and first_axis(j))):
+                j = rins[j][0][0]
+            if cls[j] == VIEW or not first_axis(i):
+                return False
+            if nd[u].op == RESHAPE and not is_root[u]:
+                return bool(pre_users[u]) and all(nd[w].op in OPERATORS for w in pre_users[u])
+            return reads_dense(i, u)
+
+        def written_out(i):
+            # a broadcast of integers that an operator reads as one tensor; not of a host scalar, not along the last of several axes
+            n, frm = nd[i], oshape(rins[i][0])
+            return (n.op == EXPAND and n.dtype == S32 and not is_imm((i, 0)) and numel(frm) != numel(n.shape)
+                    and (len(n.shape) < 2 or tuple(frm[-1:]) == n.shape[-1:]) and any(reads_dense(i, u) for u in pre_users[i]))
+
         def klass(i):
             n = nd[i]
             if n.op in (DEVICE_DATA, SCALAR_PARAM, CONSTANT):
                 return LEAF
             if n.op in (EXPAND, RESHAPE):
                 # a view that must itself be materialised (it is a root) is a copy
-                return EW if is_root[i] else VIEW
+                return EW if is_root[i] or written_out(i) else VIEW
             if n.op == PERMUTE:
                 # a permutation that only feeds contractions is addressing (operand strides), not a copy
                 return VIEW if (not is_root[i] and pre_users[i] and all(nd[u].op == MATMUL for u in pre_users[i])) else EW
             if n.op == NARROW:
-                # a window is addressing for elementwise ops, contractions and permutations; otherwise a copy
+                # a window is addressing for elementwise ops, contractions, permutations and operators; otherwise a copy
                 ok = not is_root[i] and pre_users[i] and all(
-                    nd[u].op in UNARY or nd[u].op in BINARY or nd[u].op in (MATMUL, PERMUTE) or reads_heads(i, u) for u in pre_users[i])
+                    nd[u].op in UNARY or nd[u].op in BINARY or nd[u].op in (MATMUL, PERMUTE) or reads_heads(i, u) or reads_window(i, u) for u in pre_users[i])
                 return VIEW if ok else EW
             if n.op == SLICE_UPDATE:
                 return SLICE
@@ -782,7 +809,6 @@ class Tracer:
                 for v in rins[j]:
                     if j not in pre_users[v[0]]:
                         pre_users[v[0]].append(j)
-        cls = [klass(i) if live[i] else "DEAD" for i in range(N)]
 
         def is_imm(v):
             n = nd[v[0]]
@@ -791,6 +817,10 @@ class Tracer:
             if n.op in (EXPAND, RESHAPE):
                 return is_imm(rins[v[0]][0])
             return False
+
+        cls = []                                # (a node's class may depend on those before it)
+        for i in range(N):
+            cls.append(klass(i) if live[i] else "DEAD")
 
         def base(v):
             while cls[v[0]] == VIEW:
@@ -869,7 +899,7 @@ class Tracer:
                 r = region_of[a]
                 in_shape = oshape(rins[a][0])
                 for i in range(a - 1, -1, -1):
-                    if cls[i] != EW or len(region_of[i]["members"]) != 1 or is_root[i]:
+                    if cls[i] != EW or len(region_of[i]["members"]) != 1 or is_root[i] or nd[i].dtype == S32:
                         continue
                     if nd[i].shape != in_shape or not users[i]:
                         continue
@@ -908,7 +938,7 @@ class Tracer:
                 return False
             shape = nd[i].shape
             if r["kind"] == EW:
-                return shape == nd[min(r["members"])].shape
+                return shape == nd[min(r["members"])].shape and nd[min(r["members"])].dtype != S32
             a = r["anchor"]
             if r["kind"] == MM:
                 return shape == nd[a].shape
@@ -938,7 +968,7 @@ class Tracer:
             del regions[id(other)]
 
         for i in range(N):
-            if cls[i] != EW or len(region_of[i]["members"]) != 1:
+            if cls[i] != EW or len(region_of[i]["members"]) != 1 or nd[i].dtype == S32:   # (copies of integers stay by themselves)
                 continue
             if nd[i].op == PERMUTE:
                 # a permutation of a bare contraction result that nothing else reads becomes the
@@ -975,7 +1005,7 @@ class Tracer:
                         q = region_of.get(v[0])
                         if q is None or q is home or q["kind"] != EW or id(q) not in regions:
                             continue
-                        if nd[min(q["members"])].shape != nd[i].shape or any(is_root[m] for m in q["members"]):
+                        if nd[min(q["members"])].shape != nd[i].shape or nd[min(q["members"])].dtype == S32 or any(is_root[m] for m in q["members"]):
                             continue
                         if not all(u in q["members"] or u in home["members"] for m in q["members"] for u in users[m]):
                             continue

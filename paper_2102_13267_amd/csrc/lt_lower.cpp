@@ -11,6 +11,7 @@
 //             EW (elementwise, permute, root views), ROW / COL / ALL (reductions by axis; the
 //             fixed row operators are ROW), MM (matmul), OP (rotary positions and the paged cache: nothing joins them).
 //   pass 0    every live EW / ROW / COL / ALL / MM / OP node is a region of its own.
+//             Copies of integers stay by themselves.
 //   pass 1    plain reductions absorb, walking down from the anchor, every elementwise node of the
 //             reduced tensor's shape whose users all lie inside the region (prologue).
 //   pass 2    in canonical order each still-single elementwise node joins the region of one of
@@ -112,12 +113,51 @@ struct Lowering {
   // a window of heads or of the first axis (the queries, keys and values of one projection) that such an operand can be
   bool heads_window(int32_t i, int32_t u) const {
     const Node* n = nd[i];
-    if (!is_operator(nd[u]->op) || n->rank < 3) return false;
-    for (int k = 0; k < n->n_attr; ++k)
-      if (n->attrs[k].key == LT_ATTR_AXIS && n->attrs[k].v.i != 0 && n->attrs[k].v.i != n->rank - 2) return false;
+    if (!is_operator(nd[u]->op) || n->rank < 3 || (narrow_axis(n) != 0 && narrow_axis(n) != n->rank - 2)) return false;
     for (size_t k = 0; k < rins[u].size(); ++k)
       if (rins[u][k].node == i && !heads_operand(nd[u]->op, k)) return false;
     return true;
+  }
+
+  // whether operator u reads node i as one tensor in memory (lengths, tables, positions, a cache)
+  bool dense_reader(int32_t i, int32_t u) const {
+    if (!is_operator(nd[u]->op)) return false;
+    for (size_t k = 0; k < rins[u].size(); ++k)
+      if (rins[u][k].node == i && heads_operand(nd[u]->op, k)) return false;
+    return true;
+  }
+  static int64_t narrow_axis(const Node* n) {
+    for (int k = 0; k < n->n_attr; ++k)
+      if (n->attrs[k].key == LT_ATTR_AXIS) return n->attrs[k].v.i;
+    return 0;
+  }
+  // a value whose elements lie one behind the other, at some offset (the classes of all nodes before v are known)
+  bool contiguous_value(Val v) const {
+    while (cls[v.node] == C_VIEW) {
+      const Node* n = nd[v.node];
+      if (n->op != LT_OP_RESHAPE && !(n->op == LT_OP_NARROW && narrow_axis(n) == 0)) return false;
+      v = rins[v.node][0];
+    }
+    return true;
+  }
+  // a window along the first axis of such a value (some of the lengths, some rows of a table, one layer of many caches) that
+  // operator u reads where it lies; also through a reshape that only operators read
+  bool dense_window(int32_t i, int32_t u) const {
+    if (narrow_axis(nd[i]) != 0 || !contiguous_value(rins[i][0])) return false;
+    if (nd[u]->op != LT_OP_RESHAPE || is_root[u]) return dense_reader(i, u);
+    for (int32_t w : users[u])
+      if (!is_operator(nd[w]->op)) return false;
+    return !users[u].empty();
+  }
+  // a broadcast of integers that an operator reads is written out; one of a host scalar, and one along the last of several axes, is refused
+  bool written_out(int32_t i) const {
+    const Node* n = nd[i];
+    const std::vector<int64_t> from = out_shape(rins[i][0]);
+    if (n->op != LT_OP_EXPAND || n->dtype != LT_I32 || is_imm(Val{i, 0}) || count(from) == count(shape_of(i))) return false;
+    if (n->rank > 1 && (from.empty() || from.back() != n->dims[n->rank - 1])) return false;
+    for (int32_t u : users[i])
+      if (dense_reader(i, u)) return true;
+    return false;
   }
 
   // value of a node known at lowering time (constants 0 / 1, seen through views)
@@ -205,7 +245,7 @@ struct Lowering {
       if (!live[i]) continue;
       const uint16_t op = nd[i]->op;
       if (op == OP_DEVICE_DATA || op == OP_SCALAR_PARAM || op == OP_CONSTANT) cls[i] = C_LEAF;
-      else if (op == LT_OP_EXPAND || op == LT_OP_RESHAPE) cls[i] = is_root[i] ? C_EW : C_VIEW;
+      else if (op == LT_OP_EXPAND || op == LT_OP_RESHAPE) cls[i] = is_root[i] || written_out(i) ? C_EW : C_VIEW;
       else if (op == LT_OP_PERMUTE) {
         // a permutation that only feeds contractions is addressing (operand strides), not a copy
         bool only_mm = !is_root[i] && !users[i].empty();
@@ -213,10 +253,10 @@ struct Lowering {
         cls[i] = only_mm ? C_VIEW : C_EW;
       } else if (op == LT_OP_NARROW) {
         // a window is addressing (an offset and the base's strides) for the consumers that can
-        // address it: elementwise ops, contractions, permutations, operators that read heads; otherwise a copy
+        // address it: elementwise ops, contractions, permutations, operators; otherwise a copy
         bool addr = !is_root[i] && !users[i].empty();
         for (int32_t u : users[i])
-          addr = addr && (is_unary(nd[u]->op) || is_binary(nd[u]->op) || nd[u]->op == LT_OP_MATMUL || nd[u]->op == LT_OP_PERMUTE || heads_window(i, u));
+          addr = addr && (is_unary(nd[u]->op) || is_binary(nd[u]->op) || nd[u]->op == LT_OP_MATMUL || nd[u]->op == LT_OP_PERMUTE || heads_window(i, u) || dense_window(i, u));
         cls[i] = addr ? C_VIEW : C_EW;
       } else if (op == LT_OP_SLICE_UPDATE) cls[i] = C_SLICE;
       else if (is_unary(op) || is_binary(op)) cls[i] = C_EW;
@@ -330,7 +370,7 @@ struct Lowering {
   bool compatible(const Region* r, int32_t i) const {
     if (r->sealed) return false;
     const std::vector<int64_t> shape = shape_of(i);
-    if (r->kind == C_EW) return shape == shape_of(r->members.front());
+    if (r->kind == C_EW) return shape == shape_of(r->members.front()) && nd[r->members.front()]->dtype != LT_I32;
     const int32_t a = r->anchor;
     if (r->kind == C_MM) return shape == shape_of(a);
     if (plain_reduce(nd[a]->op)) {
@@ -357,7 +397,7 @@ struct Lowering {
       Region* r = region_of[a];
       const std::vector<int64_t> in_shape = out_shape(rins[a][0]);
       for (int32_t i = a - 1; i >= 0; --i) {
-        if (cls[i] != C_EW || region_of[i]->members.size() != 1 || is_root[i]) continue;
+        if (cls[i] != C_EW || region_of[i]->members.size() != 1 || is_root[i] || nd[i]->dtype == LT_I32) continue;
         if (shape_of(i) != in_shape || users[i].empty()) continue;
         bool inside = true;
         for (int32_t u : users[i]) inside &= r->has(u);
@@ -368,7 +408,7 @@ struct Lowering {
     }
     // pass 2: epilogue / finaliser / elementwise grouping
     for (int32_t i = 0; i < N; ++i) {
-      if (cls[i] != C_EW || region_of[i]->members.size() != 1) continue;
+      if (cls[i] != C_EW || region_of[i]->members.size() != 1 || nd[i]->dtype == LT_I32) continue;
       if (nd[i]->op == LT_OP_PERMUTE) {
         // a permutation of a bare contraction result that nothing else reads becomes the
         // contraction's output layout
@@ -409,7 +449,7 @@ struct Lowering {
           for (Val v : rins[i]) {
             Region* q = region_of[v.node];
             if (!q || q == home || q->kind != C_EW || !q->alive) continue;
-            if (shape_of(q->members.front()) != shape_of(i)) continue;
+            if (shape_of(q->members.front()) != shape_of(i) || nd[q->members.front()]->dtype == LT_I32) continue;
             bool ok = true;
             for (int32_t m : q->members) {
               ok = ok && !is_root[m];
@@ -690,6 +730,10 @@ struct Lowering {
     const int64_t n = count(space);
     if (n >= ((int64_t)1 << 32)) return bad(LT_ERR_UNSUPPORTED, "iteration space of 2^32 or more elements");
     p.n = (uint64_t)n;
+    // a copy of integers moves words as they are
+    const int32_t only = members.size() == 1 && anchor.node < 0 ? members[0] : -1;
+    const bool words = only >= 0 && nd[only]->dtype == LT_I32 && rins[only].size() == 1 && !is_imm(rins[only][0]) && out_dtype(rins[only][0]) == LT_I32 &&
+                       (nd[only]->op == LT_OP_EXPAND || nd[only]->op == LT_OP_RESHAPE || nd[only]->op == LT_OP_PERMUTE || nd[only]->op == LT_OP_NARROW);
     p.cols = (uint32_t)(space.empty() ? 1 : std::max<int64_t>(space.back(), 1));
     p.vec_ok = (p.cols % 4u == 0u) ? 1u : 0u;
     p.full_vec_ok = (full_vec || p.vec_ok) ? 1u : 0u;
@@ -744,7 +788,7 @@ struct Lowering {
       if (!make_access(input_vals[k], space, input_perm[k], &acc)) return false;
       ltk::EwIn& in = p.in[k];
       in.ptr = nullptr;
-      in.dtype = acc.dtype;
+      in.dtype = words ? (uint32_t)ltk::kF32 : acc.dtype;
       // classify the access
       const std::vector<int64_t> cs = contiguous(space);
       bool full = true, zero = true, rowvec = !space.empty(), colvec = !space.empty();
@@ -875,7 +919,7 @@ struct Lowering {
       if (m == anchor.node) continue;
       const Node* n = nd[m];
       const auto& o = rins[m];
-      if (n->dtype != LT_F32 && n->dtype != LT_BF16) return bad(LT_ERR_UNSUPPORTED, "integer elementwise arithmetic has no lowering");
+      if (n->dtype != LT_F32 && n->dtype != LT_BF16 && !words) return bad(LT_ERR_UNSUPPORTED, "integer elementwise arithmetic has no lowering");
       uint32_t enc[3] = {0, 0, 0};
       const bool private_in = permute_input[m] >= 0;
       if (private_in) {
@@ -971,7 +1015,7 @@ struct Lowering {
       const Val v = outputs[k];
       ltk::EwOut& out = p.out[k];
       out.ptr = nullptr;
-      out.dtype = out_dtype(v);
+      out.dtype = words ? (uint32_t)ltk::kF32 : out_dtype(v);
       out.slot = (uint32_t)info[find_val(v)].slot;
       const int64_t on = count(out_shape(v));
       out.scalar = (on == 1 && n > 1) ? 1u : 0u;

@@ -23,10 +23,11 @@ constexpr float kLog2e = 1.44269504088896340736f;
 // on their way while it finds out where these go and computes their turns.  8 prompts of up to 2048 tokens, 8 key heads of 128 bf16,
 // 49 MB: 11.6 us, 4.2 TB/s (one thread a pair, each with a search and a turn of its own, 42); 64 single tokens 4.3 us on the device, less
 // than a call costs the host.
+typedef uint32_t WordsAny __attribute__((ext_vector_type(4), aligned(2)));   // wherever a window of caches begins
 __global__ __launch_bounds__(kBlock) void lt_cache_copy_kernel(const AppendArgs a) {
   const uint64_t n = a.cache_elems * (a.cache_dtype == kF32 ? 4u : 2u), stride = (uint64_t)gridDim.x * kBlock * 16u;
   for (uint64_t i = ((uint64_t)blockIdx.x * kBlock + threadIdx.x) * 16u; i < n; i += stride) {
-    if (i + 16u <= n) *(uint4*)((char*)a.cache + i) = *(const uint4*)((const char*)a.copy_from + i);
+    if (i + 16u <= n) *(WordsAny*)((char*)a.cache + i) = *(const WordsAny*)((const char*)a.copy_from + i);
     else
       for (uint64_t k = i; k < n; k += 2u) *(uint16_t*)((char*)a.cache + k) = *(const uint16_t*)((const char*)a.copy_from + k);
   }
@@ -179,7 +180,8 @@ template <typename C, typename T>
 hipError_t launch_append_of(AppendArgs a, bool* rode, hipStream_t s) {
   constexpr uint32_t kMost = 16u / (sizeof(C) > sizeof(T) ? sizeof(C) : sizeof(T));
   const uint64_t rows = (uint64_t)a.tokens * a.token_rows.d;
-  const uint64_t aligned = std::min(row_alignment(a.k, sizeof(T), a.k_token, a.k_head, 0), row_alignment(a.v, sizeof(T), a.v_token, a.v_head, 0));
+  const uint64_t aligned =
+      std::min(row_alignment(a.cache, sizeof(C), 0, 0, 0), std::min(row_alignment(a.k, sizeof(T), a.k_token, a.k_head, 0), row_alignment(a.v, sizeof(T), a.v_token, a.v_head, 0)));
   const uint32_t v = piece_of(a.rotary, a.dim, aligned, kMost), slots = v ? slots_of(a.rotary, a.dim, v) : 0u, pairs = a.rotary.dims / 2u;
   a.rows_each = kMaxRows;
   if (v && slots <= kBlock) {

@@ -187,7 +187,8 @@ struct RopeLayout {
   Past past;
 };
 inline bool lay_out(RopeArgs* a, uint32_t size, RopeLayout* l) {
-  const uint64_t rows = a->tokens * a->heads.d, aligned = row_alignment(a->x, size, a->s_outer, a->s_inner, a->s_head);
+  const uint64_t rows = a->tokens * a->heads.d, in = row_alignment(a->x, size, a->s_outer, a->s_inner, a->s_head), out = row_alignment(a->out, size, 0, 0, 0);
+  const uint64_t aligned = in < out ? in : out;
   const uint32_t v = piece_of(a->rotary, a->dim, aligned, 16u / size), slots = v ? slots_of(a->rotary, a->dim, v) : 0u, pairs = a->rotary.dims / 2u;
   if (v == 0 || slots > kRowBlock) return false;
   const uint64_t bytes = rows * a->dim * size, cache = (uint64_t)256 << 20;
