@@ -377,6 +377,8 @@ struct PagedArgs {
   void* list;                   // behind the pieces (the launcher sets it)
   uint32_t pieces, q_whole;     // pieces: that parts and tickets are for.  q_whole: rows of q are whole 16-byte pieces (the launcher sets it)
 
+  // pages that the table can name: the pool may be far larger
+  uint64_t reach() const { return (uint64_t)seqs * slots < pages ? (uint64_t)seqs * slots : pages; }
   uint64_t part_floats() const { return (uint64_t)blocks_of * padded + 2u * blocks_of; }
   // The instance, and how the work is shared out; `capacity` and what comes before it are set.  Tiles of all sequences must be below 2^32.
   void share_out() {

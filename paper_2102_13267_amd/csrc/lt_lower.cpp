@@ -1993,8 +1993,8 @@ struct Lowering {
     // (a launch holds less than 2^32 threads)
     if ((double)args.seqs * args.pairs * (args.capacity / args.tile + 1u) >= 2147483648.0 || args.workgroups >= 1u << 24) return bad(LT_ERR_UNSUPPORTED, "paged_attention: sequences * slots * key heads too large");
     Launch l = make_launch(L_PAGED, k, args);
-    // (how long the sequences are is known on the device alone: as if every page were read once)
-    const uint64_t held = (uint64_t)count(cs), w = dtype_size(an->dtype);
+    // (how long the sequences are is known on the device alone: as if every page that the table can name were read once)
+    const uint64_t held = args.reach() * 2u * args.kv_heads * args.rows.d * args.dim, w = dtype_size(an->dtype);
     l.bytes = held * w + 2 * (uint64_t)count(shape_of(a)) * w;
     l.flops = 2 * held * (args.heads / args.kv_heads);
     plan->launches.push_back(std::move(l));

@@ -928,9 +928,15 @@ template <typename T, int DP, int NH>
 hipError_t launch_paged_as(const PagedArgs& a, hipStream_t s) {
   const uint32_t row = a.dim * (uint32_t)sizeof(T);
   const bool whole = row % 16u == 0u && (uintptr_t)a.cache % 16u == 0u;
-  // caches larger than the last-level cache are read past it (one block of query heads a key head: others read the same keys): 537 MB 99.0 -> 86.4 us,
-  // 345 MB 75.3 -> 74.1; of 93 MB, which stay in it, the next read would take 27.5 -> 29.7
-  const bool past = (uint64_t)a.pages * 2u * a.kv_heads * a.rows.d * row >= ((uint64_t)256 << 20) && a.pairs == a.kv_heads;
+  // Read past the last-level cache (one block of query heads a key head: others read the same keys) where the pages that the table can name are half of it and more: the next
+  // layer's cache and weights would push them out, and what they push out has to be written back if it is new.  us through it / past it, the same cache
+  // again, eight of them in turn, each behind 600 MB read, behind 600 MB written, 8 key heads of 128 bf16:
+  //   20 MB of keys and values (16 sequences of 300) 8.0 / 9.1, 8.8 / 10.1, 13.3 / 13.7, 14.7 / 13.8; 45 MB (64 of 32 to 512) - , 14.9 / 15.3, 18.4 / 19.1, 22.8 / 19.3;
+  //   82 MB (one of 20000) 22.0 / 22.0, 25.0 / 23.6, 28.2 / 27.3, 36.9 / 27.6; 93 MB (32 of 128 to 2048) 22.7 / 24.5, 26.5 / 26.2, 29.9 / 30.2, 38.7 / 30.3;
+  //   188 MB (one of 46000) 36.8 / 38.3, 42.7 / 40.0, 45.8 / 43.8, 65.6 / 43.9; 345 MB (60 of 256 to 4096) 64.3 / 66.5, 71.9 / 68.7, 75.5 / 73.3, 104.8 / 74.2;
+  //   537 MB (one of 131072) 100 / 88, 100 / 90, 104 / 94, 138 / 94.
+  // (What is read in the end, lengths say, on the device alone; a table as wide as the longest context names all of its pool, and short sequences lose up to 1.5 us by it.)
+  const bool past = a.reach() * 2u * a.kv_heads * a.rows.d * row >= ((uint64_t)128 << 20) && a.pairs == a.kv_heads;
   if (whole && a.rows.d % 16u == 0u && past) LT_LAUNCH((lt_paged_attention_kernel<T, DP, NH, true, 16, true>), dim3(a.workgroups), dim3(kBlock), s, a);
   else if (whole && a.rows.d % 16u == 0u) LT_LAUNCH((lt_paged_attention_kernel<T, DP, NH, true, 16, false>), dim3(a.workgroups), dim3(kBlock), s, a);
   else if (whole) LT_LAUNCH((lt_paged_attention_kernel<T, DP, NH, false, 16, false>), dim3(a.workgroups), dim3(kBlock), s, a);
