@@ -757,10 +757,11 @@ class Tracer:
             return reads_dense(i, u)
 
         def written_out(i):
-            # a broadcast of integers that an operator reads as one tensor; not of a host scalar, not along the last of several axes
+            # a broadcast of integers that a reshape reads, or an operator as one tensor; not of a host scalar, not along the last of several axes for an operator
             n, frm = nd[i], oshape(rins[i][0])
+            along_last = len(n.shape) > 1 and tuple(frm[-1:]) != n.shape[-1:]
             return (n.op == EXPAND and n.dtype == S32 and not is_imm((i, 0)) and numel(frm) != numel(n.shape)
-                    and (len(n.shape) < 2 or tuple(frm[-1:]) == n.shape[-1:]) and any(reads_dense(i, u) for u in pre_users[i]))
+                    and any(nd[u].op == RESHAPE or (not along_last and reads_dense(i, u)) for u in pre_users[i]))
 
         def klass(i):
             n = nd[i]

@@ -149,14 +149,15 @@ struct Lowering {
       if (!is_operator(nd[w]->op)) return false;
     return !users[u].empty();
   }
-  // a broadcast of integers that an operator reads is written out; one of a host scalar, and one along the last of several axes, is refused
+  // a broadcast of integers that a reshape or an operator reads is written out; one of a host scalar is refused, and one along the last of several axes that
+  // an operator would read
   bool written_out(int32_t i) const {
     const Node* n = nd[i];
     const std::vector<int64_t> from = out_shape(rins[i][0]);
     if (n->op != LT_OP_EXPAND || n->dtype != LT_I32 || is_imm(Val{i, 0}) || count(from) == count(shape_of(i))) return false;
-    if (n->rank > 1 && (from.empty() || from.back() != n->dims[n->rank - 1])) return false;
+    const bool last = n->rank > 1 && (from.empty() || from.back() != n->dims[n->rank - 1]);
     for (int32_t u : users[i])
-      if (dense_reader(i, u)) return true;
+      if (nd[u]->op == LT_OP_RESHAPE || (!last && dense_reader(i, u))) return true;
     return false;
   }
 

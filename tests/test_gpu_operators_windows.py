@@ -99,3 +99,15 @@ def test_one_length_position_and_table_for_all(dtype):
             ctx.close()
         for a, b in zip(*outs):
             assert np.array_equal(a, b)
+
+
+def test_positions_that_all_tokens_share_in_the_tokens_shape():
+    rg = np.random.default_rng(5)
+    x, p = data(rg, (10, 3, 4, 8), "bf16"), ints(rg.integers(0, 2 ** 26, (2, 1, 3)))
+    outs = []
+    for own in (True, False):
+        ctx = context()
+        P = ctx.tensor(np.repeat(p, 5, 1).reshape(10, 3)) if own else ctx.reshape(ctx.expand(ctx.tensor(p), (2, 5, 3)), (10, 3))
+        outs.append(ctx.fetch(ctx.rope(ctx.tensor(x, "bf16"), P)))
+        ctx.close()
+    assert np.array_equal(*outs)

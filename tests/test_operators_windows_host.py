@@ -40,6 +40,12 @@ def broadcasts(B):
     return t, B.paged_attention(B.rope(t["q"], B.expand(zeros(B, (1,), "s32"), (3,)), ROT), t["cache"], lengths, table)
 
 
+def broadcasts_reshaped(B):
+    """positions that all tokens share, in the shape of the tokens"""
+    p = B.reshape(B.expand(zeros(B, (2, 1, 3), "s32"), (2, 5, 3)), (10, 3))
+    return p, B.rope(zeros(B, (10, 3, 4, 8)), p, ROT), B.rope(zeros(B, (2, 3, 4, 8)), B.reshape(B.expand(zeros(B, (1,), "s32"), (6,)), (2, 3)), ROT)
+
+
 def copies_of_integers(B):
     """columns of a table, a window that is a result, and one behind a broadcast; copies of integers that share nothing with each other or with what reads them"""
     t = paged(B)
@@ -51,7 +57,7 @@ def copies_of_integers(B):
     return t, shown, same, B.cast(lengths, "f32"), B.add(t["q"], 1.0), B.paged_attention(t["q"], t["cache"], lengths, table), B.paged_attention(t["q"], t["cache"], shown, table)
 
 
-@pytest.mark.parametrize("program", [windows_of_integers, layers_of_one_tensor, appended_layers, broadcasts, copies_of_integers])
+@pytest.mark.parametrize("program", [windows_of_integers, layers_of_one_tensor, appended_layers, broadcasts, broadcasts_reshaped, copies_of_integers])
 def test_plans_equal_the_structural_oracles(program):
     ctx, ref = Context(), Tracer()
     keep = program(ctx), program(ref)
