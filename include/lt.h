@@ -121,7 +121,8 @@ typedef enum {
  * between them does not).
  *
  * LT_ERR_SHAPE where pages * rows, slots * rows, 2 * key heads * dim, sequences or tokens is 2^31 or more.  An attention of 2^24 sequences times
- * key heads or more (less 512), or of 2^31 tiles of 64 keys (bf16: 128) that these could hold, has no lowering (LT_ERR_UNSUPPORTED at the barrier).
+ * key heads or more (less 512), each counted once for every 16 query heads of it, or of 2^31 tiles of 64 keys (bf16: 128) that these could hold, has no
+ * lowering (LT_ERR_UNSUPPORTED at the barrier).
  */
 
 typedef enum {

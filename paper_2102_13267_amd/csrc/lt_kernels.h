@@ -386,10 +386,14 @@ struct PagedArgs {
     // (heads of 80 in the instance of 96 12.9 us, of 128 14.6; 148 short sequences with 8 key heads of 160 in that of 160 14.9, of 256 29.2; 75 with 4 of 20
     // and their append in that of 32 16.4, of 64 18.3)
     padded = dim <= 32u ? 32u : dim <= 64u ? 64u : dim <= 96u ? 96u : dim <= 128u ? 128u : dim <= 160u ? 160u : 256u;
-    // Two blocks of 16 in one read keys once for more heads, but a workgroup takes longer: only where there are many anyway (in 16s / 32s, us: one sequence of
-    // 20000 keys, 32 query heads on a key head of 128 bf16 19.6 / 30.0; 60 of 256 to 4096 26.0 / 25.8, with twice 32 on 64 23.6 / 20.7).  Their
-    // sums do not fit the registers for heads over 128.
-    blocks_of = group <= 16u || padded > 128u || (uint64_t)seqs * kv_heads < 64u ? 16u : 32u;
+    // Two blocks of 16 in one read keys once for more heads, but a workgroup takes longer: in bf16, for heads of up to 64, where there are many and long ones (us, in 16s /
+    // 32s, 32 query heads a key head, sequences x key heads of up to so many keys, heads of 32: 64 x 2048 10.3 / 10.4, 64 x 8192 17.5 / 16.0, 256 x 512 7.1 / 8.3, 256 x
+    // 1024 11.7 / 12.3, 256 x 2048 15.1 / 14.8, 1024 x 1024 24.2 / 19.2, but 1024 x 300 11.0 / 9.3; of 64: 32 x 4096 12.7 / 16.3, 64 x 4096 16.8 / 16.7, 64 x 8192 24.8 / 23.7, 512 x 600 14.0 / 15.2, 128 x
+    // 2048 15.2 / 15.4, 256 x 2048 22.7 / 20.2, 1600 x 300 24.2 / 26.7, 1600 x 1000 52.3 / 43.9; 64 heads on one of 64 128 x 4096 35.2 / 28.9).  Heads of 96 and 128 leave 32s two waves a SIMD and one: of 128
+    // 256 x 2048 37.1 / 39.0, 1024 x 300 28.6 / 38.7, 1600 x 300 41.0 / 61.4, although 64 x 8192 43.4 / 39.2, 256 x 4096 62.8 / 58.4; fp32 is slower in 32s everywhere (128 x 4096 of 64 38.9 / 41.9,
+    // of 128 77.3 / 83.5).  One sequence of 20000 keys on one head of 128: 19.6 / 30.0.
+    const uint64_t rowsets = (uint64_t)seqs * kv_heads;
+    blocks_of = group <= 16u || dtype == kF32 || padded > 64u || rowsets < 64u || capacity < 512u || rowsets * capacity < (1u << 19) ? 16u : 32u;
     pairs = kv_heads * ((group + blocks_of - 1u) / blocks_of);
     tile = dtype == kF32 ? 64u : 128u;
     const uint64_t most = capacity == 0 ? 1 : (capacity - 1u) / tile + 1u, all = (uint64_t)seqs * pairs;

@@ -947,10 +947,13 @@ hipError_t launch_paged_as(const PagedArgs& a, hipStream_t s) {
 
 template <typename T>
 hipError_t launch_paged_of(const PagedArgs& a, hipStream_t s) {
-  if (a.padded == 32u) return a.blocks_of == 16u ? launch_paged_as<T, 32, 1>(a, s) : launch_paged_as<T, 32, 2>(a, s);
-  if (a.padded == 64u) return a.blocks_of == 16u ? launch_paged_as<T, 64, 1>(a, s) : launch_paged_as<T, 64, 2>(a, s);
-  if (a.padded == 96u) return a.blocks_of == 16u ? launch_paged_as<T, 96, 1>(a, s) : launch_paged_as<T, 96, 2>(a, s);
-  if (a.padded == 128u) return a.blocks_of == 16u ? launch_paged_as<T, 128, 1>(a, s) : launch_paged_as<T, 128, 2>(a, s);
+  if constexpr (sizeof(T) == 2u) {
+    if (a.blocks_of == 32u) return a.padded == 32u ? launch_paged_as<T, 32, 2>(a, s) : launch_paged_as<T, 64, 2>(a, s);
+  }
+  if (a.padded == 32u) return launch_paged_as<T, 32, 1>(a, s);
+  if (a.padded == 64u) return launch_paged_as<T, 64, 1>(a, s);
+  if (a.padded == 96u) return launch_paged_as<T, 96, 1>(a, s);
+  if (a.padded == 128u) return launch_paged_as<T, 128, 1>(a, s);
   if (a.padded == 160u) return launch_paged_as<T, 160, 1>(a, s);
   return launch_paged_as<T, 256, 1>(a, s);
 }
@@ -960,7 +963,7 @@ hipError_t launch_paged(const void* args, hipStream_t s) {
   if (a.seqs == 0) return hipSuccess;
   if (!a.q || !a.lengths || !a.out || (a.capacity > 0 && (!a.cache || !a.table)) || a.dim == 0 || a.dim > a.padded || a.kv_heads == 0 || a.heads % a.kv_heads != 0 ||
       a.rows.d == 0 || a.workgroups == 0 || (a.split && (!a.parts || !a.tickets || a.least == 0 || a.chunks == 0 || a.chunks > kPagedChunks)) || a.tile != (a.dtype == kF32 ? 64u : 128u) ||
-      a.blocks_of > (a.padded > 128u ? 16u : 32u) ||
+      (a.blocks_of != 16u && (a.blocks_of != 32u || a.padded > 64u || a.dtype == kF32)) ||
       (a.split && a.seqs > kPagedFind && a.listed != (a.workgroups + a.pairs - 1u) / a.pairs))
     return hipErrorInvalidValue;
   const int64_t size = a.dtype == kF32 ? 4 : 2;

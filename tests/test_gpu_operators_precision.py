@@ -61,11 +61,14 @@ def test_weights_are_not_rounded_to_the_cache_s_type(heads, kv, rows, dim, dtype
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-def test_weights_of_many_heads_a_key_head_are_not_rounded(dtype):
+@pytest.mark.parametrize("rows,dim", [(16, 64), (16, 32), (5, 64), (8, 24), (16, 20), (3, 50), (16, 5), (7, 3), (16, 128), (16, 96)])
+@pytest.mark.parametrize("wide", [False, True])
+def test_weights_of_many_heads_a_key_head_are_not_rounded(wide, rows, dim, dtype):
+    """with a table for long sequences two blocks of 16 heads are taken at once"""
     rg = np.random.default_rng(1)
-    lens = [int(n) for n in rg.integers(1, 90, 70)]
-    cache, table = paged_case(rg, lens, 1, 16, 64, dtype)
-    q = data(rg, (len(lens), 24, 64), dtype)
+    lens = [int(n) for n in rg.integers(0, 90, 70)] + [700]
+    cache, table = paged_case(rg, lens, 1, rows, dim, dtype, slots=8000 // rows if wide else None, fill=np.nan)
+    q = data(rg, (len(lens), 24, dim), dtype)
     check(attend(cache, table, lens, q, dtype), cache, table, lens, q, dtype)
 
 
