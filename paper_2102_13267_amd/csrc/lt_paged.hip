@@ -21,7 +21,7 @@ constexpr float kLog2e = 1.44269504088896340736f;
 // ---- new rows ------------------------------------------------------------------------------------
 // Bound by memory for prompts, by latency for single tokens: a workgroup has all rows (keys and values, head by head) of a few tokens
 // on their way while it finds out where these go and computes their turns.  8 prompts of up to 2048 tokens, 8 key heads of 128 bf16,
-// 49 MB: 11.6 us, 4.2 TB/s (one thread a pair, each with a search and a turn of its own, 42); 64 single tokens 4.3 us on the device, less
+// 49 MB: 11.7 us, 4.2 TB/s (one thread a pair, each with a search and a turn of its own, 42); 64 single tokens 4.3 us on the device, less
 // than a call costs the host.
 typedef uint32_t WordsAny __attribute__((ext_vector_type(4), aligned(2)));   // wherever a window of caches begins
 __global__ __launch_bounds__(kBlock) void lt_cache_copy_kernel(const AppendArgs a) {
@@ -268,8 +268,8 @@ hipError_t launch_append(const void* args, hipStream_t s) {
 // who comes when.
 //
 // 32 query heads, 8 key heads of 128 bf16: one sequence of 131072 keys, 537 MB, 86 us, 6.2 TB/s; 60 sequences of 256 to 4096 74 us, 4.7 TB/s
-// (workgroups whose waves happen to run late hold up the end, 15 to 20 us of it); one of 300 7.3 us, of which the chain length, page, keys,
-// softmax, join takes most.  fp32, 7 sequences of up to 3001, 4 key heads of 80: 12.9 us.  One workgroup per sequence and query head: 63749, 2070, 70 and 805.
+// (workgroups whose waves happen to run late hold up the end, 15 to 20 us of it); one of 300 7.5 us, of which the chain length, page, keys,
+// softmax, join takes most.  fp32, 7 sequences of up to 3001, 4 key heads of 80: 13.0 us.  One workgroup per sequence and query head: 63749, 2070, 70 and 805.
 template <typename T, int DP, int NH> struct Geo {
   static constexpr bool BF = sizeof(T) == 2;
   static constexpr int KT = BF ? 2 : 1;              // tiles of 16 keys in a wave's step

@@ -2,7 +2,7 @@
 // position and the pair's frequency give, and the rest as it is; the gradient turns back.
 //
 // Bound by memory: every element is read and written once.  16 bytes a lane where rows allow, up to four rows of a thread on
-// their way while the workgroup computes its tokens' turns (lt_rotary.h).  65536 tokens of 32 x 128 bf16: 172 us, 6.2 TB/s (one thread
+// their way while the workgroup computes its tokens' turns (lt_rotary.h).  65536 tokens of 32 x 128 bf16: 174 us, 6.2 TB/s (one thread
 // a pair, each with a turn of its own, 550).
 //
 // Past the last-level cache (256 MB) goes what does not fit it: reads where operand and result together are larger, two rows a
