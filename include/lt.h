@@ -114,8 +114,8 @@ typedef enum {
  * Operands that are not tensors of their own.  x, q, k and v are read where they lie if they are windows of heads or of the first axis, or broadcast along any
  * axis but the last; caches, lengths, tables, positions and offsets if they are windows along the first axis (also reshaped, as one layer of [layers, pages, 2,
  * ...]).  Other windows and permutations are copied first (heads are best told apart by a reshape before the windows), and so are broadcast lengths,
- * tables, positions and offsets.  LT_ERR_UNSUPPORTED at the barrier: a host scalar's broadcast, a broadcast along the last of several axes or of a
- * cache, and a broadcast x whose axes before `heads` take more than two strides.
+ * tables, positions and offsets, and an x whose axes before `heads` take more than two strides (four at most for the whole of it).  LT_ERR_UNSUPPORTED
+ * at the barrier: a host scalar's broadcast, a broadcast along the last of several axes, and one of a cache.
  * Rows are written in place where an assigned cache is a tensor of its own (one layer of a larger tensor, which the trace does not read otherwise:
  * lt_tensor_from_device at its address; a window of it would be copied), and by the last append to it in a trace (those before it copy the cache: a barrier
  * between them does not).

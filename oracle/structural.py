@@ -763,13 +763,31 @@ class Tracer:
             return (n.op == EXPAND and n.dtype == S32 and not is_imm((i, 0)) and numel(frm) != numel(n.shape)
                     and any(nd[u].op == RESHAPE or (not along_last and reads_dense(i, u)) for u in pre_users[i]))
 
+        def spread_out(i):
+            # a broadcast of heads whose axes before `heads` take more than two strides, for the operators that read it (also as a window)
+            n = nd[i]
+            if n.op != EXPAND or len(n.shape) < 5 or is_imm((i, 0)):
+                return False
+            by = [(i, u) for u in pre_users[i]] + [(u, w) for u in pre_users[i] if nd[u].op == NARROW and not is_root[u] for w in pre_users[u]]
+            if not any(nd[u].op in OPERATORS and not reads_dense(j, u) for j, u in by):
+                return False
+            still, j = [False] * len(n.shape), i
+            while nd[j].op == EXPAND and (j == i or cls[j] == VIEW):
+                frm, to = oshape(rins[j][0]), nd[j].shape
+                frm = (1,) * (len(to) - len(frm)) + tuple(frm)
+                for d in range(1, len(to) + 1):
+                    still[-d] = still[-d] or (to[-d] > 1 and frm[-d] == 1)
+                j = rins[j][0][0]
+            lead = [still[d] for d in range(len(n.shape) - 2) if n.shape[d] > 1]
+            return sum(1 for d, s in enumerate(lead) if d == 0 or s != lead[d - 1]) > 2
+
         def klass(i):
             n = nd[i]
             if n.op in (DEVICE_DATA, SCALAR_PARAM, CONSTANT):
                 return LEAF
             if n.op in (EXPAND, RESHAPE):
                 # a view that must itself be materialised (it is a root) is a copy
-                return EW if is_root[i] or written_out(i) else VIEW
+                return EW if is_root[i] or written_out(i) or spread_out(i) else VIEW
             if n.op == PERMUTE:
                 # a permutation that only feeds contractions is addressing (operand strides), not a copy
                 return VIEW if (not is_root[i] and pre_users[i] and all(nd[u].op == MATMUL for u in pre_users[i])) else EW

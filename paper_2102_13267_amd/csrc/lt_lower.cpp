@@ -161,6 +161,35 @@ struct Lowering {
     return false;
   }
 
+  // a broadcast of heads whose axes before `heads` take more than two strides is written out for the operators that read it, also as a window
+  bool spread_out(int32_t i) const {
+    const Node* n = nd[i];
+    if (n->op != LT_OP_EXPAND || n->rank < 5 || is_imm(Val{i, 0})) return false;
+    bool reads = false;
+    for (int32_t u : users[i]) {
+      reads = reads || (is_operator(nd[u]->op) && !dense_reader(i, u));
+      if (nd[u]->op != LT_OP_NARROW || is_root[u]) continue;
+      for (int32_t w : users[u]) reads = reads || (is_operator(nd[w]->op) && !dense_reader(u, w));
+    }
+    if (!reads) return false;
+    // which axes are broadcast, by this expand or one below it
+    std::vector<char> still(n->rank, 0);
+    for (Val v{i, 0}; cls[v.node] == C_VIEW || v.node == i; v = rins[v.node][0]) {
+      if (nd[v.node]->op != LT_OP_EXPAND) break;
+      const std::vector<int64_t> from = out_shape(rins[v.node][0]), to = shape_of(v.node);
+      const size_t off = n->rank - to.size(), more = to.size() - from.size();
+      for (size_t d = 0; d < to.size(); ++d)
+        if (to[d] > 1 && (d < more || from[d - more] == 1)) still[off + d] = 1;
+    }
+    int runs = 0, last = -1;
+    for (int d = 0; d + 2 < n->rank; ++d) {
+      if (n->dims[d] <= 1) continue;
+      runs += still[d] != last;
+      last = still[d];
+    }
+    return runs > 2;
+  }
+
   // value of a node known at lowering time (constants 0 / 1, seen through views)
   bool const_of(Val v, double* out, const std::vector<std::vector<Val>>& ins) const {
     v = res(v);
@@ -246,7 +275,7 @@ struct Lowering {
       if (!live[i]) continue;
       const uint16_t op = nd[i]->op;
       if (op == OP_DEVICE_DATA || op == OP_SCALAR_PARAM || op == OP_CONSTANT) cls[i] = C_LEAF;
-      else if (op == LT_OP_EXPAND || op == LT_OP_RESHAPE) cls[i] = is_root[i] || written_out(i) ? C_EW : C_VIEW;
+      else if (op == LT_OP_EXPAND || op == LT_OP_RESHAPE) cls[i] = is_root[i] || written_out(i) || spread_out(i) ? C_EW : C_VIEW;
       else if (op == LT_OP_PERMUTE) {
         // a permutation that only feeds contractions is addressing (operand strides), not a copy
         bool only_mm = !is_root[i] && !users[i].empty();
@@ -811,12 +840,21 @@ struct Lowering {
       else if (rowvec) in.mode = ltk::kRowVec;
       else if (colvec) in.mode = ltk::kColVec;
       else {
-        if (space.size() > 4) return bad(LT_ERR_UNSUPPORTED, "strided operand in an iteration space of rank > 4");
+        // (a copy has one operand: axes that one stride reaches are one)
+        std::vector<int64_t> dims = space, step = acc.stride;
+        for (size_t d = dims.size(); dims.size() > 4 && members.size() == 1 && input_vals.size() == 1 && d-- > 1;) {
+          if (dims[d - 1] != 1 && dims[d] != 1 && step[d - 1] != step[d] * dims[d]) continue;
+          if (dims[d] != 1) step[d - 1] = step[d];
+          dims[d - 1] *= dims[d];
+          dims.erase(dims.begin() + d);
+          step.erase(step.begin() + d);
+        }
+        if (dims.size() > 4) return bad(LT_ERR_UNSUPPORTED, "strided operand in an iteration space of rank > 4");
         in.mode = ltk::kStrided;
-        const int off = 4 - (int)space.size();
+        const int off = 4 - (int)dims.size();
         for (int d = 0; d < 4; ++d) {
-          p.dims[d] = d < off ? 1u : (uint32_t)space[d - off];
-          in.stride[d] = d < off ? 0 : acc.stride[d - off];
+          p.dims[d] = d < off ? 1u : (uint32_t)dims[d - off];
+          in.stride[d] = d < off ? 0 : step[d - off];
         }
       }
       // (a window that starts off a 16-byte boundary is read element by element)

@@ -22,6 +22,10 @@ def test_copies_of_integers_move_words():
     X, one, row = ctx.tensor(x), ctx.tensor(x[0, 4:5]), ctx.tensor(x[:1])
     outs = [(ctx.narrow(X, 0, 3, 20), x[3:23]), (ctx.narrow(X, 1, 1, 20), x[:, 1:21]), (ctx.narrow(X, 1, 3, 1), x[:, 3:4]), (ctx.permute(X, (1, 0)), x.T), (ctx.reshape(X, (24, 37)), x.reshape(24, 37)),
             (ctx.expand(one, (1001,)), np.repeat(x[0, 4:5], 1001)), (ctx.expand(row, (40, 24)), np.repeat(x[:1], 40, 0))]
+    big = ints(rg.integers(-2 ** 31, 2 ** 31, (2051, 2048)))
+    B = ctx.tensor(big)
+    outs += [(ctx.narrow(B, 0, 1, 2048), big[1:2049]), (ctx.narrow(B, 1, 4, 2000), big[:, 4:2004]), (ctx.reshape(B, (2048, 2051)), big.reshape(2048, 2051)),
+             (ctx.expand(ctx.tensor(big[5:6]), (999, 2048)), np.repeat(big[5:6], 999, 0))]
     for got, ref in outs:
         assert np.array_equal(ctx.fetch(got), ref)
     ctx.close()
@@ -99,6 +103,31 @@ def test_one_length_position_and_table_for_all(dtype):
             ctx.close()
         for a, b in zip(*outs):
             assert np.array_equal(a, b)
+
+
+@pytest.mark.parametrize("dtype,dim", [("bf16", 64), ("f32", 7)])
+def test_broadcasts_of_heads(dtype, dim):
+    rg = np.random.default_rng(6)
+    r, p = Rotary(dims=6), ints([3, 1, 4, 100, 5])
+    cases = [((2, 1, 5, 3, dim), (2, 4, 5, 3, dim), None), ((2, 5, 1, dim), (4, 2, 5, 3, dim), None), ((1, 2, 1, 3, dim), (4, 2, 5, 3, dim), None), ((2, 1, 5, 3, dim), (2, 4, 5, 3, dim), (3, 1, 2)),
+             ((2, 1, 1, 1, 1, dim), (2, 3, 1, 5, 2, dim), None), ((3, 1, 2, 5, 2, dim), (3, 4, 2, 5, 2, dim), (4, 1, 1))]
+    for frm, to, window in cases:
+        x = data(rg, frm, dtype)
+        outs = []
+        for own in (True, False):
+            ctx = context()
+            if own:
+                a = np.broadcast_to(x, to)
+                X = ctx.tensor(np.ascontiguousarray(a if window is None else np.take(a, range(window[1], window[1] + window[2]), axis=window[0])), dtype)
+            else:
+                X = ctx.expand(ctx.tensor(x, dtype), to)
+                X = X if window is None else ctx.narrow(X, *window)
+            y = ctx.rope(X, ctx.tensor(p), r)
+            del X
+            ctx.barrier()
+            outs.append(ctx.fetch(y))
+            ctx.close()
+        assert np.array_equal(*outs)
 
 
 def test_positions_that_all_tokens_share_in_the_tokens_shape():
