@@ -72,7 +72,12 @@ typedef enum {
   LT_OP_ROPE_GRAD,         /* (dy, positions), the same attrs -> dx                          */
   LT_OP_CACHE_APPEND,      /* (cache, k, v, lengths, table[, offsets]) -> the cache with the   */
                            /* new rows written; attrs LT_ATTR_ROPE_*: k is rotated on the way  */
-  LT_OP_PAGED_ATTENTION    /* (q, cache, lengths, table), attr LT_ATTR_SCALE                  */
+  LT_OP_PAGED_ATTENTION,   /* (q, cache, lengths, table), attr LT_ATTR_SCALE                  */
+  LT_OP_EMBEDDING,         /* (table, ids), attr LT_ATTR_SCALE: rows of a table, below         */
+  LT_OP_EMBEDDING_GRAD,    /* (dy, ids), attrs LT_ATTR_ROWS, _SCALE; or (dy, ids, base), attr LT_ATTR_SCALE: base + it */
+  LT_OP_DROPOUT,           /* (x, state[, residual]), attrs LT_ATTR_RATE, _SITE                */
+  LT_OP_LINEAR_XENT,       /* (x, w, labels) -> 2 outputs (loss, lse): cross entropy of x w^T  */
+  LT_OP_LINEAR_XENT_GRAD   /* (x, w, labels, lse, dloss) -> 2 outputs (dx, dw)                 */
 } lt_opcode;
 
 /*
@@ -125,12 +130,43 @@ typedef enum {
  * lowering (LT_ERR_UNSUPPORTED at the barrier).
  */
 
+/*
+ * The ends of a language model's step.
+ *
+ * LT_OP_EMBEDDING: table is [rows, dim], fp32 or bf16, ids int32 [...]; the result [..., dim], of the table's type, is scale * table[id],
+ * rounded once; zeros where an id is not one of the table's rows.  Default scale: 1.
+ * LT_OP_EMBEDDING_GRAD: dy is [..., dim], fp32 or bf16, ids int32 [...].  The result is base + scale * the sum of dy over the ids that
+ * name a row, [rows, dim]; without base (LT_ATTR_ROWS says how many rows) it has dy's type, with one base's, fp32 or bf16.  Sums
+ * are formed in fp32, in an order that depends on the ids alone, and rounded once.  With lt_assign to a donatable base that is a tensor of its own, only the rows
+ * that ids name are read and written, in place.
+ *
+ * LT_OP_DROPOUT: x is fp32 or bf16 [...], below 2^35 elements; state is int64 [2]: (seed, step); residual has x's type and shape.  With
+ * t = LT_ATTR_RATE * 65536 rounded to a whole number (ties to even; 0 <= rate, t <= 65535), element i of x in row-major order is kept if its 16 bits are at
+ * least t and multiplied by 65536 / (65536 - t), so that the mean stays what it was; otherwise it is 0, whatever it was.  The residual
+ * is added, and the result rounded once.  Its 16 bits are half-word i % 8, the low half of a word first, of the four words of
+ * Philox4x32-10 for the counter (i / 8, LT_ATTR_SITE, low and high word of step) and the two words of seed as key, low word first.  The same state and site give
+ * the same mask: the gradient of x is the dropout of the result's gradient (without a residual), and nothing is stored in between.  Places that
+ * share a state take a site each (0 <= site < 2^31, default 0); the next step another step in `state`, which is data: the trace stays the same.
+ *
+ * LT_OP_LINEAR_XENT: x is [..., dim] and w [rows, dim], both fp32 or both bf16, labels int32 [...].  With l = x w^T: lse = log of the
+ * sum of exp l over the rows, loss = lse - l[label]; both fp32 [...], and 0 where a label is not one of w's rows (a token that is not trained on).  The
+ * logits are formed in pieces, in fp32, and not kept.
+ * LT_OP_LINEAR_XENT_GRAD: lse is LT_OP_LINEAR_XENT's second output, dloss the losses' gradient, fp32 [...] or rank 0.  With g = (exp(l - lse) - [label]) * dloss,
+ * 0 for tokens whose label is no row: dx = g w, of x's type and shape, dw = g^T x, of w's.  g is rounded to their type before these
+ * products; sums are in fp32.  What x, lse and dloss hold for a token whose label is no row is not looked at.  A result that nothing uses is not computed.
+ *
+ * Operands that are not tensors of their own: windows along the first axis (also reshaped) are read where they lie, other windows, permutations and
+ * broadcasts are copied first.  LT_ERR_UNSUPPORTED at the barrier: a host scalar's broadcast (but for dloss), and one of integers along the last of
+ * several axes.  LT_ERR_SHAPE: 2^27 tokens, ids or rows or more; in a cross entropy no rows, no dim or one over 2^20.
+ */
+
 typedef enum {
   LT_ATTR_VALUE = 1, LT_ATTR_DTYPE = 2, LT_ATTR_AXIS = 3, LT_ATTR_EPS = 4,
   LT_ATTR_TRANS_A = 5, LT_ATTR_TRANS_B = 6, LT_ATTR_START = 7, LT_ATTR_LENGTH = 8, LT_ATTR_DIM0 = 16,
   LT_ATTR_ROPE_DIMS = 32, LT_ATTR_ROPE_INTERLEAVED = 33,   /* integers */
   LT_ATTR_ROPE_BASE = 34, LT_ATTR_ROPE_FACTOR = 35, LT_ATTR_ROPE_ORIGINAL = 36, LT_ATTR_ROPE_LOW = 37,
-  LT_ATTR_ROPE_HIGH = 38, LT_ATTR_ROPE_AMPLITUDE = 39, LT_ATTR_SCALE = 40
+  LT_ATTR_ROPE_HIGH = 38, LT_ATTR_ROPE_AMPLITUDE = 39, LT_ATTR_SCALE = 40,
+  LT_ATTR_RATE = 41, LT_ATTR_SITE = 42, LT_ATTR_ROWS = 43
 } lt_attr_key;
 
 typedef struct {
@@ -201,7 +237,7 @@ lt_status lt_scalar(lt_ctx* ctx, lt_dtype dtype, double value, lt_tensor* out);
 /*
  * Record one IR-compatible op (section 3): appends a node, runs nothing.  inputs: n_in live
  * handles; attrs: n_attr attributes; outputs: receives n_out new handles (n_out must equal the
- * op's output count: 3 for LT_OP_LAYER_NORM, else 1).  Binary ops broadcast like NumPy.
+ * op's output count: 3 for LT_OP_LAYER_NORM, 2 for LT_OP_LINEAR_XENT and _GRAD, else 1).  Binary ops broadcast like NumPy.
  */
 lt_status lt_op(lt_ctx* ctx, uint16_t opcode, const lt_tensor* inputs, int n_in,
                 const lt_attr* attrs, int n_attr, lt_tensor* outputs, int n_out);

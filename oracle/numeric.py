@@ -439,6 +439,77 @@ class Eager:
                 out[s, h] = p @ held[tab[s, pos // rows], 1, kh, pos % rows] / p.sum()
         return self._store(out, q.dtype)
 
+    # ---- the ends of a language model's step ------------------------------------
+    def embedding(self, table, ids, scale=1.0):
+        """Row by row; an id that is no row: zeros."""
+        rows = self._wide(table)
+        there = (ids.data >= 0) & (ids.data < rows.shape[0])
+        out = np.zeros(ids.data.shape + rows.shape[1:])
+        out[there] = rows[ids.data[there]] * float(np.float32(scale))
+        return self._store(out, table.dtype)
+
+    def embedding_grad(self, dy, ids, rows=None, into=None, scale=1.0):
+        dy = self._t(dy)
+        total = np.zeros((rows if into is None else into.data.shape[0],) + dy.data.shape[-1:])
+        there = (ids.data >= 0) & (ids.data < total.shape[0])
+        np.add.at(total, ids.data[there], self._wide(dy)[there])
+        total *= float(np.float32(scale))
+        return self._store(total if into is None else total + self._wide(into), dy.dtype if into is None else into.dtype)
+
+    @staticmethod
+    def random_words(counter, key):
+        """Philox4x32-10, from the paper's definition, on Python's whole numbers: counter of four words, key of two -> four words."""
+        c, k = list(counter), list(key)
+        for _ in range(10):
+            p, q = c[0] * 0xD2511F53, c[2] * 0xCD9E8D57
+            c = [(q >> 32) ^ c[1] ^ k[0], q & 0xFFFFFFFF, (p >> 32) ^ c[3] ^ k[1], p & 0xFFFFFFFF]
+            k = [(k[0] + 0x9E3779B9) & 0xFFFFFFFF, (k[1] + 0xBB67AE85) & 0xFFFFFFFF]
+        return c
+
+    @classmethod
+    def random_bits(cls, n, state, site, first=0):
+        """The 16 bits of elements first .. first + n - 1."""
+        seed, step = (int(v) & 0xFFFFFFFFFFFFFFFF for v in state)
+        out = []
+        for block in range(first // 8, (first + n + 7) // 8):
+            for w in cls.random_words((block, site, step & 0xFFFFFFFF, step >> 32), (seed & 0xFFFFFFFF, seed >> 32)):
+                out += [w & 0xFFFF, w >> 16]
+        return np.array(out[first % 8:first % 8 + n], np.int64)
+
+    def dropout(self, x, state, rate, site=0, residual=None):
+        x = self._t(x)
+        level = int(np.rint(rate * 65536.0))
+        kept = self.random_bits(x.data.size, state.data, site).reshape(x.data.shape) >= level
+        out = np.where(kept, self._wide(x) * (65536.0 / (65536 - level)), 0.0)
+        return self._store(out if residual is None else out + self._wide(residual), x.dtype)
+
+    def dropout_grad(self, dy, state, rate, site=0):
+        return self.dropout(dy, state, rate, site)
+
+    def _counted(self, x, w, labels):
+        """Logits of the tokens whose label is a row, those tokens, and their labels."""
+        there = (labels.data >= 0) & (labels.data < w.data.shape[0])
+        return self._wide(x)[there] @ self._wide(w).T, there, labels.data[there].astype(np.int64)
+
+    def linear_xent(self, x, w, labels):
+        logits, there, hit = self._counted(x, w, labels)
+        loss, lse = np.zeros(there.shape), np.zeros(there.shape)
+        if len(hit):
+            top = logits.max(axis=-1, keepdims=True)
+            lse[there] = np.log(np.exp(logits - top).sum(axis=-1)) + top[:, 0]
+            loss[there] = lse[there] - logits[np.arange(len(hit)), hit]
+        return self._store(loss, F32), self._store(lse, F32)
+
+    def linear_xent_grad(self, x, w, labels, lse, dloss):
+        x = self._t(x)
+        logits, there, hit = self._counted(x, w, labels)
+        g = np.exp(logits - self._wide(lse)[there][:, None])
+        g[np.arange(len(hit)), hit] -= 1.0
+        g *= np.broadcast_to(self._wide(self._t(dloss)), there.shape)[there][:, None]
+        dx = np.zeros(x.data.shape)
+        dx[there] = g @ self._wide(w)
+        return self._store(dx, x.dtype), self._store(g.T @ self._wide(x)[there], w.dtype)
+
     # ---- mutation, barrier, fetch -------------------------------------------
     def assign(self, dst: ETensor, src: ETensor) -> None:
         """In-place update = rebind the destination to the new value; a tensor whose memory is

@@ -47,6 +47,8 @@ SUM, AMAX, MEAN = 64, 65, 66
 SOFTMAX, SOFTMAX_GRAD, LAYER_NORM, LAYER_NORM_GRAD, XENT, XENT_GRAD = range(80, 86)
 MATMUL = 96
 ROPE, ROPE_GRAD, CACHE_APPEND, PAGED_ATTENTION = range(112, 116)
+EMBEDDING, EMBEDDING_GRAD, DROPOUT, LINEAR_XENT, LINEAR_XENT_GRAD = range(116, 121)
+TAKES_WHOLE = {EMBEDDING, EMBEDDING_GRAD, DROPOUT, LINEAR_XENT, LINEAR_XENT_GRAD}   # every operand is one tensor in memory
 
 OP_NAME = {
     DEVICE_DATA: "xla::device_data", SCALAR_PARAM: "xla::device_data", CONSTANT: "prim::Constant",
@@ -62,12 +64,14 @@ OP_NAME = {
     XENT: "aten::nll_loss_of_log_softmax", XENT_GRAD: "aten::nll_loss_of_log_softmax_backward",
     MATMUL: "aten::matmul",
     ROPE: "lt::rope", ROPE_GRAD: "lt::rope_backward", CACHE_APPEND: "lt::cache_append", PAGED_ATTENTION: "lt::paged_attention",
+    EMBEDDING: "lt::embedding", EMBEDDING_GRAD: "lt::embedding_backward", DROPOUT: "lt::dropout",
+    LINEAR_XENT: "lt::linear_cross_entropy", LINEAR_XENT_GRAD: "lt::linear_cross_entropy_backward",
 }
 
 # ---- attribute keys -----------------------------------------------------------
 A_VALUE, A_DTYPE, A_AXIS, A_EPS, A_TRANS_A, A_TRANS_B, A_START, A_LENGTH, A_DIM0 = 1, 2, 3, 4, 5, 6, 7, 8, 16
 
-A_ROPE_DIMS, A_ROPE_INTERLEAVED, A_ROPE_BASE, A_ROPE_FACTOR, A_ROPE_ORIGINAL, A_ROPE_LOW, A_ROPE_HIGH, A_ROPE_AMPLITUDE, A_SCALE = range(32, 41)
+A_ROPE_DIMS, A_ROPE_INTERLEAVED, A_ROPE_BASE, A_ROPE_FACTOR, A_ROPE_ORIGINAL, A_ROPE_LOW, A_ROPE_HIGH, A_ROPE_AMPLITUDE, A_SCALE, A_RATE, A_SITE, A_ROWS = range(32, 44)
 
 UNARY = {NEG, ABS, EXP, LOG, TANH, SQRT, RSQRT, RECIP, RELU, GELU, SQUARE, CAST, SIGMOID}
 BINARY = {ADD, SUB, MUL, DIV, MAXIMUM, MINIMUM, RELU_GRAD, GELU_GRAD}
@@ -286,6 +290,8 @@ class Tracer:
         n = self.nodes[idx]
         if n.op == LAYER_NORM and slot > 0:
             return n.shape[:-1]
+        if n.op == LINEAR_XENT_GRAD and slot == 1:
+            return self.out_shape(*n.ins[1])
         return n.shape
 
     def out_dtype(self, idx, slot):
@@ -460,6 +466,29 @@ class Tracer:
     def paged_attention(self, q, cache, lengths, table, scale=None):
         q = self._t(q)
         return self._emit(PAGED_ATTENTION, q.dtype, q.shape, [(A_SCALE, True, 1.0 / math.sqrt(q.shape[-1]) if scale is None else float(scale))], [q, cache, lengths, table])
+
+    def embedding(self, table, ids, scale=1.0):
+        return self._emit(EMBEDDING, table.dtype, ids.shape + table.shape[-1:], [(A_SCALE, True, float(scale))], [table, ids])
+
+    def embedding_grad(self, dy, ids, rows=None, into=None, scale=1.0):
+        dy = self._t(dy)
+        attrs = [(A_SCALE, True, float(scale))] + ([] if rows is None else [(A_ROWS, False, int(rows))])
+        base = [] if into is None else [self._t(into)]
+        return self._emit(EMBEDDING_GRAD, base[0].dtype if base else dy.dtype, base[0].shape if base else (rows, dy.shape[-1]), attrs, [dy, ids] + base)
+
+    def dropout(self, x, state, rate, site=0, residual=None):
+        x = self._t(x)
+        return self._emit(DROPOUT, x.dtype, x.shape, [(A_RATE, True, float(rate)), (A_SITE, False, int(site))], [x, state] + ([] if residual is None else [residual]))
+
+    def dropout_grad(self, dy, state, rate, site=0):
+        return self.dropout(dy, state, rate, site)
+
+    def linear_xent(self, x, w, labels):
+        return self._emit(LINEAR_XENT, F32, labels.shape, (), [x, w, labels], n_out=2)
+
+    def linear_xent_grad(self, x, w, labels, lse, dloss):
+        x = self._t(x)
+        return self._emit(LINEAR_XENT_GRAD, x.dtype, x.shape, (), [x, w, labels, lse, dloss], n_out=2)
 
     def assign(self, dst: STensor, src: STensor):
         """In-place update as substitution of the destination's computation."""
@@ -659,6 +688,8 @@ class Tracer:
 
         def oshape(v):
             n = nd[v[0]]
+            if n.op == LINEAR_XENT_GRAD and v[1] == 1:
+                return oshape(ins[v[0]][1])
             return n.shape[:-1] if (n.op == LAYER_NORM and v[1] > 0) else n.shape
 
         def odtype(v):
@@ -735,11 +766,11 @@ class Tracer:
             heads = {ROPE: (0,), ROPE_GRAD: (0,), CACHE_APPEND: (1, 2), PAGED_ATTENTION: (0,)}.get(nd[u].op, ())
             return bool(heads) and rank >= 3 and axis in (0, rank - 2) and all(k in heads for k, v in enumerate(rins[u]) if v[0] == i)
 
-        OPERATORS = (ROPE, ROPE_GRAD, CACHE_APPEND, PAGED_ATTENTION)
+        OPERATORS = (ROPE, ROPE_GRAD, CACHE_APPEND, PAGED_ATTENTION, *TAKES_WHOLE)
 
         def reads_dense(i, u):
             # operator u reads node i as one tensor in memory: lengths, tables, positions, a cache
-            heads = {CACHE_APPEND: (1, 2)}.get(nd[u].op, (0,))
+            heads = () if nd[u].op in TAKES_WHOLE else {CACHE_APPEND: (1, 2)}.get(nd[u].op, (0,))
             return nd[u].op in OPERATORS and not any(v[0] == i and k in heads for k, v in enumerate(rins[u]))
 
         def first_axis(i):
@@ -759,6 +790,12 @@ class Tracer:
         def written_out(i):
             # a broadcast of integers that a reshape reads, or an operator as one tensor; not of a host scalar, not along the last of several axes for an operator
             n, frm = nd[i], oshape(rins[i][0])
+            if n.op == EXPAND and n.dtype in (F32, BF16) and not is_imm((i, 0)) and numel(frm) != numel(n.shape):
+                # any broadcast that is read by an operator which takes its operands whole, also through a reshape
+                for u in pre_users[i]:
+                    by = pre_users[u] if nd[u].op == RESHAPE and not is_root[u] else [u]
+                    if any(nd[w].op in TAKES_WHOLE for w in by):
+                        return True
             along_last = len(n.shape) > 1 and tuple(frm[-1:]) != n.shape[-1:]
             return (n.op == EXPAND and n.dtype == S32 and not is_imm((i, 0)) and numel(frm) != numel(n.shape)
                     and any(nd[u].op == RESHAPE or (not along_last and reads_dense(i, u)) for u in pre_users[i]))
@@ -815,7 +852,7 @@ class Tracer:
                 return ROW
             if n.op == MATMUL:
                 return MM
-            if n.op in (ROPE, ROPE_GRAD, CACHE_APPEND, PAGED_ATTENTION):
+            if n.op in OPERATORS:
                 return OP
             raise NotImplementedError(n.op)
 
@@ -885,7 +922,7 @@ class Tracer:
                     if v not in inputs:
                         inputs.append(v)
             for m in sorted(members):
-                n_out = 3 if nd[m].op == LAYER_NORM else 1
+                n_out = {LAYER_NORM: 3, LINEAR_XENT: 2, LINEAR_XENT_GRAD: 2}.get(nd[m].op, 1)
                 for s in range(n_out):
                     ext = any(r == (m, s) for r in root_vals)
                     for u in users[m]:
@@ -1083,6 +1120,9 @@ class Tracer:
                             # new rows may go into their own cache
                             if (m == rw["anchor"] and nd[m].op == CACHE_APPEND and x in pn and x == rins[m][0]
                                     and base(rins[m][1]) not in pn and base(rins[m][2]) not in pn):
+                                continue
+                            # a lookup's gradient may join its own base
+                            if (m == rw["anchor"] and nd[m].op == EMBEDDING_GRAD and len(rins[m]) == 3 and x in pn and x == rins[m][2] and base(rins[m][0]) not in pn):
                                 continue
                             if m == rw["anchor"] or x not in pn or nd[m].shape != nd[x[0]].shape or nd[m].op in (PERMUTE, EXPAND, RESHAPE, NARROW):
                                 ok = False

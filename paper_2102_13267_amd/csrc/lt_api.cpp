@@ -53,6 +53,9 @@ const char* op_name(uint16_t op) {
     case LT_OP_MATMUL: return "aten::matmul";
     case LT_OP_ROPE: return "lt::rope"; case LT_OP_ROPE_GRAD: return "lt::rope_backward";
     case LT_OP_CACHE_APPEND: return "lt::cache_append"; case LT_OP_PAGED_ATTENTION: return "lt::paged_attention";
+    case LT_OP_EMBEDDING: return "lt::embedding"; case LT_OP_EMBEDDING_GRAD: return "lt::embedding_backward";
+    case LT_OP_DROPOUT: return "lt::dropout";
+    case LT_OP_LINEAR_XENT: return "lt::linear_cross_entropy"; case LT_OP_LINEAR_XENT_GRAD: return "lt::linear_cross_entropy_backward";
     default: return "?";
   }
 }
@@ -340,6 +343,41 @@ static lt_status check_paged(lt_ctx* ctx, const std::string& op, const Handle* c
   auto over = [&](int64_t a, int64_t b) { return a > most || b > most || a * b > most; };
   if (over(cache->dims[0], cache->dims[3]) || over(table->dims[1], cache->dims[3]) || over(2 * cache->dims[2], cache->dims[4]) || lengths->dims[0] > most)
     return fail(ctx, LT_ERR_SHAPE, op + ": pages * rows, slots * rows, 2 * key heads * dim and sequences must be below 2^31");
+  return LT_OK;
+}
+
+// LT_ATTR_SCALE of a lookup or its gradient, which computes in fp32.
+static lt_status lookup_scale(lt_ctx* ctx, const std::string& op, const lt_attr* attrs, int n_attr, Node* n) {
+  const lt_attr* sc = find_attr(attrs, n_attr, LT_ATTR_SCALE);
+  const double scale = sc ? (sc->is_float ? sc->v.f : (double)sc->v.i) : 1.0;
+  if (!std::isfinite(scale) || !std::isfinite((float)scale)) return fail(ctx, LT_ERR_ARG, op + ": LT_ATTR_SCALE must be finite in fp32");
+  push_attr(n, LT_ATTR_SCALE, true, 0, scale);
+  return LT_OK;
+}
+
+// x [..., dim] and one int32 for each of its rows.
+static bool token_rows(const Handle* x, const Handle* ids) {
+  return x->rank >= 2 && ids->rank == x->rank - 1 && !std::memcmp(x->dims, ids->dims, ids->rank * sizeof(int64_t));
+}
+constexpr int64_t kMostTokens = (int64_t)1 << 27;
+// Whether so many elements are fewer than `limit`.
+static bool fewer(const int64_t* dims, int rank, int64_t limit) {
+  int64_t n = 1;
+  for (int i = 0; i < rank; ++i)
+    if (dims[i] == 0) return true;
+  for (int i = 0; i < rank; ++i) {
+    if (dims[i] >= limit || n * dims[i] >= limit) return false;   // (limits are below 2^36, so a product that is looked at is one of int64)
+    n *= dims[i];
+  }
+  return true;
+}
+
+// What a cross entropy over a vocabulary and its gradient ask of x, w and labels.
+static lt_status check_linear_xent(lt_ctx* ctx, const std::string& op, const Handle* x, const Handle* w, const Handle* labels) {
+  if (!is_float(x->dtype) || w->dtype != x->dtype || labels->dtype != LT_I32) return fail(ctx, LT_ERR_DTYPE, op + ": x and w must both be f32 or both bf16, labels int32");
+  if (!token_rows(x, labels) || w->rank != 2 || w->dims[1] != x->dims[x->rank - 1]) return fail(ctx, LT_ERR_SHAPE, op + ": x must be [..., dim], w [rows, dim], labels x.shape[:-1]");
+  if (w->dims[0] < 1 || w->dims[1] < 1 || w->dims[1] > ((int64_t)1 << 20) || w->dims[0] >= kMostTokens || !fewer(labels->dims, labels->rank, kMostTokens))
+    return fail(ctx, LT_ERR_SHAPE, op + ": there must be 1 to 2^20 of dim, rows from 1 and tokens below 2^27");
   return LT_OK;
 }
 
@@ -746,6 +784,72 @@ static lt_status record_op(lt_ctx* ctx, uint16_t opcode, const lt_tensor* inputs
       n.dtype = a->dtype;
       set_shape(a->dims, a->rank);
     } break;
+    case LT_OP_EMBEDDING: {
+      if (!need(2)) return fail(ctx, LT_ERR_ARG, "embedding takes (table, ids)");
+      const Handle* ids = in[1];
+      if (!is_float(a->dtype) || ids->dtype != LT_I32) return fail(ctx, LT_ERR_DTYPE, "embedding: table must be f32 or bf16, ids int32");
+      if (a->rank != 2 || ids->rank < 1 || ids->rank >= LT_MAX_RANK) return fail(ctx, LT_ERR_SHAPE, "embedding: table must be [rows, dim], ids of 1 to 5 axes");
+      if (a->dims[0] >= kMostTokens || a->dims[1] >= kMostTokens || !fewer(ids->dims, ids->rank, kMostTokens)) return fail(ctx, LT_ERR_SHAPE, "embedding: rows, dim and ids must be below 2^27");
+      const lt_status st = lookup_scale(ctx, "embedding", attrs, n_attr, &n);
+      if (st != LT_OK) return st;
+      n.dtype = a->dtype;
+      set_shape(ids->dims, ids->rank);
+      n.dims[n.rank++] = a->dims[1];
+    } break;
+    case LT_OP_EMBEDDING_GRAD: {
+      if (!need(2) && !need(3)) return fail(ctx, LT_ERR_ARG, "embedding_grad takes (dy, ids[, base])");
+      const Handle* base = n_in == 3 ? in[2] : nullptr;
+      if (!is_float(a->dtype) || in[1]->dtype != LT_I32 || (base && !is_float(base->dtype))) return fail(ctx, LT_ERR_DTYPE, "embedding_grad: dy and base must be f32 or bf16, ids int32");
+      if (!token_rows(a, in[1])) return fail(ctx, LT_ERR_SHAPE, "embedding_grad: dy must be [..., dim], ids dy.shape[:-1]");
+      const int64_t dim = a->dims[a->rank - 1];
+      const lt_attr* rows = find_attr(attrs, n_attr, LT_ATTR_ROWS);
+      if (base ? rows != nullptr : !rows || rows->is_float || rows->v.i < 0) return fail(ctx, LT_ERR_ARG, "embedding_grad: LT_ATTR_ROWS is the number of rows where there is no base, and only there");
+      if (base && (base->rank != 2 || base->dims[1] != dim)) return fail(ctx, LT_ERR_SHAPE, "embedding_grad: base must be [rows, dim]");
+      const int64_t count = base ? base->dims[0] : rows->v.i;
+      if (count >= kMostTokens || dim >= kMostTokens || !fewer(in[1]->dims, in[1]->rank, kMostTokens)) return fail(ctx, LT_ERR_SHAPE, "embedding_grad: rows, dim and ids must be below 2^27");
+      const lt_status st = lookup_scale(ctx, "embedding_grad", attrs, n_attr, &n);
+      if (st != LT_OK) return st;
+      if (!base) push_attr(&n, LT_ATTR_ROWS, false, count, 0);
+      n.dtype = base ? base->dtype : a->dtype;
+      const int64_t dims[2] = {count, dim};
+      set_shape(dims, 2);
+    } break;
+    case LT_OP_DROPOUT: {
+      if (!need(2) && !need(3)) return fail(ctx, LT_ERR_ARG, "dropout takes (x, state[, residual])");
+      const Handle *state = in[1], *res = n_in == 3 ? in[2] : nullptr;
+      if (!is_float(a->dtype) || state->dtype != LT_I64 || (res && res->dtype != a->dtype)) return fail(ctx, LT_ERR_DTYPE, "dropout: x must be f32 or bf16, state int64, residual of x's type");
+      if (a->rank < 1 || state->rank != 1 || state->dims[0] != 2) return fail(ctx, LT_ERR_SHAPE, "dropout: x must have an axis, state must be [2]");
+      if (res && (res->rank != a->rank || std::memcmp(res->dims, a->dims, a->rank * sizeof(int64_t)))) return fail(ctx, LT_ERR_SHAPE, "dropout: residual must have x's shape");
+      if (!fewer(a->dims, a->rank, (int64_t)1 << 35)) return fail(ctx, LT_ERR_SHAPE, "dropout: x must have less than 2^35 elements");
+      const lt_attr *ra = find_attr(attrs, n_attr, LT_ATTR_RATE), *si = find_attr(attrs, n_attr, LT_ATTR_SITE);
+      const double rate = ra ? (ra->is_float ? ra->v.f : (double)ra->v.i) : -1.0;
+      if (!(rate >= 0.0 && std::nearbyint(rate * 65536.0) <= 65535.0)) return fail(ctx, LT_ERR_ARG, "dropout: LT_ATTR_RATE must be at least 0 and, rounded to 16 bits, below 1");
+      if (si && (si->is_float || si->v.i < 0 || si->v.i >= ((int64_t)1 << 31))) return fail(ctx, LT_ERR_ARG, "dropout: LT_ATTR_SITE must be from 0 to 2^31 - 1");
+      push_attr(&n, LT_ATTR_RATE, true, 0, rate == 0.0 ? 0.0 : rate);   // (one zero)
+      push_attr(&n, LT_ATTR_SITE, false, si ? si->v.i : 0, 0);
+      n.dtype = a->dtype;
+      set_shape(a->dims, a->rank);
+    } break;
+    case LT_OP_LINEAR_XENT: {
+      if (!need(3)) return fail(ctx, LT_ERR_ARG, "linear_xent takes (x, w, labels)");
+      const lt_status st = check_linear_xent(ctx, "linear_xent", a, in[1], in[2]);
+      if (st != LT_OK) return st;
+      n.dtype = LT_F32;
+      set_shape(in[2]->dims, in[2]->rank);
+      n.n_out = 2;
+    } break;
+    case LT_OP_LINEAR_XENT_GRAD: {
+      if (!need(5)) return fail(ctx, LT_ERR_ARG, "linear_xent_grad takes (x, w, labels, lse, dloss)");
+      const lt_status st = check_linear_xent(ctx, "linear_xent_grad", a, in[1], in[2]);
+      if (st != LT_OK) return st;
+      const Handle *lse = in[3], *dl = in[4];
+      if (lse->dtype != LT_F32 || dl->dtype != LT_F32) return fail(ctx, LT_ERR_DTYPE, "linear_xent_grad: lse and dloss must be f32");
+      auto per_token = [&](const Handle* h) { return h->rank == in[2]->rank && !std::memcmp(h->dims, in[2]->dims, h->rank * sizeof(int64_t)); };
+      if (!per_token(lse) || !(dl->rank == 0 || per_token(dl))) return fail(ctx, LT_ERR_SHAPE, "linear_xent_grad: lse must be x.shape[:-1], dloss too or rank 0");
+      n.dtype = a->dtype;
+      set_shape(a->dims, a->rank);
+      n.n_out = 2;
+    } break;
     default:
       if (ctx->fallback && opcode >= LT_OP_CUSTOM) return run_fallback(ctx, opcode, inputs, n_in, attrs, n_attr, outputs, n_out, nullptr);
       return fail(ctx, LT_ERR_UNSUPPORTED, "lt_op: opcode " + std::to_string(opcode) + " has no lowering");
@@ -771,6 +875,10 @@ static lt_status record_op(lt_ctx* ctx, uint16_t opcode, const lt_tensor* inputs
       h->rank = nn.rank;
     }
     for (int i = 0; i < h->rank; ++i) h->dims[i] = nn.dims[i];
+    if (nn.op == LT_OP_LINEAR_XENT_GRAD && s == 1) {   // (dw: w's type and shape)
+      h->rank = in[1]->rank;
+      for (int i = 0; i < h->rank; ++i) h->dims[i] = in[1]->dims[i];
+    }
     outputs[s] = h->id;
   }
   return LT_OK;
@@ -1063,7 +1171,7 @@ lt_status lt_dump_schedule(lt_ctx* ctx, char* buf, size_t cap, size_t* len) {
   if (!ctx) return LT_ERR_ARG;
   std::string s;
   if (ctx->last_plan) {
-    static const char* const kinds[] = {"EW", "ROW", "ALL", "COL", "ROWOP", "MM", "SPLITPOST", "SLICE", "ATTN", "ROPE", "APPEND", "PAGED"};
+    static const char* const kinds[] = {"EW", "ROW", "ALL", "COL", "ROWOP", "MM", "SPLITPOST", "SLICE", "ATTN", "ROPE", "APPEND", "PAGED", "EMBED", "EMBEDGRAD", "DROPOUT", "VOCAB"};
     static_assert(sizeof(kinds) / sizeof(kinds[0]) == kLaunchKinds, "a name per kind of launch");
     const Plan& p = *ctx->last_plan;
     for (size_t i = 0; i < p.launches.size(); ++i) {

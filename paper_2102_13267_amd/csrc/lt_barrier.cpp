@@ -181,6 +181,10 @@ static hipError_t launch_one(const Launch& l, const uint8_t* args, hipStream_t s
     case L_ROPE: return ltk::launch_operator(ltk::kOpRope, args, s);
     case L_APPEND: return ltk::launch_operator(ltk::kOpCacheAppend, args, s);
     case L_PAGED: return ltk::launch_operator(ltk::kOpPagedAttention, args, s);
+    case L_EMBED: return ltk::launch_operator(ltk::kOpEmbedding, args, s);
+    case L_EMBEDGRAD: return ltk::launch_operator(ltk::kOpEmbeddingGrad, args, s);
+    case L_DROPOUT: return ltk::launch_operator(ltk::kOpDropout, args, s);
+    case L_VOCAB: return ltk::launch_operator(ltk::kOpVocab, args, s);
   }
   return hipErrorInvalidValue;
 }
@@ -199,6 +203,10 @@ static const char* kind_name(LaunchKind k) {
     case L_ROPE: return "lt_rope_kernel";
     case L_APPEND: return "lt_cache_append_kernel";
     case L_PAGED: return "lt_paged_attention_kernel";
+    case L_EMBED: return "lt_embedding_kernel";
+    case L_EMBEDGRAD: return "lt_embedding_grad_kernel";
+    case L_DROPOUT: return "lt_dropout_kernel";
+    case L_VOCAB: return "lt_vocab_kernel";
   }
   return "?";
 }

@@ -112,8 +112,8 @@ struct Handle {
 
 // ---- a lowered, cached program ------------------------------------------------------------
 
-enum LaunchKind : uint8_t { L_EW, L_ROW, L_ALL, L_COL, L_ROWOP, L_GEMM, L_SPLITPOST, L_SLICE, L_ATTN, L_ROPE, L_APPEND, L_PAGED };
-constexpr size_t kLaunchKinds = L_PAGED + 1;
+enum LaunchKind : uint8_t { L_EW, L_ROW, L_ALL, L_COL, L_ROWOP, L_GEMM, L_SPLITPOST, L_SLICE, L_ATTN, L_ROPE, L_APPEND, L_PAGED, L_EMBED, L_EMBEDGRAD, L_DROPOUT, L_VOCAB };
+constexpr size_t kLaunchKinds = L_VOCAB + 1;
 
 struct Storage {
   int param = -1;        // >= 0: the buffer of device parameter `param` (input, or donated output)

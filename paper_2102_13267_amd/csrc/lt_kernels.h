@@ -410,10 +410,108 @@ struct PagedArgs {
   uint64_t parts_bytes() const { return (uint64_t)pieces * part_floats() * sizeof(float) + 16u * (uint64_t)listed; }
 };
 
+// ---- table lookup by token, and its gradient ---------------------------------------------------------
+// out[t] = scale * table[ids[t]], zeros where that is no row.
+struct EmbedArgs {
+  const void* table;
+  const int32_t* ids;
+  void* out;
+  uint32_t dtype, tokens, rows, dim;
+  float scale;
+};
+
+// The gradient: base + scale * the sums of dy's rows by id.  Its tokens are sorted by id (stable, so that sums have an order of their own):
+// kEmbedCount and kEmbedMove, a pair for each digit of the ids; kEmbedSum adds up the rows of pieces of `piece` sorted tokens, writes
+// what a piece holds all of, and every row that no id names; kEmbedJoin adds up what more than one piece has of a row.
+enum : uint32_t { kEmbedCount = 0, kEmbedMove, kEmbedSum, kEmbedJoin };
+constexpr uint32_t kEmbedBlock = 1024;     // threads of a sorting workgroup
+constexpr uint32_t kEmbedBlocks = 64;      // sorting workgroups at most
+constexpr uint32_t kEmbedMaxBits = 10;     // of a digit
+struct EmbedGradArgs {
+  const void* dy;
+  const int32_t* ids;
+  const void* base;          // null: none, or it is in `out` already (in_place)
+  void* out;
+  uint32_t *key, *pos;       // sorted so far: ids (rows where one names no row) and tokens; null in the first pass: ids, 0 1 2 ...
+  uint32_t *key_to, *pos_to;
+  uint32_t* counts;          // [digit][workgroup]
+  uint32_t* named;           // a bit for every row that an id names
+  float* parts;              // [piece][2][dim]: a piece's sums of the row that it shares with the piece before, and of the one that it begins and shares with the next
+  uint32_t pass, dtype, out_dtype, base_dtype, in_place;
+  uint32_t tokens, rows, dim, shift, bits, blocks, each, piece, pieces;   // each: tokens of a sorting workgroup
+  float scale;
+  // how the sort is shared out
+  void share_out() {
+    const uint32_t need = tokens / (4u * kEmbedBlock) + 1u;
+    blocks = need < kEmbedBlocks ? need : kEmbedBlocks;
+    const uint32_t rounds = (tokens + blocks * kEmbedBlock - 1u) / (blocks * kEmbedBlock);
+    each = rounds * kEmbedBlock;
+    piece = 32u;
+    while ((uint64_t)piece * 4096u < tokens) piece *= 2u;
+    pieces = (tokens + piece - 1u) / piece;
+  }
+  // digits of ids 0 .. rows (rows: no row)
+  uint32_t key_bits() const {
+    uint32_t b = 1u;
+    while (b < 31u && (1u << b) <= rows) ++b;
+    return b;
+  }
+};
+
+// ---- dropout ---------------------------------------------------------------------------------------------
+// out = (16 random bits of an element >= level ? x * scale : 0) + residual (null: none).
+struct DropoutArgs {
+  const void* x;
+  const void* residual;
+  const int64_t* state;      // seed, step
+  void* out;
+  uint64_t n;
+  uint32_t dtype, level, site;
+  float scale;
+};
+
+// ---- cross entropy of x w^T over the rows of w --------------------------------------------------------------
+// Tokens whose label is a row of w are packed first (kVocabTokens: where each goes, kVocabPack: their rows of x, padded with zeros
+// to whole slabs of 128 bytes); the products then run over those alone, as many as the device has counted.
+// Logits of a piece of the vocabulary are formed as [row of w][token]: kVocabLogits leaves every token's maximum and sum of exponentials of a
+// tile of rows, kVocabLoss joins them; kVocabGrad writes g of a piece, [token][row of the piece], from which kVocabDx adds the piece's
+// share of dx to sums in fp32 (of which kVocabDxOut makes dx) and kVocabDw makes the piece's rows of dw.
+enum : uint32_t { kVocabTokens = 0, kVocabPack, kVocabLogits, kVocabLoss, kVocabGrad, kVocabDx, kVocabDw, kVocabDxOut };
+struct VocabArgs {
+  uint32_t pass, dtype;
+  uint32_t tokens, padded;     // padded: to whole tiles of 256
+  uint32_t vocab, dim, width;  // width: dim padded to whole slabs, the stride of packed rows
+  uint32_t first, rows;        // this piece of w: its first row, and how many
+  uint32_t stride;             // of g: the rows of the largest piece, padded to whole tiles of 256
+  uint32_t tile;               // rows (and tokens) of a tile of kVocabLogits: 128 or 256
+  uint32_t tiles_all;          // of kVocabLogits, over all pieces
+  uint32_t splits;             // of kVocabDx: workgroups that share a tile, each with sums of its own
+  uint32_t add;                // kVocabDx: not the first piece
+  uint32_t pack_w;             // kVocabPack: rows of w, not tokens' rows of x
+  uint32_t w_stride;           // of w's rows as the products read them
+  uint32_t rank0;              // dloss is one number, in dloss_value unless dloss is set
+  float dloss_value;
+  const void *x, *w;           // as they are, or packed (kVocabPack: what is packed)
+  const int32_t* labels;
+  const float *lse, *dloss;
+  // by packed token
+  uint32_t* count;             // how many there are
+  int32_t *row_of, *label;
+  float *lse_of, *dloss_of, *picked;
+  int32_t* packed_of;          // by token: its packed place, or -1
+  float* parts;                // [tile of rows][2][padded]: maxima, sums of exponentials
+  void* g;
+  float* sums;                 // [split][padded][width]
+  void* packed;                // kVocabPack's result
+  float *loss, *lse_out;
+  void *dx, *dw;
+};
+constexpr uint32_t kVocabTile = 256;
+
 // Argument blocks travel by value in the kernel argument segment, which holds 4 KiB.
 static_assert(sizeof(EwArgs) <= 4096 && sizeof(RowArgs) <= 4096 && sizeof(AllArgs) <= 4096 && sizeof(ColArgs) <= 4096 &&
                   sizeof(GemmArgs) <= 4096 && sizeof(SplitPostArgs) <= 4096 && sizeof(SliceArgs) <= 4096 &&
-                  sizeof(AttnArgs) <= 4096 && sizeof(RopeArgs) <= 4096 && sizeof(AppendArgs) <= 4096 && sizeof(PagedArgs) <= 4096,
+                  sizeof(AttnArgs) <= 4096 && sizeof(RopeArgs) <= 4096 && sizeof(AppendArgs) <= 4096 && sizeof(PagedArgs) <= 4096 && sizeof(EmbedGradArgs) <= 4096 && sizeof(VocabArgs) <= 4096,
               "a kernel's argument block must fit the kernel argument segment");
 
 }  // namespace ltk

@@ -20,7 +20,7 @@ hipError_t launch_gemm_bf16(const GemmArgs& a, hipStream_t s);   // 128 x 128 ti
 
 // Operators that nothing fuses with.  Their kernel files hand their launchers over when the library is
 // loaded, so that the host files link into a program without any of them.
-enum OperatorKernel : uint32_t { kOpRope = 0, kOpCacheAppend, kOpPagedAttention, kOperatorKernels };
+enum OperatorKernel : uint32_t { kOpRope = 0, kOpCacheAppend, kOpPagedAttention, kOpEmbedding, kOpEmbeddingGrad, kOpDropout, kOpVocab, kOperatorKernels };
 typedef hipError_t (*OperatorLauncher)(const void* args, hipStream_t s);
 bool set_operator(OperatorKernel which, OperatorLauncher launch);   // true
 hipError_t launch_operator(OperatorKernel which, const void* args, hipStream_t s);

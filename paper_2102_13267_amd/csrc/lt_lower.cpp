@@ -9,7 +9,7 @@
 // Partition rules (deterministic; an independent implementation must produce the same list):
 //   classes   LEAF (device_data, scalar, constant), VIEW (expand / reshape that is not a root),
 //             EW (elementwise, permute, root views), ROW / COL / ALL (reductions by axis; the
-//             fixed row operators are ROW), MM (matmul), OP (rotary positions and the paged cache: nothing joins them).
+//             fixed row operators are ROW), MM (matmul), OP (rotary positions, the paged cache, the ends of a language model: nothing joins them).
 //   pass 0    every live EW / ROW / COL / ALL / MM / OP node is a region of its own.
 //             Copies of integers stay by themselves.
 //   pass 1    plain reductions absorb, walking down from the anchor, every elementwise node of the
@@ -81,12 +81,15 @@ struct Lowering {
   }
 
   // ---- value helpers -----------------------------------------------------------------------
+  static int n_outputs(uint16_t op) { return op == LT_OP_LAYER_NORM ? 3 : op == LT_OP_LINEAR_XENT || op == LT_OP_LINEAR_XENT_GRAD ? 2 : 1; }
   int out_rank(Val v) const {
     const Node* n = nd[v.node];
+    if (n->op == LT_OP_LINEAR_XENT_GRAD && v.slot == 1) return 2;
     return (n->op == LT_OP_LAYER_NORM && v.slot > 0) ? n->rank - 1 : n->rank;
   }
   std::vector<int64_t> out_shape(Val v) const {
     const Node* n = nd[v.node];
+    if (n->op == LT_OP_LINEAR_XENT_GRAD && v.slot == 1) return out_shape(Val{cut.index_of[n->ins[1].node], n->ins[1].slot});   // (dw: w's)
     return std::vector<int64_t>(n->dims, n->dims + out_rank(v));
   }
   uint8_t out_dtype(Val v) const {
@@ -107,9 +110,10 @@ struct Lowering {
   static bool is_unary(uint16_t op) { return op >= LT_OP_NEG && op <= LT_OP_SIGMOID; }
   static bool is_binary(uint16_t op) { return op >= LT_OP_ADD && op <= LT_OP_GELU_GRAD; }
   static bool is_row_op(uint16_t op) { return op >= LT_OP_SOFTMAX && op <= LT_OP_XENT_GRAD; }
-  static bool is_operator(uint16_t op) { return op >= LT_OP_ROPE && op <= LT_OP_PAGED_ATTENTION; }
+  static bool is_operator(uint16_t op) { return op >= LT_OP_ROPE && op <= LT_OP_LINEAR_XENT_GRAD; }
+  static bool reads_whole(uint16_t op) { return op >= LT_OP_EMBEDDING && op <= LT_OP_LINEAR_XENT_GRAD; }   // every operand is one tensor in memory
   // operand k of an operator is [..., heads, dim], read where it lies: any strides before the last axis
-  static bool heads_operand(uint16_t op, size_t k) { return op == LT_OP_CACHE_APPEND ? k == 1 || k == 2 : k == 0; }
+  static bool heads_operand(uint16_t op, size_t k) { return !reads_whole(op) && (op == LT_OP_CACHE_APPEND ? k == 1 || k == 2 : k == 0); }
   // a window of heads or of the first axis (the queries, keys and values of one projection) that such an operand can be
   bool heads_window(int32_t i, int32_t u) const {
     const Node* n = nd[i];
@@ -150,10 +154,17 @@ struct Lowering {
     return !users[u].empty();
   }
   // a broadcast of integers that a reshape or an operator reads is written out; one of a host scalar is refused, and one along the last of several axes that
-  // an operator would read
+  // an operator would read.  So is any broadcast that an operator reads which takes its operands whole.
   bool written_out(int32_t i) const {
     const Node* n = nd[i];
     const std::vector<int64_t> from = out_shape(rins[i][0]);
+    if (n->op == LT_OP_EXPAND && n->dtype != LT_I32 && n->dtype != LT_I64 && !is_imm(Val{i, 0}) && count(from) != count(shape_of(i)))
+      for (int32_t u : users[i]) {
+        if (reads_whole(nd[u]->op)) return true;
+        if (nd[u]->op != LT_OP_RESHAPE || is_root[u]) continue;
+        for (int32_t w : users[u])
+          if (reads_whole(nd[w]->op)) return true;
+      }
     if (n->op != LT_OP_EXPAND || n->dtype != LT_I32 || is_imm(Val{i, 0}) || count(from) == count(shape_of(i))) return false;
     const bool last = n->rank > 1 && (from.empty() || from.back() != n->dims[n->rank - 1]);
     for (int32_t u : users[i])
@@ -326,7 +337,7 @@ struct Lowering {
         if (std::find(inputs->begin(), inputs->end(), v) == inputs->end()) inputs->push_back(v);
       }
     for (int32_t m : members) {
-      const int n_out = nd[m]->op == LT_OP_LAYER_NORM ? 3 : 1;
+      const int n_out = n_outputs(nd[m]->op);
       for (int s = 0; s < n_out; ++s) {
         const Val v{m, s};
         bool ext = std::find(root_vals.begin(), root_vals.end(), v) != root_vals.end();
@@ -560,6 +571,8 @@ struct Lowering {
                 if (m == rw->anchor && nd[m]->op == LT_OP_CACHE_APPEND && names_donor(x) && x == rins[m][0] && !names_donor(base(rins[m][1])) &&
                     !names_donor(base(rins[m][2])))
                   continue;
+                // ... and a lookup's gradient may join its own base ...
+                if (m == rw->anchor && nd[m]->op == LT_OP_EMBEDDING_GRAD && names_donor(x) && rins[m].size() == 3 && x == rins[m][2] && !names_donor(base(rins[m][0]))) continue;
                 // ... everything else must read the donor position by position (an operand of another
                 // shape is broadcast: x[64, 64] * b[64] summed over rows into b)
                 if (m == rw->anchor || !names_donor(x) || shape_of(m) != out_shape(x) || nd[m]->op == LT_OP_PERMUTE || nd[m]->op == LT_OP_EXPAND ||
@@ -1157,7 +1170,7 @@ struct Lowering {
     plan->n_scalars = (int)cut.scalar_nodes.size();
     // storages: every live device parameter, then every region output
     for (int32_t i = 0; i < N; ++i) {
-      storage_of[i].assign(nd[i]->op == LT_OP_LAYER_NORM ? 3 : 1, -1);
+      storage_of[i].assign(n_outputs(nd[i]->op), -1);
       if (live[i] && nd[i]->op == OP_DEVICE_DATA) {
         Storage s;
         s.param = param_ordinal[i];
@@ -1296,6 +1309,8 @@ struct Lowering {
     }
     if (r->kind == C_MM) return emit_gemm(k, r, post_m, out);
     if (r->kind == C_SLICE) return emit_slice(k, r);
+    if (r->kind == C_OP && reads_whole(an->op))
+      return an->op == LT_OP_EMBEDDING ? emit_embedding(k, a) : an->op == LT_OP_EMBEDDING_GRAD ? emit_embedding_grad(k, a) : an->op == LT_OP_DROPOUT ? emit_dropout(k, a) : emit_linear_xent(k, a);
     if (r->kind == C_OP) return an->op == LT_OP_CACHE_APPEND ? emit_append(k, a) : an->op == LT_OP_PAGED_ATTENTION ? emit_paged(k, a) : emit_rope(k, a);
     if (!plain_reduce(an->op)) return emit_row_op(k, r, out);
     // ---- plain reduction
@@ -2052,6 +2067,275 @@ struct Lowering {
     return true;
   }
 
+  // ---- the ends of a language model's step ---------------------------------------------------------------
+  // An operand that is one tensor in memory.
+  struct Whole {
+    int32_t storage = -1;
+    int64_t byte_offset = 0;
+  };
+  bool operand_whole(Val v, Whole* w) {
+    if (is_imm(v)) return bad(LT_ERR_UNSUPPORTED, "a host scalar's broadcast is no operand of a lookup, a dropout or a cross entropy over a vocabulary");
+    return operand_dense(v, &w->storage, &w->byte_offset);
+  }
+  void patch(int launch, size_t at, const Whole& w) { patch(launch, at, w.storage, w.byte_offset); }
+  int32_t temporary(uint64_t bytes) {
+    Storage s;
+    s.first_launch = -1;
+    s.bytes = (size_t)bytes;
+    plan->storages.push_back(s);
+    return (int32_t)plan->storages.size() - 1;
+  }
+  template <class T>
+  int add_launch(LaunchKind kind, int k, const T& args, uint64_t bytes, uint64_t flops = 0) {
+    Launch l = make_launch(kind, k, args);
+    l.bytes = bytes;
+    l.flops = flops;
+    plan->launches.push_back(std::move(l));
+    return (int)plan->launches.size() - 1;
+  }
+  static double real_attr(const Node* n, uint16_t key) {
+    for (int i = 0; i < n->n_attr; ++i)
+      if (n->attrs[i].key == key) return n->attrs[i].is_float ? n->attrs[i].v.f : (double)n->attrs[i].v.i;
+    return 0.0;
+  }
+
+  bool emit_embedding(int k, int32_t a) {
+    const Node* an = nd[a];
+    Whole table, ids;
+    if (!operand_whole(rins[a][0], &table) || !operand_whole(rins[a][1], &ids)) return false;
+    const std::vector<int64_t> ts = out_shape(rins[a][0]);
+    ltk::EmbedArgs args{};
+    args.dtype = an->dtype;
+    args.rows = (uint32_t)ts[0];
+    args.dim = (uint32_t)ts[1];
+    args.tokens = (uint32_t)count(out_shape(rins[a][1]));
+    args.scale = (float)real_attr(an, LT_ATTR_SCALE);
+    const int l = add_launch(L_EMBED, k, args, (uint64_t)args.tokens * (2u * args.dim * dtype_size(an->dtype) + 4u));
+    patch(l, offsetof(ltk::EmbedArgs, table), table);
+    patch(l, offsetof(ltk::EmbedArgs, ids), ids);
+    patch(l, offsetof(ltk::EmbedArgs, out), storage_of[a][0], 0, true);
+    return true;
+  }
+
+  // Sorted by id, summed, joined (lt_embedding.hip).
+  bool emit_embedding_grad(int k, int32_t a) {
+    const Node* an = nd[a];
+    Whole dy, ids, base;
+    const bool has_base = rins[a].size() == 3;
+    if (!operand_whole(rins[a][0], &dy) || !operand_whole(rins[a][1], &ids) || (has_base && !operand_whole(rins[a][2], &base))) return false;
+    const int32_t out = storage_of[a][0];
+    ltk::EmbedGradArgs args{};
+    args.dtype = out_dtype(rins[a][0]);
+    args.out_dtype = an->dtype;
+    args.base_dtype = an->dtype;
+    args.rows = (uint32_t)an->dims[0];
+    args.dim = (uint32_t)an->dims[1];
+    args.tokens = (uint32_t)count(out_shape(rins[a][1]));
+    args.scale = (float)real_attr(an, LT_ATTR_SCALE);
+    args.in_place = has_base && plan->storages[out].param >= 0 && plan->storages[out].param == plan->storages[base.storage].param && base.byte_offset == 0;
+    args.share_out();
+    const uint64_t n = args.tokens, w = dtype_size(args.dtype), ow = dtype_size(an->dtype), all = (uint64_t)args.rows * args.dim;
+    const bool some = n > 0 && all > 0;
+    const uint32_t bits = args.key_bits(), passes = (bits + ltk::kEmbedMaxBits - 1) / ltk::kEmbedMaxBits;
+    const int32_t named = some ? temporary(4 * ((uint64_t)args.rows / 32 + 1)) : -1, counts = some ? temporary(4 * ((uint64_t)args.blocks << ltk::kEmbedMaxBits)) : -1,
+                  parts = some ? temporary(8 * (uint64_t)args.pieces * args.dim) : -1;
+    int32_t from[2] = {-1, -1};
+    for (uint32_t p = 0; some && p < passes; ++p) {
+      args.shift = bits * p / passes;
+      args.bits = bits * (p + 1) / passes - args.shift;
+      const int32_t to[2] = {temporary(4 * n), temporary(4 * n)};
+      for (uint32_t pass : {ltk::kEmbedCount, ltk::kEmbedMove}) {
+        args.pass = pass;
+        const int l = add_launch(L_EMBEDGRAD, k, args, 8 * n);
+        patch(l, offsetof(ltk::EmbedGradArgs, ids), ids);
+        if (p > 0) {
+          patch(l, offsetof(ltk::EmbedGradArgs, key), from[0], 0);
+          patch(l, offsetof(ltk::EmbedGradArgs, pos), from[1], 0);
+        }
+        patch(l, offsetof(ltk::EmbedGradArgs, counts), counts, 0, pass == ltk::kEmbedCount);
+        if (p == 0) patch(l, offsetof(ltk::EmbedGradArgs, named), named, 0, true);
+        if (pass == ltk::kEmbedCount) continue;
+        patch(l, offsetof(ltk::EmbedGradArgs, key_to), to[0], 0, true);
+        patch(l, offsetof(ltk::EmbedGradArgs, pos_to), to[1], 0, true);
+      }
+      from[0] = to[0];
+      from[1] = to[1];
+    }
+    for (uint32_t pass : {ltk::kEmbedSum, ltk::kEmbedJoin}) {
+      if (pass == ltk::kEmbedJoin && args.pieces < 2) break;
+      args.pass = pass;
+      const int l = add_launch(L_EMBEDGRAD, k, args, pass == ltk::kEmbedJoin ? 4 * n : n * args.dim * w + (args.in_place ? 2 * n * args.dim : has_base ? 2 * all : all) * ow);
+      if (some) {
+        patch(l, offsetof(ltk::EmbedGradArgs, key), from[0], 0);
+        patch(l, offsetof(ltk::EmbedGradArgs, pos), from[1], 0);
+        patch(l, offsetof(ltk::EmbedGradArgs, named), named, 0);
+        patch(l, offsetof(ltk::EmbedGradArgs, parts), parts, 0, pass == ltk::kEmbedSum);
+      }
+      patch(l, offsetof(ltk::EmbedGradArgs, dy), dy);
+      if (has_base && !args.in_place) patch(l, offsetof(ltk::EmbedGradArgs, base), base);
+      patch(l, offsetof(ltk::EmbedGradArgs, out), out, 0, true);
+    }
+    return true;
+  }
+
+  bool emit_dropout(int k, int32_t a) {
+    const Node* an = nd[a];
+    Whole x, state, residual;
+    const bool more = rins[a].size() == 3;
+    if (!operand_whole(rins[a][0], &x) || !operand_whole(rins[a][1], &state) || (more && !operand_whole(rins[a][2], &residual))) return false;
+    ltk::DropoutArgs args{};
+    args.dtype = an->dtype;
+    args.n = (uint64_t)count(shape_of(a));
+    args.level = (uint32_t)std::nearbyint(real_attr(an, LT_ATTR_RATE) * 65536.0);
+    args.site = (uint32_t)real_attr(an, LT_ATTR_SITE);
+    args.scale = (float)(65536.0 / (65536.0 - args.level));
+    const int l = add_launch(L_DROPOUT, k, args, (more ? 3 : 2) * args.n * dtype_size(an->dtype));
+    patch(l, offsetof(ltk::DropoutArgs, x), x);
+    patch(l, offsetof(ltk::DropoutArgs, state), state);
+    if (more) patch(l, offsetof(ltk::DropoutArgs, residual), residual);
+    patch(l, offsetof(ltk::DropoutArgs, out), storage_of[a][0], 0, true);
+    return true;
+  }
+
+  // The cross entropy of x w^T, or its gradient (lt_vocab.hip): tokens that count are packed, the vocabulary goes by in pieces.
+  bool emit_linear_xent(int k, int32_t a) {
+    const Node* an = nd[a];
+    const bool grad = an->op == LT_OP_LINEAR_XENT_GRAD;
+    Whole x, w, labels, lse, dloss;
+    if (!operand_whole(rins[a][0], &x) || !operand_whole(rins[a][1], &w) || !operand_whole(rins[a][2], &labels) || (grad && !operand_whole(rins[a][3], &lse))) return false;
+    const std::vector<int64_t> ws = out_shape(rins[a][1]);
+    const uint8_t dt = out_dtype(rins[a][0]);
+    const uint64_t e = dtype_size(dt), slab = 128 / e;
+    ltk::VocabArgs args{};
+    args.dtype = dt;
+    args.tokens = (uint32_t)count(out_shape(rins[a][2]));
+    args.padded = (args.tokens + 255u) & ~255u;
+    args.vocab = (uint32_t)ws[0];
+    args.dim = (uint32_t)ws[1];
+    args.width = (uint32_t)((args.dim + slab - 1) / slab * slab);
+    const int32_t s_loss = grad ? -1 : storage_of[a][0], s_lse = grad ? -1 : storage_of[a][1], s_dx = grad ? storage_of[a][0] : -1, s_dw = grad ? storage_of[a][1] : -1;
+    const uint64_t n = args.tokens, pad = args.padded, width = args.width;
+    // rows of w that are no whole, aligned slabs are packed, a piece at a time
+    // (a window along the first axis may start anywhere; tensors of their own start at 16 bytes)
+    const bool pack_w = args.width != args.dim || w.byte_offset % 16 != 0;
+    args.w_stride = args.width;
+    // a piece of g takes 256 MB, as many rows as that is, but 4096 at least
+    const uint64_t fit = std::max<uint64_t>(4096, ((uint64_t)256 << 20) / (std::max<uint64_t>(pad, 256) * e) & ~(uint64_t)255);
+    const uint64_t fit_w = std::max<uint64_t>(4096, ((uint64_t)256 << 20) / (width * e) & ~(uint64_t)255);
+    uint64_t piece = args.vocab;
+    if (grad) piece = std::min(piece, fit);
+    if (pack_w) piece = std::min(piece, fit_w);
+    const uint32_t pieces = (uint32_t)((args.vocab + piece - 1) / piece);
+    args.stride = (uint32_t)((piece + 255) & ~(uint64_t)255);
+    args.tile = dt == LT_BF16 ? 256u : 128u;
+    args.tiles_all = 0;
+    // by packed token: row, label, lse, dloss, picked; their count; by token: packed place
+    const int32_t lists = temporary(4 * (5 * pad + pad + 64));
+    const int32_t packed_x = temporary(pad * width * e);
+    const int32_t packed_w = pack_w ? temporary(piece * width * e) : -1;
+    std::vector<uint32_t> first_tile;
+    for (uint32_t p = 0; p < pieces; ++p) {
+      first_tile.push_back(args.tiles_all);
+      args.tiles_all += (uint32_t)((std::min<uint64_t>(piece, args.vocab - p * piece) + args.tile - 1) / args.tile);
+    }
+    const int32_t parts = grad ? -1 : temporary(8 * (uint64_t)args.tiles_all * pad);
+    const int32_t g = grad ? temporary(pad * args.stride * e) : -1;
+    // few tiles of dx and a long sum: shared by as many workgroups as compute units are left without one, each with eight slabs at least
+    const uint64_t dx_tiles = pad / args.tile * ((args.width + args.tile - 1) / args.tile), slabs = args.stride / slab;
+    args.splits = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>({256 / std::max<uint64_t>(dx_tiles, 1), slabs / 8, 16}));
+    const int32_t sums = s_dx >= 0 ? temporary(4 * pad * width * args.splits) : -1;
+    auto list = [&](int l, size_t at, uint32_t which, bool write) { patch(l, at, lists, (int64_t)(4 * pad * which), write); };
+    auto all_lists = [&](int l, bool write) {
+      list(l, offsetof(ltk::VocabArgs, row_of), 0, write);
+      list(l, offsetof(ltk::VocabArgs, label), 1, write);
+      list(l, offsetof(ltk::VocabArgs, lse_of), 2, write);
+      list(l, offsetof(ltk::VocabArgs, dloss_of), 3, write);
+      list(l, offsetof(ltk::VocabArgs, picked), 4, write);
+      list(l, offsetof(ltk::VocabArgs, packed_of), 5, write);
+      list(l, offsetof(ltk::VocabArgs, count), 6, write);
+    };
+    auto add = [&](uint32_t pass, uint64_t bytes, uint64_t flops = 0) {
+      args.pass = pass;
+      const int l = add_launch(L_VOCAB, k, args, bytes, flops);
+      all_lists(l, pass == ltk::kVocabTokens || pass == ltk::kVocabLogits);
+      return l;
+    };
+    int l = 0;
+    if (grad) {
+      const Val d = rins[a][4];
+      args.rank0 = is_imm(d) || out_shape(d).empty();
+      if (!is_imm(d) && !operand_whole(d, &dloss)) return false;
+    }
+    l = add(ltk::kVocabTokens, 4 * n * (grad ? 4 : 2));
+    patch(l, offsetof(ltk::VocabArgs, labels), labels);
+    if (grad) {
+      patch(l, offsetof(ltk::VocabArgs, lse), lse);
+      if (dloss.storage >= 0) patch(l, offsetof(ltk::VocabArgs, dloss), dloss);
+      else patch_scalar(rins[a][4], l, offsetof(ltk::VocabArgs, dloss_value), &((ltk::VocabArgs*)plan->launches[l].args.data())->dloss_value);
+    } else {
+      if (s_loss >= 0) patch(l, offsetof(ltk::VocabArgs, loss), s_loss, 0, true);
+      if (s_lse >= 0) patch(l, offsetof(ltk::VocabArgs, lse_out), s_lse, 0, true);
+    }
+    l = add(ltk::kVocabPack, 2 * n * args.dim * e);
+    patch(l, offsetof(ltk::VocabArgs, x), x);
+    patch(l, offsetof(ltk::VocabArgs, packed), packed_x, 0, true);
+    for (uint32_t p = 0; p < pieces; ++p) {
+      args.first = (uint32_t)(p * piece);
+      args.rows = (uint32_t)std::min<uint64_t>(piece, args.vocab - args.first);
+      args.add = p > 0;
+      const uint64_t w_bytes = (uint64_t)args.rows * args.dim * e, x_bytes = n * args.dim * e, product = 2 * n * args.rows * args.dim;
+      if (pack_w) {
+        args.pack_w = 1;
+        l = add(ltk::kVocabPack, 2 * w_bytes);
+        args.pack_w = 0;
+        patch(l, offsetof(ltk::VocabArgs, w), w.storage, w.byte_offset + (int64_t)(args.first * (uint64_t)args.dim * e));
+        patch(l, offsetof(ltk::VocabArgs, packed), packed_w, 0, true);
+      }
+      auto operands = [&](int at, bool reads_x, bool reads_w) {
+        if (reads_x) patch(at, offsetof(ltk::VocabArgs, x), packed_x, 0);
+        if (reads_w && pack_w) patch(at, offsetof(ltk::VocabArgs, w), packed_w, 0);
+        else if (reads_w) patch(at, offsetof(ltk::VocabArgs, w), w.storage, w.byte_offset + (int64_t)(args.first * (uint64_t)args.dim * e));
+      };
+      l = add(grad ? ltk::kVocabGrad : ltk::kVocabLogits, w_bytes + x_bytes, product);
+      operands(l, true, true);
+      if (!grad) {
+        patch(l, offsetof(ltk::VocabArgs, parts), parts, (int64_t)(8 * pad * first_tile[p]), true);
+        continue;
+      }
+      patch(l, offsetof(ltk::VocabArgs, g), g, 0, true);
+      if (s_dx >= 0) {
+        l = add(ltk::kVocabDx, w_bytes + x_bytes, product);
+        operands(l, false, true);
+        patch(l, offsetof(ltk::VocabArgs, g), g, 0);
+        patch(l, offsetof(ltk::VocabArgs, sums), sums, 0, true);
+      }
+      if (s_dw >= 0) {
+        l = add(ltk::kVocabDw, w_bytes + x_bytes, product);
+        operands(l, true, false);
+        patch(l, offsetof(ltk::VocabArgs, g), g, 0);
+        patch(l, offsetof(ltk::VocabArgs, dw), s_dw, (int64_t)(args.first * (uint64_t)args.dim * e), true);
+      }
+    }
+    if (!grad) {
+      l = add(ltk::kVocabLoss, 8 * (uint64_t)args.tiles_all * n);
+      patch(l, offsetof(ltk::VocabArgs, parts), parts, 0);
+      if (s_loss >= 0) patch(l, offsetof(ltk::VocabArgs, loss), s_loss, 0, true);
+      if (s_lse >= 0) patch(l, offsetof(ltk::VocabArgs, lse_out), s_lse, 0, true);
+    } else if (s_dx >= 0) {
+      l = add(ltk::kVocabDxOut, n * args.dim * (e + 4));
+      patch(l, offsetof(ltk::VocabArgs, sums), sums, 0);
+      patch(l, offsetof(ltk::VocabArgs, dx), s_dx, 0, true);
+    }
+    return true;
+  }
+
+  // A rank-0 operand on the host: a constant, or a scalar that every step brings.
+  void patch_scalar(Val b, int launch, size_t at, float* value) {
+    while (nd[b.node]->op == LT_OP_EXPAND || nd[b.node]->op == LT_OP_RESHAPE) b = rins[b.node][0];
+    if (nd[b.node]->op == OP_CONSTANT) *value = (float)(nd[b.node]->attrs[0].is_float ? nd[b.node]->attrs[0].v.f : (double)nd[b.node]->attrs[0].v.i);
+    else plan->scal_patches.push_back(ScalPatch{(uint32_t)launch, (uint32_t)at, scalar_ordinal[b.node], 0});
+  }
+
   // A cross-entropy and its gradient over the same logits and labels: whichever comes second joins the launch of the
   // first (which becomes the gradient's, with the losses as its second output).  Its result is written earlier than its
   // place, so it must be memory of its own.  (What it reads is what the first one reads.)
@@ -2188,7 +2472,7 @@ struct Lowering {
     }
     // outputs: every slot of the anchor that is needed; unneeded layer-norm statistics still
     // need somewhere to go, so they get storage as well
-    const int n_out = an->op == LT_OP_LAYER_NORM ? 3 : 1;
+    const int n_out = n_outputs(an->op);
     for (int s = 0; s < n_out; ++s) {
       int32_t st = storage_of[a][s];
       if (st < 0) {

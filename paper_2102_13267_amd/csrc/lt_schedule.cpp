@@ -39,7 +39,7 @@ struct MemState {
 // microseconds, only good enough to balance streams
 double estimate_us(const Launch& l) {
   const double mem = (double)l.bytes / 3.0e6;   // 3 TB/s
-  if (l.kind == L_GEMM) return 8.0 + std::max(mem, (double)l.flops / 4.0e8);   // 400 TFLOP/s
+  if (l.kind == L_GEMM || l.kind == L_VOCAB) return 8.0 + std::max(mem, (double)l.flops / 4.0e8);   // 400 TFLOP/s
   if (l.kind == L_COL) return 12.0 + mem;       // latency bound: dependent trips, ticket, last-workgroup pass
   return 6.0 + mem;
 }

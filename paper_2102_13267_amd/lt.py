@@ -23,10 +23,11 @@ OPCODES = {
     "softmax": 80, "softmax_grad": 81, "layer_norm": 82, "layer_norm_grad": 83, "xent": 84, "xent_grad": 85,
     "matmul": 96,
     "rope": 112, "rope_grad": 113, "cache_append": 114, "paged_attention": 115,
+    "embedding": 116, "embedding_grad": 117, "dropout": 118, "linear_xent": 119, "linear_xent_grad": 120,
 }
 ATTR_VALUE, ATTR_DTYPE, ATTR_AXIS, ATTR_EPS, ATTR_TRANS_A, ATTR_TRANS_B, ATTR_START, ATTR_LENGTH, ATTR_DIM0 = 1, 2, 3, 4, 5, 6, 7, 8, 16
 ATTR_ROPE_DIMS, ATTR_ROPE_INTERLEAVED, ATTR_ROPE_BASE, ATTR_ROPE_FACTOR, ATTR_ROPE_ORIGINAL, ATTR_ROPE_LOW, ATTR_ROPE_HIGH, ATTR_ROPE_AMPLITUDE = range(32, 40)
-ATTR_SCALE = 40
+ATTR_SCALE, ATTR_RATE, ATTR_SITE, ATTR_ROWS = 40, 41, 42, 43
 LT_DONATABLE = 1
 MAX_RANK = 6
 
@@ -243,6 +244,7 @@ _CAST, _EXPAND, _RESHAPE, _PERMUTE = OPCODES["cast"], OPCODES["expand"], OPCODES
 _NARROW, _SLICE_UPDATE = OPCODES["narrow"], OPCODES["slice_update"]
 _SUM, _AMAX, _MEAN = OPCODES["sum"], OPCODES["amax"], OPCODES["mean"]
 _LAYER_NORM, _MATMUL = OPCODES["layer_norm"], OPCODES["matmul"]
+_EMBEDDING, _EMBEDDING_GRAD, _DROPOUT, _LINEAR_XENT, _LINEAR_XENT_GRAD = (OPCODES[n] for n in ("embedding", "embedding_grad", "dropout", "linear_xent", "linear_xent_grad"))
 _ROPE, _ROPE_GRAD, _CACHE_APPEND, _PAGED_ATTENTION = OPCODES["rope"], OPCODES["rope_grad"], OPCODES["cache_append"], OPCODES["paged_attention"]
 
 
@@ -455,6 +457,41 @@ class Context:
         key = (_PAGED_ATTENTION, float(scale))
         at = self._attrs.get(key) or self._encode(key, [(ATTR_SCALE, key[1])])
         return _rec_op(self, self._hv, _PAGED_ATTENTION, (q, cache, lengths, table), at[0], at[1], 1)
+
+    # the ends of a language model's step (include/lt.h has the formulas)
+    def embedding(self, table, ids, scale=1.0):
+        """scale * table[ids]: table [rows, dim], ids int32 [...] -> [..., dim]; zeros where an id is no row."""
+        key = (_EMBEDDING, float(scale))
+        at = self._attrs.get(key) or self._encode(key, [(ATTR_SCALE, key[1])])
+        return _rec_op(self, self._hv, _EMBEDDING, (table, ids), at[0], at[1], 1)
+
+    def embedding_grad(self, dy, ids, rows=None, into=None, scale=1.0):
+        """The gradient of embedding's table, [rows, dim]: scale * the sum of dy [..., dim] over the ids that name a row; added to `into` if that is
+        given instead of `rows`.  Assigned to a donatable `into`, only the rows that ids name are touched: ctx.assign(g, ctx.embedding_grad(dy, ids, into=g))."""
+        if (rows is None) == (into is None):
+            raise ValueError("embedding_grad takes rows or into")
+        key = (_EMBEDDING_GRAD, rows, float(scale))
+        at = self._attrs.get(key) or self._encode(key, [(ATTR_SCALE, key[2])] + ([] if rows is None else [(ATTR_ROWS, int(rows))]))
+        return _rec_op(self, self._hv, _EMBEDDING_GRAD, (dy, ids) if into is None else (dy, ids, into), at[0], at[1], 1)
+
+    def dropout(self, x, state, rate, site=0, residual=None):
+        """x with a share `rate` of its elements (to 16 bits) 0 and the others scaled up, plus residual.  state: int64 [2], (seed, step); places that
+        share it take a `site` each.  The mask follows from state, site and an element's place, and is not stored."""
+        key = (_DROPOUT, float(rate), int(site))
+        at = self._attrs.get(key) or self._encode(key, [(ATTR_RATE, key[1]), (ATTR_SITE, key[2])])
+        return _rec_op(self, self._hv, _DROPOUT, (x, state) if residual is None else (x, state, residual), at[0], at[1], 1)
+
+    def dropout_grad(self, dy, state, rate, site=0):
+        """The gradient of dropout's x (that of its residual is dy itself): dy under the same mask."""
+        return self.dropout(dy, state, rate, site)
+
+    def linear_xent(self, x, w, labels):
+        """(loss, lse) of the logits x w^T, without keeping them: x [..., dim], w [rows, dim], labels int32 [...]; both 0 where a label is no row."""
+        return _rec_op(self, self._hv, _LINEAR_XENT, (x, w, labels), _NO_ATTRS_ADDR, 0, 2)
+
+    def linear_xent_grad(self, x, w, labels, lse, dloss):
+        """(dx, dw) of linear_xent for the losses' gradient dloss: a number, or fp32 of rank 0 or [...]."""
+        return _rec_op(self, self._hv, _LINEAR_XENT_GRAD, (x, w, labels, lse, dloss), _NO_ATTRS_ADDR, 0, 2)
 
     def narrow(self, x, axis, start, length):
         key = (_NARROW, int(axis), int(start), int(length))
