@@ -140,7 +140,7 @@ typedef enum {
  * are formed in fp32, in an order that depends on the ids alone, and rounded once.  With lt_assign to a donatable base that is a tensor of its own, only the rows
  * that ids name are read and written, in place.
  *
- * LT_OP_DROPOUT: x is fp32 or bf16 [...], below 2^35 elements; state is int64 [2]: (seed, step); residual has x's type and shape.  With
+ * LT_OP_DROPOUT: x is fp32 or bf16 [...], at most 2^35 - 2048 elements; state is int64 [2]: (seed, step); residual has x's type and shape.  With
  * t = LT_ATTR_RATE * 65536 rounded to a whole number (ties to even; 0 <= rate, t <= 65535), element i of x in row-major order is kept if its 16 bits are at
  * least t and multiplied by 65536 / (65536 - t), so that the mean stays what it was; otherwise it is 0, whatever it was.  The residual
  * is added, and the result rounded once.  Its 16 bits are half-word i % 8, the low half of a word first, of the four words of

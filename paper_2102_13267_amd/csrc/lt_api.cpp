@@ -820,7 +820,7 @@ static lt_status record_op(lt_ctx* ctx, uint16_t opcode, const lt_tensor* inputs
       if (!is_float(a->dtype) || state->dtype != LT_I64 || (res && res->dtype != a->dtype)) return fail(ctx, LT_ERR_DTYPE, "dropout: x must be f32 or bf16, state int64, residual of x's type");
       if (a->rank < 1 || state->rank != 1 || state->dims[0] != 2) return fail(ctx, LT_ERR_SHAPE, "dropout: x must have an axis, state must be [2]");
       if (res && (res->rank != a->rank || std::memcmp(res->dims, a->dims, a->rank * sizeof(int64_t)))) return fail(ctx, LT_ERR_SHAPE, "dropout: residual must have x's shape");
-      if (!fewer(a->dims, a->rank, (int64_t)1 << 35)) return fail(ctx, LT_ERR_SHAPE, "dropout: x must have less than 2^35 elements");
+      if (!fewer(a->dims, a->rank, ((int64_t)1 << 35) - 2047)) return fail(ctx, LT_ERR_SHAPE, "dropout: x must have at most 2^35 - 2048 elements");
       const lt_attr *ra = find_attr(attrs, n_attr, LT_ATTR_RATE), *si = find_attr(attrs, n_attr, LT_ATTR_SITE);
       const double rate = ra ? (ra->is_float ? ra->v.f : (double)ra->v.i) : -1.0;
       if (!(rate >= 0.0 && std::nearbyint(rate * 65536.0) <= 65535.0)) return fail(ctx, LT_ERR_ARG, "dropout: LT_ATTR_RATE must be at least 0 and, rounded to 16 bits, below 1");

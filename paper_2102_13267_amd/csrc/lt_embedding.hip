@@ -1,29 +1,95 @@
 // Rows of a table by token, and the gradient of the table.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "lt_launch.h"
 
 namespace ltk {
 namespace {
 
 constexpr uint32_t kBlock = 256;
+constexpr uint64_t kMostGrid = (uint64_t)1 << 24;   // workgroups are below that: a launch holds less than 2^32 threads
 
-// ---- lookup: one wave an output row -------------------------------------------------------------------
+__device__ __forceinline__ uint32_t divide(uint32_t n, const Divider& by) { return (uint32_t)(((uint64_t)n * by.magic) >> 31) >> by.shift; }
+
+// V elements that are moved at once.
+template <typename T, int V>
+struct Piece {
+  typedef T Vec __attribute__((ext_vector_type(V), aligned(V * sizeof(T) < 16 ? V * sizeof(T) : 16)));
+  Vec v;
+  __device__ __forceinline__ void load(const T* p) { v = *(const Vec*)p; }
+  __device__ __forceinline__ void store(T* p) const { *(Vec*)p = v; }
+  __device__ __forceinline__ float get(int j) const { return (float)v[j]; }
+  __device__ __forceinline__ void set(int j, float x) { v[j] = (T)x; }
+};
 template <typename T>
+struct Piece<T, 1> {
+  T v;
+  __device__ __forceinline__ void load(const T* p) { v = *p; }
+  __device__ __forceinline__ void store(T* p) const { *p = v; }
+  __device__ __forceinline__ float get(int) const { return (float)v; }
+  __device__ __forceinline__ void set(int, float x) { v = (T)x; }
+};
+
+// ---- lookup: one thread a piece of an output row, two of them where there are many ---------------------------
+template <typename T, int V, int N>
 __global__ __launch_bounds__(kBlock) void lt_embedding_kernel(const EmbedArgs a) {
-  const uint32_t t = blockIdx.x * (kBlock / 64u) + threadIdx.x / 64u, lane = threadIdx.x & 63u;
-  if (t >= a.tokens) return;
-  const int32_t id = a.ids[t];
-  const bool there = id >= 0 && (uint32_t)id < a.rows;
-  const T* row = (const T*)a.table + (uint64_t)(there ? id : 0) * a.dim;
-  T* out = (T*)a.out + (uint64_t)t * a.dim;
-  for (uint32_t d = lane; d < a.dim; d += 64u) out[d] = there ? (T)((float)row[d] * a.scale) : (T)0.0f;
+  const uint32_t units = a.tokens * a.row.d, first = blockIdx.x * (kBlock * N) + threadIdx.x;
+  Piece<T, V> p[N];
+  bool there[N];
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    const uint32_t u = min(first + k * kBlock, units - 1u), t = divide(u, a.row);
+    const int32_t id = a.ids[t];
+    there[k] = (uint32_t)id < a.rows;   // (a negative one is a large number)
+    if (a.rows > 0u) p[k].load((const T*)a.table + (uint64_t)(there[k] ? id : 0) * a.dim + (u - t * a.row.d) * V);
+  }
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    const uint32_t u = first + k * kBlock;
+    if (u >= units) return;
+#pragma unroll
+    for (int j = 0; j < V; ++j) p[k].set(j, there[k] ? p[k].get(j) * a.scale : 0.0f);
+    p[k].store((T*)a.out + (uint64_t)u * V);
+  }
 }
 
+template <typename T, int V>
+hipError_t launch_pieces(EmbedArgs a, hipStream_t s) {
+  const uint64_t units = (uint64_t)a.tokens * (a.dim / V);
+  if (units >= (uint64_t)1 << 31) return hipErrorInvalidValue;
+  a.row.set(a.dim / V);
+  if (units > 1024u * 2u * kBlock) LT_LAUNCH((lt_embedding_kernel<T, V, 2>), dim3((uint32_t)((units + 2u * kBlock - 1u) / (2u * kBlock))), dim3(kBlock), s, a);
+  else LT_LAUNCH((lt_embedding_kernel<T, V, 1>), dim3((uint32_t)((units + kBlock - 1u) / kBlock)), dim3(kBlock), s, a);
+  return hipGetLastError();
+}
+
+// as many elements at once as rows, and where the tensors start, allow
+uint32_t widest(uint32_t elem, uint32_t dim, uintptr_t starts) {
+  uint32_t v = 16u / elem;
+  while (v > 1u && (dim % v != 0u || starts % (v * elem) != 0u)) v /= 2u;
+  return v;
+}
+
+// (a result of 2^31 pieces and more in parts of whole rows)
 template <typename T>
 hipError_t launch_lookup(const EmbedArgs& a, hipStream_t s) {
-  LT_LAUNCH(lt_embedding_kernel<T>, dim3((a.tokens + kBlock / 64u - 1u) / (kBlock / 64u)), dim3(kBlock), s, a);
-  return hipGetLastError();
+  const uint32_t v = widest(sizeof(T), a.dim, (uintptr_t)a.table | (uintptr_t)a.out);
+  const uint32_t most = (uint32_t)std::max<uint64_t>(1u, (((uint64_t)1 << 31) - 1u) / (a.dim / v));
+  EmbedArgs part = a;
+  for (uint32_t t = 0; t < a.tokens; t += part.tokens) {
+    part.tokens = std::min(most, a.tokens - t);
+    part.ids = a.ids + t;
+    part.out = (T*)a.out + (uint64_t)t * a.dim;
+    hipError_t e;
+    if (v == 8u) e = launch_pieces<T, 16 / sizeof(T)>(part, s);   // (eight bf16; fp32 has four at most)
+    else if (v == 4u) e = launch_pieces<T, 4>(part, s);
+    else if (v == 2u) e = launch_pieces<T, 2>(part, s);
+    else e = launch_pieces<T, 1>(part, s);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 hipError_t launch_embedding(const void* args, hipStream_t s) {
@@ -33,47 +99,42 @@ hipError_t launch_embedding(const void* args, hipStream_t s) {
 }
 
 // ---- the gradient: tokens in the order of their ids ------------------------------------------------------
-// A stable radix sort, a digit of the ids at a time, lowest first.  Workgroup b has tokens b * each to (b + 1) * each - 1 of the order
-// so far, wave w of it a contiguous share.  Count: how many of each digit.  Move: a token's place is what stands before it: smaller
-// digits anywhere, its own digit in earlier workgroups, in earlier waves of this one, and in this wave before it.
+// A stable radix sort, a digit of the ids at a time, lowest first.
 __device__ __forceinline__ uint32_t key_of(const EmbedGradArgs& a, uint32_t i) {
   if (a.key) return a.key[i];
   const int32_t id = a.ids[i];
-  return id >= 0 && (uint32_t)id < a.rows ? (uint32_t)id : a.rows;
+  return (uint32_t)id < a.rows ? (uint32_t)id : a.rows;
 }
 
 // one more in LDS (counts come out the same in any order)
 __device__ __forceinline__ void one_more(uint32_t* n) { __hip_atomic_fetch_add(n, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); }
 
-__global__ __launch_bounds__(kEmbedBlock) void lt_embedding_count_kernel(const EmbedGradArgs a) {
-  __shared__ uint32_t hist[1u << kEmbedMaxBits];
-  const uint32_t digits = 1u << a.bits;
-  for (uint32_t d = threadIdx.x; d < digits; d += kEmbedBlock) hist[d] = 0u;
-  if (a.named)   // (the first pass clears them)
-    for (uint32_t i = blockIdx.x * kEmbedBlock + threadIdx.x; i <= a.rows / 32u; i += gridDim.x * kEmbedBlock) a.named[i] = 0u;
-  __syncthreads();
-  const uint32_t begin = blockIdx.x * a.each;
-  for (uint32_t i = begin + threadIdx.x; i < begin + a.each && i < a.tokens; i += kEmbedBlock) one_more(&hist[(key_of(a, i) >> a.shift) & (digits - 1u)]);
-  __syncthreads();
-  for (uint32_t d = threadIdx.x; d < digits; d += kEmbedBlock) a.counts[d * a.blocks + blockIdx.x] = hist[d];
+// How many of a wave's tokens with this digit came before this one: those of earlier rounds, which `so_far` counts (a wave's own), and
+// those of lower lanes.
+template <uint32_t BITS>   // (a digit's, at most)
+__device__ __forceinline__ uint32_t place(uint32_t* so_far, uint32_t digit, bool there, uint32_t lane) {
+  const uint64_t all = __ballot(there);
+  uint32_t low = (uint32_t)all, high = (uint32_t)(all >> 32);   // the lanes with the same digit
+#pragma unroll
+  for (uint32_t b = 0; b < BITS; ++b) {
+    const uint64_t ones = __ballot(digit >> b & 1u);
+    const uint32_t mine = (uint32_t)((int32_t)(digit << (31u - b)) >> 31);
+    low &= ~((uint32_t)ones ^ mine);
+    high &= ~((uint32_t)(ones >> 32) ^ mine);
+  }
+  const uint64_t same = (uint64_t)high << 32 | low;
+  const uint32_t earlier = __builtin_amdgcn_mbcnt_hi(high, __builtin_amdgcn_mbcnt_lo(low, 0u));
+  const uint32_t at = there ? so_far[digit] + earlier : 0u;
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  if (there && earlier == 0u) so_far[digit] = at + (uint32_t)__popcll(same);
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  return at;
 }
 
-__global__ __launch_bounds__(kEmbedBlock) void lt_embedding_move_kernel(const EmbedGradArgs a) {
-  constexpr uint32_t kWaves = kEmbedBlock / 64u;
-  __shared__ uint32_t start[1u << kEmbedMaxBits];            // where this workgroup's tokens of a digit go
-  __shared__ uint32_t mine[kWaves][1u << kEmbedMaxBits];     // a wave's tokens of a digit, then where they go
-  __shared__ uint32_t waves[kWaves];
-  const uint32_t digits = 1u << a.bits, lane = threadIdx.x & 63u, wave = threadIdx.x / 64u;
-  for (uint32_t d = threadIdx.x; d < kWaves * digits; d += kEmbedBlock) mine[d / digits][d % digits] = 0u;
-  // digit d = this thread's (at most as many digits as threads): all of it, and what earlier workgroups have
-  uint32_t all = 0u, before = 0u;
-  if (threadIdx.x < digits)
-    for (uint32_t b = 0; b < a.blocks; ++b) {
-      const uint32_t c = a.counts[threadIdx.x * a.blocks + b];
-      all += c;
-      before += b < blockIdx.x ? c : 0u;
-    }
-  uint32_t upto = all;   // inclusive scan over the workgroup
+// The sum of what the threads before this one have.
+__device__ __forceinline__ uint32_t sum_before(uint32_t mine, uint32_t* waves) {
+  const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x / 64u;
+  uint32_t upto = mine;
 #pragma unroll
   for (uint32_t o = 1; o < 64u; o *= 2u) {
     const uint32_t v = __shfl_up(upto, o);
@@ -81,123 +142,318 @@ __global__ __launch_bounds__(kEmbedBlock) void lt_embedding_move_kernel(const Em
   }
   if (lane == 63u) waves[wave] = upto;
   __syncthreads();
-  uint32_t smaller = upto - all;
-  for (uint32_t w = 0; w < wave; ++w) smaller += waves[w];
-  if (threadIdx.x < digits) start[threadIdx.x] = smaller + before;
+  uint32_t before = upto - mine;
+#pragma unroll
+  for (uint32_t w = 0; w < kEmbedBlock / 64u; ++w) before += w < wave ? waves[w] : 0u;
+  return before;
+}
+
+// Few tokens: one workgroup, an id and its token in a word, sixteen of them a thread at most.
+__global__ __launch_bounds__(kEmbedBlock) void lt_embedding_sort_kernel(const EmbedGradArgs a) {
+  constexpr uint32_t kWaves = kEmbedBlock / 64u;
+  __shared__ uint32_t items[kEmbedFew];
+  __shared__ uint32_t counts[kWaves][1u << kEmbedFewBits];
+  __shared__ uint32_t start[1u << kEmbedFewBits];
+  __shared__ uint32_t waves[kWaves];
+  const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x / 64u;
+  const uint32_t rounds = (a.tokens + kEmbedBlock - 1u) / kEmbedBlock, begin = wave * rounds * 64u + lane;
+  uint32_t item[kEmbedFew / kEmbedBlock], at[kEmbedFew / kEmbedBlock];
+#pragma unroll
+  for (uint32_t r = 0; r < kEmbedFew / kEmbedBlock; ++r) {
+    const uint32_t i = begin + r * 64u;
+    if (r < rounds && i < a.tokens) item[r] = key_of(a, i) * kEmbedFew + i;
+  }
+  for (uint32_t shift = 0; shift < a.bits; shift += kEmbedFewBits) {
+    const uint32_t bits = min(kEmbedFewBits, a.bits - shift), digits = 1u << bits;
+    for (uint32_t d = threadIdx.x; d < kWaves * digits; d += kEmbedBlock) counts[d / digits][d % digits] = 0u;
+    __syncthreads();
+#pragma unroll
+    for (uint32_t r = 0; r < kEmbedFew / kEmbedBlock; ++r)
+      if (r < rounds) at[r] = place<kEmbedFewBits>(counts[wave], (item[r] / kEmbedFew >> shift) & (digits - 1u), begin + r * 64u < a.tokens, lane);
+    __syncthreads();
+    uint32_t all = 0u;
+    if (threadIdx.x < digits) {
+      uint32_t c[kWaves];
+#pragma unroll
+      for (uint32_t w = 0; w < kWaves; ++w) c[w] = counts[w][threadIdx.x];
+#pragma unroll
+      for (uint32_t w = 0; w < kWaves; ++w) {
+        counts[w][threadIdx.x] = all;
+        all += c[w];
+      }
+    }
+    const uint32_t smaller = sum_before(all, waves);
+    if (threadIdx.x < digits) start[threadIdx.x] = smaller;
+    __syncthreads();
+#pragma unroll
+    for (uint32_t r = 0; r < kEmbedFew / kEmbedBlock; ++r)
+      if (r < rounds && begin + r * 64u < a.tokens) {
+        const uint32_t digit = (item[r] / kEmbedFew >> shift) & (digits - 1u);
+        items[start[digit] + counts[wave][digit] + at[r]] = item[r];
+      }
+    __syncthreads();
+#pragma unroll
+    for (uint32_t r = 0; r < kEmbedFew / kEmbedBlock; ++r)
+      if (r < rounds && begin + r * 64u < a.tokens) item[r] = items[begin + r * 64u];
+  }
+#pragma unroll
+  for (uint32_t r = 0; r < kEmbedFew / kEmbedBlock; ++r)
+    if (r < rounds && begin + r * 64u < a.tokens) {
+      a.key_to[begin + r * 64u] = item[r] / kEmbedFew;
+      a.pos_to[begin + r * 64u] = item[r] % kEmbedFew;
+    }
+}
+
+// Many: workgroup b has tokens b * each to (b + 1) * each - 1 of the order so far, wave w of it a contiguous share.  Count: how many of each digit
+// a workgroup has.  Move: a token's place is what stands before it: smaller digits anywhere, its own digit in earlier workgroups, in
+// earlier waves of this one, and in this wave before it.
+__global__ __launch_bounds__(kEmbedBlock) void lt_embedding_count_kernel(const EmbedGradArgs a) {
+  __shared__ uint32_t hist[1u << kEmbedMaxBits];
+  const uint32_t digits = 1u << a.bits;
+  for (uint32_t d = threadIdx.x; d < digits; d += kEmbedBlock) hist[d] = 0u;
+  __syncthreads();
+  const uint32_t begin = blockIdx.x * a.each;
+  for (uint32_t i = begin + threadIdx.x; i < begin + a.each && i < a.tokens; i += kEmbedBlock) one_more(&hist[(key_of(a, i) >> a.shift) & (digits - 1u)]);
+  __syncthreads();
+  for (uint32_t d = threadIdx.x; d < digits; d += kEmbedBlock) a.counts[blockIdx.x * digits + d] = hist[d];
+}
+
+__global__ __launch_bounds__(kEmbedBlock) void lt_embedding_move_kernel(const EmbedGradArgs a) {
+  constexpr uint32_t kWaves = kEmbedBlock / 64u;
+  __shared__ uint32_t mine[kWaves][1u << kEmbedMaxBits];     // a wave's tokens of a digit, then where they go
+  __shared__ uint32_t waves[kWaves];
+  const uint32_t digits = 1u << a.bits, lane = threadIdx.x & 63u, wave = threadIdx.x / 64u;
   const uint32_t share = a.each / kWaves, begin = blockIdx.x * a.each + wave * share;
+  uint32_t key = begin + lane < a.tokens ? key_of(a, begin + lane) : 0u;   // of the first round
+  for (uint32_t d = threadIdx.x; d < kWaves * digits; d += kEmbedBlock) mine[d / digits][d % digits] = 0u;
+  // digit d = this thread's: all of it, and what earlier workgroups have
+  uint32_t all = 0u, before = 0u;
+  if (threadIdx.x < digits) {
+#pragma unroll 16
+    for (uint32_t b = 0; b < a.blocks; ++b) {
+      const uint32_t c = a.counts[b * digits + threadIdx.x];
+      all += c;
+      before += b < blockIdx.x ? c : 0u;
+    }
+  }
+  const uint32_t smaller = sum_before(all, waves);   // (its barrier also tells that `mine` is clear)
   for (uint32_t r = 0; r < share; r += 64u) {
     const uint32_t i = begin + r + lane;
-    if (i < a.tokens) one_more(&mine[wave][(key_of(a, i) >> a.shift) & (digits - 1u)]);
+    if (i < a.tokens) one_more(&mine[wave][((r == 0u ? key : key_of(a, i)) >> a.shift) & (digits - 1u)]);
   }
   __syncthreads();
   if (threadIdx.x < digits) {
-    uint32_t at = start[threadIdx.x];
+    uint32_t at = smaller + before, c[kWaves];
+#pragma unroll
+    for (uint32_t w = 0; w < kWaves; ++w) c[w] = mine[w][threadIdx.x];
+#pragma unroll
     for (uint32_t w = 0; w < kWaves; ++w) {
-      const uint32_t c = mine[w][threadIdx.x];
       mine[w][threadIdx.x] = at;
-      at += c;
+      at += c[w];
     }
   }
   __syncthreads();
   for (uint32_t r = 0; r < share; r += 64u) {
     const uint32_t i = begin + r + lane;
     const bool there = i < a.tokens;
-    const uint32_t key = there ? key_of(a, i) : 0u, digit = (key >> a.shift) & (digits - 1u);
-    // the lanes with the same digit
-    uint64_t same = __ballot(there);
-    for (uint32_t b = 0; b < a.bits; ++b) {
-      const uint64_t ones = __ballot((digit >> b) & 1u);
-      same &= (digit >> b) & 1u ? ones : ~ones;
-    }
-    const uint32_t earlier = __popcll(same & (((uint64_t)1 << lane) - 1u));
-    const uint32_t at = there ? mine[wave][digit] + earlier : 0u;
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    if (there && earlier == 0u) mine[wave][digit] = at + (uint32_t)__popcll(same);
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    if (there) {
-      a.key_to[at] = key;
-      a.pos_to[at] = a.pos ? a.pos[i] : i;
-      if (a.named && key < a.rows && !(a.named[key / 32u] >> (key % 32u) & 1u)) atomicOr(&a.named[key / 32u], 1u << (key % 32u));
-    }
+    if (r > 0u) key = there ? key_of(a, i) : 0u;
+    const uint32_t at = place<kEmbedMaxBits>(mine[wave], (key >> a.shift) & (digits - 1u), there, lane);
+    if (!there) continue;
+    a.key_to[at] = key;
+    a.pos_to[at] = a.pos ? a.pos[i] : i;
   }
 }
 
-// One thread a column of a piece: runs of one id, added up in order.  Blocks behind the pieces': rows that no id names.
-template <typename T, typename O>
+// The first of the sorted tokens whose id is `key` or more: a wave asks 64 at a time.
+__device__ __forceinline__ uint32_t first_of(const EmbedGradArgs& a, uint32_t key, uint32_t from, uint32_t lane) {
+  uint32_t low = from, high = a.tokens;   // it is in low .. high
+  while (high - low > 64u) {
+    const uint32_t step = (high - low + 63u) / 64u, at = low + lane * step;
+    const uint32_t below = __popcll(__ballot(at < high && a.key[at] < key));   // lanes whose token is before it
+    if (below == 0u) return low;
+    high = min(high, low + below * step);
+    low += (below - 1u) * step + 1u;
+  }
+  return low + __popcll(__ballot(low + lane < high && a.key[low + lane] < key));
+}
+
+// A wave has a piece of the sorted tokens and 64 pieces of their rows: runs of one id are added up in order, eight rows on their way.  A
+// run that is whole is written; what is shared with another piece of tokens is left in `parts`.  Waves behind the pieces': sixteen rows
+// of the table each, those that no id names.
+template <typename T, typename O, int V>
 __global__ __launch_bounds__(kBlock) void lt_embedding_sum_kernel(const EmbedGradArgs a) {
-  const uint32_t tiles = (a.dim + kBlock - 1u) / kBlock;
-  uint32_t unit = blockIdx.x / tiles;
-  const uint32_t d = (blockIdx.x % tiles) * kBlock + threadIdx.x;
-  if (d >= a.dim) return;
-  const O* base = (const O*)a.base;
-  O* out = (O*)a.out;
-  if (unit >= a.pieces) {   // sixteen rows
+  const uint32_t lane = threadIdx.x & 63u, unit = __builtin_amdgcn_readfirstlane(blockIdx.x * (kBlock / 64u) + threadIdx.x / 64u);
+  const uint32_t tiles = (a.dim / V + 63u) / 64u, index = unit / tiles, d = ((unit % tiles) * 64u + lane) * V;
+  const O* const base = (const O*)a.base;
+  O* const out = (O*)a.out;
+  const bool active = d < a.dim;
+  if (index >= a.pieces) {
     if (a.in_place) return;
-    for (uint32_t r = (unit - a.pieces) * 16u, end = min(r + 16u, a.rows); r < end; ++r)
-      if (!a.named || !(a.named[r / 32u] >> (r % 32u) & 1u)) out[(uint64_t)r * a.dim + d] = base ? base[(uint64_t)r * a.dim + d] : (O)0.0f;
+    uint32_t row = (index - a.pieces) * kEmbedRows;
+    const uint32_t end = min(row + kEmbedRows, a.rows);
+    if (row >= end) return;
+    uint32_t named = 0u;   // a bit a row
+    for (uint32_t at = first_of(a, row, 0u, lane); at < a.tokens;) {
+      const uint32_t key = at + lane < a.tokens ? a.key[at + lane] : a.rows;
+      uint32_t bit = key < end ? 1u << (key - row) : 0u;
+#pragma unroll
+      for (uint32_t o = 32u; o > 0u; o /= 2u) bit |= __shfl_xor(bit, o);
+      named |= bit;
+      const uint32_t last = __shfl(key, 63);
+      if (last + 1u >= end) break;   // (past these rows, or the last one found)
+      at = first_of(a, last + 1u, at, lane);
+    }
+    named = __builtin_amdgcn_readfirstlane(named);
+    if (!active) return;
+    for (uint32_t bit = 1u; row < end; ++row, bit *= 2u) {
+      if (named & bit) continue;
+      Piece<O, V> p;
+      if (base) p.load(base + (uint64_t)row * a.dim + d);
+      else
+#pragma unroll
+        for (int j = 0; j < V; ++j) p.set(j, 0.0f);
+      p.store(out + (uint64_t)row * a.dim + d);
+    }
     return;
   }
-  const uint32_t begin = unit * a.piece, end = min(begin + a.piece, a.tokens);
-  float* parts = a.parts + (uint64_t)unit * 2u * a.dim + d;
-  const O* from = a.in_place ? out : base;
-  for (uint32_t i = begin; i < end;) {
-    const uint32_t key = a.key[i];
-    if (key >= a.rows) break;
-    const bool begins = i > begin || begin == 0u || a.key[begin - 1u] != key;
-    float sum = 0.0f;
-    do sum += (float)((const T*)a.dy)[(uint64_t)a.pos[i] * a.dim + d];
-    while (++i < end && a.key[i] == key);
-    const bool ends = i < end || end == a.tokens || a.key[end] != key;
-    const uint64_t at = (uint64_t)key * a.dim + d;
-    if (begins && ends) out[at] = (O)((from ? (float)from[at] : 0.0f) + a.scale * sum);
-    else parts[begins ? a.dim : 0u] = sum;
+  constexpr uint32_t kWay = 8;
+  const uint32_t begin = index * a.piece, end = min(begin + a.piece, a.tokens);
+  const O* const from = a.in_place ? out : base;
+  float* const parts = a.parts + (uint64_t)index * 2u * a.dim + d;
+  float sum[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) sum[j] = 0.0f;
+  bool begins = begin == 0u || a.key[begin - 1u] != a.key[begin];
+  for (uint32_t i0 = begin; i0 < end; i0 += 64u) {
+    // 64 tokens' ids and places, a lane each; a bit for each that is the last of a run, and of the rows that exist
+    const uint32_t i = i0 + lane;
+    const uint32_t key = i < end ? a.key[i] : a.rows, pos = i < end ? a.pos[i] : 0u;
+    const uint32_t after = i + 1u < a.tokens ? a.key[i + 1u] : a.rows;
+    const uint64_t last = __ballot(i < end && (i + 1u == a.tokens || after != key)), counts = __ballot(i < end && key < a.rows);
+    if (counts == 0u) return;
+    const uint32_t n = (uint32_t)__popcll(counts);   // (the ids that are no rows stand at the end)
+    for (uint32_t k0 = 0; k0 < n; k0 += kWay) {
+      Piece<T, V> p[kWay];
+      Piece<O, V> q[kWay];
+#pragma unroll
+      for (uint32_t k = 0; k < kWay; ++k) {
+        const uint32_t at = __builtin_amdgcn_readlane(pos, min(k0 + k, 63u)), row = __builtin_amdgcn_readlane(key, min(k0 + k, 63u));
+        if (k0 + k >= n || !active) continue;
+        p[k].load((const T*)a.dy + (uint64_t)at * a.dim + d);
+        if (from && (last >> (k0 + k) & 1u)) q[k].load(from + (uint64_t)row * a.dim + d);
+      }
+#pragma unroll
+      for (uint32_t k = 0; k < kWay; ++k) {
+        if (k0 + k >= n) break;
+#pragma unroll
+        for (int j = 0; j < V; ++j) sum[j] += p[k].get(j);
+        const bool ends = last >> (k0 + k) & 1u;
+        if (!ends && i0 + k0 + k + 1u < end) continue;
+        if (active) {
+          if (begins && ends) {
+            Piece<O, V> r;
+#pragma unroll
+            for (int j = 0; j < V; ++j) r.set(j, (from ? q[k].get(j) : 0.0f) + a.scale * sum[j]);
+            r.store(out + (uint64_t)__builtin_amdgcn_readlane(key, k0 + k) * a.dim + d);
+          } else {
+            Piece<float, V> r;
+#pragma unroll
+            for (int j = 0; j < V; ++j) r.set(j, sum[j]);
+            r.store(parts + (begins ? a.dim : 0u));
+          }
+        }
+        begins = true;
+#pragma unroll
+        for (int j = 0; j < V; ++j) sum[j] = 0.0f;
+      }
+    }
+    if (n < 64u) return;
   }
 }
 
-// A row that a piece begins and shares with the next: the pieces' sums in order.
-template <typename O>
+// A row that a piece begins and shares with the next: the pieces' sums in order, sixteen on their way.
+template <typename O, int V>
 __global__ __launch_bounds__(kBlock) void lt_embedding_join_kernel(const EmbedGradArgs a) {
-  const uint32_t tiles = (a.dim + kBlock - 1u) / kBlock;
-  const uint32_t piece = blockIdx.x / tiles, d = (blockIdx.x % tiles) * kBlock + threadIdx.x;
-  const uint32_t begin = piece * a.piece;
-  uint32_t next = begin + a.piece;
-  if (d >= a.dim || next >= a.tokens) return;
+  const uint32_t lane = threadIdx.x & 63u, unit = __builtin_amdgcn_readfirstlane(blockIdx.x * (kBlock / 64u) + threadIdx.x / 64u);
+  const uint32_t tiles = (a.dim / V + 63u) / 64u, index = unit / tiles, d = ((unit % tiles) * 64u + lane) * V;
+  if (index + 1u >= a.pieces) return;
+  const uint32_t begin = index * a.piece, next = begin + a.piece;
   const uint32_t key = a.key[next];
   if (key >= a.rows || a.key[next - 1u] != key || (begin > 0u && a.key[begin] == key && a.key[begin - 1u] == key)) return;
-  const float* parts = a.parts + (uint64_t)piece * 2u * a.dim + d;
-  float sum = parts[a.dim];
-  do {
-    parts += 2u * a.dim;
-    sum += parts[0];
-    next += a.piece;
-  } while (next < a.tokens && a.key[next] == key);
-  O* out = (O*)a.out;
-  const O* from = a.in_place ? out : (const O*)a.base;
+  // how many pieces further it goes
+  uint32_t more = 0u;
+  for (;;) {
+    const uint32_t at = index + 1u + more + lane;
+    const uint64_t same = __ballot(at < a.pieces && a.key[at * a.piece] == key);
+    if (same == ~(uint64_t)0) {
+      more += 64u;
+      continue;
+    }
+    more += (uint32_t)__builtin_ctzll(~same);
+    break;
+  }
+  if (d >= a.dim) return;
+  constexpr uint32_t kWay = 16;
+  O* const out = (O*)a.out;
+  const O* const from = a.in_place ? out : (const O*)a.base;
   const uint64_t at = (uint64_t)key * a.dim + d;
-  out[at] = (O)((from ? (float)from[at] : 0.0f) + a.scale * sum);
+  Piece<O, V> r;
+  if (from) r.load(from + at);
+  const float* parts = a.parts + (uint64_t)index * 2u * a.dim + d;
+  Piece<float, V> sum;
+  sum.load(parts + a.dim);
+  for (uint32_t k0 = 1u; k0 <= more; k0 += kWay) {
+    Piece<float, V> p[kWay];
+#pragma unroll
+    for (uint32_t k = 0; k < kWay; ++k) p[k].load(parts + (uint64_t)min(k0 + k, more) * 2u * a.dim);
+#pragma unroll
+    for (uint32_t k = 0; k < kWay; ++k)
+      if (k0 + k <= more)
+#pragma unroll
+        for (int j = 0; j < V; ++j) sum.set(j, sum.get(j) + p[k].get(j));
+  }
+#pragma unroll
+  for (int j = 0; j < V; ++j) r.set(j, (from ? r.get(j) : 0.0f) + a.scale * sum.get(j));
+  r.store(out + at);
+}
+
+template <typename T, typename O, int V>
+hipError_t launch_wide(const EmbedGradArgs& a, hipStream_t s) {
+  const uint64_t tiles = (a.dim / V + 63u) / 64u;
+  const uint64_t units = tiles * (a.pass == kEmbedJoin ? a.pieces : a.pieces + (a.in_place ? 0u : (a.rows + kEmbedRows - 1u) / kEmbedRows));
+  const uint64_t grid = (units + kBlock / 64u - 1u) / (kBlock / 64u);
+  if (grid == 0) return hipSuccess;
+  if (grid >= kMostGrid) return hipErrorInvalidValue;
+  if (a.pass == kEmbedJoin) LT_LAUNCH((lt_embedding_join_kernel<O, V>), dim3((uint32_t)grid), dim3(kBlock), s, a);
+  else LT_LAUNCH((lt_embedding_sum_kernel<T, O, V>), dim3((uint32_t)grid), dim3(kBlock), s, a);
+  return hipGetLastError();
 }
 
 template <typename T, typename O>
 hipError_t launch_sums(const EmbedGradArgs& a, hipStream_t s) {
-  const uint64_t tiles = (a.dim + kBlock - 1u) / kBlock;
-  if (a.pass == kEmbedJoin) {
-    const uint64_t grid = tiles * a.pieces;
-    if (grid * kBlock >= (uint64_t)1 << 32) return hipErrorInvalidValue;
-    LT_LAUNCH(lt_embedding_join_kernel<O>, dim3((uint32_t)grid), dim3(kBlock), s, a);
-    return hipGetLastError();
-  }
-  const uint64_t grid = tiles * (a.pieces + (a.in_place ? 0u : (a.rows + 15u) / 16u));
-  if (grid == 0) return hipSuccess;
-  if (grid * kBlock >= (uint64_t)1 << 32) return hipErrorInvalidValue;
-  LT_LAUNCH((lt_embedding_sum_kernel<T, O>), dim3((uint32_t)grid), dim3(kBlock), s, a);
-  return hipGetLastError();
+  // (`parts` starts at 256 bytes)
+  auto fits = [&](uint32_t v) {
+    auto lies = [&](const void* p, uint32_t elem) { return (uintptr_t)p % std::min(16u, v * elem) == 0; };
+    return a.dim % v == 0 && lies(a.dy, sizeof(T)) && lies(a.base, sizeof(O)) && lies(a.out, sizeof(O));
+  };
+  if constexpr (sizeof(T) == 2 && sizeof(O) == 2)
+    if (fits(8u)) return launch_wide<T, O, 8>(a, s);
+  if (fits(4u)) return launch_wide<T, O, 4>(a, s);
+  if (fits(2u)) return launch_wide<T, O, 2>(a, s);
+  return launch_wide<T, O, 1>(a, s);
 }
 
 hipError_t launch_embedding_grad(const void* args, hipStream_t s) {
   const EmbedGradArgs& a = *(const EmbedGradArgs*)args;
   if ((uint64_t)a.rows * a.dim == 0) return hipSuccess;
+  if (a.pass == kEmbedSort) {
+    if (a.tokens == 0 || a.tokens > kEmbedFew || a.rows >= 1u << (2u * kEmbedFewBits) || a.bits > 2u * kEmbedFewBits) return hipErrorInvalidValue;
+    LT_LAUNCH(lt_embedding_sort_kernel, dim3(1), dim3(kEmbedBlock), s, a);
+    return hipGetLastError();
+  }
   if (a.pass == kEmbedCount || a.pass == kEmbedMove) {
-    if (a.tokens == 0 || a.bits > kEmbedMaxBits || a.blocks == 0 || a.blocks > kEmbedBlocks || a.each % kEmbedBlock != 0 || (uint64_t)a.each * a.blocks < a.tokens) return hipErrorInvalidValue;
+    if (a.tokens == 0 || a.bits > kEmbedMaxBits || a.blocks == 0 || a.blocks > kEmbedBlocks || a.each % kEmbedBlock != 0 || (uint64_t)a.each * a.blocks < a.tokens)
+      return hipErrorInvalidValue;
     if (a.pass == kEmbedCount) LT_LAUNCH(lt_embedding_count_kernel, dim3(a.blocks), dim3(kEmbedBlock), s, a);
     else LT_LAUNCH(lt_embedding_move_kernel, dim3(a.blocks), dim3(kEmbedBlock), s, a);
     return hipGetLastError();

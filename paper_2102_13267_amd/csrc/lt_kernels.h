@@ -418,15 +418,19 @@ struct EmbedArgs {
   void* out;
   uint32_t dtype, tokens, rows, dim;
   float scale;
+  Divider row;               // pieces of a row (the launcher's)
 };
 
 // The gradient: base + scale * the sums of dy's rows by id.  Its tokens are sorted by id (stable, so that sums have an order of their own):
-// kEmbedCount and kEmbedMove, a pair for each digit of the ids; kEmbedSum adds up the rows of pieces of `piece` sorted tokens, writes
-// what a piece holds all of, and every row that no id names; kEmbedJoin adds up what more than one piece has of a row.
-enum : uint32_t { kEmbedCount = 0, kEmbedMove, kEmbedSum, kEmbedJoin };
+// kEmbedSort, one workgroup, where they are few; else kEmbedCount and kEmbedMove for each digit of the ids.  kEmbedSum adds up the rows of pieces of `piece`
+// sorted tokens, writes what a piece holds all of, and every row that no id names; kEmbedJoin adds up what more than one piece has of a row.
+enum : uint32_t { kEmbedSort = 0, kEmbedCount, kEmbedMove, kEmbedSum, kEmbedJoin };
 constexpr uint32_t kEmbedBlock = 1024;     // threads of a sorting workgroup
+constexpr uint32_t kEmbedFew = 8192;       // tokens that one of them sorts by itself,
+constexpr uint32_t kEmbedFewBits = 9;      // by ids of two digits of so many bits
 constexpr uint32_t kEmbedBlocks = 64;      // sorting workgroups at most
 constexpr uint32_t kEmbedMaxBits = 10;     // of a digit
+constexpr uint32_t kEmbedRows = 16;        // rows of the table that a wave looks for among the ids
 struct EmbedGradArgs {
   const void* dy;
   const int32_t* ids;
@@ -434,28 +438,23 @@ struct EmbedGradArgs {
   void* out;
   uint32_t *key, *pos;       // sorted so far: ids (rows where one names no row) and tokens; null in the first pass: ids, 0 1 2 ...
   uint32_t *key_to, *pos_to;
-  uint32_t* counts;          // [digit][workgroup]
-  uint32_t* named;           // a bit for every row that an id names
+  uint32_t* counts;          // [workgroup][digit]
   float* parts;              // [piece][2][dim]: a piece's sums of the row that it shares with the piece before, and of the one that it begins and shares with the next
-  uint32_t pass, dtype, out_dtype, base_dtype, in_place;
+  uint32_t pass, dtype, out_dtype, in_place;
   uint32_t tokens, rows, dim, shift, bits, blocks, each, piece, pieces;   // each: tokens of a sorting workgroup
   float scale;
-  // how the sort is shared out
+  // how the work is shared out
   void share_out() {
-    const uint32_t need = tokens / (4u * kEmbedBlock) + 1u;
-    blocks = need < kEmbedBlocks ? need : kEmbedBlocks;
-    const uint32_t rounds = (tokens + blocks * kEmbedBlock - 1u) / (blocks * kEmbedBlock);
-    each = rounds * kEmbedBlock;
+    const uint32_t need = (tokens + kEmbedBlock - 1u) / kEmbedBlock;
+    blocks = need < 1u ? 1u : need < kEmbedBlocks ? need : kEmbedBlocks;
+    each = (tokens + blocks * kEmbedBlock - 1u) / (blocks * kEmbedBlock) * kEmbedBlock;
     piece = 32u;
     while ((uint64_t)piece * 4096u < tokens) piece *= 2u;
     pieces = (tokens + piece - 1u) / piece;
+    bits = 1u;                // of ids 0 .. rows (rows: no row)
+    while (bits < 31u && rows >> bits) ++bits;
   }
-  // digits of ids 0 .. rows (rows: no row)
-  uint32_t key_bits() const {
-    uint32_t b = 1u;
-    while (b < 31u && (1u << b) <= rows) ++b;
-    return b;
-  }
+  bool few() const { return tokens <= kEmbedFew && bits <= 2u * kEmbedFewBits; }
 };
 
 // ---- dropout ---------------------------------------------------------------------------------------------

@@ -2127,7 +2127,6 @@ struct Lowering {
     ltk::EmbedGradArgs args{};
     args.dtype = out_dtype(rins[a][0]);
     args.out_dtype = an->dtype;
-    args.base_dtype = an->dtype;
     args.rows = (uint32_t)an->dims[0];
     args.dim = (uint32_t)an->dims[1];
     args.tokens = (uint32_t)count(out_shape(rins[a][1]));
@@ -2136,39 +2135,43 @@ struct Lowering {
     args.share_out();
     const uint64_t n = args.tokens, w = dtype_size(args.dtype), ow = dtype_size(an->dtype), all = (uint64_t)args.rows * args.dim;
     const bool some = n > 0 && all > 0;
-    const uint32_t bits = args.key_bits(), passes = (bits + ltk::kEmbedMaxBits - 1) / ltk::kEmbedMaxBits;
-    const int32_t named = some ? temporary(4 * ((uint64_t)args.rows / 32 + 1)) : -1, counts = some ? temporary(4 * ((uint64_t)args.blocks << ltk::kEmbedMaxBits)) : -1,
-                  parts = some ? temporary(8 * (uint64_t)args.pieces * args.dim) : -1;
-    int32_t from[2] = {-1, -1};
-    for (uint32_t p = 0; some && p < passes; ++p) {
-      args.shift = bits * p / passes;
-      args.bits = bits * (p + 1) / passes - args.shift;
-      const int32_t to[2] = {temporary(4 * n), temporary(4 * n)};
-      for (uint32_t pass : {ltk::kEmbedCount, ltk::kEmbedMove}) {
-        args.pass = pass;
-        const int l = add_launch(L_EMBEDGRAD, k, args, 8 * n);
-        patch(l, offsetof(ltk::EmbedGradArgs, ids), ids);
-        if (p > 0) {
-          patch(l, offsetof(ltk::EmbedGradArgs, key), from[0], 0);
-          patch(l, offsetof(ltk::EmbedGradArgs, pos), from[1], 0);
+    int32_t key = -1, pos = -1;
+    const int32_t parts = some ? temporary(8 * (uint64_t)args.pieces * args.dim) : -1;
+    // a launch that reads the order so far (none: the ids as they come) and writes the next
+    auto order = [&](int l, bool writes) {
+      patch(l, offsetof(ltk::EmbedGradArgs, ids), ids);
+      if (key >= 0) patch(l, offsetof(ltk::EmbedGradArgs, key), key, 0);
+      if (pos >= 0) patch(l, offsetof(ltk::EmbedGradArgs, pos), pos, 0);
+      if (!writes) return;
+      key = temporary(4 * n);
+      pos = temporary(4 * n);
+      patch(l, offsetof(ltk::EmbedGradArgs, key_to), key, 0, true);
+      patch(l, offsetof(ltk::EmbedGradArgs, pos_to), pos, 0, true);
+    };
+    if (some && args.few()) {
+      args.pass = ltk::kEmbedSort;
+      order(add_launch(L_EMBEDGRAD, k, args, 12 * n), true);
+    } else if (some) {
+      const uint32_t bits = args.bits, passes = (bits + ltk::kEmbedMaxBits - 1) / ltk::kEmbedMaxBits;
+      const int32_t counts = temporary(4 * ((uint64_t)args.blocks << ltk::kEmbedMaxBits));
+      for (uint32_t p = 0; p < passes; ++p) {
+        args.shift = bits * p / passes;
+        args.bits = bits * (p + 1) / passes - args.shift;
+        for (uint32_t pass : {ltk::kEmbedCount, ltk::kEmbedMove}) {
+          args.pass = pass;
+          const int l = add_launch(L_EMBEDGRAD, k, args, 12 * n);
+          patch(l, offsetof(ltk::EmbedGradArgs, counts), counts, 0, pass == ltk::kEmbedCount);
+          order(l, pass == ltk::kEmbedMove);
         }
-        patch(l, offsetof(ltk::EmbedGradArgs, counts), counts, 0, pass == ltk::kEmbedCount);
-        if (p == 0) patch(l, offsetof(ltk::EmbedGradArgs, named), named, 0, true);
-        if (pass == ltk::kEmbedCount) continue;
-        patch(l, offsetof(ltk::EmbedGradArgs, key_to), to[0], 0, true);
-        patch(l, offsetof(ltk::EmbedGradArgs, pos_to), to[1], 0, true);
       }
-      from[0] = to[0];
-      from[1] = to[1];
     }
     for (uint32_t pass : {ltk::kEmbedSum, ltk::kEmbedJoin}) {
       if (pass == ltk::kEmbedJoin && args.pieces < 2) break;
       args.pass = pass;
       const int l = add_launch(L_EMBEDGRAD, k, args, pass == ltk::kEmbedJoin ? 4 * n : n * args.dim * w + (args.in_place ? 2 * n * args.dim : has_base ? 2 * all : all) * ow);
       if (some) {
-        patch(l, offsetof(ltk::EmbedGradArgs, key), from[0], 0);
-        patch(l, offsetof(ltk::EmbedGradArgs, pos), from[1], 0);
-        patch(l, offsetof(ltk::EmbedGradArgs, named), named, 0);
+        patch(l, offsetof(ltk::EmbedGradArgs, key), key, 0);
+        patch(l, offsetof(ltk::EmbedGradArgs, pos), pos, 0);
         patch(l, offsetof(ltk::EmbedGradArgs, parts), parts, 0, pass == ltk::kEmbedSum);
       }
       patch(l, offsetof(ltk::EmbedGradArgs, dy), dy);
