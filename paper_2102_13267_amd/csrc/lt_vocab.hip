@@ -102,19 +102,23 @@ struct Slab {
   __device__ static __forceinline__ uint32_t swz(uint32_t row) { return KC ? (row >> 1) & 7u : (row & 3u) << 2; }
 };
 
+// What a wave's matrix instructions take and give: blocks of kX rows (columns), kSteps of them for a slab of k; a lane's results are kQuads times
+// four consecutive rows, 8 q + 4 * (lane / kX) on, of column lane % kX.
 template <typename T> struct Mma;
 template <> struct Mma<__bf16> {
   typedef v8bf Frag;
+  typedef v4f Acc;
+  static constexpr uint32_t kX = 16, kSteps = 2, kQuads = 1, kProducts = 1, kReadsAcross = 2;
   template <int BX, bool KC>
   static __device__ __forceinline__ Frag read(const char* tile, uint32_t x0, uint32_t kk, uint32_t lane) {
     typedef Slab<__bf16, BX, KC> S;
     if constexpr (KC) {
-      const uint32_t row = x0 + (lane & 31u), c = kk * 2u + (lane >> 5);
+      const uint32_t row = x0 + (lane & 15u), c = kk * 4u + (lane >> 4);
       return *(const v8bf*)(tile + row * 128u + ((c ^ S::swz(row)) << 4));
     } else {
       // the hardware's transposing read: lane i of sixteen gets element i of each of four rows of k
-      const uint32_t i16 = lane & 15u, k = kk * 16u + (lane >> 5) * 8u + (i16 >> 2);
-      const uint32_t col = (x0 + ((lane & 31u) >> 4) * 16u + 4u * (i16 & 3u)) * 2u;
+      const uint32_t i16 = lane & 15u, k = kk * 32u + (lane >> 4) * 8u + (i16 >> 2);
+      const uint32_t col = (x0 + 4u * (i16 & 3u)) * 2u;
       const char* p = tile + k * (BX * 2u) + (((col >> 4) ^ S::swz(k)) << 4) + (col & 15u);
       const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_ptr)p);
       const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_ptr)(p + 4 * BX * 2));   // (k + 4: the same swizzle)
@@ -122,10 +126,12 @@ template <> struct Mma<__bf16> {
       return __builtin_bit_cast(v8bf, r);
     }
   }
-  static __device__ __forceinline__ v16f mma(Frag a, Frag b, v16f c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+  static __device__ __forceinline__ Acc mma(Frag a, Frag b, Acc c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 };
 template <> struct Mma<float> {
   typedef v4f Frag;   // k (2 kk + lane / 32) * 4 + j, j = 0 .. 3, of both operands: one product each
+  typedef v16f Acc;
+  static constexpr uint32_t kX = 32, kSteps = 4, kQuads = 4, kProducts = 4, kReadsAcross = 4;
   template <int BX, bool KC>
   static __device__ __forceinline__ Frag read(const char* tile, uint32_t x0, uint32_t kk, uint32_t lane) {
     typedef Slab<float, BX, KC> S;
@@ -139,7 +145,7 @@ template <> struct Mma<float> {
       return f;
     }
   }
-  static __device__ __forceinline__ v16f mma(Frag a, Frag b, v16f c) {
+  static __device__ __forceinline__ Acc mma(Frag a, Frag b, Acc c) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
     return c;
@@ -154,7 +160,9 @@ template <typename T, int BM, int BN, int WM, int WN, uint32_t PASS>
 __global__ __launch_bounds__(WM * WN * 64, 2) void lt_vocab_product_kernel(const VocabArgs a) {
   constexpr bool kLogit = PASS == kVocabLogits || PASS == kVocabGrad, kAK = PASS != kVocabDw, kBK = kLogit;
   constexpr uint32_t kThreads = WM * WN * 64;
-  constexpr int MB = BM / WM / 32, NB = BN / WN / 32;
+  typedef Mma<T> M;
+  constexpr uint32_t X = M::kX;
+  constexpr int MB = BM / WM / X, NB = BN / WN / X;
   typedef Slab<T, BM, kAK> SA;
   typedef Slab<T, BN, kBK> SB;
   constexpr uint32_t kStage = SA::kBytes + SB::kBytes, kPad = BM + 16 / sizeof(T);
@@ -206,61 +214,105 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void lt_vocab_product_kernel(const
     copy(SB(), B, ldb, tile_n, bx, bk, first_slab + slab, lds0 + which * kStage + SA::kBytes);
   };
 
-  v16f acc[MB][NB];
+  typename M::Acc acc[MB][NB];
 #pragma unroll
   for (int i = 0; i < MB; ++i)
 #pragma unroll
     for (int j = 0; j < NB; ++j)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
-  if (slabs > 0u) stage(0u, 0u);
-  for (uint32_t s = 0; s < slabs; ++s) {
-    // behind the barrier slab s has landed for every wave, and every wave has read slab s - 1, whose place slab s + 1 takes
-    landed_and_read<0>();
-    __syncthreads();
-    if (s + 1u < slabs) stage(s + 1u, (s + 1u) & 1u);
-    const char* const As = smem + (s & 1u) * kStage;
+      for (uint32_t r = 0; r < 4u * M::kQuads; ++r) acc[i][j][r] = 0.0f;
+  // A step of k of every fragment at a time, read while the products of the one before are formed.
+  struct Frags {
+    typename M::Frag a[MB], b[NB];
+  };
+  auto read = [&](uint32_t which, uint32_t kk) __attribute__((always_inline)) {
+    const char* const As = smem + which * kStage;
     const char* const Bs = As + SA::kBytes;
+    Frags f;
 #pragma unroll
-    for (uint32_t kk = 0; kk < 4u; ++kk) {
-      typename Mma<T>::Frag fa[MB], fb[NB];
+    for (int j = 0; j < NB; ++j) f.b[j] = M::template read<BN, kBK>(Bs, wn * (BN / WN) + j * X, kk, lane);
 #pragma unroll
-      for (int i = 0; i < MB; ++i) fa[i] = Mma<T>::template read<BM, kAK>(As, wm * (BM / WM) + i * 32u, kk, lane);
+    for (int i = 0; i < MB; ++i) f.a[i] = M::template read<BM, kAK>(As, wm * (BM / WM) + i * X, kk, lane);
+    return f;
+  };
+  auto multiply = [&](const Frags& f) __attribute__((always_inline)) {
 #pragma unroll
-      for (int j = 0; j < NB; ++j) fb[j] = Mma<T>::template read<BN, kBK>(Bs, wn * (BN / WN) + j * 32u, kk, lane);
+    for (int i = 0; i < MB; ++i)
 #pragma unroll
-      for (int i = 0; i < MB; ++i)
+      for (int j = 0; j < NB; ++j) acc[i][j] = M::mma(f.a[i], f.b[j], acc[i][j]);
+    // the reads of the next step among the products, evenly
+    constexpr int kReads = (kAK ? 1 : M::kReadsAcross) * MB + (kBK ? 1 : M::kReadsAcross) * NB, kProducts = MB * NB * M::kProducts;
 #pragma unroll
-        for (int j = 0; j < NB; ++j) acc[i][j] = Mma<T>::mma(fa[i], fb[j], acc[i][j]);
+    for (int q = 0; q < kProducts; ++q) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      if ((q + 1) * kReads / kProducts > q * kReads / kProducts) __builtin_amdgcn_sched_group_barrier(0x100, (kReads + kProducts - 1) / kProducts, 0);
+    }
+  };
+  if (slabs > 0u) {
+    stage(0u, 0u);
+    landed<0>();
+    __syncthreads();
+    Frags f = read(0u, 0u);
+    for (uint32_t s = 0; s < slabs; ++s) {
+      const uint32_t which = s & 1u;
+      if (s + 1u < slabs) stage(s + 1u, which ^ 1u);
+#pragma unroll
+      for (uint32_t kk = 1; kk < M::kSteps; ++kk) {
+        const Frags g = read(which, kk);
+        multiply(f);
+        f = g;
+      }
+      // behind the barrier the next slab has landed for every wave, and every wave has read this one, whose place the one after takes
+      landed_and_read<0>();
+      __syncthreads();
+      const Frags g = read(which ^ 1u, 0u);   // (behind the last slab: what is there, unused)
+      multiply(f);
+      f = g;
     }
   }
   __syncthreads();
 
-  // a lane's results: column y = wn .. + j * 32 + lane % 32, rows x = wm .. + i * 32 + 8 * (r / 4) + 4 * (lane / 32) + r % 4
-  const uint32_t y0 = wn * (BN / WN) + (lane & 31u), x0 = wm * (BM / WM) + 4u * (lane >> 5);
+  // a lane's results: column y = wn .. + j * X + lane % X, rows x = wm .. + i * X + 8 * q + 4 * (lane / X) + 0 .. 3
+  const uint32_t y0 = wn * (BN / WN) + lane % X, x0 = wm * (BM / WM) + 4u * (lane / X);
+  auto each_quad = [&](auto f) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+      for (uint32_t q = 0; q < M::kQuads; ++q) f(i, q, x0 + i * X + 8u * q);
+  };
   if constexpr (PASS == kVocabLogits) {
+    const bool edge = tile_m + BM > m;
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
-      const uint32_t y = y0 + j * 32u, token = tile_n + y;
-      const int32_t label = a.label[token] - (int32_t)(a.first + tile_m);
+      const uint32_t y = y0 + j * X, token = tile_n + y;
+      const uint32_t label = (uint32_t)a.label[token] - (a.first + tile_m) - wm * (BM / WM);   // (of this wave's rows)
+      if (__ballot(label < (uint32_t)(BM / WM)) != 0u)
+        each_quad([&](int i, uint32_t q, uint32_t x) {
+#pragma unroll
+          for (uint32_t r = 0; r < 4u; ++r)
+            if (x + r - wm * (BM / WM) == label) a.picked[token] = acc[i][j][4 * q + r];
+        });
+      if (edge)
+        each_quad([&](int i, uint32_t q, uint32_t x) {
+#pragma unroll
+          for (uint32_t r = 0; r < 4u; ++r)
+            if (tile_m + x + r >= m) acc[i][j][4 * q + r] = -INFINITY;
+        });
       float top = -INFINITY, sum = 0.0f;
+      each_quad([&](int i, uint32_t q, uint32_t) {
 #pragma unroll
-      for (int i = 0; i < MB; ++i)
+        for (uint32_t r = 0; r < 4u; ++r) top = fmaxf(top, acc[i][j][4 * q + r]);
+      });
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const uint32_t x = x0 + i * 32u + 8u * (r / 4) + r % 4;
-          if (tile_m + x >= m) acc[i][j][r] = -INFINITY;
-          if ((int32_t)x == label) a.picked[token] = acc[i][j][r];
-          top = fmaxf(top, acc[i][j][r]);
-        }
-      top = fmaxf(top, __shfl_xor(top, 32));
+      for (uint32_t o = X; o < 64u; o *= 2u) top = fmaxf(top, __shfl_xor(top, o));
       const float from = top == -INFINITY ? 0.0f : top;
+      each_quad([&](int i, uint32_t q, uint32_t) {
 #pragma unroll
-      for (int i = 0; i < MB; ++i)
+        for (uint32_t r = 0; r < 4u; ++r) sum += __builtin_amdgcn_exp2f((acc[i][j][4 * q + r] - from) * kLog2e);
+      });
 #pragma unroll
-        for (int r = 0; r < 16; ++r) sum += __builtin_amdgcn_exp2f((acc[i][j][r] - from) * kLog2e);
-      sum += __shfl_xor(sum, 32);
-      if (lane < 32u) red[wm * BN + y] = make_float2(top, sum);
+      for (uint32_t o = X; o < 64u; o *= 2u) sum += __shfl_xor(sum, o);
+      if (lane < X) red[wm * BN + y] = make_float2(top, sum);
     }
     __syncthreads();
     float* const parts = a.parts + (uint64_t)(tile_m / BM) * 2u * a.padded + tile_n;
@@ -278,46 +330,51 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void lt_vocab_product_kernel(const
     float* const sums = a.sums + (uint64_t)blockIdx.y * a.padded * a.width;
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
-      const uint32_t d = tile_n + y0 + j * 32u;
+      const uint32_t d = tile_n + y0 + j * X;
       if (d >= n) continue;
+      each_quad([&](int i, uint32_t q, uint32_t x) {
 #pragma unroll
-      for (int i = 0; i < MB; ++i)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          float* const at = sums + (uint64_t)(tile_m + x0 + i * 32u + 8u * (r / 4) + r % 4) * a.width + d;
-          *at = a.add ? *at + acc[i][j][r] : acc[i][j][r];
+        for (uint32_t r = 0; r < 4u; ++r) {
+          float* const at = sums + (uint64_t)(tile_m + x + r) * a.width + d;
+          *at = a.add ? *at + acc[i][j][4 * q + r] : acc[i][j][4 * q + r];
         }
+      });
     }
   } else {
     // through LDS, [y][x], to whole rows in memory
     T* const out = (T*)smem;
+    const bool edge = tile_m + BM > m || tile_n + BN > n;
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
-      const uint32_t y = y0 + j * 32u, token = tile_n + y;
-      float lse = 0.0f, dloss = 0.0f;
-      int32_t label = 0;
-      if (PASS == kVocabGrad) {
-        lse = a.lse_of[token];
-        dloss = a.dloss_of[token];
-        label = a.label[token] - (int32_t)(a.first + tile_m);
+      const uint32_t y = y0 + j * X, token = tile_n + y;
+      if constexpr (PASS == kVocabGrad) {
+        const float lse = a.lse_of[token], dloss = a.dloss_of[token];
+        const uint32_t label = (uint32_t)a.label[token] - (a.first + tile_m) - wm * (BM / WM);
+        each_quad([&](int i, uint32_t q, uint32_t) {
+#pragma unroll
+          for (uint32_t r = 0; r < 4u; ++r) acc[i][j][4 * q + r] = __builtin_amdgcn_exp2f((acc[i][j][4 * q + r] - lse) * kLog2e);
+        });
+        if (__ballot(label < (uint32_t)(BM / WM)) != 0u)
+          each_quad([&](int i, uint32_t q, uint32_t x) {
+#pragma unroll
+            for (uint32_t r = 0; r < 4u; ++r) acc[i][j][4 * q + r] -= x + r - wm * (BM / WM) == label ? 1.0f : 0.0f;
+          });
+        each_quad([&](int i, uint32_t q, uint32_t) {
+#pragma unroll
+          for (uint32_t r = 0; r < 4u; ++r) acc[i][j][4 * q + r] *= dloss;
+        });
+        if (edge)
+          each_quad([&](int i, uint32_t q, uint32_t x) {
+#pragma unroll
+            for (uint32_t r = 0; r < 4u; ++r)
+              if (tile_m + x + r >= m || token >= n) acc[i][j][4 * q + r] = 0.0f;
+          });
       }
-#pragma unroll
-      for (int i = 0; i < MB; ++i)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const uint32_t x = x0 + i * 32u + 8u * q;
-          float v[4];
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            v[r] = acc[i][j][4 * q + r];
-            if (PASS == kVocabGrad) {
-              const float p = __builtin_amdgcn_exp2f((v[r] - lse) * kLog2e) - ((int32_t)(x + r) == label ? 1.0f : 0.0f);
-              v[r] = tile_m + x + r < m && token < n ? p * dloss : 0.0f;
-            }
-          }
-          if constexpr (sizeof(T) == 4) *(v4f*)(out + y * kPad + x) = v4f{v[0], v[1], v[2], v[3]};
-          else *(v4bf*)(out + y * kPad + x) = v4bf{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
-        }
+      each_quad([&](int i, uint32_t q, uint32_t x) {
+        const v4f v = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+        if constexpr (sizeof(T) == 4) *(v4f*)(out + y * kPad + x) = v;
+        else *(v4bf*)(out + y * kPad + x) = v4bf{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
+      });
     }
     __syncthreads();
     constexpr uint32_t V = 16 / sizeof(T), kChunks = BM / V;
