@@ -1,6 +1,7 @@
 // Softmax cross entropy over a vocabulary, l = x w^T, and its gradient, without the logits ever being in memory as a whole.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cstdio>
 
 #include "lt_dma.h"
@@ -152,6 +153,12 @@ template <> struct Mma<float> {
   }
 };
 
+template <int N> struct Num {
+  static constexpr int value = N;
+};
+
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __builtin_amdgcn_readfirstlane(x); }
+
 // C = A B over tiles of BM x BN, WM x WN waves.
 //   kVocabLogits, kVocabGrad  A: rows of w [x][k], B: packed tokens [x][k], k = width; a lane has sixteen rows of one token
 //   kVocabDx                  A: g [token][row]: [x][k], B: rows of w: [k][x], k = rows of the piece
@@ -166,30 +173,41 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void lt_vocab_product_kernel(const
   typedef Slab<T, BM, kAK> SA;
   typedef Slab<T, BN, kBK> SB;
   constexpr uint32_t kStage = SA::kBytes + SB::kBytes, kPad = BM + 16 / sizeof(T);
-  constexpr size_t kOut = PASS == kVocabGrad || PASS == kVocabDw ? (size_t)BN * kPad * sizeof(T) : 0;
-  __shared__ __attribute__((aligned(16))) char smem[2 * kStage > kOut ? 2 * kStage : kOut];
+  // results that go through LDS leave the first stage to the next tile's first slab: half of the columns at a time behind it
+  constexpr uint32_t kHalf = BN / 2, kOut = PASS == kVocabGrad || PASS == kVocabDw ? kHalf * kPad * sizeof(T) : 0u;
+  __shared__ __attribute__((aligned(16))) char smem[kStage + (kStage > kOut ? kStage : kOut)];
   __shared__ float2 red[PASS == kVocabLogits ? WM * BN : 1];
 
-  const uint32_t n_tokens = *a.count;
+  const uint32_t n_tokens = __builtin_amdgcn_readfirstlane(*a.count);
   const uint32_t m = kLogit ? a.rows : PASS == kVocabDx ? n_tokens : a.width, n = kLogit ? n_tokens : PASS == kVocabDx ? a.width : a.rows;
   const uint32_t k = kLogit ? a.width : PASS == kVocabDx ? (a.rows + SA::kK - 1u) / SA::kK * SA::kK : (n_tokens + SA::kK - 1u) / SA::kK * SA::kK;
-  // as many tiles as there are tokens for, an even and contiguous share for each of the eight dies (one set of panels in its cache),
-  // walked eight rows of tiles at a time
-  const uint32_t tiles_m = (m + BM - 1u) / BM, tiles_n = (n + BN - 1u) / BN, nt = tiles_m * tiles_n;
-  const uint32_t die = blockIdx.x & 7u, own = nt / 8u + (die < nt % 8u ? 1u : 0u);
-  if (blockIdx.x / 8u >= own) return;
-  const uint32_t t = die * (nt / 8u) + min(die, nt % 8u) + blockIdx.x / 8u;
-  const uint32_t strip = t / (8u * tiles_n), strip_rows = min(8u, tiles_m - strip * 8u), in_strip = t - strip * 8u * tiles_n;
-  const uint32_t tile_n = in_strip / strip_rows * BN, tile_m = (strip * 8u + in_strip % strip_rows) * BM;
+  // as many tiles as there are tokens for (of dx: times the splits of k), an even and contiguous share for each of the eight dies (one set of
+  // panels in its cache), walked eight rows of tiles at a time, by as many workgroups as there are
+  const uint32_t tiles_m = (m + BM - 1u) / BM, tiles_n = (n + BN - 1u) / BN, tiles = tiles_m * tiles_n, nt = PASS == kVocabDx ? tiles * a.splits : tiles;
+  const uint32_t die = blockIdx.x & 7u, own = nt / 8u + (die < nt % 8u ? 1u : 0u), first_own = die * (nt / 8u) + min(die, nt % 8u);
+  const uint32_t all_slabs = k / SA::kK, per = PASS == kVocabDx ? uniform((all_slabs + a.splits - 1u) / a.splits) : all_slabs;
+  struct Tile {
+    uint32_t m, n, split, first_slab, slabs;
+  };
+  auto tile_at = [&](uint32_t index) {
+    Tile r;
+    uint32_t t = first_own + index;
+    r.split = PASS == kVocabDx ? uniform(t / tiles) : 0u;
+    t -= r.split * tiles;
+    const uint32_t strip = uniform(t / (8u * tiles_n)), strip_rows = min(8u, tiles_m - strip * 8u), in_strip = t - strip * 8u * tiles_n;
+    r.n = uniform(in_strip / strip_rows) * BN;
+    r.m = (strip * 8u + uniform(in_strip % strip_rows)) * BM;
+    r.first_slab = min(all_slabs, r.split * per);
+    r.slabs = min(all_slabs - r.first_slab, per);
+    return r;
+  };
+  uint32_t index = blockIdx.x / 8u;
+  if (index >= own) return;
 
   const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = __builtin_amdgcn_readfirstlane(tid / 64u), wm = wave / WN, wn = wave % WN;
   const void* const A = kLogit ? a.w : PASS == kVocabDx ? a.g : a.x;
   const void* const B = kLogit ? a.x : PASS == kVocabDx ? a.w : a.g;
   const uint64_t lda = (kLogit ? a.w_stride : PASS == kVocabDx ? a.stride : a.width) * sizeof(T), ldb = (kLogit ? a.width : PASS == kVocabDx ? a.w_stride : a.stride) * sizeof(T);
-  // the slabs of this workgroup's share of k
-  const uint32_t all_slabs = k / SA::kK, per = PASS == kVocabDx ? (all_slabs + a.splits - 1u) / a.splits : all_slabs;
-  const uint32_t first_slab = PASS == kVocabDx ? min(all_slabs, blockIdx.y * per) : 0u, slabs = min(all_slabs - first_slab, per);
-
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
   // a slab of an operand of nx rows or columns and nk of k, from x0 on: what is behind either is a copy of the last (of a result never
   // stored, of k met by zeros)
@@ -197,101 +215,148 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void lt_vocab_product_kernel(const
     typedef decltype(slab_type) S;
     constexpr bool KC = S::kAlongK;
     constexpr uint32_t kInstr = S::kBytes / 16 / kThreads;
-    const char* const from = (const char*)base + (KC ? (uint64_t)x0 * ld + (uint64_t)slab * 128u : (uint64_t)slab * S::kK * ld + (uint64_t)x0 * sizeof(T));
+    const uint64_t start = (uint64_t)base + (KC ? (uint64_t)x0 * ld + (uint64_t)slab * 128u : (uint64_t)slab * S::kK * ld + (uint64_t)x0 * sizeof(T));
+    const char* const from = (const char*)((uint64_t)uniform((uint32_t)(start >> 32)) << 32 | uniform((uint32_t)start));
+    const uint32_t place = uniform(to + wave * 1024u);
 #pragma unroll
     for (uint32_t it = 0; it < kInstr; ++it) {
       const uint32_t e = it * kThreads + tid, row = e / S::kPerRow, c = (e % S::kPerRow) ^ S::swz(row);
       const uint32_t off = KC ? min(row, nx - 1u - x0) * (uint32_t)ld + c * 16u
                               : min(row, nk - 1u - slab * S::kK) * (uint32_t)ld + min(c * (uint32_t)(16 / sizeof(T)), nx - x0 - (uint32_t)(16 / sizeof(T))) * (uint32_t)sizeof(T);
-      copy_1k(from, off, to + (it * kThreads + wave * 64u) * 16u);
+      copy_1k(from, off, place + it * kThreads * 16u);
     }
   };
   // rows that exist: w's of the piece; packed tokens and rows of g up to whole tiles
   const uint32_t ax = kLogit ? a.rows : PASS == kVocabDx ? a.padded : a.width, bx = kLogit ? a.padded : PASS == kVocabDx ? a.w_stride : a.stride;
   const uint32_t ak = a.padded, bk = PASS == kVocabDx ? a.rows : a.padded;
-  auto stage = [&](uint32_t slab, uint32_t which) __attribute__((always_inline)) {
-    copy(SA(), A, lda, tile_m, ax, ak, first_slab + slab, lds0 + which * kStage);
-    copy(SB(), B, ldb, tile_n, bx, bk, first_slab + slab, lds0 + which * kStage + SA::kBytes);
+  auto stage = [&](const Tile& t, uint32_t slab, uint32_t which) __attribute__((always_inline)) {
+    copy(SA(), A, lda, t.m, ax, ak, t.first_slab + slab, lds0 + which * kStage);
+    copy(SB(), B, ldb, t.n, bx, bk, t.first_slab + slab, lds0 + which * kStage + SA::kBytes);
   };
 
   typename M::Acc acc[MB][NB];
+  // The products of a slab in parts: a step of k, half of the wave's rows.  The fragments of the next part (its rows', and with a new
+  // step its columns') are read while the products of one are formed, evenly among them.
+  constexpr int kHalves = MB >= 4 ? 2 : 1, kRows = MB / kHalves, kParts = (int)M::kSteps * kHalves;
+  typename M::Frag fa[kRows], fb[NB];
+  auto read_rows = [&](uint32_t which, uint32_t part, typename M::Frag(&f)[kRows]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) f[i] = M::template read<BM, kAK>(smem + which * kStage, wm * (BM / WM) + (part % kHalves * kRows + i) * X, part / kHalves, lane);
+  };
+  auto read_columns = [&](uint32_t which, uint32_t part, typename M::Frag(&f)[NB]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < NB; ++j) f[j] = M::template read<BN, kBK>(smem + which * kStage + SA::kBytes, wn * (BN / WN) + j * X, part / kHalves, lane);
+  };
+  // part P, and the reads of part NEXT of the slab in stage `which` (none: kParts)
+  auto part = [&](auto p, auto then, uint32_t which) __attribute__((always_inline)) {
+    constexpr int P = (int)decltype(p)::value, NEXT = (int)decltype(then)::value;
+    constexpr bool columns = NEXT < kParts && NEXT % kHalves == 0;
+    typename M::Frag ga[kRows], gb[NB];
+    if constexpr (columns) read_columns(which, NEXT, gb);
+    if constexpr (NEXT < kParts) read_rows(which, NEXT, ga);
+#pragma unroll
+    for (int i = 0; i < kRows; ++i)
+#pragma unroll
+      for (int j = 0; j < NB; ++j) acc[P % kHalves * kRows + i][j] = M::mma(fa[i], fb[j], acc[P % kHalves * kRows + i][j]);
+    if constexpr (NEXT < kParts) {
+      constexpr int kReads = (kAK ? 1 : M::kReadsAcross) * kRows + (columns ? (kBK ? 1 : M::kReadsAcross) * NB : 0), kProducts = kRows * NB * M::kProducts;
+#pragma unroll
+      for (int q = 0; q < kProducts; ++q) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        if ((q + 1) * kReads / kProducts > q * kReads / kProducts) __builtin_amdgcn_sched_group_barrier(0x100, (kReads + kProducts - 1) / kProducts, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < kRows; ++i) fa[i] = ga[i];
+      if constexpr (columns)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) fb[j] = gb[j];
+    }
+  };
+  auto parts_but_last = [&](uint32_t which) __attribute__((always_inline)) {
+    part(Num<0>(), Num<1>(), which);
+    part(Num<1>(), Num<2>(), which);
+    part(Num<2>(), Num<3>(), which);
+  };
+  static_assert(kParts == 4, "four parts");
+  Tile next = tile_at(index);
+  if (next.slabs > 0u) stage(next, 0u, 0u);
+  for (;;) {
+  const Tile tile = next;
+  const uint32_t tile_m = tile.m, tile_n = tile.n, slabs = tile.slabs;
+  // what the results of this tile's tokens will ask for: on its way under the products
+  uint32_t label[NB];
+  float lse[NB], dloss[NB];
+#pragma unroll
+  for (int j = 0; kLogit && j < NB; ++j) {
+    const uint32_t token = tile_n + wn * (BN / WN) + lane % X + j * X;
+    label[j] = (uint32_t)a.label[token] - (a.first + tile_m) - wm * (BM / WM);   // (of this wave's rows)
+    lse[j] = PASS == kVocabGrad ? a.lse_of[token] : 0.0f;
+    dloss[j] = PASS == kVocabGrad ? a.dloss_of[token] : 0.0f;
+  }
 #pragma unroll
   for (int i = 0; i < MB; ++i)
 #pragma unroll
     for (int j = 0; j < NB; ++j)
 #pragma unroll
       for (uint32_t r = 0; r < 4u * M::kQuads; ++r) acc[i][j][r] = 0.0f;
-  // A step of k of every fragment at a time, read while the products of the one before are formed.
-  struct Frags {
-    typename M::Frag a[MB], b[NB];
-  };
-  auto read = [&](uint32_t which, uint32_t kk) __attribute__((always_inline)) {
-    const char* const As = smem + which * kStage;
-    const char* const Bs = As + SA::kBytes;
-    Frags f;
-#pragma unroll
-    for (int j = 0; j < NB; ++j) f.b[j] = M::template read<BN, kBK>(Bs, wn * (BN / WN) + j * X, kk, lane);
-#pragma unroll
-    for (int i = 0; i < MB; ++i) f.a[i] = M::template read<BM, kAK>(As, wm * (BM / WM) + i * X, kk, lane);
-    return f;
-  };
-  auto multiply = [&](const Frags& f) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < MB; ++i)
-#pragma unroll
-      for (int j = 0; j < NB; ++j) acc[i][j] = M::mma(f.a[i], f.b[j], acc[i][j]);
-    // the reads of the next step among the products, evenly
-    constexpr int kReads = (kAK ? 1 : M::kReadsAcross) * MB + (kBK ? 1 : M::kReadsAcross) * NB, kProducts = MB * NB * M::kProducts;
-#pragma unroll
-    for (int q = 0; q < kProducts; ++q) {
-      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-      if ((q + 1) * kReads / kProducts > q * kReads / kProducts) __builtin_amdgcn_sched_group_barrier(0x100, (kReads + kProducts - 1) / kProducts, 0);
-    }
-  };
+  landed<0>();
+  __syncthreads();   // the first slab is there for every wave, and every wave is done with the tile before
   if (slabs > 0u) {
-    stage(0u, 0u);
-    landed<0>();
-    __syncthreads();
-    Frags f = read(0u, 0u);
-    for (uint32_t s = 0; s < slabs; ++s) {
+    read_columns(0u, 0u, fb);
+    read_rows(0u, 0u, fa);
+    for (uint32_t s = 0; s + 1u < slabs; ++s) {
       const uint32_t which = s & 1u;
-      if (s + 1u < slabs) stage(s + 1u, which ^ 1u);
-#pragma unroll
-      for (uint32_t kk = 1; kk < M::kSteps; ++kk) {
-        const Frags g = read(which, kk);
-        multiply(f);
-        f = g;
-      }
+      stage(tile, s + 1u, which ^ 1u);
+      parts_but_last(which);
       // behind the barrier the next slab has landed for every wave, and every wave has read this one, whose place the one after takes
       landed_and_read<0>();
       __syncthreads();
-      const Frags g = read(which ^ 1u, 0u);   // (behind the last slab: what is there, unused)
-      multiply(f);
-      f = g;
+      part(Num<kParts - 1>(), Num<0>(), which ^ 1u);
     }
+    parts_but_last((slabs - 1u) & 1u);
+    landed_and_read<0>();
+    __syncthreads();
+    part(Num<kParts - 1>(), Num<kParts>(), 0u);
   }
-  __syncthreads();
+  // the next tile's first slab is on its way under this one's results
+  index += gridDim.x / 8u;
+  const bool more = index < own;
+  if (more) {
+    next = tile_at(index);
+    if (next.slabs > 0u) stage(next, 0u, 0u);
+  }
 
   // a lane's results: column y = wn .. + j * X + lane % X, rows x = wm .. + i * X + 8 * q + 4 * (lane / X) + 0 .. 3
-  const uint32_t y0 = wn * (BN / WN) + lane % X, x0 = wm * (BM / WM) + 4u * (lane / X);
+  // (where they go is worked out anew for every tile: kept from one to the next it would take registers that the products need)
+  uint32_t own_lane = lane;
+  asm volatile("" : "+v"(own_lane));
+  const uint32_t own_tid = wave * 64u + own_lane;
+  const uint32_t y0 = wn * (BN / WN) + own_lane % X, x0 = wm * (BM / WM) + 4u * (own_lane / X);
   auto each_quad = [&](auto f) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < MB; ++i)
 #pragma unroll
       for (uint32_t q = 0; q < M::kQuads; ++q) f(i, q, x0 + i * X + 8u * q);
   };
+
   if constexpr (PASS == kVocabLogits) {
     const bool edge = tile_m + BM > m;
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
       const uint32_t y = y0 + j * X, token = tile_n + y;
-      const uint32_t label = (uint32_t)a.label[token] - (a.first + tile_m) - wm * (BM / WM);   // (of this wave's rows)
-      if (__ballot(label < (uint32_t)(BM / WM)) != 0u)
+      if (__ballot(label[j] < (uint32_t)(BM / WM)) != 0u) {
+        float hit = 0.0f;
+        bool mine = false;
         each_quad([&](int i, uint32_t q, uint32_t x) {
 #pragma unroll
-          for (uint32_t r = 0; r < 4u; ++r)
-            if (x + r - wm * (BM / WM) == label) a.picked[token] = acc[i][j][4 * q + r];
+          for (uint32_t r = 0; r < 4u; ++r) {
+            const bool here = x + r - wm * (BM / WM) == label[j];
+            hit = here ? acc[i][j][4 * q + r] : hit;
+            mine = mine || here;
+          }
         });
+        if (mine) a.picked[token] = hit;
+      }
       if (edge)
         each_quad([&](int i, uint32_t q, uint32_t x) {
 #pragma unroll
@@ -316,7 +381,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void lt_vocab_product_kernel(const
     }
     __syncthreads();
     float* const parts = a.parts + (uint64_t)(tile_m / BM) * 2u * a.padded + tile_n;
-    for (uint32_t y = tid; y < (uint32_t)BN; y += kThreads) {
+    for (uint32_t y = own_tid; y < (uint32_t)BN; y += kThreads) {
       float top = red[y].x, sum = 0.0f;
 #pragma unroll
       for (int w = 1; w < WM; ++w) top = fmaxf(top, red[w * BN + y].x);
@@ -327,7 +392,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void lt_vocab_product_kernel(const
       parts[a.padded + y] = sum;
     }
   } else if constexpr (PASS == kVocabDx) {
-    float* const sums = a.sums + (uint64_t)blockIdx.y * a.padded * a.width;
+    float* const sums = a.sums + (uint64_t)tile.split * a.padded * a.width;
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
       const uint32_t d = tile_n + y0 + j * X;
@@ -342,56 +407,66 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void lt_vocab_product_kernel(const
     }
   } else {
     // through LDS, [y][x], to whole rows in memory
-    T* const out = (T*)smem;
+    T* const out = (T*)(smem + kStage);
     const bool edge = tile_m + BM > m || tile_n + BN > n;
+    constexpr uint32_t V = 16 / sizeof(T), kChunks = BM / V;
+    if constexpr (PASS == kVocabGrad) {
 #pragma unroll
-    for (int j = 0; j < NB; ++j) {
-      const uint32_t y = y0 + j * X, token = tile_n + y;
-      if constexpr (PASS == kVocabGrad) {
-        const float lse = a.lse_of[token], dloss = a.dloss_of[token];
-        const uint32_t label = (uint32_t)a.label[token] - (a.first + tile_m) - wm * (BM / WM);
+      for (int j = 0; j < NB; ++j) {
         each_quad([&](int i, uint32_t q, uint32_t) {
 #pragma unroll
-          for (uint32_t r = 0; r < 4u; ++r) acc[i][j][4 * q + r] = __builtin_amdgcn_exp2f((acc[i][j][4 * q + r] - lse) * kLog2e);
+          for (uint32_t r = 0; r < 4u; ++r) acc[i][j][4 * q + r] = __builtin_amdgcn_exp2f((acc[i][j][4 * q + r] - lse[j]) * kLog2e);
         });
-        if (__ballot(label < (uint32_t)(BM / WM)) != 0u)
+        if (__ballot(label[j] < (uint32_t)(BM / WM)) != 0u)
           each_quad([&](int i, uint32_t q, uint32_t x) {
 #pragma unroll
-            for (uint32_t r = 0; r < 4u; ++r) acc[i][j][4 * q + r] -= x + r - wm * (BM / WM) == label ? 1.0f : 0.0f;
+            for (uint32_t r = 0; r < 4u; ++r) acc[i][j][4 * q + r] -= x + r - wm * (BM / WM) == label[j] ? 1.0f : 0.0f;
           });
         each_quad([&](int i, uint32_t q, uint32_t) {
 #pragma unroll
-          for (uint32_t r = 0; r < 4u; ++r) acc[i][j][4 * q + r] *= dloss;
+          for (uint32_t r = 0; r < 4u; ++r) acc[i][j][4 * q + r] *= dloss[j];
         });
         if (edge)
           each_quad([&](int i, uint32_t q, uint32_t x) {
 #pragma unroll
             for (uint32_t r = 0; r < 4u; ++r)
-              if (tile_m + x + r >= m || token >= n) acc[i][j][4 * q + r] = 0.0f;
+              if (tile_m + x + r >= m || tile_n + y0 + j * X >= n) acc[i][j][4 * q + r] = 0.0f;
           });
       }
-      each_quad([&](int i, uint32_t q, uint32_t x) {
-        const v4f v = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-        if constexpr (sizeof(T) == 4) *(v4f*)(out + y * kPad + x) = v;
-        else *(v4bf*)(out + y * kPad + x) = v4bf{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
-      });
     }
-    __syncthreads();
-    constexpr uint32_t V = 16 / sizeof(T), kChunks = BM / V;
-    if constexpr (PASS == kVocabGrad) {
-      T* const g = (T*)a.g + (uint64_t)tile_n * a.stride + tile_m;
-      for (uint32_t e = tid; e < BN * kChunks; e += kThreads) *(uint4*)(g + (uint64_t)(e / kChunks) * a.stride + e % kChunks * V) = *(const uint4*)(out + e / kChunks * kPad + e % kChunks * V);
-    } else {
-      const uint32_t rows = min((uint32_t)BN, n - tile_n), cols = min((uint32_t)BM, a.dim > tile_m ? a.dim - tile_m : 0u);
-      T* const dw = (T*)a.dw + (uint64_t)tile_n * a.dim + tile_m;
-      if (((uintptr_t)a.dw & 15u) == 0u && a.dim % V == 0u) {
-        for (uint32_t e = tid; e < rows * kChunks; e += kThreads)
-          if (e % kChunks * V < cols) *(uint4*)(dw + (uint64_t)(e / kChunks) * a.dim + e % kChunks * V) = *(const uint4*)(out + e / kChunks * kPad + e % kChunks * V);
+#pragma unroll
+    for (uint32_t half = 0; half < 2u; ++half) {
+      if (half > 0u) __syncthreads();   // (the first half's rows have been read)
+      if (wn / (WN / 2) == half) {
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+          each_quad([&](int i, uint32_t q, uint32_t x) {
+            T* const at = out + (y0 + j * X - half * kHalf) * kPad + x;
+            const v4f v = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+            if constexpr (sizeof(T) == 4) *(v4f*)at = v;
+            else *(v4bf*)at = v4bf{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
+          });
+      }
+      __syncthreads();
+      const uint32_t from = tile_n + half * kHalf;
+      if constexpr (PASS == kVocabGrad) {
+        T* const g = (T*)a.g + (uint64_t)from * a.stride + tile_m;
+#pragma unroll 4
+        for (uint32_t e = own_tid; e < kHalf * kChunks; e += kThreads) *(uint4*)(g + (uint64_t)(e / kChunks) * a.stride + e % kChunks * V) = *(const uint4*)(out + e / kChunks * kPad + e % kChunks * V);
       } else {
-        for (uint32_t e = tid; e < rows * BM; e += kThreads)
-          if (e % BM < cols) dw[(uint64_t)(e / BM) * a.dim + e % BM] = out[e / BM * kPad + e % BM];
+        const uint32_t rows = min(kHalf, n > from ? n - from : 0u), cols = min((uint32_t)BM, a.dim > tile_m ? a.dim - tile_m : 0u);
+        T* const dw = (T*)a.dw + (uint64_t)from * a.dim + tile_m;
+        if (((uintptr_t)a.dw & 15u) == 0u && a.dim % V == 0u) {
+          for (uint32_t e = own_tid; e < rows * kChunks; e += kThreads)
+            if (e % kChunks * V < cols) *(uint4*)(dw + (uint64_t)(e / kChunks) * a.dim + e % kChunks * V) = *(const uint4*)(out + e / kChunks * kPad + e % kChunks * V);
+        } else {
+          for (uint32_t e = own_tid; e < rows * BM; e += kThreads)
+            if (e % BM < cols) dw[(uint64_t)(e / BM) * a.dim + e % BM] = out[e / BM * kPad + e % BM];
+        }
       }
     }
+  }
+  if (!more) return;
   }
 }
 
@@ -442,11 +517,13 @@ __global__ __launch_bounds__(kRowsBlock) void lt_vocab_dx_kernel(const VocabArgs
 template <typename T, int B, int WM, int WN, uint32_t PASS>
 hipError_t launch_product(const VocabArgs& a, hipStream_t s) {
   const uint64_t m = PASS == kVocabDx ? a.padded : PASS == kVocabDw ? a.width : a.rows, n = PASS == kVocabDx ? a.width : PASS == kVocabDw ? a.rows : a.padded;
-  const uint64_t tiles = (m + B - 1) / B * ((n + B - 1) / B), grid = (tiles + 7) / 8 * 8;
+  const uint64_t tiles = (m + B - 1) / B * ((n + B - 1) / B) * (PASS == kVocabDx ? a.splits : 1u);
   if (tiles == 0) return hipSuccess;
-  if (grid * WM * WN * 64 >= (uint64_t)1 << 32) return hipErrorInvalidValue;
+  if (tiles >= (uint64_t)1 << 31) return hipErrorInvalidValue;
+  // as many workgroups as run at once: one a compute unit, or two where LDS holds two
+  const uint64_t grid = std::min<uint64_t>((tiles + 7) / 8 * 8, sizeof(T) == 4 ? 512 : 256);
   if (((uintptr_t)a.x & 15u) || ((uintptr_t)a.w & 15u) || ((uintptr_t)a.g & 15u)) return hipErrorInvalidValue;
-  LT_LAUNCH((lt_vocab_product_kernel<T, B, B, WM, WN, PASS>), dim3((uint32_t)grid, PASS == kVocabDx ? a.splits : 1u), dim3(WM * WN * 64), s, a);
+  LT_LAUNCH((lt_vocab_product_kernel<T, B, B, WM, WN, PASS>), dim3((uint32_t)grid), dim3(WM * WN * 64), s, a);
   static const char* const names[] = {"", "", "logits", "", "grad", "dx", "dw"};
   char name[48];
   snprintf(name, sizeof(name), "lt_vocab_product_kernel<%s,%d,%s>", sizeof(T) == 4 ? "f32" : "bf16", B, names[PASS]);
