@@ -2223,7 +2223,7 @@ struct Lowering {
     const bool pack_w = args.width != args.dim || w.byte_offset % 16 != 0;
     args.w_stride = args.width;
     // a piece of g takes 256 MB, as many rows as that is, but 4096 at least
-    const uint64_t fit = std::max<uint64_t>(4096, ((uint64_t)256 << 20) / (std::max<uint64_t>(pad, 256) * e) & ~(uint64_t)255);
+    const uint64_t fit = std::max<uint64_t>(4096, ((uint64_t)128 << 20) / (std::max<uint64_t>(pad, 256) * e) & ~(uint64_t)255);
     const uint64_t fit_w = std::max<uint64_t>(4096, ((uint64_t)256 << 20) / (width * e) & ~(uint64_t)255);
     uint64_t piece = args.vocab;
     if (grad) piece = std::min(piece, fit);

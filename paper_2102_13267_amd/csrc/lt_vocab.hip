@@ -100,7 +100,7 @@ struct Slab {
   static constexpr uint32_t kBytes = BX * 128;
   static constexpr bool kAlongK = KC;
   static constexpr uint32_t kPerRow = KC ? 8 : BX * sizeof(T) / 16;
-  __device__ static __forceinline__ uint32_t swz(uint32_t row) { return KC ? (row >> 1) & 7u : (row & 3u) << 2; }
+  __host__ __device__ static constexpr uint32_t swz(uint32_t row) { return KC ? (row >> 1) & 7u : (row & 3u) << 2; }
 };
 
 // What a wave's matrix instructions take and give: blocks of kX rows (columns), kSteps of them for a slab of k; a lane's results are kQuads times
@@ -161,11 +161,11 @@ __device__ __forceinline__ uint32_t uniform(uint32_t x) { return __builtin_amdgc
 
 // C = A B over tiles of BM x BN, WM x WN waves.
 //   kVocabLogits, kVocabGrad  A: rows of w [x][k], B: packed tokens [x][k], k = width; a lane has sixteen rows of one token
-//   kVocabDx                  A: g [token][row]: [x][k], B: rows of w: [k][x], k = rows of the piece
+//   kVocabDx                  A: rows of w [k][x] (columns of dim), B: g [token][row]: [x][k], k = rows of the piece
 //   kVocabDw                  A: packed tokens [k][x] (columns of dim), B: g [k][x] (rows of w), k = tokens; a lane has sixteen columns of one row
 template <typename T, int BM, int BN, int WM, int WN, uint32_t PASS>
 __global__ __launch_bounds__(WM * WN * 64, 2) void lt_vocab_product_kernel(const VocabArgs a) {
-  constexpr bool kLogit = PASS == kVocabLogits || PASS == kVocabGrad, kAK = PASS != kVocabDw, kBK = kLogit;
+  constexpr bool kLogit = PASS == kVocabLogits || PASS == kVocabGrad, kAK = kLogit, kBK = PASS != kVocabDw;
   constexpr uint32_t kThreads = WM * WN * 64;
   typedef Mma<T> M;
   constexpr uint32_t X = M::kX;
@@ -179,7 +179,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void lt_vocab_product_kernel(const
   __shared__ float2 red[PASS == kVocabLogits ? WM * BN : 1];
 
   const uint32_t n_tokens = __builtin_amdgcn_readfirstlane(*a.count);
-  const uint32_t m = kLogit ? a.rows : PASS == kVocabDx ? n_tokens : a.width, n = kLogit ? n_tokens : PASS == kVocabDx ? a.width : a.rows;
+  const uint32_t m = kLogit ? a.rows : a.width, n = PASS == kVocabDw ? a.rows : n_tokens;
   const uint32_t k = kLogit ? a.width : PASS == kVocabDx ? (a.rows + SA::kK - 1u) / SA::kK * SA::kK : (n_tokens + SA::kK - 1u) / SA::kK * SA::kK;
   // as many tiles as there are tokens for (of dx: times the splits of k), an even and contiguous share for each of the eight dies (one set of
   // panels in its cache), walked eight rows of tiles at a time, by as many workgroups as there are
@@ -205,9 +205,9 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void lt_vocab_product_kernel(const
   if (index >= own) return;
 
   const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = __builtin_amdgcn_readfirstlane(tid / 64u), wm = wave / WN, wn = wave % WN;
-  const void* const A = kLogit ? a.w : PASS == kVocabDx ? a.g : a.x;
-  const void* const B = kLogit ? a.x : PASS == kVocabDx ? a.w : a.g;
-  const uint64_t lda = (kLogit ? a.w_stride : PASS == kVocabDx ? a.stride : a.width) * sizeof(T), ldb = (kLogit ? a.width : PASS == kVocabDx ? a.w_stride : a.stride) * sizeof(T);
+  const void* const A = PASS == kVocabDw ? a.x : a.w;
+  const void* const B = kLogit ? a.x : a.g;
+  const uint64_t lda = (PASS == kVocabDw ? a.width : a.w_stride) * sizeof(T), ldb = (kLogit ? a.width : a.stride) * sizeof(T);
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
   // a slab of an operand of nx rows or columns and nk of k, from x0 on: what is behind either is a copy of the last (of a result never
   // stored, of k met by zeros)
@@ -218,17 +218,17 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void lt_vocab_product_kernel(const
     const uint64_t start = (uint64_t)base + (KC ? (uint64_t)x0 * ld + (uint64_t)slab * 128u : (uint64_t)slab * S::kK * ld + (uint64_t)x0 * sizeof(T));
     const char* const from = (const char*)((uint64_t)uniform((uint32_t)(start >> 32)) << 32 | uniform((uint32_t)start));
     const uint32_t place = uniform(to + wave * 1024u);
+    // (rows of a copy are kThreads / kPerRow apart, so a lane's chunk is the same one in all of them)
+    static_assert(S::swz(kThreads / S::kPerRow) == 0u && S::swz(2u * kThreads / S::kPerRow) == 0u, "the same place in every row");
+    const uint32_t row0 = tid / S::kPerRow, c = (tid % S::kPerRow) ^ S::swz(row0);
+    const uint32_t col = KC ? c * 16u : min(c * (uint32_t)(16 / sizeof(T)), nx - x0 - (uint32_t)(16 / sizeof(T))) * (uint32_t)sizeof(T), left = KC ? nx - 1u - x0 : nk - 1u - slab * S::kK;
 #pragma unroll
-    for (uint32_t it = 0; it < kInstr; ++it) {
-      const uint32_t e = it * kThreads + tid, row = e / S::kPerRow, c = (e % S::kPerRow) ^ S::swz(row);
-      const uint32_t off = KC ? min(row, nx - 1u - x0) * (uint32_t)ld + c * 16u
-                              : min(row, nk - 1u - slab * S::kK) * (uint32_t)ld + min(c * (uint32_t)(16 / sizeof(T)), nx - x0 - (uint32_t)(16 / sizeof(T))) * (uint32_t)sizeof(T);
-      copy_1k(from, off, place + it * kThreads * 16u);
-    }
+    for (uint32_t it = 0; it < kInstr; ++it)
+      copy_1k(from, min(row0 + it * (kThreads / S::kPerRow), left) * (uint32_t)ld + col, place + it * kThreads * 16u);
   };
   // rows that exist: w's of the piece; packed tokens and rows of g up to whole tiles
-  const uint32_t ax = kLogit ? a.rows : PASS == kVocabDx ? a.padded : a.width, bx = kLogit ? a.padded : PASS == kVocabDx ? a.w_stride : a.stride;
-  const uint32_t ak = a.padded, bk = PASS == kVocabDx ? a.rows : a.padded;
+  const uint32_t ax = kLogit ? a.rows : PASS == kVocabDx ? a.w_stride : a.width, bx = PASS == kVocabDw ? a.stride : a.padded;
+  const uint32_t ak = PASS == kVocabDx ? a.rows : a.padded, bk = a.padded;
   auto stage = [&](const Tile& t, uint32_t slab, uint32_t which) __attribute__((always_inline)) {
     copy(SA(), A, lda, t.m, ax, ak, t.first_slab + slab, lds0 + which * kStage);
     copy(SB(), B, ldb, t.n, bx, bk, t.first_slab + slab, lds0 + which * kStage + SA::kBytes);
@@ -392,17 +392,23 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void lt_vocab_product_kernel(const
       parts[a.padded + y] = sum;
     }
   } else if constexpr (PASS == kVocabDx) {
-    float* const sums = a.sums + (uint64_t)tile.split * a.padded * a.width;
+    // four columns of a token at a time, all of a block of tokens' on their way when they are added to
+    float* const sums = a.sums + ((uint64_t)tile.split * a.padded + tile_n) * a.width + tile_m;
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
-      const uint32_t d = tile_n + y0 + j * X;
-      if (d >= n) continue;
-      each_quad([&](int i, uint32_t q, uint32_t x) {
+      float* const row = sums + (uint64_t)(y0 + j * X) * a.width;
+      if (a.add) {
+        v4f old[MB][M::kQuads];
+        each_quad([&](int i, uint32_t q, uint32_t x) {
+          if (tile_m + x < m) old[i][q] = *(const v4f*)(row + x);
+        });
+        each_quad([&](int i, uint32_t q, uint32_t) {
 #pragma unroll
-        for (uint32_t r = 0; r < 4u; ++r) {
-          float* const at = sums + (uint64_t)(tile_m + x + r) * a.width + d;
-          *at = a.add ? *at + acc[i][j][4 * q + r] : acc[i][j][4 * q + r];
-        }
+          for (uint32_t r = 0; r < 4u; ++r) acc[i][j][4 * q + r] += old[i][q][r];
+        });
+      }
+      each_quad([&](int i, uint32_t q, uint32_t x) {
+        if (tile_m + x < m) *(v4f*)(row + x) = v4f{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
       });
     }
   } else {
@@ -473,17 +479,28 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void lt_vocab_product_kernel(const
 // ---- losses: a token's maxima and sums of all tiles, sixty-four tokens a workgroup, a sixteenth of the tiles a thread --------
 constexpr uint32_t kLossBlock = 1024;
 __global__ __launch_bounds__(kLossBlock) void lt_vocab_loss_kernel(const VocabArgs a) {
-  constexpr uint32_t kShares = kLossBlock / 64u;
+  constexpr uint32_t kShares = kLossBlock / 64u, kWay = 8;
   __shared__ float2 red[kShares][64];
   const uint32_t lane = threadIdx.x & 63u, share = threadIdx.x / 64u, token = blockIdx.x * 64u + lane;
   const uint32_t n = *a.count;
   if (blockIdx.x * 64u >= n) return;
   float top = -INFINITY, sum = 0.0f;
   if (token < n)
-    for (uint32_t t = share; t < a.tiles_all; t += kShares) {
-      const float m = a.parts[(uint64_t)t * 2u * a.padded + token], s = a.parts[((uint64_t)t * 2u + 1u) * a.padded + token];
-      const float both = fmaxf(top, m), from = both == -INFINITY ? 0.0f : both;
-      sum = sum * __builtin_amdgcn_exp2f((top - from) * kLog2e) + s * __builtin_amdgcn_exp2f((m - from) * kLog2e);
+    for (uint32_t t0 = share; t0 < a.tiles_all; t0 += kShares * kWay) {
+      float m[kWay], s[kWay];
+#pragma unroll
+      for (uint32_t k = 0; k < kWay; ++k) {   // (behind the last tile: nothing)
+        const uint32_t t = t0 + k * kShares;
+        m[k] = t < a.tiles_all ? a.parts[(uint64_t)t * 2u * a.padded + token] : -INFINITY;
+        s[k] = t < a.tiles_all ? a.parts[((uint64_t)t * 2u + 1u) * a.padded + token] : 0.0f;
+      }
+      float both = top;
+#pragma unroll
+      for (uint32_t k = 0; k < kWay; ++k) both = fmaxf(both, m[k]);
+      const float from = both == -INFINITY ? 0.0f : both;
+      sum *= __builtin_amdgcn_exp2f((top - from) * kLog2e);
+#pragma unroll
+      for (uint32_t k = 0; k < kWay; ++k) sum += s[k] * __builtin_amdgcn_exp2f((m[k] - from) * kLog2e);
       top = both;
     }
   red[share][lane] = make_float2(top, sum);
@@ -499,24 +516,35 @@ __global__ __launch_bounds__(kLossBlock) void lt_vocab_loss_kernel(const VocabAr
   if (a.lse_out) a.lse_out[i] = lse;
 }
 
-// ---- dx: the workgroups' sums of a token, one wave a row ---------------------------------------------------
+// ---- dx: the workgroups' sums of a token, four columns a thread (packed rows are whole slabs), one wave a row -----------------
 template <typename T>
 __global__ __launch_bounds__(kRowsBlock) void lt_vocab_dx_kernel(const VocabArgs a) {
   const uint32_t i = blockIdx.x * (kRowsBlock / 64u) + threadIdx.x / 64u, lane = threadIdx.x & 63u;
   if (i >= a.tokens) return;
   const int32_t p = a.packed_of[i];
-  T* out = (T*)a.dx + (uint64_t)i * a.dim;
-  for (uint32_t d = lane; d < a.dim; d += 64u) {
-    float v = 0.0f;
-    if (p >= 0)
-      for (uint32_t s = 0; s < a.splits; ++s) v += a.sums[((uint64_t)s * a.padded + (uint32_t)p) * a.width + d];
-    out[d] = (T)v;
+  T* const out = (T*)a.dx + (uint64_t)i * a.dim;
+  const bool whole = a.dim % 4u == 0u && ((uintptr_t)a.dx & 15u) == 0u;
+  for (uint32_t d = lane * 4u; d < a.dim; d += 256u) {
+    v4f v = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (p >= 0) {
+      const float* from = a.sums + (uint64_t)p * a.width + d;
+#pragma unroll 8
+      for (uint32_t s = 0; s < a.splits; ++s, from += (uint64_t)a.padded * a.width) v += *(const v4f*)from;
+    }
+    if (whole) {
+      if constexpr (sizeof(T) == 4) *(v4f*)(out + d) = v;
+      else *(v4bf*)(out + d) = v4bf{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
+    } else {
+#pragma unroll
+      for (uint32_t r = 0; r < 4u; ++r)
+        if (d + r < a.dim) out[d + r] = (T)v[r];
+    }
   }
 }
 
 template <typename T, int B, int WM, int WN, uint32_t PASS>
 hipError_t launch_product(const VocabArgs& a, hipStream_t s) {
-  const uint64_t m = PASS == kVocabDx ? a.padded : PASS == kVocabDw ? a.width : a.rows, n = PASS == kVocabDx ? a.width : PASS == kVocabDw ? a.rows : a.padded;
+  const uint64_t m = PASS == kVocabDx || PASS == kVocabDw ? a.width : a.rows, n = PASS == kVocabDw ? a.rows : a.padded;
   const uint64_t tiles = (m + B - 1) / B * ((n + B - 1) / B) * (PASS == kVocabDx ? a.splits : 1u);
   if (tiles == 0) return hipSuccess;
   if (tiles >= (uint64_t)1 << 31) return hipErrorInvalidValue;
