@@ -488,6 +488,7 @@ struct VocabArgs {
   uint32_t add;                // kVocabDx: not the first piece
   uint32_t pack_w;             // kVocabPack: rows of w, not tokens' rows of x
   uint32_t w_stride;           // of w's rows as the products read them
+  uint32_t few;                // kVocabLogits, kVocabGrad: few tokens (and kVocabLogits, kVocabLoss: not packed)
   uint32_t rank0;              // dloss is one number, in dloss_value unless dloss is set
   float dloss_value;
   const void *x, *w;           // as they are, or packed (kVocabPack: what is packed)
@@ -506,6 +507,12 @@ struct VocabArgs {
   void *dx, *dw;
 };
 constexpr uint32_t kVocabTile = 256;
+// Few tokens: their rows of x in LDS, padded to 256 bytes, in one, two or four blocks of sixteen; so many workgroups share the rows of w.
+constexpr uint32_t kVocabFewBytes = 128u << 10, kVocabFewGrid = 256;
+inline uint32_t vocab_few_blocks(uint32_t tokens) { return tokens <= 16u ? 1u : tokens <= 32u ? 2u : 4u; }
+inline bool vocab_few(uint32_t tokens, uint32_t width, uint32_t elem) {
+  return tokens <= 64u && (uint64_t)vocab_few_blocks(tokens) * 16u * ((width * elem + 255u) & ~255u) <= kVocabFewBytes;
+}
 
 // Argument blocks travel by value in the kernel argument segment, which holds 4 KiB.
 static_assert(sizeof(EwArgs) <= 4096 && sizeof(RowArgs) <= 4096 && sizeof(AllArgs) <= 4096 && sizeof(ColArgs) <= 4096 &&

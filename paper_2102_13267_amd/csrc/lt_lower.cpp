@@ -2232,15 +2232,19 @@ struct Lowering {
     args.stride = (uint32_t)((piece + 255) & ~(uint64_t)255);
     args.tile = dt == LT_BF16 ? 256u : 128u;
     args.tiles_all = 0;
+    // few tokens, whose rows of x fit in LDS, and rows of w that need no packing: w goes by once
+    const bool few = !pack_w && n > 0 && ltk::vocab_few(args.tokens, args.width, (uint32_t)e) && (grad || x.byte_offset % 16 == 0);
+    args.few = few;
     // by packed token: row, label, lse, dloss, picked; their count; by token: packed place
     const int32_t lists = temporary(4 * (5 * pad + pad + 64));
-    const int32_t packed_x = temporary(pad * width * e);
+    const int32_t packed_x = few && !grad ? -1 : temporary(pad * width * e);
     const int32_t packed_w = pack_w ? temporary(piece * width * e) : -1;
     std::vector<uint32_t> first_tile;
     for (uint32_t p = 0; p < pieces; ++p) {
       first_tile.push_back(args.tiles_all);
       args.tiles_all += (uint32_t)((std::min<uint64_t>(piece, args.vocab - p * piece) + args.tile - 1) / args.tile);
     }
+    if (few) args.tiles_all = ltk::kVocabFewGrid;
     const int32_t parts = grad ? -1 : temporary(8 * (uint64_t)args.tiles_all * pad);
     const int32_t g = grad ? temporary(pad * args.stride * e) : -1;
     // few tiles of dx and a long sum: shared by as many workgroups as compute units are left without one, each with eight slabs at least
@@ -2269,6 +2273,7 @@ struct Lowering {
       args.rank0 = is_imm(d) || out_shape(d).empty();
       if (!is_imm(d) && !operand_whole(d, &dloss)) return false;
     }
+    if (grad || !few) {
     l = add(ltk::kVocabTokens, 4 * n * (grad ? 4 : 2));
     patch(l, offsetof(ltk::VocabArgs, labels), labels);
     if (grad) {
@@ -2282,6 +2287,7 @@ struct Lowering {
     l = add(ltk::kVocabPack, 2 * n * args.dim * e);
     patch(l, offsetof(ltk::VocabArgs, x), x);
     patch(l, offsetof(ltk::VocabArgs, packed), packed_x, 0, true);
+    }
     for (uint32_t p = 0; p < pieces; ++p) {
       args.first = (uint32_t)(p * piece);
       args.rows = (uint32_t)std::min<uint64_t>(piece, args.vocab - args.first);
@@ -2295,12 +2301,14 @@ struct Lowering {
         patch(l, offsetof(ltk::VocabArgs, packed), packed_w, 0, true);
       }
       auto operands = [&](int at, bool reads_x, bool reads_w) {
-        if (reads_x) patch(at, offsetof(ltk::VocabArgs, x), packed_x, 0);
+        if (reads_x && packed_x < 0) patch(at, offsetof(ltk::VocabArgs, x), x);
+        else if (reads_x) patch(at, offsetof(ltk::VocabArgs, x), packed_x, 0);
         if (reads_w && pack_w) patch(at, offsetof(ltk::VocabArgs, w), packed_w, 0);
         else if (reads_w) patch(at, offsetof(ltk::VocabArgs, w), w.storage, w.byte_offset + (int64_t)(args.first * (uint64_t)args.dim * e));
       };
       l = add(grad ? ltk::kVocabGrad : ltk::kVocabLogits, w_bytes + x_bytes, product);
       operands(l, true, true);
+      if (few && !grad) patch(l, offsetof(ltk::VocabArgs, labels), labels);
       if (!grad) {
         patch(l, offsetof(ltk::VocabArgs, parts), parts, (int64_t)(8 * pad * first_tile[p]), true);
         continue;
@@ -2322,6 +2330,7 @@ struct Lowering {
     if (!grad) {
       l = add(ltk::kVocabLoss, 8 * (uint64_t)args.tiles_all * n);
       patch(l, offsetof(ltk::VocabArgs, parts), parts, 0);
+      if (few) patch(l, offsetof(ltk::VocabArgs, labels), labels);
       if (s_loss >= 0) patch(l, offsetof(ltk::VocabArgs, loss), s_loss, 0, true);
       if (s_lse >= 0) patch(l, offsetof(ltk::VocabArgs, lse_out), s_lse, 0, true);
     } else if (s_dx >= 0) {

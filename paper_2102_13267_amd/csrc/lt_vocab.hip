@@ -476,13 +476,152 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void lt_vocab_product_kernel(const
   }
 }
 
+// ---- few tokens: w goes by once, straight into registers --------------------------------------------------
+// The tokens' rows of x stay in LDS, sixteen tokens a block (chunk c of token t at place c ^ (t & 15)); a wave takes sixteen rows of w at a time, eight steps of k on their way
+// while eight are multiplied, and on to its next rows.  A lane has four rows of one token of a block: it keeps a running maximum and sum.
+//   kVocabLogits  x and labels as they are, a maximum and a sum a workgroup and token;   kVocabGrad  packed tokens, g
+template <typename T> struct Narrow;
+template <> struct Narrow<__bf16> {
+  typedef v8bf Frag;
+  static constexpr uint32_t kStep = 32;   // of k
+  static __device__ __forceinline__ v4f mma(Frag a, Frag b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+};
+template <> struct Narrow<float> {
+  typedef v4f Frag;
+  static constexpr uint32_t kStep = 16;
+  static __device__ __forceinline__ v4f mma(Frag a, Frag b, v4f c) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], b[j], c, 0, 0, 0);   // (k 4 (lane / 16) + j of both)
+    return c;
+  }
+};
+
+constexpr uint32_t kFewBlock = 512, kFewWaves = kFewBlock / 64;
+template <typename T, int TB, uint32_t PASS>
+__global__ __launch_bounds__(kFewBlock, 2) void lt_vocab_few_kernel(const VocabArgs a) {
+  typedef Narrow<T> M;
+  typedef typename M::Frag Frag;
+  constexpr uint32_t kWay = 8, V = 16 / sizeof(T);
+  __shared__ __attribute__((aligned(16))) char xs[kVocabFewBytes];
+  __shared__ float2 red[PASS == kVocabLogits ? kFewWaves * TB * 16 : 1];
+  const uint32_t n = PASS == kVocabLogits ? a.tokens : __builtin_amdgcn_readfirstlane(*a.count);
+  const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = __builtin_amdgcn_readfirstlane(tid / 64u), t16 = lane & 15u, group = lane >> 4;
+  const uint32_t row_bytes = (a.width * (uint32_t)sizeof(T) + 255u) & ~255u, chunks = a.width / V;
+  for (uint32_t e = tid; e < TB * 16u * chunks; e += kFewBlock) {
+    const uint32_t t = e / chunks, c = e - t * chunks;
+    *(uint4*)(xs + t * row_bytes + ((c ^ (t & 15u)) << 4)) = t < n ? *(const uint4*)((const T*)a.x + (uint64_t)t * a.width + c * V) : make_uint4(0u, 0u, 0u, 0u);
+  }
+  float top[TB], sum[TB], lse[TB], dloss[TB];
+  uint32_t label[TB];
+#pragma unroll
+  for (int b = 0; b < TB; ++b) {
+    const uint32_t t = b * 16u + t16;
+    top[b] = -INFINITY;
+    sum[b] = 0.0f;
+    label[b] = t < n ? (uint32_t)(PASS == kVocabLogits ? a.labels[t] : a.label[t]) - a.first : ~0u;
+    lse[b] = PASS == kVocabGrad && t < n ? a.lse_of[t] : 0.0f;
+    dloss[b] = PASS == kVocabGrad && t < n ? a.dloss_of[t] : 0.0f;
+  }
+  __syncthreads();
+  const uint32_t steps = a.width / M::kStep, units = ((PASS == kVocabGrad ? a.stride : a.rows) + 15u) / 16u, all = gridDim.x * kFewWaves;
+  // (rows of g up to its stride are zeros, and tokens up to a whole slab of them)
+  if constexpr (PASS == kVocabGrad && TB * 16 < 128 / sizeof(T)) {
+    const uint32_t each = a.stride / V, many = ((uint32_t)(128 / sizeof(T)) - TB * 16u) * each;
+    for (uint32_t e = blockIdx.x * kFewBlock + tid; e < many; e += gridDim.x * kFewBlock) *(uint4*)((T*)a.g + (uint64_t)(TB * 16u) * a.stride + (uint64_t)e * V) = make_uint4(0u, 0u, 0u, 0u);
+  }
+  auto fetch = [&](uint32_t unit, uint32_t s0, Frag(&f)[kWay]) __attribute__((always_inline)) {
+    const T* const row = (const T*)a.w + (uint64_t)min(unit * 16u + t16, a.rows - 1u) * a.width + group * V;
+#pragma unroll
+    for (uint32_t k = 0; k < kWay; ++k)
+      if (s0 + k < steps) f[k] = *(const Frag*)(row + (s0 + k) * M::kStep);
+  };
+  uint32_t unit = blockIdx.x * kFewWaves + wave, s0 = 0u;
+  Frag f[kWay], g[kWay];
+  v4f acc[TB];
+#pragma unroll
+  for (int b = 0; b < TB; ++b) acc[b] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+  if (unit < units) fetch(unit, 0u, f);
+  while (unit < units) {
+    const bool last = s0 + kWay >= steps;
+    const uint32_t next = last ? unit + all : unit, next_s = last ? 0u : s0 + kWay;
+    if (next < units) fetch(next, next_s, g);
+#pragma unroll
+    for (uint32_t k = 0; k < kWay; ++k) {
+      if (s0 + k >= steps) break;
+      const uint32_t c = (s0 + k) * 4u + group;
+#pragma unroll
+      for (int b = 0; b < TB; ++b) acc[b] = M::mma(f[k], *(const Frag*)(xs + (b * 16u + t16) * row_bytes + ((c ^ t16) << 4)), acc[b]);
+    }
+    if (last) {
+      const uint32_t row = unit * 16u + group * 4u;
+#pragma unroll
+      for (int b = 0; b < TB; ++b) {
+        if constexpr (PASS == kVocabLogits) {
+          float here = top[b];
+#pragma unroll
+          for (uint32_t r = 0; r < 4u; ++r) {
+            if (row + r == label[b] && row + r < a.rows) a.picked[b * 16u + t16] = acc[b][r];
+            if (row + r >= a.rows) acc[b][r] = -INFINITY;
+            here = fmaxf(here, acc[b][r]);
+          }
+          const float from = here == -INFINITY ? 0.0f : here;
+          sum[b] *= __builtin_amdgcn_exp2f((top[b] - from) * kLog2e);
+#pragma unroll
+          for (uint32_t r = 0; r < 4u; ++r) sum[b] += __builtin_amdgcn_exp2f((acc[b][r] - from) * kLog2e);
+          top[b] = here;
+        } else {
+          const uint32_t t = b * 16u + t16;
+          float v[4];
+#pragma unroll
+          for (uint32_t r = 0; r < 4u; ++r) {
+            v[r] = (__builtin_amdgcn_exp2f((acc[b][r] - lse[b]) * kLog2e) - (row + r == label[b] ? 1.0f : 0.0f)) * dloss[b];
+            if (row + r >= a.rows || t >= n) v[r] = 0.0f;
+          }
+          T* const at = (T*)a.g + (uint64_t)t * a.stride + row;
+          if constexpr (sizeof(T) == 4) *(v4f*)at = v4f{v[0], v[1], v[2], v[3]};
+          else *(v4bf*)at = v4bf{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
+        }
+        acc[b] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+      }
+    }
+    unit = next;
+    s0 = next_s;
+#pragma unroll
+    for (uint32_t k = 0; k < kWay; ++k) f[k] = g[k];
+  }
+  if constexpr (PASS == kVocabLogits) {
+#pragma unroll
+    for (int b = 0; b < TB; ++b) {
+#pragma unroll
+      for (uint32_t o = 16u; o < 64u; o *= 2u) {
+        const float other = __shfl_xor(top[b], o), more = __shfl_xor(sum[b], o), both = fmaxf(top[b], other), from = both == -INFINITY ? 0.0f : both;
+        sum[b] = sum[b] * __builtin_amdgcn_exp2f((top[b] - from) * kLog2e) + more * __builtin_amdgcn_exp2f((other - from) * kLog2e);
+        top[b] = both;
+      }
+      if (group == 0u) red[(wave * TB + b) * 16u + t16] = make_float2(top[b], sum[b]);
+    }
+    __syncthreads();
+    if (tid < TB * 16u) {
+      float most = -INFINITY, total = 0.0f;
+#pragma unroll
+      for (uint32_t w = 0; w < kFewWaves; ++w) most = fmaxf(most, red[w * TB * 16u + tid].x);
+      const float from = most == -INFINITY ? 0.0f : most;
+#pragma unroll
+      for (uint32_t w = 0; w < kFewWaves; ++w) total += red[w * TB * 16u + tid].y * __builtin_amdgcn_exp2f((red[w * TB * 16u + tid].x - from) * kLog2e);
+      float* const parts = a.parts + (uint64_t)blockIdx.x * 2u * a.padded;
+      parts[tid] = most;
+      parts[a.padded + tid] = total;
+    }
+  }
+}
+
 // ---- losses: a token's maxima and sums of all tiles, sixty-four tokens a workgroup, a sixteenth of the tiles a thread --------
 constexpr uint32_t kLossBlock = 1024;
 __global__ __launch_bounds__(kLossBlock) void lt_vocab_loss_kernel(const VocabArgs a) {
   constexpr uint32_t kShares = kLossBlock / 64u, kWay = 8;
   __shared__ float2 red[kShares][64];
   const uint32_t lane = threadIdx.x & 63u, share = threadIdx.x / 64u, token = blockIdx.x * 64u + lane;
-  const uint32_t n = *a.count;
+  const uint32_t n = a.few ? a.tokens : *a.count;
   if (blockIdx.x * 64u >= n) return;
   float top = -INFINITY, sum = 0.0f;
   if (token < n)
@@ -511,9 +650,10 @@ __global__ __launch_bounds__(kLossBlock) void lt_vocab_loss_kernel(const VocabAr
   sum = 0.0f;
   for (uint32_t w = 0; w < kShares; ++w) sum += red[w][lane].y * __builtin_amdgcn_exp2f((red[w][lane].x - from) * kLog2e);
   const float lse = from + kLn2 * __builtin_amdgcn_logf(sum);
-  const uint32_t i = (uint32_t)a.row_of[token];
-  if (a.loss) a.loss[i] = lse - a.picked[token];
-  if (a.lse_out) a.lse_out[i] = lse;
+  const uint32_t i = a.few ? token : (uint32_t)a.row_of[token];
+  const bool counts = !a.few || (uint32_t)a.labels[i] < a.vocab;
+  if (a.loss) a.loss[i] = counts ? lse - a.picked[token] : 0.0f;
+  if (a.lse_out) a.lse_out[i] = counts ? lse : 0.0f;
 }
 
 // ---- dx: the workgroups' sums of a token, four columns a thread (packed rows are whole slabs), one wave a row -----------------
@@ -559,6 +699,18 @@ hipError_t launch_product(const VocabArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
+template <typename T, uint32_t PASS>
+hipError_t launch_few(const VocabArgs& a, hipStream_t s) {
+  const uint32_t blocks = vocab_few_blocks(a.tokens);
+  if (a.tokens == 0u) return hipSuccess;
+  if (!vocab_few(a.tokens, a.width, sizeof(T)) || a.width % (128 / sizeof(T)) != 0u || a.w_stride != a.width) return hipErrorInvalidValue;
+  if (((uintptr_t)a.x & 15u) || ((uintptr_t)a.w & 15u) || ((uintptr_t)a.g & 15u)) return hipErrorInvalidValue;
+  if (blocks == 1u) LT_LAUNCH((lt_vocab_few_kernel<T, 1, PASS>), dim3(kVocabFewGrid), dim3(kFewBlock), s, a);
+  else if (blocks == 2u) LT_LAUNCH((lt_vocab_few_kernel<T, 2, PASS>), dim3(kVocabFewGrid), dim3(kFewBlock), s, a);
+  else LT_LAUNCH((lt_vocab_few_kernel<T, 4, PASS>), dim3(kVocabFewGrid), dim3(kFewBlock), s, a);
+  return hipGetLastError();
+}
+
 template <typename T, int B, int WM, int WN>
 hipError_t launch_of(const VocabArgs& a, hipStream_t s) {
   const dim3 block(kRowsBlock);
@@ -571,8 +723,12 @@ hipError_t launch_of(const VocabArgs& a, hipStream_t s) {
       else LT_LAUNCH((lt_vocab_pack_kernel<T, false>), dim3((rows + 3u) / 4u), block, s, a);
       return hipGetLastError();
     }
-    case kVocabLogits: return launch_product<T, B, WM, WN, kVocabLogits>(a, s);
-    case kVocabGrad: return launch_product<T, B, WM, WN, kVocabGrad>(a, s);
+    case kVocabLogits:
+      if (a.few) return launch_few<T, kVocabLogits>(a, s);
+      return launch_product<T, B, WM, WN, kVocabLogits>(a, s);
+    case kVocabGrad:
+      if (a.few) return launch_few<T, kVocabGrad>(a, s);
+      return launch_product<T, B, WM, WN, kVocabGrad>(a, s);
     case kVocabDx: return launch_product<T, B, WM, WN, kVocabDx>(a, s);
     case kVocabDw: return launch_product<T, B, WM, WN, kVocabDw>(a, s);
     case kVocabDxOut:

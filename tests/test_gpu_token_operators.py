@@ -240,7 +240,7 @@ def grads_bound(x, w, labels, lse, dloss, dtype):
 
 
 ENTROPIES = [((1,), 1, 1), ((1,), 2, 3), ((1,), 300, 64), ((3,), 257, 8), ((2, 3), 1000, 100), ((16,), 4000, 256), ((17,), 513, 96), ((5, 13), 255, 331), ((300,), 700, 200), ((257,), 256, 64),
-             ((64,), 10007, 72), ((600,), 300, 520), ((33,), 9000, 1024)]
+             ((64,), 10007, 72), ((600,), 300, 520), ((33,), 9000, 1024), ((1,), 5003, 1024), ((16,), 777, 128), ((17,), 4100, 192), ((40,), 3000, 512), ((64,), 20000, 64), ((65,), 1000, 64), ((5,), 9, 2048)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
