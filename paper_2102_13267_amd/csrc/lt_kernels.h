@@ -475,14 +475,15 @@ struct DropoutArgs {
 // Logits of a piece of the vocabulary are formed as [row of w][token]: kVocabLogits leaves every token's maximum and sum of exponentials of a
 // tile of rows, kVocabLoss joins them; kVocabGrad writes g of a piece, [token][row of the piece], from which kVocabDx adds the piece's
 // share of dx to sums in fp32 (of which kVocabDxOut makes dx) and kVocabDw makes the piece's rows of dw.
-enum : uint32_t { kVocabTokens = 0, kVocabPack, kVocabLogits, kVocabLoss, kVocabGrad, kVocabDx, kVocabDw, kVocabDxOut };
+// Logits that are kept for the gradient (kVocabLogits writes them as fp32 too) are made into g by kVocabKept.
+enum : uint32_t { kVocabTokens = 0, kVocabPack, kVocabLogits, kVocabLoss, kVocabGrad, kVocabDx, kVocabDw, kVocabDxOut, kVocabKept };
 struct VocabArgs {
   uint32_t pass, dtype;
   uint32_t tokens, padded;     // padded: to whole tiles of 256
   uint32_t vocab, dim, width;  // width: dim padded to whole slabs, the stride of packed rows
   uint32_t first, rows;        // this piece of w: its first row, and how many
   uint32_t stride;             // of g: the rows of the largest piece, padded to whole tiles of 256
-  uint32_t tile;               // rows (and tokens) of a tile of kVocabLogits: 128 or 256
+  uint32_t tile;               // of a product: 256, or 128 rows and columns
   uint32_t tiles_all;          // of kVocabLogits, over all pieces
   uint32_t splits;             // of kVocabDx: workgroups that share a tile, each with sums of its own
   uint32_t add;                // kVocabDx: not the first piece
@@ -497,9 +498,10 @@ struct VocabArgs {
   // by packed token
   uint32_t* count;             // how many there are
   int32_t *row_of, *label;
-  float *lse_of, *dloss_of, *picked;
+  float *lse_of, *picked;
   int32_t* packed_of;          // by token: its packed place, or -1
   float* parts;                // [tile of rows][2][padded]: maxima, sums of exponentials
+  float* logits;               // [padded][stride], or null
   void* g;
   float* sums;                 // [split][padded][width]
   void* packed;                // kVocabPack's result

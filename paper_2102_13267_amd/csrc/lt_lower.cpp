@@ -29,6 +29,7 @@
 #include <cmath>
 #include <cstdio>
 #include <functional>
+#include <map>
 #include <set>
 
 #include "lt_core.h"
@@ -2200,6 +2201,19 @@ struct Lowering {
     return true;
   }
 
+  // What a cross entropy leaves for its gradient in the same trace, by node: its tokens' lists, their packed rows, and its logits where
+  // they are kept.
+  struct EntropyShared {
+    int32_t lists = -1, packed_x = -1, logits = -1;
+  };
+  std::map<int32_t, EntropyShared> entropy_shared;
+  // the gradient of cross entropy `a` of the same operands, or -1
+  int32_t gradient_of(int32_t a) const {
+    for (int32_t u : users[a])
+      if (nd[u]->op == LT_OP_LINEAR_XENT_GRAD && rins[u][3] == Val{a, 1} && rins[u][0] == rins[a][0] && rins[u][1] == rins[a][1] && rins[u][2] == rins[a][2]) return u;
+    return -1;
+  }
+
   // The cross entropy of x w^T, or its gradient (lt_vocab.hip): tokens that count are packed, the vocabulary goes by in pieces.
   bool emit_linear_xent(int k, int32_t a) {
     const Node* an = nd[a];
@@ -2218,11 +2232,16 @@ struct Lowering {
     args.width = (uint32_t)((args.dim + slab - 1) / slab * slab);
     const int32_t s_loss = grad ? -1 : storage_of[a][0], s_lse = grad ? -1 : storage_of[a][1], s_dx = grad ? storage_of[a][0] : -1, s_dw = grad ? storage_of[a][1] : -1;
     const uint64_t n = args.tokens, pad = args.padded, width = args.width;
+    if (grad) {
+      const Val d = rins[a][4];
+      args.rank0 = is_imm(d) || out_shape(d).empty();
+      if (!is_imm(d) && !operand_whole(d, &dloss)) return false;
+    }
     // rows of w that are no whole, aligned slabs are packed, a piece at a time
     // (a window along the first axis may start anywhere; tensors of their own start at 16 bytes)
     const bool pack_w = args.width != args.dim || w.byte_offset % 16 != 0;
     args.w_stride = args.width;
-    // a piece of g takes 256 MB, as many rows as that is, but 4096 at least
+    // A piece of g takes 128 MB, as many rows as that is, but 4096 at least.
     const uint64_t fit = std::max<uint64_t>(4096, ((uint64_t)128 << 20) / (std::max<uint64_t>(pad, 256) * e) & ~(uint64_t)255);
     const uint64_t fit_w = std::max<uint64_t>(4096, ((uint64_t)256 << 20) / (width * e) & ~(uint64_t)255);
     uint64_t piece = args.vocab;
@@ -2230,107 +2249,117 @@ struct Lowering {
     if (pack_w) piece = std::min(piece, fit_w);
     const uint32_t pieces = (uint32_t)((args.vocab + piece - 1) / piece);
     args.stride = (uint32_t)((piece + 255) & ~(uint64_t)255);
-    args.tile = dt == LT_BF16 ? 256u : 128u;
-    args.tiles_all = 0;
+    // Tiles of 256 x 256, one workgroup a compute unit, where every one gets a tile; else of 128 x 128, two.
+    auto tiles_of = [&](uint64_t rows, uint64_t columns, uint64_t t) { return (rows + t - 1) / t * ((columns + t - 1) / t); };
+    auto tile_for = [&](uint64_t rows, uint64_t columns) { return dt == LT_BF16 && tiles_of(rows, columns, 256) >= 256 ? 256u : 128u; };
+    args.tile = tile_for(piece, pad);
     // few tokens, whose rows of x fit in LDS, and rows of w that need no packing: w goes by once
-    const bool few = !pack_w && n > 0 && ltk::vocab_few(args.tokens, args.width, (uint32_t)e) && (grad || x.byte_offset % 16 == 0);
-    args.few = few;
-    // by packed token: row, label, lse, dloss, picked; their count; by token: packed place
-    const int32_t lists = temporary(4 * (5 * pad + pad + 64));
-    const int32_t packed_x = few && !grad ? -1 : temporary(pad * width * e);
+    args.few = !pack_w && n > 0 && ltk::vocab_few(args.tokens, args.width, (uint32_t)e) && (grad || x.byte_offset % 16 == 0);
+    const bool few_losses = args.few && !grad;   // (they are not packed)
+    // Tokens are packed once for a cross entropy and its gradient.  Where g is one piece, the logits that it is made of, as much memory or
+    // twice as much, are kept from one to the other if forming them again takes longer than their way to memory and back.
+    EntropyShared shared;
+    const int32_t source = grad ? rins[a][3].node : a, partner = grad ? a : merge && !few_losses ? gradient_of(a) : -1;
+    const bool given = grad && entropy_shared.count(source) && gradient_of(source) == a;
+    if (given) shared = entropy_shared[source];
+    else {
+      shared.lists = temporary(4 * (5 * pad + 64));
+      if (!few_losses) shared.packed_x = temporary(pad * width * e);
+      if (partner >= 0 && !grad) {
+        if (pieces == 1 && args.vocab <= fit && args.dim >= (dt == LT_F32 ? 128u : 1536u)) shared.logits = temporary(pad * args.stride * 4);
+        entropy_shared[a] = shared;
+        plan->merged = true;
+      }
+    }
+    const bool kept = given && shared.logits >= 0;
     const int32_t packed_w = pack_w ? temporary(piece * width * e) : -1;
     std::vector<uint32_t> first_tile;
     for (uint32_t p = 0; p < pieces; ++p) {
       first_tile.push_back(args.tiles_all);
       args.tiles_all += (uint32_t)((std::min<uint64_t>(piece, args.vocab - p * piece) + args.tile - 1) / args.tile);
     }
-    if (few) args.tiles_all = ltk::kVocabFewGrid;
+    if (few_losses) args.tiles_all = ltk::kVocabFewGrid;
     const int32_t parts = grad ? -1 : temporary(8 * (uint64_t)args.tiles_all * pad);
-    const int32_t g = grad ? temporary(pad * args.stride * e) : -1;
-    // few tiles of dx and a long sum: shared by as many workgroups as compute units are left without one, each with eight slabs at least
-    const uint64_t dx_tiles = pad / args.tile * ((args.width + args.tile - 1) / args.tile), slabs = args.stride / slab;
-    args.splits = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>({256 / std::max<uint64_t>(dx_tiles, 1), slabs / 8, 16}));
+    const int32_t g = !grad ? -1 : kept && dt == LT_F32 ? shared.logits : temporary(pad * args.stride * e);   // (fp32: in the logits' place)
+    // few tiles of dx and a long sum: shared by as many workgroups as there is room for, each with eight slabs at least
+    const uint64_t slabs = args.stride / slab;
+    auto splits_of = [&](uint64_t t) { return std::max<uint64_t>(1, std::min<uint64_t>({(t == 256 ? 256 : 512) / std::max<uint64_t>(tiles_of(pad, width, t), 1), slabs / 8, 16})); };
+    const uint32_t dx_tile = dt == LT_BF16 && tiles_of(pad, width, 256) * splits_of(256) >= 224 ? 256u : 128u;
+    args.splits = (uint32_t)splits_of(dx_tile);
     const int32_t sums = s_dx >= 0 ? temporary(4 * pad * width * args.splits) : -1;
-    auto list = [&](int l, size_t at, uint32_t which, bool write) { patch(l, at, lists, (int64_t)(4 * pad * which), write); };
-    auto all_lists = [&](int l, bool write) {
-      list(l, offsetof(ltk::VocabArgs, row_of), 0, write);
-      list(l, offsetof(ltk::VocabArgs, label), 1, write);
-      list(l, offsetof(ltk::VocabArgs, lse_of), 2, write);
-      list(l, offsetof(ltk::VocabArgs, dloss_of), 3, write);
-      list(l, offsetof(ltk::VocabArgs, picked), 4, write);
-      list(l, offsetof(ltk::VocabArgs, packed_of), 5, write);
-      list(l, offsetof(ltk::VocabArgs, count), 6, write);
-    };
     auto add = [&](uint32_t pass, uint64_t bytes, uint64_t flops = 0) {
       args.pass = pass;
       const int l = add_launch(L_VOCAB, k, args, bytes, flops);
-      all_lists(l, pass == ltk::kVocabTokens || pass == ltk::kVocabLogits);
+      // by packed token: row, label, lse, picked logit; by token: packed place; how many are packed
+      const size_t at[] = {offsetof(ltk::VocabArgs, row_of), offsetof(ltk::VocabArgs, label), offsetof(ltk::VocabArgs, lse_of),
+                           offsetof(ltk::VocabArgs, picked), offsetof(ltk::VocabArgs, packed_of), offsetof(ltk::VocabArgs, count)};
+      for (int64_t i = 0; i < 6; ++i) patch(l, at[i], shared.lists, (int64_t)(4 * pad) * i, pass == ltk::kVocabTokens || pass == ltk::kVocabLogits || pass == ltk::kVocabLoss);
       return l;
     };
     int l = 0;
-    if (grad) {
-      const Val d = rins[a][4];
-      args.rank0 = is_imm(d) || out_shape(d).empty();
-      if (!is_imm(d) && !operand_whole(d, &dloss)) return false;
-    }
-    if (grad || !few) {
-    l = add(ltk::kVocabTokens, 4 * n * (grad ? 4 : 2));
-    patch(l, offsetof(ltk::VocabArgs, labels), labels);
-    if (grad) {
-      patch(l, offsetof(ltk::VocabArgs, lse), lse);
-      if (dloss.storage >= 0) patch(l, offsetof(ltk::VocabArgs, dloss), dloss);
-      else patch_scalar(rins[a][4], l, offsetof(ltk::VocabArgs, dloss_value), &((ltk::VocabArgs*)plan->launches[l].args.data())->dloss_value);
-    } else {
+    if (!given && !few_losses) {
+      l = add(ltk::kVocabTokens, 4 * n * (grad ? 3 : 2));
+      patch(l, offsetof(ltk::VocabArgs, labels), labels);
+      if (grad) patch(l, offsetof(ltk::VocabArgs, lse), lse);
       if (s_loss >= 0) patch(l, offsetof(ltk::VocabArgs, loss), s_loss, 0, true);
       if (s_lse >= 0) patch(l, offsetof(ltk::VocabArgs, lse_out), s_lse, 0, true);
-    }
-    l = add(ltk::kVocabPack, 2 * n * args.dim * e);
-    patch(l, offsetof(ltk::VocabArgs, x), x);
-    patch(l, offsetof(ltk::VocabArgs, packed), packed_x, 0, true);
+      l = add(ltk::kVocabPack, 2 * n * args.dim * e);
+      patch(l, offsetof(ltk::VocabArgs, x), x);
+      patch(l, offsetof(ltk::VocabArgs, packed), shared.packed_x, 0, true);
     }
     for (uint32_t p = 0; p < pieces; ++p) {
       args.first = (uint32_t)(p * piece);
       args.rows = (uint32_t)std::min<uint64_t>(piece, args.vocab - args.first);
       args.add = p > 0;
       const uint64_t w_bytes = (uint64_t)args.rows * args.dim * e, x_bytes = n * args.dim * e, product = 2 * n * args.rows * args.dim;
-      if (pack_w) {
+      const int64_t w_at = (int64_t)(args.first * (uint64_t)args.dim * e);
+      if (pack_w && !(kept && s_dx < 0)) {
         args.pack_w = 1;
         l = add(ltk::kVocabPack, 2 * w_bytes);
         args.pack_w = 0;
-        patch(l, offsetof(ltk::VocabArgs, w), w.storage, w.byte_offset + (int64_t)(args.first * (uint64_t)args.dim * e));
+        patch(l, offsetof(ltk::VocabArgs, w), w.storage, w.byte_offset + w_at);
         patch(l, offsetof(ltk::VocabArgs, packed), packed_w, 0, true);
       }
       auto operands = [&](int at, bool reads_x, bool reads_w) {
-        if (reads_x && packed_x < 0) patch(at, offsetof(ltk::VocabArgs, x), x);
-        else if (reads_x) patch(at, offsetof(ltk::VocabArgs, x), packed_x, 0);
+        if (reads_x && few_losses) patch(at, offsetof(ltk::VocabArgs, x), x);
+        else if (reads_x) patch(at, offsetof(ltk::VocabArgs, x), shared.packed_x, 0);
         if (reads_w && pack_w) patch(at, offsetof(ltk::VocabArgs, w), packed_w, 0);
-        else if (reads_w) patch(at, offsetof(ltk::VocabArgs, w), w.storage, w.byte_offset + (int64_t)(args.first * (uint64_t)args.dim * e));
+        else if (reads_w) patch(at, offsetof(ltk::VocabArgs, w), w.storage, w.byte_offset + w_at);
       };
-      l = add(grad ? ltk::kVocabGrad : ltk::kVocabLogits, w_bytes + x_bytes, product);
-      operands(l, true, true);
-      if (few && !grad) patch(l, offsetof(ltk::VocabArgs, labels), labels);
       if (!grad) {
+        l = add(ltk::kVocabLogits, w_bytes + x_bytes, product);
+        operands(l, true, true);
+        if (few_losses) patch(l, offsetof(ltk::VocabArgs, labels), labels);
         patch(l, offsetof(ltk::VocabArgs, parts), parts, (int64_t)(8 * pad * first_tile[p]), true);
+        if (shared.logits >= 0) patch(l, offsetof(ltk::VocabArgs, logits), shared.logits, 0, true);
         continue;
       }
+      args.tile = tile_for(args.rows, pad);
+      l = kept ? add(ltk::kVocabKept, n * args.rows * (4 + e)) : add(ltk::kVocabGrad, w_bytes + x_bytes, product);
+      if (kept) patch(l, offsetof(ltk::VocabArgs, logits), shared.logits, 0);
+      else operands(l, true, true);
+      if (dloss.storage >= 0) patch(l, offsetof(ltk::VocabArgs, dloss), dloss);
+      else patch_scalar(rins[a][4], l, offsetof(ltk::VocabArgs, dloss_value), &((ltk::VocabArgs*)plan->launches[l].args.data())->dloss_value);
       patch(l, offsetof(ltk::VocabArgs, g), g, 0, true);
       if (s_dx >= 0) {
+        args.tile = dx_tile;
         l = add(ltk::kVocabDx, w_bytes + x_bytes, product);
         operands(l, false, true);
         patch(l, offsetof(ltk::VocabArgs, g), g, 0);
         patch(l, offsetof(ltk::VocabArgs, sums), sums, 0, true);
       }
       if (s_dw >= 0) {
+        args.tile = tile_for(args.rows, width);
         l = add(ltk::kVocabDw, w_bytes + x_bytes, product);
         operands(l, true, false);
         patch(l, offsetof(ltk::VocabArgs, g), g, 0);
-        patch(l, offsetof(ltk::VocabArgs, dw), s_dw, (int64_t)(args.first * (uint64_t)args.dim * e), true);
+        patch(l, offsetof(ltk::VocabArgs, dw), s_dw, w_at, true);
       }
     }
     if (!grad) {
       l = add(ltk::kVocabLoss, 8 * (uint64_t)args.tiles_all * n);
       patch(l, offsetof(ltk::VocabArgs, parts), parts, 0);
-      if (few) patch(l, offsetof(ltk::VocabArgs, labels), labels);
+      if (few_losses) patch(l, offsetof(ltk::VocabArgs, labels), labels);
       if (s_loss >= 0) patch(l, offsetof(ltk::VocabArgs, loss), s_loss, 0, true);
       if (s_lse >= 0) patch(l, offsetof(ltk::VocabArgs, lse_out), s_lse, 0, true);
     } else if (s_dx >= 0) {

@@ -45,7 +45,6 @@ __global__ __launch_bounds__(kTokensBlock) void lt_vocab_tokens_kernel(const Voc
       a.row_of[p] = (int32_t)i;
       a.label[p] = label;
       if (a.lse) a.lse_of[p] = a.lse[i];
-      if (a.lse) a.dloss_of[p] = a.dloss ? a.dloss[a.rank0 ? 0u : i] : a.dloss_value;
     } else {
       if (a.loss) a.loss[i] = 0.0f;
       if (a.lse_out) a.lse_out[i] = 0.0f;
@@ -53,9 +52,15 @@ __global__ __launch_bounds__(kTokensBlock) void lt_vocab_tokens_kernel(const Voc
   }
   for (uint32_t p = all + threadIdx.x; p < a.padded; p += kTokensBlock) {
     a.label[p] = -1;
-    if (a.lse) a.lse_of[p] = a.dloss_of[p] = 0.0f;
+    a.row_of[p] = 0;
+    a.lse_of[p] = 0.0f;
   }
   if (threadIdx.x == 0u) *a.count = all;
+}
+
+// dloss of a packed token
+__device__ __forceinline__ float dloss_of(const VocabArgs& a, uint32_t token) {
+  return a.dloss ? a.dloss[a.rank0 ? 0 : a.row_of[token]] : a.dloss_value;
 }
 
 // ---- rows one behind the other, padded to whole slabs: one wave a row ------------------------------------
@@ -152,6 +157,8 @@ template <> struct Mma<float> {
     return c;
   }
 };
+
+typedef uint32_t AnyWhere __attribute__((ext_vector_type(4), aligned(2)));
 
 template <int N> struct Num {
   static constexpr int value = N;
@@ -291,7 +298,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void lt_vocab_product_kernel(const
     const uint32_t token = tile_n + wn * (BN / WN) + lane % X + j * X;
     label[j] = (uint32_t)a.label[token] - (a.first + tile_m) - wm * (BM / WM);   // (of this wave's rows)
     lse[j] = PASS == kVocabGrad ? a.lse_of[token] : 0.0f;
-    dloss[j] = PASS == kVocabGrad ? a.dloss_of[token] : 0.0f;
+    dloss[j] = PASS == kVocabGrad ? dloss_of(a, token) : 0.0f;
   }
 #pragma unroll
   for (int i = 0; i < MB; ++i)
@@ -341,6 +348,13 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void lt_vocab_product_kernel(const
 
   if constexpr (PASS == kVocabLogits) {
     const bool edge = tile_m + BM > m;
+    if (a.logits) {
+#pragma unroll
+      for (int j = 0; j < NB; ++j) {
+        float* const row = a.logits + (uint64_t)(tile_n + y0 + j * X) * a.stride + tile_m;
+        each_quad([&](int i, uint32_t q, uint32_t x) { *(v4f*)(row + x) = v4f{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]}; });
+      }
+    }
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
       const uint32_t y = y0 + j * X, token = tile_n + y;
@@ -462,12 +476,14 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void lt_vocab_product_kernel(const
       } else {
         const uint32_t rows = min(kHalf, n > from ? n - from : 0u), cols = min((uint32_t)BM, a.dim > tile_m ? a.dim - tile_m : 0u);
         T* const dw = (T*)a.dw + (uint64_t)from * a.dim + tile_m;
-        if (((uintptr_t)a.dw & 15u) == 0u && a.dim % V == 0u) {
-          for (uint32_t e = own_tid; e < rows * kChunks; e += kThreads)
-            if (e % kChunks * V < cols) *(uint4*)(dw + (uint64_t)(e / kChunks) * a.dim + e % kChunks * V) = *(const uint4*)(out + e / kChunks * kPad + e % kChunks * V);
-        } else {
-          for (uint32_t e = own_tid; e < rows * BM; e += kThreads)
-            if (e % BM < cols) dw[(uint64_t)(e / BM) * a.dim + e % BM] = out[e / BM * kPad + e % BM];
+        // (sixteen bytes wherever they start: the hardware takes them)
+        for (uint32_t e = own_tid; e < rows * kChunks; e += kThreads) {
+          const uint32_t y = e / kChunks, x = e % kChunks * V;
+          if (x >= cols) continue;
+          T* const to = dw + (uint64_t)y * a.dim + x;
+          if (x + V <= cols) *(AnyWhere*)to = *(const AnyWhere*)(out + y * kPad + x);
+          else
+            for (uint32_t k = 0; x + k < cols; ++k) to[k] = out[y * kPad + x + k];
         }
       }
     }
@@ -520,7 +536,7 @@ __global__ __launch_bounds__(kFewBlock, 2) void lt_vocab_few_kernel(const VocabA
     sum[b] = 0.0f;
     label[b] = t < n ? (uint32_t)(PASS == kVocabLogits ? a.labels[t] : a.label[t]) - a.first : ~0u;
     lse[b] = PASS == kVocabGrad && t < n ? a.lse_of[t] : 0.0f;
-    dloss[b] = PASS == kVocabGrad && t < n ? a.dloss_of[t] : 0.0f;
+    dloss[b] = PASS == kVocabGrad && t < n ? dloss_of(a, t) : 0.0f;
   }
   __syncthreads();
   const uint32_t steps = a.width / M::kStep, units = ((PASS == kVocabGrad ? a.stride : a.rows) + 15u) / 16u, all = gridDim.x * kFewWaves;
@@ -652,8 +668,29 @@ __global__ __launch_bounds__(kLossBlock) void lt_vocab_loss_kernel(const VocabAr
   const float lse = from + kLn2 * __builtin_amdgcn_logf(sum);
   const uint32_t i = a.few ? token : (uint32_t)a.row_of[token];
   const bool counts = !a.few || (uint32_t)a.labels[i] < a.vocab;
+  if (!a.few) a.lse_of[token] = lse;   // (for a gradient that shares the lists)
   if (a.loss) a.loss[i] = counts ? lse - a.picked[token] : 0.0f;
   if (a.lse_out) a.lse_out[i] = counts ? lse : 0.0f;
+}
+
+// ---- g from logits that were kept: one wave 256 of a token's, up to whole tiles of tokens and rows -------------------
+template <typename T>
+__global__ __launch_bounds__(kRowsBlock) void lt_vocab_kept_kernel(const VocabArgs a) {
+  const uint32_t tiles = a.stride / 256u, unit = blockIdx.x * (kRowsBlock / 64u) + threadIdx.x / 64u, lane = threadIdx.x & 63u;
+  const uint32_t token = unit / tiles, row = (unit - token * tiles) * 256u + lane * 4u, n = *a.count;
+  if (token >= ((n + kVocabTile - 1u) & ~(kVocabTile - 1u))) return;
+  const uint64_t at = (uint64_t)token * a.stride + row;
+  v4f v = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (token < n) {
+    const v4f l = *(const v4f*)(a.logits + at);
+    const uint32_t label = (uint32_t)a.label[token] - a.first;
+    const float lse = a.lse_of[token], dloss = dloss_of(a, token);
+#pragma unroll
+    for (uint32_t r = 0; r < 4u; ++r)
+      if (row + r < a.rows) v[r] = (__builtin_amdgcn_exp2f((l[r] - lse) * kLog2e) - (row + r == label ? 1.0f : 0.0f)) * dloss;
+  }
+  if constexpr (sizeof(T) == 4) *(v4f*)((float*)a.g + at) = v;
+  else *(v4bf*)((__bf16*)a.g + at) = v4bf{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
 }
 
 // ---- dx: the workgroups' sums of a token, four columns a thread (packed rows are whole slabs), one wave a row -----------------
@@ -689,7 +726,7 @@ hipError_t launch_product(const VocabArgs& a, hipStream_t s) {
   if (tiles == 0) return hipSuccess;
   if (tiles >= (uint64_t)1 << 31) return hipErrorInvalidValue;
   // as many workgroups as run at once: one a compute unit, or two where LDS holds two
-  const uint64_t grid = std::min<uint64_t>((tiles + 7) / 8 * 8, sizeof(T) == 4 ? 512 : 256);
+  const uint64_t grid = std::min<uint64_t>((tiles + 7) / 8 * 8, B == 256 ? 256 : 512);
   if (((uintptr_t)a.x & 15u) || ((uintptr_t)a.w & 15u) || ((uintptr_t)a.g & 15u)) return hipErrorInvalidValue;
   LT_LAUNCH((lt_vocab_product_kernel<T, B, B, WM, WN, PASS>), dim3((uint32_t)grid), dim3(WM * WN * 64), s, a);
   static const char* const names[] = {"", "", "logits", "", "grad", "dx", "dw"};
@@ -731,6 +768,13 @@ hipError_t launch_of(const VocabArgs& a, hipStream_t s) {
       return launch_product<T, B, WM, WN, kVocabGrad>(a, s);
     case kVocabDx: return launch_product<T, B, WM, WN, kVocabDx>(a, s);
     case kVocabDw: return launch_product<T, B, WM, WN, kVocabDw>(a, s);
+    case kVocabKept: {
+      const uint64_t grid = (uint64_t)a.padded * (a.stride / 256u) / 4u;   // (padded: a multiple of 256)
+      if (grid == 0) return hipSuccess;
+      if (grid >= (uint64_t)1 << 24) return hipErrorInvalidValue;
+      LT_LAUNCH(lt_vocab_kept_kernel<T>, dim3((uint32_t)grid), block, s, a);
+      return hipGetLastError();
+    }
     case kVocabDxOut:
       if (a.tokens > 0) LT_LAUNCH(lt_vocab_dx_kernel<T>, dim3((a.tokens + 3u) / 4u), block, s, a);
       return hipGetLastError();
@@ -748,7 +792,7 @@ hipError_t launch_vocab(const void* args, hipStream_t s) {
     if (a.padded > 0) LT_LAUNCH(lt_vocab_loss_kernel, dim3(a.padded / 64u), dim3(kLossBlock), s, a);
     return hipGetLastError();
   }
-  if (a.dtype == kBF16) return launch_of<__bf16, 256, 2, 4>(a, s);
+  if (a.dtype == kBF16) return a.tile == 256u ? launch_of<__bf16, 256, 2, 4>(a, s) : launch_of<__bf16, 128, 2, 2>(a, s);
   return a.dtype == kF32 ? launch_of<float, 128, 2, 2>(a, s) : hipErrorInvalidValue;
 }
 
