@@ -473,8 +473,9 @@ struct DropoutArgs {
 // Tokens whose label is a row of w are packed first (kVocabTokens: where each goes, kVocabPack: their rows of x, padded with zeros
 // to whole slabs of 128 bytes); the products then run over those alone, as many as the device has counted.
 // Logits of a piece of the vocabulary are formed as [row of w][token]: kVocabLogits leaves every token's maximum and sum of exponentials of a
-// tile of rows, kVocabLoss joins them; kVocabGrad writes g of a piece, [token][row of the piece], from which kVocabDx adds the piece's
-// share of dx to sums in fp32 (of which kVocabDxOut makes dx) and kVocabDw makes the piece's rows of dw.
+// tile of rows, kVocabLoss joins them; kVocabGrad writes g = exp(l - lse) - [label] of a piece, [token][row of the piece], from which kVocabDx adds
+// the piece's share of dx to sums in fp32 (of which kVocabDxOut makes dx) and kVocabDw makes the piece's rows of dw.  dloss stays out of g: an
+// entry of -1 that little is added to is then exact in bf16, and one number is a factor of the results.
 // Logits that are kept for the gradient (kVocabLogits writes them as fp32 too) are made into g by kVocabKept.
 enum : uint32_t { kVocabTokens = 0, kVocabPack, kVocabLogits, kVocabLoss, kVocabGrad, kVocabDx, kVocabDw, kVocabDxOut, kVocabKept };
 struct VocabArgs {
@@ -484,12 +485,13 @@ struct VocabArgs {
   uint32_t first, rows;        // this piece of w: its first row, and how many
   uint32_t stride;             // of g: the rows of the largest piece, padded to whole tiles of 256
   uint32_t tile;               // of a product: 256, or 128 rows and columns
-  uint32_t tiles_all;          // of kVocabLogits, over all pieces
+  uint32_t tiles, last;        // kVocabLoss: tiles of rows of this piece, and whether it is the last one
   uint32_t splits;             // of kVocabDx: workgroups that share a tile, each with sums of its own
-  uint32_t add;                // kVocabDx: not the first piece
+  uint32_t add;                // kVocabDx, kVocabLoss: not the first piece
   uint32_t pack_w;             // kVocabPack: rows of w, not tokens' rows of x
   uint32_t w_stride;           // of w's rows as the products read them
   uint32_t few;                // kVocabLogits, kVocabGrad: few tokens (and kVocabLogits, kVocabLoss: not packed)
+  uint32_t weigh;              // kVocabPack: rows of x times dloss
   uint32_t rank0;              // dloss is one number, in dloss_value unless dloss is set
   float dloss_value;
   const void *x, *w;           // as they are, or packed (kVocabPack: what is packed)
@@ -500,7 +502,7 @@ struct VocabArgs {
   int32_t *row_of, *label;
   float *lse_of, *picked;
   int32_t* packed_of;          // by token: its packed place, or -1
-  float* parts;                // [tile of rows][2][padded]: maxima, sums of exponentials
+  float* parts;                // [2][padded]: maxima and sums of exponentials; kVocabLogits: of its tiles; kVocabLoss: of the pieces so far, then of the tiles
   float* logits;               // [padded][stride], or null
   void* g;
   float* sums;                 // [split][padded][width]

@@ -2246,6 +2246,7 @@ struct Lowering {
     const uint64_t fit_w = std::max<uint64_t>(4096, ((uint64_t)256 << 20) / (width * e) & ~(uint64_t)255);
     uint64_t piece = args.vocab;
     if (grad) piece = std::min(piece, fit);
+    else piece = std::min<uint64_t>(piece, std::max<uint64_t>(4096, ((uint64_t)256 << 20) / (8 * std::max<uint64_t>(pad, 256)) * 128 & ~(uint64_t)255));   // (so much for maxima and sums)
     if (pack_w) piece = std::min(piece, fit_w);
     const uint32_t pieces = (uint32_t)((args.vocab + piece - 1) / piece);
     args.stride = (uint32_t)((piece + 255) & ~(uint64_t)255);
@@ -2273,13 +2274,9 @@ struct Lowering {
     }
     const bool kept = given && shared.logits >= 0;
     const int32_t packed_w = pack_w ? temporary(piece * width * e) : -1;
-    std::vector<uint32_t> first_tile;
-    for (uint32_t p = 0; p < pieces; ++p) {
-      first_tile.push_back(args.tiles_all);
-      args.tiles_all += (uint32_t)((std::min<uint64_t>(piece, args.vocab - p * piece) + args.tile - 1) / args.tile);
-    }
-    if (few_losses) args.tiles_all = ltk::kVocabFewGrid;
-    const int32_t parts = grad ? -1 : temporary(8 * (uint64_t)args.tiles_all * pad);
+    // maxima and sums of a piece's tiles, behind those of the pieces before it
+    auto parts_of = [&](uint64_t rows) { return few_losses ? (uint64_t)ltk::kVocabFewGrid : (rows + args.tile - 1) / args.tile; };
+    const int32_t parts = grad ? -1 : temporary(8 * pad * (1 + parts_of(piece)));
     const int32_t g = !grad ? -1 : kept && dt == LT_F32 ? shared.logits : temporary(pad * args.stride * e);   // (fp32: in the logits' place)
     // few tiles of dx and a long sum: shared by as many workgroups as there is room for, each with eight slabs at least
     const uint64_t slabs = args.stride / slab;
@@ -2307,6 +2304,21 @@ struct Lowering {
       patch(l, offsetof(ltk::VocabArgs, x), x);
       patch(l, offsetof(ltk::VocabArgs, packed), shared.packed_x, 0, true);
     }
+    auto weight = [&](int at) {
+      if (dloss.storage >= 0) patch(at, offsetof(ltk::VocabArgs, dloss), dloss);
+      else patch_scalar(rins[a][4], at, offsetof(ltk::VocabArgs, dloss_value), &((ltk::VocabArgs*)plan->launches[at].args.data())->dloss_value);
+    };
+    // dw takes the tokens' rows times what their losses count, where that is not the same number for all
+    int32_t weighed_x = shared.packed_x;
+    if (grad && s_dw >= 0 && !args.rank0) {
+      weighed_x = temporary(pad * width * e);
+      args.weigh = 1;
+      l = add(ltk::kVocabPack, 2 * n * args.dim * e);
+      args.weigh = 0;
+      weight(l);
+      patch(l, offsetof(ltk::VocabArgs, x), x);
+      patch(l, offsetof(ltk::VocabArgs, packed), weighed_x, 0, true);
+    }
     for (uint32_t p = 0; p < pieces; ++p) {
       args.first = (uint32_t)(p * piece);
       args.rows = (uint32_t)std::min<uint64_t>(piece, args.vocab - args.first);
@@ -2320,50 +2332,51 @@ struct Lowering {
         patch(l, offsetof(ltk::VocabArgs, w), w.storage, w.byte_offset + w_at);
         patch(l, offsetof(ltk::VocabArgs, packed), packed_w, 0, true);
       }
-      auto operands = [&](int at, bool reads_x, bool reads_w) {
+      auto operands = [&](int at, bool reads_x) {
         if (reads_x && few_losses) patch(at, offsetof(ltk::VocabArgs, x), x);
         else if (reads_x) patch(at, offsetof(ltk::VocabArgs, x), shared.packed_x, 0);
-        if (reads_w && pack_w) patch(at, offsetof(ltk::VocabArgs, w), packed_w, 0);
-        else if (reads_w) patch(at, offsetof(ltk::VocabArgs, w), w.storage, w.byte_offset + w_at);
+        if (pack_w) patch(at, offsetof(ltk::VocabArgs, w), packed_w, 0);
+        else patch(at, offsetof(ltk::VocabArgs, w), w.storage, w.byte_offset + w_at);
       };
       if (!grad) {
         l = add(ltk::kVocabLogits, w_bytes + x_bytes, product);
-        operands(l, true, true);
+        operands(l, true);
         if (few_losses) patch(l, offsetof(ltk::VocabArgs, labels), labels);
-        patch(l, offsetof(ltk::VocabArgs, parts), parts, (int64_t)(8 * pad * first_tile[p]), true);
+        patch(l, offsetof(ltk::VocabArgs, parts), parts, (int64_t)(8 * pad), true);
         if (shared.logits >= 0) patch(l, offsetof(ltk::VocabArgs, logits), shared.logits, 0, true);
+        args.tiles = (uint32_t)parts_of(args.rows);
+        args.last = p + 1 == pieces;
+        l = add(ltk::kVocabLoss, 8 * (uint64_t)args.tiles * n);
+        patch(l, offsetof(ltk::VocabArgs, parts), parts, 0, !args.last);
+        if (few_losses) patch(l, offsetof(ltk::VocabArgs, labels), labels);
+        if (args.last && s_loss >= 0) patch(l, offsetof(ltk::VocabArgs, loss), s_loss, 0, true);
+        if (args.last && s_lse >= 0) patch(l, offsetof(ltk::VocabArgs, lse_out), s_lse, 0, true);
         continue;
       }
       args.tile = tile_for(args.rows, pad);
       l = kept ? add(ltk::kVocabKept, n * args.rows * (4 + e)) : add(ltk::kVocabGrad, w_bytes + x_bytes, product);
       if (kept) patch(l, offsetof(ltk::VocabArgs, logits), shared.logits, 0);
-      else operands(l, true, true);
-      if (dloss.storage >= 0) patch(l, offsetof(ltk::VocabArgs, dloss), dloss);
-      else patch_scalar(rins[a][4], l, offsetof(ltk::VocabArgs, dloss_value), &((ltk::VocabArgs*)plan->launches[l].args.data())->dloss_value);
+      else operands(l, true);
       patch(l, offsetof(ltk::VocabArgs, g), g, 0, true);
       if (s_dx >= 0) {
         args.tile = dx_tile;
         l = add(ltk::kVocabDx, w_bytes + x_bytes, product);
-        operands(l, false, true);
+        operands(l, false);
         patch(l, offsetof(ltk::VocabArgs, g), g, 0);
         patch(l, offsetof(ltk::VocabArgs, sums), sums, 0, true);
       }
       if (s_dw >= 0) {
         args.tile = tile_for(args.rows, width);
         l = add(ltk::kVocabDw, w_bytes + x_bytes, product);
-        operands(l, true, false);
+        if (args.rank0) weight(l);
+        patch(l, offsetof(ltk::VocabArgs, x), weighed_x, 0);
         patch(l, offsetof(ltk::VocabArgs, g), g, 0);
         patch(l, offsetof(ltk::VocabArgs, dw), s_dw, w_at, true);
       }
     }
-    if (!grad) {
-      l = add(ltk::kVocabLoss, 8 * (uint64_t)args.tiles_all * n);
-      patch(l, offsetof(ltk::VocabArgs, parts), parts, 0);
-      if (few_losses) patch(l, offsetof(ltk::VocabArgs, labels), labels);
-      if (s_loss >= 0) patch(l, offsetof(ltk::VocabArgs, loss), s_loss, 0, true);
-      if (s_lse >= 0) patch(l, offsetof(ltk::VocabArgs, lse_out), s_lse, 0, true);
-    } else if (s_dx >= 0) {
+    if (s_dx >= 0) {
       l = add(ltk::kVocabDxOut, n * args.dim * (e + 4));
+      weight(l);
       patch(l, offsetof(ltk::VocabArgs, sums), sums, 0);
       patch(l, offsetof(ltk::VocabArgs, dx), s_dx, 0, true);
     }

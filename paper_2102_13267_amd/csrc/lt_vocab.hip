@@ -58,10 +58,8 @@ __global__ __launch_bounds__(kTokensBlock) void lt_vocab_tokens_kernel(const Voc
   if (threadIdx.x == 0u) *a.count = all;
 }
 
-// dloss of a packed token
-__device__ __forceinline__ float dloss_of(const VocabArgs& a, uint32_t token) {
-  return a.dloss ? a.dloss[a.rank0 ? 0 : a.row_of[token]] : a.dloss_value;
-}
+// the losses' gradient where it is one number
+__device__ __forceinline__ float one_dloss(const VocabArgs& a) { return a.dloss ? a.dloss[0] : a.dloss_value; }
 
 // ---- rows one behind the other, padded to whole slabs: one wave a row ------------------------------------
 constexpr uint32_t kRowsBlock = 256;
@@ -78,6 +76,14 @@ __global__ __launch_bounds__(kRowsBlock) void lt_vocab_pack_kernel(const VocabAr
     src = row < n ? (const T*)a.x + (uint64_t)a.row_of[row] * a.dim : nullptr;
   }
   T* out = (T*)a.packed + (uint64_t)row * a.width;
+  if (a.weigh) {   // (times dloss, rounded)
+    const float weight = src ? a.dloss[a.row_of[row]] : 0.0f;
+    for (uint32_t d = lane * 2u; d < a.width; d += 128u) {   // (a width is whole slabs)
+      out[d] = src && d < a.dim ? (T)((float)src[d] * weight) : (T)0.0f;
+      out[d + 1u] = src && d + 1u < a.dim ? (T)((float)src[d + 1u] * weight) : (T)0.0f;
+    }
+    return;
+  }
   if (VEC) {
     constexpr uint32_t V = 16 / sizeof(T);
     for (uint32_t d = lane * V; d < a.width; d += 64u * V) *(uint4*)(out + d) = src && d < a.dim ? *(const uint4*)(src + d) : make_uint4(0u, 0u, 0u, 0u);
@@ -169,7 +175,7 @@ __device__ __forceinline__ uint32_t uniform(uint32_t x) { return __builtin_amdgc
 // C = A B over tiles of BM x BN, WM x WN waves.
 //   kVocabLogits, kVocabGrad  A: rows of w [x][k], B: packed tokens [x][k], k = width; a lane has sixteen rows of one token
 //   kVocabDx                  A: rows of w [k][x] (columns of dim), B: g [token][row]: [x][k], k = rows of the piece
-//   kVocabDw                  A: packed tokens [k][x] (columns of dim), B: g [k][x] (rows of w), k = tokens; a lane has sixteen columns of one row
+//   kVocabDw                  A: packed tokens (times dloss, where they have one each) [k][x] (columns of dim), B: g [k][x] (rows of w), k = tokens; a lane has sixteen columns of one row
 template <typename T, int BM, int BN, int WM, int WN, uint32_t PASS>
 __global__ __launch_bounds__(WM * WN * 64, 2) void lt_vocab_product_kernel(const VocabArgs a) {
   constexpr bool kLogit = PASS == kVocabLogits || PASS == kVocabGrad, kAK = kLogit, kBK = PASS != kVocabDw;
@@ -292,13 +298,12 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void lt_vocab_product_kernel(const
   const uint32_t tile_m = tile.m, tile_n = tile.n, slabs = tile.slabs;
   // what the results of this tile's tokens will ask for: on its way under the products
   uint32_t label[NB];
-  float lse[NB], dloss[NB];
+  float lse[NB];
 #pragma unroll
   for (int j = 0; kLogit && j < NB; ++j) {
     const uint32_t token = tile_n + wn * (BN / WN) + lane % X + j * X;
     label[j] = (uint32_t)a.label[token] - (a.first + tile_m) - wm * (BM / WM);   // (of this wave's rows)
     lse[j] = PASS == kVocabGrad ? a.lse_of[token] : 0.0f;
-    dloss[j] = PASS == kVocabGrad ? dloss_of(a, token) : 0.0f;
   }
 #pragma unroll
   for (int i = 0; i < MB; ++i)
@@ -442,10 +447,6 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void lt_vocab_product_kernel(const
 #pragma unroll
             for (uint32_t r = 0; r < 4u; ++r) acc[i][j][4 * q + r] -= x + r - wm * (BM / WM) == label[j] ? 1.0f : 0.0f;
           });
-        each_quad([&](int i, uint32_t q, uint32_t) {
-#pragma unroll
-          for (uint32_t r = 0; r < 4u; ++r) acc[i][j][4 * q + r] *= dloss[j];
-        });
         if (edge)
           each_quad([&](int i, uint32_t q, uint32_t x) {
 #pragma unroll
@@ -454,6 +455,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void lt_vocab_product_kernel(const
           });
       }
     }
+    const float factor = PASS == kVocabDw && a.rank0 ? one_dloss(a) : 1.0f;
 #pragma unroll
     for (uint32_t half = 0; half < 2u; ++half) {
       if (half > 0u) __syncthreads();   // (the first half's rows have been read)
@@ -462,7 +464,8 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void lt_vocab_product_kernel(const
         for (int j = 0; j < NB; ++j)
           each_quad([&](int i, uint32_t q, uint32_t x) {
             T* const at = out + (y0 + j * X - half * kHalf) * kPad + x;
-            const v4f v = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+            v4f v = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+            if constexpr (PASS == kVocabDw) v *= factor;
             if constexpr (sizeof(T) == 4) *(v4f*)at = v;
             else *(v4bf*)at = v4bf{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
           });
@@ -527,7 +530,7 @@ __global__ __launch_bounds__(kFewBlock, 2) void lt_vocab_few_kernel(const VocabA
     const uint32_t t = e / chunks, c = e - t * chunks;
     *(uint4*)(xs + t * row_bytes + ((c ^ (t & 15u)) << 4)) = t < n ? *(const uint4*)((const T*)a.x + (uint64_t)t * a.width + c * V) : make_uint4(0u, 0u, 0u, 0u);
   }
-  float top[TB], sum[TB], lse[TB], dloss[TB];
+  float top[TB], sum[TB], lse[TB];
   uint32_t label[TB];
 #pragma unroll
   for (int b = 0; b < TB; ++b) {
@@ -536,7 +539,6 @@ __global__ __launch_bounds__(kFewBlock, 2) void lt_vocab_few_kernel(const VocabA
     sum[b] = 0.0f;
     label[b] = t < n ? (uint32_t)(PASS == kVocabLogits ? a.labels[t] : a.label[t]) - a.first : ~0u;
     lse[b] = PASS == kVocabGrad && t < n ? a.lse_of[t] : 0.0f;
-    dloss[b] = PASS == kVocabGrad && t < n ? dloss_of(a, t) : 0.0f;
   }
   __syncthreads();
   const uint32_t steps = a.width / M::kStep, units = ((PASS == kVocabGrad ? a.stride : a.rows) + 15u) / 16u, all = gridDim.x * kFewWaves;
@@ -590,7 +592,7 @@ __global__ __launch_bounds__(kFewBlock, 2) void lt_vocab_few_kernel(const VocabA
           float v[4];
 #pragma unroll
           for (uint32_t r = 0; r < 4u; ++r) {
-            v[r] = (__builtin_amdgcn_exp2f((acc[b][r] - lse[b]) * kLog2e) - (row + r == label[b] ? 1.0f : 0.0f)) * dloss[b];
+            v[r] = __builtin_amdgcn_exp2f((acc[b][r] - lse[b]) * kLog2e) - (row + r == label[b] ? 1.0f : 0.0f);
             if (row + r >= a.rows || t >= n) v[r] = 0.0f;
           }
           T* const at = (T*)a.g + (uint64_t)t * a.stride + row;
@@ -641,13 +643,13 @@ __global__ __launch_bounds__(kLossBlock) void lt_vocab_loss_kernel(const VocabAr
   if (blockIdx.x * 64u >= n) return;
   float top = -INFINITY, sum = 0.0f;
   if (token < n)
-    for (uint32_t t0 = share; t0 < a.tiles_all; t0 += kShares * kWay) {
+    for (uint32_t t0 = share + (a.add ? 0u : 1u); t0 <= a.tiles; t0 += kShares * kWay) {
       float m[kWay], s[kWay];
 #pragma unroll
       for (uint32_t k = 0; k < kWay; ++k) {   // (behind the last tile: nothing)
         const uint32_t t = t0 + k * kShares;
-        m[k] = t < a.tiles_all ? a.parts[(uint64_t)t * 2u * a.padded + token] : -INFINITY;
-        s[k] = t < a.tiles_all ? a.parts[((uint64_t)t * 2u + 1u) * a.padded + token] : 0.0f;
+        m[k] = t <= a.tiles ? a.parts[(uint64_t)t * 2u * a.padded + token] : -INFINITY;
+        s[k] = t <= a.tiles ? a.parts[((uint64_t)t * 2u + 1u) * a.padded + token] : 0.0f;
       }
       float both = top;
 #pragma unroll
@@ -665,6 +667,11 @@ __global__ __launch_bounds__(kLossBlock) void lt_vocab_loss_kernel(const VocabAr
   const float from = top == -INFINITY ? 0.0f : top;
   sum = 0.0f;
   for (uint32_t w = 0; w < kShares; ++w) sum += red[w][lane].y * __builtin_amdgcn_exp2f((red[w][lane].x - from) * kLog2e);
+  if (!a.last) {
+    a.parts[token] = top;
+    a.parts[a.padded + token] = sum;
+    return;
+  }
   const float lse = from + kLn2 * __builtin_amdgcn_logf(sum);
   const uint32_t i = a.few ? token : (uint32_t)a.row_of[token];
   const bool counts = !a.few || (uint32_t)a.labels[i] < a.vocab;
@@ -684,10 +691,10 @@ __global__ __launch_bounds__(kRowsBlock) void lt_vocab_kept_kernel(const VocabAr
   if (token < n) {
     const v4f l = *(const v4f*)(a.logits + at);
     const uint32_t label = (uint32_t)a.label[token] - a.first;
-    const float lse = a.lse_of[token], dloss = dloss_of(a, token);
+    const float lse = a.lse_of[token];
 #pragma unroll
     for (uint32_t r = 0; r < 4u; ++r)
-      if (row + r < a.rows) v[r] = (__builtin_amdgcn_exp2f((l[r] - lse) * kLog2e) - (row + r == label ? 1.0f : 0.0f)) * dloss;
+      if (row + r < a.rows) v[r] = __builtin_amdgcn_exp2f((l[r] - lse) * kLog2e) - (row + r == label ? 1.0f : 0.0f);
   }
   if constexpr (sizeof(T) == 4) *(v4f*)((float*)a.g + at) = v;
   else *(v4bf*)((__bf16*)a.g + at) = v4bf{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
@@ -701,12 +708,14 @@ __global__ __launch_bounds__(kRowsBlock) void lt_vocab_dx_kernel(const VocabArgs
   const int32_t p = a.packed_of[i];
   T* const out = (T*)a.dx + (uint64_t)i * a.dim;
   const bool whole = a.dim % 4u == 0u && ((uintptr_t)a.dx & 15u) == 0u;
+  const float weight = p < 0 ? 0.0f : a.rank0 ? one_dloss(a) : a.dloss[i];
   for (uint32_t d = lane * 4u; d < a.dim; d += 256u) {
     v4f v = {0.0f, 0.0f, 0.0f, 0.0f};
     if (p >= 0) {
       const float* from = a.sums + (uint64_t)p * a.width + d;
 #pragma unroll 8
       for (uint32_t s = 0; s < a.splits; ++s, from += (uint64_t)a.padded * a.width) v += *(const v4f*)from;
+      v *= weight;
     }
     if (whole) {
       if constexpr (sizeof(T) == 4) *(v4f*)(out + d) = v;

@@ -6,8 +6,9 @@ Dropout: the factor's rounding, the product's, the sum's: 2 E |x factor| + (E + 
 Cross entropy: a logit is a sum of dim products: dl = (dim + 1) E max_v sum |x w| off at most.  exp(l - top) has its argument rounded
 three times (the difference, the factor, the product): 3 E |l - top|, at most 3 E span, and two roundings of its own; a sum's path has 64 additions in a lane, a tile's
 few, and one per 16 tiles of 128: depth = 96 + V / 2048.  So lse is off by dl + (3 span + depth + 8) E + 3 E |lse| (its logarithm's), called dlse, and
-loss by dlse + dl + E |loss|.  The gradient takes lse as given: p is off by p (dl + (3 |l - lse| + 4) E), g = (p - [label]) dloss by |dloss| times that, two
-roundings of its own and R |g| where it is rounded to the type; dx and dw by |dg| |w| + n E |g| |w| + R |ref|, n the length of the sum."""
+loss by dlse + dl + E |loss|.  The gradient takes lse as given: p is off by p (dl + (3 |l - lse| + 4) E), p - [label] by that, a rounding E and one to
+the type R, and g by |dloss| times that; dx and dw by |dg| |w| + (n + 2) E |g| |w| + R |ref|, n the length of the sum, and dw, where every token has a dloss of its own
+and x dloss is rounded, by R |g| |x| more."""
 import numpy as np
 import pytest
 import torch
@@ -233,9 +234,9 @@ def grads_bound(x, w, labels, lse, dloss, dtype):
     g = p.copy()
     g[np.arange(len(g)), labels[there]] -= 1
     g *= d
-    dg = np.abs(d) * p * (dl + (3 * np.abs(logits - s) + 4) * E24) + (2 * E24 + (HALF[dtype] if dtype == "bf16" else 0)) * np.abs(g)
-    bx = dg @ np.abs(W) + len(w) * E24 * (np.abs(g) @ np.abs(W)) + HALF[dtype] * np.abs(g @ W) + TINY
-    bw = dg.T @ np.abs(X) + len(g) * E24 * (np.abs(g).T @ np.abs(X)) + HALF[dtype] * np.abs(g.T @ X) + TINY
+    dg = np.abs(d) * p * (dl + (3 * np.abs(logits - s) + 4) * E24) + (E24 + (HALF[dtype] if dtype == "bf16" else 0)) * np.abs(g)
+    bx = dg @ np.abs(W) + (len(w) + 2) * E24 * (np.abs(g) @ np.abs(W)) + HALF[dtype] * np.abs(g @ W) + TINY
+    bw = dg.T @ np.abs(X) + ((len(g) + 2) * E24 + (HALF[dtype] if np.ndim(dloss) else 0)) * (np.abs(g).T @ np.abs(X)) + HALF[dtype] * np.abs(g.T @ X) + TINY
     return there, bx, bw
 
 
