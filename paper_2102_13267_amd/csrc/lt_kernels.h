@@ -512,10 +512,10 @@ struct VocabArgs {
 };
 constexpr uint32_t kVocabTile = 256;
 // Few tokens: their rows of x in LDS, padded to 256 bytes, in one, two or four blocks of sixteen; so many workgroups share the rows of w.
-constexpr uint32_t kVocabFewBytes = 128u << 10, kVocabFewGrid = 256;
+constexpr uint32_t kVocabFewBytes = 152u << 10, kVocabFewGrid = 256;
 inline uint32_t vocab_few_blocks(uint32_t tokens) { return tokens <= 16u ? 1u : tokens <= 32u ? 2u : 4u; }
 inline bool vocab_few(uint32_t tokens, uint32_t width, uint32_t elem) {
-  return tokens <= 64u && (uint64_t)vocab_few_blocks(tokens) * 16u * ((width * elem + 255u) & ~255u) <= kVocabFewBytes;
+  return tokens <= 64u && (uint64_t)tokens * (((uint64_t)width * elem + 255u) & ~(uint64_t)255u) <= kVocabFewBytes;
 }
 
 // Argument blocks travel by value in the kernel argument segment, which holds 4 KiB.

@@ -2204,7 +2204,7 @@ struct Lowering {
   // What a cross entropy leaves for its gradient in the same trace, by node: its tokens' lists, their packed rows, and its logits where
   // they are kept.
   struct EntropyShared {
-    int32_t lists = -1, packed_x = -1, logits = -1;
+    int32_t lists = -1, packed_x = -1, packed_w = -1, logits = -1;
   };
   std::map<int32_t, EntropyShared> entropy_shared;
   // the gradient of cross entropy `a` of the same operands, or -1
@@ -2273,7 +2273,9 @@ struct Lowering {
       }
     }
     const bool kept = given && shared.logits >= 0;
-    const int32_t packed_w = pack_w ? temporary(piece * width * e) : -1;
+    const bool packed_before = given && shared.packed_w >= 0 && pieces == 1;
+    const int32_t packed_w = packed_before ? shared.packed_w : pack_w ? temporary(piece * width * e) : -1;
+    if (partner >= 0 && !grad && pieces == 1) entropy_shared[a].packed_w = packed_w;
     // maxima and sums of a piece's tiles, behind those of the pieces before it
     auto parts_of = [&](uint64_t rows) { return few_losses ? (uint64_t)ltk::kVocabFewGrid : (rows + args.tile - 1) / args.tile; };
     const int32_t parts = grad ? -1 : temporary(8 * pad * (1 + parts_of(piece)));
@@ -2325,7 +2327,7 @@ struct Lowering {
       args.add = p > 0;
       const uint64_t w_bytes = (uint64_t)args.rows * args.dim * e, x_bytes = n * args.dim * e, product = 2 * n * args.rows * args.dim;
       const int64_t w_at = (int64_t)(args.first * (uint64_t)args.dim * e);
-      if (pack_w && !(kept && s_dx < 0)) {
+      if (pack_w && !packed_before && !(kept && s_dx < 0)) {
         args.pack_w = 1;
         l = add(ltk::kVocabPack, 2 * w_bytes);
         args.pack_w = 0;

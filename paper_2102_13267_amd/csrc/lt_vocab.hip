@@ -58,6 +58,9 @@ __global__ __launch_bounds__(kTokensBlock) void lt_vocab_tokens_kernel(const Voc
   if (threadIdx.x == 0u) *a.count = all;
 }
 
+// What a maximum takes from logits before their exponentials: nothing if it is infinite (the sum is then 0, or infinite, and no NaN).
+__device__ __forceinline__ float finite_or_0(float top) { return fabsf(top) == INFINITY ? 0.0f : top; }
+
 // the losses' gradient where it is one number
 __device__ __forceinline__ float one_dloss(const VocabArgs& a) { return a.dloss ? a.dloss[0] : a.dloss_value; }
 
@@ -248,6 +251,21 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void lt_vocab_product_kernel(const
   };
 
   typename M::Acc acc[MB][NB];
+  // fp32: a sum of 256 products at most, and the sum of those sums (one chain of 4096 has three times the error)
+  constexpr uint32_t kChain = 8;
+  constexpr bool kChains = sizeof(T) == 4;
+  typename M::Acc total[kChains ? MB : 1][kChains ? NB : 1];
+  auto join_chain = [&]() __attribute__((always_inline)) {
+    if constexpr (kChains) {
+#pragma unroll
+      for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+          total[i][j] += acc[i][j];
+          acc[i][j] = {};
+        }
+    }
+  };
   // The products of a slab in parts: a step of k, half of the wave's rows.  The fragments of the next part (its rows', and with a new
   // step its columns') are read while the products of one are formed, evenly among them.
   constexpr int kHalves = MB >= 4 ? 2 : 1, kRows = MB / kHalves, kParts = (int)M::kSteps * kHalves;
@@ -310,7 +328,10 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void lt_vocab_product_kernel(const
 #pragma unroll
     for (int j = 0; j < NB; ++j)
 #pragma unroll
-      for (uint32_t r = 0; r < 4u * M::kQuads; ++r) acc[i][j][r] = 0.0f;
+      for (uint32_t r = 0; r < 4u * M::kQuads; ++r) {
+        acc[i][j][r] = 0.0f;
+        if constexpr (kChains) total[i][j][r] = 0.0f;
+      }
   landed<0>();
   __syncthreads();   // the first slab is there for every wave, and every wave is done with the tile before
   if (slabs > 0u) {
@@ -324,11 +345,18 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void lt_vocab_product_kernel(const
       landed_and_read<0>();
       __syncthreads();
       part(Num<kParts - 1>(), Num<0>(), which ^ 1u);
+      if (kChains && s % kChain == kChain - 1u) join_chain();
     }
     parts_but_last((slabs - 1u) & 1u);
     landed_and_read<0>();
     __syncthreads();
     part(Num<kParts - 1>(), Num<kParts>(), 0u);
+    if constexpr (kChains) {
+#pragma unroll
+      for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) acc[i][j] += total[i][j];
+    }
   }
   // the next tile's first slab is on its way under this one's results
   index += gridDim.x / 8u;
@@ -389,7 +417,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void lt_vocab_product_kernel(const
       });
 #pragma unroll
       for (uint32_t o = X; o < 64u; o *= 2u) top = fmaxf(top, __shfl_xor(top, o));
-      const float from = top == -INFINITY ? 0.0f : top;
+      const float from = finite_or_0(top);
       each_quad([&](int i, uint32_t q, uint32_t) {
 #pragma unroll
         for (uint32_t r = 0; r < 4u; ++r) sum += __builtin_amdgcn_exp2f((acc[i][j][4 * q + r] - from) * kLog2e);
@@ -404,7 +432,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void lt_vocab_product_kernel(const
       float top = red[y].x, sum = 0.0f;
 #pragma unroll
       for (int w = 1; w < WM; ++w) top = fmaxf(top, red[w * BN + y].x);
-      const float from = top == -INFINITY ? 0.0f : top;
+      const float from = finite_or_0(top);
 #pragma unroll
       for (int w = 0; w < WM; ++w) sum += red[w * BN + y].y * __builtin_amdgcn_exp2f((red[w * BN + y].x - from) * kLog2e);
       parts[y] = top;
@@ -526,12 +554,13 @@ __global__ __launch_bounds__(kFewBlock, 2) void lt_vocab_few_kernel(const VocabA
   const uint32_t n = PASS == kVocabLogits ? a.tokens : __builtin_amdgcn_readfirstlane(*a.count);
   const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = __builtin_amdgcn_readfirstlane(tid / 64u), t16 = lane & 15u, group = lane >> 4;
   const uint32_t row_bytes = (a.width * (uint32_t)sizeof(T) + 255u) & ~255u, chunks = a.width / V;
-  for (uint32_t e = tid; e < TB * 16u * chunks; e += kFewBlock) {
+  for (uint32_t e = tid; e < n * chunks; e += kFewBlock) {
     const uint32_t t = e / chunks, c = e - t * chunks;
-    *(uint4*)(xs + t * row_bytes + ((c ^ (t & 15u)) << 4)) = t < n ? *(const uint4*)((const T*)a.x + (uint64_t)t * a.width + c * V) : make_uint4(0u, 0u, 0u, 0u);
+    *(uint4*)(xs + t * row_bytes + ((c ^ (t & 15u)) << 4)) = *(const uint4*)((const T*)a.x + (uint64_t)t * a.width + c * V);
   }
   float top[TB], sum[TB], lse[TB];
   uint32_t label[TB];
+  const uint32_t last_token = max(n, 1u) - 1u;   // (columns behind the last token: the last one's again, of results never used)
 #pragma unroll
   for (int b = 0; b < TB; ++b) {
     const uint32_t t = b * 16u + t16;
@@ -539,6 +568,13 @@ __global__ __launch_bounds__(kFewBlock, 2) void lt_vocab_few_kernel(const VocabA
     sum[b] = 0.0f;
     label[b] = t < n ? (uint32_t)(PASS == kVocabLogits ? a.labels[t] : a.label[t]) - a.first : ~0u;
     lse[b] = PASS == kVocabGrad && t < n ? a.lse_of[t] : 0.0f;
+  }
+  uint32_t at[TB], key[TB];
+#pragma unroll
+  for (int b = 0; b < TB; ++b) {
+    const uint32_t t = min(b * 16u + t16, last_token);
+    at[b] = t * row_bytes;
+    key[b] = t & 15u;
   }
   __syncthreads();
   const uint32_t steps = a.width / M::kStep, units = ((PASS == kVocabGrad ? a.stride : a.rows) + 15u) / 16u, all = gridDim.x * kFewWaves;
@@ -555,9 +591,10 @@ __global__ __launch_bounds__(kFewBlock, 2) void lt_vocab_few_kernel(const VocabA
   };
   uint32_t unit = blockIdx.x * kFewWaves + wave, s0 = 0u;
   Frag f[kWay], g[kWay];
-  v4f acc[TB];
+  constexpr bool kChains = sizeof(T) == 4;   // (sums of 128 products, and their sum)
+  v4f acc[TB], total[TB];
 #pragma unroll
-  for (int b = 0; b < TB; ++b) acc[b] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int b = 0; b < TB; ++b) acc[b] = total[b] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
   if (unit < units) fetch(unit, 0u, f);
   while (unit < units) {
     const bool last = s0 + kWay >= steps;
@@ -568,7 +605,14 @@ __global__ __launch_bounds__(kFewBlock, 2) void lt_vocab_few_kernel(const VocabA
       if (s0 + k >= steps) break;
       const uint32_t c = (s0 + k) * 4u + group;
 #pragma unroll
-      for (int b = 0; b < TB; ++b) acc[b] = M::mma(f[k], *(const Frag*)(xs + (b * 16u + t16) * row_bytes + ((c ^ t16) << 4)), acc[b]);
+      for (int b = 0; b < TB; ++b) acc[b] = M::mma(f[k], *(const Frag*)(xs + at[b] + ((c ^ key[b]) << 4)), acc[b]);
+    }
+    if constexpr (kChains) {
+#pragma unroll
+      for (int b = 0; b < TB; ++b) {
+        total[b] += acc[b];
+        acc[b] = last ? total[b] : v4f{0.0f, 0.0f, 0.0f, 0.0f};
+      }
     }
     if (last) {
       const uint32_t row = unit * 16u + group * 4u;
@@ -582,7 +626,7 @@ __global__ __launch_bounds__(kFewBlock, 2) void lt_vocab_few_kernel(const VocabA
             if (row + r >= a.rows) acc[b][r] = -INFINITY;
             here = fmaxf(here, acc[b][r]);
           }
-          const float from = here == -INFINITY ? 0.0f : here;
+          const float from = finite_or_0(here);
           sum[b] *= __builtin_amdgcn_exp2f((top[b] - from) * kLog2e);
 #pragma unroll
           for (uint32_t r = 0; r < 4u; ++r) sum[b] += __builtin_amdgcn_exp2f((acc[b][r] - from) * kLog2e);
@@ -599,7 +643,7 @@ __global__ __launch_bounds__(kFewBlock, 2) void lt_vocab_few_kernel(const VocabA
           if constexpr (sizeof(T) == 4) *(v4f*)at = v4f{v[0], v[1], v[2], v[3]};
           else *(v4bf*)at = v4bf{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
         }
-        acc[b] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+        acc[b] = total[b] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
       }
     }
     unit = next;
@@ -612,7 +656,7 @@ __global__ __launch_bounds__(kFewBlock, 2) void lt_vocab_few_kernel(const VocabA
     for (int b = 0; b < TB; ++b) {
 #pragma unroll
       for (uint32_t o = 16u; o < 64u; o *= 2u) {
-        const float other = __shfl_xor(top[b], o), more = __shfl_xor(sum[b], o), both = fmaxf(top[b], other), from = both == -INFINITY ? 0.0f : both;
+        const float other = __shfl_xor(top[b], o), more = __shfl_xor(sum[b], o), both = fmaxf(top[b], other), from = finite_or_0(both);
         sum[b] = sum[b] * __builtin_amdgcn_exp2f((top[b] - from) * kLog2e) + more * __builtin_amdgcn_exp2f((other - from) * kLog2e);
         top[b] = both;
       }
@@ -623,7 +667,7 @@ __global__ __launch_bounds__(kFewBlock, 2) void lt_vocab_few_kernel(const VocabA
       float most = -INFINITY, total = 0.0f;
 #pragma unroll
       for (uint32_t w = 0; w < kFewWaves; ++w) most = fmaxf(most, red[w * TB * 16u + tid].x);
-      const float from = most == -INFINITY ? 0.0f : most;
+      const float from = finite_or_0(most);
 #pragma unroll
       for (uint32_t w = 0; w < kFewWaves; ++w) total += red[w * TB * 16u + tid].y * __builtin_amdgcn_exp2f((red[w * TB * 16u + tid].x - from) * kLog2e);
       float* const parts = a.parts + (uint64_t)blockIdx.x * 2u * a.padded;
@@ -654,7 +698,7 @@ __global__ __launch_bounds__(kLossBlock) void lt_vocab_loss_kernel(const VocabAr
       float both = top;
 #pragma unroll
       for (uint32_t k = 0; k < kWay; ++k) both = fmaxf(both, m[k]);
-      const float from = both == -INFINITY ? 0.0f : both;
+      const float from = finite_or_0(both);
       sum *= __builtin_amdgcn_exp2f((top - from) * kLog2e);
 #pragma unroll
       for (uint32_t k = 0; k < kWay; ++k) sum += s[k] * __builtin_amdgcn_exp2f((m[k] - from) * kLog2e);
@@ -664,7 +708,7 @@ __global__ __launch_bounds__(kLossBlock) void lt_vocab_loss_kernel(const VocabAr
   __syncthreads();
   if (share != 0u || token >= n) return;
   for (uint32_t w = 0; w < kShares; ++w) top = fmaxf(top, red[w][lane].x);
-  const float from = top == -INFINITY ? 0.0f : top;
+  const float from = finite_or_0(top);
   sum = 0.0f;
   for (uint32_t w = 0; w < kShares; ++w) sum += red[w][lane].y * __builtin_amdgcn_exp2f((red[w][lane].x - from) * kLog2e);
   if (!a.last) {

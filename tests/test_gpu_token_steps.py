@@ -402,3 +402,82 @@ def test_lookups_of_tied_rows_in_bf16_round_once():
     ref = E.embedding_grad(E.tensor(dy, "bf16"), E.tensor(ids), into=E.tensor(base, "bf16")).data
     within(got, ref, grad_bound(dy, ids, 3, 1.0, ref, "bf16"))
     ctx.close()
+
+
+@pytest.mark.parametrize("tokens", [3, 17, 90])
+def test_long_sums_in_fp32(tokens):
+    """all terms of one sign, 4096 of them: a sum is of sums of 256 at most, each off by as many half steps as it has terms"""
+    rg = np.random.default_rng(11)
+    ctx = context()
+    dim, vocab = 4096, 300
+    x, w = rg.uniform(0.5, 1.0, (tokens, dim)).astype(np.float32), (rg.uniform(0.5, 1.0, (vocab, dim)) / 512).astype(np.float32)
+    labels = rg.integers(0, vocab, tokens).astype(np.int32)
+    X, W, L = ctx.tensor(x), ctx.tensor(w), ctx.tensor(labels)
+    loss, lse = ctx.linear_xent(X, W, L)
+    dx, dw = ctx.linear_xent_grad(X, W, L, lse, 1.0)
+    logits = x.astype(np.float64) @ w.astype(np.float64).T
+    top = logits.max(-1)
+    want = np.log(np.exp(logits - top[:, None]).sum(-1)) + top
+    dl = (256 + dim / 256 + 2) * E24 * top
+    dlse = dl + (3 * (top - logits.min(-1)) + 96 + vocab / 2048 + 8) * E24 + 3 * E24 * want
+    got = ctx.fetch(lse)
+    within(got, want, dlse, "lse")
+    within(ctx.fetch(loss), want - logits[np.arange(tokens), labels], 2 * dlse, "loss")
+    # the gradient's terms have both signs: what the logits are off goes through p, what the sums of 300 and of the tokens are off is by their terms
+    g = np.exp(logits - want[:, None])
+    dg = g * (dl + dlse)[:, None] + g * (3 * np.abs(logits - want[:, None]) + 4) * E24
+    g[np.arange(tokens), labels] -= 1
+    dg += E24 * np.abs(g)
+    within(ctx.fetch(dx), g @ w, dg @ w + (256 + 8) * E24 * (np.abs(g) @ w) + TINY, "dx")
+    within(ctx.fetch(dw), g.T @ x, dg.T @ x + (tokens + 8) * E24 * (np.abs(g).T @ x) + TINY, "dw")
+    ctx.close()
+
+
+@pytest.mark.parametrize("tokens", [2, 70])
+def test_infinite_logits(tokens):
+    """a logit of +inf makes its token's lse +inf, and its loss where that row is not the label's"""
+    ctx = context()
+    x, w = np.zeros((tokens, 64), np.float32), np.zeros((300, 64), np.float32)
+    x[:, 0] = 1.0
+    w[:, 0] = np.linspace(-1, 1, 300)
+    w[7, 1], w[8, 1] = 3e38, -3e38
+    x[0, 1], x[1, 1] = 10.0, -10.0       # token 0: +inf at row 7, -inf at row 8; token 1 the other way round
+    labels = np.full(tokens, 5, np.int32)
+    want = np.array([np.inf, np.inf] + [np.log(np.exp(np.float64(w[:, 0])).sum())] * (tokens - 2))
+    loss, lse = (ctx.fetch(t) for t in ctx.linear_xent(ctx.tensor(x), ctx.tensor(w), ctx.tensor(labels)))
+    assert np.isposinf(lse[:2]).all() and np.isposinf(loss[:2]).all()
+    assert np.allclose(lse[2:], want[2:], rtol=0, atol=1e-4) and np.allclose(loss[2:], want[2:] - w[5, 0], rtol=0, atol=1e-4)
+    ctx.close()
+
+
+@pytest.mark.parametrize("dtype,tokens,dim", [("f32", 9, 4096), ("f32", 8, 2080), ("f32", 19, 2048), ("bf16", 2, 16384), ("bf16", 3, 30016), ("bf16", 40, 1920)])
+def test_few_tokens_of_long_rows(dtype, tokens, dim):
+    """rows of x that fit in shared memory, or just do not"""
+    rg = np.random.default_rng(12)
+    ctx, E = context(), Eager("f64")
+    x, w, labels = entropy_case(rg, (tokens,), 1003, dim, dtype)
+    there, dlse, dloss = entropy_bounds(x, w, labels, dtype)
+    ref = [t.data for t in E.linear_xent(E.tensor(x, dtype), E.tensor(w, dtype), E.tensor(labels))]
+    loss, lse = ctx.linear_xent(ctx.tensor(x, dtype), ctx.tensor(w, dtype), ctx.tensor(labels))
+    within(ctx.fetch(lse)[there], ref[1][there], dlse, "lse")
+    within(ctx.fetch(loss)[there], ref[0][there], dloss, "loss")
+    ctx.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dim", [33, 200])
+def test_rows_packed_once(dtype, dim):
+    """rows of w that are no whole slabs, a cross entropy and its gradient in one trace and in two: the same bits"""
+    rg = np.random.default_rng(13)
+    ctx = context()
+    x, w, labels = entropy_case(rg, (130,), 700, dim, dtype)
+    X, W, L = ctx.tensor(x, dtype), ctx.tensor(w, dtype), ctx.tensor(labels)
+    loss, lse = ctx.linear_xent(X, W, L)
+    dx, dw = ctx.linear_xent_grad(X, W, L, lse, 0.25)
+    one = [ctx.fetch(t) for t in (loss, lse, dx, dw)]
+    loss, lse = ctx.linear_xent(X, W, L)
+    two = [ctx.fetch(loss), ctx.fetch(lse)]
+    two += [ctx.fetch(t) for t in ctx.linear_xent_grad(X, W, L, lse, 0.25)]
+    for a, b in zip(one, two):
+        assert np.array_equal(a, b)
+    ctx.close()
