@@ -3,9 +3,9 @@
 // seed.  Ten rounds of two 32 x 32 -> 64 bit products give 128 bits, eight elements' worth: sixteen bits each, because 32 would take as long to compute as
 // the elements take to travel.
 //
-// Bound by memory: every element is read and written once.  16 bytes a load, two blocks of eight elements a thread where there are
-// enough (two workgroups' worth a compute unit).  16384 x 4096 bf16: 44 us, 6.1 TB/s, with a residual 62 us, 6.5 TB/s (element by element 113 and 220).
-// Past the last-level cache (256 MB) goes what does not fit it: without that 56 and 72 us.
+// Bound by memory: every element is read and written once, 16 bytes a load.  16384 x 4096 bf16: 42 us, 6.4 TB/s, with a residual
+// 61 us, 6.6 TB/s (element by element 113 and 220).
+// Past the last-level cache (256 MB) goes what does not fit it: without that 51 and 72 us; 16384 x 1024 takes 11.0 us through it and 12.6 past it.
 #include <hip/hip_runtime.h>
 
 #include "lt_launch.h"
@@ -69,48 +69,41 @@ struct Eight {
 
 __device__ __forceinline__ bool kept(const Words& r, uint32_t j, uint32_t level) { return ((r.w[j >> 1] >> (16u * (j & 1u))) & 0xffffu) >= level; }
 
-// One thread, N times eight elements, all on their way while the words are computed.  A dropped element is 0 whatever it
-// was (selected, not multiplied).
-template <typename T, bool MORE, int N, bool PAST>
+// One thread, eight elements, on their way while the words are computed.  A dropped element is 0 whatever it was (selected,
+// not multiplied).  (Sixteen elements a thread: 12.1 us where eight take 11.0 at 16384 x 1024 bf16, 169 where they take 162 at 262144 x 1024.)
+template <typename T, bool MORE, bool PAST>
 __global__ __launch_bounds__(kBlock) void lt_dropout_kernel(const DropoutArgs a) {
-  const uint64_t first = (uint64_t)blockIdx.x * (kBlock * N) + threadIdx.x, whole = a.n / 8u;
+  const uint64_t block = (uint64_t)blockIdx.x * kBlock + threadIdx.x, whole = a.n / 8u;
+  if (block * 8u >= a.n) return;
   const T* const x = (const T*)a.x;
   const T* const more = (const T*)a.residual;
   T* const out = (T*)a.out;
-  Eight<T> v[N], w[N];
-#pragma unroll
-  for (int k = 0; k < N; ++k) {
-    const uint64_t block = first + k * kBlock;
-    if (block >= whole) continue;
-    v[k].template load<PAST>(x + block * 8u);
-    if (MORE) w[k].template load<PAST>(more + block * 8u);
+  Eight<T> v, w;
+  if (block < whole) {
+    v.template load<PAST>(x + block * 8u);
+    if (MORE) w.template load<PAST>(more + block * 8u);
   }
   const uint64_t seed = (uint64_t)a.state[0], step = (uint64_t)a.state[1];
+  const Words r = philox((uint32_t)block, a.site, (uint32_t)step, (uint32_t)(step >> 32), (uint32_t)seed, (uint32_t)(seed >> 32));
+  if (block < whole) {
 #pragma unroll
-  for (int k = 0; k < N; ++k) {
-    const uint64_t block = first + k * kBlock;
-    if (block > whole || block * 8u >= a.n) continue;
-    const Words r = philox((uint32_t)block, a.site, (uint32_t)step, (uint32_t)(step >> 32), (uint32_t)seed, (uint32_t)(seed >> 32));
-    if (block < whole) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        float lo = kept(r, 2 * j, a.level) ? v[k].get(2 * j) * a.scale : 0.0f, hi = kept(r, 2 * j + 1, a.level) ? v[k].get(2 * j + 1) * a.scale : 0.0f;
-        if (MORE) {
-          lo += w[k].get(2 * j);
-          hi += w[k].get(2 * j + 1);
-        }
-        v[k].set_pair(j, lo, hi);
+    for (int j = 0; j < 4; ++j) {
+      float lo = kept(r, 2 * j, a.level) ? v.get(2 * j) * a.scale : 0.0f, hi = kept(r, 2 * j + 1, a.level) ? v.get(2 * j + 1) * a.scale : 0.0f;
+      if (MORE) {
+        lo += w.get(2 * j);
+        hi += w.get(2 * j + 1);
       }
-      v[k].template store<PAST>(out + block * 8u);
-    } else {   // the last few
+      v.set_pair(j, lo, hi);
+    }
+    v.template store<PAST>(out + block * 8u);
+  } else {   // the last few
 #pragma unroll
-      for (uint32_t j = 0; j < 7u; ++j) {
-        const uint64_t at = block * 8u + j;
-        if (at >= a.n) break;
-        float e = kept(r, j, a.level) ? (float)x[at] * a.scale : 0.0f;
-        if (MORE) e += (float)more[at];
-        out[at] = (T)e;
-      }
+    for (uint32_t j = 0; j < 7u; ++j) {
+      const uint64_t at = block * 8u + j;
+      if (at >= a.n) break;
+      float e = kept(r, j, a.level) ? (float)x[at] * a.scale : 0.0f;
+      if (MORE) e += (float)more[at];
+      out[at] = (T)e;
     }
   }
 }
@@ -131,19 +124,11 @@ __global__ __launch_bounds__(kBlock) void lt_dropout_any_kernel(const DropoutArg
   }
 }
 
-template <typename T, bool MORE, int N>
-void launch_wide(const DropoutArgs& a, bool past, hipStream_t s) {
-  const dim3 grid((uint32_t)((a.n + 8u * kBlock * N - 1) / (8u * kBlock * N)));
-  if (past) LT_LAUNCH((lt_dropout_kernel<T, MORE, N, true>), grid, dim3(kBlock), s, a);
-  else LT_LAUNCH((lt_dropout_kernel<T, MORE, N, false>), grid, dim3(kBlock), s, a);
-}
-
 template <typename T, bool MORE>
 void launch_of(const DropoutArgs& a, hipStream_t s) {
-  const uint64_t blocks = (a.n + 7u) / 8u;
-  const bool past = a.n * sizeof(T) * (MORE ? 3u : 2u) >= ((uint64_t)256 << 20);
-  if (blocks > (uint64_t)1024 * kBlock * 2u) launch_wide<T, MORE, 2>(a, past, s);
-  else launch_wide<T, MORE, 1>(a, past, s);
+  const dim3 grid((uint32_t)((a.n + 8u * kBlock - 1) / (8u * kBlock)));
+  if (a.n * sizeof(T) * (MORE ? 3u : 2u) >= ((uint64_t)256 << 20)) LT_LAUNCH((lt_dropout_kernel<T, MORE, true>), grid, dim3(kBlock), s, a);
+  else LT_LAUNCH((lt_dropout_kernel<T, MORE, false>), grid, dim3(kBlock), s, a);
 }
 
 template <typename T>
