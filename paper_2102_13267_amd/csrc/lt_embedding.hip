@@ -1,4 +1,12 @@
-// Rows of a table by token, and the gradient of the table.
+// Rows of a table by token, y[n] = scale * table[id[n]], and the gradient of the table, base[v] + scale * sum over id[n] = v of dy[n].
+//
+// Both are bound by memory.  The lookup reads the rows and writes them once: 16384 x 1024 bf16 of 50000 rows 10.6 us, 6.3 TB/s.
+// The gradient sorts the tokens by id first, a stable radix sort, so that a row's sum is taken in ascending order of its tokens, in fp32, rounded
+// once, the same on every run, whatever the number of tokens of an id (a text's most frequent one is a tenth of it); atomic adds would
+// be neither the same on every run nor quick on that row.  The sorted tokens are then cut into pieces of equal length, so a frequent id's sum is shared
+// by many waves, and joined.  Its own bytes: dy once, the gradient once, and the rows that it is added to.  16384 x 1024 bf16, 50000 rows: sort
+// 3.1 + 4.9 us for each of two digits, sums 24.6 (132 MB, 5.4 TB/s), join 5.0; into rows in place 32768 x 2048: sort 11 x 2, sums 40, join 11.6;
+// 5331 tokens: sorted by one workgroup in 12.2.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -33,6 +41,8 @@ struct Piece<T, 1> {
 };
 
 // ---- lookup: one thread a piece of an output row, two of them where there are many ---------------------------
+// (two: four workgroups a compute unit and more.  us with one / two: 16384 x 1024 bf16 11.5 / 10.9, x 4096 48.8 / 45.3, 32768 x 203 fp32
+// 15.2 / 12.4, 2048 x 1024 5.4 / 5.2)
 template <typename T, int V, int N>
 __global__ __launch_bounds__(kBlock) void lt_embedding_kernel(const EmbedArgs a) {
   const uint32_t units = a.tokens * a.row.d, first = blockIdx.x * (kBlock * N) + threadIdx.x;
@@ -99,7 +109,8 @@ hipError_t launch_embedding(const void* args, hipStream_t s) {
 }
 
 // ---- the gradient: tokens in the order of their ids ------------------------------------------------------
-// A stable radix sort, a digit of the ids at a time, lowest first.
+// A stable radix sort, a digit of the ids at a time, lowest first.  (Counting the next digit while tokens are moved was slower: a frequent id's
+// digit is one counter in memory for all of them.)
 __device__ __forceinline__ uint32_t key_of(const EmbedGradArgs& a, uint32_t i) {
   if (a.key) return a.key[i];
   const int32_t id = a.ids[i];

@@ -2241,7 +2241,8 @@ struct Lowering {
     // (a window along the first axis may start anywhere; tensors of their own start at 16 bytes)
     const bool pack_w = args.width != args.dim || w.byte_offset % 16 != 0;
     args.w_stride = args.width;
-    // A piece of g takes 128 MB, as many rows as that is, but 4096 at least.
+    // A piece of g takes 128 MB, as many rows as that is, but 4096 at least.  (8192 tokens x 4096 bf16, us for 16384 rows of w: pieces of 64 MB
+    // 2456, of 128 2406, of 256 2445; half of the last-level cache holds one beside what the products read.)
     const uint64_t fit = std::max<uint64_t>(4096, ((uint64_t)128 << 20) / (std::max<uint64_t>(pad, 256) * e) & ~(uint64_t)255);
     const uint64_t fit_w = std::max<uint64_t>(4096, ((uint64_t)256 << 20) / (width * e) & ~(uint64_t)255);
     uint64_t piece = args.vocab;
@@ -2250,15 +2251,20 @@ struct Lowering {
     if (pack_w) piece = std::min(piece, fit_w);
     const uint32_t pieces = (uint32_t)((args.vocab + piece - 1) / piece);
     args.stride = (uint32_t)((piece + 255) & ~(uint64_t)255);
-    // Tiles of 256 x 256, one workgroup a compute unit, where every one gets a tile; else of 128 x 128, two.
+    // Tiles of 256 x 256, one workgroup a compute unit, where every one gets a tile; else of 128 x 128, two.  (Losses and gradient in bf16, us
+    // by this rule / 128 throughout / 256 throughout: 1024 x 16384 x 1024 170 / 180 / 171, 2048 x 8192 x 1024 163 / 165 / 175, 4096 x 4096 x 1024
+    // 180 / 177 / 205, 512 x 32768 x 1024 157 / 172 / 172, 1501 x 10007 x 384 96 / 96 / 114.  fp32 products are as long as these tiles allow: 128.)
     auto tiles_of = [&](uint64_t rows, uint64_t columns, uint64_t t) { return (rows + t - 1) / t * ((columns + t - 1) / t); };
     auto tile_for = [&](uint64_t rows, uint64_t columns) { return dt == LT_BF16 && tiles_of(rows, columns, 256) >= 256 ? 256u : 128u; };
     args.tile = tile_for(piece, pad);
-    // few tokens, whose rows of x fit in LDS, and rows of w that need no packing: w goes by once
+    // few tokens, whose rows of x fit in LDS, and rows of w that need no packing: w goes by once.  (Losses, us with / without: 64 tokens
+    // against 131072 x 1024 bf16 56 / 80, x 512 fp32 98 / 155, 8 against 4096 x 512 bf16 12.4 / 18.3; with a gradient 16 against 32768 x 1024 95 / 104, 64 108 / 104.)
     args.few = !pack_w && n > 0 && ltk::vocab_few(args.tokens, args.width, (uint32_t)e) && (grad || x.byte_offset % 16 == 0);
     const bool few_losses = args.few && !grad;   // (they are not packed)
     // Tokens are packed once for a cross entropy and its gradient.  Where g is one piece, the logits that it is made of, as much memory or
-    // twice as much, are kept from one to the other if forming them again takes longer than their way to memory and back.
+    // twice as much, are kept from one to the other if forming them again takes longer than their way to memory and back.  (us kept / formed
+    // again: bf16 2048 x 32768 tokens x rows, dim 1024 519 / 485, 1536 693 / 702, 2048 847 / 917, 4096 1489 / 1748; fp32 1024 x 16000, dim 64
+    // 209 / 211, 128 227 / 244, 256 262 / 309.)
     EntropyShared shared;
     const int32_t source = grad ? rins[a][3].node : a, partner = grad ? a : merge && !few_losses ? gradient_of(a) : -1;
     const bool given = grad && entropy_shared.count(source) && gradient_of(source) == a;
