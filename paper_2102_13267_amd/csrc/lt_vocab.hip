@@ -10,9 +10,10 @@
 // slower: nothing is left to run while one waits; 32x32x16 products were 1 % slower.)
 // fp32: tiles of 128 x 128, v_mfma_f32_32x32x2_f32.
 //
-// 8192 tokens x 131072 rows x 4096 bf16 (8.8 Tflop a product): logits 5.6 - 5.8 ms, 1.5 - 1.6 PFLOP/s; g 6.7, dx 7.0, dw 5.7 ms over sixteen pieces,
-// where a plain product of that size reaches 1.5: the chip lowers its clock under this load.  2048 x 32768 x 1024: 102 - 115 us a product, 1.2 - 1.3 PFLOP/s.
-// fp32 1024 x 16000 x 768: 220 - 230 us a product, 112 TFLOP/s, the matrix units 87 % busy; kept logits to g 21 us where forming them again takes 220.
+// 8192 tokens, nine tenths of them with a label, x 131072 rows x 4096 bf16 (7.9 Tflop a product): logits 5.6 ms, 1.41 PFLOP/s; sixteen pieces of g 6.0, of dx 7.0
+// (its sums in fp32 are read and written once a piece), of dw 5.8 ms, where a library's product of that size reaches 1.5: the chip lowers its
+// clock under this load.  2048 x 32768 x 1024: 113 us a product, 1.2 PFLOP/s, as the library's.
+// fp32 1024 x 16000 x 768: 230 us a product, 109 TFLOP/s, the matrix units 87 % busy at 2.2 GHz; kept logits to g 21 us where forming them again takes 230.
 // One token x 131072 x 4096: 190 us, 5.6 TB/s.
 #include <hip/hip_runtime.h>
 
