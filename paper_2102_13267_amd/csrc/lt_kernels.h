@@ -448,7 +448,9 @@ struct EmbedGradArgs {
     const uint32_t need = (tokens + kEmbedBlock - 1u) / kEmbedBlock;
     blocks = need < 1u ? 1u : need < kEmbedBlocks ? need : kEmbedBlocks;
     each = (tokens + blocks * kEmbedBlock - 1u) / (blocks * kEmbedBlock) * kEmbedBlock;
-    piece = 32u;
+    // pieces long enough that few sums meet in a join, and enough of them for the chip (us of the gradient into 32768 x 1024 bf16 in pieces of
+    // 8 / 16 / 32: 1024 tokens 16 / 18 / 23, 4096 22 / 23 / 27, 8192 35 / 33 / 38, 16384 42 / 38 / 41)
+    piece = tokens <= 4096u ? 8u : tokens <= 16384u ? 16u : 32u;
     while ((uint64_t)piece * 4096u < tokens) piece *= 2u;
     pieces = (tokens + piece - 1u) / piece;
     bits = 1u;                // of ids 0 .. rows (rows: no row)

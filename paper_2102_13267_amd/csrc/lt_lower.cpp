@@ -1219,6 +1219,7 @@ struct Lowering {
     }
     // launches
     elide_copies();
+    add_where_it_lies();
     std::vector<int> order = emission_order();
     columns_behind_contractions(&order);
     for (int k : order) {
@@ -1261,6 +1262,28 @@ struct Lowering {
       storage_of[v.node][v.slot] = to;
       elided[k] = 1;
       plan->merged = true;
+    }
+  }
+
+  // A table's gradient that is added to one of the same trace which nothing else reads (a table at both ends of a model) is added
+  // where that one lies: it is written to the sum's memory, and only the rows that are named are read and written again.
+  // (4096 tokens x 32768 rows x 1024 bf16 with what leads to it: 1045 -> 1034 us.)  Back to front, so that of a chain of them all take the last one's memory.
+  void add_where_it_lies() {
+    if (!merge) return;
+    for (size_t k = ordered.size(); k-- > 0;) {
+      const int32_t a = ordered[k]->anchor;
+      if (a < 0 || nd[a]->op != LT_OP_EMBEDDING_GRAD || rins[a].size() != 3) continue;
+      const Val v = rins[a][2];
+      const uint16_t made_by = nd[v.node]->op;
+      if ((made_by != LT_OP_LINEAR_XENT_GRAD || v.slot != 1) && made_by != LT_OP_EMBEDDING_GRAD) continue;
+      int readers = 0;
+      for (int32_t u : users[v.node])
+        for (const Val& x : rins[u]) readers += x == v ? 1 : 0;
+      const int32_t from = storage_of[v.node][v.slot], to = storage_of[a][0];
+      if (readers != 1 || from < 0 || to < 0 || from == to) continue;
+      if (plan->storages[from].param >= 0 || plan->storages[to].param >= 0 || plan->storages[from].bound_to_root) continue;   // (memory of a caller's, or a result)
+      plan->storages[from].bytes = 0;
+      storage_of[v.node][v.slot] = to;
     }
   }
 
@@ -2132,7 +2155,7 @@ struct Lowering {
     args.dim = (uint32_t)an->dims[1];
     args.tokens = (uint32_t)count(out_shape(rins[a][1]));
     args.scale = (float)real_attr(an, LT_ATTR_SCALE);
-    args.in_place = has_base && plan->storages[out].param >= 0 && plan->storages[out].param == plan->storages[base.storage].param && base.byte_offset == 0;
+    args.in_place = has_base && (base.storage == out || (plan->storages[out].param >= 0 && plan->storages[out].param == plan->storages[base.storage].param)) && base.byte_offset == 0;
     args.share_out();
     const uint64_t n = args.tokens, w = dtype_size(args.dtype), ow = dtype_size(an->dtype), all = (uint64_t)args.rows * args.dim;
     const bool some = n > 0 && all > 0;

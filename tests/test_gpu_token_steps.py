@@ -481,3 +481,41 @@ def test_rows_packed_once(dtype, dim):
     for a, b in zip(one, two):
         assert np.array_equal(a, b)
     ctx.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_gradients_added_where_they_lie(dtype):
+    """chains of table gradients on top of a cross entropy's: the same bits as one barrier after the other, whatever else reads them or is kept"""
+    rg = np.random.default_rng(14)
+    ctx = context()
+    x, w, labels = entropy_case(rg, (130,), 700, 64, dtype)
+    X, W, L = ctx.tensor(x, dtype), ctx.tensor(w, dtype), ctx.tensor(labels)
+    I, J, N = (ctx.tensor(rg.integers(-1, 701, n).astype(np.int32)) for n in (90, 300, 0))
+    Y, Z = ctx.tensor(data(rg, (90, 64), dtype), dtype), ctx.tensor(data(rg, (300, 64), dtype), dtype)
+    none = ctx.tensor(np.zeros((0, 64), np.float32), dtype)
+
+    def program(after, keep):
+        loss, lse = ctx.linear_xent(X, W, L)
+        after(lse)
+        dx, dw = ctx.linear_xent_grad(X, W, L, lse, 0.25)
+        after(dw)
+        one = ctx.embedding_grad(Y, I, into=dw)
+        after(one)
+        two = ctx.embedding_grad(Z, J, into=one, scale=0.5)
+        after(two)
+        three = ctx.embedding_grad(none, N, into=two)
+        after(three)
+        r = dict(dx=dx, dw=dw, one=one, two=two, three=three)
+        if keep == "read":
+            r = dict(three=three, more=ctx.add(dw, one))
+        elif keep == "itself":
+            r = dict(again=ctx.embedding_grad(ctx.narrow(one, 0, 3, 90), I, into=one))
+        elif keep != "all":
+            r = {k: r[k] for k in keep.split()}
+        return r
+    for keep in ("three", "all", "dx three", "dw three", "one three", "two", "read", "itself"):
+        lazy = {k: ctx.fetch(t) for k, t in program(lambda t: None, keep).items()}
+        eager = {k: ctx.fetch(t) for k, t in program(ctx.fetch, keep).items()}
+        for k in lazy:
+            assert np.array_equal(lazy[k], eager[k]), (keep, k)
+    ctx.close()
