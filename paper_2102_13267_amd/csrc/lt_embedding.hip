@@ -5,7 +5,7 @@
 // once, the same on every run, whatever the number of tokens of an id (a text's most frequent one is a tenth of it); atomic adds would
 // be neither the same on every run nor quick on that row.  The sorted tokens are then cut into pieces of equal length, so a frequent id's sum is shared
 // by many waves, and joined.  Its own bytes: dy once, the gradient once, and the rows that it is added to.  16384 x 1024 bf16, 50000 rows: sort
-// 3.1 + 4.9 us for each of two digits, sums 24.6 (132 MB, 5.4 TB/s), join 5.0; into rows in place 32768 x 2048: sort 11 x 2, sums 40, join 11.6;
+// 2.9 + 5.0 us for each of two digits, sums 22 (132 MB, 6 TB/s), join 8.0; into rows in place 32768 x 2048: sort 11 x 2, sums 40, join 11.6;
 // 5331 tokens: sorted by one workgroup in 12.2.
 #include <hip/hip_runtime.h>
 
