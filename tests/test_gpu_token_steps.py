@@ -519,3 +519,43 @@ def test_gradients_added_where_they_lie(dtype):
         for k in lazy:
             assert np.array_equal(lazy[k], eager[k]), (keep, k)
     ctx.close()
+
+
+@pytest.mark.parametrize("streams", [1, 4])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_table_updated_in_place_behind_its_readers(dtype, streams):
+    """the table that a step looks up, multiplies by and differentiates is added to in place at its end: every reader sees the old one"""
+    rg = np.random.default_rng(15)
+    ctx = context()
+    ctx.set_streams(streams)
+    table, ids, labels = data(rg, (300, 64), dtype, 0.25), rg.integers(-1, 300, 200).astype(np.int32), rg.integers(-1, 300, 200).astype(np.int32)
+    given = torch.tensor(table, device="cuda").to(TORCH[dtype])
+    T, I, L = ctx.tensor(given, donatable=True), ctx.tensor(ids), ctx.tensor(labels)
+    S = ctx.tensor(table, dtype)   # the same, a step of which is a barrier an operator
+    for step in range(5):
+        x = ctx.embedding(T, I, scale=2.0)
+        loss, lse = ctx.linear_xent(x, T, L)
+        dx, dw = ctx.linear_xent_grad(x, T, L, lse, 0.5)
+        if step % 2:
+            ctx.assign(T, ctx.embedding_grad(dx, I, into=T, scale=-0.25))
+        else:
+            ctx.assign(T, ctx.sub(T, ctx.embedding_grad(dx, I, into=dw)))
+        y = ctx.embedding(T, I)    # (the new one)
+        ctx.barrier()
+        u = ctx.embedding(S, I, scale=2.0)
+        ctx.barrier()
+        loss2, lse2 = ctx.linear_xent(u, S, L)
+        ctx.barrier()
+        du, dw2 = ctx.linear_xent_grad(u, S, L, lse2, 0.5)
+        ctx.barrier()
+        if step % 2:
+            S = ctx.embedding_grad(du, I, into=S, scale=-0.25)
+        else:
+            g = ctx.embedding_grad(du, I, into=dw2)
+            ctx.barrier()
+            S = ctx.sub(S, g)
+        ctx.barrier()
+        for a, b in ((loss, loss2), (lse, lse2), (T, S), (y, ctx.embedding(S, I))):
+            assert np.array_equal(ctx.fetch(a), ctx.fetch(b)), step
+        assert np.array_equal(given.float().cpu().numpy(), ctx.fetch(T))
+    ctx.close()
