@@ -2264,9 +2264,15 @@ struct Lowering {
     // (a window along the first axis may start anywhere; tensors of their own start at 16 bytes)
     const bool pack_w = args.width != args.dim || w.byte_offset % 16 != 0;
     args.w_stride = args.width;
-    // A piece of g takes 128 MB, as many rows as that is, but 4096 at least.  (8192 tokens x 4096 bf16, us for 16384 rows of w: pieces of 64 MB
-    // 2456, of 128 2406, of 256 2445; half of the last-level cache holds one beside what the products read.)
-    const uint64_t fit = std::max<uint64_t>(4096, ((uint64_t)128 << 20) / (std::max<uint64_t>(pad, 256) * e) & ~(uint64_t)255);
+    // A piece of g takes 128 MB in bf16 (8192 tokens x 4096, us for 16384 rows of w: pieces of 64 MB 2456, of 128 2406, of 256 2445; half of the
+    // last-level cache holds one beside what the products read) and 512 in fp32, whose products take too long for that to count and whose logits are
+    // kept in one of its pieces; more, up to 512 MB, where its rows of dw would be fewer tiles than a round (us in pieces of 128 / 512 MB: bf16
+    // 8192 x 32768 x 256 964 / 777, x 512 1221 / 1093, 16384 x 50000 x 512 4857 / 3761, but 8192 x 32768 x 1024 1862 / 1866; fp32 8192 x
+    // 32768 x 256 7731 / 3594, x 1024 16452 / 12525); and 4096 rows at least.  A plan that does without what it can takes 128 MB throughout.
+    const uint64_t row_of_g = std::max<uint64_t>(pad, 256) * e, mb = (uint64_t)1 << 20, most = 512 * mb / row_of_g & ~(uint64_t)255;
+    const uint64_t small = std::max<uint64_t>(4096, 128 * mb / row_of_g & ~(uint64_t)255), round = (((uint64_t)1 << (dt == LT_BF16 ? 24 : 23)) / width + 255) & ~(uint64_t)255;
+    const uint64_t fit = !merge ? small : std::max(small, dt == LT_BF16 ? std::min(round, most) : most);
+    if (grad && args.vocab > small && fit > small) plan->merged = true;
     const uint64_t fit_w = std::max<uint64_t>(4096, ((uint64_t)256 << 20) / (width * e) & ~(uint64_t)255);
     uint64_t piece = args.vocab;
     if (grad) piece = std::min(piece, fit);
