@@ -2271,7 +2271,8 @@ struct Lowering {
     // 32768 x 256 7731 / 3594, x 1024 16452 / 12525); and 4096 rows at least.  A plan that does without what it can takes 128 MB throughout.
     const uint64_t row_of_g = std::max<uint64_t>(pad, 256) * e, mb = (uint64_t)1 << 20, most = 512 * mb / row_of_g & ~(uint64_t)255;
     const uint64_t small = std::max<uint64_t>(4096, 128 * mb / row_of_g & ~(uint64_t)255), round = (((uint64_t)1 << (dt == LT_BF16 ? 24 : 23)) / width + 255) & ~(uint64_t)255;
-    const uint64_t fit = !merge ? small : std::max(small, dt == LT_BF16 ? std::min(round, most) : most);
+    const bool kept_in_one = dt == LT_F32 && args.dim >= 128u && args.vocab * row_of_g <= 1024 * mb;   // (a product less: 1035 x 131072 x 4096 44.0 / 35.1 ms)
+    const uint64_t fit = !merge ? small : std::max({small, dt == LT_BF16 ? std::min(round, most) : most, kept_in_one ? (uint64_t)args.vocab : 0});
     if (grad && args.vocab > small && fit > small) plan->merged = true;
     const uint64_t fit_w = std::max<uint64_t>(4096, ((uint64_t)256 << 20) / (width * e) & ~(uint64_t)255);
     uint64_t piece = args.vocab;
@@ -2315,10 +2316,23 @@ struct Lowering {
     auto parts_of = [&](uint64_t rows) { return few_losses ? (uint64_t)ltk::kVocabFewGrid : (rows + args.tile - 1) / args.tile; };
     const int32_t parts = grad ? -1 : temporary(8 * pad * (1 + parts_of(piece)));
     const int32_t g = !grad ? -1 : kept && dt == LT_F32 ? shared.logits : temporary(pad * args.stride * e);   // (fp32: in the logits' place)
-    // few tiles of dx and a long sum: shared by as many workgroups as there is room for, each with eight slabs at least
-    const uint64_t slabs = args.stride / slab;
-    auto splits_of = [&](uint64_t t) { return std::max<uint64_t>(1, std::min<uint64_t>({(t == 256 ? 256 : 512) / std::max<uint64_t>(tiles_of(pad, width, t), 1), slabs / 8, 16})); };
-    const uint32_t dx_tile = dt == LT_BF16 && tiles_of(pad, width, 256) * splits_of(256) >= 224 ? 256u : 128u;
+    // Few tiles of dx and a long sum: shared by workgroups that have eight slabs at least, as many as fill whole rounds best for what
+    // their sums cost on the way to memory and back.  (Losses and gradient of 1035 x 131072 x 4096 fp32,
+    // 288 tiles for 512 places: one workgroup a tile 35.7 ms, seven 27.0; 5000 x 32768 x 2048 bf16 2620 / 2578 us.)
+    const uint64_t slabs = args.stride / slab, most_splits = std::max<uint64_t>(1, std::min<uint64_t>(slabs / 8, 16));
+    auto places = [](uint64_t t) { return t == 256 ? 256 : 512; };
+    auto splits_of = [&](uint64_t t) {
+      const uint64_t tiles = std::max<uint64_t>(tiles_of(n, width, t), 1);
+      const double tile_us = 2.0 * (double)(t * t * args.stride) * (double)places(t) / (dt == LT_BF16 ? 1.3e9 : 1.35e8), sums_us = 8.0 * (double)(pad * width) / 5e6;
+      uint64_t best = 1;
+      double least = 0.0;
+      for (uint64_t k = 1; k <= most_splits; ++k) {
+        const double us = (double)((tiles * k + places(t) - 1) / places(t)) * tile_us / (double)k + (double)k * sums_us;
+        if (k == 1 || us < least) best = k, least = us;
+      }
+      return best;
+    };
+    const uint32_t dx_tile = dt == LT_BF16 && tiles_of(n, width, 256) * std::min<uint64_t>(most_splits, std::max<uint64_t>(1, 256 / std::max<uint64_t>(tiles_of(n, width, 256), 1))) >= 224 ? 256u : 128u;
     args.splits = (uint32_t)splits_of(dx_tile);
     const int32_t sums = s_dx >= 0 ? temporary(4 * pad * width * args.splits) : -1;
     auto add = [&](uint32_t pass, uint64_t bytes, uint64_t flops = 0) {

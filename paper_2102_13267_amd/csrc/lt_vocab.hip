@@ -788,21 +788,30 @@ __global__ __launch_bounds__(kRowsBlock) void lt_vocab_dx_kernel(const VocabArgs
   }
 }
 
-template <typename T, int B, int WM, int WN, uint32_t PASS>
-hipError_t launch_product(const VocabArgs& a, hipStream_t s) {
-  const uint64_t m = PASS == kVocabDx || PASS == kVocabDw ? a.width : a.rows, n = PASS == kVocabDw ? a.rows : a.padded;
-  const uint64_t tiles = (m + B - 1) / B * ((n + B - 1) / B) * (PASS == kVocabDx ? a.splits : 1u);
+template <typename T, int BM, int BN, int WM, int WN, uint32_t PASS>
+hipError_t launch_tiles(const VocabArgs& a, hipStream_t s) {
+  const uint64_t m = PASS == kVocabDx || PASS == kVocabDw ? a.width : a.rows, n = PASS == kVocabDw ? a.rows : a.tokens;
+  const uint64_t tiles = (m + BM - 1) / BM * ((n + BN - 1) / BN) * (PASS == kVocabDx ? a.splits : 1u);
   if (tiles == 0) return hipSuccess;
   if (tiles >= (uint64_t)1 << 31) return hipErrorInvalidValue;
   // as many workgroups as run at once: one a compute unit, or two where LDS holds two
-  const uint64_t grid = std::min<uint64_t>((tiles + 7) / 8 * 8, B == 256 ? 256 : 512);
+  const uint64_t grid = std::min<uint64_t>((tiles + 7) / 8 * 8, BM == 256 ? 256 : 512);
   if (((uintptr_t)a.x & 15u) || ((uintptr_t)a.w & 15u) || ((uintptr_t)a.g & 15u)) return hipErrorInvalidValue;
-  LT_LAUNCH((lt_vocab_product_kernel<T, B, B, WM, WN, PASS>), dim3((uint32_t)grid), dim3(WM * WN * 64), s, a);
+  LT_LAUNCH((lt_vocab_product_kernel<T, BM, BN, WM, WN, PASS>), dim3((uint32_t)grid), dim3(WM * WN * 64), s, a);
   static const char* const names[] = {"", "", "logits", "", "grad", "dx", "dw"};
   char name[48];
-  snprintf(name, sizeof(name), "lt_vocab_product_kernel<%s,%d,%s>", sizeof(T) == 4 ? "f32" : "bf16", B, names[PASS]);
+  snprintf(name, sizeof(name), "lt_vocab_product_kernel<%s,%d,%d,%s>", sizeof(T) == 4 ? "f32" : "bf16", BM, BN, names[PASS]);
   note_kernel(name);
   return hipGetLastError();
+}
+
+template <typename T, int B, int WM, int WN, uint32_t PASS>
+hipError_t launch_product(const VocabArgs& a, hipStream_t s) {
+  // fp32 and up to 64 tokens: tiles of 128 x 64, half of a square one's columns would be of no token (64 x 131072 x 4096: losses 997 / 602 us; with a
+  // gradient 22 2730 / 1811).  In bf16 such products are bound by w's bytes already.
+  if constexpr (sizeof(T) == 4 && PASS != kVocabDw)
+    if (a.tokens <= 64u) return launch_tiles<T, B, 64, WM, WN, PASS>(a, s);
+  return launch_tiles<T, B, B, WM, WN, PASS>(a, s);
 }
 
 template <typename T, uint32_t PASS>
