@@ -410,6 +410,17 @@ struct PagedArgs {
   uint64_t parts_bytes() const { return (uint64_t)pieces * part_floats() * sizeof(float) + 16u * (uint64_t)listed; }
 };
 
+// So many workgroups of 256 threads: a launch holds less than 2^32 threads along x, so many of them stand in rows of 2^23 along y (the kernel takes
+// blockIdx.y * gridDim.x + blockIdx.x, and what is behind the last one has nothing to do).
+struct ManyWorkgroups {
+  uint32_t x, y;
+};
+inline ManyWorkgroups many_workgroups(uint64_t n) {
+  constexpr uint64_t kRow = (uint64_t)1 << 23;
+  return n <= kRow ? ManyWorkgroups{(uint32_t)n, 1u} : ManyWorkgroups{(uint32_t)kRow, (uint32_t)((n + kRow - 1u) / kRow)};
+}
+constexpr uint64_t kMostWorkgroups = (uint64_t)1 << 29;   // (four waves each, counted in 32 bits; the tensors of so many are larger than the memory)
+
 // ---- table lookup by token, and its gradient ---------------------------------------------------------
 // out[t] = scale * table[ids[t]], zeros where that is no row.
 struct EmbedArgs {
@@ -511,6 +522,11 @@ struct VocabArgs {
   void* packed;                // kVocabPack's result
   float *loss, *lse_out;
   void *dx, *dw;
+  // workgroups of the passes that have a wave for each row, or for 256 elements of one
+  uint64_t workgroups() const {
+    const uint64_t waves = pass == kVocabPack ? (pack_w ? rows : padded) : pass == kVocabKept ? (uint64_t)padded * (stride / 256u) : pass == kVocabDxOut ? tokens : 0u;
+    return (waves + 3u) / 4u;
+  }
 };
 constexpr uint32_t kVocabTile = 256;
 // Few tokens: their rows of x in LDS, padded to 256 bytes, in one, two or four blocks of sixteen; so many workgroups share the rows of w.

@@ -82,9 +82,11 @@ __device__ __forceinline__ float one_dloss(const VocabArgs& a) { return a.dloss 
 
 // ---- rows one behind the other, padded to whole slabs: one wave a row ------------------------------------
 constexpr uint32_t kRowsBlock = 256;
+// which wave this is of all of a launch's (many_workgroups)
+__device__ __forceinline__ uint32_t wave_of_many() { return (blockIdx.y * gridDim.x + blockIdx.x) * (kRowsBlock / 64u) + threadIdx.x / 64u; }
 template <typename T, bool VEC>
 __global__ __launch_bounds__(kRowsBlock) void lt_vocab_pack_kernel(const VocabArgs a) {
-  const uint32_t row = blockIdx.x * (kRowsBlock / 64u) + threadIdx.x / 64u, lane = threadIdx.x & 63u;
+  const uint32_t row = wave_of_many(), lane = threadIdx.x & 63u;
   const T* src;
   if (a.pack_w) {
     if (row >= a.rows) return;
@@ -743,7 +745,7 @@ __global__ __launch_bounds__(kLossBlock) void lt_vocab_loss_kernel(const VocabAr
 // ---- g from logits that were kept: one wave 256 of a token's, up to whole tiles of tokens and rows -------------------
 template <typename T>
 __global__ __launch_bounds__(kRowsBlock) void lt_vocab_kept_kernel(const VocabArgs a) {
-  const uint32_t tiles = a.stride / 256u, unit = blockIdx.x * (kRowsBlock / 64u) + threadIdx.x / 64u, lane = threadIdx.x & 63u;
+  const uint32_t tiles = a.stride / 256u, unit = wave_of_many(), lane = threadIdx.x & 63u;
   const uint32_t token = unit / tiles, row = (unit - token * tiles) * 256u + lane * 4u, n = *a.count;
   if (token >= ((n + kVocabTile - 1u) & ~(kVocabTile - 1u))) return;
   const uint64_t at = (uint64_t)token * a.stride + row;
@@ -763,7 +765,7 @@ __global__ __launch_bounds__(kRowsBlock) void lt_vocab_kept_kernel(const VocabAr
 // ---- dx: the workgroups' sums of a token, four columns a thread (packed rows are whole slabs), one wave a row -----------------
 template <typename T>
 __global__ __launch_bounds__(kRowsBlock) void lt_vocab_dx_kernel(const VocabArgs a) {
-  const uint32_t i = blockIdx.x * (kRowsBlock / 64u) + threadIdx.x / 64u, lane = threadIdx.x & 63u;
+  const uint32_t i = wave_of_many(), lane = threadIdx.x & 63u;
   if (i >= a.tokens) return;
   const int32_t p = a.packed_of[i];
   T* const out = (T*)a.dx + (uint64_t)i * a.dim;
@@ -828,14 +830,14 @@ hipError_t launch_few(const VocabArgs& a, hipStream_t s) {
 
 template <typename T, int B, int WM, int WN>
 hipError_t launch_of(const VocabArgs& a, hipStream_t s) {
-  const dim3 block(kRowsBlock);
+  const ManyWorkgroups many = many_workgroups(a.workgroups());
+  const dim3 grid(many.x, many.y), block(kRowsBlock);
   switch (a.pass) {
     case kVocabPack: {
-      const uint32_t rows = a.pack_w ? a.rows : a.padded;
-      if (rows == 0) return hipSuccess;
+      if (many.x == 0) return hipSuccess;
       const bool vec = (((uintptr_t)(a.pack_w ? a.w : a.x)) & 15u) == 0 && a.dim * sizeof(T) % 16 == 0;
-      if (vec) LT_LAUNCH((lt_vocab_pack_kernel<T, true>), dim3((rows + 3u) / 4u), block, s, a);
-      else LT_LAUNCH((lt_vocab_pack_kernel<T, false>), dim3((rows + 3u) / 4u), block, s, a);
+      if (vec) LT_LAUNCH((lt_vocab_pack_kernel<T, true>), grid, block, s, a);
+      else LT_LAUNCH((lt_vocab_pack_kernel<T, false>), grid, block, s, a);
       return hipGetLastError();
     }
     case kVocabLogits:
@@ -846,15 +848,12 @@ hipError_t launch_of(const VocabArgs& a, hipStream_t s) {
       return launch_product<T, B, WM, WN, kVocabGrad>(a, s);
     case kVocabDx: return launch_product<T, B, WM, WN, kVocabDx>(a, s);
     case kVocabDw: return launch_product<T, B, WM, WN, kVocabDw>(a, s);
-    case kVocabKept: {
-      const uint64_t grid = (uint64_t)a.padded * (a.stride / 256u) / 4u;   // (padded: a multiple of 256)
-      if (grid == 0) return hipSuccess;
-      if (grid >= (uint64_t)1 << 24) return hipErrorInvalidValue;
-      LT_LAUNCH(lt_vocab_kept_kernel<T>, dim3((uint32_t)grid), block, s, a);
+    case kVocabKept:
+      if (a.workgroups() >= kMostWorkgroups) return hipErrorInvalidValue;
+      if (many.x > 0) LT_LAUNCH(lt_vocab_kept_kernel<T>, grid, block, s, a);
       return hipGetLastError();
-    }
     case kVocabDxOut:
-      if (a.tokens > 0) LT_LAUNCH(lt_vocab_dx_kernel<T>, dim3((a.tokens + 3u) / 4u), block, s, a);
+      if (many.x > 0) LT_LAUNCH(lt_vocab_dx_kernel<T>, grid, block, s, a);
       return hipGetLastError();
   }
   return hipErrorInvalidValue;
