@@ -17,7 +17,6 @@ namespace ltk {
 namespace {
 
 constexpr uint32_t kBlock = 256;
-constexpr uint64_t kMostGrid = (uint64_t)1 << 24;   // workgroups are below that: a launch holds less than 2^32 threads
 
 __device__ __forceinline__ uint32_t divide(uint32_t n, const Divider& by) { return (uint32_t)(((uint64_t)n * by.magic) >> 31) >> by.shift; }
 
@@ -288,12 +287,15 @@ __device__ __forceinline__ uint32_t first_of(const EmbedGradArgs& a, uint32_t ke
   return low + __popcll(__ballot(low + lane < high && a.key[low + lane] < key));
 }
 
+// which wave this is of all of a launch's (many_workgroups)
+__device__ __forceinline__ uint32_t wave_of_many() { return __builtin_amdgcn_readfirstlane((blockIdx.y * gridDim.x + blockIdx.x) * (kBlock / 64u) + threadIdx.x / 64u); }
+
 // A wave has a piece of the sorted tokens and 64 pieces of their rows: runs of one id are added up in order, eight rows on their way.  A
 // run that is whole is written; what is shared with another piece of tokens is left in `parts`.  Waves behind the pieces': sixteen rows
 // of the table each, those that no id names.
 template <typename T, typename O, int V>
 __global__ __launch_bounds__(kBlock) void lt_embedding_sum_kernel(const EmbedGradArgs a) {
-  const uint32_t lane = threadIdx.x & 63u, unit = __builtin_amdgcn_readfirstlane(blockIdx.x * (kBlock / 64u) + threadIdx.x / 64u);
+  const uint32_t lane = threadIdx.x & 63u, unit = wave_of_many();
   const uint32_t tiles = (a.dim / V + 63u) / 64u, index = unit / tiles, d = ((unit % tiles) * 64u + lane) * V;
   const O* const base = (const O*)a.base;
   O* const out = (O*)a.out;
@@ -385,7 +387,7 @@ __global__ __launch_bounds__(kBlock) void lt_embedding_sum_kernel(const EmbedGra
 // A row that a piece begins and shares with the next: the pieces' sums in order, sixteen on their way.
 template <typename O, int V>
 __global__ __launch_bounds__(kBlock) void lt_embedding_join_kernel(const EmbedGradArgs a) {
-  const uint32_t lane = threadIdx.x & 63u, unit = __builtin_amdgcn_readfirstlane(blockIdx.x * (kBlock / 64u) + threadIdx.x / 64u);
+  const uint32_t lane = threadIdx.x & 63u, unit = wave_of_many();
   const uint32_t tiles = (a.dim / V + 63u) / 64u, index = unit / tiles, d = ((unit % tiles) * 64u + lane) * V;
   if (index + 1u >= a.pieces) return;
   const uint32_t begin = index * a.piece, next = begin + a.piece;
@@ -430,13 +432,13 @@ __global__ __launch_bounds__(kBlock) void lt_embedding_join_kernel(const EmbedGr
 
 template <typename T, typename O, int V>
 hipError_t launch_wide(const EmbedGradArgs& a, hipStream_t s) {
-  const uint64_t tiles = (a.dim / V + 63u) / 64u;
-  const uint64_t units = tiles * (a.pass == kEmbedJoin ? a.pieces : a.pieces + (a.in_place ? 0u : (a.rows + kEmbedRows - 1u) / kEmbedRows));
-  const uint64_t grid = (units + kBlock / 64u - 1u) / (kBlock / 64u);
-  if (grid == 0) return hipSuccess;
-  if (grid >= kMostGrid) return hipErrorInvalidValue;
-  if (a.pass == kEmbedJoin) LT_LAUNCH((lt_embedding_join_kernel<O, V>), dim3((uint32_t)grid), dim3(kBlock), s, a);
-  else LT_LAUNCH((lt_embedding_sum_kernel<T, O, V>), dim3((uint32_t)grid), dim3(kBlock), s, a);
+  const uint64_t n = a.workgroups(V);
+  if (n == 0) return hipSuccess;
+  if (n >= kMostWorkgroups) return hipErrorInvalidValue;
+  const ManyWorkgroups many = many_workgroups(n);
+  const dim3 grid(many.x, many.y);
+  if (a.pass == kEmbedJoin) LT_LAUNCH((lt_embedding_join_kernel<O, V>), grid, dim3(kBlock), s, a);
+  else LT_LAUNCH((lt_embedding_sum_kernel<T, O, V>), grid, dim3(kBlock), s, a);
   return hipGetLastError();
 }
 

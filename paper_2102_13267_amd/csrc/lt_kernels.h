@@ -468,6 +468,11 @@ struct EmbedGradArgs {
     while (bits < 31u && rows >> bits) ++bits;
   }
   bool few() const { return tokens <= kEmbedFew && bits <= 2u * kEmbedFewBits; }
+  // workgroups of kEmbedSum and kEmbedJoin, whose waves have 64 pieces of v elements of a row
+  uint64_t workgroups(uint32_t v) const {
+    const uint64_t tiles = (dim / v + 63u) / 64u;
+    return (tiles * (pass == kEmbedJoin ? pieces : pieces + (in_place ? 0u : (rows + kEmbedRows - 1u) / kEmbedRows)) + 3u) / 4u;
+  }
 };
 
 // ---- dropout ---------------------------------------------------------------------------------------------

@@ -34,10 +34,14 @@ static void holds(uint64_t workgroups, uint64_t at_least) {
 }
 
 // every launch of the plan; the passes of a cross entropy that were seen, a bit each
-static uint32_t look() {
+static uint32_t look(uint32_t v) {
   uint32_t seen = 0;
   for (const lt::Launch& l : ctx->last_plan->launches) {
-    if (l.kind == lt::L_VOCAB) {
+    if (l.kind == lt::L_EMBEDGRAD) {
+      const ltk::EmbedGradArgs& a = *(const ltk::EmbedGradArgs*)l.args.data();
+      if (a.pass == ltk::kEmbedSum || a.pass == ltk::kEmbedJoin) holds(a.workgroups(v), 1);
+      else CHECK(a.blocks <= ltk::kEmbedBlocks);
+    } else if (l.kind == lt::L_VOCAB) {
       const ltk::VocabArgs& a = *(const ltk::VocabArgs*)l.args.data();
       seen |= 1u << a.pass;
       if (a.pass == ltk::kVocabPack) holds(a.workgroups(), ((a.pack_w ? a.rows : a.tokens) + 3u) / 4u);
@@ -55,9 +59,21 @@ static uint32_t entropy(int64_t tokens, int64_t vocab, int64_t dim, lt_dtype dt,
   op(LT_OP_LINEAR_XENT, {x, w, labels}, {}, both, 2);
   op(LT_OP_LINEAR_XENT_GRAD, {x, w, labels, both[1], dloss}, {}, grads, 2);
   CHECK(lt_barrier(ctx, 1, nullptr) == LT_OK);
-  const uint32_t seen = look();
+  const uint32_t seen = look(1);
   for (lt_tensor t : {x, w, labels, dloss, both[0], both[1], grads[0], grads[1]}) CHECK(lt_release(ctx, t) == LT_OK);
   return seen;
+}
+
+static void gradient(int64_t tokens, int64_t rows, int64_t dim, uint32_t v) {
+  const lt_tensor dy = dev({tokens, dim}, LT_BF16), ids = dev({tokens}, LT_I32);
+  lt_attr n{};
+  n.key = LT_ATTR_ROWS;
+  n.v.i = rows;
+  lt_tensor out = 0;
+  op(LT_OP_EMBEDDING_GRAD, {dy, ids}, {n}, &out, 1);
+  CHECK(lt_barrier(ctx, 1, nullptr) == LT_OK);
+  look(v);
+  for (lt_tensor t : {dy, ids, out}) CHECK(lt_release(ctx, t) == LT_OK);
 }
 
 int main() {
@@ -69,6 +85,14 @@ int main() {
       for (int64_t tokens : {most, (int64_t)1 << 26, ((int64_t)1 << 26) - 1, (int64_t)1 << 25}) CHECK((entropy(tokens, 200, 8, dt, each) & rows) == rows);
   CHECK(entropy(1 << 23, 2048, 128, LT_F32, false) & kept);   // (69 GB of logits)
   CHECK(entropy((1 << 23) - 1, 4000, 128, LT_F32, true) & kept);
+  // tables of 200 GB, and few rows that are long, element by element and eight at once
+  gradient(1000, ((int64_t)1 << 21) - 1, 50001, 1);
+  gradient(1000, ((int64_t)1 << 21) - 1, 50000, 8);
+  gradient(4096, 8, ((int64_t)1 << 23) + 1, 1);
+  gradient(40000, 3, ((int64_t)1 << 21) + 1, 1);
+  gradient(4096, 8, (int64_t)1 << 24, 8);
+  gradient(most, most, 1, 1);
+  gradient(most, most, 512, 8);
   CHECK(lt_shutdown(ctx) == LT_OK);
   std::puts("reach: ok");
   return 0;

@@ -85,3 +85,28 @@ def _as_torch(ctx, t):
         __cuda_array_interface__ = {"shape": t.shape, "typestr": {"f32": "<f4", "bf16": "<i2"}[t.dtype], "data": (ctx.device_ptr(t), False), "version": 2, "strides": None}
     v = torch.as_tensor(Memory(), device="cuda")
     return v.view(torch.bfloat16) if t.dtype == "bf16" else v
+
+
+@pytest.mark.gpu
+def test_a_gradient_of_rows_so_long():
+    """4096 tokens of 2^23 + 1 columns, read element by element: 2^26 waves and more, for the sums and for joining them; in place and beside its base"""
+    from test_gpu_token_operators import context
+    tokens, rows, dim = 4096, 8, 2 ** 23 + 1
+    rg = np.random.default_rng(2)
+    dy = torch.ones((tokens, dim), dtype=torch.bfloat16, device="cuda")
+    dy[:, -1] = 2.0
+    dy[:, dim // 2] = 0.5
+    ids = rg.integers(0, rows, tokens).astype(np.int32)
+    counts = torch.tensor(np.bincount(ids, minlength=rows), device="cuda").float()
+    base = torch.zeros((rows, dim), dtype=torch.bfloat16, device="cuda")
+    ctx = context(workspace_bytes=40 << 30)
+    D, I, B = ctx.tensor(dy), ctx.tensor(ids), ctx.tensor(base, donatable=True)
+    beside = ctx.embedding_grad(D, I, rows=rows)
+    ctx.barrier()
+    ctx.assign(B, ctx.embedding_grad(D, I, into=B))
+    ctx.barrier()
+    want = counts[:, None].to(torch.bfloat16).expand(rows, dim).clone()      # (whole numbers below 2^24, summed exactly and rounded once)
+    want[:, -1] = (2 * counts).to(torch.bfloat16)
+    want[:, dim // 2] = (counts / 2).to(torch.bfloat16)
+    assert torch.equal(_as_torch(ctx, beside), want) and torch.equal(base, want)
+    ctx.close()
