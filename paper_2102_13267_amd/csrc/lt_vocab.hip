@@ -501,7 +501,8 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void lt_vocab_product_kernel(const
           });
       }
     }
-    const float factor = PASS == kVocabDw && a.rank0 ? one_dloss(a) : 1.0f;
+    // (where no token counts, dw is 0 whatever dloss is: as the mean over none it is infinite)
+    const float factor = PASS == kVocabDw && a.rank0 && n_tokens > 0u ? one_dloss(a) : 1.0f;
 #pragma unroll
     for (uint32_t half = 0; half < 2u; ++half) {
       if (half > 0u) __syncthreads();   // (the first half's rows have been read)
