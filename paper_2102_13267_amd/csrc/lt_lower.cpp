@@ -2273,12 +2273,16 @@ struct Lowering {
     const uint64_t small = std::max<uint64_t>(4096, 128 * mb / row_of_g & ~(uint64_t)255), round = (((uint64_t)1 << (dt == LT_BF16 ? 24 : 23)) / width + 255) & ~(uint64_t)255;
     const bool kept_in_one = dt == LT_F32 && args.dim >= 128u && args.vocab * row_of_g <= 1024 * mb;   // (a product less: 1035 x 131072 x 4096 44.0 / 35.1 ms)
     const uint64_t fit = !merge ? small : std::max({small, dt == LT_BF16 ? std::min(round, most) : most, kept_in_one ? (uint64_t)args.vocab : 0});
-    if (grad && args.vocab > small && fit > small) plan->merged = true;
-    const uint64_t fit_w = std::max<uint64_t>(4096, ((uint64_t)256 << 20) / (width * e) & ~(uint64_t)255);
-    uint64_t piece = args.vocab;
-    if (grad) piece = std::min(piece, fit);
-    else piece = std::min<uint64_t>(piece, std::max<uint64_t>(4096, ((uint64_t)256 << 20) / (8 * std::max<uint64_t>(pad, 256)) * 128 & ~(uint64_t)255));   // (so much for maxima and sums)
-    if (pack_w) piece = std::min(piece, fit_w);
+    // what a piece's maxima and sums of the losses, and its packed rows of w, may take besides: 256 MB, 128 in such a plan
+    auto piece_in = [&](uint64_t rows_of_g, uint64_t room) {
+      uint64_t rows = args.vocab;
+      if (grad) rows = std::min(rows, rows_of_g);
+      else rows = std::min(rows, std::max<uint64_t>(4096, room / (8 * std::max<uint64_t>(pad, 256)) * 128 & ~(uint64_t)255));
+      if (pack_w) rows = std::min(rows, std::max<uint64_t>(4096, room / (width * e) & ~(uint64_t)255));
+      return rows;
+    };
+    const uint64_t least_piece = piece_in(small, 128 * mb), piece = merge ? piece_in(fit, 256 * mb) : least_piece;
+    if (piece > least_piece) plan->merged = true;
     const uint32_t pieces = (uint32_t)((args.vocab + piece - 1) / piece);
     args.stride = (uint32_t)((piece + 255) & ~(uint64_t)255);
     // Tiles of 256 x 256, one workgroup a compute unit, where every one gets a tile; else of 128 x 128, two.  (Losses and gradient in bf16, us
@@ -2318,8 +2322,9 @@ struct Lowering {
     const int32_t g = !grad ? -1 : kept && dt == LT_F32 ? shared.logits : temporary(pad * args.stride * e);   // (fp32: in the logits' place)
     // Few tiles of dx and a long sum: shared by workgroups that have eight slabs at least, as many as fill whole rounds best for what
     // their sums cost on the way to memory and back.  (Losses and gradient of 1035 x 131072 x 4096 fp32,
-    // 288 tiles for 512 places: one workgroup a tile 35.7 ms, seven 27.0; 5000 x 32768 x 2048 bf16 2620 / 2578 us.)
-    const uint64_t slabs = args.stride / slab, most_splits = std::max<uint64_t>(1, std::min<uint64_t>(slabs / 8, 16));
+    // 288 tiles for 512 places: one workgroup a tile 35.7 ms, seven 27.0; 5000 x 32768 x 2048 bf16 2620 / 2578 us.)  A plan that does without what it
+    // can has one.
+    const uint64_t slabs = args.stride / slab, most_splits = merge ? std::max<uint64_t>(1, std::min<uint64_t>(slabs / 8, 16)) : 1;
     auto places = [](uint64_t t) { return t == 256 ? 256 : 512; };
     auto splits_of = [&](uint64_t t) {
       const uint64_t tiles = std::max<uint64_t>(tiles_of(n, width, t), 1);
@@ -2334,6 +2339,7 @@ struct Lowering {
     };
     const uint32_t dx_tile = dt == LT_BF16 && tiles_of(n, width, 256) * std::min<uint64_t>(most_splits, std::max<uint64_t>(1, 256 / std::max<uint64_t>(tiles_of(n, width, 256), 1))) >= 224 ? 256u : 128u;
     args.splits = (uint32_t)splits_of(dx_tile);
+    if (s_dx >= 0 && args.splits > 1) plan->merged = true;
     const int32_t sums = s_dx >= 0 ? temporary(4 * pad * width * args.splits) : -1;
     auto add = [&](uint32_t pass, uint64_t bytes, uint64_t flops = 0) {
       args.pass = pass;
