@@ -150,14 +150,17 @@ typedef enum {
  *
  * LT_OP_LINEAR_XENT: x is [..., dim] and w [rows, dim], both fp32 or both bf16, labels int32 [...].  With l = x w^T: lse = log of the
  * sum of exp l over the rows, loss = lse - l[label]; both fp32 [...], and 0 where a label is not one of w's rows (a token that is not trained on).  The
- * logits are formed in pieces, in fp32, and not kept but for a gradient in the same barrier that needs one piece of them.
+ * logits are formed in pieces, in fp32, and not kept but for a gradient in the same barrier that needs one piece of them: up to 1 GB, or 4096 rows.
  * LT_OP_LINEAR_XENT_GRAD: lse is LT_OP_LINEAR_XENT's second output, dloss the losses' gradient, fp32 [...] or rank 0.  With g = (exp(l - lse) - [label]) * dloss,
  * 0 for tokens whose label is no row: dx = g w, of x's type and shape, dw = g^T x, of w's.  exp(l - lse) - [label] is rounded to their type before these
- * products, and so is x times dloss if dloss is not rank 0; sums are in fp32.  What x, lse and dloss hold for a token whose label is no row is not looked at.  A result that nothing uses is not computed.
+ * products, and so is x times dloss if dloss is not rank 0; sums are in fp32.  What x, lse and dloss hold for a token whose label is no row is not looked at; where there are only such tokens,
+ * dw is 0.  A result that nothing uses is not computed.
  *
  * Operands that are not tensors of their own: windows along the first axis (also reshaped) are read where they lie, other windows, permutations and
  * broadcasts are copied first.  LT_ERR_UNSUPPORTED at the barrier: a host scalar's broadcast (but for dloss), and one of integers along the last of
- * several axes, and a window of int64 that is a result itself.  LT_ERR_SHAPE: 2^27 tokens, ids or rows or more; in a cross entropy no rows, no dim or one over 2^20.
+ * several axes, a window of int64 that is a result itself, and, as everywhere, a reshape of a broadcast (but for one between a broadcast and the operator).
+ * Packed rows, pieces of the logits' gradient, sorted ids and partial sums are temporaries: a cross entropy or a table's gradient of a training step's size
+ * has no room in lt_barrier_static's array (LT_ERR_OOM), and lt_barrier takes less of it, more slowly, where the workspace is short.  LT_ERR_SHAPE: 2^27 tokens, ids or rows or more; in a cross entropy no rows, no dim or one over 2^20.
  */
 
 typedef enum {

@@ -5,8 +5,8 @@
 // once, the same on every run, whatever the number of tokens of an id (a text's most frequent one is a tenth of it); atomic adds would
 // be neither the same on every run nor quick on that row.  The sorted tokens are then cut into pieces of equal length, so a frequent id's sum is shared
 // by many waves, and joined.  Its own bytes: dy once, the gradient once, and the rows that it is added to.  16384 x 1024 bf16, 50000 rows: sort
-// 2.9 + 5.0 us for each of two digits, sums 22 (132 MB, 6 TB/s), join 8.0; into rows in place 32768 x 2048: sort 11 x 2, sums 40, join 11.6;
-// 5331 tokens: sorted by one workgroup in 12.2.
+// 2.8 + 4.9 us for each of two digits, sums 22 (132 MB, 6 TB/s), join 7.8; into rows in place 32768 x 2048: sort 9.8 x 2, sums 39, join 10.8;
+// 5331 tokens: sorted by one workgroup in 13.6.  Rows that are no multiple of 16 bytes go by shorter pieces, one element where their number is odd.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

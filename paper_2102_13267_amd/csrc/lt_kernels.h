@@ -441,7 +441,7 @@ constexpr uint32_t kEmbedFew = 8192;       // tokens that one of them sorts by i
 constexpr uint32_t kEmbedFewBits = 9;      // by ids of two digits of so many bits
 constexpr uint32_t kEmbedBlocks = 64;      // sorting workgroups at most
 constexpr uint32_t kEmbedMaxBits = 10;     // of a digit
-constexpr uint32_t kEmbedRows = 16;        // rows of the table that a wave looks for among the ids
+constexpr uint32_t kEmbedRows = 16;        // rows of the table that a wave looks for among the ids (us of the gradient with 8 / 16 / 32: 16384 x 1024 into 50000 bf16 44.6 / 44.1 / 45.0, 1024 x 512 into 131072 29.9 / 30.3 / 30.0)
 struct EmbedGradArgs {
   const void* dy;
   const int32_t* ids;

@@ -2268,7 +2268,8 @@ struct Lowering {
     // last-level cache holds one beside what the products read) and 512 in fp32, whose products take too long for that to count and whose logits are
     // kept in one of its pieces; more, up to 512 MB, where its rows of dw would be fewer tiles than a round (us in pieces of 128 / 512 MB: bf16
     // 8192 x 32768 x 256 964 / 777, x 512 1221 / 1093, 16384 x 50000 x 512 4857 / 3761, but 8192 x 32768 x 1024 1862 / 1866; fp32 8192 x
-    // 32768 x 256 7731 / 3594, x 1024 16452 / 12525); and 4096 rows at least.  A plan that does without what it can takes 128 MB throughout.
+    // 32768 x 256 7731 / 3594, x 1024 16452 / 12525); and 4096 rows at least, whatever the tokens are.  A plan that does without what it can takes
+    // 128 MB throughout.
     const uint64_t row_of_g = std::max<uint64_t>(pad, 256) * e, mb = (uint64_t)1 << 20, most = 512 * mb / row_of_g & ~(uint64_t)255;
     const uint64_t small = std::max<uint64_t>(4096, 128 * mb / row_of_g & ~(uint64_t)255), round = (((uint64_t)1 << (dt == LT_BF16 ? 24 : 23)) / width + 255) & ~(uint64_t)255;
     const bool kept_in_one = dt == LT_F32 && args.dim >= 128u && args.vocab * row_of_g <= 1024 * mb;   // (a product less: 1035 x 131072 x 4096 44.0 / 35.1 ms)
@@ -2322,8 +2323,10 @@ struct Lowering {
     const int32_t g = !grad ? -1 : kept && dt == LT_F32 ? shared.logits : temporary(pad * args.stride * e);   // (fp32: in the logits' place)
     // Few tiles of dx and a long sum: shared by workgroups that have eight slabs at least, as many as fill whole rounds best for what
     // their sums cost on the way to memory and back.  (Losses and gradient of 1035 x 131072 x 4096 fp32,
-    // 288 tiles for 512 places: one workgroup a tile 35.7 ms, seven 27.0; 5000 x 32768 x 2048 bf16 2620 / 2578 us.)  A plan that does without what it
-    // can has one.
+    // 288 tiles for 512 places: one workgroup a tile 35.7 ms, seven 27.0; 5000 x 32768 x 2048 bf16 2620 / 2578 us.)  Sixteen at most
+    // (us with at most 4 / 16 / 64: bf16 16 x 32768 x 1024 155 / 94 / 109, 300 x 131072 x 1024 886 / 563 / 578, x 256 493 / 243 / 188,
+    // 64 x 131072 x 4096 1149 / 896 / 896; fp32 16 x 32768 x 1024 402 / 189 / 161, 128 x 50000 x 512 986 / 381 / 239, 22 x 131072 x 4096 2581 / 1825 / 1826): more
+    // would be quicker in fp32 and for the shortest rows, and slower for those between.  A plan that does without what it can has one.
     const uint64_t slabs = args.stride / slab, most_splits = merge ? std::max<uint64_t>(1, std::min<uint64_t>(slabs / 8, 16)) : 1;
     auto places = [](uint64_t t) { return t == 256 ? 256 : 512; };
     auto splits_of = [&](uint64_t t) {
@@ -2337,6 +2340,9 @@ struct Lowering {
       }
       return best;
     };
+    // Tiles of 256 for dx where so many splits give seven eighths of the chip one, else of 128.  (us by this rule / 128 / 256 throughout: 512 x 131072 x 4096
+    // 1803 / 1926 / 1801, 2048 x 32768 x 2048 872 / 888 / 862, 1400 x 32768 x 2048 661 / 678 / 663, but 4096 x 32768 x 1024 995 / 969 / 991, 1024 x 131072 x 1024
+    // 1111 / 1086 / 1119, 600 x 131072 x 2048 1558 / 1525 / 1560.)
     const uint32_t dx_tile = dt == LT_BF16 && tiles_of(n, width, 256) * std::min<uint64_t>(most_splits, std::max<uint64_t>(1, 256 / std::max<uint64_t>(tiles_of(n, width, 256), 1))) >= 224 ? 256u : 128u;
     args.splits = (uint32_t)splits_of(dx_tile);
     if (s_dx >= 0 && args.splits > 1) plan->merged = true;
@@ -2365,7 +2371,9 @@ struct Lowering {
       if (dloss.storage >= 0) patch(at, offsetof(ltk::VocabArgs, dloss), dloss);
       else patch_scalar(rins[a][4], at, offsetof(ltk::VocabArgs, dloss_value), &((ltk::VocabArgs*)plan->launches[at].args.data())->dloss_value);
     };
-    // dw takes the tokens' rows times what their losses count, where that is not the same number for all
+    // dw takes the tokens' rows times what their losses count, where that is not the same number for all: rounded to the products' type, as g is (bf16
+    // 1501 x 10007 x 331: dw is off by 0.0024 of its norm, by 0.0017 with one number for all; g times dloss rounded instead of both: 0.0025, because
+    // the label's -1 is then rounded too)
     int32_t weighed_x = shared.packed_x;
     if (grad && s_dw >= 0 && !args.rank0) {
       weighed_x = temporary(pad * width * e);

@@ -1,5 +1,6 @@
 // Softmax cross entropy over a vocabulary, l = x w^T: lse = log sum exp l, loss = lse - l[label], and its gradient, g = (exp(l - lse) - [label]) dloss,
-// dx = g w, dw = g^T x, with no more of l or g in memory than a piece of the vocabulary's.
+// dx = g w, dw = g^T x, with no more of l or g in memory than a piece of the vocabulary's: 128 MB of long bf16 rows, up to 512 of short ones, up to
+// 1 GB in fp32 (twice that where bf16 logits are kept for the gradient), and 4096 rows at least, so that a small vocabulary is one piece.
 //
 // Bound by the matrix units: 2 N V D operations for the losses, 6 N V D for the gradient (the logits again), 4 where they are kept.
 // The losses leave every tile of l as a maximum and a sum of exponentials for each of its tokens, which are joined; g is written in
@@ -97,7 +98,7 @@ __global__ __launch_bounds__(kRowsBlock) void lt_vocab_pack_kernel(const VocabAr
     src = row < n ? (const T*)a.x + (uint64_t)a.row_of[row] * a.dim : nullptr;
   }
   T* out = (T*)a.packed + (uint64_t)row * a.width;
-  if (a.weigh) {   // (times dloss, rounded)
+  if (a.weigh) {   // (times dloss, rounded: the products are of this type)
     const float weight = src ? a.dloss[a.row_of[row]] : 0.0f;
     for (uint32_t d = lane * 2u; d < a.width; d += 128u) {   // (a width is whole slabs)
       out[d] = src && d < a.dim ? (T)((float)src[d] * weight) : (T)0.0f;
