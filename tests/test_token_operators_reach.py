@@ -24,6 +24,13 @@ def test_launches_of_the_largest_sizes(tmp_path):
     assert run.returncode == 0 and "reach: ok" in run.stdout, (run.stdout + run.stderr)[-4000:]
 
 
+@pytest.fixture
+def room():
+    """gives back what the large tensors of a test took"""
+    yield
+    torch.cuda.empty_cache()
+
+
 def sampled(rg, tokens):
     """the first and last tokens, and some between"""
     return torch.tensor(np.unique(np.concatenate([np.arange(50), tokens - 1 - np.arange(50), rg.integers(0, tokens, 300)])), device="cuda")
@@ -31,15 +38,15 @@ def sampled(rg, tokens):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("each", [False, True])
-@pytest.mark.parametrize("dtype,tokens,vocab,dim,room", [("bf16", 2 ** 26 + 300, 200, 8, 110), ("f32", 2 ** 23, 2048, 128, 110)])
-def test_a_cross_entropy_of_so_many_tokens(dtype, tokens, vocab, dim, room, each):
+@pytest.mark.parametrize("dtype,tokens,vocab,dim,gigabytes", [("bf16", 2 ** 26 + 300, 200, 8, 110), ("f32", 2 ** 23, 2048, 128, 110)])
+def test_a_cross_entropy_of_so_many_tokens(room, dtype, tokens, vocab, dim, gigabytes, each):
     """2^26 tokens: a wave each for packing and for dx; 2^23 whose logits are kept: a wave for 256 of them.  The first, the last and some other tokens are compared by
     themselves, with the bounds of test_gpu_token_operators; dw as the sum over all of them: p and lse are off by less than 10^-3 of p (logits of below 100 in
     all their terms), g and x dloss by a rounding, and a sum in fp32 takes 32 products a step in bf16, in fp32 chains of 256 and their sum."""
     from test_gpu_token_operators import E24, HALF, Eager, context, entropy_bounds, grads_bound, within
     rg = np.random.default_rng(1)
     kind = {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
-    ctx, E = context(workspace_bytes=room << 30), Eager("f64")
+    ctx, E = context(workspace_bytes=gigabytes << 30), Eager("f64")
     x = torch.empty((tokens, dim), dtype=kind, device="cuda")
     some = torch.randn((1 << 20, dim), device="cuda").to(kind)
     for at in range(0, tokens, 1 << 20):
@@ -88,7 +95,7 @@ def _as_torch(ctx, t):
 
 
 @pytest.mark.gpu
-def test_a_gradient_of_rows_so_long():
+def test_a_gradient_of_rows_so_long(room):
     """4096 tokens of 2^23 + 1 columns, read element by element: 2^26 waves and more, for the sums and for joining them; in place and beside its base"""
     from test_gpu_token_operators import context
     tokens, rows, dim = 4096, 8, 2 ** 23 + 1
@@ -110,3 +117,30 @@ def test_a_gradient_of_rows_so_long():
     want[:, dim // 2] = (counts / 2).to(torch.bfloat16)
     assert torch.equal(_as_torch(ctx, beside), want) and torch.equal(base, want)
     ctx.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tokens", [131072, 131073, 262145, 700001])
+@pytest.mark.parametrize("kind", ["any", "one", "few", "padding"])
+def test_gradients_of_so_many_tokens_that_a_piece_is_more_than_a_wave_reads(tokens, kind):
+    """pieces of up to 256 sorted tokens, 64 at a time: whole numbers, whose sums are exact"""
+    from test_gpu_token_operators import context
+    torch.manual_seed(tokens)
+    for rows, dim, into in ((1000, 9, "f32"), (300001, 16, "bf16"), (70, 33, None)):
+        ids = {"any": torch.randint(-1, rows + 1, (tokens,), device="cuda"), "one": torch.full((tokens,), rows - 1, device="cuda"), "few": torch.randint(0, 3, (tokens,), device="cuda"),
+               "padding": torch.where(torch.rand(tokens, device="cuda") < 0.9, -1, torch.randint(0, rows, (tokens,), device="cuda"))}[kind].int()
+        dy = torch.randint(-2, 3, (tokens, dim), device="cuda").float()
+        there = (ids >= 0) & (ids < rows)
+        want = torch.zeros((rows, dim), dtype=torch.float64).index_add_(0, ids[there].long().cpu(), dy[there].double().cpu()).cuda()
+        ctx = context(workspace_bytes=512 << 20)
+        D, I = ctx.tensor(dy), ctx.tensor(ids)
+        if into is None:
+            got, want = ctx.embedding_grad(D, I, rows=rows), want.float()
+        else:
+            kind_of = torch.float32 if into == "f32" else torch.bfloat16
+            base = torch.randint(-3, 4, (rows, dim), device="cuda").to(kind_of)
+            want = (want + base.double()).float().to(kind_of)
+            got = ctx.embedding_grad(D, I, into=ctx.tensor(base))
+        ctx.barrier()
+        assert torch.equal(_as_torch(ctx, got), want), (rows, dim, into)
+        ctx.close()
