@@ -70,8 +70,9 @@ struct Lowering {
   std::string err;
   lt_status status = LT_OK;
   const bool merge;   // regroup and merge launches (not for a spare plan, nor with one region per op)
+  const bool spare;   // a plan for little memory
 
-  Lowering(lt_ctx* c, const Cut& k, bool spare) : ctx(c), cut(k), N((int32_t)k.order.size()), merge(c->fusion && !spare) {}
+  Lowering(lt_ctx* c, const Cut& k, bool is_spare) : ctx(c), cut(k), N((int32_t)k.order.size()), merge(c->fusion && !is_spare), spare(is_spare) {}
 
   bool bad(lt_status s, const std::string& m) {
     if (status == LT_OK) {
@@ -2269,12 +2270,12 @@ struct Lowering {
     // kept in one of its pieces; more, up to 512 MB, where its rows of dw would be fewer tiles than a round (us in pieces of 128 / 512 MB: bf16
     // 8192 x 32768 x 256 964 / 777, x 512 1221 / 1093, 16384 x 50000 x 512 4857 / 3761, but 8192 x 32768 x 1024 1862 / 1866; fp32 8192 x
     // 32768 x 256 7731 / 3594, x 1024 16452 / 12525); and 4096 rows at least, whatever the tokens are.  A plan that does without what it can takes
-    // 128 MB throughout.
+    // 128 MB of g throughout.
     const uint64_t row_of_g = std::max<uint64_t>(pad, 256) * e, mb = (uint64_t)1 << 20, most = 512 * mb / row_of_g & ~(uint64_t)255;
     const uint64_t small = std::max<uint64_t>(4096, 128 * mb / row_of_g & ~(uint64_t)255), round = (((uint64_t)1 << (dt == LT_BF16 ? 24 : 23)) / width + 255) & ~(uint64_t)255;
     const bool kept_in_one = dt == LT_F32 && args.dim >= 128u && args.vocab * row_of_g <= 1024 * mb;   // (a product less: 1035 x 131072 x 4096 44.0 / 35.1 ms)
     const uint64_t fit = !merge ? small : std::max({small, dt == LT_BF16 ? std::min(round, most) : most, kept_in_one ? (uint64_t)args.vocab : 0});
-    // what a piece's maxima and sums of the losses, and its packed rows of w, may take besides: 256 MB, 128 in such a plan
+    // what a piece's maxima and sums of the losses, and its packed rows of w, may take besides: 256 MB, 128 in a spare plan
     auto piece_in = [&](uint64_t rows_of_g, uint64_t room) {
       uint64_t rows = args.vocab;
       if (grad) rows = std::min(rows, rows_of_g);
@@ -2282,7 +2283,7 @@ struct Lowering {
       if (pack_w) rows = std::min(rows, std::max<uint64_t>(4096, room / (width * e) & ~(uint64_t)255));
       return rows;
     };
-    const uint64_t least_piece = piece_in(small, 128 * mb), piece = merge ? piece_in(fit, 256 * mb) : least_piece;
+    const uint64_t least_piece = piece_in(small, 128 * mb), piece = spare ? least_piece : piece_in(fit, 256 * mb);
     if (piece > least_piece) plan->merged = true;
     const uint32_t pieces = (uint32_t)((args.vocab + piece - 1) / piece);
     args.stride = (uint32_t)((piece + 255) & ~(uint64_t)255);
@@ -2326,8 +2327,8 @@ struct Lowering {
     // 288 tiles for 512 places: one workgroup a tile 35.7 ms, seven 27.0; 5000 x 32768 x 2048 bf16 2620 / 2578 us.)  Sixteen at most
     // (us with at most 4 / 16 / 64: bf16 16 x 32768 x 1024 155 / 94 / 109, 300 x 131072 x 1024 886 / 563 / 578, x 256 493 / 243 / 188,
     // 64 x 131072 x 4096 1149 / 896 / 896; fp32 16 x 32768 x 1024 402 / 189 / 161, 128 x 50000 x 512 986 / 381 / 239, 22 x 131072 x 4096 2581 / 1825 / 1826): more
-    // would be quicker in fp32 and for the shortest rows, and slower for those between.  A plan that does without what it can has one.
-    const uint64_t slabs = args.stride / slab, most_splits = merge ? std::max<uint64_t>(1, std::min<uint64_t>(slabs / 8, 16)) : 1;
+    // would be quicker in fp32 and for the shortest rows, and slower for those between.  A spare plan has one.
+    const uint64_t slabs = args.stride / slab, most_splits = spare ? 1 : std::max<uint64_t>(1, std::min<uint64_t>(slabs / 8, 16));
     auto places = [](uint64_t t) { return t == 256 ? 256 : 512; };
     auto splits_of = [&](uint64_t t) {
       const uint64_t tiles = std::max<uint64_t>(tiles_of(n, width, t), 1);

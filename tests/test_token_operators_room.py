@@ -28,19 +28,21 @@ def results(c, case, x, w, labels, lse=None):
     return c.linear_xent_grad(x, w, labels, lse, 0.5)[:1]
 
 
+@pytest.mark.parametrize("fusion", [True, False])
 @pytest.mark.parametrize("case", [SPLIT, PACKED, MAXIMA, BOTH])
-def test_what_a_plan_takes_for_speed_it_does_without(case):
+def test_what_a_plan_takes_for_speed_it_does_without(case, fusion):
     tokens, rows, dim, dtype, _, room = case
     sizes = []
     for n in (2048, room):
         c = Context(workspace_bytes=library_bytes() + n * MB)
+        c.set_fusion(fusion)
         x, w = c.from_device(0, dtype, (tokens, dim)), c.from_device(0, dtype, (rows, dim))
         out = results(c, case, x, w, zeros(c, (tokens,), "s32"), zeros(c, (tokens,)))
         c.barrier()
         sizes.append((c.stats().arena_bytes_in_use, c.dump_schedule()))
         del out
         c.close()
-    assert sizes[0][1] != sizes[1][1]
+    assert sizes[0][1] != sizes[1][1] or (not fusion and case is SPLIT)    # (whose splits are all that differs: one launch either way)
 
 
 @pytest.mark.gpu
